@@ -284,6 +284,63 @@ rad_status rad_backward_dX(rad_ctx* ctx, const rad_layer* layer, const rad_store
 rad_status rad_softmax_ce(rad_ctx* ctx, const void* logits, const int32_t* labels, int64_t rows,
                           int64_t classes, int32_t dtype, void* dlogits, float* loss_dev);
 
+/* ---- losses over a vocabulary ---------------------------------------------
+ * The last layer of a model with many classes, where the logits z = x W + bias
+ * [batch, d_out] are the largest tensor of the step.
+ *
+ * A teacher's most likely classes: row r's list is the entries index[r][j],
+ * logit[r][j] with index in [0, classes) and logit above -infinity; others are
+ * left out, so a list may be shorter than k (fill with index -1) or empty.  The
+ * target is the softmax of logit / temperature over the list; an index that
+ * comes twice has the sum of its probabilities. */
+typedef struct {
+  int32_t k;            /* entries per row, 1 to 1024 */
+  double temperature;   /* T, 1e-6 to 1e6 */
+  const int32_t* index; /* DEVICE [rows, k] */
+  const float* logit;   /* DEVICE [rows, k] */
+} rad_teacher;
+
+/* Distillation: with q = softmax(logits[r] / T) and targets p of row r,
+ *   row_loss[r] = T^2 sum_j p_j log(p_j / q_j),
+ *   loss = sum_r w_r row_loss[r],   dlogits[r] = w_r T (q - p),
+ * w_r = row_weight[r] (DEVICE [rows]), or, where that is null, 1 / the number
+ * of rows whose list is not empty.  A row with an empty list has no loss and a
+ * gradient of zeros, whatever its weight.  logits and dlogits [rows, classes]
+ * in dtype; dlogits may be logits.  row_loss [rows] and loss [1]: fp32 on the
+ * device.  Any of dlogits, row_loss, loss may be null, not all.  Statistics and
+ * sums are fp32, in a fixed order.  A logit of -infinity has probability zero;
+ * a row of nothing else gives NaN.  Enqueued on the context's stream. */
+rad_status rad_distill_ce(rad_ctx* ctx, const void* logits, const rad_teacher* teacher, const float* row_weight,
+                          int64_t rows, int64_t classes, int32_t dtype, void* dlogits, float* row_loss, float* loss);
+
+/* Softmax cross-entropy of a linear layer (RAD_LINEAR, no ReLU) and all its
+ * gradients in one call, which keeps neither the logits nor anything else for
+ * a backward pass: x is at hand when dW is formed, so there is nothing to store.
+ *   row_loss[r] = log sum_v exp(z[r][v]) - z[r][labels[r]],
+ *   loss = sum_r w_r row_loss[r],  dz[r] = w_r (softmax(z[r]) - onehot(labels[r])),
+ *   dX = dz W^T,  dW = beta dW + x^T dz,  dbias = beta dbias + sum_r dz[r].
+ * labels: int32 DEVICE [batch]; a row whose label lies outside [0, d_out) has no
+ * loss and adds to no gradient (its dX is zero).  w_r = row_weight[r] (DEVICE
+ * [batch], may be null: 1 / the number of the other rows).  dX is in the
+ * layer's dtype; dw_dtype is RAD_F32 or the layer's dtype (dz, which dW and dX
+ * are formed from, is rounded to that type; sums are fp32).  bias, dbias,
+ * row_loss [batch] and loss [1] are fp32.  beta is 0 or 1.  Outputs may be null,
+ * not all: without dX, dW and dbias the call scores, as for the
+ * log-probabilities of tokens that a model has answered.  Logits exist for a
+ * piece of the rows at a time, in a context workspace of at most 1 GiB (or 256
+ * rows, if they are more); a bf16 dW takes one of d_in d_out fp32 sums.
+ * d_in * d_out < 2^32.  Enqueued on the context's stream; results do not vary
+ * from call to call. */
+rad_status rad_linear_ce(rad_ctx* ctx, const rad_layer* layer, const void* x, const void* W, const float* bias,
+                         const int32_t* labels, const float* row_weight, float* row_loss, float* loss, void* dX,
+                         void* dW, int32_t dw_dtype, float* dbias, float beta);
+
+/* The same with a teacher's lists in the place of labels: the loss and dz of
+ * rad_distill_ce on the logits of the layer. */
+rad_status rad_linear_distill(rad_ctx* ctx, const rad_layer* layer, const void* x, const void* W, const float* bias,
+                              const rad_teacher* teacher, const float* row_weight, float* row_loss, float* loss,
+                              void* dX, void* dW, int32_t dw_dtype, float* dbias, float beta);
+
 /* ---- whole training steps ------------------------------------------------
  * A model owns its stores and transient activation buffers; parameters and
  * gradients stay with the caller.  `params` / `grads` are HOST arrays of

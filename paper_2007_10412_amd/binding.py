@@ -54,6 +54,11 @@ class rad_graph(C.Structure):
                 ("succ_ptr", P), ("succ", P), ("partial", P)]
 
 
+class rad_teacher(C.Structure):
+    _fields_ = [("k", C.c_int32), ("temperature", C.c_double), ("index", P), ("logit", P)]
+
+
+_HEAD = [P, P, P, P, P, C.c_int32, P, C.c_float]     # row_weight, row_loss, loss, dX, dW, dw_dtype, dbias, beta
 SIGNATURES = {
     "rad_fixed_k": (C.c_int64, [C.c_double, C.c_int64]),
     "rad_ctx_create": (C.c_int, [C.POINTER(P), P]),
@@ -81,6 +86,9 @@ SIGNATURES = {
     "rad_backward_dW": (C.c_int, [P, C.POINTER(rad_layer), P, P, P, P, C.c_float]),
     "rad_backward_dX": (C.c_int, [P, C.POINTER(rad_layer), P, P, P, P]),
     "rad_softmax_ce": (C.c_int, [P, P, P, C.c_int64, C.c_int64, C.c_int32, P, P]),
+    "rad_distill_ce": (C.c_int, [P, P, C.POINTER(rad_teacher), P, C.c_int64, C.c_int64, C.c_int32, P, P, P]),
+    "rad_linear_ce": (C.c_int, [P, C.POINTER(rad_layer), P, P, P, P] + _HEAD),
+    "rad_linear_distill": (C.c_int, [P, C.POINTER(rad_layer), P, P, P, C.POINTER(rad_teacher)] + _HEAD),
     "rad_model_create_mlp": (C.c_int, [P, C.c_int32, C.c_int64, C.c_int32, C.POINTER(C.c_int64), C.c_int32,
                                        C.c_int32, C.c_double, C.POINTER(P)]),
     "rad_model_create_rnn": (C.c_int, [P, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32,
@@ -287,6 +295,50 @@ def rad_softmax_ce(ctx, logits, labels, dtype, dlogits, loss_dev):
     rows, classes = logits.shape
     _check(ctx, lib().rad_softmax_ce(ctx, _ptr(logits), _ptr(labels), rows, classes, dtype, _ptr(dlogits),
                                      _ptr(loss_dev)))
+
+
+def make_teacher(index, logit, temperature=1.0):
+    """index (int32) and logit (fp32) [rows, k]: device tensors, which the caller keeps until the calls that take the
+    teacher have been made."""
+    import torch
+    if index.dtype != torch.int32 or logit.dtype != torch.float32 or index.dim() != 2 or index.shape != logit.shape:
+        raise RadError(RAD_ERR_SHAPE, "a teacher's lists are int32 and fp32 tensors [rows, k]")
+    _contiguous(index=index, logit=logit)
+    return rad_teacher(int(index.shape[1]), float(temperature), index.data_ptr(), logit.data_ptr())
+
+
+def _contiguous(**tensors):
+    for name, t in tensors.items():
+        if t is not None and not t.is_contiguous():
+            raise RadError(RAD_ERR_SHAPE, name + " is not contiguous")
+
+
+def rad_distill_ce(ctx, logits, teacher, dtype, dlogits=None, row_weight=None, row_loss=None, loss=None):
+    rows, classes = logits.shape
+    _contiguous(logits=logits, dlogits=dlogits, row_weight=row_weight, row_loss=row_loss)
+    _check(ctx, lib().rad_distill_ce(ctx, _ptr(logits), C.byref(teacher), _ptr(row_weight), rows, classes, dtype,
+                                     _ptr(dlogits), _ptr(row_loss), _ptr(loss)))
+
+
+def _head_args(row_weight, row_loss, loss, dX, dW, dbias, beta):
+    import torch
+    kind = RAD_BF16 if dW is not None and dW.dtype == torch.bfloat16 else RAD_F32
+    return _ptr(row_weight), _ptr(row_loss), _ptr(loss), _ptr(dX), _ptr(dW), kind, _ptr(dbias), beta
+
+
+def rad_linear_ce(ctx, layer, x, W, bias, labels, row_weight=None, row_loss=None, loss=None, dX=None, dW=None, dbias=None,
+                  beta=0.0):
+    """dW: an fp32 tensor, or one of the layer's type."""
+    _contiguous(x=x, W=W, bias=bias, labels=labels, row_weight=row_weight, row_loss=row_loss, dX=dX, dW=dW, dbias=dbias)
+    _check(ctx, lib().rad_linear_ce(ctx, C.byref(layer), _ptr(x), _ptr(W), _ptr(bias), _ptr(labels),
+                                    *_head_args(row_weight, row_loss, loss, dX, dW, dbias, beta)))
+
+
+def rad_linear_distill(ctx, layer, x, W, bias, teacher, row_weight=None, row_loss=None, loss=None, dX=None, dW=None,
+                       dbias=None, beta=0.0):
+    _contiguous(x=x, W=W, bias=bias, row_weight=row_weight, row_loss=row_loss, dX=dX, dW=dW, dbias=dbias)
+    _check(ctx, lib().rad_linear_distill(ctx, C.byref(layer), _ptr(x), _ptr(W), _ptr(bias), C.byref(teacher),
+                                         *_head_args(row_weight, row_loss, loss, dX, dW, dbias, beta)))
 
 
 def rad_model_create_mlp(ctx, dtype, batch, dims, has_bias, scheme, p):

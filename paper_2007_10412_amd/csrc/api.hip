@@ -44,13 +44,13 @@ struct rad_ctx {
   std::vector<hipEvent_t> pool;
   // grow-only workspaces, a set for each of the two streams: what is enqueued on one never shares a buffer with what
   // runs beside it on the other
-  void* ws[2][12] = {};
-  size_t ws_bytes[2][12] = {};
+  void* ws[2][16] = {};
+  size_t ws_bytes[2][16] = {};
   float* loss_dev = nullptr;
 };
 
 enum { WS_BITMAP = 0, WS_DENSE = 1, WS_ROWLOSS = 2, WS_COLSUM = 3, WS_SPLITK = 4, WS_WT = 5, WS_PROJ_R = 6, WS_PROJ_T = 7,
-       WS_PROJ_TB = 8, WS_REINDEX = 9, WS_CONVG = 10, WS_RNNSYNC = 11 };
+       WS_PROJ_TB = 8, WS_REINDEX = 9, WS_CONVG = 10, WS_RNNSYNC = 11, WS_TARGETS = 12, WS_LOGITS = 13, WS_LOGITGRAD = 14, WS_HEADDW = 15 };
 
 static const char* kNoCtx = "no context";
 
@@ -1414,6 +1414,209 @@ extern "C" rad_status rad_softmax_ce(rad_ctx* c, const void* logits, const int32
   if (rows < 1 || classes < 1 || rows > (1 << 24) || classes > (1 << 24)) return fail(c, RAD_ERR_SHAPE, "bad shape");
   if (dtype != RAD_F32 && dtype != RAD_BF16) return fail(c, RAD_ERR_PARAM, "unknown dtype");
   return softmax_call(c, logits, labels, (int)rows, (int)classes, dtype, dlogits, loss_dev);
+}
+
+// ------------------------------------------------------------------ losses over a vocabulary
+// the context's device is the current one while a call runs
+struct DeviceGuard {
+  int before = -1;
+  explicit DeviceGuard(int device) {
+    int now = device;
+    if (hipGetDevice(&now) == hipSuccess && now != device && hipSetDevice(device) == hipSuccess) before = now;
+  }
+  ~DeviceGuard() { if (before >= 0) (void)hipSetDevice(before); }
+};
+
+static rad_status check_teacher(rad_ctx* c, const rad_teacher* t) {
+  if (!t || !t->index || !t->logit) return fail(c, RAD_ERR_NULL, "null teacher");
+  if (t->k < 1 || t->k > kTeacherMax) return fail(c, RAD_ERR_SHAPE, "a teacher's lists hold 1 to 1024 entries");
+  if (!(t->temperature > 0.0) || !(t->temperature <= 1e6) || !(t->temperature >= 1e-6))
+    return fail(c, RAD_ERR_PARAM, "temperature must be in [1e-6, 1e6]");
+  return RAD_OK;
+}
+
+// What the rows are to learn, made ready for the kernels, and room for their losses where the caller wants none.
+static rad_status vocab_targets(rad_ctx* c, const int32_t* labels, const rad_teacher* teacher, const float* weight,
+                                int rows, int classes, VocabTargets* t, float** row_loss) {
+  const size_t lists = teacher ? (size_t)rows * teacher->k : 0;
+  char* ws = nullptr;
+  RAD_TRY(ws_get(c, WS_TARGETS, 256 + (size_t)rows * 12 + lists * 8, reinterpret_cast<void**>(&ws)));
+  float* const inv_count = reinterpret_cast<float*>(ws);
+  float* const losses = reinterpret_cast<float*>(ws + 256);
+  float* const entropy = losses + rows;
+  int32_t* const counts = reinterpret_cast<int32_t*>(entropy + rows);
+  int32_t* const index = counts + rows;
+  float* const prob = reinterpret_cast<float*>(index + lists);
+  *t = VocabTargets{labels, nullptr, nullptr, nullptr, nullptr, 1, 1.f, weight, inv_count};
+  if (!*row_loss) *row_loss = losses;
+  if (teacher) {
+    t->index = index; t->prob = prob; t->entropy = entropy; t->counts = counts;
+    t->k = teacher->k; t->temperature = (float)teacher->temperature;
+    HIP_TRY(c, timed(c, "teacher", [&](const char**) {
+      return launch_teacher(teacher->index, teacher->logit, rows, teacher->k, classes, t->temperature, index, prob, entropy, counts, c->stream);
+    }));
+  }
+  if (!weight)
+    HIP_TRY(c, timed(c, "count_rows", [&](const char**) { return launch_count_rows(*t, rows, classes, inv_count, c->stream); }));
+  return RAD_OK;
+}
+
+static rad_status vocab_rows(rad_ctx* c, VocabRows a) {
+  void* stats = nullptr;
+  RAD_TRY(ws_get(c, WS_ROWLOSS, (size_t)vocab_rows_stats_floats(a.rows, a.classes) * 4, &stats));
+  a.stats = static_cast<float*>(stats);
+  HIP_TRY(c, timed(c, "vocab_rows", [&](const char**) { return launch_vocab_rows(a, c->stream); }));
+  return RAD_OK;
+}
+
+static rad_status vocab_loss_sum(rad_ctx* c, const VocabTargets& t, const float* row_loss, int rows, int classes, float* loss) {
+  if (!loss) return RAD_OK;
+  HIP_TRY(c, timed(c, "weighted_loss", [&](const char**) { return launch_weighted_loss(t, row_loss, rows, classes, loss, c->stream); }));
+  return RAD_OK;
+}
+
+extern "C" rad_status rad_distill_ce(rad_ctx* c, const void* logits, const rad_teacher* teacher, const float* row_weight,
+                                     int64_t rows, int64_t classes, int32_t dtype, void* dlogits, float* row_loss, float* loss) {
+  if (!c) return RAD_ERR_NULL;
+  if (!logits) return fail(c, RAD_ERR_NULL, "null argument");
+  RAD_TRY(check_teacher(c, teacher));
+  if (!dlogits && !row_loss && !loss) return fail(c, RAD_ERR_NULL, "no output asked for");
+  if (rows < 1 || classes < 1 || rows > (1 << 24) || classes > (1 << 24)) return fail(c, RAD_ERR_SHAPE, "bad shape");
+  if (dtype != RAD_F32 && dtype != RAD_BF16) return fail(c, RAD_ERR_PARAM, "unknown dtype");
+  DeviceGuard guard(c->device);
+  VocabRows a;
+  std::memset(&a, 0, sizeof(a));
+  float* losses = row_loss;
+  RAD_TRY(vocab_targets(c, nullptr, teacher, row_weight, (int)rows, (int)classes, &a.t, &losses));
+  a.z = logits; a.z_dtype = dtype; a.z_ld = classes; a.parts = 1;
+  a.rows = (int)rows; a.classes = (int)classes;
+  a.dz = dlogits; a.dz_dtype = dtype; a.dz_ld = classes;
+  a.row_loss = losses;
+  RAD_TRY(vocab_rows(c, a));
+  return vocab_loss_sum(c, a.t, losses, (int)rows, (int)classes, loss);
+}
+
+// Bytes of logits and of their gradient that exist at a time: rows go through the layer in pieces of this size.
+constexpr size_t kLogitPieceBytes = (size_t)1 << 30;
+
+struct HeadCall {
+  const void* x; const void* W; const float* bias;
+  float* row_loss; float* loss;
+  void* dX; void* dW; int dw_dtype; float* dbias; float beta;
+};
+
+// dW (+)= x^T g over the rows of one piece, fp32
+static rad_status head_dW(rad_ctx* c, int dtype, int rows, int d_in, int d_out, const void* x, const void* g, int64_t g_ld,
+                          float* dW, int beta) {
+  GemmArgs a = gemm_zero();
+  a.M = d_in; a.N = d_out; a.K = rows;
+  a.A = x; a.lda = d_in; a.B = g; a.ldb = g_ld;
+  a.C = dW; a.ldc = d_out; a.beta = beta; a.c_dtype = kF32;
+  if (dtype == kF32) return dw_dense_f32(c, a, 0.0);
+  SplitPlan sp;
+  RAD_TRY(split_k_for_few_tiles(c, &a, &sp));
+  RAD_TRY(run_gemm_call(c, dtype, kOpMN, kOpMN, kEpiStore, a));
+  return split_k_finish(c, a, sp);
+}
+
+// z = x W of one piece: fp32, `parts` arrays part_stride apart
+static rad_status head_logits(rad_ctx* c, int dtype, int rows, int d_in, int d_out, const void* x, const HeadCall& h, VocabRows* a) {
+  void* z = nullptr;
+  if (dtype == kF32) {
+    RAD_TRY(ws_get(c, WS_LOGITS, (size_t)rows * d_out * 4, &z));
+    RAD_TRY(forward_gemm(c, kF32, rows, d_out, d_in, x, d_in, h.W, h.bias, 0, z, nullptr, 0, nullptr, nullptr, 0, 0, nullptr));
+    a->z = z; a->z_ld = d_out; a->parts = 1;
+    return RAD_OK;
+  }
+  GemmArgs g = gemm_zero();
+  g.M = rows; g.N = d_out; g.K = d_in;
+  g.A = x; g.lda = d_in; g.B = h.W; g.ldb = d_out;
+  g.ldc = (d_out + 63) / 64 * 64; g.c_dtype = kF32;
+  g.split_stride = (int64_t)rows * g.ldc;
+  const int tiles = ((rows + 255) / 256) * ((d_out + 255) / 256);
+  int splits = std::min(256 / tiles, 8);
+  if (splits > 1 && d_in >= 512) {
+    g.k_split = std::max((d_in + splits - 1) / splits, 256);
+    g.k_split = (g.k_split + 63) / 64 * 64;
+    g.k_splits = (d_in + g.k_split - 1) / g.k_split;
+  }
+  a->parts = std::max(g.k_splits, 1);
+  RAD_TRY(ws_get(c, WS_LOGITS, (size_t)a->parts * g.split_stride * 4, &z));
+  g.C = z;
+  RAD_TRY(run_gemm_call(c, dtype, kOpK, kOpMN, kEpiStore, g));
+  a->z = z; a->z_ld = g.ldc; a->part_stride = g.split_stride; a->bias = h.bias;
+  return RAD_OK;
+}
+
+static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* labels, const rad_teacher* teacher,
+                            const float* row_weight, HeadCall h) {
+  RAD_TRY(check_layer(c, L));
+  if (L->kind != RAD_LINEAR || L->relu) return fail(c, RAD_ERR_PARAM, "the loss takes a linear layer without ReLU");
+  if (!h.x || !h.W) return fail(c, RAD_ERR_NULL, "null argument");
+  if (!L->has_bias != !h.bias) return fail(c, RAD_ERR_NULL, "bias must be given iff the layer has one");
+  if (!h.row_loss && !h.loss && !h.dX && !h.dW && !h.dbias) return fail(c, RAD_ERR_NULL, "no output asked for");
+  if (h.beta != 0.f && h.beta != 1.f) return fail(c, RAD_ERR_PARAM, "beta must be 0 or 1");
+  if (h.dW && h.dw_dtype != RAD_F32 && h.dw_dtype != L->dtype) return fail(c, RAD_ERR_PARAM, "dW is fp32 or of the layer's type");
+  if (L->d_in * L->d_out >= ((int64_t)1 << 32)) return fail(c, RAD_ERR_SHAPE, "weights of 2^32 elements or more");
+  DeviceGuard guard(c->device);
+  const int rows = (int)L->batch, d_in = (int)L->d_in, d_out = (int)L->d_out, dtype = L->dtype;
+  const size_t esz = dtype == kF32 ? 4 : 2;
+  VocabTargets t;
+  float* losses = h.row_loss;
+  RAD_TRY(vocab_targets(c, labels, teacher, row_weight, rows, d_out, &t, &losses));
+  const bool train = h.dX || h.dW || h.dbias;
+  const int64_t pitch = dtype == kF32 ? d_out : (d_out + 63) / 64 * 64;
+  int64_t piece = (int64_t)(kLogitPieceBytes / ((size_t)pitch * 4));
+  piece = std::max<int64_t>(piece / 256 * 256, 256);
+  const bool cast = h.dW && h.dw_dtype == kBF16;
+  float* dW32 = static_cast<float*>(h.dW);
+  if (cast) RAD_TRY(ws_get(c, WS_HEADDW, (size_t)d_in * d_out * 4, reinterpret_cast<void**>(&dW32)));
+  for (int64_t r0 = 0; r0 < rows; r0 += piece) {
+    const int n = (int)std::min<int64_t>(piece, rows - r0);
+    const char* const xp = static_cast<const char*>(h.x) + (size_t)r0 * d_in * esz;
+    VocabRows a;
+    std::memset(&a, 0, sizeof(a));
+    a.t = t;
+    if (t.labels) a.t.labels += r0;
+    else { a.t.index += r0 * t.k; a.t.prob += r0 * t.k; a.t.entropy += r0; a.t.counts += r0; }
+    if (t.weight) a.t.weight += r0;
+    a.rows = n; a.classes = d_out; a.z_dtype = kF32;
+    a.row_loss = losses + r0;
+    RAD_TRY(head_logits(c, dtype, n, d_in, d_out, xp, h, &a));
+    if (train) {
+      void* g = const_cast<void*>(a.z);
+      if (dtype != kF32) RAD_TRY(ws_get(c, WS_LOGITGRAD, (size_t)n * pitch * esz, &g));
+      a.dz = g; a.dz_dtype = dtype; a.dz_ld = pitch;
+    }
+    RAD_TRY(vocab_rows(c, a));
+    if (h.dX)
+      RAD_TRY(dX_gemm(c, dtype, n, d_in, d_out, a.dz, nullptr, 0, h.W, static_cast<char*>(h.dX) + (size_t)r0 * d_in * esz, nullptr, 0, (int)pitch));
+    const int beta = r0 > 0 || (h.beta != 0.f && !cast);
+    if (h.dW) RAD_TRY(head_dW(c, dtype, n, d_in, d_out, xp, a.dz, pitch, dW32, beta));
+    if (h.dbias)
+      RAD_TRY(colsum_call(c, a.dz, dtype, n, d_out, nullptr, 0, nullptr, 0, 0, h.dbias, nullptr, r0 > 0 || h.beta != 0.f, 0, 0, pitch));
+  }
+  if (cast)
+    HIP_TRY(c, timed(c, "cast_add", [&](const char**) {
+      return launch_cast_add(dW32, static_cast<uint16_t*>(h.dW), (int64_t)d_in * d_out, h.beta != 0.f, c->stream);
+    }));
+  return vocab_loss_sum(c, t, losses, rows, d_out, h.loss);
+}
+
+extern "C" rad_status rad_linear_ce(rad_ctx* c, const rad_layer* L, const void* x, const void* W, const float* bias,
+                                    const int32_t* labels, const float* row_weight, float* row_loss, float* loss, void* dX,
+                                    void* dW, int32_t dw_dtype, float* dbias, float beta) {
+  if (!c) return RAD_ERR_NULL;
+  if (!labels) return fail(c, RAD_ERR_NULL, "null argument");
+  return head_loss(c, L, labels, nullptr, row_weight, HeadCall{x, W, bias, row_loss, loss, dX, dW, dw_dtype, dbias, beta});
+}
+
+extern "C" rad_status rad_linear_distill(rad_ctx* c, const rad_layer* L, const void* x, const void* W, const float* bias,
+                                         const rad_teacher* teacher, const float* row_weight, float* row_loss, float* loss,
+                                         void* dX, void* dW, int32_t dw_dtype, float* dbias, float beta) {
+  if (!c) return RAD_ERR_NULL;
+  RAD_TRY(check_teacher(c, teacher));
+  return head_loss(c, L, nullptr, teacher, row_weight, HeadCall{x, W, bias, row_loss, loss, dX, dW, dw_dtype, dbias, beta});
 }
 
 // ------------------------------------------------------------------ parameter updates

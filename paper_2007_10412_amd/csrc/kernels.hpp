@@ -247,6 +247,43 @@ int conv_dw_direct_splits(int batch, int ci, int co, int H, int W, int ks);
 hipError_t launch_conv_dw_direct(const float* xt, const float* g, float* part, int batch, int ci, int co, int H, int W,
                                  int ks, hipStream_t st);
 
+// ---- losses over a vocabulary (vocab_loss.hip).  What the rows are to learn, cross entropy being the list of one entry
+// of probability 1: labels [rows], or prepared lists index [rows][k] (ascending; a row's missing entries, -1, at the end)
+// with probabilities prob [rows][k] (entries of one index joined in the first of them, 0 in the others), entropy [rows]
+// (sum p log p) and counts [rows] (1 where a row has an entry, else 0).
+struct VocabTargets {
+  const int32_t* labels;
+  const int32_t* index; const float* prob; const float* entropy; const int32_t* counts;
+  int k;
+  float temperature;
+  const float* weight;          // the caller's row weights, or null: every row that counts weighs *inv_count
+  const float* inv_count;
+};
+constexpr int kTeacherMax = 1024;                     // longest list
+// lists sorted, joined and turned into probabilities (softmax of logit / temperature over the entries in [0, classes) whose
+// logit is not -inf)
+hipError_t launch_teacher(const int32_t* index, const float* logit, int rows, int k, int classes, float temperature,
+                          int32_t* index_out, float* prob, float* entropy, int32_t* counts, hipStream_t st);
+// *inv_count = 1 / rows that count (0 where none does)
+hipError_t launch_count_rows(const VocabTargets& t, int rows, int classes, float* inv_count, hipStream_t st);
+// loss = sum over rows of weight x row_loss, added in a fixed order
+hipError_t launch_weighted_loss(const VocabTargets& t, const float* row_loss, int rows, int classes, float* loss, hipStream_t st);
+// Losses and gradients of dense logits, rows z_ld apart: z, or (parts > 1) the sum of that many fp32 arrays part_stride
+// apart, plus bias (fp32 z only).  dz (nullable; rows dz_ld apart, zeros in columns classes .. dz_ld - 1) may be z itself.
+// stats: vocab_rows_stats_floats floats of scratch.
+struct VocabRows {
+  const void* z; int z_dtype; int64_t z_ld; int parts; int64_t part_stride; const float* bias;
+  int rows, classes;
+  VocabTargets t;
+  void* dz; int dz_dtype; int64_t dz_ld;
+  float* row_loss;              // [rows]
+  float* stats;
+};
+int64_t vocab_rows_stats_floats(int rows, int classes);
+hipError_t launch_vocab_rows(const VocabRows& a, hipStream_t st);
+// out (bf16) = beta out + in (fp32), n elements
+hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, hipStream_t st);
+
 // Ceiling probes (ceilings.hip): kind 0 HBM read, 1 HBM copy, 2 / 3 bf16 MFMA 32x32x16 / 16x16x32 register loops,
 // 4 fp32 MFMA 32x32x2, 5 integer 32 x 32 -> 64 multiply-adds.  a: operands (probe_min_bytes at least), b: sink
 // (copy: destination of `bytes`; else 1 KiB).

@@ -1,0 +1,442 @@
+// Losses over a vocabulary, and their gradients, from logits that are there: softmax cross entropy and distillation from
+// a teacher's most likely tokens.
+//
+// With q = softmax(z / T) and a list of targets (i_j, p_j), sum p_j = 1, a row's loss is T^2 sum_j p_j log(p_j / q_{i_j})
+// = T^2 (sum_j p_j log p_j + lse(z / T) - sum_j p_j z_{i_j} / T), and its gradient T (q_v - sum_{j: i_j = v} p_j): dense
+// in q, with k corrections.  A row is read once, 16 bytes a lane, and kept in registers between the statistics and the
+// gradient; the targets' logits are read beside it, and the corrections written over the row's vectors after them.
+#include <math.h>
+
+#include "kernels.hpp"
+
+namespace rad {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__device__ __forceinline__ float ld_elem(const float* p) { return *p; }
+__device__ __forceinline__ float ld_elem(const uint16_t* p) { return bf16_bits_to_f32(*p); }
+// (a NaN stays one: its mantissa's upper half would otherwise round into the infinity's pattern, or past it)
+__device__ __forceinline__ uint16_t to_bf16(float v) { return v != v ? (uint16_t)0x7FC0u : f32_to_bf16_bits(v); }
+__device__ __forceinline__ void st_elem(float* p, float v) { *p = v; }
+__device__ __forceinline__ void st_elem(uint16_t* p, float v) { *p = to_bf16(v); }
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+// sum over a workgroup of NT threads, the same for all of them; s_w: NT / 64 floats
+template <int NT> __device__ __forceinline__ float block_sum(float v, float* s_w) {
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float t = 0.f;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) t += s_w[w];
+  return t;
+}
+
+// exp((v - m) / T) with c = log2(e) / T; m is finite
+__device__ __forceinline__ float exp_from(float v, float m, float c) { return __builtin_amdgcn_exp2f((v - m) * c); }
+// what exponentials are taken from: the maximum, or 0 where nothing is left of a row (every exponential is 0 then)
+__device__ __forceinline__ float exp_base(float m) { return m == -INFINITY ? 0.f : m; }
+
+// a part's sum of exponentials (from exp_base of its maximum m) as one from b; a part with nothing in it adds its 0, or its NaN
+__device__ __forceinline__ float rebased(float s, float m, float b, float c) { return m == -INFINITY ? s : s * exp_from(m, b, c); }
+
+__device__ __forceinline__ bool row_counts(const VocabTargets& t, int row, int classes) {
+  return t.labels ? (uint32_t)t.labels[row] < (uint32_t)classes : t.counts[row] != 0;
+}
+__device__ __forceinline__ float row_weight(const VocabTargets& t, int row) { return t.weight ? t.weight[row] : *t.inv_count; }
+// entry j of a row that counts
+__device__ __forceinline__ int target_index(const VocabTargets& t, int row, int j) {
+  return t.labels ? t.labels[row] : t.index[(int64_t)row * t.k + j];
+}
+__device__ __forceinline__ float target_prob(const VocabTargets& t, int row, int j) {
+  return t.labels ? 1.f : t.prob[(int64_t)row * t.k + j];
+}
+
+// ------------------------------------------------------------------ targets
+// A wave per row.  Keys (index, place in the list) are sorted in LDS by a bitonic network over P >= k places, which puts
+// entries of one index side by side; the first of them takes their probabilities.  Missing entries sort to the end.
+template <int P>
+__global__ __launch_bounds__(256) void teacher_kernel(const int32_t* __restrict__ index, const float* __restrict__ logit, int rows,
+                                                      int k, int classes, float inv_t, int32_t* __restrict__ index_out,
+                                                      float* __restrict__ prob, float* __restrict__ entropy,
+                                                      int32_t* __restrict__ counts) {
+  __shared__ uint64_t s_key[4][P];
+  __shared__ float s_p[4][P];
+  constexpr uint64_t kNone = ~0ull;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int row = blockIdx.x * 4 + w;
+  const bool live = row < rows;                         // (all waves stay for the barriers)
+  uint64_t* const key = s_key[w];
+  float* const p = s_p[w];
+  const int64_t at = (int64_t)(live ? row : 0) * k;
+  float m = -INFINITY;
+  bool bad = false;
+  for (int j = lane; j < P; j += 64) {
+    uint64_t kj = kNone;
+    float t = -INFINITY;
+    if (live && j < k) {
+      const int32_t i = index[at + j];
+      const float l = logit[at + j] * inv_t;
+      if ((uint32_t)i < (uint32_t)classes && l != -INFINITY) { kj = ((uint64_t)(uint32_t)i << 32) | (uint32_t)j; t = l; }
+    }
+    key[j] = kj;
+    p[j] = t;
+    bad = bad || t != t;
+    m = fmaxf(m, t);
+  }
+  m = wave_max(m);
+  if (__any(bad)) m = NAN;
+  float s = 0.f, h = 0.f;
+  for (int j = lane; j < P; j += 64)
+    if (key[j] != kNone) s += expf(p[j] - m);
+  s = wave_sum(s);
+  const float log_s = logf(s), inv_s = 1.f / s;
+  for (int j = lane; j < P; j += 64) {
+    float pj = 0.f;
+    if (key[j] != kNone) {
+      const float d = p[j] - m;
+      pj = expf(d) * inv_s;
+      if (pj != 0.f) h += pj * (d - log_s);             // p log p -> 0
+    }
+    p[j] = pj;
+  }
+  h = wave_sum(h);
+  __syncthreads();
+  for (int size = 2; size <= P; size <<= 1)
+    for (int d = size >> 1; d > 0; d >>= 1) {
+      for (int q = lane; q < P / 2; q += 64) {
+        const int a = (q / d) * 2 * d + q % d, b = a + d;
+        const bool up = (a & size) == 0;
+        const uint64_t ka = key[a], kb = key[b];
+        if ((ka > kb) == up) { key[a] = kb; key[b] = ka; }
+      }
+      __syncthreads();
+    }
+  if (!live) return;
+  const bool some = key[0] != kNone;
+  for (int j = lane; j < k; j += 64) {
+    const uint64_t kj = key[j];
+    float sum = 0.f;
+    if (kj != kNone && (j == 0 || (key[j - 1] >> 32) != (kj >> 32)))
+      for (int q = j; q < k && (key[q] >> 32) == (kj >> 32) && key[q] != kNone; ++q) sum += p[(uint32_t)key[q]];
+    index_out[at + j] = kj == kNone ? -1 : (int32_t)(kj >> 32);
+    prob[at + j] = sum;
+  }
+  if (lane == 0) { entropy[row] = some ? h : 0.f; counts[row] = some ? 1 : 0; }
+}
+
+__global__ __launch_bounds__(1024) void count_rows_kernel(VocabTargets t, int rows, int classes, float* __restrict__ inv_count) {
+  __shared__ int s_n[16];
+  int n = 0;
+  for (int r = threadIdx.x; r < rows; r += 1024) n += row_counts(t, r, classes) ? 1 : 0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+  if ((threadIdx.x & 63) == 0) s_n[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  int all = 0;
+  for (int w = 0; w < 16; ++w) all += s_n[w];
+  *inv_count = all > 0 ? 1.f / (float)all : 0.f;
+}
+
+// thread i adds rows i, i + 1024, ...; then a fixed tree
+__global__ __launch_bounds__(1024) void weighted_loss_kernel(VocabTargets t, const float* __restrict__ row_loss, int rows,
+                                                             int classes, float* __restrict__ loss) {
+  __shared__ float s_w[16];
+  float acc = 0.f;
+  for (int r = threadIdx.x; r < rows; r += 1024)
+    if (row_counts(t, r, classes)) acc += row_weight(t, r) * row_loss[r];
+  acc = block_sum<1024>(acc, s_w);
+  if (threadIdx.x == 0) *loss = acc;
+}
+
+// ------------------------------------------------------------------ dense rows
+// A workgroup's part of a row: vectors v0 .. v0 + NT NV - 1 of 16 bytes, counted from the 16-byte boundary at or below the
+// row's first element (rows of odd widths start anywhere).  A vector that the row does not fill is taken element by element.
+template <typename T, int NT, int NV> struct RowPart {
+  static constexpr int VPL = 16 / (int)sizeof(T);
+  u32x4 raw[NV];
+  static __device__ __forceinline__ int lead(const T* row) { return (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)); }
+  static __device__ __forceinline__ int col(int v0, int i, int lead) { return (v0 + i * NT + (int)threadIdx.x) * VPL - lead; }
+  static constexpr uint32_t kEmpty = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;     // -inf
+  __device__ __forceinline__ void load(const T* row, int v0, int lead, int classes) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = col(v0, i, lead);
+      if (c >= 0 && c + VPL <= classes) {
+        raw[i] = *reinterpret_cast<const u32x4*>(row + c);
+      } else {
+        raw[i] = u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
+        T* e = reinterpret_cast<T*>(&raw[i]);
+#pragma unroll
+        for (int q = 0; q < VPL; ++q) if (c + q >= 0 && c + q < classes) e[q] = row[c + q];
+      }
+    }
+  }
+  __device__ __forceinline__ float at(int i, int q) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(raw[i][q]);
+    else return __uint_as_float(q & 1 ? raw[i][q >> 1] & 0xFFFF0000u : raw[i][q >> 1] << 16);
+  }
+  // more addends of fp32 logits
+  __device__ __forceinline__ void add(const float* row, int v0, int lead, int classes) {
+    static_assert(sizeof(T) == 4, "fp32 logits");
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = col(v0, i, lead);
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) if (c + q >= 0 && c + q < classes) raw[i][q] = __float_as_uint(__uint_as_float(raw[i][q]) + row[c + q]);
+    }
+  }
+  // maximum and sum of exponentials of the whole wave
+  __device__ __forceinline__ void stats(float c, float* m_out, float* s_out) const {
+    float m = -INFINITY, s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) m = fmaxf(m, at(i, q));
+    m = wave_max(m);
+    const float b = exp_base(m);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) s += exp_from(at(i, q), b, c);
+    *m_out = m;
+    *s_out = wave_sum(s);
+  }
+};
+
+// stores vector i of a part: out columns [0, classes) take f(value), columns [classes, dz_ld) zeros
+template <typename O, int VPL, class F>
+__device__ __forceinline__ void store_vec(O* out, int c, int classes, int64_t width, bool aligned, F f) {
+  if (c >= 0 && c + VPL <= classes && aligned) {
+    constexpr int W = VPL * (int)sizeof(O) / 4;         // 8 bytes (fp32 in, bf16 out) or 16
+    uint32_t w[W];
+#pragma unroll
+    for (int q = 0; q < W; ++q) {
+      if constexpr (sizeof(O) == 4) w[q] = __float_as_uint(f(q));
+      else w[q] = (uint32_t)to_bf16(f(2 * q)) | ((uint32_t)to_bf16(f(2 * q + 1)) << 16);
+    }
+    if constexpr (W == 4) *reinterpret_cast<u32x4*>(out + c) = u32x4{w[0], w[1], w[2], w[3]};
+    else *reinterpret_cast<u32x2*>(out + c) = u32x2{w[0], w[1]};
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < VPL; ++q) {
+    if (c + q < 0 || c + q >= width) continue;
+    st_elem(out + c + q, c + q < classes ? f(q) : 0.f);
+  }
+}
+
+// SPLIT: the row's parts are dealt to gridDim.x workgroups.  PASS 0 leaves each part's maximum and sum in stats
+// [rows][parts][2] and, with part 0, sum_j p_j z_{i_j} in dots [rows]; PASS 1 joins them, part by part in order, and writes.
+// Without SPLIT one workgroup has the whole row in its registers.
+template <typename T, typename O, int NT, int NV, bool SPLIT, int PASS>
+__global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __restrict__ dots) {
+  typedef RowPart<T, NT, NV> Part;
+  constexpr int VPL = Part::VPL, NW = NT / 64;
+  __shared__ float s_m[NW], s_s[NW], s_w[NW];
+  const int row = SPLIT ? blockIdx.y + blockIdx.z * 65535 : blockIdx.x;
+  if (row >= a.rows) return;
+  const int part = SPLIT ? blockIdx.x : 0, v0 = part * NT * NV;
+  const VocabTargets& t = a.t;
+  const T* const z = static_cast<const T*>(a.z) + (int64_t)row * a.z_ld;
+  O* const dz = static_cast<O*>(a.dz) + (int64_t)row * a.dz_ld;
+  const int lead = Part::lead(z);
+  const int classes = a.classes;
+  const float c = kLog2e / t.temperature;
+  const bool counts = row_counts(t, row, classes);
+  const bool out_aligned = (reinterpret_cast<uintptr_t>(dz - lead) & (VPL * sizeof(O) - 1)) == 0;
+
+  if (!counts) {                                        // (the same for the whole workgroup)
+    if (a.row_loss && part == 0 && threadIdx.x == 0 && !(SPLIT && PASS == 0)) a.row_loss[row] = 0.f;
+    if (a.dz && !(SPLIT && PASS == 0)) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) store_vec<O, VPL>(dz, Part::col(v0, i, lead), classes, a.dz_ld, out_aligned, [](int) { return 0.f; });
+    }
+    return;
+  }
+
+  auto logit = [&](int i) {                             // one logit, for a target
+    float v = ld_elem(z + i);
+    if constexpr (sizeof(T) == 4) {
+      for (int q = 1; q < a.parts; ++q) v += reinterpret_cast<const float*>(z)[q * a.part_stride + i];
+      if (a.bias) v += a.bias[i];
+    }
+    return v;
+  };
+  Part p;
+  p.load(z, v0, lead, classes);
+  if constexpr (sizeof(T) == 4) {
+    for (int q = 1; q < a.parts; ++q) p.add(reinterpret_cast<const float*>(z) + q * a.part_stride, v0, lead, classes);
+    if (a.bias) p.add(a.bias, v0, lead, classes);
+  }
+  // this thread's targets: all of them for the loss (one part of a row), those of this part for the gradient.  Their logits
+  // are read here, ahead of any store: dz may be z.
+  constexpr int KT = (kTeacherMax + NT - 1) / NT;
+  const int c_lo = v0 * VPL - lead, c_hi = c_lo + NT * NV * VPL;
+  float tz[KT], tp[KT]; int ti[KT];
+  float dot = 0.f;
+#pragma unroll
+  for (int q = 0; q < KT; ++q) {
+    const int j = (int)threadIdx.x + q * NT;
+    ti[q] = -1; tz[q] = tp[q] = 0.f;
+    if (j >= t.k) continue;
+    const int i = target_index(t, row, j);
+    const float pj = target_prob(t, row, j);
+    if (i < 0 || pj == 0.f) continue;
+    const bool mine = i >= c_lo && i < c_hi;
+    if (!mine && (PASS == 1 || part != 0)) continue;
+    const float v = logit(i);
+    dot += pj * v;
+    if (mine) { ti[q] = i; tz[q] = v; tp[q] = pj; }
+  }
+
+  float m = -INFINITY, s = 0.f;
+  if (!SPLIT || PASS == 0) {
+    float wm, ws;
+    p.stats(c, &wm, &ws);
+    if ((threadIdx.x & 63) == 0) { s_m[threadIdx.x >> 6] = wm; s_s[threadIdx.x >> 6] = ws; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, s_m[w]);
+    const float b = exp_base(m);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) s += rebased(s_s[w], s_m[w], b, c);
+    if (part == 0) dot = block_sum<NT>(dot, s_w);
+  }
+  if (SPLIT && PASS == 0) {
+    if (threadIdx.x == 0) {
+      float* const st = a.stats + ((int64_t)row * gridDim.x + part) * 2;
+      st[0] = m; st[1] = s;
+      if (part == 0) dots[row] = dot;
+    }
+    return;
+  }
+  if (SPLIT) {
+    const float* const st = a.stats + (int64_t)row * gridDim.x * 2;
+    for (int w = 0; w < (int)gridDim.x; ++w) m = fmaxf(m, st[2 * w]);
+    const float b = exp_base(m);
+    for (int w = 0; w < (int)gridDim.x; ++w) s += rebased(st[2 * w + 1], st[2 * w], b, c);
+    if (part == 0) dot = dots[row];
+    __syncthreads();                                    // every target's logit has been read
+  }
+  const float b = exp_base(m);
+  if (a.row_loss && part == 0 && threadIdx.x == 0) {
+    const float T1 = t.temperature;
+    const float lse = b / T1 + logf(s);
+    a.row_loss[row] = T1 * T1 * ((t.labels ? 0.f : t.entropy[row]) + (lse - dot / T1));
+  }
+  if (!a.dz) return;
+  const float wt = row_weight(t, row) * t.temperature, f = wt / s;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    store_vec<O, VPL>(dz, Part::col(v0, i, lead), classes, a.dz_ld, out_aligned, [&](int q) { return exp_from(p.at(i, q), b, c) * f; });
+  __threadfence_block();
+  __syncthreads();                                      // the targets' elements are written again, after their vectors
+#pragma unroll
+  for (int q = 0; q < KT; ++q)
+    if (ti[q] >= 0) st_elem(dz + ti[q], exp_from(tz[q], b, c) * f - wt * tp[q]);
+}
+
+__global__ __launch_bounds__(256) void cast_add_kernel(const float* __restrict__ in, uint16_t* __restrict__ out, int64_t n, int beta) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i + 8 <= n && (reinterpret_cast<uintptr_t>(out) & 15) == 0) {
+    const floatx4 a = *reinterpret_cast<const floatx4*>(in + i), b = *reinterpret_cast<const floatx4*>(in + i + 4);
+    float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    u32x4 o = {0u, 0u, 0u, 0u};
+    if (beta) o = *reinterpret_cast<const u32x4*>(out + i);
+    u32x4 r;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (beta) { v[2 * q] += __uint_as_float(o[q] << 16); v[2 * q + 1] += __uint_as_float(o[q] & 0xFFFF0000u); }
+      r[q] = (uint32_t)to_bf16(v[2 * q]) | ((uint32_t)to_bf16(v[2 * q + 1]) << 16);
+    }
+    *reinterpret_cast<u32x4*>(out + i) = r;
+    return;
+  }
+  for (int64_t j = i; j < n && j < i + 8; ++j) out[j] = to_bf16(in[j] + (beta ? bf16_bits_to_f32(out[j]) : 0.f));
+}
+
+constexpr int kPartThreads = 256, kPartVecs = 4;
+
+template <typename T, typename O, int NT, int NV>
+hipError_t rows_whole(const VocabRows& a, hipStream_t st) {
+  hipLaunchKernelGGL((vocab_rows_kernel<T, O, NT, NV, false, 1>), dim3(a.rows), dim3(NT), 0, st, a, (float*)nullptr);
+  return hipGetLastError();
+}
+template <typename T, typename O>
+hipError_t rows_any(const VocabRows& a, hipStream_t st) {
+  constexpr int VPL = 16 / (int)sizeof(T);
+  // vectors of a row, the ones that it only begins or ends in and the padding of dz included
+  const int64_t cols = a.dz && a.dz_ld > a.classes ? a.dz_ld : a.classes;
+  const int64_t vecs = (cols + VPL - 1) / VPL + 1;
+  if (vecs <= 256 * 2) return rows_whole<T, O, 256, 2>(a, st);
+  if (a.rows >= 256 && vecs <= 512 * 4) return rows_whole<T, O, 512, 4>(a, st);
+  if (a.rows >= 256 && vecs <= 512 * 8) return rows_whole<T, O, 512, 8>(a, st);
+  if (a.rows >= 256 && vecs <= 1024 * 16) return rows_whole<T, O, 1024, 16>(a, st);
+  const int64_t parts = (vecs + kPartThreads * kPartVecs - 1) / (kPartThreads * kPartVecs);
+  float* const dots = a.stats + (int64_t)a.rows * parts * 2;
+  const dim3 grid((unsigned)parts, (unsigned)(a.rows < 65535 ? a.rows : 65535), (unsigned)((a.rows + 65534) / 65535));
+  hipLaunchKernelGGL((vocab_rows_kernel<T, O, kPartThreads, kPartVecs, true, 0>), grid, dim3(kPartThreads), 0, st, a, dots);
+  hipLaunchKernelGGL((vocab_rows_kernel<T, O, kPartThreads, kPartVecs, true, 1>), grid, dim3(kPartThreads), 0, st, a, dots);
+  return hipGetLastError();
+}
+
+template <int P>
+hipError_t teacher_of(const int32_t* index, const float* logit, int rows, int k, int classes, float temperature,
+                      int32_t* index_out, float* prob, float* entropy, int32_t* counts, hipStream_t st) {
+  hipLaunchKernelGGL(teacher_kernel<P>, dim3((rows + 3) / 4), dim3(256), 0, st, index, logit, rows, k, classes,
+                     1.f / temperature, index_out, prob, entropy, counts);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_teacher(const int32_t* index, const float* logit, int rows, int k, int classes, float temperature,
+                          int32_t* index_out, float* prob, float* entropy, int32_t* counts, hipStream_t st) {
+  if (k < 1 || k > kTeacherMax) return hipErrorInvalidValue;
+  if (k <= 64) return teacher_of<64>(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, st);
+  if (k <= 256) return teacher_of<256>(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, st);
+  return teacher_of<1024>(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, st);
+}
+
+hipError_t launch_count_rows(const VocabTargets& t, int rows, int classes, float* inv_count, hipStream_t st) {
+  hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, st, t, rows, classes, inv_count);
+  return hipGetLastError();
+}
+
+hipError_t launch_weighted_loss(const VocabTargets& t, const float* row_loss, int rows, int classes, float* loss, hipStream_t st) {
+  hipLaunchKernelGGL(weighted_loss_kernel, dim3(1), dim3(1024), 0, st, t, row_loss, rows, classes, loss);
+  return hipGetLastError();
+}
+
+int64_t vocab_rows_stats_floats(int rows, int classes) {
+  const int64_t parts = (classes / 4 + 2 + 64 + kPartThreads * kPartVecs) / (kPartThreads * kPartVecs) + 1;   // (fp32 vectors)
+  return (int64_t)rows * (parts * 2 + 1);
+}
+
+hipError_t launch_vocab_rows(const VocabRows& a, hipStream_t st) {
+  if (a.rows <= 0) return hipSuccess;
+  if (a.z_dtype == kBF16) {
+    if (a.parts > 1 || a.bias || a.dz_dtype != kBF16) return hipErrorInvalidValue;
+    return rows_any<uint16_t, uint16_t>(a, st);
+  }
+  return a.dz_dtype == kBF16 ? rows_any<float, uint16_t>(a, st) : rows_any<float, float>(a, st);
+}
+
+hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, hipStream_t st) {
+  hipLaunchKernelGGL(cast_add_kernel, dim3((unsigned)((n + 2047) / 2048)), dim3(256), 0, st, in, out, n, beta);
+  return hipGetLastError();
+}
+
+}  // namespace rad
