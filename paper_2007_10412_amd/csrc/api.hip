@@ -44,13 +44,13 @@ struct rad_ctx {
   std::vector<hipEvent_t> pool;
   // grow-only workspaces, a set for each of the two streams: what is enqueued on one never shares a buffer with what
   // runs beside it on the other
-  void* ws[2][16] = {};
-  size_t ws_bytes[2][16] = {};
+  void* ws[2][18] = {};
+  size_t ws_bytes[2][18] = {};
   float* loss_dev = nullptr;
 };
 
 enum { WS_BITMAP = 0, WS_DENSE = 1, WS_ROWLOSS = 2, WS_COLSUM = 3, WS_SPLITK = 4, WS_WT = 5, WS_PROJ_R = 6, WS_PROJ_T = 7,
-       WS_PROJ_TB = 8, WS_REINDEX = 9, WS_CONVG = 10, WS_RNNSYNC = 11, WS_TARGETS = 12, WS_LOGITS = 13, WS_LOGITGRAD = 14, WS_HEADDW = 15 };
+       WS_PROJ_TB = 8, WS_REINDEX = 9, WS_CONVG = 10, WS_RNNSYNC = 11, WS_TARGETS = 12, WS_LOGITS = 13, WS_LOGITGRAD = 14, WS_HEADDW = 15, WS_HEADW = 16, WS_HEADX = 17 };
 
 static const char* kNoCtx = "no context";
 
@@ -1497,7 +1497,7 @@ extern "C" rad_status rad_distill_ce(rad_ctx* c, const void* logits, const rad_t
 }
 
 // Bytes of logits and of their gradient that exist at a time: rows go through the layer in pieces of this size.
-constexpr size_t kLogitPieceBytes = (size_t)1 << 30;
+constexpr size_t kLogitPieceBytes = (size_t)2 << 30;
 
 struct HeadCall {
   const void* x; const void* W; const float* bias;
@@ -1548,6 +1548,161 @@ static rad_status head_logits(rad_ctx* c, int dtype, int rows, int d_in, int d_o
   return RAD_OK;
 }
 
+// Workgroups that share the K range of a 256 x 256 tile, so that they come close to filling the chip's 256 CUs a whole number
+// of times; a split has at least four slices and costs 3 % in partial sums.
+static int head_splits(int64_t tiles, int64_t K) {
+  int best = 1;
+  double best_rate = 0.0;
+  for (int s = 1; s <= 8 && (s == 1 || K / s >= 256); ++s) {
+    const int64_t waves = (tiles * s + 255) / 256;
+    const double rate = (double)(tiles * s) / (double)(waves * 256) * (s > 1 ? 0.97 - 0.01 * s : 1.0);
+    if (rate > best_rate) { best_rate = rate; best = s; }
+  }
+  return best;
+}
+
+// The bf16 layer with its loss in the epilogue of the logits' product (vocab_head.hip).
+static bool head_fused_pays(int dtype, int64_t rows, int64_t d_out) {
+  return dtype == kBF16 && ((rows + 255) / 256) * ((d_out + 255) / 256) >= 100;
+}
+static rad_status head_fused(rad_ctx* c, int rows, int d_in, int d_out, const VocabTargets& t, const HeadCall& h, float* losses) {
+  const int64_t dp = (d_in + 7) / 8 * 8, vp8 = (d_out + 7) / 8 * 8, vp = (d_out + 63) / 64 * 64;
+  const int parts = (d_out + 127) / 128;
+  const bool train = h.dX || h.dW || h.dbias;
+  int64_t piece = std::min<int64_t>((int64_t)(kLogitPieceBytes / ((size_t)vp * 2)), (((int64_t)1 << 32) - 1) / (dp * 2));
+  piece = std::max<int64_t>(std::min<int64_t>(piece / 256 * 256, 1 << 19), 256);
+  if (piece > rows) piece = rows;
+  // operands whose rows are not whole 16-byte vectors are copied once
+  const uint16_t* W = static_cast<const uint16_t*>(h.W);
+  if (d_out % 8 || (reinterpret_cast<uintptr_t>(W) & 15)) {
+    void* ws = nullptr;
+    RAD_TRY(ws_get(c, WS_HEADW, (size_t)d_in * vp8 * 2, &ws));
+    HIP_TRY(c, timed(c, "pad_rows", [&](const char**) { return launch_pad_rows(W, d_in, d_out, static_cast<uint16_t*>(ws), vp8, c->stream); }));
+    W = static_cast<uint16_t*>(ws);
+  }
+  const uint16_t* x = static_cast<const uint16_t*>(h.x);
+  if (d_in % 8 || (reinterpret_cast<uintptr_t>(x) & 15)) {
+    void* ws = nullptr;
+    RAD_TRY(ws_get(c, WS_HEADX, (size_t)rows * dp * 2, &ws));
+    HIP_TRY(c, timed(c, "pad_rows", [&](const char**) { return launch_pad_rows(x, rows, d_in, static_cast<uint16_t*>(ws), dp, c->stream); }));
+    x = static_cast<uint16_t*>(ws);
+  }
+  const int first_ld = parts + 1;
+  const size_t first_bytes = t.labels ? 0 : ((size_t)rows * first_ld * 2 + 255) / 256 * 256;
+  char* ws = nullptr;
+  RAD_TRY(ws_get(c, WS_ROWLOSS, 256 + first_bytes + (size_t)piece * (8 * (size_t)parts + 16 + 4 * (size_t)t.k), reinterpret_cast<void**>(&ws)));
+  int32_t* const live = reinterpret_cast<int32_t*>(ws);
+  uint16_t* const first = reinterpret_cast<uint16_t*>(ws + 256);
+  float* const stats = reinterpret_cast<float*>(ws + 256 + first_bytes);
+  int32_t* const list = reinterpret_cast<int32_t*>(stats + (size_t)piece * parts * 2);
+  float* const top = reinterpret_cast<float*>(list + piece);
+  float* const log2_sum = top + piece;
+  float* const factor = log2_sum + piece;
+  float* const target = factor + piece;
+  if (!t.labels)
+    HIP_TRY(c, timed(c, "list_parts", [&](const char**) { return launch_list_parts(t.index, rows, t.k, parts, first, first_ld, c->stream); }));
+
+  const bool one = piece >= rows;
+  const bool cast = h.dW && h.dw_dtype == kBF16 && (!one || h.beta != 0.f);     // sums of several pieces are kept in fp32
+  float* dW32 = h.dw_dtype == kBF16 ? nullptr : static_cast<float*>(h.dW);
+  if (cast) RAD_TRY(ws_get(c, WS_HEADDW, (size_t)d_in * d_out * 4, reinterpret_cast<void**>(&dW32)));
+  void *P = nullptr, *xs = nullptr;
+  if (train) RAD_TRY(ws_get(c, WS_LOGITS, (size_t)piece * vp * 2, &P));
+  if (h.dW) RAD_TRY(ws_get(c, WS_LOGITGRAD, (size_t)piece * dp * 2, &xs));
+
+  for (int64_t r0 = 0; r0 < rows; r0 += piece) {
+    const int n = (int)std::min<int64_t>(piece, rows - r0);
+    VocabTargets tp = t;
+    if (tp.labels) tp.labels += r0;
+    else { tp.index += r0 * t.k; tp.prob += r0 * t.k; tp.entropy += r0; tp.counts += r0; }
+    if (tp.weight) tp.weight += r0;
+    HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(tp, n, d_out, list, live, c->stream); }));
+    GemmArgs g = gemm_zero();
+    g.M = n; g.N = d_out; g.K = d_in;
+    g.A = x + r0 * dp; g.lda = dp; g.B = W; g.ldb = vp8;
+    g.bias = h.bias; g.y = P; g.ldy = vp;
+    HeadArgs& a = g.head;
+    a.live = live; a.row_map = list; a.n_load = (int)vp8;
+    a.c = 1.44269504088896340736f / t.temperature;
+    a.stats = stats; a.stats_ld = piece;
+    a.labels = tp.labels; a.index = tp.index; a.first = t.labels ? nullptr : first + r0 * first_ld; a.k = t.k; a.first_ld = first_ld;
+    a.target = target;
+    RAD_TRY(run_gemm_call(c, kBF16, kOpK, kOpMN, kEpiVocab, g));
+    VocabFinish f;
+    std::memset(&f, 0, sizeof(f));
+    f.list = list; f.live = live; f.rows = n; f.classes = d_out; f.parts = parts; f.t = tp;
+    f.stats = stats; f.stats_ld = piece; f.target = target;
+    f.row_loss = losses + r0; f.top = top; f.log2_sum = log2_sum; f.factor = factor;
+    f.z = static_cast<uint16_t*>(P); f.z_ld = vp; f.first = a.first; f.first_ld = first_ld;
+    f.x = x + r0 * dp; f.x_ld = dp; f.d_in = d_in; f.xs = static_cast<uint16_t*>(xs); f.xs_ld = dp;
+    f.dx = h.dX ? static_cast<uint16_t*>(h.dX) + r0 * d_in : nullptr;
+    HIP_TRY(c, timed(c, "vocab_finish", [&](const char**) { return launch_vocab_finish(f, c->stream); }));
+    if (train) HIP_TRY(c, timed(c, "vocab_gradient", [&](const char**) { return launch_vocab_gradient(f, c->stream); }));
+    if (h.dX) {
+      GemmArgs gx = gemm_zero();
+      gx.M = n; gx.N = d_in; gx.K = (int)vp8;
+      gx.A = P; gx.lda = vp; gx.B = W; gx.ldb = vp8;
+      gx.C = f.dx; gx.ldc = d_in; gx.c_dtype = kBF16;
+      gx.head.live = live; gx.head.row_map = list;
+      const int splits = n <= 65535 ? head_splits((int64_t)((n + 255) / 256) * ((d_in + 255) / 256), vp8) : 1;
+      SplitSum sum;
+      std::memset(&sum, 0, sizeof(sum));
+      if (splits > 1) {
+        gx.k_split = (int)((vp8 + splits - 1) / splits + 63) / 64 * 64;
+        gx.k_splits = (int)((vp8 + gx.k_split - 1) / gx.k_split);
+        gx.ldc = (d_in + 63) / 64 * 64;
+        gx.split_stride = (int64_t)n * gx.ldc;
+        RAD_TRY(ws_get(c, WS_SPLITK, (size_t)gx.k_splits * gx.split_stride * 4, &gx.C));
+      }
+      RAD_TRY(run_gemm_call(c, kBF16, kOpK, kOpK, kEpiHeadX, gx));
+      if (splits > 1) {
+        sum.in = static_cast<const float*>(gx.C); sum.splits = gx.k_splits; sum.stride = gx.split_stride; sum.in_ld = gx.ldc;
+        sum.rows = n; sum.cols = d_in; sum.live = live; sum.map = list;
+        sum.out = f.dx; sum.out_dtype = kBF16; sum.out_ld = d_in;
+        HIP_TRY(c, timed(c, "split_sum", [&](const char**) { return launch_split_sum(sum, c->stream); }));
+      }
+    }
+    if (h.dW) {
+      GemmArgs gw = gemm_zero();
+      gw.M = d_in; gw.N = d_out; gw.K = n; gw.m_load = (int)dp;
+      gw.A = xs; gw.lda = dp; gw.B = P; gw.ldb = vp;
+      void* const out = dW32 ? dW32 : h.dW;
+      const int out_dtype = dW32 ? kF32 : kBF16, beta = dW32 && (r0 > 0 || (h.beta != 0.f && !cast));
+      gw.C = out; gw.ldc = d_out; gw.c_dtype = out_dtype; gw.beta = beta;
+      gw.head.live = live; gw.head.n_load = (int)vp8; gw.head.whole = f.x; gw.head.rows = n;
+      const int splits = d_in <= 65535 ? head_splits((int64_t)((d_in + 255) / 256) * ((d_out + 255) / 256), n) : 1;
+      if (splits > 1) {
+        gw.k_split = ((n + splits - 1) / splits + 63) / 64 * 64;
+        gw.k_splits = (n + gw.k_split - 1) / gw.k_split;
+        gw.ldc = vp;
+        gw.split_stride = (int64_t)d_in * vp;
+        RAD_TRY(ws_get(c, WS_SPLITK, (size_t)gw.k_splits * gw.split_stride * 4, &gw.C));
+      }
+      RAD_TRY(run_gemm_call(c, kBF16, kOpMN, kOpMN, kEpiHeadW, gw));
+      if (splits > 1) {
+        SplitSum sum;
+        std::memset(&sum, 0, sizeof(sum));
+        sum.in = static_cast<const float*>(gw.C); sum.splits = gw.k_splits; sum.stride = gw.split_stride; sum.in_ld = vp;
+        sum.rows = d_in; sum.cols = d_out;
+        sum.out = out; sum.out_dtype = out_dtype; sum.out_ld = d_out; sum.beta = beta;
+        HIP_TRY(c, timed(c, "split_sum", [&](const char**) { return launch_split_sum(sum, c->stream); }));
+      }
+    }
+    if (h.dbias) {
+      void* part = nullptr;
+      RAD_TRY(ws_get(c, WS_COLSUM, (size_t)kHeadColsumSplits * d_out * 4, &part));
+      HIP_TRY(c, timed(c, "head_colsum", [&](const char**) {
+        return launch_head_colsum(f.z, vp, live, d_out, static_cast<float*>(part), h.dbias, r0 > 0 || h.beta != 0.f, c->stream);
+      }));
+    }
+  }
+  if (cast)
+    HIP_TRY(c, timed(c, "cast_add", [&](const char**) {
+      return launch_cast_add(dW32, static_cast<uint16_t*>(h.dW), (int64_t)d_in * d_out, h.beta != 0.f, c->stream);
+    }));
+  return RAD_OK;
+}
+
 static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* labels, const rad_teacher* teacher,
                             const float* row_weight, HeadCall h) {
   RAD_TRY(check_layer(c, L));
@@ -1564,6 +1719,10 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   VocabTargets t;
   float* losses = h.row_loss;
   RAD_TRY(vocab_targets(c, labels, teacher, row_weight, rows, d_out, &t, &losses));
+  if (head_fused_pays(dtype, rows, d_out)) {
+    RAD_TRY(head_fused(c, rows, d_in, d_out, t, h, losses));
+    return vocab_loss_sum(c, t, losses, rows, d_out, h.loss);
+  }
   const bool train = h.dX || h.dW || h.dbias;
   const int64_t pitch = dtype == kF32 ? d_out : (d_out + 63) / 64 * 64;
   int64_t piece = (int64_t)(kLogitPieceBytes / ((size_t)pitch * 4));

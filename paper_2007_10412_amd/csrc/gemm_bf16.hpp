@@ -463,15 +463,17 @@ static_assert(MfmaOrder<4, 1>::at(3) == 3 && MfmaOrder<4, 1>::frag(4) == 6 && Mf
 static_assert(MfmaOrder<4, 2>::at(1) == 1 && MfmaOrder<4, 2>::at(2) == 2 && MfmaOrder<4, 2>::at(7) == 7, "");
 
 // The MFMAs of one half iteration are issued in eight pieces, each followed by its share of the other work;
-// piece P takes the MFMAs m with m*8/(TM*TN) == P of that order.
-template <int P, int TM, int TN>
+// piece P takes the MFMAs m with m*8/(TM*TN) == P of that order.  SWAP: the transposed product, whose lanes hold a row of
+// the tile each (columns acc_row(e, lane) of a 32 x 32 block), where otherwise they hold a column.
+template <int P, int TM, int TN, bool SWAP = false>
 __device__ __forceinline__ void mfma_piece(const bf16x8 (&a)[TM], const bf16x8 (&b)[TN], floatx16 (&acc)[TM][TN]) {
   constexpr int CNT = TM * TN, LO = P * CNT / 8, HI = (P + 1) * CNT / 8;
   typedef MfmaOrder<TM, TN> O;
 #pragma unroll
   for (int m = LO; m < HI; ++m) {
     const int i = O::at(m) / TN, j = O::at(m) % TN;
-    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+    if constexpr (SWAP) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
+    else acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
   }
 }
 // the Q-th fragment read of a k-step: ra(i) or rb(j)

@@ -12,6 +12,7 @@
 // them are written out.
 #pragma once
 #include "gemm_bf16.hpp"
+#include "head_epilogue.hpp"
 
 namespace rad {
 
@@ -55,15 +56,26 @@ template <int R> struct DmaOperandK64 {
   uint32_t voff[NI];
   const unsigned char* base;
   uint32_t wave_lds;
-  __device__ __forceinline__ void init(const void* p, int64_t ld, int r0, int kbeg, int) {
+  // rows past the operand's last read that one: they only feed outputs that are never stored
+  __device__ __forceinline__ void init(const void* p, int64_t ld, int r0, int kbeg, int rmax) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int u = i * kGemmThreads + (int)threadIdx.x;
       const int row = u >> 3, kc = (u & 7) ^ ((row >> 1) & 7);          // inverse of Lds64::unit
-      voff[i] = (uint32_t)row * (uint32_t)ld * 2u + (uint32_t)kc * 16u;
+      voff[i] = (uint32_t)min(row, rmax - 1 - r0) * (uint32_t)ld * 2u + (uint32_t)kc * 16u;
     }
     base = static_cast<const unsigned char*>(p) + ((int64_t)r0 * ld + kbeg) * 2;
     wave_lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * 1024u;
+  }
+  // row r of the tile is row map[r0 + r] of the operand (which has fewer than 2^32 bytes)
+  __device__ __forceinline__ void init_mapped(const void* p, int64_t ld, int r0, int kbeg, int rmax, const int32_t* map) {
+    init(p, ld, 0, kbeg, R);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int u = i * kGemmThreads + (int)threadIdx.x;
+      const int row = u >> 3, kc = (u & 7) ^ ((row >> 1) & 7);
+      voff[i] = (uint32_t)map[min(r0 + row, rmax - 1)] * (uint32_t)ld * 2u + (uint32_t)kc * 16u;
+    }
   }
   template <int I> __device__ __forceinline__ void issue(uint32_t lds, int k) const {
     if constexpr (I < NI) dma16(base + (int64_t)k * 2, voff[I], lds + wave_lds + (uint32_t)I * 4096u);
@@ -143,15 +155,26 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
   const uint32_t smem_lds = (uint32_t)reinterpret_cast<uintptr_t>(smem_raw);
   constexpr int kStageElems = S::STAGE / 2, kAElems = BM * BK;
 
-  const int tiles_n = (g.N + BN - 1) / BN, tiles_m = g.M / BM;     // (N may be ragged for an M/N-contiguous B)
+  constexpr bool kHead = EPI == kEpiVocab || EPI == kEpiHeadX || EPI == kEpiHeadW;
+  constexpr bool kSwap = EPI == kEpiVocab;
+  // (N may be ragged for an M/N-contiguous B; under a loss M too, and N whatever B is)
+  const int tiles_n = (g.N + BN - 1) / BN, tiles_m = kHead ? (g.M + BM - 1) / BM : g.M / BM;
   const int T = tiles_m * tiles_n;
   int lin = blockIdx.x;
-  if ((T & 7) == 0) lin = (lin & 7) * (T >> 3) + (lin >> 3);
+  if (kHead) {                          // chunks per XCD whose lengths differ by one at most
+    const int q = T >> 3, r = T & 7, x = lin & 7;
+    lin = x * q + min(x, r) + (lin >> 3);
+  } else if ((T & 7) == 0) lin = (lin & 7) * (T >> 3) + (lin >> 3);
   constexpr int GM = 4;
   const int grp = lin / (GM * tiles_n), within = lin - grp * (GM * tiles_n);
   const int gh = min(GM, tiles_m - grp * GM);
   const int tm = grp * GM + within % gh, tn = within / gh;
   const int m0 = tm * BM, n0 = tn * BN;
+  int live = 0;
+  if constexpr (kHead) {
+    live = *g.head.live;
+    if (EPI != kEpiHeadW && m0 >= live) return;         // (the whole workgroup)
+  }
   const int w = threadIdx.x >> 6;
   const int wm0 = (w >> 1) * (BM / 2), wn0 = (w & 1) * (BN / 2);
   const int lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;
@@ -165,14 +188,17 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
   const int kbeg = g.k_splits > 1 ? (int)blockIdx.y * g.k_split : 0;
-  const int kend = g.k_splits > 1 ? min(g.K, kbeg + g.k_split) : g.K;
-  const int KT = (kend - kbeg + BK - 1) / BK;
+  const int k_all = EPI == kEpiHeadW ? min(g.K, live) : g.K;
+  const int kend = g.k_splits > 1 ? min(k_all, kbeg + g.k_split) : k_all;
+  const int KT = kHead ? max(0, (kend - kbeg + BK - 1) / BK) : (kend - kbeg + BK - 1) / BK;
   const int krem = kend - kbeg - (KT - 1) * BK;        // valid k of the last slice
   const bool ragged = krem < BK;                       // its loads read zeros past K; the steady loop never issues it
   const int KTs = ragged ? KT - 1 : KT;
   LoadA la; LoadB lb;
-  la.init(g.A, g.lda, m0, kbeg, g.M);
-  lb.init(g.B, g.ldb, n0, kbeg, g.N);
+  if constexpr (EPI == kEpiVocab) la.init_mapped(g.A, g.lda, m0, kbeg, live, g.head.row_map);
+  else if constexpr (EPI == kEpiHeadW) la.init(live == g.head.rows ? g.head.whole : g.A, g.lda, m0, kbeg, g.m_load);
+  else la.init(g.A, g.lda, m0, kbeg, g.M);
+  lb.init(g.B, g.ldb, n0, kbeg, kHead && kBT ? g.head.n_load : g.N);
 
   // load number Q (0 .. 15) of slice s into stage st: A and B alternate
   auto issue = [&](auto Q_, int st, int s) {
@@ -240,36 +266,36 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
     const bool tail1 = !steady && ragged && kt + 1 == KT - 1, tail2 = !steady && ragged && kt + 2 == KT - 1;
     {  // k-step 0
       auto f = rd(fa1, fb1, curA, curB, 1);
-      RAD_K0_AIM(8) mfma_piece<0, TM, TN>(fa0, fb0, acc); frag_read<0, TM, TN>(f.first, f.second); RAD_K0_DMA(8) RAD_FENCE();
-      RAD_K0_AIM(9) mfma_piece<1, TM, TN>(fa0, fb0, acc); frag_read<1, TM, TN>(f.first, f.second); RAD_K0_DMA(9) RAD_FENCE();
-      RAD_K0_AIM(10) mfma_piece<2, TM, TN>(fa0, fb0, acc); frag_read<2, TM, TN>(f.first, f.second); RAD_K0_DMA(10) RAD_FENCE();
-      RAD_K0_AIM(11) mfma_piece<3, TM, TN>(fa0, fb0, acc); frag_read<3, TM, TN>(f.first, f.second); RAD_K0_DMA(11) RAD_FENCE();
-      RAD_K0_AIM(12) mfma_piece<4, TM, TN>(fa0, fb0, acc); frag_read<4, TM, TN>(f.first, f.second); RAD_K0_DMA(12) RAD_FENCE();
-      RAD_K0_AIM(13) mfma_piece<5, TM, TN>(fa0, fb0, acc); frag_read<5, TM, TN>(f.first, f.second); RAD_K0_DMA(13) RAD_FENCE();
-      RAD_K0_AIM(14) mfma_piece<6, TM, TN>(fa0, fb0, acc); frag_read<6, TM, TN>(f.first, f.second); RAD_K0_DMA(14) RAD_FENCE();
-      RAD_K0_AIM(15) mfma_piece<7, TM, TN>(fa0, fb0, acc); frag_read<7, TM, TN>(f.first, f.second); RAD_K0_DMA(15) RAD_FENCE();
+      RAD_K0_AIM(8) mfma_piece<0, TM, TN, kSwap>(fa0, fb0, acc); frag_read<0, TM, TN>(f.first, f.second); RAD_K0_DMA(8) RAD_FENCE();
+      RAD_K0_AIM(9) mfma_piece<1, TM, TN, kSwap>(fa0, fb0, acc); frag_read<1, TM, TN>(f.first, f.second); RAD_K0_DMA(9) RAD_FENCE();
+      RAD_K0_AIM(10) mfma_piece<2, TM, TN, kSwap>(fa0, fb0, acc); frag_read<2, TM, TN>(f.first, f.second); RAD_K0_DMA(10) RAD_FENCE();
+      RAD_K0_AIM(11) mfma_piece<3, TM, TN, kSwap>(fa0, fb0, acc); frag_read<3, TM, TN>(f.first, f.second); RAD_K0_DMA(11) RAD_FENCE();
+      RAD_K0_AIM(12) mfma_piece<4, TM, TN, kSwap>(fa0, fb0, acc); frag_read<4, TM, TN>(f.first, f.second); RAD_K0_DMA(12) RAD_FENCE();
+      RAD_K0_AIM(13) mfma_piece<5, TM, TN, kSwap>(fa0, fb0, acc); frag_read<5, TM, TN>(f.first, f.second); RAD_K0_DMA(13) RAD_FENCE();
+      RAD_K0_AIM(14) mfma_piece<6, TM, TN, kSwap>(fa0, fb0, acc); frag_read<6, TM, TN>(f.first, f.second); RAD_K0_DMA(14) RAD_FENCE();
+      RAD_K0_AIM(15) mfma_piece<7, TM, TN, kSwap>(fa0, fb0, acc); frag_read<7, TM, TN>(f.first, f.second); RAD_K0_DMA(15) RAD_FENCE();
     }
     {  // k-step 1
       auto f = rd(fa0, fb0, curA, curB, 2);
-      mfma_piece<0, TM, TN>(fa1, fb1, acc); frag_read<0, TM, TN>(f.first, f.second); RAD_FENCE();
-      mfma_piece<1, TM, TN>(fa1, fb1, acc); frag_read<1, TM, TN>(f.first, f.second); RAD_FENCE();
-      mfma_piece<2, TM, TN>(fa1, fb1, acc); frag_read<2, TM, TN>(f.first, f.second); RAD_FENCE();
-      mfma_piece<3, TM, TN>(fa1, fb1, acc); frag_read<3, TM, TN>(f.first, f.second); RAD_FENCE();
-      mfma_piece<4, TM, TN>(fa1, fb1, acc); frag_read<4, TM, TN>(f.first, f.second); RAD_FENCE();
-      mfma_piece<5, TM, TN>(fa1, fb1, acc); frag_read<5, TM, TN>(f.first, f.second); RAD_FENCE();
-      mfma_piece<6, TM, TN>(fa1, fb1, acc); frag_read<6, TM, TN>(f.first, f.second); RAD_FENCE();
-      mfma_piece<7, TM, TN>(fa1, fb1, acc); frag_read<7, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<0, TM, TN, kSwap>(fa1, fb1, acc); frag_read<0, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<1, TM, TN, kSwap>(fa1, fb1, acc); frag_read<1, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<2, TM, TN, kSwap>(fa1, fb1, acc); frag_read<2, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<3, TM, TN, kSwap>(fa1, fb1, acc); frag_read<3, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<4, TM, TN, kSwap>(fa1, fb1, acc); frag_read<4, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<5, TM, TN, kSwap>(fa1, fb1, acc); frag_read<5, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<6, TM, TN, kSwap>(fa1, fb1, acc); frag_read<6, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<7, TM, TN, kSwap>(fa1, fb1, acc); frag_read<7, TM, TN>(f.first, f.second); RAD_FENCE();
     }
     {  // k-step 2: its fragment reads are the last of this stage and go first, two per piece
       auto f = rd(fa1, fb1, curA, curB, 3);
-      mfma_piece<0, TM, TN>(fa0, fb0, acc); frag_read<0, TM, TN>(f.first, f.second); frag_read<1, TM, TN>(f.first, f.second); RAD_FENCE();
-      mfma_piece<1, TM, TN>(fa0, fb0, acc); frag_read<2, TM, TN>(f.first, f.second); frag_read<3, TM, TN>(f.first, f.second); RAD_FENCE();
-      mfma_piece<2, TM, TN>(fa0, fb0, acc); frag_read<4, TM, TN>(f.first, f.second); frag_read<5, TM, TN>(f.first, f.second); RAD_FENCE();
-      mfma_piece<3, TM, TN>(fa0, fb0, acc); frag_read<6, TM, TN>(f.first, f.second); frag_read<7, TM, TN>(f.first, f.second); RAD_FENCE();
-      mfma_piece<4, TM, TN>(fa0, fb0, acc); RAD_FENCE();
-      mfma_piece<5, TM, TN>(fa0, fb0, acc); RAD_FENCE();
-      mfma_piece<6, TM, TN>(fa0, fb0, acc); RAD_FENCE();
-      mfma_piece<7, TM, TN>(fa0, fb0, acc); RAD_FENCE();
+      mfma_piece<0, TM, TN, kSwap>(fa0, fb0, acc); frag_read<0, TM, TN>(f.first, f.second); frag_read<1, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<1, TM, TN, kSwap>(fa0, fb0, acc); frag_read<2, TM, TN>(f.first, f.second); frag_read<3, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<2, TM, TN, kSwap>(fa0, fb0, acc); frag_read<4, TM, TN>(f.first, f.second); frag_read<5, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<3, TM, TN, kSwap>(fa0, fb0, acc); frag_read<6, TM, TN>(f.first, f.second); frag_read<7, TM, TN>(f.first, f.second); RAD_FENCE();
+      mfma_piece<4, TM, TN, kSwap>(fa0, fb0, acc); RAD_FENCE();
+      mfma_piece<5, TM, TN, kSwap>(fa0, fb0, acc); RAD_FENCE();
+      mfma_piece<6, TM, TN, kSwap>(fa0, fb0, acc); RAD_FENCE();
+      mfma_piece<7, TM, TN, kSwap>(fa0, fb0, acc); RAD_FENCE();
     }
     // slice kt+1 has landed (this thread's part) and this stage is read for the last time
     dma_wait<0>();
@@ -277,14 +303,14 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
     RAD_FENCE();
     {  // k-step 3
       auto f = rd(fa0, fb0, nxtA, nxtB, 0);
-      RAD_K3_AIM(0) mfma_piece<0, TM, TN>(fa1, fb1, acc); if (more) frag_read<0, TM, TN>(f.first, f.second); RAD_K3_DMA(0) RAD_FENCE();
-      RAD_K3_AIM(1) mfma_piece<1, TM, TN>(fa1, fb1, acc); if (more) frag_read<1, TM, TN>(f.first, f.second); RAD_K3_DMA(1) RAD_FENCE();
-      RAD_K3_AIM(2) mfma_piece<2, TM, TN>(fa1, fb1, acc); if (more) frag_read<2, TM, TN>(f.first, f.second); RAD_K3_DMA(2) RAD_FENCE();
-      RAD_K3_AIM(3) mfma_piece<3, TM, TN>(fa1, fb1, acc); if (more) frag_read<3, TM, TN>(f.first, f.second); RAD_K3_DMA(3) RAD_FENCE();
-      RAD_K3_AIM(4) mfma_piece<4, TM, TN>(fa1, fb1, acc); if (more) frag_read<4, TM, TN>(f.first, f.second); RAD_K3_DMA(4) RAD_FENCE();
-      RAD_K3_AIM(5) mfma_piece<5, TM, TN>(fa1, fb1, acc); if (more) frag_read<5, TM, TN>(f.first, f.second); RAD_K3_DMA(5) RAD_FENCE();
-      RAD_K3_AIM(6) mfma_piece<6, TM, TN>(fa1, fb1, acc); if (more) frag_read<6, TM, TN>(f.first, f.second); RAD_K3_DMA(6) RAD_FENCE();
-      RAD_K3_AIM(7) mfma_piece<7, TM, TN>(fa1, fb1, acc); if (more) frag_read<7, TM, TN>(f.first, f.second); RAD_K3_DMA(7) RAD_FENCE();
+      RAD_K3_AIM(0) mfma_piece<0, TM, TN, kSwap>(fa1, fb1, acc); if (more) frag_read<0, TM, TN>(f.first, f.second); RAD_K3_DMA(0) RAD_FENCE();
+      RAD_K3_AIM(1) mfma_piece<1, TM, TN, kSwap>(fa1, fb1, acc); if (more) frag_read<1, TM, TN>(f.first, f.second); RAD_K3_DMA(1) RAD_FENCE();
+      RAD_K3_AIM(2) mfma_piece<2, TM, TN, kSwap>(fa1, fb1, acc); if (more) frag_read<2, TM, TN>(f.first, f.second); RAD_K3_DMA(2) RAD_FENCE();
+      RAD_K3_AIM(3) mfma_piece<3, TM, TN, kSwap>(fa1, fb1, acc); if (more) frag_read<3, TM, TN>(f.first, f.second); RAD_K3_DMA(3) RAD_FENCE();
+      RAD_K3_AIM(4) mfma_piece<4, TM, TN, kSwap>(fa1, fb1, acc); if (more) frag_read<4, TM, TN>(f.first, f.second); RAD_K3_DMA(4) RAD_FENCE();
+      RAD_K3_AIM(5) mfma_piece<5, TM, TN, kSwap>(fa1, fb1, acc); if (more) frag_read<5, TM, TN>(f.first, f.second); RAD_K3_DMA(5) RAD_FENCE();
+      RAD_K3_AIM(6) mfma_piece<6, TM, TN, kSwap>(fa1, fb1, acc); if (more) frag_read<6, TM, TN>(f.first, f.second); RAD_K3_DMA(6) RAD_FENCE();
+      RAD_K3_AIM(7) mfma_piece<7, TM, TN, kSwap>(fa1, fb1, acc); if (more) frag_read<7, TM, TN>(f.first, f.second); RAD_K3_DMA(7) RAD_FENCE();
     }
   };
 
@@ -335,16 +361,20 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
 #undef RAD_K3_DMA
   // every wave is past the last barrier only after all its reads of the stages; nothing is in flight
   __syncthreads();
-  if constexpr (EPI == kEpiStore) {
+  if constexpr (EPI == kEpiStore || EPI == kEpiHeadX || EPI == kEpiHeadW) {
     if (g.split_stride > 0) {            // this split's partial sums go, as fp32, to an array of its own
       GemmArgs gs = g;
       gs.C = static_cast<float*>(g.C) + (int64_t)blockIdx.y * g.split_stride;
-      if (g.N % BN) epilogue_store<TM, TN, float, true, false, false, false>(gs, acc, m0, n0, wm0, wn0);
+      if (kHead || g.N % BN) epilogue_store<TM, TN, float, true, false, false, false>(gs, acc, m0, n0, wm0, wn0);
       else epilogue_store<TM, TN, float, false, false, false, false>(gs, acc, m0, n0, wm0, wn0);
       return;
     }
   }
-  if constexpr (EPI == kEpiStore && AKIND == kOpMN) {      // dW from a dense store: fp32 out
+  if constexpr (EPI == kEpiVocab) {
+    epilogue_vocab<BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, live);
+  } else if constexpr (EPI == kEpiHeadX || EPI == kEpiHeadW) {
+    epilogue_head<EPI == kEpiHeadX, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, EPI == kEpiHeadX ? live : g.M);
+  } else if constexpr (EPI == kEpiStore && AKIND == kOpMN) {      // dW from a dense store: fp32 out
     if (g.N % BN) epilogue_store_dispatch<kOpMN, TM, TN, uint16_t, true>(g, acc, m0, n0, wm0, wn0);
     else epilogue_store_dispatch<kOpMN, TM, TN, uint16_t, false>(g, acc, m0, n0, wm0, wn0);
   } else if constexpr (EPI == kEpiStore) {

@@ -1,0 +1,174 @@
+// Epilogues of the products of a layer under a loss over its classes (see HeadArgs): 256 x 256 tiles, four waves of
+// 128 x 128.
+#pragma once
+#include "gemm.hpp"
+
+namespace rad {
+
+// fp32 pair -> two bf16 (round to nearest even) in one word
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  uint16_t p[2];
+  put_pair(p, a, b);
+  return (uint32_t)p[0] | ((uint32_t)p[1] << 16);
+}
+
+// two distances below a maximum, as shares of the range, to 16 bits each (round to nearest; clamped to [0, 1])
+constexpr float kCodeRange = 128.f;
+constexpr uint32_t kCodeLast = 65535u;
+__device__ __forceinline__ uint32_t code_pair(float a, float b) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  union { u16x2 v; uint32_t w; } u;
+  u.v = __builtin_amdgcn_cvt_pknorm_u16(a, b);
+  return u.w;
+}
+
+// rows and columns of a 16-bit tile in LDS to global memory, 16 bytes a lane: row r of the tile goes to row place(r) of C
+template <int BM, int BN, class PLACE>
+__device__ __forceinline__ void store_tile(const uint16_t* ct, uint16_t* C, int64_t ldc, int rows, int n0, int N, PLACE place) {
+  constexpr int CP = BN + 8, CPR = BN / 8, NV = BM * CPR / kGemmThreads;
+#pragma unroll
+  for (int it = 0; it < NV; ++it) {
+    const int c = (int)threadIdx.x + it * kGemmThreads;
+    const int r = c / CPR, ch = c % CPR, col = n0 + ch * 8;
+    if (r >= rows || col >= N) continue;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(&ct[r * CP + ch * 8]);
+    uint16_t* const dst = C + (int64_t)place(r) * ldc + col;
+    if (col + 8 <= N) {
+      __builtin_memcpy(dst, &v, 16);                       // (at element alignment: rows of any width)
+    } else {
+      const uint16_t* ve = reinterpret_cast<const uint16_t*>(&v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (col + e < N) dst[e] = ve[e];
+    }
+  }
+}
+
+// The logits z = acc + bias never leave the registers.  What does, per row and 128 columns: their maximum m and the sum of
+// 2^((z - m) c) in fp32, the targets' logits, and, where there is a backward pass, how far every logit lies below m, as
+// 16 bits of a range of 128 powers of two (y, rows ldy apart, columns up to ldy; the last code stands for anything lower,
+// whose exponential is zero in fp32 too).  A step of that code is 2^-9 of a power of two, 0.04 % rms of a probability, a
+// quarter of what rounding the exponentials themselves to bf16 would cost, and they would be rounded once more when their
+// row's sum is known: dW of 4096 x 4096 x 128000 was 0.29 % rms off that way, against 0.17 % of a sum rounded once.
+// The product is transposed (lane = row of the tile): a row's 64 values are one lane's, so maximum and sum take one exchange
+// between the two lanes that share the row.
+template <int BM, int BN, int TM, int TN>
+__device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc)[TM][TN], uint16_t* ct, int m0, int n0, int wm0,
+                                               int wn0, int live) {
+  static_assert(TN == 4, "a wave's columns are one part of a row");
+  constexpr int CP = BN + 8;
+  const HeadArgs& h = g.head;
+  const int lane = threadIdx.x & 63, lr = lane & 31, hh = lane >> 5;
+  const int nw = n0 + wn0, part = nw / 128;
+  const float c = h.c, c_code = -c / kCodeRange;
+  if (g.bias) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int cb = nw + j * 32 + q * 8 + hh * 4;
+        float b[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = g.bias[min(cb + e, g.N - 1)];
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += b[e];
+        if (q & 1) __builtin_amdgcn_sched_barrier(0);        // (a few values of the bias in registers at a time)
+      }
+  }
+  if (nw + 128 > g.N) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const bool out = nw + j * 32 + acc_row(e, lane) >= g.N;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) acc[i][j][e] = out ? -INFINITY : acc[i][j][e];
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int place = m0 + wm0 + i * 32 + lr;
+    const bool there = place < live && nw < g.N;         // (the last tile may reach a whole part past the classes)
+    // targets among these 128 columns
+    int t0 = 0, t1 = 0, row = 0;
+    if (there) {
+      row = h.row_map[place];
+      if (h.labels) { t1 = (uint32_t)(h.labels[row] - nw) < 128u ? 1 : 0; }
+      else {
+        const uint16_t* const f = h.first + (int64_t)row * h.first_ld + part;
+        t0 = f[0]; t1 = f[1];
+      }
+    }
+    for (int t = t0; __any(t < t1); ++t) {
+      int col = -1;
+      if (t < t1) col = (h.labels ? h.labels[row] : h.index[(int64_t)row * h.k + t]) - nw;
+      float z = 0.f;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z = col == j * 32 + acc_row(e, lane) ? acc[i][j][e] : z;
+      if (col >= 0 && ((col >> 2) & 1) == hh) h.target[(int64_t)place * h.k + t] = z;
+    }
+    float m = -INFINITY, s = 0.f;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const float from = m == -INFINITY ? 0.f : m;
+    uint16_t* const crow = ct + (wm0 + i * 32 + lr) * CP + wn0 + hh * 4;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float below[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float d = acc[i][j][4 * q + e] - from;
+          s += __builtin_amdgcn_exp2f(d * c);
+          below[e] = d * c_code;
+        }
+        if (g.y)
+          *reinterpret_cast<u32x2*>(crow + j * 32 + q * 8) = u32x2{code_pair(below[0], below[1]), code_pair(below[2], below[3])};
+      }
+    s += __shfl_xor(s, 32);
+    if (there && hh == 0) *reinterpret_cast<float2*>(h.stats + ((int64_t)part * h.stats_ld + place) * 2) = make_float2(m, s);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (!g.y) return;
+  __syncthreads();
+  store_tile<BM, BN>(ct, static_cast<uint16_t*>(g.y), g.ldy, live - m0, n0, (int)g.ldy, [&](int r) { return m0 + r; });
+}
+
+// dX (rows sent to their places in the batch) and dW in bf16 through LDS, or in fp32 as they are
+template <bool X, int BM, int BN, int TM, int TN>
+__device__ __forceinline__ void epilogue_head(const GemmArgs& g, floatx16 (&acc)[TM][TN], uint16_t* ct, int m0, int n0, int wm0,
+                                              int wn0, int rows) {
+  const int lane = threadIdx.x & 63;
+  if (g.c_dtype == kF32) {                               // (dW only; partial sums of either return before)
+    if (g.beta) epilogue_store<TM, TN, float, true, false, true, false>(g, acc, m0, n0, wm0, wn0);
+    else epilogue_store<TM, TN, float, true, false, false, false>(g, acc, m0, n0, wm0, wn0);
+    return;
+  }
+  constexpr int CP = BN + 8;
+  uint16_t* const cbase = ct + (wm0 + 4 * (lane >> 5)) * CP + wn0 + (lane & 31);
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      const int r0 = i * 32 + (e >> 2) * 8 + (e & 3);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        uint16_t st[2];
+        put_pair(st, acc[i][j][e], acc[i][j][e + 1]);
+        cbase[r0 * CP + j * 32] = st[0];
+        cbase[(r0 + 1) * CP + j * 32] = st[1];
+      }
+    }
+  __syncthreads();
+  store_tile<BM, BN>(ct, static_cast<uint16_t*>(g.C), g.ldc, rows - m0, n0, g.N,
+                          [&](int r) { return X ? g.head.row_map[m0 + r] : m0 + r; });
+}
+
+}  // namespace rad

@@ -47,7 +47,26 @@ enum EpiKind : int {
   kEpiStore = 0, // C (+= if beta) = acc, optional output row map
   kEpiFwd = 1,   // bias / rank-u addend / ReLU / bits / dense y / pack next store
   kEpiConv = 2,  // rows are positions (b,yx), columns channels: bias / ReLU / bits, NCHW output
-  kEpiSplitK = 3 // plain store of the split's partial sums to C + split*M*N
+  kEpiSplitK = 3, // plain store of the split's partial sums to C + split*M*N
+  // a layer under a loss over its classes (bf16, direct-to-LDS kernels; HeadArgs):
+  kEpiVocab = 4,  // what a softmax needs of the logits, per row and 128 columns, and the logits in 16 bits
+  kEpiHeadX = 5,  // dX: rows put in their places, bf16; or fp32 partial sums
+  kEpiHeadW = 6   // dW: bf16 or fp32 (+= if beta); or fp32 partial sums
+};
+
+// The rows of the batch that have a target come first in a list; the products run over that list, whose length only the
+// device knows.
+struct HeadArgs {
+  const int32_t* live;          // length of the list
+  const int32_t* row_map;       // row of x and dX of every place in the list (kEpiVocab: of A; kEpiHeadX: of C)
+  const void* whole; int rows;  // kEpiHeadW: what A is where the list has all `rows` rows
+  int n_load;                   // B: readable columns (a multiple of 8, >= N), M/N contiguous
+  // kEpiVocab: logits z; c = log2(e) / T
+  float c;
+  float* stats; int64_t stats_ld;   // [columns / 128][stats_ld] pairs (maximum m, sum of 2^((z - m) c))
+  const int32_t* labels;        // [rows of the batch], or
+  const int32_t* index; const uint16_t* first; int k, first_ld;   // lists [rows][k], and how many of a row's entries lie before column 128 t
+  float* target;                // [place][k]: the logits of the targets
 };
 
 struct GemmArgs {
@@ -81,6 +100,7 @@ struct GemmArgs {
   // host side only: when set, the launch itself carries these two HIP events (start and end of the kernel),
   // which costs no extra packets on the stream
   void* ev_start; void* ev_stop;
+  HeadArgs head;
 };
 
 // dtype: operand element type; returns hipErrorInvalidValue for combinations
@@ -283,6 +303,46 @@ int64_t vocab_rows_stats_floats(int rows, int classes);
 hipError_t launch_vocab_rows(const VocabRows& a, hipStream_t st);
 // out (bf16) = beta out + in (fp32), n elements
 hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, hipStream_t st);
+
+// ---- the layer under such a loss (vocab_head.hip), around the products with HeadArgs
+// list [rows]: the rows that count, in order, then the others; *live: how many count
+hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, hipStream_t st);
+// first [rows][first_ld]: how many of a row's (sorted) entries lie before class 128 t, t = 0 .. parts
+hipError_t launch_list_parts(const int32_t* index, int rows, int k, int parts, uint16_t* first, int first_ld, hipStream_t st);
+// After the logits' product, for every place of the list: the row's loss, its maximum top, log2 sum 2^((z - top) c) and its
+// factor weight T.
+// For dW the rows of x side by side (xs, rows xs_ld apart, zeros past d_in), unless the list has them all.  Rows that do not
+// count: no loss, dX zero.
+struct VocabFinish {
+  const int32_t* list; const int32_t* live;
+  int rows, classes, parts;
+  VocabTargets t;               // of the rows of x
+  const float* stats; int64_t stats_ld;
+  const float* target;          // [place][k]
+  float* row_loss;              // [rows], in the batch's order
+  float* top; float* log2_sum; float* factor;   // [place]
+  uint16_t* z; int64_t z_ld;    // the logits' 16 bits, which launch_vocab_gradient turns into dz; null: forward only
+  const uint16_t* first; int first_ld;
+  const uint16_t* x; int64_t x_ld; int d_in; uint16_t* xs; int64_t xs_ld;   // xs null: no dW
+  uint16_t* dx;                 // rows d_in apart; null: no dX
+};
+hipError_t launch_vocab_finish(const VocabFinish& a, hipStream_t st);
+// dz = factor (2^((z - top) c - log2_sum) - p) in bf16, in the place of the codes; columns classes .. z_ld - 1 become zeros
+hipError_t launch_vocab_gradient(const VocabFinish& a, hipStream_t st);
+// out[map[i]] (rows out_ld apart; map null: i) (+)= sum of `splits` arrays' row i (rows in_ld apart, arrays stride apart),
+// i < min(rows, *live); live null: rows
+struct SplitSum {
+  const float* in; int splits; int64_t stride, in_ld;
+  int rows, cols; const int32_t* live; const int32_t* map;
+  void* out; int out_dtype; int64_t out_ld; int beta;
+};
+hipError_t launch_split_sum(const SplitSum& a, hipStream_t st);
+// out [cols] (+)= sum over the first *live rows of g[i][c]; part: [kHeadColsumSplits][cols]
+constexpr int kHeadColsumSplits = 32;
+hipError_t launch_head_colsum(const uint16_t* g, int64_t g_ld, const int32_t* live, int cols, float* part,
+                              float* out, int beta, hipStream_t st);
+// bf16 rows of any width and alignment to rows out_ld apart (a multiple of 8), zeros past cols
+hipError_t launch_pad_rows(const uint16_t* in, int64_t rows, int cols, uint16_t* out, int64_t out_ld, hipStream_t st);
 
 // Ceiling probes (ceilings.hip): kind 0 HBM read, 1 HBM copy, 2 / 3 bf16 MFMA 32x32x16 / 16x16x32 register loops,
 // 4 fp32 MFMA 32x32x2, 5 integer 32 x 32 -> 64 multiply-adds.  a: operands (probe_min_bytes at least), b: sink

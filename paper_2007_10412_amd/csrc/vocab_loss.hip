@@ -238,7 +238,7 @@ __device__ __forceinline__ void store_vec(O* out, int c, int classes, int64_t wi
 }
 
 // SPLIT: the row's parts are dealt to gridDim.x workgroups.  PASS 0 leaves each part's maximum and sum in stats
-// [rows][parts][2] and, with part 0, sum_j p_j z_{i_j} in dots [rows]; PASS 1 joins them, part by part in order, and writes.
+// [rows][parts][2] and, with part 0, the first target's logit z_0 and sum_j p_j (z_{i_j} - z_0) in dots [rows][2]; PASS 1 joins them, part by part in order, and writes.
 // Without SPLIT one workgroup has the whole row in its registers.
 template <typename T, typename O, int NT, int NV, bool SPLIT, int PASS>
 __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __restrict__ dots) {
@@ -285,7 +285,8 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
   constexpr int KT = (kTeacherMax + NT - 1) / NT;
   const int c_lo = v0 * VPL - lead, c_hi = c_lo + NT * NV * VPL;
   float tz[KT], tp[KT]; int ti[KT];
-  float dot = 0.f;
+  float dot = 0.f, z0 = 0.f;
+  if (part == 0 && !(SPLIT && PASS == 1)) { z0 = logit(target_index(t, row, 0)); if (z0 == -INFINITY) z0 = 0.f; }
 #pragma unroll
   for (int q = 0; q < KT; ++q) {
     const int j = (int)threadIdx.x + q * NT;
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
     const bool mine = i >= c_lo && i < c_hi;
     if (!mine && (PASS == 1 || part != 0)) continue;
     const float v = logit(i);
-    dot += pj * v;
+    dot += pj * (v - z0);
     if (mine) { ti[q] = i; tz[q] = v; tp[q] = pj; }
   }
 
@@ -318,7 +319,7 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
     if (threadIdx.x == 0) {
       float* const st = a.stats + ((int64_t)row * gridDim.x + part) * 2;
       st[0] = m; st[1] = s;
-      if (part == 0) dots[row] = dot;
+      if (part == 0) { dots[2 * row] = z0; dots[2 * row + 1] = dot; }
     }
     return;
   }
@@ -327,14 +328,14 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
     for (int w = 0; w < (int)gridDim.x; ++w) m = fmaxf(m, st[2 * w]);
     const float b = exp_base(m);
     for (int w = 0; w < (int)gridDim.x; ++w) s += rebased(st[2 * w + 1], st[2 * w], b, c);
-    if (part == 0) dot = dots[row];
+    if (part == 0) { z0 = dots[2 * row]; dot = dots[2 * row + 1]; }
     __syncthreads();                                    // every target's logit has been read
   }
   const float b = exp_base(m);
   if (a.row_loss && part == 0 && threadIdx.x == 0) {
     const float T1 = t.temperature;
-    const float lse = b / T1 + logf(s);
-    a.row_loss[row] = T1 * T1 * ((t.labels ? 0.f : t.entropy[row]) + (lse - dot / T1));
+    // lse - sum_j p_j z_j / T, from differences of logits (the probabilities' sum is 1)
+    a.row_loss[row] = T1 * T1 * ((t.labels ? 0.f : t.entropy[row]) + (logf(s) + ((b - z0) - dot) / T1));
   }
   if (!a.dz) return;
   const float wt = row_weight(t, row) * t.temperature, f = wt / s;
@@ -422,7 +423,7 @@ hipError_t launch_weighted_loss(const VocabTargets& t, const float* row_loss, in
 
 int64_t vocab_rows_stats_floats(int rows, int classes) {
   const int64_t parts = (classes / 4 + 2 + 64 + kPartThreads * kPartVecs) / (kPartThreads * kPartVecs) + 1;   // (fp32 vectors)
-  return (int64_t)rows * (parts * 2 + 1);
+  return (int64_t)rows * (parts * 2 + 2);
 }
 
 hipError_t launch_vocab_rows(const VocabRows& a, hipStream_t st) {

@@ -186,7 +186,8 @@ def check_linear(ctx, dtype, rows, d_in, classes, bias=False, ignored=0.0, k=0, 
 
 
 SHAPES = [(1, 1, 1), (1, 5, 3), (3, 7, 1), (5, 64, 33), (150, 300, 10), (64, 256, 1000), (130, 129, 131), (257, 520, 1003),
-          (300, 512, 4096), (1000, 72, 2500), (512, 1024, 8192), (17, 1030, 20011)]
+          (300, 512, 4096), (1000, 72, 2500), (512, 1024, 8192), (17, 1030, 20011),
+          (513, 260, 25601), (700, 512, 32000), (20, 129, 30000), (2000, 264, 4104), (1025, 1000, 8200), (4096, 64, 2048)]
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
@@ -199,7 +200,8 @@ def test_linear_ce(dtype, rows, d_in, classes):
 @pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("rows,d_in,classes,k,T,missing", [(1, 5, 3, 3, 1.0, 0.0), (5, 64, 33, 1, 2.0, 0.0), (150, 300, 10, 7, 1.5, 0.4),
                                                            (257, 520, 1003, 65, 0.7, 0.3), (300, 512, 4096, 300, 4.0, 0.0),
-                                                           (512, 1024, 8192, 16, 1.0, 0.2), (17, 1030, 20011, 1024, 2.0, 0.1)])
+                                                           (512, 1024, 8192, 16, 1.0, 0.2), (17, 1030, 20011, 1024, 2.0, 0.1),
+                                                           (700, 520, 30001, 33, 1.3, 0.3), (1025, 256, 8200, 1000, 1.0, 0.1)])
 def test_linear_distill(dtype, rows, d_in, classes, k, T, missing):
     with Ctx() as ctx:
         check_linear(ctx, dtype, rows, d_in, classes, bias=rows % 2 == 1, k=k, T=T, missing=missing)
@@ -207,7 +209,7 @@ def test_linear_distill(dtype, rows, d_in, classes, k, T, missing):
 
 @pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("rows,d_in,classes", [(1, 256, 5000), (2, 300, 1001), (9, 1024, 32000), (33, 768, 10007), (64, 512, 4096),
-                                               (100, 2048, 8000), (500, 512, 3001)])
+                                               (100, 2048, 8000), (500, 512, 3001), (1, 520, 40003), (260, 512, 40000)])
 def test_scoring(dtype, rows, d_in, classes):
     """Forward only."""
     with Ctx() as ctx:
@@ -216,7 +218,7 @@ def test_scoring(dtype, rows, d_in, classes):
 
 
 @pytest.mark.parametrize("dtype,dw_dtype", [(0, 0), (1, 0), (1, 1)])
-@pytest.mark.parametrize("rows,d_in,classes", [(70, 136, 264), (257, 129, 1003), (512, 512, 4096)])
+@pytest.mark.parametrize("rows,d_in,classes", [(70, 136, 264), (257, 129, 1003), (512, 512, 4096), (600, 200, 20005)])
 def test_weights_and_accumulation(dtype, dw_dtype, rows, d_in, classes):
     """Row weights of any sign, gradients added to what is there."""
     import torch
@@ -232,10 +234,11 @@ def test_weights_and_accumulation(dtype, dw_dtype, rows, d_in, classes):
 def test_some_outputs(dtype, outputs):
     with Ctx() as ctx:
         check_linear(ctx, dtype, 260, 136, 1030, bias=True, ignored=0.1, outputs=outputs)
+        check_linear(ctx, dtype, 600, 136, 20005, bias=True, ignored=0.1, outputs=outputs)
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
-@pytest.mark.parametrize("rows,d_in,classes", [(150, 300, 10), (300, 256, 4096)])
+@pytest.mark.parametrize("rows,d_in,classes", [(150, 300, 10), (300, 256, 4096), (600, 256, 20000)])
 def test_no_row_counts(dtype, rows, d_in, classes):
     """Every label outside the vocabulary: no loss, gradients of zeros (or what was there)."""
     with Ctx() as ctx:
@@ -244,7 +247,7 @@ def test_no_row_counts(dtype, rows, d_in, classes):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
-@pytest.mark.parametrize("rows,d_in,classes", [(20, 64, 1000), (300, 256, 4096), (512, 512, 8192)])
+@pytest.mark.parametrize("rows,d_in,classes", [(20, 64, 1000), (300, 256, 4096), (512, 512, 8192), (600, 256, 20000)])
 @pytest.mark.parametrize("masked", [-math.inf, -3.0e38])
 def test_masked_classes(dtype, rows, d_in, classes, masked):
     """Classes that a bias of -infinity, or of the type's lowest values, takes out (whole tiles of them among these)."""
@@ -291,7 +294,7 @@ def test_masked_classes(dtype, rows, d_in, classes, masked):
 def test_logits_far_from_zero(dtype, offset):
     """Rows whose logits all lie far from zero, where exponentials of the logits themselves leave the type."""
     with Ctx() as ctx:
-        for rows, d_in, classes in ((20, 64, 1000), (512, 512, 4096)):
+        for rows, d_in, classes in ((20, 64, 1000), (512, 512, 4096), (600, 256, 20001)):
             check_linear(ctx, dtype, rows, d_in, classes, bias=True, bias_values=lambda b: b + offset)
 
 
@@ -299,7 +302,7 @@ def test_logits_far_from_zero(dtype, offset):
 def test_peaked_rows(dtype):
     """Logits of a standard deviation of 60: one class has all of a row, and the label's loss is a hundred and more."""
     with Ctx() as ctx:
-        for rows, d_in, classes in ((20, 64, 1000), (512, 512, 4096)):
+        for rows, d_in, classes in ((20, 64, 1000), (512, 512, 4096), (600, 256, 20001)):
             check_linear(ctx, dtype, rows, d_in, classes, scale=60.0, ignored=0.1)
 
 
@@ -309,7 +312,39 @@ def test_more_rows_than_a_piece(dtype):
     with Ctx() as ctx:
         check_linear(ctx, dtype, 600, 16, 1100003, ignored=0.2, dw_dtype=0)
         if dtype:
-            check_linear(ctx, dtype, 530, 8, 1100000, k=3, dw_dtype=1)
+            check_linear(ctx, dtype, 1000, 16, 1300003, ignored=0.2, dw_dtype=0)
+            check_linear(ctx, dtype, 900, 8, 1300000, k=3, dw_dtype=1)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,classes", [(5, 40), (5, 9000), (300, 1000), (600, 20000)])
+def test_every_class_at_the_lowest_value(dtype, rows, classes):
+    """A mask of the lowest value over all classes leaves a uniform softmax (one of -infinity leaves none: NaN)."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    x = torch.zeros(rows, 64, device="cuda", dtype=torch_dtype(dtype))
+    W = torch.zeros(64, classes, device="cuda", dtype=torch_dtype(dtype))
+    labels = torch.arange(rows, device="cuda", dtype=torch.int32)
+    index = torch.stack([labels, labels + 1], dim=1).clamp(max=classes - 1).contiguous()
+    logit = torch.zeros(rows, 2, device="cuda")
+    layer = B.make_layer(rows, 64, classes, dtype=dtype, relu=False, has_bias=True)
+    row, db = torch.empty(rows, device="cuda"), torch.empty(classes, device="cuda")
+    with Ctx() as ctx:
+        for low, want in ((torch.finfo(torch.float32).min, math.log(classes)), (-math.inf, math.nan)):
+            b = torch.full((classes,), low, device="cuda")
+            B.rad_linear_ce(ctx, layer, x, W, b, labels, row_loss=row, dbias=db)
+            B.rad_ctx_synchronize(ctx)
+            if math.isnan(want):
+                assert torch.isnan(row).all() and torch.isnan(db).all()
+                continue
+            assert float((row - want).abs().max()) < 1e-5 * want
+            assert float((db[rows:] - 1 / classes).abs().max()) <= 2 ** -8 / classes if rows < classes else True
+            z = torch.full((rows, classes), torch.finfo(torch_dtype(dtype)).min, device="cuda", dtype=torch_dtype(dtype))
+            dz = torch.empty_like(z)
+            B.rad_distill_ce(ctx, z, B.make_teacher(index, logit), dtype, dz, row_loss=row)
+            B.rad_ctx_synchronize(ctx)
+            assert float((row[:-1] - (want - math.log(2))).abs().max()) < 1e-5 * want
+            assert torch.isfinite(dz.float()).all()
 
 
 def test_not_a_number_stays_in_its_row():
@@ -453,9 +488,10 @@ def test_two_calls_agree_bit_by_bit():
     import torch
     with Ctx() as ctx:
         for dtype in (0, 1):
-            a = check_linear(ctx, dtype, 300, 512, 4096, bias=True, k=9)
-            b = check_linear(ctx, dtype, 300, 512, 4096, bias=True, k=9)
-            assert all(torch.equal(a[n], b[n]) for n in a)
+            for shape in ((300, 512, 4096), (600, 512, 20000)):
+                a = check_linear(ctx, dtype, *shape, bias=True, k=9)
+                b = check_linear(ctx, dtype, *shape, bias=True, k=9)
+                assert all(torch.equal(a[n], b[n]) for n in a)
 
 
 def test_other_stream():
@@ -469,7 +505,8 @@ def test_other_stream():
             check_distill(ctx, 1, 300, 4097, 5)
 
 
-@pytest.mark.parametrize("dtype,rows,d_in,classes", [(0, 150, 300, 10), (1, 300, 512, 4096), (1, 5, 512, 4096), (0, 40, 256, 3000)])
+@pytest.mark.parametrize("dtype,rows,d_in,classes", [(0, 150, 300, 10), (1, 300, 512, 4096), (1, 5, 512, 4096), (0, 40, 256, 3000),
+                                                     (1, 600, 264, 20001)])
 def test_captured(dtype, rows, d_in, classes):
     """Recorded after one call of the same sizes, replayed with other inputs and eager work in between."""
     import torch
