@@ -326,11 +326,14 @@ rad_status rad_distill_ce(rad_ctx* ctx, const void* logits, const rad_teacher* t
  * are formed from, is rounded to that type; sums are fp32).  bias, dbias,
  * row_loss [batch] and loss [1] are fp32.  beta is 0 or 1.  Outputs may be null,
  * not all: without dX, dW and dbias the call scores, as for the
- * log-probabilities of tokens that a model has answered.  Logits exist for a
- * piece of the rows at a time, in a context workspace of at most 1 GiB (or 256
- * rows, if they are more); a bf16 dW takes one of d_in d_out fp32 sums.
- * d_in * d_out < 2^32.  Enqueued on the context's stream; results do not vary
- * from call to call. */
+ * log-probabilities of tokens that a model has answered.  Logits (bf16 layers:
+ * 16-bit codes of them, then dz) exist for a piece of the rows at a time, in a
+ * context workspace of at most 2 GiB (or 256 rows, if they are more).  Further
+ * workspaces: a copy of W or x where its rows are not whole 16-byte vectors (or
+ * its address is no multiple of 16); for a bf16 dW of several pieces, or with
+ * beta = 1, the fp32 sums [d_in, d_out]; partial sums where a product has few
+ * tiles.  d_in * d_out < 2^32, both at most 2^22 - 64.  Enqueued on the
+ * context's stream; results do not vary from call to call. */
 rad_status rad_linear_ce(rad_ctx* ctx, const rad_layer* layer, const void* x, const void* W, const float* bias,
                          const int32_t* labels, const float* row_weight, float* row_loss, float* loss, void* dX,
                          void* dW, int32_t dw_dtype, float* dbias, float beta);

@@ -1435,9 +1435,10 @@ static rad_status check_teacher(rad_ctx* c, const rad_teacher* t) {
   return RAD_OK;
 }
 
-// What the rows are to learn, made ready for the kernels, and room for their losses where the caller wants none.
+// What the rows are to learn, made ready for the kernels, and room for their losses where the caller wants none.  count: how
+// many rows there are to learn from is counted here (not where another kernel does).
 static rad_status vocab_targets(rad_ctx* c, const int32_t* labels, const rad_teacher* teacher, const float* weight,
-                                int rows, int classes, VocabTargets* t, float** row_loss) {
+                                int rows, int classes, bool count, VocabTargets* t, float** row_loss) {
   const size_t lists = teacher ? (size_t)rows * teacher->k : 0;
   char* ws = nullptr;
   RAD_TRY(ws_get(c, WS_TARGETS, 256 + (size_t)rows * 12 + lists * 8, reinterpret_cast<void**>(&ws)));
@@ -1456,7 +1457,7 @@ static rad_status vocab_targets(rad_ctx* c, const int32_t* labels, const rad_tea
       return launch_teacher(teacher->index, teacher->logit, rows, teacher->k, classes, t->temperature, index, prob, entropy, counts, c->stream);
     }));
   }
-  if (!weight)
+  if (!weight && count)
     HIP_TRY(c, timed(c, "count_rows", [&](const char**) { return launch_count_rows(*t, rows, classes, inv_count, c->stream); }));
   return RAD_OK;
 }
@@ -1487,16 +1488,17 @@ extern "C" rad_status rad_distill_ce(rad_ctx* c, const void* logits, const rad_t
   VocabRows a;
   std::memset(&a, 0, sizeof(a));
   float* losses = row_loss;
-  RAD_TRY(vocab_targets(c, nullptr, teacher, row_weight, (int)rows, (int)classes, &a.t, &losses));
-  a.z = logits; a.z_dtype = dtype; a.z_ld = classes; a.parts = 1;
+  RAD_TRY(vocab_targets(c, nullptr, teacher, row_weight, (int)rows, (int)classes, true, &a.t, &losses));
+  a.z = logits; a.dtype = dtype;
   a.rows = (int)rows; a.classes = (int)classes;
-  a.dz = dlogits; a.dz_dtype = dtype; a.dz_ld = classes;
+  a.dz = dlogits;
   a.row_loss = losses;
   RAD_TRY(vocab_rows(c, a));
   return vocab_loss_sum(c, a.t, losses, (int)rows, (int)classes, loss);
 }
 
-// Bytes of logits and of their gradient that exist at a time: rows go through the layer in pieces of this size.
+// Bytes of logits (bf16: their 16-bit codes) and then of their gradient that exist at a time: rows go through the layer in
+// pieces of this size.
 constexpr size_t kLogitPieceBytes = (size_t)2 << 30;
 
 struct HeadCall {
@@ -1505,206 +1507,68 @@ struct HeadCall {
   void* dX; void* dW; int dw_dtype; float* dbias; float beta;
 };
 
-// dW (+)= x^T g over the rows of one piece, fp32
-static rad_status head_dW(rad_ctx* c, int dtype, int rows, int d_in, int d_out, const void* x, const void* g, int64_t g_ld,
-                          float* dW, int beta) {
-  GemmArgs a = gemm_zero();
-  a.M = d_in; a.N = d_out; a.K = rows;
-  a.A = x; a.lda = d_in; a.B = g; a.ldb = g_ld;
-  a.C = dW; a.ldc = d_out; a.beta = beta; a.c_dtype = kF32;
-  if (dtype == kF32) return dw_dense_f32(c, a, 0.0);
-  SplitPlan sp;
-  RAD_TRY(split_k_for_few_tiles(c, &a, &sp));
-  RAD_TRY(run_gemm_call(c, dtype, kOpMN, kOpMN, kEpiStore, a));
-  return split_k_finish(c, a, sp);
-}
-
-// z = x W of one piece: fp32, `parts` arrays part_stride apart
-static rad_status head_logits(rad_ctx* c, int dtype, int rows, int d_in, int d_out, const void* x, const HeadCall& h, VocabRows* a) {
-  void* z = nullptr;
-  if (dtype == kF32) {
-    RAD_TRY(ws_get(c, WS_LOGITS, (size_t)rows * d_out * 4, &z));
-    RAD_TRY(forward_gemm(c, kF32, rows, d_out, d_in, x, d_in, h.W, h.bias, 0, z, nullptr, 0, nullptr, nullptr, 0, 0, nullptr));
-    a->z = z; a->z_ld = d_out; a->parts = 1;
-    return RAD_OK;
-  }
-  GemmArgs g = gemm_zero();
-  g.M = rows; g.N = d_out; g.K = d_in;
-  g.A = x; g.lda = d_in; g.B = h.W; g.ldb = d_out;
-  g.ldc = (d_out + 63) / 64 * 64; g.c_dtype = kF32;
-  g.split_stride = (int64_t)rows * g.ldc;
-  const int tiles = ((rows + 255) / 256) * ((d_out + 255) / 256);
-  int splits = std::min(256 / tiles, 8);
-  if (splits > 1 && d_in >= 512) {
-    g.k_split = std::max((d_in + splits - 1) / splits, 256);
-    g.k_split = (g.k_split + 63) / 64 * 64;
-    g.k_splits = (d_in + g.k_split - 1) / g.k_split;
-  }
-  a->parts = std::max(g.k_splits, 1);
-  RAD_TRY(ws_get(c, WS_LOGITS, (size_t)a->parts * g.split_stride * 4, &z));
-  g.C = z;
-  RAD_TRY(run_gemm_call(c, dtype, kOpK, kOpMN, kEpiStore, g));
-  a->z = z; a->z_ld = g.ldc; a->part_stride = g.split_stride; a->bias = h.bias;
-  return RAD_OK;
-}
-
-// Workgroups that share the K range of a 256 x 256 tile, so that they come close to filling the chip's 256 CUs a whole number
-// of times; a split has at least four slices and costs 3 % in partial sums.
-static int head_splits(int64_t tiles, int64_t K) {
-  int best = 1;
-  double best_rate = 0.0;
-  for (int s = 1; s <= 8 && (s == 1 || K / s >= 256); ++s) {
-    const int64_t waves = (tiles * s + 255) / 256;
-    const double rate = (double)(tiles * s) / (double)(waves * 256) * (s > 1 ? 0.97 - 0.01 * s : 1.0);
-    if (rate > best_rate) { best_rate = rate; best = s; }
+// Tiles of a product M x N x K under a loss, and how many workgroups share the K range of one: the least of
+//   filling the chip + (tiles a CU gets) x (their slices + their epilogue) + (the partial sums' way through memory at 4 TB/s,
+//   and a launch)
+// with what these took for 16 to 4000 rows, 300 to 4096 columns of x and 1000 to 100000 classes, in us.  In bf16, 256-row
+// tiles are the cheapest per slice and the dearest to begin and end, and a CU alone runs them faster than all together:
+// x W of 4000 x 1000 x 20000 takes 236 us in 256-row tiles, 233 in 128, 277 in 64; 1500 x 4096 x 20000 244, 277, 367;
+// 300 x 1000 x 20000 43, 26, 30; 100 x 1000 x 5000 38, 18, 14.
+struct HeadPlan { int tile, k_split, splits; };
+static HeadPlan head_plan(int dtype, int epi, int64_t M, int64_t N, int64_t K, bool may_split) {
+  struct Kind { int dtype, tile, cols; double fill_us, slice_us, alone_us, end_us; };
+  static const Kind kinds[] = {{kBF16, 256, 256, 3.0, 1.60, 1.00, 13.0}, {kBF16, 128, 128, 4.5, 0.58, 0.55, 2.5}, {kBF16, 64, 128, 4.5, 0.41, 0.40, 2.0},
+                               {kF32, 128, 128, 4.5, 1.90, 1.60, 2.5}, {kF32, 64, 128, 4.5, 1.05, 0.90, 2.0}};
+  const int bk = dtype == kBF16 ? 64 : 32;
+  HeadPlan best{128, 0, 1};
+  double best_us = 1e30;
+  for (const Kind& k : kinds) {
+    if (k.dtype != dtype || (k.tile == 64 && epi == kEpiHeadW)) continue;
+    const double end_us = k.end_us + (k.tile == 256 && epi == kEpiVocab ? 7.0 : 0.0);
+    const int64_t tiles = ((M + k.tile - 1) / k.tile) * ((N + k.cols - 1) / k.cols);
+    for (int s = 1; s <= 16 && (s == 1 || (may_split && K / s >= 128)); ++s) {
+      const int64_t k_split = ((K + s - 1) / s + 63) / 64 * 64;
+      const int splits = (int)((K + k_split - 1) / k_split);
+      const double each = (double)((tiles * splits + 255) / 256), full = std::min(1.0, (double)(tiles * splits) / 256.0);
+      const double slices = (double)((s > 1 ? k_split : K) + bk - 1) / bk;
+      const double us = k.fill_us + each * (slices * (k.alone_us + full * (k.slice_us - k.alone_us)) + end_us) +
+                        (splits > 1 ? (double)M * N * (8.0 * splits + 2.0) / 4e6 + 4.0 : 0.0);
+      if (us < best_us) { best_us = us; best = {k.tile, splits > 1 ? (int)k_split : 0, splits}; }
+    }
   }
   return best;
 }
 
-// The bf16 layer with its loss in the epilogue of the logits' product (vocab_head.hip).
-static bool head_fused_pays(int dtype, int64_t rows, int64_t d_out) {
-  return dtype == kBF16 && ((rows + 255) / 256) * ((d_out + 255) / 256) >= 100;
+// rows of whole 16-byte vectors from such an address on: a tensor itself, or a copy of it
+static rad_status head_padded(rad_ctx* c, int ws, int dtype, const void* in, int64_t rows, int cols, int64_t ld, const void** out) {
+  *out = in;
+  if (cols == ld && (reinterpret_cast<uintptr_t>(in) & 15) == 0) return RAD_OK;
+  void* copy = nullptr;
+  RAD_TRY(ws_get(c, ws, (size_t)rows * ld * (dtype == kF32 ? 4 : 2), &copy));
+  HIP_TRY(c, timed(c, "pad_rows", [&](const char**) { return launch_pad_rows(dtype, in, rows, cols, copy, ld, c->stream); }));
+  *out = copy;
+  return RAD_OK;
 }
-static rad_status head_fused(rad_ctx* c, int rows, int d_in, int d_out, const VocabTargets& t, const HeadCall& h, float* losses) {
-  const int64_t dp = (d_in + 7) / 8 * 8, vp8 = (d_out + 7) / 8 * 8, vp = (d_out + 63) / 64 * 64;
-  const int parts = (d_out + 127) / 128;
-  const bool train = h.dX || h.dW || h.dbias;
-  int64_t piece = std::min<int64_t>((int64_t)(kLogitPieceBytes / ((size_t)vp * 2)), (((int64_t)1 << 32) - 1) / (dp * 2));
-  piece = std::max<int64_t>(std::min<int64_t>(piece / 256 * 256, 1 << 19), 256);
-  if (piece > rows) piece = rows;
-  // operands whose rows are not whole 16-byte vectors are copied once
-  const uint16_t* W = static_cast<const uint16_t*>(h.W);
-  if (d_out % 8 || (reinterpret_cast<uintptr_t>(W) & 15)) {
-    void* ws = nullptr;
-    RAD_TRY(ws_get(c, WS_HEADW, (size_t)d_in * vp8 * 2, &ws));
-    HIP_TRY(c, timed(c, "pad_rows", [&](const char**) { return launch_pad_rows(W, d_in, d_out, static_cast<uint16_t*>(ws), vp8, c->stream); }));
-    W = static_cast<uint16_t*>(ws);
-  }
-  const uint16_t* x = static_cast<const uint16_t*>(h.x);
-  if (d_in % 8 || (reinterpret_cast<uintptr_t>(x) & 15)) {
-    void* ws = nullptr;
-    RAD_TRY(ws_get(c, WS_HEADX, (size_t)rows * dp * 2, &ws));
-    HIP_TRY(c, timed(c, "pad_rows", [&](const char**) { return launch_pad_rows(x, rows, d_in, static_cast<uint16_t*>(ws), dp, c->stream); }));
-    x = static_cast<uint16_t*>(ws);
-  }
-  const int first_ld = parts + 1;
-  const size_t first_bytes = t.labels ? 0 : ((size_t)rows * first_ld * 2 + 255) / 256 * 256;
-  char* ws = nullptr;
-  RAD_TRY(ws_get(c, WS_ROWLOSS, 256 + first_bytes + (size_t)piece * (8 * (size_t)parts + 16 + 4 * (size_t)t.k), reinterpret_cast<void**>(&ws)));
-  int32_t* const live = reinterpret_cast<int32_t*>(ws);
-  uint16_t* const first = reinterpret_cast<uint16_t*>(ws + 256);
-  float* const stats = reinterpret_cast<float*>(ws + 256 + first_bytes);
-  int32_t* const list = reinterpret_cast<int32_t*>(stats + (size_t)piece * parts * 2);
-  float* const top = reinterpret_cast<float*>(list + piece);
-  float* const log2_sum = top + piece;
-  float* const factor = log2_sum + piece;
-  float* const target = factor + piece;
-  if (!t.labels)
-    HIP_TRY(c, timed(c, "list_parts", [&](const char**) { return launch_list_parts(t.index, rows, t.k, parts, first, first_ld, c->stream); }));
 
-  const bool one = piece >= rows;
-  const bool cast = h.dW && h.dw_dtype == kBF16 && (!one || h.beta != 0.f);     // sums of several pieces are kept in fp32
-  float* dW32 = h.dw_dtype == kBF16 ? nullptr : static_cast<float*>(h.dW);
-  if (cast) RAD_TRY(ws_get(c, WS_HEADDW, (size_t)d_in * d_out * 4, reinterpret_cast<void**>(&dW32)));
-  void *P = nullptr, *xs = nullptr;
-  if (train) RAD_TRY(ws_get(c, WS_LOGITS, (size_t)piece * vp * 2, &P));
-  if (h.dW) RAD_TRY(ws_get(c, WS_LOGITGRAD, (size_t)piece * dp * 2, &xs));
-
-  for (int64_t r0 = 0; r0 < rows; r0 += piece) {
-    const int n = (int)std::min<int64_t>(piece, rows - r0);
-    VocabTargets tp = t;
-    if (tp.labels) tp.labels += r0;
-    else { tp.index += r0 * t.k; tp.prob += r0 * t.k; tp.entropy += r0; tp.counts += r0; }
-    if (tp.weight) tp.weight += r0;
-    HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(tp, n, d_out, list, live, c->stream); }));
-    GemmArgs g = gemm_zero();
-    g.M = n; g.N = d_out; g.K = d_in;
-    g.A = x + r0 * dp; g.lda = dp; g.B = W; g.ldb = vp8;
-    g.bias = h.bias; g.y = P; g.ldy = vp;
-    HeadArgs& a = g.head;
-    a.live = live; a.row_map = list; a.n_load = (int)vp8;
-    a.c = 1.44269504088896340736f / t.temperature;
-    a.stats = stats; a.stats_ld = piece;
-    a.labels = tp.labels; a.index = tp.index; a.first = t.labels ? nullptr : first + r0 * first_ld; a.k = t.k; a.first_ld = first_ld;
-    a.target = target;
-    RAD_TRY(run_gemm_call(c, kBF16, kOpK, kOpMN, kEpiVocab, g));
-    VocabFinish f;
-    std::memset(&f, 0, sizeof(f));
-    f.list = list; f.live = live; f.rows = n; f.classes = d_out; f.parts = parts; f.t = tp;
-    f.stats = stats; f.stats_ld = piece; f.target = target;
-    f.row_loss = losses + r0; f.top = top; f.log2_sum = log2_sum; f.factor = factor;
-    f.z = static_cast<uint16_t*>(P); f.z_ld = vp; f.first = a.first; f.first_ld = first_ld;
-    f.x = x + r0 * dp; f.x_ld = dp; f.d_in = d_in; f.xs = static_cast<uint16_t*>(xs); f.xs_ld = dp;
-    f.dx = h.dX ? static_cast<uint16_t*>(h.dX) + r0 * d_in : nullptr;
-    HIP_TRY(c, timed(c, "vocab_finish", [&](const char**) { return launch_vocab_finish(f, c->stream); }));
-    if (train) HIP_TRY(c, timed(c, "vocab_gradient", [&](const char**) { return launch_vocab_gradient(f, c->stream); }));
-    if (h.dX) {
-      GemmArgs gx = gemm_zero();
-      gx.M = n; gx.N = d_in; gx.K = (int)vp8;
-      gx.A = P; gx.lda = vp; gx.B = W; gx.ldb = vp8;
-      gx.C = f.dx; gx.ldc = d_in; gx.c_dtype = kBF16;
-      gx.head.live = live; gx.head.row_map = list;
-      const int splits = n <= 65535 ? head_splits((int64_t)((n + 255) / 256) * ((d_in + 255) / 256), vp8) : 1;
-      SplitSum sum;
-      std::memset(&sum, 0, sizeof(sum));
-      if (splits > 1) {
-        gx.k_split = (int)((vp8 + splits - 1) / splits + 63) / 64 * 64;
-        gx.k_splits = (int)((vp8 + gx.k_split - 1) / gx.k_split);
-        gx.ldc = (d_in + 63) / 64 * 64;
-        gx.split_stride = (int64_t)n * gx.ldc;
-        RAD_TRY(ws_get(c, WS_SPLITK, (size_t)gx.k_splits * gx.split_stride * 4, &gx.C));
-      }
-      RAD_TRY(run_gemm_call(c, kBF16, kOpK, kOpK, kEpiHeadX, gx));
-      if (splits > 1) {
-        sum.in = static_cast<const float*>(gx.C); sum.splits = gx.k_splits; sum.stride = gx.split_stride; sum.in_ld = gx.ldc;
-        sum.rows = n; sum.cols = d_in; sum.live = live; sum.map = list;
-        sum.out = f.dx; sum.out_dtype = kBF16; sum.out_ld = d_in;
-        HIP_TRY(c, timed(c, "split_sum", [&](const char**) { return launch_split_sum(sum, c->stream); }));
-      }
-    }
-    if (h.dW) {
-      GemmArgs gw = gemm_zero();
-      gw.M = d_in; gw.N = d_out; gw.K = n; gw.m_load = (int)dp;
-      gw.A = xs; gw.lda = dp; gw.B = P; gw.ldb = vp;
-      void* const out = dW32 ? dW32 : h.dW;
-      const int out_dtype = dW32 ? kF32 : kBF16, beta = dW32 && (r0 > 0 || (h.beta != 0.f && !cast));
-      gw.C = out; gw.ldc = d_out; gw.c_dtype = out_dtype; gw.beta = beta;
-      gw.head.live = live; gw.head.n_load = (int)vp8; gw.head.whole = f.x; gw.head.rows = n;
-      const int splits = d_in <= 65535 ? head_splits((int64_t)((d_in + 255) / 256) * ((d_out + 255) / 256), n) : 1;
-      if (splits > 1) {
-        gw.k_split = ((n + splits - 1) / splits + 63) / 64 * 64;
-        gw.k_splits = (n + gw.k_split - 1) / gw.k_split;
-        gw.ldc = vp;
-        gw.split_stride = (int64_t)d_in * vp;
-        RAD_TRY(ws_get(c, WS_SPLITK, (size_t)gw.k_splits * gw.split_stride * 4, &gw.C));
-      }
-      RAD_TRY(run_gemm_call(c, kBF16, kOpMN, kOpMN, kEpiHeadW, gw));
-      if (splits > 1) {
-        SplitSum sum;
-        std::memset(&sum, 0, sizeof(sum));
-        sum.in = static_cast<const float*>(gw.C); sum.splits = gw.k_splits; sum.stride = gw.split_stride; sum.in_ld = vp;
-        sum.rows = d_in; sum.cols = d_out;
-        sum.out = out; sum.out_dtype = out_dtype; sum.out_ld = d_out; sum.beta = beta;
-        HIP_TRY(c, timed(c, "split_sum", [&](const char**) { return launch_split_sum(sum, c->stream); }));
-      }
-    }
-    if (h.dbias) {
-      void* part = nullptr;
-      RAD_TRY(ws_get(c, WS_COLSUM, (size_t)kHeadColsumSplits * d_out * 4, &part));
-      HIP_TRY(c, timed(c, "head_colsum", [&](const char**) {
-        return launch_head_colsum(f.z, vp, live, d_out, static_cast<float*>(part), h.dbias, r0 > 0 || h.beta != 0.f, c->stream);
-      }));
-    }
-  }
-  if (cast)
-    HIP_TRY(c, timed(c, "cast_add", [&](const char**) {
-      return launch_cast_add(dW32, static_cast<uint16_t*>(h.dW), (int64_t)d_in * d_out, h.beta != 0.f, c->stream);
-    }));
+// a product with its plan: partial sums of a split K go through a workspace to `sum`'s output
+static rad_status head_product(rad_ctx* c, int dtype, int epi, const HeadPlan& plan, GemmArgs g, const SplitSum& sum) {
+  g.head.tile = plan.tile;
+  const int ak = epi == kEpiHeadW ? kOpMN : kOpK, bk = epi == kEpiHeadX ? kOpK : kOpMN;
+  if (plan.splits <= 1) return run_gemm_call(c, dtype, ak, bk, epi, g);
+  g.k_split = plan.k_split; g.k_splits = plan.splits;
+  g.ldc = (g.N + 63) / 64 * 64;
+  g.split_stride = (int64_t)g.M * g.ldc;
+  RAD_TRY(ws_get(c, WS_SPLITK, (size_t)plan.splits * g.split_stride * 4, &g.C));
+  RAD_TRY(run_gemm_call(c, dtype, ak, bk, epi, g));
+  SplitSum s = sum;
+  s.in = static_cast<const float*>(g.C); s.splits = plan.splits; s.stride = g.split_stride; s.in_ld = g.ldc;
+  s.rows = g.M; s.cols = g.N;
+  HIP_TRY(c, timed(c, "split_sum", [&](const char**) { return launch_split_sum(s, c->stream); }));
   return RAD_OK;
 }
 
 static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* labels, const rad_teacher* teacher,
-                            const float* row_weight, HeadCall h) {
+                            const float* row_weight, const HeadCall& h) {
   RAD_TRY(check_layer(c, L));
   if (L->kind != RAD_LINEAR || L->relu) return fail(c, RAD_ERR_PARAM, "the loss takes a linear layer without ReLU");
   if (!h.x || !h.W) return fail(c, RAD_ERR_NULL, "null argument");
@@ -1713,53 +1577,115 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   if (h.beta != 0.f && h.beta != 1.f) return fail(c, RAD_ERR_PARAM, "beta must be 0 or 1");
   if (h.dW && h.dw_dtype != RAD_F32 && h.dw_dtype != L->dtype) return fail(c, RAD_ERR_PARAM, "dW is fp32 or of the layer's type");
   if (L->d_in * L->d_out >= ((int64_t)1 << 32)) return fail(c, RAD_ERR_SHAPE, "weights of 2^32 elements or more");
+  if (std::max(L->d_in, L->d_out) > ((int64_t)1 << 22) - 64) return fail(c, RAD_ERR_SHAPE, "d_in or d_out above 2^22 - 64");
   DeviceGuard guard(c->device);
   const int rows = (int)L->batch, d_in = (int)L->d_in, d_out = (int)L->d_out, dtype = L->dtype;
-  const size_t esz = dtype == kF32 ? 4 : 2;
+  const int64_t esz = dtype == kF32 ? 4 : 2, vec = 16 / esz;
+  const int64_t dp = (d_in + vec - 1) / vec * vec, vp8 = (d_out + vec - 1) / vec * vec, vp = (d_out + 63) / 64 * 64;
+  const bool train = h.dX || h.dW || h.dbias;
+  // a piece: logits of 2 GiB, rows of x that 32-bit byte offsets reach
+  int64_t piece = std::min<int64_t>((int64_t)(kLogitPieceBytes / ((size_t)vp * esz)), (((int64_t)1 << 32) - 1) / (dp * esz));
+  piece = std::max<int64_t>(std::min<int64_t>(piece / 256 * 256, 1 << 19), 256);
+  if (piece > rows) piece = rows;
+  const bool one = piece >= rows;
+
   VocabTargets t;
   float* losses = h.row_loss;
-  RAD_TRY(vocab_targets(c, labels, teacher, row_weight, rows, d_out, &t, &losses));
-  if (head_fused_pays(dtype, rows, d_out)) {
-    RAD_TRY(head_fused(c, rows, d_in, d_out, t, h, losses));
-    return vocab_loss_sum(c, t, losses, rows, d_out, h.loss);
-  }
-  const bool train = h.dX || h.dW || h.dbias;
-  const int64_t pitch = dtype == kF32 ? d_out : (d_out + 63) / 64 * 64;
-  int64_t piece = (int64_t)(kLogitPieceBytes / ((size_t)pitch * 4));
-  piece = std::max<int64_t>(piece / 256 * 256, 256);
-  const bool cast = h.dW && h.dw_dtype == kBF16;
-  float* dW32 = static_cast<float*>(h.dW);
+  RAD_TRY(vocab_targets(c, labels, teacher, row_weight, rows, d_out, !one, &t, &losses));
+  const void *W = nullptr, *x = nullptr;
+  RAD_TRY(head_padded(c, WS_HEADW, dtype, h.W, d_in, d_out, vp8, &W));
+  RAD_TRY(head_padded(c, WS_HEADX, dtype, h.x, rows, d_in, dp, &x));
+
+  const HeadPlan fwd = head_plan(dtype, kEpiVocab, piece, d_out, d_in, false);
+  const int part = head_part(fwd.tile), parts = (d_out + part - 1) / part;
+  const int first_ld = parts + 1;
+  const size_t first_bytes = t.labels ? 0 : ((size_t)rows * first_ld * 2 + 255) / 256 * 256;
+  char* ws = nullptr;
+  RAD_TRY(ws_get(c, WS_ROWLOSS, 256 + first_bytes + (size_t)piece * (8 * (size_t)parts + 12 + 4 * (size_t)t.k), reinterpret_cast<void**>(&ws)));
+  int32_t* const live = reinterpret_cast<int32_t*>(ws);
+  uint16_t* const first = reinterpret_cast<uint16_t*>(ws + 256);
+  float* const stats = reinterpret_cast<float*>(ws + 256 + first_bytes);
+  int32_t* const list = reinterpret_cast<int32_t*>(stats + (size_t)piece * parts * 2);
+  float* const top = reinterpret_cast<float*>(list + piece);
+  float* const factor = top + piece;
+  float* const target = factor + piece;
+  if (!t.labels)
+    HIP_TRY(c, timed(c, "list_parts", [&](const char**) { return launch_list_parts(t.index, rows, t.k, part, parts, first, first_ld, c->stream); }));
+
+  const bool cast = h.dW && h.dw_dtype == kBF16 && (!one || h.beta != 0.f);     // sums of several pieces are kept in fp32
+  float* dW32 = h.dw_dtype == kBF16 ? nullptr : static_cast<float*>(h.dW);
   if (cast) RAD_TRY(ws_get(c, WS_HEADDW, (size_t)d_in * d_out * 4, reinterpret_cast<void**>(&dW32)));
+  void *z = nullptr, *xs = nullptr;
+  if (train) RAD_TRY(ws_get(c, WS_LOGITS, (size_t)(piece * vp * esz), &z));
+  if (h.dW) RAD_TRY(ws_get(c, WS_LOGITGRAD, (size_t)(piece * dp * esz), &xs));
+  bool summed = false;
+
   for (int64_t r0 = 0; r0 < rows; r0 += piece) {
     const int n = (int)std::min<int64_t>(piece, rows - r0);
-    const char* const xp = static_cast<const char*>(h.x) + (size_t)r0 * d_in * esz;
-    VocabRows a;
-    std::memset(&a, 0, sizeof(a));
-    a.t = t;
-    if (t.labels) a.t.labels += r0;
-    else { a.t.index += r0 * t.k; a.t.prob += r0 * t.k; a.t.entropy += r0; a.t.counts += r0; }
-    if (t.weight) a.t.weight += r0;
-    a.rows = n; a.classes = d_out; a.z_dtype = kF32;
-    a.row_loss = losses + r0;
-    RAD_TRY(head_logits(c, dtype, n, d_in, d_out, xp, h, &a));
-    if (train) {
-      void* g = const_cast<void*>(a.z);
-      if (dtype != kF32) RAD_TRY(ws_get(c, WS_LOGITGRAD, (size_t)n * pitch * esz, &g));
-      a.dz = g; a.dz_dtype = dtype; a.dz_ld = pitch;
+    VocabTargets tp = t;
+    if (tp.labels) tp.labels += r0;
+    else { tp.index += r0 * t.k; tp.prob += r0 * t.k; tp.entropy += r0; tp.counts += r0; }
+    if (tp.weight) tp.weight += r0;
+    float* const inv_count = one && !row_weight ? const_cast<float*>(t.inv_count) : nullptr;
+    HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(tp, n, d_out, list, live, inv_count, c->stream); }));
+    GemmArgs g = gemm_zero();
+    g.M = n; g.N = d_out; g.K = d_in;
+    g.A = static_cast<const char*>(x) + r0 * dp * esz; g.lda = dp; g.B = W; g.ldb = vp8;
+    g.bias = h.bias; g.y = z; g.ldy = vp;
+    HeadArgs& a = g.head;
+    a.live = live; a.row_map = list; a.n_load = (int)vp8;
+    a.c = 1.44269504088896340736f / t.temperature;
+    a.stats = stats; a.stats_ld = piece;
+    a.labels = tp.labels; a.index = tp.index; a.first = t.labels ? nullptr : first + r0 * first_ld; a.k = t.k; a.first_ld = first_ld;
+    a.target = target;
+    RAD_TRY(head_product(c, dtype, kEpiVocab, fwd, g, SplitSum{}));
+    VocabFinish f;
+    std::memset(&f, 0, sizeof(f));
+    f.dtype = dtype;
+    f.list = list; f.live = live; f.rows = n; f.classes = d_out; f.parts = parts; f.part = part; f.t = tp;
+    f.stats = stats; f.stats_ld = piece; f.target = target;
+    f.row_loss = losses + r0; f.top = top; f.factor = factor;
+    f.z = z; f.z_ld = vp; f.first = a.first; f.first_ld = first_ld;
+    f.x = g.A; f.x_ld = dp; f.d_in = d_in; f.xs = xs;
+    f.dx = h.dX ? static_cast<char*>(h.dX) + r0 * d_in * esz : nullptr;
+    if (one && h.loss && vocab_loss_inside(f)) { f.loss = h.loss; summed = true; }
+    HIP_TRY(c, timed(c, "vocab_finish", [&](const char**) { return launch_vocab_finish(f, c->stream); }));
+    if (train) HIP_TRY(c, timed(c, "vocab_gradient", [&](const char**) { return launch_vocab_gradient(f, c->stream); }));
+    SplitSum sum;
+    if (h.dX) {
+      GemmArgs gx = gemm_zero();
+      gx.M = n; gx.N = d_in; gx.K = (int)vp8;
+      gx.A = z; gx.lda = vp; gx.B = W; gx.ldb = vp8;
+      gx.C = f.dx; gx.ldc = d_in; gx.c_dtype = dtype;
+      gx.head.live = live; gx.head.row_map = list;
+      std::memset(&sum, 0, sizeof(sum));
+      sum.live = live; sum.map = list; sum.out = f.dx; sum.out_dtype = dtype; sum.out_ld = d_in;
+      RAD_TRY(head_product(c, dtype, kEpiHeadX, head_plan(dtype, kEpiHeadX, n, d_in, vp8, n <= 65535), gx, sum));
     }
-    RAD_TRY(vocab_rows(c, a));
-    if (h.dX)
-      RAD_TRY(dX_gemm(c, dtype, n, d_in, d_out, a.dz, nullptr, 0, h.W, static_cast<char*>(h.dX) + (size_t)r0 * d_in * esz, nullptr, 0, (int)pitch));
-    const int beta = r0 > 0 || (h.beta != 0.f && !cast);
-    if (h.dW) RAD_TRY(head_dW(c, dtype, n, d_in, d_out, xp, a.dz, pitch, dW32, beta));
-    if (h.dbias)
-      RAD_TRY(colsum_call(c, a.dz, dtype, n, d_out, nullptr, 0, nullptr, 0, 0, h.dbias, nullptr, r0 > 0 || h.beta != 0.f, 0, 0, pitch));
+    if (h.dW) {
+      GemmArgs gw = gemm_zero();
+      gw.M = d_in; gw.N = d_out; gw.K = n; gw.m_load = (int)dp;
+      gw.A = xs; gw.lda = dp; gw.B = z; gw.ldb = vp;
+      gw.C = dW32 ? dW32 : h.dW; gw.ldc = d_out; gw.c_dtype = dW32 ? kF32 : kBF16;
+      gw.beta = dW32 && (r0 > 0 || (h.beta != 0.f && !cast));
+      gw.head.live = live; gw.head.n_load = (int)vp8; gw.head.whole = f.x; gw.head.rows = n;
+      std::memset(&sum, 0, sizeof(sum));
+      sum.out = gw.C; sum.out_dtype = gw.c_dtype; sum.out_ld = d_out; sum.beta = gw.beta;
+      RAD_TRY(head_product(c, dtype, kEpiHeadW, head_plan(dtype, kEpiHeadW, d_in, d_out, n, d_in <= 65535), gw, sum));
+    }
+    if (h.dbias) {
+      void* partial = nullptr;
+      RAD_TRY(ws_get(c, WS_COLSUM, (size_t)kHeadColsumSplits * d_out * 4, &partial));
+      HIP_TRY(c, timed(c, "head_colsum", [&](const char**) {
+        return launch_head_colsum(dtype, z, vp, live, d_out, static_cast<float*>(partial), h.dbias, r0 > 0 || h.beta != 0.f, c->stream);
+      }));
+    }
   }
   if (cast)
     HIP_TRY(c, timed(c, "cast_add", [&](const char**) {
       return launch_cast_add(dW32, static_cast<uint16_t*>(h.dW), (int64_t)d_in * d_out, h.beta != 0.f, c->stream);
     }));
-  return vocab_loss_sum(c, t, losses, rows, d_out, h.loss);
+  return summed ? RAD_OK : vocab_loss_sum(c, t, losses, rows, d_out, h.loss);
 }
 
 extern "C" rad_status rad_linear_ce(rad_ctx* c, const rad_layer* L, const void* x, const void* W, const float* bias,

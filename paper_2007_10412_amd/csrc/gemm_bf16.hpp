@@ -849,7 +849,7 @@ __global__ __launch_bounds__(kGemmThreads * ((FLAGS & kFlagKHalves) ? 2 : 1)) vo
   }
 
   if constexpr (EPI == kEpiStore) {
-    if (g.split_stride > 0) {     // this split's partial sums go, as fp32, to an array of its own
+    if (g.k_splits > 1 && g.split_stride > 0) {     // this split's partial sums go, as fp32, to an array of its own
       GemmArgs gs = g;
       gs.C = static_cast<float*>(g.C) + (int64_t)blockIdx.y * g.split_stride;
       epilogue_store<TM, TN, float, EDGE, false, false, false>(gs, acc, m0, n0, wm0, wn0);

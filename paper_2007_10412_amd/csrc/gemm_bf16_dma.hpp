@@ -362,7 +362,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
   // every wave is past the last barrier only after all its reads of the stages; nothing is in flight
   __syncthreads();
   if constexpr (EPI == kEpiStore || EPI == kEpiHeadX || EPI == kEpiHeadW) {
-    if (g.split_stride > 0) {            // this split's partial sums go, as fp32, to an array of its own
+    if (g.k_splits > 1 && g.split_stride > 0) {            // this split's partial sums go, as fp32, to an array of its own
       GemmArgs gs = g;
       gs.C = static_cast<float*>(g.C) + (int64_t)blockIdx.y * g.split_stride;
       if (kHead || g.N % BN) epilogue_store<TM, TN, float, true, false, false, false>(gs, acc, m0, n0, wm0, wn0);
@@ -371,7 +371,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
     }
   }
   if constexpr (EPI == kEpiVocab) {
-    epilogue_vocab<BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, live);
+    epilogue_vocab<uint16_t, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, live);
   } else if constexpr (EPI == kEpiHeadX || EPI == kEpiHeadW) {
     epilogue_head<EPI == kEpiHeadX, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, EPI == kEpiHeadX ? live : g.M);
   } else if constexpr (EPI == kEpiStore && AKIND == kOpMN) {      // dW from a dense store: fp32 out

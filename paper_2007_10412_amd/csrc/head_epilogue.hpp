@@ -1,5 +1,4 @@
-// Epilogues of the products of a layer under a loss over its classes (see HeadArgs): 256 x 256 tiles, four waves of
-// 128 x 128.
+// Epilogues of the products of a layer under a loss over its classes (see HeadArgs): four waves, two by two on a tile.
 #pragma once
 #include "gemm.hpp"
 
@@ -22,43 +21,45 @@ __device__ __forceinline__ uint32_t code_pair(float a, float b) {
   return u.w;
 }
 
-// rows and columns of a 16-bit tile in LDS to global memory, 16 bytes a lane: row r of the tile goes to row place(r) of C
-template <int BM, int BN, class PLACE>
-__device__ __forceinline__ void store_tile(const uint16_t* ct, uint16_t* C, int64_t ldc, int rows, int n0, int N, PLACE place) {
-  constexpr int CP = BN + 8, CPR = BN / 8, NV = BM * CPR / kGemmThreads;
+// rows and columns of a tile in LDS to global memory, 16 bytes a lane: row r of the tile goes to row place(r) of C
+template <typename T, int BM, int BN, class PLACE>
+__device__ __forceinline__ void store_tile(const T* ct, T* C, int64_t ldc, int rows, int n0, int N, PLACE place) {
+  constexpr int VPL = 16 / (int)sizeof(T), CP = BN + VPL, CPR = BN / VPL, NV = BM * CPR / kGemmThreads;
 #pragma unroll
   for (int it = 0; it < NV; ++it) {
     const int c = (int)threadIdx.x + it * kGemmThreads;
-    const int r = c / CPR, ch = c % CPR, col = n0 + ch * 8;
+    const int r = c / CPR, ch = c % CPR, col = n0 + ch * VPL;
     if (r >= rows || col >= N) continue;
-    const u32x4 v = *reinterpret_cast<const u32x4*>(&ct[r * CP + ch * 8]);
-    uint16_t* const dst = C + (int64_t)place(r) * ldc + col;
-    if (col + 8 <= N) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(&ct[r * CP + ch * VPL]);
+    T* const dst = C + (int64_t)place(r) * ldc + col;
+    if (col + VPL <= N) {
       __builtin_memcpy(dst, &v, 16);                       // (at element alignment: rows of any width)
     } else {
-      const uint16_t* ve = reinterpret_cast<const uint16_t*>(&v);
+      const T* ve = reinterpret_cast<const T*>(&v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) if (col + e < N) dst[e] = ve[e];
+      for (int e = 0; e < VPL; ++e) if (col + e < N) dst[e] = ve[e];
     }
   }
 }
 
-// The logits z = acc + bias never leave the registers.  What does, per row and 128 columns: their maximum m and the sum of
+// bf16: the logits z = acc + bias never leave the registers.  What does, per row and part of its columns (a wave's: 128, or 64 in
+// smaller tiles): their maximum m and the sum of
 // 2^((z - m) c) in fp32, the targets' logits, and, where there is a backward pass, how far every logit lies below m, as
 // 16 bits of a range of 128 powers of two (y, rows ldy apart, columns up to ldy; the last code stands for anything lower,
 // whose exponential is zero in fp32 too).  A step of that code is 2^-9 of a power of two, 0.04 % rms of a probability, a
 // quarter of what rounding the exponentials themselves to bf16 would cost, and they would be rounded once more when their
 // row's sum is known: dW of 4096 x 4096 x 128000 was 0.29 % rms off that way, against 0.17 % of a sum rounded once.
+// fp32: the logits themselves take the place of the codes.
 // The product is transposed (lane = row of the tile): a row's 64 values are one lane's, so maximum and sum take one exchange
 // between the two lanes that share the row.
-template <int BM, int BN, int TM, int TN>
-__device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc)[TM][TN], uint16_t* ct, int m0, int n0, int wm0,
+template <typename T, int BM, int BN, int TM, int TN>
+__device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc)[TM][TN], T* ct, int m0, int n0, int wm0,
                                                int wn0, int live) {
-  static_assert(TN == 4, "a wave's columns are one part of a row");
-  constexpr int CP = BN + 8;
+  constexpr bool kCodes = sizeof(T) == 2;
+  constexpr int CP = BN + 16 / (int)sizeof(T), kPart = 32 * TN;            // a wave's columns are one part of a row
   const HeadArgs& h = g.head;
   const int lane = threadIdx.x & 63, lr = lane & 31, hh = lane >> 5;
-  const int nw = n0 + wn0, part = nw / 128;
+  const int nw = n0 + wn0, part = nw / kPart;
   const float c = h.c, c_code = -c / kCodeRange;
   if (g.bias) {
 #pragma unroll
@@ -76,7 +77,7 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
         if (q & 1) __builtin_amdgcn_sched_barrier(0);        // (a few values of the bias in registers at a time)
       }
   }
-  if (nw + 128 > g.N) {
+  if (nw + kPart > g.N) {
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -90,11 +91,11 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
   for (int i = 0; i < TM; ++i) {
     const int place = m0 + wm0 + i * 32 + lr;
     const bool there = place < live && nw < g.N;         // (the last tile may reach a whole part past the classes)
-    // targets among these 128 columns
+    // targets among these columns
     int t0 = 0, t1 = 0, row = 0;
     if (there) {
       row = h.row_map[place];
-      if (h.labels) { t1 = (uint32_t)(h.labels[row] - nw) < 128u ? 1 : 0; }
+      if (h.labels) { t1 = (uint32_t)(h.labels[row] - nw) < (uint32_t)kPart ? 1 : 0; }
       else {
         const uint16_t* const f = h.first + (int64_t)row * h.first_ld + part;
         t0 = f[0]; t1 = f[1];
@@ -117,7 +118,7 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
       for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
     m = fmaxf(m, __shfl_xor(m, 32));
     const float from = m == -INFINITY ? 0.f : m;
-    uint16_t* const crow = ct + (wm0 + i * 32 + lr) * CP + wn0 + hh * 4;
+    T* const crow = ct + (wm0 + i * 32 + lr) * CP + wn0 + hh * 4;
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -127,9 +128,11 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
         for (int e = 0; e < 4; ++e) {
           const float d = acc[i][j][4 * q + e] - from;
           s += __builtin_amdgcn_exp2f(d * c);
-          below[e] = d * c_code;
+          below[e] = kCodes ? d * c_code : acc[i][j][4 * q + e];
         }
-        if (g.y)
+        if (!g.y) continue;
+        if constexpr (!kCodes) *reinterpret_cast<floatx4*>(crow + j * 32 + q * 8) = floatx4{below[0], below[1], below[2], below[3]};
+        else
           *reinterpret_cast<u32x2*>(crow + j * 32 + q * 8) = u32x2{code_pair(below[0], below[1]), code_pair(below[2], below[3])};
       }
     s += __shfl_xor(s, 32);
@@ -138,7 +141,7 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
   }
   if (!g.y) return;
   __syncthreads();
-  store_tile<BM, BN>(ct, static_cast<uint16_t*>(g.y), g.ldy, live - m0, n0, (int)g.ldy, [&](int r) { return m0 + r; });
+  store_tile<T, BM, BN>(ct, static_cast<T*>(g.y), g.ldy, live - m0, n0, (int)g.ldy, [&](int r) { return m0 + r; });
 }
 
 // dX (rows sent to their places in the batch) and dW in bf16 through LDS, or in fp32 as they are
@@ -146,8 +149,19 @@ template <bool X, int BM, int BN, int TM, int TN>
 __device__ __forceinline__ void epilogue_head(const GemmArgs& g, floatx16 (&acc)[TM][TN], uint16_t* ct, int m0, int n0, int wm0,
                                               int wn0, int rows) {
   const int lane = threadIdx.x & 63;
-  if (g.c_dtype == kF32) {                               // (dW only; partial sums of either return before)
-    if (g.beta) epilogue_store<TM, TN, float, true, false, true, false>(g, acc, m0, n0, wm0, wn0);
+  if (g.c_dtype == kF32) {                               // (partial sums of either return before)
+    if (X) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int place = m0 + wm0 + i * 32 + acc_row(e, lane);
+          if (place >= rows) continue;
+          float* const dst = static_cast<float*>(g.C) + (int64_t)g.head.row_map[place] * g.ldc + n0 + wn0 + (lane & 31);
+#pragma unroll
+          for (int j = 0; j < TN; ++j) if (n0 + wn0 + j * 32 + (lane & 31) < g.N) dst[j * 32] = acc[i][j][e];
+        }
+    } else if (g.beta) epilogue_store<TM, TN, float, true, false, true, false>(g, acc, m0, n0, wm0, wn0);
     else epilogue_store<TM, TN, float, true, false, false, false>(g, acc, m0, n0, wm0, wn0);
     return;
   }
@@ -167,8 +181,8 @@ __device__ __forceinline__ void epilogue_head(const GemmArgs& g, floatx16 (&acc)
       }
     }
   __syncthreads();
-  store_tile<BM, BN>(ct, static_cast<uint16_t*>(g.C), g.ldc, rows - m0, n0, g.N,
-                          [&](int r) { return X ? g.head.row_map[m0 + r] : m0 + r; });
+  store_tile<uint16_t, BM, BN>(ct, static_cast<uint16_t*>(g.C), g.ldc, rows - m0, n0, g.N,
+                                    [&](int r) { return X ? g.head.row_map[m0 + r] : m0 + r; });
 }
 
 }  // namespace rad

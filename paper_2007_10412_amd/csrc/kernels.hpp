@@ -48,10 +48,10 @@ enum EpiKind : int {
   kEpiFwd = 1,   // bias / rank-u addend / ReLU / bits / dense y / pack next store
   kEpiConv = 2,  // rows are positions (b,yx), columns channels: bias / ReLU / bits, NCHW output
   kEpiSplitK = 3, // plain store of the split's partial sums to C + split*M*N
-  // a layer under a loss over its classes (bf16, direct-to-LDS kernels; HeadArgs):
-  kEpiVocab = 4,  // what a softmax needs of the logits, per row and 128 columns, and the logits in 16 bits
-  kEpiHeadX = 5,  // dX: rows put in their places, bf16; or fp32 partial sums
-  kEpiHeadW = 6   // dW: bf16 or fp32 (+= if beta); or fp32 partial sums
+  // a layer under a loss over its classes (direct-to-LDS kernels; HeadArgs):
+  kEpiVocab = 4,  // what a softmax needs of the logits, per row and part of its columns, and the logits (bf16: in 16 bits)
+  kEpiHeadX = 5,  // dX: rows put in their places; or fp32 partial sums
+  kEpiHeadW = 6   // dW, in fp32 (+= if beta) or bf16; or fp32 partial sums
 };
 
 // The rows of the batch that have a target come first in a list; the products run over that list, whose length only the
@@ -60,12 +60,13 @@ struct HeadArgs {
   const int32_t* live;          // length of the list
   const int32_t* row_map;       // row of x and dX of every place in the list (kEpiVocab: of A; kEpiHeadX: of C)
   const void* whole; int rows;  // kEpiHeadW: what A is where the list has all `rows` rows
+  int tile;
   int n_load;                   // B: readable columns (a multiple of 8, >= N), M/N contiguous
   // kEpiVocab: logits z; c = log2(e) / T
   float c;
-  float* stats; int64_t stats_ld;   // [columns / 128][stats_ld] pairs (maximum m, sum of 2^((z - m) c))
+  float* stats; int64_t stats_ld;   // [columns / part][stats_ld] pairs (maximum m, sum of 2^((z - m) c))
   const int32_t* labels;        // [rows of the batch], or
-  const int32_t* index; const uint16_t* first; int k, first_ld;   // lists [rows][k], and how many of a row's entries lie before column 128 t
+  const int32_t* index; const uint16_t* first; int k, first_ld;   // lists [rows][k], and how many of a row's entries lie before part t
   float* target;                // [place][k]: the logits of the targets
 };
 
@@ -105,6 +106,9 @@ struct GemmArgs {
 
 // dtype: operand element type; returns hipErrorInvalidValue for combinations
 // without a kernel.  `name` (out, may be null) receives the kernel's label.
+// (head products: tile is the height of the tiles, 64, 128 or 256; the part of a row that kEpiVocab's statistics are for is
+// head_part(tile) columns wide)
+inline int head_part(int tile) { return tile == 256 ? 128 : 64; }
 hipError_t launch_gemm(int dtype, int a_kind, int b_kind, int epi, const GemmArgs& g,
                        hipStream_t st, const char** name);
 
@@ -288,14 +292,13 @@ hipError_t launch_teacher(const int32_t* index, const float* logit, int rows, in
 hipError_t launch_count_rows(const VocabTargets& t, int rows, int classes, float* inv_count, hipStream_t st);
 // loss = sum over rows of weight x row_loss, added in a fixed order
 hipError_t launch_weighted_loss(const VocabTargets& t, const float* row_loss, int rows, int classes, float* loss, hipStream_t st);
-// Losses and gradients of dense logits, rows z_ld apart: z, or (parts > 1) the sum of that many fp32 arrays part_stride
-// apart, plus bias (fp32 z only).  dz (nullable; rows dz_ld apart, zeros in columns classes .. dz_ld - 1) may be z itself.
-// stats: vocab_rows_stats_floats floats of scratch.
+// Losses and gradients of dense logits z [rows][classes].  dz (nullable) may be z itself.  stats: vocab_rows_stats_floats
+// floats of scratch.
 struct VocabRows {
-  const void* z; int z_dtype; int64_t z_ld; int parts; int64_t part_stride; const float* bias;
+  const void* z; int dtype;
   int rows, classes;
   VocabTargets t;
-  void* dz; int dz_dtype; int64_t dz_ld;
+  void* dz;
   float* row_loss;              // [rows]
   float* stats;
 };
@@ -304,31 +307,34 @@ hipError_t launch_vocab_rows(const VocabRows& a, hipStream_t st);
 // out (bf16) = beta out + in (fp32), n elements
 hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, hipStream_t st);
 
-// ---- the layer under such a loss (vocab_head.hip), around the products with HeadArgs
-// list [rows]: the rows that count, in order, then the others; *live: how many count
-hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, hipStream_t st);
-// first [rows][first_ld]: how many of a row's (sorted) entries lie before class 128 t, t = 0 .. parts
-hipError_t launch_list_parts(const int32_t* index, int rows, int k, int parts, uint16_t* first, int first_ld, hipStream_t st);
-// After the logits' product, for every place of the list: the row's loss, its maximum top, log2 sum 2^((z - top) c) and its
-// factor weight T.
-// For dW the rows of x side by side (xs, rows xs_ld apart, zeros past d_in), unless the list has them all.  Rows that do not
-// count: no loss, dX zero.
+// ---- the layer under such a loss, fp32 or bf16 (vocab_head.hip), around the products with HeadArgs
+// list [rows]: the rows that count, in order, then the others; *live: how many count; *inv_count (nullable): 1 / that
+hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, hipStream_t st);
+// first [rows][first_ld]: how many of a row's (sorted) entries lie before class `part` t, t = 0 .. parts
+hipError_t launch_list_parts(const int32_t* index, int rows, int k, int part, int parts, uint16_t* first, int first_ld, hipStream_t st);
+// After the logits' product, for every place of the list: the row's loss, its maximum top and what its exponentials
+// 2^((z - top) c) are multiplied by, factor = weight T / their sum.  For dW the rows of x side by side (xs, rows x_ld apart),
+// unless the list has them all.  Rows that do not count: no loss, dX zero.
 struct VocabFinish {
+  int dtype;
   const int32_t* list; const int32_t* live;
-  int rows, classes, parts;
+  int rows, classes, parts, part;   // `parts` parts of `part` (64 or 128) classes
   VocabTargets t;               // of the rows of x
   const float* stats; int64_t stats_ld;
   const float* target;          // [place][k]
   float* row_loss;              // [rows], in the batch's order
-  float* top; float* log2_sum; float* factor;   // [place]
-  uint16_t* z; int64_t z_ld;    // the logits' 16 bits, which launch_vocab_gradient turns into dz; null: forward only
+  float* loss;                  // the sum over these rows, or null: left to another call
+  float* top; float* factor;    // [place]
+  void* z; int64_t z_ld;        // the logits (bf16: their codes), which launch_vocab_gradient turns into dz; null: forward only
   const uint16_t* first; int first_ld;
-  const uint16_t* x; int64_t x_ld; int d_in; uint16_t* xs; int64_t xs_ld;   // xs null: no dW
-  uint16_t* dx;                 // rows d_in apart; null: no dX
+  const void* x; int64_t x_ld; int d_in; void* xs;   // rows of x of whole 16-byte vectors; xs null: no dW
+  void* dx;                     // rows d_in apart; null: no dX
 };
 hipError_t launch_vocab_finish(const VocabFinish& a, hipStream_t st);
-// dz = factor (2^((z - top) c - log2_sum) - p) in bf16, in the place of the codes; columns classes .. z_ld - 1 become zeros
+// dz = factor 2^((z - top) c) - weight T p in the layer's type, in the place of z; columns classes .. z_ld - 1 become zeros
 hipError_t launch_vocab_gradient(const VocabFinish& a, hipStream_t st);
+// whether one of those two writes *loss
+bool vocab_loss_inside(const VocabFinish& a);
 // out[map[i]] (rows out_ld apart; map null: i) (+)= sum of `splits` arrays' row i (rows in_ld apart, arrays stride apart),
 // i < min(rows, *live); live null: rows
 struct SplitSum {
@@ -339,10 +345,10 @@ struct SplitSum {
 hipError_t launch_split_sum(const SplitSum& a, hipStream_t st);
 // out [cols] (+)= sum over the first *live rows of g[i][c]; part: [kHeadColsumSplits][cols]
 constexpr int kHeadColsumSplits = 32;
-hipError_t launch_head_colsum(const uint16_t* g, int64_t g_ld, const int32_t* live, int cols, float* part,
+hipError_t launch_head_colsum(int dtype, const void* g, int64_t g_ld, const int32_t* live, int cols, float* part,
                               float* out, int beta, hipStream_t st);
-// bf16 rows of any width and alignment to rows out_ld apart (a multiple of 8), zeros past cols
-hipError_t launch_pad_rows(const uint16_t* in, int64_t rows, int cols, uint16_t* out, int64_t out_ld, hipStream_t st);
+// rows of any width and alignment to rows out_ld apart (whole 16-byte vectors), zeros past cols
+hipError_t launch_pad_rows(int dtype, const void* in, int64_t rows, int cols, void* out, int64_t out_ld, hipStream_t st);
 
 // Ceiling probes (ceilings.hip): kind 0 HBM read, 1 HBM copy, 2 / 3 bf16 MFMA 32x32x16 / 16x16x32 register loops,
 // 4 fp32 MFMA 32x32x2, 5 integer 32 x 32 -> 64 multiply-adds.  a: operands (probe_min_bytes at least), b: sink

@@ -1,7 +1,7 @@
-// What surrounds the three bf16 products of a layer under a loss over its classes.  Those products take the rows that have a
-// target only (row_list), so that a batch of which half are prompts costs half.  The logits' product leaves each logit in 16
-// bits and the softmax's statistics per 128 columns (epilogue_vocab); with a row's sum known, one pass over those codes leaves
-// dz in their place.
+// What surrounds the three products of a layer under a loss over its classes.  Those products take the rows that have a target
+// only (row_list), so that a batch of which half are prompts costs half.  The logits' product leaves the logits (bf16: each in
+// 16 bits) and the softmax's statistics per part of a row (epilogue_vocab); with a row's sum known, one pass leaves dz in
+// their place.
 #include <math.h>
 
 #include "head_epilogue.hpp"
@@ -15,7 +15,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // ------------------------------------------------------------------ the list of rows
 // One workgroup: a thread has 8 consecutive rows of 8192 at a time, and places them by a count over the threads before it.
 __global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows, int classes, int32_t* __restrict__ list,
-                                                        int32_t* __restrict__ live) {
+                                                        int32_t* __restrict__ live, float* __restrict__ inv_count) {
   __shared__ int s_n[16];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   int total = 0;                                        // rows that count, first of all
@@ -51,11 +51,14 @@ __global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows
     }
     before += all;
   }
-  if (threadIdx.x == 0) *live = total;
+  if (threadIdx.x == 0) {
+    *live = total;
+    if (inv_count) *inv_count = total > 0 ? 1.f / (float)total : 0.f;
+  }
 }
 
-// a wave per row: entry j (ascending, -1 at the end) is before class 128 t for every t past its part
-__global__ __launch_bounds__(256) void list_parts_kernel(const int32_t* __restrict__ index, int rows, int k, int parts,
+// a wave per row: entry j (ascending, -1 at the end) is before class part t for every t past its own part
+__global__ __launch_bounds__(256) void list_parts_kernel(const int32_t* __restrict__ index, int rows, int k, int part, int parts,
                                                          uint16_t* __restrict__ first, int first_ld) {
   const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= rows) return;
@@ -64,111 +67,162 @@ __global__ __launch_bounds__(256) void list_parts_kernel(const int32_t* __restri
     int lo = 0, hi = k;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if ((uint32_t)e[mid] < (uint32_t)t * 128u) lo = mid + 1; else hi = mid;     // (-1 lies after every class)
+      if ((uint32_t)e[mid] < (uint32_t)t * (uint32_t)part) lo = mid + 1; else hi = mid;     // (-1 lies after every class)
     }
     first[(int64_t)row * first_ld + t] = (uint16_t)lo;
   }
 }
 
 // ------------------------------------------------------------------ between the products
-// 16 places a workgroup.  Their parts' statistics lie side by side, so a load brings 16 rows' pairs of one part.
-constexpr int kFinishRows = 16, kFinishGroups = 64;
-__global__ __launch_bounds__(kFinishRows * kFinishGroups) void vocab_finish_kernel(VocabFinish a) {
-  __shared__ float s_m[kFinishGroups][kFinishRows], s_s[kFinishGroups][kFinishRows];
+// (maximum, sum of exponentials from it) of two parts; one with nothing in it adds its 0, or its NaN
+__device__ __forceinline__ void join(float& m, float& s, float m2, float s2, float c) {
+  if (m2 == -INFINITY) { s += s2; return; }
+  if (m == -INFINITY) { m = m2; s += s2; return; }
+  const float M = fmaxf(m, m2);
+  s = s * __builtin_amdgcn_exp2f((m - M) * c) + s2 * __builtin_amdgcn_exp2f((m2 - M) * c);
+  m = M;
+}
+
+// R = 2^shift places a workgroup, 1024 / R threads for the parts of each: the statistics of neighbouring places lie side by
+// side, so a load brings R rows' pairs of several parts.
+constexpr int kFinishThreads = 1024, kFinishRows = 16, kFinishAhead = 4;
+template <typename T>
+__global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinish a, int shift) {
+  __shared__ float s_m[16][kFinishRows], s_s[16][kFinishRows], s_d[16][kFinishRows];
   __shared__ int s_row[kFinishRows];
-  const int r = threadIdx.x % kFinishRows, grp = threadIdx.x / kFinishRows;
-  const int place0 = blockIdx.x * kFinishRows, place = place0 + r;
+  const int R = 1 << shift, r = (int)threadIdx.x & (R - 1), grp = (int)threadIdx.x >> shift, groups = kFinishThreads >> shift;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int place0 = (int)blockIdx.x << shift, place = place0 + r;
   const int live = *a.live;
   const VocabTargets& t = a.t;
   const float c = kLog2e / t.temperature;
   const bool counts = place < live;
+  const int row = place < a.rows ? a.list[place] : -1;
 
-  float m = -INFINITY, s = 0.f;
-  if (counts)
-    for (int p = grp; p < a.parts; p += kFinishGroups) {
-      const float2 v = *reinterpret_cast<const float2*>(a.stats + ((int64_t)p * a.stats_ld + place) * 2);
-      if (v.x == -INFINITY) { s += v.y; continue; }     // nothing there (or a NaN)
-      if (v.x > m) { s = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - v.x) * c); m = v.x; }
-      s += v.x == m ? v.y : v.y * __builtin_amdgcn_exp2f((v.x - m) * c);
-    }
-  s_m[grp][r] = m; s_s[grp][r] = s;
-  if (grp == 0) s_row[r] = place < a.rows ? a.list[place] : -1;
-  __syncthreads();
-  if (grp == 0) {
-    float M = -INFINITY, S = 0.f;
-    for (int q = 0; q < kFinishGroups; ++q) M = fmaxf(M, s_m[q][r]);
-    const float b = M == -INFINITY ? 0.f : M;
-    for (int q = 0; q < kFinishGroups; ++q) S += s_m[q][r] == -INFINITY ? s_s[q][r] : s_s[q][r] * __builtin_amdgcn_exp2f((s_m[q][r] - b) * c);
-    if (counts) {
-      const int row = s_row[r];
-      float dot = 0.f;
-      for (int j = 0; j < t.k; ++j) {
-        const float pj = t.labels ? 1.f : t.prob[(int64_t)row * t.k + j];
-        if (pj != 0.f) dot += pj * (a.target[(int64_t)place * t.k + j] - b);
+  float m = -INFINITY, s = 0.f, dot = 0.f, z0 = 0.f;
+  if (counts) {
+    for (int p = grp; p < a.parts; p += groups * kFinishAhead) {
+      float2 v[kFinishAhead];
+#pragma unroll
+      for (int q = 0; q < kFinishAhead; ++q) {
+        const int pq = p + q * groups;
+        v[q] = pq < a.parts ? *reinterpret_cast<const float2*>(a.stats + ((int64_t)pq * a.stats_ld + place) * 2) : make_float2(-INFINITY, 0.f);
       }
-      const float T = t.temperature;
-      if (a.row_loss) a.row_loss[row] = T * T * ((t.labels ? 0.f : t.entropy[row]) + (logf(S) - dot / T));
-      a.top[place] = b;
-      a.log2_sum[place] = log2f(S);
-      a.factor[place] = (t.weight ? t.weight[row] : *t.inv_count) * T;
-    } else if (place < a.rows && a.row_loss) {
-      a.row_loss[s_row[r]] = 0.f;
+#pragma unroll
+      for (int q = 0; q < kFinishAhead; ++q) join(m, s, v[q].x, v[q].y, c);
+    }
+    // sum_j p_j (z_j - z_0), z_0 the first target's logit
+    z0 = a.target[(int64_t)place * t.k];
+    if (z0 == -INFINITY) z0 = 0.f;
+    for (int j = grp; j < t.k; j += groups) {
+      const float pj = t.labels ? 1.f : t.prob[(int64_t)row * t.k + j];
+      if (pj != 0.f) dot += pj * (a.target[(int64_t)place * t.k + j] - z0);
     }
   }
+  for (int o = R; o < 64; o <<= 1) {
+    join(m, s, __shfl_xor(m, o), __shfl_xor(s, o), c);
+    dot += __shfl_xor(dot, o);
+  }
+  if (lane < R) { s_m[wave][r] = m; s_s[wave][r] = s; s_d[wave][r] = dot; }
+  __syncthreads();
+  if ((int)threadIdx.x < R) {
+    for (int w = 1; w < 16; ++w) { join(m, s, s_m[w][r], s_s[w][r], c); dot += s_d[w][r]; }
+    s_row[r] = row;
+    float part = 0.f;                                   // of the batch's loss
+    if (counts) {
+      const float T1 = t.temperature, top = m == -INFINITY ? 0.f : m;
+      const float weight = t.weight ? t.weight[row] : *t.inv_count;
+      const float loss = T1 * T1 * ((t.labels ? 0.f : t.entropy[row]) + (logf(s) + ((top - z0) - dot) / T1));
+      a.row_loss[row] = loss;
+      a.top[place] = top;
+      a.factor[place] = weight * T1 / s;
+      part = weight * loss;
+    } else if (place < a.rows) {
+      a.row_loss[row] = 0.f;
+    }
+    if (a.loss && gridDim.x == 1 && !a.z) {
+      for (int o = 1; o < R; o <<= 1) part += __shfl_xor(part, o);
+      if (r == 0) *a.loss = part;
+    }
+  }
+  __syncthreads();
   if (a.xs && live < a.rows) {
-    const int vecs = (int)(a.xs_ld / 8);
-    for (int q = threadIdx.x; q < kFinishRows * vecs; q += kFinishRows * kFinishGroups) {
+    const int64_t bytes = a.x_ld * (int64_t)sizeof(T);
+    const int vecs = (int)(bytes / 16);
+    for (int q = threadIdx.x; q < R * vecs; q += kFinishThreads) {
       const int rr = q / vecs, v = q - rr * vecs;
       if (place0 + rr < live)
-        *reinterpret_cast<u32x4*>(a.xs + (int64_t)(place0 + rr) * a.xs_ld + v * 8) =
-            *reinterpret_cast<const u32x4*>(a.x + (int64_t)s_row[rr] * a.x_ld + v * 8);
+        *reinterpret_cast<u32x4*>(static_cast<char*>(a.xs) + (place0 + rr) * bytes + v * 16) =
+            *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.x) + s_row[rr] * bytes + v * 16);
     }
   }
   if (a.dx)
-    for (int rr = 0; rr < kFinishRows; ++rr) {
+    for (int rr = 0; rr < R; ++rr) {
       if (place0 + rr < live || place0 + rr >= a.rows) continue;
-      uint16_t* const d = a.dx + (int64_t)s_row[rr] * a.d_in;
-      for (int v = threadIdx.x; v < a.d_in; v += kFinishRows * kFinishGroups) d[v] = 0;
+      T* const d = static_cast<T*>(a.dx) + (int64_t)s_row[rr] * a.d_in;
+      for (int v = threadIdx.x; v < a.d_in; v += kFinishThreads) d[v] = 0;
     }
 }
 
-// 16 rows x 2048 columns a workgroup: 16 lanes have a row's 128 columns of one part.  Reads and writes two bytes a logit, and is
-// bound by that.
-constexpr int kGradRows = 16, kGradParts = 16;
-__global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a) {
-  const int l = threadIdx.x & 15, place = (int)blockIdx.y * kGradRows + (threadIdx.x >> 4);
+// 16 rows x kSteps 16-byte vectors of 16 lanes a workgroup.  Reads and writes a logit, and is bound by that.  The last column of
+// workgroups (where there is a loss to sum) has no logits: its first one adds the rows' losses.
+constexpr int kGradRows = 16, kGradSteps = 16;
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int sum_column) {
+  constexpr int VPL = 16 / (int)sizeof(T), kCols = 16 * VPL * kGradSteps;
+  __shared__ float s_w[4];
   const int live = *a.live;
-  if ((int)blockIdx.y * kGradRows >= live) return;
   const VocabTargets& t = a.t;
-  const float c = kLog2e / t.temperature;
-  const int p0 = (int)blockIdx.x * kGradParts;
-  const bool counts = place < live;
-  uint16_t* const zr = a.z + (int64_t)place * a.z_ld;
-  float top = 0.f, log2_sum = 0.f, f = 0.f;
-  if (counts) {
-    top = a.top[place]; log2_sum = a.log2_sum[place]; f = a.factor[place];
-    u32x4 w[kGradParts];
-    float m[kGradParts];
+  if ((int)blockIdx.x == sum_column) {
+    if (blockIdx.y != 0) return;
+    float sum = 0.f;
+    for (int p = threadIdx.x; p < live; p += 256) {
+      const int row = a.list[p];
+      sum += (t.weight ? t.weight[row] : *t.inv_count) * a.row_loss[row];
+    }
 #pragma unroll
-    for (int q = 0; q < kGradParts; ++q) {
-      const int64_t col = (int64_t)(p0 + q) * 128 + l * 8;
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) *a.loss = (s_w[0] + s_w[1]) + (s_w[2] + s_w[3]);
+    return;
+  }
+  if ((int)blockIdx.y * kGradRows >= live) return;
+  const int l = threadIdx.x & 15, place = (int)blockIdx.y * kGradRows + (threadIdx.x >> 4);
+  const float c = kLog2e / t.temperature;
+  const int c0 = (int)blockIdx.x * kCols, shift = a.part == 64 ? 6 : 7;
+  const bool counts = place < live;
+  T* const zr = static_cast<T*>(a.z) + (int64_t)place * a.z_ld;
+  float top = 0.f, f = 0.f;
+  if (counts) {
+    top = a.top[place]; f = a.factor[place];
+    u32x4 w[kGradSteps];
+    float m[kGradSteps];
+#pragma unroll
+    for (int q = 0; q < kGradSteps; ++q) {
+      const int64_t col = (int64_t)c0 + (q * 16 + l) * VPL;
       w[q] = u32x4{0u, 0u, 0u, 0u};
       m[q] = -INFINITY;
       if (col < a.z_ld) w[q] = *reinterpret_cast<const u32x4*>(zr + col);
-      if (p0 + q < a.parts) m[q] = a.stats[((int64_t)(p0 + q) * a.stats_ld + place) * 2];
+      if (sizeof(T) == 2 && col < a.classes) m[q] = a.stats[((col >> shift) * a.stats_ld + place) * 2];
     }
 #pragma unroll
-    for (int q = 0; q < kGradParts; ++q) {
-      const int64_t col = (int64_t)(p0 + q) * 128 + l * 8;
+    for (int q = 0; q < kGradSteps; ++q) {
+      const int64_t col = (int64_t)c0 + (q * 16 + l) * VPL;
       if (col >= a.z_ld) continue;
-      const float off = (m[q] == -INFINITY ? 0.f : (m[q] - top) * c) - log2_sum;
       u32x4 o;
+      if constexpr (sizeof(T) == 2) {
+        const float off = m[q] == -INFINITY ? 0.f : (m[q] - top) * c;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t lo = w[q][e] & 0xFFFFu, hi = w[q][e] >> 16;
-        const float a0 = f * __builtin_amdgcn_exp2f(fmaf((float)lo, -kCodeRange / 65535.f, off));
-        const float a1 = f * __builtin_amdgcn_exp2f(fmaf((float)hi, -kCodeRange / 65535.f, off));
-        o[e] = bf16_pair(lo == kCodeLast ? 0.f * log2_sum : a0, hi == kCodeLast ? 0.f * log2_sum : a1);   // (a NaN row stays one)
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t lo = w[q][e] & 0xFFFFu, hi = w[q][e] >> 16;
+          const float e0 = __builtin_amdgcn_exp2f(fmaf((float)lo, -kCodeRange / 65535.f, off));
+          const float e1 = __builtin_amdgcn_exp2f(fmaf((float)hi, -kCodeRange / 65535.f, off));
+          o[e] = bf16_pair((lo == kCodeLast ? 0.f : e0) * f, (hi == kCodeLast ? 0.f : e1) * f);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(__builtin_amdgcn_exp2f((__uint_as_float(w[q][e]) - top) * c) * f);
       }
       *reinterpret_cast<u32x4*>(zr + col) = o;
     }
@@ -178,17 +232,19 @@ __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a) {
   if (!counts) return;
   const int row = a.list[place];
   int t0 = 0, t1 = 0;
-  if (t.labels) t1 = (t.labels[row] >> 7) >= p0 && (t.labels[row] >> 7) < p0 + kGradParts ? 1 : 0;
+  if (t.labels) t1 = (uint32_t)(t.labels[row] - c0) < (uint32_t)kCols ? 1 : 0;
   else {
     const uint16_t* const fr = a.first + (int64_t)row * a.first_ld;
-    t0 = fr[p0]; t1 = fr[min(p0 + kGradParts, a.parts)];
+    t0 = fr[c0 >> shift]; t1 = fr[min((c0 + kCols) >> shift, a.parts)];
   }
+  const float wt = (t.weight ? t.weight[row] : *t.inv_count) * t.temperature;
   for (int j = t0 + l; j < t1; j += 16) {
     const float pj = t.labels ? 1.f : t.prob[(int64_t)row * t.k + j];
     if (pj == 0.f) continue;
     const int col = t.labels ? t.labels[row] : t.index[(int64_t)row * t.k + j];
-    const float e = __builtin_amdgcn_exp2f((a.target[(int64_t)place * t.k + j] - top) * c - log2_sum);
-    zr[col] = (uint16_t)bf16_pair(f * (e - pj), 0.f);
+    const float g = __builtin_amdgcn_exp2f((a.target[(int64_t)place * t.k + j] - top) * c) * f - wt * pj;
+    if constexpr (sizeof(T) == 2) zr[col] = (uint16_t)bf16_pair(g, 0.f);
+    else zr[col] = g;
   }
 }
 
@@ -224,26 +280,31 @@ __global__ __launch_bounds__(256) void split_sum_kernel(SplitSum a) {
   for (int e = 0; e < 4; ++e) if (c + e < a.cols) o[e] = (uint16_t)bf16_pair(a.beta ? bf16_bits_to_f32(o[e]) + v[e] : v[e], 0.f);
 }
 
-// 512 columns and one range of rows a workgroup, its four waves every fourth row
-__global__ __launch_bounds__(256) void head_colsum_kernel(const uint16_t* __restrict__ g, int64_t g_ld, const int32_t* __restrict__ live,
+// 64 lanes' vectors of columns and one range of rows a workgroup, its four waves every fourth row
+template <typename T>
+__global__ __launch_bounds__(256) void head_colsum_kernel(const T* __restrict__ g, int64_t g_ld, const int32_t* __restrict__ live,
                                                           int cols, float* __restrict__ part) {
-  __shared__ float s_sum[4][512];
+  constexpr int VPL = 16 / (int)sizeof(T), W = 64 * VPL;
+  __shared__ float s_sum[4][W];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int n = *live, per = (n + kHeadColsumSplits - 1) / kHeadColsumSplits;
   const int r0 = (int)blockIdx.y * per, r1 = min(n, r0 + per);
-  const int c = (int)blockIdx.x * 512 + lane * 8;
-  float sum[8] = {};
+  const int c = (int)blockIdx.x * W + lane * VPL;
+  float sum[VPL] = {};
   if (c < g_ld)
     for (int r = r0 + w; r < r1; r += 4) {
       const u32x4 v = *reinterpret_cast<const u32x4*>(g + (int64_t)r * g_ld + c);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { sum[2 * e] += __uint_as_float(v[e] << 16); sum[2 * e + 1] += __uint_as_float(v[e] & 0xFFFF0000u); }
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 2) { sum[2 * e] += __uint_as_float(v[e] << 16); sum[2 * e + 1] += __uint_as_float(v[e] & 0xFFFF0000u); }
+        else sum[e] += __uint_as_float(v[e]);
+      }
     }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s_sum[w][lane * 8 + e] = sum[e];
+  for (int e = 0; e < VPL; ++e) s_sum[w][lane * VPL + e] = sum[e];
   __syncthreads();
-  for (int q = threadIdx.x; q < 512; q += 256) {
-    const int col = (int)blockIdx.x * 512 + q;
+  for (int q = threadIdx.x; q < W; q += 256) {
+    const int col = (int)blockIdx.x * W + q;
     if (col < cols) part[(int64_t)blockIdx.y * cols + col] = (s_sum[0][q] + s_sum[1][q]) + (s_sum[2][q] + s_sum[3][q]);
   }
 }
@@ -255,42 +316,56 @@ __global__ __launch_bounds__(256) void head_colsum_final_kernel(const float* __r
   out[c] = s;
 }
 
-__global__ __launch_bounds__(256) void pad_rows_kernel(const uint16_t* __restrict__ in, int64_t rows, int cols, uint16_t* __restrict__ out,
-                                                       int vecs) {
+template <typename T>
+__global__ __launch_bounds__(256) void pad_rows_kernel(const T* __restrict__ in, int64_t rows, int cols, T* __restrict__ out, int vecs) {
+  constexpr int VPL = 16 / (int)sizeof(T);
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= rows * vecs) return;
   const int64_t row = i / vecs;
-  const int c = (int)(i - row * vecs) * 8;
-  const uint16_t* const src = in + row * cols + c;
+  const int c = (int)(i - row * vecs) * VPL;
+  const T* const src = in + row * cols + c;
   u32x4 w = {0u, 0u, 0u, 0u};
-  if (c + 8 <= cols) __builtin_memcpy(&w, src, 16);
+  if (c + VPL <= cols) __builtin_memcpy(&w, src, 16);
   else {
-    uint16_t* we = reinterpret_cast<uint16_t*>(&w);
+    T* we = reinterpret_cast<T*>(&w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) if (c + e < cols) we[e] = src[e];
+    for (int e = 0; e < VPL; ++e) if (c + e < cols) we[e] = src[e];
   }
-  *reinterpret_cast<u32x4*>(out + i * 8) = w;
+  *reinterpret_cast<u32x4*>(out + i * VPL) = w;
 }
 
 }  // namespace
 
-hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, hipStream_t st) {
-  hipLaunchKernelGGL(row_list_kernel, dim3(1), dim3(1024), 0, st, t, rows, classes, list, live);
+hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, hipStream_t st) {
+  hipLaunchKernelGGL(row_list_kernel, dim3(1), dim3(1024), 0, st, t, rows, classes, list, live, inv_count);
   return hipGetLastError();
 }
-hipError_t launch_list_parts(const int32_t* index, int rows, int k, int parts, uint16_t* first, int first_ld, hipStream_t st) {
-  hipLaunchKernelGGL(list_parts_kernel, dim3((rows + 3) / 4), dim3(256), 0, st, index, rows, k, parts, first, first_ld);
+hipError_t launch_list_parts(const int32_t* index, int rows, int k, int part, int parts, uint16_t* first, int first_ld, hipStream_t st) {
+  hipLaunchKernelGGL(list_parts_kernel, dim3((rows + 3) / 4), dim3(256), 0, st, index, rows, k, part, parts, first, first_ld);
   return hipGetLastError();
 }
+// places of a finishing workgroup: up to 16, while there is a workgroup for every other CU
+static int finish_shift(int rows) {
+  int shift = 4;
+  while (shift > 0 && (rows >> shift) < 128) --shift;
+  return shift;
+}
+bool vocab_loss_inside(const VocabFinish& a) { return a.z || a.rows <= 1 << finish_shift(a.rows); }
 hipError_t launch_vocab_finish(const VocabFinish& a, hipStream_t st) {
-  hipLaunchKernelGGL(vocab_finish_kernel, dim3((a.rows + kFinishRows - 1) / kFinishRows), dim3(kFinishRows * kFinishGroups), 0, st, a);
+  const int shift = finish_shift(a.rows);
+  const dim3 grid((a.rows + (1 << shift) - 1) >> shift);
+  if (a.dtype == kBF16) hipLaunchKernelGGL(vocab_finish_kernel<uint16_t>, grid, dim3(kFinishThreads), 0, st, a, shift);
+  else hipLaunchKernelGGL(vocab_finish_kernel<float>, grid, dim3(kFinishThreads), 0, st, a, shift);
   return hipGetLastError();
 }
 hipError_t launch_vocab_gradient(const VocabFinish& a, hipStream_t st) {
-  const unsigned cols = (unsigned)((a.z_ld + 128 * kGradParts - 1) / (128 * kGradParts));
-  const unsigned rows = (unsigned)((a.rows + kGradRows - 1) / kGradRows);
+  const int kCols = kGradSteps * 16 * (a.dtype == kBF16 ? 8 : 4);
+  const unsigned cols = (unsigned)((a.z_ld + kCols - 1) / kCols), rows = (unsigned)((a.rows + kGradRows - 1) / kGradRows);
   if (rows > 65535) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(vocab_gradient_kernel, dim3(cols, rows), dim3(256), 0, st, a);
+  const dim3 grid(cols + (a.loss ? 1 : 0), rows);
+  const int sum_column = a.loss ? (int)cols : -1;
+  if (a.dtype == kBF16) hipLaunchKernelGGL(vocab_gradient_kernel<uint16_t>, grid, dim3(256), 0, st, a, sum_column);
+  else hipLaunchKernelGGL(vocab_gradient_kernel<float>, grid, dim3(256), 0, st, a, sum_column);
   return hipGetLastError();
 }
 hipError_t launch_split_sum(const SplitSum& a, hipStream_t st) {
@@ -298,15 +373,20 @@ hipError_t launch_split_sum(const SplitSum& a, hipStream_t st) {
   hipLaunchKernelGGL(split_sum_kernel, dim3((a.cols + 1023) / 1024, a.rows), dim3(256), 0, st, a);
   return hipGetLastError();
 }
-hipError_t launch_head_colsum(const uint16_t* g, int64_t g_ld, const int32_t* live, int cols, float* part,
-                              float* out, int beta, hipStream_t st) {
-  hipLaunchKernelGGL(head_colsum_kernel, dim3((cols + 511) / 512, kHeadColsumSplits), dim3(256), 0, st, g, g_ld, live, cols, part);
+hipError_t launch_head_colsum(int dtype, const void* g, int64_t g_ld, const int32_t* live, int cols, float* part, float* out,
+                              int beta, hipStream_t st) {
+  const int W = dtype == kBF16 ? 512 : 256;
+  const dim3 grid((cols + W - 1) / W, kHeadColsumSplits);
+  if (dtype == kBF16) hipLaunchKernelGGL(head_colsum_kernel<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)g, g_ld, live, cols, part);
+  else hipLaunchKernelGGL(head_colsum_kernel<float>, grid, dim3(256), 0, st, (const float*)g, g_ld, live, cols, part);
   hipLaunchKernelGGL(head_colsum_final_kernel, dim3((cols + 255) / 256), dim3(256), 0, st, part, cols, out, beta);
   return hipGetLastError();
 }
-hipError_t launch_pad_rows(const uint16_t* in, int64_t rows, int cols, uint16_t* out, int64_t out_ld, hipStream_t st) {
-  const int64_t n = rows * (out_ld / 8);
-  hipLaunchKernelGGL(pad_rows_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, in, rows, cols, out, (int)(out_ld / 8));
+hipError_t launch_pad_rows(int dtype, const void* in, int64_t rows, int cols, void* out, int64_t out_ld, hipStream_t st) {
+  const int vecs = (int)(out_ld / (dtype == kBF16 ? 8 : 4));
+  const dim3 grid((unsigned)((rows * vecs + 255) / 256));
+  if (dtype == kBF16) hipLaunchKernelGGL(pad_rows_kernel<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)in, rows, cols, (uint16_t*)out, vecs);
+  else hipLaunchKernelGGL(pad_rows_kernel<float>, grid, dim3(256), 0, st, (const float*)in, rows, cols, (float*)out, vecs);
   return hipGetLastError();
 }
 

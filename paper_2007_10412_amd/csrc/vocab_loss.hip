@@ -7,6 +7,7 @@
 // gradient; the targets' logits are read beside it, and the corrections written over the row's vectors after them.
 #include <math.h>
 
+#include "head_epilogue.hpp"
 #include "kernels.hpp"
 
 namespace rad {
@@ -16,8 +17,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 __device__ __forceinline__ float ld_elem(const float* p) { return *p; }
 __device__ __forceinline__ float ld_elem(const uint16_t* p) { return bf16_bits_to_f32(*p); }
-// (a NaN stays one: its mantissa's upper half would otherwise round into the infinity's pattern, or past it)
-__device__ __forceinline__ uint16_t to_bf16(float v) { return v != v ? (uint16_t)0x7FC0u : f32_to_bf16_bits(v); }
+__device__ __forceinline__ uint16_t to_bf16(float v) { uint16_t p[2]; put_pair(p, v, 0.f); return p[0]; }
 __device__ __forceinline__ void st_elem(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st_elem(uint16_t* p, float v) { *p = to_bf16(v); }
 __device__ __forceinline__ float wave_max(float v) {
@@ -187,16 +187,6 @@ template <typename T, int NT, int NV> struct RowPart {
     if constexpr (sizeof(T) == 4) return __uint_as_float(raw[i][q]);
     else return __uint_as_float(q & 1 ? raw[i][q >> 1] & 0xFFFF0000u : raw[i][q >> 1] << 16);
   }
-  // more addends of fp32 logits
-  __device__ __forceinline__ void add(const float* row, int v0, int lead, int classes) {
-    static_assert(sizeof(T) == 4, "fp32 logits");
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = col(v0, i, lead);
-#pragma unroll
-      for (int q = 0; q < VPL; ++q) if (c + q >= 0 && c + q < classes) raw[i][q] = __float_as_uint(__uint_as_float(raw[i][q]) + row[c + q]);
-    }
-  }
   // maximum and sum of exponentials of the whole wave
   __device__ __forceinline__ void stats(float c, float* m_out, float* s_out) const {
     float m = -INFINITY, s = 0.f;
@@ -215,32 +205,28 @@ template <typename T, int NT, int NV> struct RowPart {
   }
 };
 
-// stores vector i of a part: out columns [0, classes) take f(value), columns [classes, dz_ld) zeros
-template <typename O, int VPL, class F>
-__device__ __forceinline__ void store_vec(O* out, int c, int classes, int64_t width, bool aligned, F f) {
+// stores a vector of a part, f(q) in the q-th column
+template <typename T, class F>
+__device__ __forceinline__ void store_vec(T* out, int c, int classes, bool aligned, F f) {
+  constexpr int VPL = 16 / (int)sizeof(T);
   if (c >= 0 && c + VPL <= classes && aligned) {
-    constexpr int W = VPL * (int)sizeof(O) / 4;         // 8 bytes (fp32 in, bf16 out) or 16
-    uint32_t w[W];
+    u32x4 w;
 #pragma unroll
-    for (int q = 0; q < W; ++q) {
-      if constexpr (sizeof(O) == 4) w[q] = __float_as_uint(f(q));
-      else w[q] = (uint32_t)to_bf16(f(2 * q)) | ((uint32_t)to_bf16(f(2 * q + 1)) << 16);
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (sizeof(T) == 4) w[q] = __float_as_uint(f(q));
+      else w[q] = bf16_pair(f(2 * q), f(2 * q + 1));
     }
-    if constexpr (W == 4) *reinterpret_cast<u32x4*>(out + c) = u32x4{w[0], w[1], w[2], w[3]};
-    else *reinterpret_cast<u32x2*>(out + c) = u32x2{w[0], w[1]};
+    *reinterpret_cast<u32x4*>(out + c) = w;
     return;
   }
 #pragma unroll
-  for (int q = 0; q < VPL; ++q) {
-    if (c + q < 0 || c + q >= width) continue;
-    st_elem(out + c + q, c + q < classes ? f(q) : 0.f);
-  }
+  for (int q = 0; q < VPL; ++q) if (c + q >= 0 && c + q < classes) st_elem(out + c + q, f(q));
 }
 
 // SPLIT: the row's parts are dealt to gridDim.x workgroups.  PASS 0 leaves each part's maximum and sum in stats
 // [rows][parts][2] and, with part 0, the first target's logit z_0 and sum_j p_j (z_{i_j} - z_0) in dots [rows][2]; PASS 1 joins them, part by part in order, and writes.
 // Without SPLIT one workgroup has the whole row in its registers.
-template <typename T, typename O, int NT, int NV, bool SPLIT, int PASS>
+template <typename T, int NT, int NV, bool SPLIT, int PASS>
 __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __restrict__ dots) {
   typedef RowPart<T, NT, NV> Part;
   constexpr int VPL = Part::VPL, NW = NT / 64;
@@ -249,44 +235,32 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
   if (row >= a.rows) return;
   const int part = SPLIT ? blockIdx.x : 0, v0 = part * NT * NV;
   const VocabTargets& t = a.t;
-  const T* const z = static_cast<const T*>(a.z) + (int64_t)row * a.z_ld;
-  O* const dz = static_cast<O*>(a.dz) + (int64_t)row * a.dz_ld;
-  const int lead = Part::lead(z);
   const int classes = a.classes;
+  const T* const z = static_cast<const T*>(a.z) + (int64_t)row * classes;
+  T* const dz = static_cast<T*>(a.dz) + (int64_t)row * classes;
+  const int lead = Part::lead(z);
   const float c = kLog2e / t.temperature;
   const bool counts = row_counts(t, row, classes);
-  const bool out_aligned = (reinterpret_cast<uintptr_t>(dz - lead) & (VPL * sizeof(O) - 1)) == 0;
+  const bool out_aligned = (reinterpret_cast<uintptr_t>(dz - lead) & 15) == 0;
 
   if (!counts) {                                        // (the same for the whole workgroup)
     if (a.row_loss && part == 0 && threadIdx.x == 0 && !(SPLIT && PASS == 0)) a.row_loss[row] = 0.f;
     if (a.dz && !(SPLIT && PASS == 0)) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) store_vec<O, VPL>(dz, Part::col(v0, i, lead), classes, a.dz_ld, out_aligned, [](int) { return 0.f; });
+      for (int i = 0; i < NV; ++i) store_vec<T>(dz, Part::col(v0, i, lead), classes, out_aligned, [](int) { return 0.f; });
     }
     return;
   }
 
-  auto logit = [&](int i) {                             // one logit, for a target
-    float v = ld_elem(z + i);
-    if constexpr (sizeof(T) == 4) {
-      for (int q = 1; q < a.parts; ++q) v += reinterpret_cast<const float*>(z)[q * a.part_stride + i];
-      if (a.bias) v += a.bias[i];
-    }
-    return v;
-  };
   Part p;
   p.load(z, v0, lead, classes);
-  if constexpr (sizeof(T) == 4) {
-    for (int q = 1; q < a.parts; ++q) p.add(reinterpret_cast<const float*>(z) + q * a.part_stride, v0, lead, classes);
-    if (a.bias) p.add(a.bias, v0, lead, classes);
-  }
   // this thread's targets: all of them for the loss (one part of a row), those of this part for the gradient.  Their logits
   // are read here, ahead of any store: dz may be z.
   constexpr int KT = (kTeacherMax + NT - 1) / NT;
   const int c_lo = v0 * VPL - lead, c_hi = c_lo + NT * NV * VPL;
   float tz[KT], tp[KT]; int ti[KT];
   float dot = 0.f, z0 = 0.f;
-  if (part == 0 && !(SPLIT && PASS == 1)) { z0 = logit(target_index(t, row, 0)); if (z0 == -INFINITY) z0 = 0.f; }
+  if (part == 0 && !(SPLIT && PASS == 1)) { z0 = ld_elem(z + target_index(t, row, 0)); if (z0 == -INFINITY) z0 = 0.f; }
 #pragma unroll
   for (int q = 0; q < KT; ++q) {
     const int j = (int)threadIdx.x + q * NT;
@@ -297,7 +271,7 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
     if (i < 0 || pj == 0.f) continue;
     const bool mine = i >= c_lo && i < c_hi;
     if (!mine && (PASS == 1 || part != 0)) continue;
-    const float v = logit(i);
+    const float v = ld_elem(z + i);
     dot += pj * (v - z0);
     if (mine) { ti[q] = i; tz[q] = v; tp[q] = pj; }
   }
@@ -341,7 +315,7 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
   const float wt = row_weight(t, row) * t.temperature, f = wt / s;
 #pragma unroll
   for (int i = 0; i < NV; ++i)
-    store_vec<O, VPL>(dz, Part::col(v0, i, lead), classes, a.dz_ld, out_aligned, [&](int q) { return exp_from(p.at(i, q), b, c) * f; });
+    store_vec<T>(dz, Part::col(v0, i, lead), classes, out_aligned, [&](int q) { return exp_from(p.at(i, q), b, c) * f; });
   __threadfence_block();
   __syncthreads();                                      // the targets' elements are written again, after their vectors
 #pragma unroll
@@ -360,7 +334,7 @@ __global__ __launch_bounds__(256) void cast_add_kernel(const float* __restrict__
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (beta) { v[2 * q] += __uint_as_float(o[q] << 16); v[2 * q + 1] += __uint_as_float(o[q] & 0xFFFF0000u); }
-      r[q] = (uint32_t)to_bf16(v[2 * q]) | ((uint32_t)to_bf16(v[2 * q + 1]) << 16);
+      r[q] = bf16_pair(v[2 * q], v[2 * q + 1]);
     }
     *reinterpret_cast<u32x4*>(out + i) = r;
     return;
@@ -370,26 +344,24 @@ __global__ __launch_bounds__(256) void cast_add_kernel(const float* __restrict__
 
 constexpr int kPartThreads = 256, kPartVecs = 4;
 
-template <typename T, typename O, int NT, int NV>
+template <typename T, int NT, int NV>
 hipError_t rows_whole(const VocabRows& a, hipStream_t st) {
-  hipLaunchKernelGGL((vocab_rows_kernel<T, O, NT, NV, false, 1>), dim3(a.rows), dim3(NT), 0, st, a, (float*)nullptr);
+  hipLaunchKernelGGL((vocab_rows_kernel<T, NT, NV, false, 1>), dim3(a.rows), dim3(NT), 0, st, a, (float*)nullptr);
   return hipGetLastError();
 }
-template <typename T, typename O>
+template <typename T>
 hipError_t rows_any(const VocabRows& a, hipStream_t st) {
   constexpr int VPL = 16 / (int)sizeof(T);
-  // vectors of a row, the ones that it only begins or ends in and the padding of dz included
-  const int64_t cols = a.dz && a.dz_ld > a.classes ? a.dz_ld : a.classes;
-  const int64_t vecs = (cols + VPL - 1) / VPL + 1;
-  if (vecs <= 256 * 2) return rows_whole<T, O, 256, 2>(a, st);
-  if (a.rows >= 256 && vecs <= 512 * 4) return rows_whole<T, O, 512, 4>(a, st);
-  if (a.rows >= 256 && vecs <= 512 * 8) return rows_whole<T, O, 512, 8>(a, st);
-  if (a.rows >= 256 && vecs <= 1024 * 16) return rows_whole<T, O, 1024, 16>(a, st);
+  const int64_t vecs = ((int64_t)a.classes + VPL - 1) / VPL + 1;     // of a row, the ones that it only begins or ends in included
+  if (vecs <= 256 * 2) return rows_whole<T, 256, 2>(a, st);
+  if (a.rows >= 256 && vecs <= 512 * 4) return rows_whole<T, 512, 4>(a, st);
+  if (a.rows >= 256 && vecs <= 512 * 8) return rows_whole<T, 512, 8>(a, st);
+  if (a.rows >= 256 && vecs <= 1024 * 16) return rows_whole<T, 1024, 16>(a, st);
   const int64_t parts = (vecs + kPartThreads * kPartVecs - 1) / (kPartThreads * kPartVecs);
   float* const dots = a.stats + (int64_t)a.rows * parts * 2;
   const dim3 grid((unsigned)parts, (unsigned)(a.rows < 65535 ? a.rows : 65535), (unsigned)((a.rows + 65534) / 65535));
-  hipLaunchKernelGGL((vocab_rows_kernel<T, O, kPartThreads, kPartVecs, true, 0>), grid, dim3(kPartThreads), 0, st, a, dots);
-  hipLaunchKernelGGL((vocab_rows_kernel<T, O, kPartThreads, kPartVecs, true, 1>), grid, dim3(kPartThreads), 0, st, a, dots);
+  hipLaunchKernelGGL((vocab_rows_kernel<T, kPartThreads, kPartVecs, true, 0>), grid, dim3(kPartThreads), 0, st, a, dots);
+  hipLaunchKernelGGL((vocab_rows_kernel<T, kPartThreads, kPartVecs, true, 1>), grid, dim3(kPartThreads), 0, st, a, dots);
   return hipGetLastError();
 }
 
@@ -422,17 +394,13 @@ hipError_t launch_weighted_loss(const VocabTargets& t, const float* row_loss, in
 }
 
 int64_t vocab_rows_stats_floats(int rows, int classes) {
-  const int64_t parts = (classes / 4 + 2 + 64 + kPartThreads * kPartVecs) / (kPartThreads * kPartVecs) + 1;   // (fp32 vectors)
+  const int64_t parts = (classes / 4 + 2 + kPartThreads * kPartVecs) / (kPartThreads * kPartVecs) + 1;   // (fp32 vectors)
   return (int64_t)rows * (parts * 2 + 2);
 }
 
 hipError_t launch_vocab_rows(const VocabRows& a, hipStream_t st) {
   if (a.rows <= 0) return hipSuccess;
-  if (a.z_dtype == kBF16) {
-    if (a.parts > 1 || a.bias || a.dz_dtype != kBF16) return hipErrorInvalidValue;
-    return rows_any<uint16_t, uint16_t>(a, st);
-  }
-  return a.dz_dtype == kBF16 ? rows_any<float, uint16_t>(a, st) : rows_any<float, float>(a, st);
+  return a.dtype == kBF16 ? rows_any<uint16_t>(a, st) : rows_any<float>(a, st);
 }
 
 hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, hipStream_t st) {
