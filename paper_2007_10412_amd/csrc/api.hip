@@ -1488,10 +1488,11 @@ extern "C" rad_status rad_distill_ce(rad_ctx* c, const void* logits, const rad_t
   VocabRows a;
   std::memset(&a, 0, sizeof(a));
   float* losses = row_loss;
-  RAD_TRY(vocab_targets(c, nullptr, teacher, row_weight, (int)rows, (int)classes, true, &a.t, &losses));
   a.z = logits; a.dtype = dtype;
   a.rows = (int)rows; a.classes = (int)classes;
   a.dz = dlogits;
+  a.t.weight = row_weight;
+  RAD_TRY(vocab_targets(c, nullptr, teacher, row_weight, (int)rows, (int)classes, a.dz && !vocab_rows_count(a), &a.t, &losses));
   a.row_loss = losses;
   RAD_TRY(vocab_rows(c, a));
   return vocab_loss_sum(c, a.t, losses, (int)rows, (int)classes, loss);

@@ -303,6 +303,8 @@ struct VocabRows {
   float* stats;
 };
 int64_t vocab_rows_stats_floats(int rows, int classes);
+// whether the kernel counts the rows that count itself, and *t.inv_count is not read
+bool vocab_rows_count(const VocabRows& a);
 hipError_t launch_vocab_rows(const VocabRows& a, hipStream_t st);
 // out (bf16) = beta out + in (fp32), n elements
 hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, hipStream_t st);

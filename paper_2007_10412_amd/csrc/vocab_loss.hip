@@ -53,13 +53,18 @@ __device__ __forceinline__ float rebased(float s, float m, float b, float c) { r
 __device__ __forceinline__ bool row_counts(const VocabTargets& t, int row, int classes) {
   return t.labels ? (uint32_t)t.labels[row] < (uint32_t)classes : t.counts[row] != 0;
 }
-__device__ __forceinline__ float row_weight(const VocabTargets& t, int row) { return t.weight ? t.weight[row] : *t.inv_count; }
 // entry j of a row that counts
 __device__ __forceinline__ int target_index(const VocabTargets& t, int row, int j) {
   return t.labels ? t.labels[row] : t.index[(int64_t)row * t.k + j];
 }
 __device__ __forceinline__ float target_prob(const VocabTargets& t, int row, int j) {
   return t.labels ? 1.f : t.prob[(int64_t)row * t.k + j];
+}
+
+// a wave's LDS writes before, its reads after (LDS serves a wave in order: only the compiler has to keep it)
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
 // ------------------------------------------------------------------ targets
@@ -75,7 +80,7 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int32_t* __restrict_
   constexpr uint64_t kNone = ~0ull;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int row = blockIdx.x * 4 + w;
-  const bool live = row < rows;                         // (all waves stay for the barriers)
+  const bool live = row < rows;
   uint64_t* const key = s_key[w];
   float* const p = s_p[w];
   const int64_t at = (int64_t)(live ? row : 0) * k;
@@ -111,7 +116,7 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int32_t* __restrict_
     p[j] = pj;
   }
   h = wave_sum(h);
-  __syncthreads();
+  wave_lds_fence();
   for (int size = 2; size <= P; size <<= 1)
     for (int d = size >> 1; d > 0; d >>= 1) {
       for (int q = lane; q < P / 2; q += 64) {
@@ -120,7 +125,7 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int32_t* __restrict_
         const uint64_t ka = key[a], kb = key[b];
         if ((ka > kb) == up) { key[a] = kb; key[b] = ka; }
       }
-      __syncthreads();
+      wave_lds_fence();
     }
   if (!live) return;
   const bool some = key[0] != kNone;
@@ -149,88 +154,120 @@ __global__ __launch_bounds__(1024) void count_rows_kernel(VocabTargets t, int ro
   *inv_count = all > 0 ? 1.f / (float)all : 0.f;
 }
 
-// thread i adds rows i, i + 1024, ...; then a fixed tree
+// thread i adds rows i, i + 1024, ...; then a fixed tree.  Without weights: the mean over the rows that count.
 __global__ __launch_bounds__(1024) void weighted_loss_kernel(VocabTargets t, const float* __restrict__ row_loss, int rows,
                                                              int classes, float* __restrict__ loss) {
   __shared__ float s_w[16];
-  float acc = 0.f;
+  float acc = 0.f, n = 0.f;
   for (int r = threadIdx.x; r < rows; r += 1024)
-    if (row_counts(t, r, classes)) acc += row_weight(t, r) * row_loss[r];
+    if (row_counts(t, r, classes)) { acc += (t.weight ? t.weight[r] : 1.f) * row_loss[r]; n += 1.f; }
   acc = block_sum<1024>(acc, s_w);
-  if (threadIdx.x == 0) *loss = acc;
+  n = block_sum<1024>(n, s_w);
+  if (threadIdx.x == 0) *loss = t.weight ? acc : n > 0.f ? acc / n : 0.f;
 }
 
 // ------------------------------------------------------------------ dense rows
-// A workgroup's part of a row: vectors v0 .. v0 + NT NV - 1 of 16 bytes, counted from the 16-byte boundary at or below the
-// row's first element (rows of odd widths start anywhere).  A vector that the row does not fill is taken element by element.
+// A workgroup's part of a row: vectors v0 .. v0 + NT NV - 1 of 16 bytes, counted from the row's first 16-byte boundary (rows of
+// odd widths start anywhere; 4096 x 32001 bf16 with vectors from the row's start: 132 us, of which unaligned stores are 20).
+// The up to VPL - 1 elements before it, and those that the last vector lacks, are single ones, one to a thread of the first part
+// and of the part that the next vector would belong to.
 template <typename T, int NT, int NV> struct RowPart {
   static constexpr int VPL = 16 / (int)sizeof(T);
+  // Parts of up to 64 values a lane keep their exponentials (from the wave's maximum), of which the gradient is a multiple;
+  // longer ones their packed logits, and take the exponentials again.  4096 x 32000 bf16 (64 values): 105 us, 120 the other way.
+  static constexpr bool kKeep = NV * VPL <= 64;
   u32x4 raw[NV];
-  static __device__ __forceinline__ int lead(const T* row) { return (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)); }
-  static __device__ __forceinline__ int col(int v0, int i, int lead) { return (v0 + i * NT + (int)threadIdx.x) * VPL - lead; }
+  float e[kKeep ? NV * VPL : 1];
+  float single; int single_col;                         // -1: none
+  static __device__ __forceinline__ int head(const T* row) {
+    return (int)((16u - ((uint32_t)reinterpret_cast<uintptr_t>(row) & 15u)) & 15u) / (int)sizeof(T);
+  }
+  static __device__ __forceinline__ int col(int v0, int i, int head) { return head + (v0 + i * NT + (int)threadIdx.x) * VPL; }
   static constexpr uint32_t kEmpty = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;     // -inf
-  __device__ __forceinline__ void load(const T* row, int v0, int lead, int classes) {
+  __device__ __forceinline__ void load(const T* row, int v0, int head, int classes) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = col(v0, i, lead);
-      if (c >= 0 && c + VPL <= classes) {
-        raw[i] = *reinterpret_cast<const u32x4*>(row + c);
-      } else {
-        raw[i] = u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
-        T* e = reinterpret_cast<T*>(&raw[i]);
-#pragma unroll
-        for (int q = 0; q < VPL; ++q) if (c + q >= 0 && c + q < classes) e[q] = row[c + q];
-      }
+      const int c = col(v0, i, head);
+      raw[i] = u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
+      if (c + VPL <= classes) raw[i] = *reinterpret_cast<const u32x4*>(row + c);
     }
+    const int whole = max(0, classes - head) / VPL, t = (int)threadIdx.x;
+    single_col = -1;
+    if (t < VPL) { if (v0 == 0 && t < head && t < classes) single_col = t; }
+    else if (t < 2 * VPL && whole >= v0 && whole < v0 + NT * NV) {
+      const int c = head + whole * VPL + t - VPL;
+      if (c < classes) single_col = c;
+    }
+    single = single_col >= 0 ? ld_elem(row + single_col) : -INFINITY;
   }
   __device__ __forceinline__ float at(int i, int q) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(raw[i][q]);
     else return __uint_as_float(q & 1 ? raw[i][q >> 1] & 0xFFFF0000u : raw[i][q >> 1] << 16);
   }
-  // maximum and sum of exponentials of the whole wave
-  __device__ __forceinline__ void stats(float c, float* m_out, float* s_out) const {
-    float m = -INFINITY, s = 0.f;
+  // The compiler forgets what it has unpacked of the vectors: each pass over them unpacks again (an instruction a value),
+  // where it would otherwise keep two registers for every packed one.
+  __device__ __forceinline__ void forget() {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(raw[i][0]), "+v"(raw[i][1]), "+v"(raw[i][2]), "+v"(raw[i][3]));
+  }
+  // maximum and sum of exponentials of the whole wave
+  __device__ __forceinline__ void stats(float c, float* m_out, float* s_out) {
+    float m = single;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
 #pragma unroll
       for (int q = 0; q < VPL; ++q) m = fmaxf(m, at(i, q));
+      if (i % 2) __builtin_amdgcn_sched_barrier(0);     // (the vectors stay packed: few of their values at a time)
+    }
     m = wave_max(m);
+    if (sizeof(T) == 2 && !kKeep) forget();
     const float b = exp_base(m);
+    float s = exp_from(single, b, c);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
 #pragma unroll
-      for (int q = 0; q < VPL; ++q) s += exp_from(at(i, q), b, c);
+      for (int q = 0; q < VPL; ++q) {
+        const float v = exp_from(at(i, q), b, c);
+        if (kKeep) e[kKeep ? i * VPL + q : 0] = v;
+        s += v;
+      }
+      if (i % 2) __builtin_amdgcn_sched_barrier(0);
+    }
     *m_out = m;
     *s_out = wave_sum(s);
   }
 };
 
-// stores a vector of a part, f(q) in the q-th column
-template <typename T, class F>
-__device__ __forceinline__ void store_vec(T* out, int c, int classes, bool aligned, F f) {
+// stores a part of a row: f(i, q) is element q of vector i, single what the single element becomes
+template <typename T, int NT, int NV, class F>
+__device__ __forceinline__ void store_part(T* out, const RowPart<T, NT, NV>& p, int v0, int head, int classes, float single, F f) {
   constexpr int VPL = 16 / (int)sizeof(T);
-  if (c >= 0 && c + VPL <= classes && aligned) {
-    u32x4 w;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if constexpr (sizeof(T) == 4) w[q] = __float_as_uint(f(q));
-      else w[q] = bf16_pair(f(2 * q), f(2 * q + 1));
+  for (int i = 0; i < NV; ++i) {
+    const int c = RowPart<T, NT, NV>::col(v0, i, head);
+    if (c + VPL <= classes) {
+      u32x4 w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if constexpr (sizeof(T) == 4) w[q] = __float_as_uint(f(i, q));
+        else w[q] = bf16_pair(f(i, 2 * q), f(i, 2 * q + 1));
+      }
+      __builtin_memcpy(out + c, &w, 16);                // (dz may be aligned otherwise)
     }
-    *reinterpret_cast<u32x4*>(out + c) = w;
-    return;
+    if (i % 2) __builtin_amdgcn_sched_barrier(0);
   }
-#pragma unroll
-  for (int q = 0; q < VPL; ++q) if (c + q >= 0 && c + q < classes) st_elem(out + c + q, f(q));
+  if (p.single_col >= 0) st_elem(out + p.single_col, single);
 }
 
 // SPLIT: the row's parts are dealt to gridDim.x workgroups.  PASS 0 leaves each part's maximum and sum in stats
 // [rows][parts][2] and, with part 0, the first target's logit z_0 and sum_j p_j (z_{i_j} - z_0) in dots [rows][2]; PASS 1 joins them, part by part in order, and writes.
 // Without SPLIT one workgroup has the whole row in its registers.
+// count: the rows that count are counted here (by every workgroup for itself).
 template <typename T, int NT, int NV, bool SPLIT, int PASS>
-__global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __restrict__ dots) {
+__global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __restrict__ dots, int count) {
   typedef RowPart<T, NT, NV> Part;
   constexpr int VPL = Part::VPL, NW = NT / 64;
-  __shared__ float s_m[NW], s_s[NW], s_w[NW];
+  __shared__ float s_m[NW], s_s[NW], s_w[NW], s_tz[kTeacherMax];
   const int row = SPLIT ? blockIdx.y + blockIdx.z * 65535 : blockIdx.x;
   if (row >= a.rows) return;
   const int part = SPLIT ? blockIdx.x : 0, v0 = part * NT * NV;
@@ -238,47 +275,42 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
   const int classes = a.classes;
   const T* const z = static_cast<const T*>(a.z) + (int64_t)row * classes;
   T* const dz = static_cast<T*>(a.dz) + (int64_t)row * classes;
-  const int lead = Part::lead(z);
   const float c = kLog2e / t.temperature;
   const bool counts = row_counts(t, row, classes);
-  const bool out_aligned = (reinterpret_cast<uintptr_t>(dz - lead) & 15) == 0;
+  const int head = Part::head(z), c_lo = part == 0 ? 0 : head + v0 * VPL, c_hi = min(classes, head + (v0 + NT * NV) * VPL);
 
   if (!counts) {                                        // (the same for the whole workgroup)
     if (a.row_loss && part == 0 && threadIdx.x == 0 && !(SPLIT && PASS == 0)) a.row_loss[row] = 0.f;
-    if (a.dz && !(SPLIT && PASS == 0)) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) store_vec<T>(dz, Part::col(v0, i, lead), classes, out_aligned, [](int) { return 0.f; });
-    }
+    if (a.dz && !(SPLIT && PASS == 0))
+      for (int q = c_lo + (int)threadIdx.x; q < c_hi; q += NT) st_elem(dz + q, 0.f);
     return;
   }
 
   Part p;
-  p.load(z, v0, lead, classes);
-  // this thread's targets: all of them for the loss (one part of a row), those of this part for the gradient.  Their logits
-  // are read here, ahead of any store: dz may be z.
-  constexpr int KT = (kTeacherMax + NT - 1) / NT;
-  const int c_lo = v0 * VPL - lead, c_hi = c_lo + NT * NV * VPL;
-  float tz[KT], tp[KT]; int ti[KT];
+  p.load(z, v0, head, classes);
+  float inv_count = 0.f;
+  if (count) {
+    float n = 0.f;
+    for (int q = threadIdx.x; q < a.rows; q += NT) n += row_counts(t, q, classes) ? 1.f : 0.f;
+    inv_count = 1.f / block_sum<NT>(n, s_w);            // (this row counts)
+  }
+  // The targets' logits: all of them for the loss (one part of a row), those of this part for the gradient.  They are read
+  // here, ahead of any store: dz may be z.
   float dot = 0.f, z0 = 0.f;
   if (part == 0 && !(SPLIT && PASS == 1)) { z0 = ld_elem(z + target_index(t, row, 0)); if (z0 == -INFINITY) z0 = 0.f; }
-#pragma unroll
-  for (int q = 0; q < KT; ++q) {
-    const int j = (int)threadIdx.x + q * NT;
-    ti[q] = -1; tz[q] = tp[q] = 0.f;
-    if (j >= t.k) continue;
+  for (int j = threadIdx.x; j < t.k; j += NT) {
     const int i = target_index(t, row, j);
     const float pj = target_prob(t, row, j);
-    if (i < 0 || pj == 0.f) continue;
     const bool mine = i >= c_lo && i < c_hi;
-    if (!mine && (PASS == 1 || part != 0)) continue;
+    if (i < 0 || pj == 0.f || (!mine && (PASS == 1 && SPLIT ? true : part != 0))) continue;
     const float v = ld_elem(z + i);
     dot += pj * (v - z0);
-    if (mine) { ti[q] = i; tz[q] = v; tp[q] = pj; }
+    s_tz[j] = v;
   }
 
-  float m = -INFINITY, s = 0.f;
+  float m = -INFINITY, s = 0.f, wm = -INFINITY;
   if (!SPLIT || PASS == 0) {
-    float wm, ws;
+    float ws;
     p.stats(c, &wm, &ws);
     if ((threadIdx.x & 63) == 0) { s_m[threadIdx.x >> 6] = wm; s_s[threadIdx.x >> 6] = ws; }
     __syncthreads();
@@ -312,15 +344,23 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
     a.row_loss[row] = T1 * T1 * ((t.labels ? 0.f : t.entropy[row]) + (logf(s) + ((b - z0) - dot) / T1));
   }
   if (!a.dz) return;
-  const float wt = row_weight(t, row) * t.temperature, f = wt / s;
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-    store_vec<T>(dz, Part::col(v0, i, lead), classes, out_aligned, [&](int q) { return exp_from(p.at(i, q), b, c) * f; });
+  const float weight = t.weight ? t.weight[row] : count ? inv_count : *t.inv_count;
+  const float wt = weight * t.temperature, f = wt / s;
+  const float single = exp_from(p.single, b, c) * f;
+  if constexpr (Part::kKeep && !SPLIT) {
+    const float fw = wm == -INFINITY ? f : f * exp_from(wm, b, c);
+    store_part<T, NT, NV>(dz, p, v0, head, classes, single, [&](int i, int q) { return p.e[i * VPL + q] * fw; });
+  } else {
+    if (sizeof(T) == 2) p.forget();
+    store_part<T, NT, NV>(dz, p, v0, head, classes, single, [&](int i, int q) { return exp_from(p.at(i, q), b, c) * f; });
+  }
   __threadfence_block();
   __syncthreads();                                      // the targets' elements are written again, after their vectors
-#pragma unroll
-  for (int q = 0; q < KT; ++q)
-    if (ti[q] >= 0) st_elem(dz + ti[q], exp_from(tz[q], b, c) * f - wt * tp[q]);
+  for (int j = threadIdx.x; j < t.k; j += NT) {
+    const int i = target_index(t, row, j);
+    const float pj = target_prob(t, row, j);
+    if (i >= c_lo && i < c_hi && pj != 0.f) st_elem(dz + i, exp_from(s_tz[j], b, c) * f - wt * pj);
+  }
 }
 
 __global__ __launch_bounds__(256) void cast_add_kernel(const float* __restrict__ in, uint16_t* __restrict__ out, int64_t n, int beta) {
@@ -344,24 +384,27 @@ __global__ __launch_bounds__(256) void cast_add_kernel(const float* __restrict__
 
 constexpr int kPartThreads = 256, kPartVecs = 4;
 
+
 template <typename T, int NT, int NV>
 hipError_t rows_whole(const VocabRows& a, hipStream_t st) {
-  hipLaunchKernelGGL((vocab_rows_kernel<T, NT, NV, false, 1>), dim3(a.rows), dim3(NT), 0, st, a, (float*)nullptr);
+  hipLaunchKernelGGL((vocab_rows_kernel<T, NT, NV, false, 1>), dim3(a.rows), dim3(NT), 0, st, a, (float*)nullptr, vocab_rows_count(a) ? 1 : 0);
   return hipGetLastError();
 }
 template <typename T>
 hipError_t rows_any(const VocabRows& a, hipStream_t st) {
   constexpr int VPL = 16 / (int)sizeof(T);
-  const int64_t vecs = ((int64_t)a.classes + VPL - 1) / VPL + 1;     // of a row, the ones that it only begins or ends in included
-  if (vecs <= 256 * 2) return rows_whole<T, 256, 2>(a, st);
-  if (a.rows >= 256 && vecs <= 512 * 4) return rows_whole<T, 512, 4>(a, st);
-  if (a.rows >= 256 && vecs <= 512 * 8) return rows_whole<T, 512, 8>(a, st);
-  if (a.rows >= 256 && vecs <= 1024 * 16) return rows_whole<T, 1024, 16>(a, st);
+  const int64_t vecs = (int64_t)a.classes / VPL + 1;                  // (one for the single elements at the end)
+  if (vecs <= 64 * 4) return rows_whole<T, 64, 4>(a, st);
+  if (vecs <= 128 * 4) return rows_whole<T, 128, 4>(a, st);
+  if (vecs <= 256 * 4) return rows_whole<T, 256, 4>(a, st);
+  if (vecs <= 256 * 8) return rows_whole<T, 256, 8>(a, st);
+  if (vecs <= 512 * 8) return rows_whole<T, 512, 8>(a, st);
+  if (vecs <= 512 * 16) return rows_whole<T, 512, 16>(a, st);
   const int64_t parts = (vecs + kPartThreads * kPartVecs - 1) / (kPartThreads * kPartVecs);
   float* const dots = a.stats + (int64_t)a.rows * parts * 2;
   const dim3 grid((unsigned)parts, (unsigned)(a.rows < 65535 ? a.rows : 65535), (unsigned)((a.rows + 65534) / 65535));
-  hipLaunchKernelGGL((vocab_rows_kernel<T, kPartThreads, kPartVecs, true, 0>), grid, dim3(kPartThreads), 0, st, a, dots);
-  hipLaunchKernelGGL((vocab_rows_kernel<T, kPartThreads, kPartVecs, true, 1>), grid, dim3(kPartThreads), 0, st, a, dots);
+  hipLaunchKernelGGL((vocab_rows_kernel<T, kPartThreads, kPartVecs, true, 0>), grid, dim3(kPartThreads), 0, st, a, dots, 0);
+  hipLaunchKernelGGL((vocab_rows_kernel<T, kPartThreads, kPartVecs, true, 1>), grid, dim3(kPartThreads), 0, st, a, dots, vocab_rows_count(a) ? 1 : 0);
   return hipGetLastError();
 }
 
@@ -375,10 +418,13 @@ hipError_t teacher_of(const int32_t* index, const float* logit, int rows, int k,
 
 }  // namespace
 
+bool vocab_rows_count(const VocabRows& a) { return a.dz && !a.t.weight && a.rows <= 2048; }
+
 hipError_t launch_teacher(const int32_t* index, const float* logit, int rows, int k, int classes, float temperature,
                           int32_t* index_out, float* prob, float* entropy, int32_t* counts, hipStream_t st) {
   if (k < 1 || k > kTeacherMax) return hipErrorInvalidValue;
   if (k <= 64) return teacher_of<64>(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, st);
+  if (k <= 128) return teacher_of<128>(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, st);
   if (k <= 256) return teacher_of<256>(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, st);
   return teacher_of<1024>(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, st);
 }
