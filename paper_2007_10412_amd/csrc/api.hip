@@ -1519,7 +1519,7 @@ struct HeadPlan { int tile, k_split, splits; };
 static HeadPlan head_plan(int dtype, int epi, int64_t M, int64_t N, int64_t K, bool may_split) {
   struct Kind { int dtype, tile, cols; double fill_us, slice_us, alone_us, end_us; };
   static const Kind kinds[] = {{kBF16, 256, 256, 3.0, 1.60, 1.00, 13.0}, {kBF16, 128, 128, 4.5, 0.58, 0.55, 2.5}, {kBF16, 64, 128, 4.5, 0.41, 0.40, 2.0},
-                               {kF32, 128, 128, 4.5, 1.90, 1.60, 2.5}, {kF32, 64, 128, 4.5, 1.05, 0.90, 2.0}};
+                               {kF32, 128, 128, 6.0, 1.98, 2.00, 2.5}, {kF32, 64, 128, 6.0, 1.04, 1.15, 2.0}};
   const int bk = dtype == kBF16 ? 64 : 32;
   HeadPlan best{128, 0, 1};
   double best_us = 1e30;
@@ -1527,13 +1527,13 @@ static HeadPlan head_plan(int dtype, int epi, int64_t M, int64_t N, int64_t K, b
     if (k.dtype != dtype || (k.tile == 64 && epi == kEpiHeadW)) continue;
     const double end_us = k.end_us + (k.tile == 256 && epi == kEpiVocab ? 7.0 : 0.0);
     const int64_t tiles = ((M + k.tile - 1) / k.tile) * ((N + k.cols - 1) / k.cols);
-    for (int s = 1; s <= 16 && (s == 1 || (may_split && K / s >= 128)); ++s) {
+    for (int s = 1; s <= 64 && (s == 1 || (may_split && K / s >= 128)); ++s) {
       const int64_t k_split = ((K + s - 1) / s + 63) / 64 * 64;
       const int splits = (int)((K + k_split - 1) / k_split);
       const double each = (double)((tiles * splits + 255) / 256), full = std::min(1.0, (double)(tiles * splits) / 256.0);
       const double slices = (double)((s > 1 ? k_split : K) + bk - 1) / bk;
       const double us = k.fill_us + each * (slices * (k.alone_us + full * (k.slice_us - k.alone_us)) + end_us) +
-                        (splits > 1 ? (double)M * N * (8.0 * splits + 2.0) / 4e6 + 4.0 : 0.0);
+                        (splits > 1 ? (double)M * N * (8.0 * splits + 2.0) / 4e6 + 5.0 : 0.0);
       if (us < best_us) { best_us = us; best = {k.tile, splits > 1 ? (int)k_split : 0, splits}; }
     }
   }
@@ -1597,8 +1597,8 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   RAD_TRY(head_padded(c, WS_HEADW, dtype, h.W, d_in, d_out, vp8, &W));
   RAD_TRY(head_padded(c, WS_HEADX, dtype, h.x, rows, d_in, dp, &x));
 
-  const HeadPlan fwd = head_plan(dtype, kEpiVocab, piece, d_out, d_in, false);
-  const int part = head_part(fwd.tile), parts = (d_out + part - 1) / part;
+  const HeadPlan fwd = head_plan(dtype, kEpiVocab, piece, d_out, d_in, true);
+  const int part = fwd.splits > 1 ? 64 : head_part(fwd.tile), parts = (d_out + part - 1) / part;
   const int first_ld = parts + 1;
   const size_t first_bytes = t.labels ? 0 : ((size_t)rows * first_ld * 2 + 255) / 256 * 256;
   char* ws = nullptr;
@@ -1639,7 +1639,15 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     a.stats = stats; a.stats_ld = piece;
     a.labels = tp.labels; a.index = tp.index; a.first = t.labels ? nullptr : first + r0 * first_ld; a.k = t.k; a.first_ld = first_ld;
     a.target = target;
-    RAD_TRY(head_product(c, dtype, kEpiVocab, fwd, g, SplitSum{}));
+    if (fwd.splits > 1) {
+      g.k_split = fwd.k_split; g.k_splits = fwd.splits;
+      g.ldc = vp;
+      g.split_stride = (int64_t)n * vp;
+      RAD_TRY(ws_get(c, WS_SPLITK, (size_t)fwd.splits * g.split_stride * 4, &g.C));
+    }
+    a.tile = fwd.tile;
+    RAD_TRY(run_gemm_call(c, dtype, kOpK, kOpMN, kEpiVocab, g));
+    if (fwd.splits > 1) HIP_TRY(c, timed(c, "vocab_join", [&](const char**) { return launch_vocab_join(dtype, g, c->stream); }));
     VocabFinish f;
     std::memset(&f, 0, sizeof(f));
     f.dtype = dtype;

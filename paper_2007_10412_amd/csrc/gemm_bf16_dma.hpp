@@ -371,6 +371,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
     }
   }
   if constexpr (EPI == kEpiVocab) {
+    if (g.k_splits > 1) { store_partial_rows<TM, TN>(g, acc, m0, n0, wm0, wn0, live); return; }
     epilogue_vocab<uint16_t, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, live);
   } else if constexpr (EPI == kEpiHeadX || EPI == kEpiHeadW) {
     epilogue_head<EPI == kEpiHeadX, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, EPI == kEpiHeadX ? live : g.M);

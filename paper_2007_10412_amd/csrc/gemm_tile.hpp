@@ -213,6 +213,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_tile_kernel(GemmArgs g) {
   __syncthreads();                                      // the stages become the output tile
   T* const ct = reinterpret_cast<T*>(smem_raw);
   if constexpr (EPI == kEpiVocab) {
+    if (g.k_splits > 1) { store_partial_rows<TM, TN>(g, acc, m0, n0, wm0, wn0, live); return; }
     epilogue_vocab<T, BM, BN, TM, TN>(g, acc, ct, m0, n0, wm0, wn0, live);
   } else {
     if (g.k_splits > 1) {                               // this split's partial sums, in fp32

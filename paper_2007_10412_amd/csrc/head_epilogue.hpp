@@ -144,6 +144,27 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
   store_tile<T, BM, BN>(ct, static_cast<T*>(g.y), g.ldy, live - m0, n0, (int)g.ldy, [&](int r) { return m0 + r; });
 }
 
+// a transposed tile's partial sums, four columns of a row a lane (rows are whole vectors)
+template <int TM, int TN>
+__device__ __forceinline__ void store_partial_rows(const GemmArgs& g, floatx16 (&acc)[TM][TN], int m0, int n0, int wm0, int wn0, int live) {
+  const int lane = threadIdx.x & 63, lr = lane & 31, hh = lane >> 5;
+  float* const C = static_cast<float*>(g.C) + (int64_t)blockIdx.y * g.split_stride;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int place = m0 + wm0 + i * 32 + lr;
+    if (place >= live) continue;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int col = n0 + wn0 + j * 32 + q * 8 + hh * 4;
+        if (col < g.ldc)
+          *reinterpret_cast<floatx4*>(C + (int64_t)place * g.ldc + col) =
+              floatx4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+      }
+  }
+}
+
 // dX (rows sent to their places in the batch) and dW in bf16 through LDS, or in fp32 as they are
 template <bool X, int BM, int BN, int TM, int TN>
 __device__ __forceinline__ void epilogue_head(const GemmArgs& g, floatx16 (&acc)[TM][TN], uint16_t* ct, int m0, int n0, int wm0,

@@ -314,6 +314,8 @@ hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, 
 hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, hipStream_t st);
 // first [rows][first_ld]: how many of a row's (sorted) entries lie before class `part` t, t = 0 .. parts
 hipError_t launch_list_parts(const int32_t* index, int rows, int k, int part, int parts, uint16_t* first, int first_ld, hipStream_t st);
+// kEpiVocab's work on the partial sums of a product with a split K, which that epilogue has left in C; parts are 64 wide
+hipError_t launch_vocab_join(int dtype, const GemmArgs& g, hipStream_t st);
 // After the logits' product, for every place of the list: the row's loss, its maximum top and what its exponentials
 // 2^((z - top) c) are multiplied by, factor = weight T / their sum.  For dW the rows of x side by side (xs, rows x_ld apart),
 // unless the list has them all.  Rows that do not count: no loss, dX zero.

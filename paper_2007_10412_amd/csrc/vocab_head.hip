@@ -74,6 +74,56 @@ __global__ __launch_bounds__(256) void list_parts_kernel(const int32_t* __restri
 }
 
 // ------------------------------------------------------------------ between the products
+// What epilogue_vocab does, on partial sums: 16 lanes have 64 columns of a row, four each.
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_join_kernel(GemmArgs g) {
+  const HeadArgs& h = g.head;
+  const int l = threadIdx.x & 15, place = (int)blockIdx.y * 16 + (threadIdx.x >> 4), live = *h.live;
+  if (place >= live) return;
+  const int part = blockIdx.x, col = part * 64 + l * 4;
+  const float* const in = static_cast<const float*>(g.C) + (int64_t)place * g.ldc + col;
+  floatx4 z = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < g.k_splits; s += 4) {
+    floatx4 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = s + q < g.k_splits ? *reinterpret_cast<const floatx4*>(in + (s + q) * g.split_stride) : floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[e] += v[q][e];
+  }
+  float m = -INFINITY, s = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (g.bias) z[e] += g.bias[min(col + e, g.N - 1)];
+    if (col + e >= g.N) z[e] = -INFINITY;
+    m = fmaxf(m, z[e]);
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  const float from = m == -INFINITY ? 0.f : m;
+  float below[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) { below[e] = z[e] - from; s += __builtin_amdgcn_exp2f(below[e] * h.c); }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if (l == 0) *reinterpret_cast<float2*>(h.stats + ((int64_t)part * h.stats_ld + place) * 2) = make_float2(m, s);
+  if (g.y) {
+    T* const y = static_cast<T*>(g.y) + (int64_t)place * g.ldy + col;
+    const float k = -h.c / kCodeRange;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(y) = u32x2{code_pair(below[0] * k, below[1] * k), code_pair(below[2] * k, below[3] * k)};
+    else *reinterpret_cast<floatx4*>(y) = z;
+  }
+  const int row = h.row_map[place];
+  int t0 = 0, t1 = 0;
+  if (h.labels) t1 = 1;
+  else { t0 = h.first[(int64_t)row * h.first_ld + part]; t1 = h.first[(int64_t)row * h.first_ld + part + 1]; }
+  for (int t = t0; t < t1; ++t) {
+    const int at = (h.labels ? h.labels[row] : h.index[(int64_t)row * h.k + t]) - col;
+    if (at >= 0 && at < 4) h.target[(int64_t)place * h.k + t] = at == 0 ? z[0] : at == 1 ? z[1] : at == 2 ? z[2] : z[3];
+  }
+}
+
 // (maximum, sum of exponentials from it) of two parts; one with nothing in it adds its 0, or its NaN
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2, float c) {
   if (m2 == -INFINITY) { s += s2; return; }
@@ -342,6 +392,13 @@ hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t
 }
 hipError_t launch_list_parts(const int32_t* index, int rows, int k, int part, int parts, uint16_t* first, int first_ld, hipStream_t st) {
   hipLaunchKernelGGL(list_parts_kernel, dim3((rows + 3) / 4), dim3(256), 0, st, index, rows, k, part, parts, first, first_ld);
+  return hipGetLastError();
+}
+hipError_t launch_vocab_join(int dtype, const GemmArgs& g, hipStream_t st) {
+  const dim3 grid((g.N + 63) / 64, (g.M + 15) / 16);
+  if (grid.y > 65535 || g.ldc % 64) return hipErrorInvalidValue;
+  if (dtype == kBF16) hipLaunchKernelGGL(vocab_join_kernel<uint16_t>, grid, dim3(256), 0, st, g);
+  else hipLaunchKernelGGL(vocab_join_kernel<float>, grid, dim3(256), 0, st, g);
   return hipGetLastError();
 }
 // places of a finishing workgroup: up to 16, while there is a workgroup for every other CU

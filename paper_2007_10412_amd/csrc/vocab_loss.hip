@@ -400,6 +400,7 @@ hipError_t rows_any(const VocabRows& a, hipStream_t st) {
   if (vecs <= 256 * 8) return rows_whole<T, 256, 8>(a, st);
   if (vecs <= 512 * 8) return rows_whole<T, 512, 8>(a, st);
   if (vecs <= 512 * 16) return rows_whole<T, 512, 16>(a, st);
+  if (vecs <= 1024 * 16) return rows_whole<T, 1024, 16>(a, st);
   const int64_t parts = (vecs + kPartThreads * kPartVecs - 1) / (kPartThreads * kPartVecs);
   float* const dots = a.stats + (int64_t)a.rows * parts * 2;
   const dim3 grid((unsigned)parts, (unsigned)(a.rows < 65535 ? a.rows : 65535), (unsigned)((a.rows + 65534) / 65535));
