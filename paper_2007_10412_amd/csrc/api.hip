@@ -1594,7 +1594,9 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   float* losses = h.row_loss;
   RAD_TRY(vocab_targets(c, labels, teacher, row_weight, rows, d_out, !one, &t, &losses));
   const void *W = nullptr, *x = nullptr;
-  RAD_TRY(head_padded(c, WS_HEADW, dtype, h.W, d_in, d_out, vp8, &W));
+  // (a copy's rows are whole cache lines: the tiles' 256-byte pieces of them then take two lines, not three)
+  const int64_t w_ld = vp8 == d_out && (reinterpret_cast<uintptr_t>(h.W) & 15) == 0 ? d_out : vp;
+  RAD_TRY(head_padded(c, WS_HEADW, dtype, h.W, d_in, d_out, w_ld, &W));
   RAD_TRY(head_padded(c, WS_HEADX, dtype, h.x, rows, d_in, dp, &x));
 
   const HeadPlan fwd = head_plan(dtype, kEpiVocab, piece, d_out, d_in, true);
@@ -1631,7 +1633,7 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(tp, n, d_out, list, live, inv_count, c->stream); }));
     GemmArgs g = gemm_zero();
     g.M = n; g.N = d_out; g.K = d_in;
-    g.A = static_cast<const char*>(x) + r0 * dp * esz; g.lda = dp; g.B = W; g.ldb = vp8;
+    g.A = static_cast<const char*>(x) + r0 * dp * esz; g.lda = dp; g.B = W; g.ldb = w_ld;
     g.bias = h.bias; g.y = z; g.ldy = vp;
     HeadArgs& a = g.head;
     a.live = live; a.row_map = list; a.n_load = (int)vp8;
@@ -1664,7 +1666,7 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     if (h.dX) {
       GemmArgs gx = gemm_zero();
       gx.M = n; gx.N = d_in; gx.K = (int)vp8;
-      gx.A = z; gx.lda = vp; gx.B = W; gx.ldb = vp8;
+      gx.A = z; gx.lda = vp; gx.B = W; gx.ldb = w_ld;
       gx.C = f.dx; gx.ldc = d_in; gx.c_dtype = dtype;
       gx.head.live = live; gx.head.row_map = list;
       std::memset(&sum, 0, sizeof(sum));

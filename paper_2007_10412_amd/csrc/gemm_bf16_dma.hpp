@@ -157,11 +157,16 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
 
   constexpr bool kHead = EPI == kEpiVocab || EPI == kEpiHeadX || EPI == kEpiHeadW;
   constexpr bool kSwap = EPI == kEpiVocab;
-  // (N may be ragged for an M/N-contiguous B; under a loss M too, and N whatever B is)
-  const int tiles_n = (g.N + BN - 1) / BN, tiles_m = kHead ? (g.M + BM - 1) / BM : g.M / BM;
+  // (N may be ragged for an M/N-contiguous B; under a loss M too, and N whatever B is, and only the tiles of the rows that
+  // count are dealt out)
+  int live = 0;
+  if constexpr (kHead) live = *g.head.live;
+  const int tiles_n = (g.N + BN - 1) / BN;
+  const int tiles_m = kHead ? ((EPI == kEpiHeadW ? g.M : live) + BM - 1) / BM : g.M / BM;
   const int T = tiles_m * tiles_n;
   int lin = blockIdx.x;
   if (kHead) {                          // chunks per XCD whose lengths differ by one at most
+    if (lin >= T) return;
     const int q = T >> 3, r = T & 7, x = lin & 7;
     lin = x * q + min(x, r) + (lin >> 3);
   } else if ((T & 7) == 0) lin = (lin & 7) * (T >> 3) + (lin >> 3);
@@ -170,11 +175,6 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
   const int gh = min(GM, tiles_m - grp * GM);
   const int tm = grp * GM + within % gh, tn = within / gh;
   const int m0 = tm * BM, n0 = tn * BN;
-  int live = 0;
-  if constexpr (kHead) {
-    live = *g.head.live;
-    if (EPI != kEpiHeadW && m0 >= live) return;         // (the whole workgroup)
-  }
   const int w = threadIdx.x >> 6;
   const int wm0 = (w >> 1) * (BM / 2), wn0 = (w & 1) * (BN / 2);
   const int lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;

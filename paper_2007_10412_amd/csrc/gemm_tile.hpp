@@ -162,14 +162,15 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_tile_kernel(GemmArgs g) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   const uint32_t smem_lds = (uint32_t)reinterpret_cast<uintptr_t>(smem_raw);
 
-  // the workgroups of an XCD (ids equal mod 8) take neighbouring tiles, in columns of up to 8 tile rows
-  const int tiles_n = (g.N + BN - 1) / BN, tiles_m = (g.M + BM - 1) / BM, tiles = tiles_m * tiles_n;
+  // the workgroups of an XCD (ids equal mod 8) take neighbouring tiles, in columns of up to 8 tile rows; the grid is made for
+  // all rows, the tiles dealt out are those of the rows that count
+  const int live = *g.head.live;
+  const int tiles_n = (g.N + BN - 1) / BN, tiles_m = ((EPI == kEpiHeadW ? g.M : live) + BM - 1) / BM, tiles = tiles_m * tiles_n;
+  if ((int)blockIdx.x >= tiles) return;
   const int x = (int)blockIdx.x & 7, lin = x * (tiles >> 3) + min(x, tiles & 7) + ((int)blockIdx.x >> 3);
   constexpr int GM = 8;
   const int grp = lin / (GM * tiles_n), within = lin - grp * (GM * tiles_n), gh = min(GM, tiles_m - grp * GM);
   const int m0 = (grp * GM + within % gh) * BM, n0 = (within / gh) * BN;
-  const int live = *g.head.live;
-  if (EPI != kEpiHeadW && m0 >= live) return;           // (the whole workgroup)
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int wm0 = (w >> 1) * (BM / 2), wn0 = (w & 1) * (BN / 2);
 
