@@ -1524,7 +1524,7 @@ static HeadPlan head_plan(int dtype, int epi, int64_t M, int64_t N, int64_t K, b
   HeadPlan best{128, 0, 1};
   double best_us = 1e30;
   for (const Kind& k : kinds) {
-    if (k.dtype != dtype || (k.tile == 64 && epi == kEpiHeadW)) continue;
+    if (k.dtype != dtype || (k.tile == 64 && epi == kEpiHeadW && dtype == kBF16)) continue;
     const double end_us = k.end_us + (k.tile == 256 && epi == kEpiVocab ? 7.0 : 0.0);
     const int64_t tiles = ((M + k.tile - 1) / k.tile) * ((N + k.cols - 1) / k.cols);
     for (int s = 1; s <= 64 && (s == 1 || (may_split && K / s >= 128)); ++s) {
@@ -1551,20 +1551,31 @@ static rad_status head_padded(rad_ctx* c, int ws, int dtype, const void* in, int
   return RAD_OK;
 }
 
-// a product with its plan: partial sums of a split K go through a workspace to `sum`'s output
-static rad_status head_product(rad_ctx* c, int dtype, int epi, const HeadPlan& plan, GemmArgs g, const SplitSum& sum) {
-  g.head.tile = plan.tile;
-  const int ak = epi == kEpiHeadW ? kOpMN : kOpK, bk = epi == kEpiHeadX ? kOpK : kOpMN;
-  if (plan.splits <= 1) return run_gemm_call(c, dtype, ak, bk, epi, g);
-  g.k_split = plan.k_split; g.k_splits = plan.splits;
-  g.ldc = (g.N + 63) / 64 * 64;
-  g.split_stride = (int64_t)g.M * g.ldc;
-  RAD_TRY(ws_get(c, WS_SPLITK, (size_t)plan.splits * g.split_stride * 4, &g.C));
-  RAD_TRY(run_gemm_call(c, dtype, ak, bk, epi, g));
-  SplitSum s = sum;
-  s.in = static_cast<const float*>(g.C); s.splits = plan.splits; s.stride = g.split_stride; s.in_ld = g.ldc;
-  s.rows = g.M; s.cols = g.N;
-  HIP_TRY(c, timed(c, "split_sum", [&](const char**) { return launch_split_sum(s, c->stream); }));
+// A product after its plan: where K is split, C becomes a workspace of partial sums (from `used` bytes on) and *sum says how
+// they are joined in what was C.
+static rad_status head_plan_apply(rad_ctx* c, const HeadPlan& plan, GemmArgs* g, SplitSum* sum, size_t total, size_t used) {
+  g->head.tile = plan.tile;
+  sum->splits = 1;
+  if (plan.splits <= 1) return RAD_OK;
+  char* part = nullptr;
+  RAD_TRY(ws_get(c, WS_SPLITK, total, reinterpret_cast<void**>(&part)));
+  sum->out = g->C; sum->out_ld = g->ldc; sum->out_dtype = g->c_dtype; sum->beta = g->beta;
+  g->k_split = plan.k_split; g->k_splits = plan.splits;
+  g->ldc = (g->N + 63) / 64 * 64;
+  g->split_stride = (int64_t)g->M * g->ldc;
+  g->C = part + used;
+  sum->in = static_cast<const float*>(g->C); sum->splits = plan.splits; sum->stride = g->split_stride; sum->in_ld = g->ldc;
+  sum->rows = g->M; sum->cols = g->N;
+  return RAD_OK;
+}
+static size_t head_plan_bytes(const HeadPlan& plan, const GemmArgs& g) {
+  return plan.splits > 1 ? (size_t)plan.splits * g.M * ((g.N + 63) / 64 * 64) * 4 : 0;
+}
+static int64_t head_workgroups(const HeadPlan& plan, const GemmArgs& g) {
+  return (int64_t)((g.M + plan.tile - 1) / plan.tile) * ((g.N + 127) / 128) * plan.splits;
+}
+static rad_status head_split_sum(rad_ctx* c, const SplitSum& sum) {
+  if (sum.splits > 1) HIP_TRY(c, timed(c, "split_sum", [&](const char**) { return launch_split_sum(sum, c->stream); }));
   return RAD_OK;
 }
 
@@ -1630,13 +1641,16 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     else { tp.index += r0 * t.k; tp.prob += r0 * t.k; tp.entropy += r0; tp.counts += r0; }
     if (tp.weight) tp.weight += r0;
     float* const inv_count = one && !row_weight ? const_cast<float*>(t.inv_count) : nullptr;
-    HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(tp, n, d_out, list, live, inv_count, c->stream); }));
+    const bool own_list = n <= kOwnListRows;
+    if (!own_list)
+      HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(tp, n, d_out, list, live, inv_count, c->stream); }));
     GemmArgs g = gemm_zero();
     g.M = n; g.N = d_out; g.K = d_in;
     g.A = static_cast<const char*>(x) + r0 * dp * esz; g.lda = dp; g.B = W; g.ldb = w_ld;
     g.bias = h.bias; g.y = z; g.ldy = vp;
     HeadArgs& a = g.head;
-    a.live = live; a.row_map = list; a.n_load = (int)vp8;
+    a.live = live; a.row_map = list; a.rows = n; a.n_load = (int)vp8;
+    if (own_list) { a.counts = tp.counts; a.list_out = list; a.live_out = live; a.inv_count_out = inv_count; }
     a.c = 1.44269504088896340736f / t.temperature;
     a.stats = stats; a.stats_ld = piece;
     a.labels = tp.labels; a.index = tp.index; a.first = t.labels ? nullptr : first + r0 * first_ld; a.k = t.k; a.first_ld = first_ld;
@@ -1662,27 +1676,42 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     if (one && h.loss && vocab_loss_inside(f)) { f.loss = h.loss; summed = true; }
     HIP_TRY(c, timed(c, "vocab_finish", [&](const char**) { return launch_vocab_finish(f, c->stream); }));
     if (train) HIP_TRY(c, timed(c, "vocab_gradient", [&](const char**) { return launch_vocab_gradient(f, c->stream); }));
-    SplitSum sum;
+    GemmArgs gx = gemm_zero(), gw = gemm_zero();
+    HeadPlan px{0, 0, 1}, pw{0, 0, 1};
+    SplitSum sx, sw;
+    std::memset(&sx, 0, sizeof(sx));
+    std::memset(&sw, 0, sizeof(sw));
     if (h.dX) {
-      GemmArgs gx = gemm_zero();
       gx.M = n; gx.N = d_in; gx.K = (int)vp8;
       gx.A = z; gx.lda = vp; gx.B = W; gx.ldb = w_ld;
       gx.C = f.dx; gx.ldc = d_in; gx.c_dtype = dtype;
       gx.head.live = live; gx.head.row_map = list;
-      std::memset(&sum, 0, sizeof(sum));
-      sum.live = live; sum.map = list; sum.out = f.dx; sum.out_dtype = dtype; sum.out_ld = d_in;
-      RAD_TRY(head_product(c, dtype, kEpiHeadX, head_plan(dtype, kEpiHeadX, n, d_in, vp8, n <= 65535), gx, sum));
+      sx.live = live; sx.map = list;
+      px = head_plan(dtype, kEpiHeadX, n, d_in, vp8, n <= 65535);
     }
     if (h.dW) {
-      GemmArgs gw = gemm_zero();
       gw.M = d_in; gw.N = d_out; gw.K = n; gw.m_load = (int)dp;
       gw.A = xs; gw.lda = dp; gw.B = z; gw.ldb = vp;
       gw.C = dW32 ? dW32 : h.dW; gw.ldc = d_out; gw.c_dtype = dW32 ? kF32 : kBF16;
       gw.beta = dW32 && (r0 > 0 || (h.beta != 0.f && !cast));
       gw.head.live = live; gw.head.n_load = (int)vp8; gw.head.whole = f.x; gw.head.rows = n;
-      std::memset(&sum, 0, sizeof(sum));
-      sum.out = gw.C; sum.out_dtype = gw.c_dtype; sum.out_ld = d_out; sum.beta = gw.beta;
-      RAD_TRY(head_product(c, dtype, kEpiHeadW, head_plan(dtype, kEpiHeadW, d_in, d_out, n, d_in <= 65535), gw, sum));
+      pw = head_plan(dtype, kEpiHeadW, d_in, d_out, n, d_in <= 65535);
+    }
+    // One launch for both where both have small tiles: in bf16 (4096 x 1024 x 1000 84 -> 73 us, 500 x 1000 x 10000 90 -> 83), in
+    // fp32 where together they do not fill the chip (150 x 300 x 10 51 -> 45; 30 x 1000 x 20000 would go from 119 to 127).
+    const bool pair = h.dX && h.dW && px.tile != 256 && pw.tile == 128 &&
+                      (dtype == kBF16 || head_workgroups(px, gx) + head_workgroups(pw, gw) <= 256);
+    const size_t x_bytes = head_plan_bytes(px, gx), w_bytes = head_plan_bytes(pw, gw);
+    const size_t split_bytes = pair ? x_bytes + w_bytes : std::max(x_bytes, w_bytes);
+    if (h.dX) RAD_TRY(head_plan_apply(c, px, &gx, &sx, split_bytes, 0));
+    if (h.dW) RAD_TRY(head_plan_apply(c, pw, &gw, &sw, split_bytes, pair ? x_bytes : 0));
+    if (pair) {
+      HIP_TRY(c, timed(c, "gemm_head_dx_dw", [&](const char**) { return launch_gemm_head_pair(dtype, gx, gw, c->stream); }));
+      RAD_TRY(head_split_sum(c, sx));
+      RAD_TRY(head_split_sum(c, sw));
+    } else {
+      if (h.dX) { RAD_TRY(run_gemm_call(c, dtype, kOpK, kOpK, kEpiHeadX, gx)); RAD_TRY(head_split_sum(c, sx)); }
+      if (h.dW) { RAD_TRY(run_gemm_call(c, dtype, kOpMN, kOpMN, kEpiHeadW, gw)); RAD_TRY(head_split_sum(c, sw)); }
     }
     if (h.dbias) {
       void* partial = nullptr;

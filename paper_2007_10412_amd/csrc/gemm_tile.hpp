@@ -151,23 +151,31 @@ template <bool AT, bool BT, int BM, int BN, int TM, int TN, bool SWAP> struct Ti
   }
 };
 
+// workgroup `block` of split `split` of a product
 template <typename T, int AKIND, int BKIND, int EPI, int BM, int BN, int S>
-__global__ __launch_bounds__(kGemmThreads) void gemm_tile_kernel(GemmArgs g) {
+__device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* smem_raw, int block, int split) {
   constexpr int TM = BM / 64, TN = BN / 64;
   constexpr bool kAT = AKIND == kOpMN, kBT = BKIND == kOpMN, kSwap = EPI == kEpiVocab;
   typedef TileOperand<T, BM, kAT> LoadA;
   typedef TileOperand<T, BN, kBT> LoadB;
   typedef TileSmem<T, BM, BN, S> Smem;
   constexpr int BK = LoadA::BK, kLoads = LoadA::NI + LoadB::NI;
-  extern __shared__ __align__(16) unsigned char smem_raw[];
   const uint32_t smem_lds = (uint32_t)reinterpret_cast<uintptr_t>(smem_raw);
 
   // the workgroups of an XCD (ids equal mod 8) take neighbouring tiles, in columns of up to 8 tile rows; the grid is made for
   // all rows, the tiles dealt out are those of the rows that count
-  const int live = *g.head.live;
+  const int32_t* row_map = g.head.row_map;
+  int live;
+  if (EPI == kEpiVocab && g.head.list_out) {
+    __shared__ int32_t s_list[kOwnListRows], s_n[kGemmThreads / 64];
+    live = own_row_list(g.head, g.N, s_list, s_n, block == 0 && split == 0);
+    row_map = s_list;
+  } else {
+    live = *g.head.live;
+  }
   const int tiles_n = (g.N + BN - 1) / BN, tiles_m = ((EPI == kEpiHeadW ? g.M : live) + BM - 1) / BM, tiles = tiles_m * tiles_n;
-  if ((int)blockIdx.x >= tiles) return;
-  const int x = (int)blockIdx.x & 7, lin = x * (tiles >> 3) + min(x, tiles & 7) + ((int)blockIdx.x >> 3);
+  if (block >= tiles) return;
+  const int x = block & 7, lin = x * (tiles >> 3) + min(x, tiles & 7) + (block >> 3);
   constexpr int GM = 8;
   const int grp = lin / (GM * tiles_n), within = lin - grp * (GM * tiles_n), gh = min(GM, tiles_m - grp * GM);
   const int m0 = (grp * GM + within % gh) * BM, n0 = (within / gh) * BN;
@@ -182,12 +190,12 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_tile_kernel(GemmArgs g) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  const int kbeg = g.k_splits > 1 ? (int)blockIdx.y * g.k_split : 0;
+  const int kbeg = g.k_splits > 1 ? split * g.k_split : 0;
   const int k_all = EPI == kEpiHeadW ? min(g.K, live) : g.K;
   const int kend = g.k_splits > 1 ? min(k_all, kbeg + g.k_split) : k_all;
   const int KT = max(0, (kend - kbeg + BK - 1) / BK);
   LoadA la; LoadB lb;
-  if (EPI == kEpiVocab) la.init(g.A, g.lda, m0, kbeg, live, g.head.row_map);
+  if (EPI == kEpiVocab) la.init(g.A, g.lda, m0, kbeg, live, row_map);
   else if (EPI == kEpiHeadW) la.init(live == g.head.rows ? g.head.whole : g.A, g.lda, m0, kbeg, g.m_load, nullptr);
   else la.init(g.A, g.lda, m0, kbeg, g.M, nullptr);
   lb.init(g.B, g.ldb, n0, kbeg, kBT ? g.head.n_load : g.N, nullptr);
@@ -214,18 +222,34 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_tile_kernel(GemmArgs g) {
   __syncthreads();                                      // the stages become the output tile
   T* const ct = reinterpret_cast<T*>(smem_raw);
   if constexpr (EPI == kEpiVocab) {
-    if (g.k_splits > 1) { store_partial_rows<TM, TN>(g, acc, m0, n0, wm0, wn0, live); return; }
-    epilogue_vocab<T, BM, BN, TM, TN>(g, acc, ct, m0, n0, wm0, wn0, live);
+    if (g.k_splits > 1) { store_partial_rows<TM, TN>(g, acc, m0, n0, wm0, wn0, live, split); return; }
+    epilogue_vocab<T, BM, BN, TM, TN>(g, acc, ct, m0, n0, wm0, wn0, live, row_map);
   } else {
     if (g.k_splits > 1) {                               // this split's partial sums, in fp32
       GemmArgs gs = g;
-      gs.C = static_cast<float*>(g.C) + (int64_t)blockIdx.y * g.split_stride;
+      gs.C = static_cast<float*>(g.C) + (int64_t)split * g.split_stride;
       epilogue_store<TM, TN, float, true, false, false, false>(gs, acc, m0, n0, wm0, wn0);
       return;
     }
     epilogue_head<EPI == kEpiHeadX, BM, BN, TM, TN>(g, acc, reinterpret_cast<uint16_t*>(ct), m0, n0, wm0, wn0,
                                                     EPI == kEpiHeadX ? live : g.M);
   }
+}
+
+template <typename T, int AKIND, int BKIND, int EPI, int BM, int BN, int S>
+__global__ __launch_bounds__(kGemmThreads) void gemm_tile_kernel(GemmArgs g) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  tile_product<T, AKIND, BKIND, EPI, BM, BN, S>(g, smem_raw, blockIdx.x, blockIdx.y);
+}
+
+// dX and dW in one launch: neither waits for the other, and where rows are few neither fills the chip.  The first w_blocks
+// workgroups (a multiple of 8) have dW's tiles, split by split; the others dX's.
+template <typename T, int BM, int S>
+__global__ __launch_bounds__(kGemmThreads) void gemm_tile_pair_kernel(GemmArgs x, GemmArgs w, int w_blocks, int w_tiles8, int x_tiles8) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  const int b = blockIdx.x;
+  if (b < w_blocks) tile_product<T, kOpMN, kOpMN, kEpiHeadW, 128, 128, 2>(w, smem_raw, b % w_tiles8, b / w_tiles8);
+  else tile_product<T, kOpK, kOpK, kEpiHeadX, BM, 128, S>(x, smem_raw, (b - w_blocks) % x_tiles8, (b - w_blocks) / x_tiles8);
 }
 
 }  // namespace rad

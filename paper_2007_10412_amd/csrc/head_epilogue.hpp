@@ -4,6 +4,40 @@
 
 namespace rad {
 
+// The rows that count, in order, into LDS (kOwnListRows entries, and 4 for the waves' counts); returns their number.  A thread
+// has four consecutive rows.
+__device__ __forceinline__ int own_row_list(const HeadArgs& h, int classes, int32_t* s_list, int32_t* s_n, bool write) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r0 = (int)threadIdx.x * 4;
+  uint32_t mine = 0u;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (r0 + q < h.rows && (h.labels ? (uint32_t)h.labels[r0 + q] < (uint32_t)classes : h.counts[r0 + q] != 0)) mine |= 1u << q;
+  const int n = __popc(mine);
+  int up = n;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(up, o); if (lane >= o) up += v; }
+  if (lane == 63) s_n[w] = up;
+  __syncthreads();
+  int at = up - n, all = 0;
+#pragma unroll
+  for (int q = 0; q < kGemmThreads / 64; ++q) { if (q < w) at += s_n[q]; all += s_n[q]; }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int r = r0 + q;
+    if (r >= h.rows) break;
+    const bool c = (mine >> q) & 1u;
+    if (c) s_list[at] = r;
+    if (write) h.list_out[c ? at : all + (r - at)] = r;      // (r - at rows before this one do not count)
+    at += c ? 1 : 0;
+  }
+  if (write && threadIdx.x == 0) {
+    *h.live_out = all;
+    if (h.inv_count_out) *h.inv_count_out = all > 0 ? 1.f / (float)all : 0.f;
+  }
+  __syncthreads();
+  return all;
+}
+
 // fp32 pair -> two bf16 (round to nearest even) in one word
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   uint16_t p[2];
@@ -54,7 +88,7 @@ __device__ __forceinline__ void store_tile(const T* ct, T* C, int64_t ldc, int r
 // between the two lanes that share the row.
 template <typename T, int BM, int BN, int TM, int TN>
 __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc)[TM][TN], T* ct, int m0, int n0, int wm0,
-                                               int wn0, int live) {
+                                               int wn0, int live, const int32_t* row_map) {
   constexpr bool kCodes = sizeof(T) == 2;
   constexpr int CP = BN + 16 / (int)sizeof(T), kPart = 32 * TN;            // a wave's columns are one part of a row
   const HeadArgs& h = g.head;
@@ -94,7 +128,7 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
     // targets among these columns
     int t0 = 0, t1 = 0, row = 0;
     if (there) {
-      row = h.row_map[place];
+      row = row_map[place];
       if (h.labels) { t1 = (uint32_t)(h.labels[row] - nw) < (uint32_t)kPart ? 1 : 0; }
       else {
         const uint16_t* const f = h.first + (int64_t)row * h.first_ld + part;
@@ -146,9 +180,10 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
 
 // a transposed tile's partial sums, four columns of a row a lane (rows are whole vectors)
 template <int TM, int TN>
-__device__ __forceinline__ void store_partial_rows(const GemmArgs& g, floatx16 (&acc)[TM][TN], int m0, int n0, int wm0, int wn0, int live) {
+__device__ __forceinline__ void store_partial_rows(const GemmArgs& g, floatx16 (&acc)[TM][TN], int m0, int n0, int wm0, int wn0, int live,
+                                                   int split) {
   const int lane = threadIdx.x & 63, lr = lane & 31, hh = lane >> 5;
-  float* const C = static_cast<float*>(g.C) + (int64_t)blockIdx.y * g.split_stride;
+  float* const C = static_cast<float*>(g.C) + (int64_t)split * g.split_stride;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int place = m0 + wm0 + i * 32 + lr;

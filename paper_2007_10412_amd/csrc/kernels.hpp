@@ -56,10 +56,14 @@ enum EpiKind : int {
 
 // The rows of the batch that have a target come first in a list; the products run over that list, whose length only the
 // device knows.
+constexpr int kOwnListRows = 1024;
 struct HeadArgs {
   const int32_t* live;          // length of the list
+  // kEpiVocab with few rows: the list is made here, by every workgroup for itself, and written by one (rows <= kOwnListRows)
+  const int32_t* counts;        // which rows count, where there are no labels
+  int32_t* list_out; int32_t* live_out; float* inv_count_out;   // list_out null: the list is there (inv_count_out may be null)
   const int32_t* row_map;       // row of x and dX of every place in the list (kEpiVocab: of A; kEpiHeadX: of C)
-  const void* whole; int rows;  // kEpiHeadW: what A is where the list has all `rows` rows
+  const void* whole; int rows;  // rows of the batch; kEpiHeadW: what A is where the list has them all
   int tile;
   int n_load;                   // B: readable columns (a multiple of 8, >= N), M/N contiguous
   // kEpiVocab: logits z; c = log2(e) / T
@@ -109,6 +113,8 @@ struct GemmArgs {
 // (head products: tile is the height of the tiles, 64, 128 or 256; the part of a row that kEpiVocab's statistics are for is
 // head_part(tile) columns wide)
 inline int head_part(int tile) { return tile == 256 ? 128 : 64; }
+// dX and dW of such a layer in one launch: tiles of 64 or 128 rows, and of 128
+hipError_t launch_gemm_head_pair(int dtype, const GemmArgs& x, const GemmArgs& w, hipStream_t st);
 hipError_t launch_gemm(int dtype, int a_kind, int b_kind, int epi, const GemmArgs& g,
                        hipStream_t st, const char** name);
 

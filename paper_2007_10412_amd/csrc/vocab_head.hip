@@ -18,21 +18,24 @@ __global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows
                                                         int32_t* __restrict__ live, float* __restrict__ inv_count) {
   __shared__ int s_n[16];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int total = 0;                                        // rows that count, first of all
-  for (int r = threadIdx.x; r < rows; r += 1024) total += (t.labels ? (uint32_t)t.labels[r] < (uint32_t)classes : t.counts[r] != 0) ? 1 : 0;
+  auto counts = [&](int r) { return t.labels ? (uint32_t)t.labels[r] < (uint32_t)classes : t.counts[r] != 0; };
+  int total = 0;                                        // rows that count (of one block of rows: below)
+  if (rows > 8192) {
+    for (int r = threadIdx.x; r < rows; r += 1024) total += counts(r) ? 1 : 0;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-  if (lane == 0) s_n[w] = total;
-  __syncthreads();
-  total = 0;
-  for (int q = 0; q < 16; ++q) total += s_n[q];
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+    if (lane == 0) s_n[w] = total;
+    __syncthreads();
+    total = 0;
+    for (int q = 0; q < 16; ++q) total += s_n[q];
+  }
   int before = 0;                                       // rows that count before this block of 8192
   for (int r0 = 0; r0 < rows; r0 += 8192) {
     uint32_t mine = 0u;
     const int r1 = r0 + (int)threadIdx.x * 8;
 #pragma unroll
     for (int q = 0; q < 8; ++q)
-      if (r1 + q < rows && (t.labels ? (uint32_t)t.labels[r1 + q] < (uint32_t)classes : t.counts[r1 + q] != 0)) mine |= 1u << q;
+      if (r1 + q < rows && counts(r1 + q)) mine |= 1u << q;
     int n = __popc(mine), up = n;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(up, o); if (lane >= o) up += v; }
@@ -41,6 +44,7 @@ __global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows
     __syncthreads();
     int at = before + up - n, all = 0;
     for (int q = 0; q < 16; ++q) { if (q < w) at += s_n[q]; all += s_n[q]; }
+    if (rows <= 8192) total = all;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       const int r = r1 + q;
@@ -216,8 +220,8 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinis
 
 // 16 rows x kSteps 16-byte vectors of 16 lanes a workgroup.  Reads and writes a logit, and is bound by that.  The last column of
 // workgroups (where there is a loss to sum) has no logits: its first one adds the rows' losses.
-constexpr int kGradRows = 16, kGradSteps = 16;
-template <typename T>
+constexpr int kGradRows = 16;
+template <typename T, int kGradSteps>
 __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int sum_column) {
   constexpr int VPL = 16 / (int)sizeof(T), kCols = 16 * VPL * kGradSteps;
   __shared__ float s_w[4];
@@ -407,6 +411,19 @@ static int finish_shift(int rows) {
   while (shift > 0 && (rows >> shift) < 128) --shift;
   return shift;
 }
+// 16 vectors a lane where that makes a workgroup for every other CU, 4 where it does not
+template <typename T> static hipError_t gradient_of(const VocabFinish& a, hipStream_t st) {
+  const unsigned rows = (unsigned)((a.rows + kGradRows - 1) / kGradRows);
+  if (rows > 65535) return hipErrorInvalidValue;
+  const int64_t width = 16 * (16 / (int)sizeof(T));
+  const bool wide = rows * ((a.z_ld + 16 * width - 1) / (16 * width)) >= 128;
+  const unsigned cols = (unsigned)((a.z_ld + (wide ? 16 : 4) * width - 1) / ((wide ? 16 : 4) * width));
+  const dim3 grid(cols + (a.loss ? 1 : 0), rows);
+  const int sum_column = a.loss ? (int)cols : -1;
+  if (wide) hipLaunchKernelGGL((vocab_gradient_kernel<T, 16>), grid, dim3(256), 0, st, a, sum_column);
+  else hipLaunchKernelGGL((vocab_gradient_kernel<T, 4>), grid, dim3(256), 0, st, a, sum_column);
+  return hipGetLastError();
+}
 bool vocab_loss_inside(const VocabFinish& a) { return a.z || a.rows <= 1 << finish_shift(a.rows); }
 hipError_t launch_vocab_finish(const VocabFinish& a, hipStream_t st) {
   const int shift = finish_shift(a.rows);
@@ -416,14 +433,7 @@ hipError_t launch_vocab_finish(const VocabFinish& a, hipStream_t st) {
   return hipGetLastError();
 }
 hipError_t launch_vocab_gradient(const VocabFinish& a, hipStream_t st) {
-  const int kCols = kGradSteps * 16 * (a.dtype == kBF16 ? 8 : 4);
-  const unsigned cols = (unsigned)((a.z_ld + kCols - 1) / kCols), rows = (unsigned)((a.rows + kGradRows - 1) / kGradRows);
-  if (rows > 65535) return hipErrorInvalidValue;
-  const dim3 grid(cols + (a.loss ? 1 : 0), rows);
-  const int sum_column = a.loss ? (int)cols : -1;
-  if (a.dtype == kBF16) hipLaunchKernelGGL(vocab_gradient_kernel<uint16_t>, grid, dim3(256), 0, st, a, sum_column);
-  else hipLaunchKernelGGL(vocab_gradient_kernel<float>, grid, dim3(256), 0, st, a, sum_column);
-  return hipGetLastError();
+  return a.dtype == kBF16 ? gradient_of<uint16_t>(a, st) : gradient_of<float>(a, st);
 }
 hipError_t launch_split_sum(const SplitSum& a, hipStream_t st) {
   if (a.rows > 65535 || a.in_ld % 4) return hipErrorInvalidValue;
