@@ -1527,7 +1527,7 @@ static HeadPlan head_plan(int dtype, int epi, int64_t M, int64_t N, int64_t K, b
     if (k.dtype != dtype || (k.tile == 64 && epi == kEpiHeadW && dtype == kBF16)) continue;
     const double end_us = k.end_us + (k.tile == 256 && epi == kEpiVocab ? 7.0 : 0.0);
     const int64_t tiles = ((M + k.tile - 1) / k.tile) * ((N + k.cols - 1) / k.cols);
-    for (int s = 1; s <= 64 && (s == 1 || (may_split && K / s >= 128)); ++s) {
+    for (int s = 1; s <= 64 && (s == 1 || (may_split && K / s >= 128 && !(k.tile == 256 && epi == kEpiVocab))); ++s) {
       const int64_t k_split = ((K + s - 1) / s + 63) / 64 * 64;
       const int splits = (int)((K + k_split - 1) / k_split);
       const double each = (double)((tiles * splits + 255) / 256), full = std::min(1.0, (double)(tiles * splits) / 256.0);
@@ -1579,6 +1579,12 @@ static rad_status head_split_sum(rad_ctx* c, const SplitSum& sum) {
   return RAD_OK;
 }
 
+// Two kernels against the general route's five or more, us with all gradients, fp32 / bf16: 150 x 300 x 10 20 / 22 against
+// 43 / 28; 1000 x 300 x 10 50 against 48, 150 x 4096 x 10 53 against 43, 1000 x 4096 x 10 88 / 97 against 62 / 38.
+static bool few_classes_pay(int64_t rows, int64_t d_in, int64_t d_out) {
+  return d_out <= kFewClasses && rows <= 1024 && rows * d_in <= 100000;
+}
+
 static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* labels, const rad_teacher* teacher,
                             const float* row_weight, const HeadCall& h) {
   RAD_TRY(check_layer(c, L));
@@ -1592,6 +1598,20 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   if (std::max(L->d_in, L->d_out) > ((int64_t)1 << 22) - 64) return fail(c, RAD_ERR_SHAPE, "d_in or d_out above 2^22 - 64");
   DeviceGuard guard(c->device);
   const int rows = (int)L->batch, d_in = (int)L->d_in, d_out = (int)L->d_out, dtype = L->dtype;
+  if (few_classes_pay(rows, d_in, d_out)) {
+    FewClasses f;
+    std::memset(&f, 0, sizeof(f));
+    f.dtype = dtype; f.rows = rows; f.d_in = d_in; f.classes = d_out;
+    f.x = h.x; f.W = h.W; f.bias = h.bias;
+    f.row_loss = h.row_loss;
+    RAD_TRY(vocab_targets(c, labels, teacher, row_weight, rows, d_out, false, &f.t, &f.row_loss));
+    f.loss = h.loss; f.dx = h.dX; f.dw = h.dW; f.dw_dtype = h.dw_dtype; f.dbias = h.dbias; f.beta = h.beta != 0.f;
+    void* dz = nullptr;
+    if (h.dW || h.dbias) RAD_TRY(ws_get(c, WS_LOGITGRAD, (size_t)rows * kFewClasses * 4, &dz));
+    f.dz = static_cast<float*>(dz);
+    HIP_TRY(c, timed(c, "few_classes", [&](const char**) { return launch_few_classes(f, c->stream); }));
+    return RAD_OK;
+  }
   const int64_t esz = dtype == kF32 ? 4 : 2, vec = 16 / esz;
   const int64_t dp = (d_in + vec - 1) / vec * vec, vp8 = (d_out + vec - 1) / vec * vec, vp = (d_out + 63) / 64 * 64;
   const bool train = h.dX || h.dW || h.dbias;
@@ -1617,6 +1637,7 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   char* ws = nullptr;
   RAD_TRY(ws_get(c, WS_ROWLOSS, 256 + first_bytes + (size_t)piece * (8 * (size_t)parts + 12 + 4 * (size_t)t.k), reinterpret_cast<void**>(&ws)));
   int32_t* const live = reinterpret_cast<int32_t*>(ws);
+  float* const common = reinterpret_cast<float*>(ws) + 1;
   uint16_t* const first = reinterpret_cast<uint16_t*>(ws + 256);
   float* const stats = reinterpret_cast<float*>(ws + 256 + first_bytes);
   int32_t* const list = reinterpret_cast<int32_t*>(stats + (size_t)piece * parts * 2);
@@ -1641,16 +1662,17 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     else { tp.index += r0 * t.k; tp.prob += r0 * t.k; tp.entropy += r0; tp.counts += r0; }
     if (tp.weight) tp.weight += r0;
     float* const inv_count = one && !row_weight ? const_cast<float*>(t.inv_count) : nullptr;
-    const bool own_list = n <= kOwnListRows;
+    const bool own_list = n <= kOwnListRows && fwd.tile != 256;
     if (!own_list)
-      HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(tp, n, d_out, list, live, inv_count, c->stream); }));
+      HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(tp, n, d_out, list, live, inv_count, common, c->stream); }));
     GemmArgs g = gemm_zero();
     g.M = n; g.N = d_out; g.K = d_in;
     g.A = static_cast<const char*>(x) + r0 * dp * esz; g.lda = dp; g.B = W; g.ldb = w_ld;
     g.bias = h.bias; g.y = z; g.ldy = vp;
     HeadArgs& a = g.head;
     a.live = live; a.row_map = list; a.rows = n; a.n_load = (int)vp8;
-    if (own_list) { a.counts = tp.counts; a.list_out = list; a.live_out = live; a.inv_count_out = inv_count; }
+    if (own_list) { a.counts = tp.counts; a.list_out = list; a.live_out = live; a.inv_count_out = inv_count; a.common_out = common; }
+    a.weight = tp.weight; a.inv_count = t.inv_count; a.temperature = t.temperature;
     a.c = 1.44269504088896340736f / t.temperature;
     a.stats = stats; a.stats_ld = piece;
     a.labels = tp.labels; a.index = tp.index; a.first = t.labels ? nullptr : first + r0 * first_ld; a.k = t.k; a.first_ld = first_ld;
@@ -1669,7 +1691,7 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     f.dtype = dtype;
     f.list = list; f.live = live; f.rows = n; f.classes = d_out; f.parts = parts; f.part = part; f.t = tp;
     f.stats = stats; f.stats_ld = piece; f.target = target;
-    f.row_loss = losses + r0; f.top = top; f.factor = factor;
+    f.row_loss = losses + r0; f.top = top; f.factor = factor; f.common = common;
     f.z = z; f.z_ld = vp; f.first = a.first; f.first_ld = first_ld;
     f.x = g.A; f.x_ld = dp; f.d_in = d_in; f.xs = xs;
     f.dx = h.dX ? static_cast<char*>(h.dX) + r0 * d_in * esz : nullptr;
@@ -1685,8 +1707,8 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
       gx.M = n; gx.N = d_in; gx.K = (int)vp8;
       gx.A = z; gx.lda = vp; gx.B = W; gx.ldb = w_ld;
       gx.C = f.dx; gx.ldc = d_in; gx.c_dtype = dtype;
-      gx.head.live = live; gx.head.row_map = list;
-      sx.live = live; sx.map = list;
+      gx.head.live = live; gx.head.row_map = list; gx.head.common = common;
+      sx.live = live; sx.map = list; sx.scale = common;
       px = head_plan(dtype, kEpiHeadX, n, d_in, vp8, n <= 65535);
     }
     if (h.dW) {
@@ -1694,7 +1716,8 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
       gw.A = xs; gw.lda = dp; gw.B = z; gw.ldb = vp;
       gw.C = dW32 ? dW32 : h.dW; gw.ldc = d_out; gw.c_dtype = dW32 ? kF32 : kBF16;
       gw.beta = dW32 && (r0 > 0 || (h.beta != 0.f && !cast));
-      gw.head.live = live; gw.head.n_load = (int)vp8; gw.head.whole = f.x; gw.head.rows = n;
+      gw.head.live = live; gw.head.n_load = (int)vp8; gw.head.whole = f.x; gw.head.rows = n; gw.head.common = common;
+      sw.scale = common;
       pw = head_plan(dtype, kEpiHeadW, d_in, d_out, n, d_in <= 65535);
     }
     // One launch for both where both have small tiles: in bf16 (4096 x 1024 x 1000 84 -> 73 us, 500 x 1000 x 10000 90 -> 83), in
@@ -1717,7 +1740,7 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
       void* partial = nullptr;
       RAD_TRY(ws_get(c, WS_COLSUM, (size_t)kHeadColsumSplits * d_out * 4, &partial));
       HIP_TRY(c, timed(c, "head_colsum", [&](const char**) {
-        return launch_head_colsum(dtype, z, vp, live, d_out, static_cast<float*>(partial), h.dbias, r0 > 0 || h.beta != 0.f, c->stream);
+        return launch_head_colsum(dtype, z, vp, live, common, d_out, static_cast<float*>(partial), h.dbias, r0 > 0 || h.beta != 0.f, c->stream);
       }));
     }
   }

@@ -160,17 +160,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
   // (N may be ragged for an M/N-contiguous B; under a loss M too, and N whatever B is, and only the tiles of the rows that
   // count are dealt out)
   int live = 0;
-  const int32_t* row_map = nullptr;
-  if constexpr (EPI == kEpiVocab) {
-    row_map = g.head.row_map;
-    if (g.head.list_out) {
-      __shared__ int32_t s_list[kOwnListRows], s_n[kGemmThreads / 64];
-      live = own_row_list(g.head, g.N, s_list, s_n, blockIdx.x == 0 && blockIdx.y == 0);
-      row_map = s_list;
-    } else {
-      live = *g.head.live;
-    }
-  } else if constexpr (kHead) live = *g.head.live;
+  if constexpr (kHead) live = *g.head.live;
   const int tiles_n = (g.N + BN - 1) / BN;
   const int tiles_m = kHead ? ((EPI == kEpiHeadW ? g.M : live) + BM - 1) / BM : g.M / BM;
   const int T = tiles_m * tiles_n;
@@ -205,7 +195,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
   const bool ragged = krem < BK;                       // its loads read zeros past K; the steady loop never issues it
   const int KTs = ragged ? KT - 1 : KT;
   LoadA la; LoadB lb;
-  if constexpr (EPI == kEpiVocab) la.init_mapped(g.A, g.lda, m0, kbeg, live, row_map);
+  if constexpr (EPI == kEpiVocab) la.init_mapped(g.A, g.lda, m0, kbeg, live, g.head.row_map);
   else if constexpr (EPI == kEpiHeadW) la.init(live == g.head.rows ? g.head.whole : g.A, g.lda, m0, kbeg, g.m_load);
   else la.init(g.A, g.lda, m0, kbeg, g.M);
   lb.init(g.B, g.ldb, n0, kbeg, kHead && kBT ? g.head.n_load : g.N);
@@ -381,8 +371,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
     }
   }
   if constexpr (EPI == kEpiVocab) {
-    if (g.k_splits > 1) { store_partial_rows<TM, TN>(g, acc, m0, n0, wm0, wn0, live, (int)blockIdx.y); return; }
-    epilogue_vocab<uint16_t, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, live, row_map);
+    epilogue_vocab<uint16_t, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, live, g.head.row_map);
   } else if constexpr (EPI == kEpiHeadX || EPI == kEpiHeadW) {
     epilogue_head<EPI == kEpiHeadX, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, EPI == kEpiHeadX ? live : g.M);
   } else if constexpr (EPI == kEpiStore && AKIND == kOpMN) {      // dW from a dense store: fp32 out

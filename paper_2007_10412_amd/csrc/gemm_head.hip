@@ -51,6 +51,7 @@ template <typename T, int AKIND, int BKIND, int EPI> hipError_t run_head(const G
   if (e != hipSuccess || g.dry_run) return e;
   if constexpr (sizeof(T) == 2) {
     if (g.head.tile == 256) {
+      if (EPI == kEpiVocab && (g.head.list_out || g.k_splits > 1)) return hipErrorInvalidValue;
       static bool prepared = false;
       return launch_sized(gemm_dma64_bf16_kernel<AKIND, BKIND, EPI, 256, 256>, &prepared, GemmDma64Smem<EPI, 256, 256>::BYTES, 256, 256, g, st);
     }

@@ -17,10 +17,29 @@ __device__ __forceinline__ int own_row_list(const HeadArgs& h, int classes, int3
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(up, o); if (lane >= o) up += v; }
   if (lane == 63) s_n[w] = up;
+  if (write && h.weight) {
+    float m = 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) if ((mine >> q) & 1u) m = fmaxf(m, fabsf(h.weight[r0 + q]));
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if (lane == 0) s_list[w] = (int32_t)__float_as_uint(m);
+  }
   __syncthreads();
   int at = up - n, all = 0;
 #pragma unroll
   for (int q = 0; q < kGemmThreads / 64; ++q) { if (q < w) at += s_n[q]; all += s_n[q]; }
+  if (write) {
+    if (threadIdx.x == 0) {
+      const float inv = h.inv_count_out ? (all > 0 ? 1.f / (float)all : 0.f) : h.weight ? 0.f : *h.inv_count;
+      float m = 0.f;
+      if (h.weight) for (int q = 0; q < kGemmThreads / 64; ++q) m = fmaxf(m, __uint_as_float((uint32_t)s_list[q]));
+      *h.live_out = all;
+      if (h.inv_count_out) *h.inv_count_out = inv;
+      *h.common_out = h.temperature * (h.weight ? m : inv);
+    }
+    __syncthreads();
+  }
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int r = r0 + q;
@@ -29,10 +48,6 @@ __device__ __forceinline__ int own_row_list(const HeadArgs& h, int classes, int3
     if (c) s_list[at] = r;
     if (write) h.list_out[c ? at : all + (r - at)] = r;      // (r - at rows before this one do not count)
     at += c ? 1 : 0;
-  }
-  if (write && threadIdx.x == 0) {
-    *h.live_out = all;
-    if (h.inv_count_out) *h.inv_count_out = all > 0 ? 1.f / (float)all : 0.f;
   }
   __syncthreads();
   return all;
@@ -152,25 +167,27 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
       for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
     m = fmaxf(m, __shfl_xor(m, 32));
     const float from = m == -INFINITY ? 0.f : m;
-    T* const crow = ct + (wm0 + i * 32 + lr) * CP + wn0 + hh * 4;
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float below[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float d = acc[i][j][4 * q + e] - from;
-          s += __builtin_amdgcn_exp2f(d * c);
-          below[e] = kCodes ? d * c_code : acc[i][j][4 * q + e];
-        }
-        if (!g.y) continue;
-        if constexpr (!kCodes) *reinterpret_cast<floatx4*>(crow + j * 32 + q * 8) = floatx4{below[0], below[1], below[2], below[3]};
-        else
-          *reinterpret_cast<u32x2*>(crow + j * 32 + q * 8) = u32x2{code_pair(below[0], below[1]), code_pair(below[2], below[3])};
+      for (int e = 0; e < 16; ++e) {
+        const float d = acc[i][j][e] - from;
+        s += __builtin_amdgcn_exp2f(d * c);
+        if (kCodes) acc[i][j][e] = d * c_code;
       }
     s += __shfl_xor(s, 32);
     if (there && hh == 0) *reinterpret_cast<float2*>(h.stats + ((int64_t)part * h.stats_ld + place) * 2) = make_float2(m, s);
+    if (g.y) {
+      T* const crow = ct + (wm0 + i * 32 + lr) * CP + wn0 + hh * 4;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float v0 = acc[i][j][4 * q], v1 = acc[i][j][4 * q + 1], v2 = acc[i][j][4 * q + 2], v3 = acc[i][j][4 * q + 3];
+          if constexpr (kCodes) *reinterpret_cast<u32x2*>(crow + j * 32 + q * 8) = u32x2{code_pair(v0, v1), code_pair(v2, v3)};
+          else *reinterpret_cast<floatx4*>(crow + j * 32 + q * 8) = floatx4{v0, v1, v2, v3};
+        }
+    }
     __builtin_amdgcn_sched_barrier(0);
   }
   if (!g.y) return;
@@ -205,20 +222,19 @@ template <bool X, int BM, int BN, int TM, int TN>
 __device__ __forceinline__ void epilogue_head(const GemmArgs& g, floatx16 (&acc)[TM][TN], uint16_t* ct, int m0, int n0, int wm0,
                                               int wn0, int rows) {
   const int lane = threadIdx.x & 63;
-  if (g.c_dtype == kF32) {                               // (partial sums of either return before)
-    if (X) {
+  const float common = *g.head.common;                   // (partial sums of either return before)
+  if (g.c_dtype == kF32) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int place = m0 + wm0 + i * 32 + acc_row(e, lane);
-          if (place >= rows) continue;
-          float* const dst = static_cast<float*>(g.C) + (int64_t)g.head.row_map[place] * g.ldc + n0 + wn0 + (lane & 31);
+      for (int e = 0; e < 16; ++e) {
+        const int place = m0 + wm0 + i * 32 + acc_row(e, lane);
+        if (place >= rows) continue;
+        float* const dst = static_cast<float*>(g.C) + (int64_t)(X ? g.head.row_map[place] : place) * g.ldc + n0 + wn0 + (lane & 31);
 #pragma unroll
-          for (int j = 0; j < TN; ++j) if (n0 + wn0 + j * 32 + (lane & 31) < g.N) dst[j * 32] = acc[i][j][e];
-        }
-    } else if (g.beta) epilogue_store<TM, TN, float, true, false, true, false>(g, acc, m0, n0, wm0, wn0);
-    else epilogue_store<TM, TN, float, true, false, false, false>(g, acc, m0, n0, wm0, wn0);
+        for (int j = 0; j < TN; ++j)
+          if (n0 + wn0 + j * 32 + (lane & 31) < g.N) dst[j * 32] = acc[i][j][e] * common + (!X && g.beta ? dst[j * 32] : 0.f);
+      }
     return;
   }
   constexpr int CP = BN + 8;
@@ -231,7 +247,7 @@ __device__ __forceinline__ void epilogue_head(const GemmArgs& g, floatx16 (&acc)
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         uint16_t st[2];
-        put_pair(st, acc[i][j][e], acc[i][j][e + 1]);
+        put_pair(st, acc[i][j][e] * common, acc[i][j][e + 1] * common);
         cbase[r0 * CP + j * 32] = st[0];
         cbase[(r0 + 1) * CP + j * 32] = st[1];
       }

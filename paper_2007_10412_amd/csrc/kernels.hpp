@@ -61,7 +61,9 @@ struct HeadArgs {
   const int32_t* live;          // length of the list
   // kEpiVocab with few rows: the list is made here, by every workgroup for itself, and written by one (rows <= kOwnListRows)
   const int32_t* counts;        // which rows count, where there are no labels
-  int32_t* list_out; int32_t* live_out; float* inv_count_out;   // list_out null: the list is there (inv_count_out may be null)
+  int32_t* list_out; int32_t* live_out; float* inv_count_out;   // list_out null: the list is there; the others as in launch_row_list
+  float* common_out; const float* weight; const float* inv_count; float temperature;
+  const float* common;          // kEpiHeadX, kEpiHeadW: factor of the product
   const int32_t* row_map;       // row of x and dX of every place in the list (kEpiVocab: of A; kEpiHeadX: of C)
   const void* whole; int rows;  // rows of the batch; kEpiHeadW: what A is where the list has them all
   int tile;
@@ -316,14 +318,18 @@ hipError_t launch_vocab_rows(const VocabRows& a, hipStream_t st);
 hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, hipStream_t st);
 
 // ---- the layer under such a loss, fp32 or bf16 (vocab_head.hip), around the products with HeadArgs
-// list [rows]: the rows that count, in order, then the others; *live: how many count; *inv_count (nullable): 1 / that
-hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, hipStream_t st);
+// list [rows]: the rows that count, in order, then the others; *live: how many count; *inv_count: 1 / that (null: *t.inv_count
+// is there); *common = T x (the largest |weight| of these rows, or, without weights, the inverse count): what dX, dW and dbias
+// are multiplied by at their ends.  dz holds row gradients of weight 1 (or a share of 1): a factor that all rows have in common,
+// rounded into each of them, would put its one rounding error on the whole gradient (0.3 % of dW where 1 / n falls badly).
+hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, float* common,
+                           hipStream_t st);
 // first [rows][first_ld]: how many of a row's (sorted) entries lie before class `part` t, t = 0 .. parts
 hipError_t launch_list_parts(const int32_t* index, int rows, int k, int part, int parts, uint16_t* first, int first_ld, hipStream_t st);
 // kEpiVocab's work on the partial sums of a product with a split K, which that epilogue has left in C; parts are 64 wide
 hipError_t launch_vocab_join(int dtype, const GemmArgs& g, hipStream_t st);
 // After the logits' product, for every place of the list: the row's loss, its maximum top and what its exponentials
-// 2^((z - top) c) are multiplied by, factor = weight T / their sum.  For dW the rows of x side by side (xs, rows x_ld apart),
+// 2^((z - top) c) are multiplied by, factor = share / their sum, share = weight T / *common.  For dW the rows of x side by side (xs, rows x_ld apart),
 // unless the list has them all.  Rows that do not count: no loss, dX zero.
 struct VocabFinish {
   int dtype;
@@ -335,30 +341,43 @@ struct VocabFinish {
   float* row_loss;              // [rows], in the batch's order
   float* loss;                  // the sum over these rows, or null: left to another call
   float* top; float* factor;    // [place]
+  const float* common;
   void* z; int64_t z_ld;        // the logits (bf16: their codes), which launch_vocab_gradient turns into dz; null: forward only
   const uint16_t* first; int first_ld;
   const void* x; int64_t x_ld; int d_in; void* xs;   // rows of x of whole 16-byte vectors; xs null: no dW
   void* dx;                     // rows d_in apart; null: no dX
 };
 hipError_t launch_vocab_finish(const VocabFinish& a, hipStream_t st);
-// dz = factor 2^((z - top) c) - weight T p in the layer's type, in the place of z; columns classes .. z_ld - 1 become zeros
+// dz / *common = factor 2^((z - top) c) - share p in the layer's type, in the place of z; columns classes .. z_ld - 1 become zeros
 hipError_t launch_vocab_gradient(const VocabFinish& a, hipStream_t st);
 // whether one of those two writes *loss
 bool vocab_loss_inside(const VocabFinish& a);
-// out[map[i]] (rows out_ld apart; map null: i) (+)= sum of `splits` arrays' row i (rows in_ld apart, arrays stride apart),
+// out[map[i]] (rows out_ld apart; map null: i) (+)= *scale x sum of `splits` arrays' row i (rows in_ld apart, arrays stride apart),
 // i < min(rows, *live); live null: rows
 struct SplitSum {
   const float* in; int splits; int64_t stride, in_ld;
-  int rows, cols; const int32_t* live; const int32_t* map;
+  int rows, cols; const int32_t* live; const int32_t* map; const float* scale;
   void* out; int out_dtype; int64_t out_ld; int beta;
 };
 hipError_t launch_split_sum(const SplitSum& a, hipStream_t st);
-// out [cols] (+)= sum over the first *live rows of g[i][c]; part: [kHeadColsumSplits][cols]
+// out [cols] (+)= *scale x sum over the first *live rows of g[i][c]; part: [kHeadColsumSplits][cols]
 constexpr int kHeadColsumSplits = 32;
-hipError_t launch_head_colsum(int dtype, const void* g, int64_t g_ld, const int32_t* live, int cols, float* part,
+hipError_t launch_head_colsum(int dtype, const void* g, int64_t g_ld, const int32_t* live, const float* scale, int cols, float* part,
                               float* out, int beta, hipStream_t st);
 // rows of any width and alignment to rows out_ld apart (whole 16-byte vectors), zeros past cols
 hipError_t launch_pad_rows(int dtype, const void* in, int64_t rows, int cols, void* out, int64_t out_ld, hipStream_t st);
+
+// A small layer under a loss over up to 16 classes, everything in two kernels (vocab_small.hip).  dz [rows][kFewClasses] fp32 is
+// scratch, null where neither dW nor dbias is asked for.
+constexpr int kFewClasses = 16;
+struct FewClasses {
+  int dtype, rows, d_in, classes;
+  const void* x; const void* W; const float* bias;
+  VocabTargets t;
+  float* row_loss; float* loss;
+  void* dx; float* dz; void* dw; int dw_dtype; float* dbias; int beta;
+};
+hipError_t launch_few_classes(const FewClasses& a, hipStream_t st);
 
 // Ceiling probes (ceilings.hip): kind 0 HBM read, 1 HBM copy, 2 / 3 bf16 MFMA 32x32x16 / 16x16x32 register loops,
 // 4 fp32 MFMA 32x32x2, 5 integer 32 x 32 -> 64 multiply-adds.  a: operands (probe_min_bytes at least), b: sink

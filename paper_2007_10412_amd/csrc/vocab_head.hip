@@ -15,7 +15,8 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // ------------------------------------------------------------------ the list of rows
 // One workgroup: a thread has 8 consecutive rows of 8192 at a time, and places them by a count over the threads before it.
 __global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows, int classes, int32_t* __restrict__ list,
-                                                        int32_t* __restrict__ live, float* __restrict__ inv_count) {
+                                                        int32_t* __restrict__ live, float* __restrict__ inv_count,
+                                                        float* __restrict__ common) {
   __shared__ int s_n[16];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   auto counts = [&](int r) { return t.labels ? (uint32_t)t.labels[r] < (uint32_t)classes : t.counts[r] != 0; };
@@ -55,9 +56,21 @@ __global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows
     }
     before += all;
   }
+  float m = 0.f;
+  if (t.weight) {
+    for (int r = threadIdx.x; r < rows; r += 1024) if (counts(r)) m = fmaxf(m, fabsf(t.weight[r]));
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    __syncthreads();
+    if (lane == 0) s_n[w] = (int)__float_as_uint(m);
+    __syncthreads();
+    for (int q = 0; q < 16; ++q) m = fmaxf(m, __uint_as_float((uint32_t)s_n[q]));
+  }
   if (threadIdx.x == 0) {
+    const float inv = inv_count ? (total > 0 ? 1.f / (float)total : 0.f) : t.weight ? 0.f : *t.inv_count;
     *live = total;
-    if (inv_count) *inv_count = total > 0 ? 1.f / (float)total : 0.f;
+    if (inv_count) *inv_count = inv;
+    *common = t.temperature * (t.weight ? m : inv);
   }
 }
 
@@ -128,6 +141,11 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(GemmArgs g) {
   }
 }
 
+// a row's share of *common
+__device__ __forceinline__ float row_share(const VocabTargets& t, int row, float common) {
+  return !t.weight ? 1.f : common > 0.f ? t.weight[row] * t.temperature / common : 0.f;
+}
+
 // (maximum, sum of exponentials from it) of two parts; one with nothing in it adds its 0, or its NaN
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2, float c) {
   if (m2 == -INFINITY) { s += s2; return; }
@@ -189,7 +207,7 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinis
       const float loss = T1 * T1 * ((t.labels ? 0.f : t.entropy[row]) + (logf(s) + ((top - z0) - dot) / T1));
       a.row_loss[row] = loss;
       a.top[place] = top;
-      a.factor[place] = weight * T1 / s;
+      a.factor[place] = row_share(t, row, *a.common) / s;
       part = weight * loss;
     } else if (place < a.rows) {
       a.row_loss[row] = 0.f;
@@ -291,7 +309,7 @@ __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int 
     const uint16_t* const fr = a.first + (int64_t)row * a.first_ld;
     t0 = fr[c0 >> shift]; t1 = fr[min((c0 + kCols) >> shift, a.parts)];
   }
-  const float wt = (t.weight ? t.weight[row] : *t.inv_count) * t.temperature;
+  const float wt = row_share(t, row, *a.common);
   for (int j = t0 + l; j < t1; j += 16) {
     const float pj = t.labels ? 1.f : t.prob[(int64_t)row * t.k + j];
     if (pj == 0.f) continue;
@@ -317,6 +335,9 @@ __global__ __launch_bounds__(256) void split_sum_kernel(SplitSum a) {
     for (int e = 0; e < 4; ++e) v[e] += w[e];
   }
   const int64_t at = (int64_t)(a.map ? a.map[row] : row) * a.out_ld + c;
+  const float f = *a.scale;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] *= f;
   if (a.out_dtype == kF32) {
     float* const o = static_cast<float*>(a.out) + at;
     if (c + 4 <= a.cols && !a.beta) { __builtin_memcpy(o, &v, 16); return; }
@@ -362,12 +383,13 @@ __global__ __launch_bounds__(256) void head_colsum_kernel(const T* __restrict__ 
     if (col < cols) part[(int64_t)blockIdx.y * cols + col] = (s_sum[0][q] + s_sum[1][q]) + (s_sum[2][q] + s_sum[3][q]);
   }
 }
-__global__ __launch_bounds__(256) void head_colsum_final_kernel(const float* __restrict__ part, int cols, float* __restrict__ out, int beta) {
+__global__ __launch_bounds__(256) void head_colsum_final_kernel(const float* __restrict__ part, int cols, const float* __restrict__ scale,
+                                                                float* __restrict__ out, int beta) {
   const int c = blockIdx.x * 256 + threadIdx.x;
   if (c >= cols) return;
-  float s = beta ? out[c] : 0.f;
+  float s = 0.f;
   for (int q = 0; q < kHeadColsumSplits; ++q) s += part[(int64_t)q * cols + c];
-  out[c] = s;
+  out[c] = (beta ? out[c] : 0.f) + *scale * s;
 }
 
 template <typename T>
@@ -390,8 +412,9 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const T* __restrict__ in,
 
 }  // namespace
 
-hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, hipStream_t st) {
-  hipLaunchKernelGGL(row_list_kernel, dim3(1), dim3(1024), 0, st, t, rows, classes, list, live, inv_count);
+hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, float* common,
+                           hipStream_t st) {
+  hipLaunchKernelGGL(row_list_kernel, dim3(1), dim3(1024), 0, st, t, rows, classes, list, live, inv_count, common);
   return hipGetLastError();
 }
 hipError_t launch_list_parts(const int32_t* index, int rows, int k, int part, int parts, uint16_t* first, int first_ld, hipStream_t st) {
@@ -440,13 +463,13 @@ hipError_t launch_split_sum(const SplitSum& a, hipStream_t st) {
   hipLaunchKernelGGL(split_sum_kernel, dim3((a.cols + 1023) / 1024, a.rows), dim3(256), 0, st, a);
   return hipGetLastError();
 }
-hipError_t launch_head_colsum(int dtype, const void* g, int64_t g_ld, const int32_t* live, int cols, float* part, float* out,
-                              int beta, hipStream_t st) {
+hipError_t launch_head_colsum(int dtype, const void* g, int64_t g_ld, const int32_t* live, const float* scale, int cols, float* part,
+                              float* out, int beta, hipStream_t st) {
   const int W = dtype == kBF16 ? 512 : 256;
   const dim3 grid((cols + W - 1) / W, kHeadColsumSplits);
   if (dtype == kBF16) hipLaunchKernelGGL(head_colsum_kernel<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)g, g_ld, live, cols, part);
   else hipLaunchKernelGGL(head_colsum_kernel<float>, grid, dim3(256), 0, st, (const float*)g, g_ld, live, cols, part);
-  hipLaunchKernelGGL(head_colsum_final_kernel, dim3((cols + 255) / 256), dim3(256), 0, st, part, cols, out, beta);
+  hipLaunchKernelGGL(head_colsum_final_kernel, dim3((cols + 255) / 256), dim3(256), 0, st, part, cols, scale, out, beta);
   return hipGetLastError();
 }
 hipError_t launch_pad_rows(int dtype, const void* in, int64_t rows, int cols, void* out, int64_t out_ld, hipStream_t st) {

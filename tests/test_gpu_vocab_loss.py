@@ -636,3 +636,38 @@ def test_training_step_of_two_layers(dtype):
     assert rel_err(g0.cpu().numpy(), (x.double().t().contiguous() @ dhd).cpu().numpy()) < tol
     moved = (master if dtype else [p0, p1])
     assert rel_err(moved[1].cpu().numpy(), (w1 - 0.5 * (hd.t().contiguous() @ dz)).cpu().numpy()) < tol
+
+
+@pytest.mark.parametrize("rows,d_in,classes", [(463, 256, 3990), (455, 300, 30000)])
+@pytest.mark.parametrize("how", ["mean", "weight", "temperature"])
+def test_a_common_factor_is_not_rounded(rows, d_in, classes, how):
+    """A factor of all rows (1 / n, a weight that they share, T) belongs to the fp32 ends of the gradients: rounded to bf16 into
+    every dz, its error of up to 2^-9 would be that of all of dX and dW.  Seen as the scale of what comes out along what should:
+    the roundings that are left are independent ones, of 2^-8 at most, over 10^5 elements and more, whose share of that scale is
+    8 standard deviations of 2^-8 / sqrt(10^5) < 2^-13 at most; targets near -1 and 0.5 themselves round by less than 2^-11 of
+    the whole (1 - q and 0.5 - q with q of a few thousandths)."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, d_in, device="cuda", generator=gen).to(torch.bfloat16)
+    W = (torch.randn(d_in, classes, device="cuda", generator=gen) / math.sqrt(d_in)).to(torch.bfloat16)
+    index = torch.stack([torch.arange(rows, device="cuda"), torch.arange(rows, device="cuda") + rows], dim=1).to(torch.int32)
+    logit = torch.zeros(rows, 2, device="cuda")
+    T = 0.7 if how == "temperature" else 1.0
+    weight = torch.full((rows,), 0.3003, device="cuda") if how == "weight" else None
+    layer = B.make_layer(rows, d_in, classes, dtype=B.RAD_BF16, relu=False)
+    xd, Wd = x.double(), W.double()
+    with Ctx() as ctx:
+        for kind in ("ce", "distill"):
+            dX, dW = torch.empty_like(x), torch.empty(d_in, classes, device="cuda")
+            if kind == "ce":
+                labels = index[:, 0].contiguous()
+                B.rad_linear_ce(ctx, layer, x, W, None, labels, row_weight=weight, dX=dX, dW=dW)
+                _, _, dz, _, _ = definition(xd @ Wd, lists(labels=labels, classes=classes), weight, 1.0)
+            else:
+                B.rad_linear_distill(ctx, layer, x, W, None, B.make_teacher(index, logit, T), row_weight=weight, dX=dX, dW=dW)
+                _, _, dz, _, _ = definition(xd @ Wd, lists(teacher=(index, logit), classes=classes, T=T), weight, T)
+            B.rad_ctx_synchronize(ctx)
+            for got, want in ((dX, dz @ Wd.t().contiguous()), (dW, xd.t().contiguous() @ dz)):
+                scale = float((got.double() * want).sum() / (want * want).sum())
+                assert abs(scale - 1) < 2.0 ** -11 + 2.0 ** -13, (kind, how, scale)
