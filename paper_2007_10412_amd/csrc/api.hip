@@ -1437,8 +1437,8 @@ static rad_status check_teacher(rad_ctx* c, const rad_teacher* t) {
 
 // What the rows are to learn, made ready for the kernels, and room for their losses where the caller wants none.  count: how
 // many rows there are to learn from is counted here (not where another kernel does).
-static rad_status vocab_targets(rad_ctx* c, const int32_t* labels, const rad_teacher* teacher, const float* weight,
-                                int rows, int classes, bool count, VocabTargets* t, float** row_loss) {
+static rad_status vocab_targets(rad_ctx* c, const int32_t* labels, const rad_teacher* teacher, const float* weight, int rows, int classes,
+                                bool count, VocabTargets* t, float** row_loss, uint16_t* first = nullptr, int part = 0, int parts = 0) {
   const size_t lists = teacher ? (size_t)rows * teacher->k : 0;
   char* ws = nullptr;
   RAD_TRY(ws_get(c, WS_TARGETS, 256 + (size_t)rows * 12 + lists * 8, reinterpret_cast<void**>(&ws)));
@@ -1454,7 +1454,8 @@ static rad_status vocab_targets(rad_ctx* c, const int32_t* labels, const rad_tea
     t->index = index; t->prob = prob; t->entropy = entropy; t->counts = counts;
     t->k = teacher->k; t->temperature = (float)teacher->temperature;
     HIP_TRY(c, timed(c, "teacher", [&](const char**) {
-      return launch_teacher(teacher->index, teacher->logit, rows, teacher->k, classes, t->temperature, index, prob, entropy, counts, c->stream);
+      return launch_teacher(teacher->index, teacher->logit, rows, teacher->k, classes, t->temperature, index, prob, entropy, counts, first,
+                            part, parts, c->stream);
     }));
   }
   if (!weight && count)
@@ -1621,9 +1622,6 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   if (piece > rows) piece = rows;
   const bool one = piece >= rows;
 
-  VocabTargets t;
-  float* losses = h.row_loss;
-  RAD_TRY(vocab_targets(c, labels, teacher, row_weight, rows, d_out, !one, &t, &losses));
   const void *W = nullptr, *x = nullptr;
   // (a copy's rows are whole cache lines: the tiles' 256-byte pieces of them then take two lines, not three)
   const int64_t w_ld = vp8 == d_out && (reinterpret_cast<uintptr_t>(h.W) & 15) == 0 ? d_out : vp;
@@ -1632,10 +1630,10 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
 
   const HeadPlan fwd = head_plan(dtype, kEpiVocab, piece, d_out, d_in, true);
   const int part = fwd.splits > 1 ? 64 : head_part(fwd.tile), parts = (d_out + part - 1) / part;
-  const int first_ld = parts + 1;
-  const size_t first_bytes = t.labels ? 0 : ((size_t)rows * first_ld * 2 + 255) / 256 * 256;
+  const int first_ld = parts + 1, list_k = teacher ? teacher->k : 1;
+  const size_t first_bytes = teacher ? ((size_t)rows * first_ld * 2 + 255) / 256 * 256 : 0;
   char* ws = nullptr;
-  RAD_TRY(ws_get(c, WS_ROWLOSS, 256 + first_bytes + (size_t)piece * (8 * (size_t)parts + 12 + 4 * (size_t)t.k), reinterpret_cast<void**>(&ws)));
+  RAD_TRY(ws_get(c, WS_ROWLOSS, 256 + first_bytes + (size_t)piece * (8 * (size_t)parts + 12 + 4 * (size_t)list_k), reinterpret_cast<void**>(&ws)));
   int32_t* const live = reinterpret_cast<int32_t*>(ws);
   float* const common = reinterpret_cast<float*>(ws) + 1;
   uint16_t* const first = reinterpret_cast<uint16_t*>(ws + 256);
@@ -1644,8 +1642,9 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   float* const top = reinterpret_cast<float*>(list + piece);
   float* const factor = top + piece;
   float* const target = factor + piece;
-  if (!t.labels)
-    HIP_TRY(c, timed(c, "list_parts", [&](const char**) { return launch_list_parts(t.index, rows, t.k, part, parts, first, first_ld, c->stream); }));
+  VocabTargets t;
+  float* losses = h.row_loss;
+  RAD_TRY(vocab_targets(c, labels, teacher, row_weight, rows, d_out, !one, &t, &losses, first, part, parts));
 
   const bool cast = h.dW && h.dw_dtype == kBF16 && (!one || h.beta != 0.f);     // sums of several pieces are kept in fp32
   float* dW32 = h.dw_dtype == kBF16 ? nullptr : static_cast<float*>(h.dW);

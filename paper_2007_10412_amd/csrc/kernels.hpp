@@ -293,9 +293,9 @@ struct VocabTargets {
 };
 constexpr int kTeacherMax = 1024;                     // longest list
 // lists sorted, joined and turned into probabilities (softmax of logit / temperature over the entries in [0, classes) whose
-// logit is not -inf)
-hipError_t launch_teacher(const int32_t* index, const float* logit, int rows, int k, int classes, float temperature,
-                          int32_t* index_out, float* prob, float* entropy, int32_t* counts, hipStream_t st);
+// logit is not -inf); first [rows][parts + 1] (nullable): how many of a row's entries lie before class `part` t, t = 0 .. parts
+hipError_t launch_teacher(const int32_t* index, const float* logit, int rows, int k, int classes, float temperature, int32_t* index_out,
+                          float* prob, float* entropy, int32_t* counts, uint16_t* first, int part, int parts, hipStream_t st);
 // *inv_count = 1 / rows that count (0 where none does)
 hipError_t launch_count_rows(const VocabTargets& t, int rows, int classes, float* inv_count, hipStream_t st);
 // loss = sum over rows of weight x row_loss, added in a fixed order
@@ -324,8 +324,6 @@ hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, 
 // rounded into each of them, would put its one rounding error on the whole gradient (0.3 % of dW where 1 / n falls badly).
 hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, float* common,
                            hipStream_t st);
-// first [rows][first_ld]: how many of a row's (sorted) entries lie before class `part` t, t = 0 .. parts
-hipError_t launch_list_parts(const int32_t* index, int rows, int k, int part, int parts, uint16_t* first, int first_ld, hipStream_t st);
 // kEpiVocab's work on the partial sums of a product with a split K, which that epilogue has left in C; parts are 64 wide
 hipError_t launch_vocab_join(int dtype, const GemmArgs& g, hipStream_t st);
 // After the logits' product, for every place of the list: the row's loss, its maximum top and what its exponentials

@@ -74,22 +74,6 @@ __global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows
   }
 }
 
-// a wave per row: entry j (ascending, -1 at the end) is before class part t for every t past its own part
-__global__ __launch_bounds__(256) void list_parts_kernel(const int32_t* __restrict__ index, int rows, int k, int part, int parts,
-                                                         uint16_t* __restrict__ first, int first_ld) {
-  const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  const int32_t* const e = index + (int64_t)row * k;
-  for (int t = lane; t <= parts; t += 64) {
-    int lo = 0, hi = k;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if ((uint32_t)e[mid] < (uint32_t)t * (uint32_t)part) lo = mid + 1; else hi = mid;     // (-1 lies after every class)
-    }
-    first[(int64_t)row * first_ld + t] = (uint16_t)lo;
-  }
-}
-
 // ------------------------------------------------------------------ between the products
 // What epilogue_vocab does, on partial sums: 16 lanes have 64 columns of a row, four each.
 template <typename T>
@@ -415,10 +399,6 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const T* __restrict__ in,
 hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, float* common,
                            hipStream_t st) {
   hipLaunchKernelGGL(row_list_kernel, dim3(1), dim3(1024), 0, st, t, rows, classes, list, live, inv_count, common);
-  return hipGetLastError();
-}
-hipError_t launch_list_parts(const int32_t* index, int rows, int k, int part, int parts, uint16_t* first, int first_ld, hipStream_t st) {
-  hipLaunchKernelGGL(list_parts_kernel, dim3((rows + 3) / 4), dim3(256), 0, st, index, rows, k, part, parts, first, first_ld);
   return hipGetLastError();
 }
 hipError_t launch_vocab_join(int dtype, const GemmArgs& g, hipStream_t st) {

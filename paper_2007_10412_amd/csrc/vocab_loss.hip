@@ -74,7 +74,7 @@ template <int P>
 __global__ __launch_bounds__(256) void teacher_kernel(const int32_t* __restrict__ index, const float* __restrict__ logit, int rows,
                                                       int k, int classes, float inv_t, int32_t* __restrict__ index_out,
                                                       float* __restrict__ prob, float* __restrict__ entropy,
-                                                      int32_t* __restrict__ counts) {
+                                                      int32_t* __restrict__ counts, uint16_t* __restrict__ first, int part, int parts) {
   __shared__ uint64_t s_key[4][P];
   __shared__ float s_p[4][P];
   constexpr uint64_t kNone = ~0ull;
@@ -138,6 +138,16 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int32_t* __restrict_
     prob[at + j] = sum;
   }
   if (lane == 0) { entropy[row] = some ? h : 0.f; counts[row] = some ? 1 : 0; }
+  if (!first) return;
+  // entries before class part t (missing ones lie after all); a kernel of its own for this: 200 x 768 x 10007, k = 16 174 us, not 170
+  for (int t = lane; t <= parts; t += 64) {
+    int lo = 0, hi = k;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if ((uint32_t)(key[mid] >> 32) < (uint32_t)t * (uint32_t)part) lo = mid + 1; else hi = mid;
+    }
+    first[(int64_t)row * (parts + 1) + t] = (uint16_t)lo;
+  }
 }
 
 __global__ __launch_bounds__(1024) void count_rows_kernel(VocabTargets t, int rows, int classes, float* __restrict__ inv_count) {
@@ -410,10 +420,10 @@ hipError_t rows_any(const VocabRows& a, hipStream_t st) {
 }
 
 template <int P>
-hipError_t teacher_of(const int32_t* index, const float* logit, int rows, int k, int classes, float temperature,
-                      int32_t* index_out, float* prob, float* entropy, int32_t* counts, hipStream_t st) {
+hipError_t teacher_of(const int32_t* index, const float* logit, int rows, int k, int classes, float temperature, int32_t* index_out,
+                      float* prob, float* entropy, int32_t* counts, uint16_t* first, int part, int parts, hipStream_t st) {
   hipLaunchKernelGGL(teacher_kernel<P>, dim3((rows + 3) / 4), dim3(256), 0, st, index, logit, rows, k, classes,
-                     1.f / temperature, index_out, prob, entropy, counts);
+                     1.f / temperature, index_out, prob, entropy, counts, first, part, parts);
   return hipGetLastError();
 }
 
@@ -421,13 +431,11 @@ hipError_t teacher_of(const int32_t* index, const float* logit, int rows, int k,
 
 bool vocab_rows_count(const VocabRows& a) { return a.dz && !a.t.weight && a.rows <= 2048; }
 
-hipError_t launch_teacher(const int32_t* index, const float* logit, int rows, int k, int classes, float temperature,
-                          int32_t* index_out, float* prob, float* entropy, int32_t* counts, hipStream_t st) {
+hipError_t launch_teacher(const int32_t* index, const float* logit, int rows, int k, int classes, float temperature, int32_t* index_out,
+                          float* prob, float* entropy, int32_t* counts, uint16_t* first, int part, int parts, hipStream_t st) {
   if (k < 1 || k > kTeacherMax) return hipErrorInvalidValue;
-  if (k <= 64) return teacher_of<64>(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, st);
-  if (k <= 128) return teacher_of<128>(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, st);
-  if (k <= 256) return teacher_of<256>(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, st);
-  return teacher_of<1024>(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, st);
+  auto of = k <= 64 ? teacher_of<64> : k <= 128 ? teacher_of<128> : k <= 256 ? teacher_of<256> : teacher_of<1024>;
+  return of(index, logit, rows, k, classes, temperature, index_out, prob, entropy, counts, first, part, parts, st);
 }
 
 hipError_t launch_count_rows(const VocabTargets& t, int rows, int classes, float* inv_count, hipStream_t st) {
