@@ -306,8 +306,8 @@ typedef struct {
  * w_r = row_weight[r] (DEVICE [rows]), or, where that is null, 1 / the number
  * of rows whose list is not empty.  A row with an empty list has no loss and a
  * gradient of zeros, whatever its weight.  logits and dlogits [rows, classes]
- * in dtype; dlogits may be logits.  row_loss [rows] and loss [1]: fp32 on the
- * device.  Any of dlogits, row_loss, loss may be null, not all.  Statistics and
+ * in dtype; dlogits may be logits (outputs that overlap an input or each other in
+ * any other way are refused).  row_loss [rows] and loss [1]: fp32 on the device.  Any of dlogits, row_loss, loss may be null, not all.  Statistics and
  * sums are fp32, in a fixed order.  A logit of -infinity has probability zero;
  * a row of nothing else gives NaN.  Enqueued on the context's stream. */
 rad_status rad_distill_ce(rad_ctx* ctx, const void* logits, const rad_teacher* teacher, const float* row_weight,
@@ -332,14 +332,16 @@ rad_status rad_distill_ce(rad_ctx* ctx, const void* logits, const rad_teacher* t
  * workspaces: a copy of W or x where its rows are not whole 16-byte vectors (or
  * its address is no multiple of 16); for a bf16 dW of several pieces, or with
  * beta = 1, the fp32 sums [d_in, d_out]; partial sums where a product has few
- * tiles.  d_in * d_out < 2^32, both at most 2^22 - 64.  Enqueued on the
- * context's stream; results do not vary from call to call. */
+ * tiles.  d_in * d_out < 2^32, both at most 2^22 - 64.  Outputs overlap neither
+ * inputs nor each other.  Enqueued on the context's stream; results do not vary
+ * from call to call. */
 rad_status rad_linear_ce(rad_ctx* ctx, const rad_layer* layer, const void* x, const void* W, const float* bias,
                          const int32_t* labels, const float* row_weight, float* row_loss, float* loss, void* dX,
                          void* dW, int32_t dw_dtype, float* dbias, float beta);
 
 /* The same with a teacher's lists in the place of labels: the loss and dz of
- * rad_distill_ce on the logits of the layer. */
+ * rad_distill_ce on the logits of the layer.  Its workspaces hold 8 k + d_out / 32
+ * bytes a row besides. */
 rad_status rad_linear_distill(rad_ctx* ctx, const rad_layer* layer, const void* x, const void* W, const float* bias,
                               const rad_teacher* teacher, const float* row_weight, float* row_loss, float* loss,
                               void* dX, void* dW, int32_t dw_dtype, float* dbias, float beta);

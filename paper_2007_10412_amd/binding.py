@@ -298,30 +298,50 @@ def rad_softmax_ce(ctx, logits, labels, dtype, dlogits, loss_dev):
 
 
 def make_teacher(index, logit, temperature=1.0):
-    """index (int32) and logit (fp32) [rows, k]: device tensors, which the caller keeps until the calls that take the
-    teacher have been made."""
+    """index (int32) and logit (fp32) [rows, k]: device tensors, which the teacher holds on to."""
     import torch
     if index.dtype != torch.int32 or logit.dtype != torch.float32 or index.dim() != 2 or index.shape != logit.shape:
         raise RadError(RAD_ERR_SHAPE, "a teacher's lists are int32 and fp32 tensors [rows, k]")
-    _contiguous(index=index, logit=logit)
-    return rad_teacher(int(index.shape[1]), float(temperature), index.data_ptr(), logit.data_ptr())
+    if not index.is_contiguous() or not logit.is_contiguous():
+        raise RadError(RAD_ERR_SHAPE, "a teacher's lists are not contiguous")
+    teacher = rad_teacher(int(index.shape[1]), float(temperature), index.data_ptr(), logit.data_ptr())
+    teacher.lists = index, logit
+    return teacher
 
 
-def _contiguous(**tensors):
-    for name, t in tensors.items():
-        if t is not None and not t.is_contiguous():
-            raise RadError(RAD_ERR_SHAPE, name + " is not contiguous")
+def _check_tensors(*tensors):
+    """(name, tensor or None, elements, dtype or None: any) of what a call reads and writes"""
+    for name, t, n, dtype in tensors:
+        if t is not None and (t.numel() != n or not t.is_contiguous() or (dtype is not None and t.dtype != dtype)):
+            raise RadError(RAD_ERR_SHAPE, "%s is not a contiguous tensor of %d elements%s" % (
+                name, n, "" if dtype is None else " of " + str(dtype)))
+
+
+def _check_lists(teacher, rows):
+    if len(teacher.lists[0]) != rows:
+        raise RadError(RAD_ERR_SHAPE, "the teacher has %d rows, not %d" % (len(teacher.lists[0]), rows))
 
 
 def rad_distill_ce(ctx, logits, teacher, dtype, dlogits=None, row_weight=None, row_loss=None, loss=None):
+    import torch
     rows, classes = logits.shape
-    _contiguous(logits=logits, dlogits=dlogits, row_weight=row_weight, row_loss=row_loss)
+    f32, kind = torch.float32, {RAD_F32: torch.float32, RAD_BF16: torch.bfloat16}.get(dtype)
+    _check_lists(teacher, rows)
+    _check_tensors(("logits", logits, rows * classes, kind), ("dlogits", dlogits, rows * classes, kind),
+                   ("row_weight", row_weight, rows, f32), ("row_loss", row_loss, rows, f32), ("loss", loss, 1, f32))
     _check(ctx, lib().rad_distill_ce(ctx, _ptr(logits), C.byref(teacher), _ptr(row_weight), rows, classes, dtype,
                                      _ptr(dlogits), _ptr(row_loss), _ptr(loss)))
 
 
-def _head_args(row_weight, row_loss, loss, dX, dW, dbias, beta):
+def _head_args(layer, x, W, bias, row_weight, row_loss, loss, dX, dW, dbias, beta):
     import torch
+    n, d, v = layer.batch, layer.d_in, layer.d_out
+    f32, td = torch.float32, {RAD_F32: torch.float32, RAD_BF16: torch.bfloat16}.get(layer.dtype)
+    _check_tensors(("x", x, n * d, td), ("W", W, d * v, td), ("bias", bias, v, f32), ("row_weight", row_weight, n, f32),
+                   ("row_loss", row_loss, n, f32), ("loss", loss, 1, f32), ("dX", dX, n * d, td), ("dW", dW, d * v, None),
+                   ("dbias", dbias, v, f32))
+    if dW is not None and dW.dtype not in (f32, torch.bfloat16):
+        raise RadError(RAD_ERR_PARAM, "dW is fp32 or of the layer's type")
     kind = RAD_BF16 if dW is not None and dW.dtype == torch.bfloat16 else RAD_F32
     return _ptr(row_weight), _ptr(row_loss), _ptr(loss), _ptr(dX), _ptr(dW), kind, _ptr(dbias), beta
 
@@ -329,16 +349,17 @@ def _head_args(row_weight, row_loss, loss, dX, dW, dbias, beta):
 def rad_linear_ce(ctx, layer, x, W, bias, labels, row_weight=None, row_loss=None, loss=None, dX=None, dW=None, dbias=None,
                   beta=0.0):
     """dW: an fp32 tensor, or one of the layer's type."""
-    _contiguous(x=x, W=W, bias=bias, labels=labels, row_weight=row_weight, row_loss=row_loss, dX=dX, dW=dW, dbias=dbias)
+    import torch
+    _check_tensors(("labels", labels, layer.batch, torch.int32))
     _check(ctx, lib().rad_linear_ce(ctx, C.byref(layer), _ptr(x), _ptr(W), _ptr(bias), _ptr(labels),
-                                    *_head_args(row_weight, row_loss, loss, dX, dW, dbias, beta)))
+                                    *_head_args(layer, x, W, bias, row_weight, row_loss, loss, dX, dW, dbias, beta)))
 
 
 def rad_linear_distill(ctx, layer, x, W, bias, teacher, row_weight=None, row_loss=None, loss=None, dX=None, dW=None,
                        dbias=None, beta=0.0):
-    _contiguous(x=x, W=W, bias=bias, row_weight=row_weight, row_loss=row_loss, dX=dX, dW=dW, dbias=dbias)
+    _check_lists(teacher, layer.batch)
     _check(ctx, lib().rad_linear_distill(ctx, C.byref(layer), _ptr(x), _ptr(W), _ptr(bias), C.byref(teacher),
-                                         *_head_args(row_weight, row_loss, loss, dX, dW, dbias, beta)))
+                                         *_head_args(layer, x, W, bias, row_weight, row_loss, loss, dX, dW, dbias, beta)))
 
 
 def rad_model_create_mlp(ctx, dtype, batch, dims, has_bias, scheme, p):

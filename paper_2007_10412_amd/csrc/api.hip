@@ -1427,6 +1427,21 @@ struct DeviceGuard {
   ~DeviceGuard() { if (before >= 0) (void)hipSetDevice(before); }
 };
 
+// Memory that a call reads or writes (null: none).  A call's kernels run one after the other, so an input that an output lies
+// over would be read after it is written.
+struct Span { const void* p; size_t bytes; };
+static bool spans_meet(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+}
+template <size_t N, size_t M> static rad_status check_apart(rad_ctx* c, const Span (&out)[N], const Span (&in)[M]) {
+  for (size_t i = 0; i < N; ++i) {
+    for (size_t j = 0; j < i; ++j) if (spans_meet(out[i], out[j])) return fail(c, RAD_ERR_PARAM, "outputs overlap");
+    for (size_t j = 0; j < M; ++j) if (spans_meet(out[i], in[j])) return fail(c, RAD_ERR_PARAM, "an output overlaps an input");
+  }
+  return RAD_OK;
+}
+
 static rad_status check_teacher(rad_ctx* c, const rad_teacher* t) {
   if (!t || !t->index || !t->logit) return fail(c, RAD_ERR_NULL, "null teacher");
   if (t->k < 1 || t->k > kTeacherMax) return fail(c, RAD_ERR_SHAPE, "a teacher's lists hold 1 to 1024 entries");
@@ -1485,6 +1500,9 @@ extern "C" rad_status rad_distill_ce(rad_ctx* c, const void* logits, const rad_t
   if (!dlogits && !row_loss && !loss) return fail(c, RAD_ERR_NULL, "no output asked for");
   if (rows < 1 || classes < 1 || rows > (1 << 24) || classes > (1 << 24)) return fail(c, RAD_ERR_SHAPE, "bad shape");
   if (dtype != RAD_F32 && dtype != RAD_BF16) return fail(c, RAD_ERR_PARAM, "unknown dtype");
+  const size_t n = (size_t)rows, lists = n * teacher->k * 4, all = n * (size_t)classes * (dtype == RAD_F32 ? 4 : 2);
+  RAD_TRY(check_apart(c, {{dlogits, all}, {row_loss, n * 4}, {loss, 4}},
+                      {{dlogits == logits ? nullptr : logits, all}, {teacher->index, lists}, {teacher->logit, lists}, {row_weight, n * 4}}));
   DeviceGuard guard(c->device);
   VocabRows a;
   std::memset(&a, 0, sizeof(a));
@@ -1597,6 +1615,13 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   if (h.dW && h.dw_dtype != RAD_F32 && h.dw_dtype != L->dtype) return fail(c, RAD_ERR_PARAM, "dW is fp32 or of the layer's type");
   if (L->d_in * L->d_out >= ((int64_t)1 << 32)) return fail(c, RAD_ERR_SHAPE, "weights of 2^32 elements or more");
   if (std::max(L->d_in, L->d_out) > ((int64_t)1 << 22) - 64) return fail(c, RAD_ERR_SHAPE, "d_in or d_out above 2^22 - 64");
+  const size_t esize = L->dtype == RAD_F32 ? 4 : 2, xs_n = (size_t)L->batch * L->d_in, ws_n = (size_t)L->d_in * L->d_out;
+  const size_t lists = teacher ? (size_t)L->batch * teacher->k * 4 : 0;
+  RAD_TRY(check_apart(c, {{h.dX, xs_n * esize}, {h.dW, ws_n * (h.dw_dtype == RAD_F32 ? 4 : 2)}, {h.dbias, (size_t)L->d_out * 4},
+                          {h.row_loss, (size_t)L->batch * 4}, {h.loss, 4}},
+                      {{h.x, xs_n * esize}, {h.W, ws_n * esize}, {h.bias, (size_t)L->d_out * 4}, {labels, (size_t)L->batch * 4},
+                       {teacher ? teacher->index : nullptr, lists}, {teacher ? teacher->logit : nullptr, lists},
+                       {row_weight, (size_t)L->batch * 4}}));
   DeviceGuard guard(c->device);
   const int rows = (int)L->batch, d_in = (int)L->d_in, d_out = (int)L->d_out, dtype = L->dtype;
   if (few_classes_pay(rows, d_in, d_out)) {

@@ -671,3 +671,194 @@ def test_a_common_factor_is_not_rounded(rows, d_in, classes, how):
             for got, want in ((dX, dz @ Wd.t().contiguous()), (dW, xd.t().contiguous() @ dz)):
                 scale = float((got.double() * want).sum() / (want * want).sum())
                 assert abs(scale - 1) < 2.0 ** -11 + 2.0 ** -13, (kind, how, scale)
+
+
+# ------------------------------------------------------------------ what a call may meet
+# small layers of few classes, tiles of 64, 128 and 256 rows, products with a split K
+ROUTES = [(150, 300, 10), (40, 1024, 5000), (300, 512, 4096), (600, 256, 20000), (1100, 512, 1000)]
+
+
+def run_linear(ctx, layer, x, W, labels=None, teacher=None, weight=None, shift=0):
+    """All outputs, each a view `shift` elements into its memory."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+
+    def room(like, dtype=None):
+        t = torch.full((like.numel() + shift,), math.nan, device="cuda", dtype=dtype or like.dtype)
+        return t[shift:].view(like.shape)
+    one = torch.empty(1, device="cuda")
+    out = {"row_loss": room(x[:, 0], torch.float32), "loss": room(one), "dX": room(x), "dW": room(W), "dbias": room(W[0], torch.float32)}
+    if labels is not None:
+        B.rad_linear_ce(ctx, layer, x, W, None, labels, row_weight=weight, **out)
+    else:
+        B.rad_linear_distill(ctx, layer, x, W, None, teacher, row_weight=weight, **out)
+    B.rad_ctx_synchronize(ctx)
+    return out
+
+
+def inputs(dtype, rows, d_in, classes, seed=3):
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(rows, d_in, device="cuda", generator=gen).to(torch_dtype(dtype))
+    W = (torch.randn(d_in, classes, device="cuda", generator=gen) * (3 / math.sqrt(d_in))).to(torch_dtype(dtype))
+    return gen, x, W, B.make_layer(rows, d_in, classes, dtype=dtype, relu=False)
+
+
+def same(a, b, tag):
+    import torch
+    for n in a:
+        assert torch.equal(a[n], b[n]), "%s: %s" % (tag, n)
+        assert torch.isfinite(a[n].float()).all(), "%s: %s" % (tag, n)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,d_in,classes", ROUTES)
+def test_views_at_odd_addresses(dtype, rows, d_in, classes):
+    """Inputs and outputs that begin at any element give what others give, bit by bit."""
+    import torch
+    gen, x, W, layer = inputs(dtype, rows, d_in, classes)
+    labels = labels_for(rows, classes, gen, 0.2)
+
+    def moved(t):
+        m = torch.empty(t.numel() + 3, device="cuda", dtype=t.dtype)[3:].view(t.shape)
+        m.copy_(t)
+        return m
+    with Ctx() as ctx:
+        want = run_linear(ctx, layer, x, W, labels)
+        same(run_linear(ctx, layer, moved(x), moved(W), moved(labels), shift=1), want, "moved")
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,d_in,classes", ROUTES)
+@pytest.mark.parametrize("k", [0, 4])
+def test_rows_without_a_target_hold_anything(dtype, rows, d_in, classes, k):
+    """What x and the weights hold in such rows, and what an earlier call left in the workspaces, reaches no output."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen, x, W, layer = inputs(dtype, rows, d_in, classes)
+    labels = labels_for(rows, classes, gen, 0.3)
+    gone = (labels < 0) | (labels >= classes)
+    gone[-3:] = True
+    labels[-3:] = -1
+    assert gone.any() and not gone.all()
+    index, logit = teacher_for(rows, classes, k or 1, gen)
+    index[gone] = -1
+    weight = torch.randn(rows, device="cuda", generator=gen)
+    x[gone] = 0
+    bad_x, bad_weight = x.clone(), weight.clone()
+    bad_x[gone] = torch.tensor([math.nan, math.inf, -math.inf], device="cuda").to(x.dtype)[torch.arange(d_in, device="cuda") % 3]
+    bad_weight[gone] = math.nan
+    asked = dict(labels=labels) if not k else dict(teacher=B.make_teacher(index, logit, 1.5))
+    with Ctx() as ctx:
+        want = [run_linear(ctx, layer, x, W, weight=w, **asked) for w in (None, weight)]
+        got = [run_linear(ctx, layer, bad_x, W, weight=w, **asked) for w in (None, bad_weight)]
+        run_linear(ctx, layer, torch.full_like(x, math.nan), W, labels=torch.zeros_like(labels))
+        got += [run_linear(ctx, layer, bad_x, W, weight=w, **asked) for w in (None, bad_weight)]
+    for n, g in enumerate(got):
+        same(g, want[n % 2], "call %d" % n)
+        assert (g["dX"][gone] == 0).all() and (g["row_loss"][gone] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,dw_dtype", [(0, 0), (1, 0), (1, 1)])
+@pytest.mark.parametrize("rows,d_in,classes,k", [(1, 1, 16, 1), (37, 65, 16, 16), (1000, 99, 7, 3), (256, 390, 12, 0), (5, 3001, 2, 0), (33, 64, 1, 2)])
+def test_few_classes(dtype, dw_dtype, rows, d_in, classes, k):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    weight = torch.randn(rows, device="cuda", generator=gen)
+    with Ctx() as ctx:
+        for w, beta in ((None, 0.0), (None, 1.0), (weight, 0.0), (weight, 1.0)):
+            check_linear(ctx, dtype, rows, d_in, classes, bias=beta == 0.0, k=k, T=1.0 if not k else 1.7, ignored=0.3, missing=0.2,
+                         weight=w, beta=beta, dw_dtype=dw_dtype)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,d_in,classes,k", [(1100, 64, 520, 3), (8192, 40, 130, 0), (8193, 40, 130, 2), (20000, 24, 77, 0), (17000, 16, 33, 5)])
+def test_many_rows(dtype, rows, d_in, classes, k):
+    """Lists of rows that one workgroup makes in one step, and in several."""
+    import torch
+    weight = torch.randn(rows, device="cuda", generator=torch.Generator(device="cuda").manual_seed(rows))
+    with Ctx() as ctx:
+        for w in (None, weight):
+            check_linear(ctx, dtype, rows, d_in, classes, bias=True, k=k, T=1.0 if not k else 2.0, ignored=0.3, missing=0.2, weight=w)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,d_in,classes,k", [(3, 2048, 1500, 0), (3, 2048, 1500, 9), (40, 1024, 5000, 7), (1, 4096, 257, 2), (70, 1500, 999, 0)])
+def test_few_tiles(dtype, rows, d_in, classes, k):
+    """Products whose K is split, with biases, lists and weights."""
+    import torch
+    weight = torch.randn(rows, device="cuda", generator=torch.Generator(device="cuda").manual_seed(rows))
+    with Ctx() as ctx:
+        for w in (None, weight):
+            check_linear(ctx, dtype, rows, d_in, classes, bias=True, k=k, T=1.0 if not k else 0.7, ignored=0.3 if rows > 8 else 0.0, weight=w)
+            check_linear(ctx, dtype, rows, d_in, classes, bias=True, k=k, T=1.0 if not k else 0.7, weight=w, outputs=("row_loss", "loss"))
+
+
+def test_two_contexts_at_once():
+    """Calls of two contexts on two streams, with nothing between them that waits."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    jobs = []
+    for n, (dtype, rows, d_in, classes) in enumerate(((1, 600, 256, 20000), (0, 300, 512, 4096))):
+        gen, x, W, layer = inputs(dtype, rows, d_in, classes, seed=n)
+        jobs.append((layer, x, W, labels_for(rows, classes, gen, 0.2), *teacher_for(rows, classes, 6, gen, 0.1)))
+
+    def outputs():
+        return [[torch.empty(1, device="cuda"), torch.empty_like(j[1]), torch.empty_like(j[2]), torch.empty(1, device="cuda"),
+                 torch.empty_like(j[1]), torch.empty_like(j[2])] for j in jobs]
+
+    def calls(ctx, j, o):
+        B.rad_linear_ce(ctx, j[0], j[1], j[2], None, j[3], loss=o[0], dX=o[1], dW=o[2])
+        B.rad_linear_distill(ctx, j[0], j[1], j[2], None, B.make_teacher(j[4], j[5]), loss=o[3], dX=o[4], dW=o[5])
+    alone, together = outputs(), outputs()
+    torch.cuda.synchronize()
+    with Ctx(streams[0]) as a, Ctx(streams[1]) as b:
+        for ctx, j, o in zip((a, b), jobs, alone):
+            calls(ctx, j, o)
+            torch.cuda.synchronize()
+        for _ in range(5):
+            for ctx, j, o in zip((a, b), jobs, together):
+                calls(ctx, j, o)
+        torch.cuda.synchronize()
+    for x, y in zip(alone, together):
+        assert all(torch.equal(p, q) for p, q in zip(x, y))
+
+
+@pytest.mark.parametrize("dtype,rows,d_in,classes", [(1, 2500, 512, 1000), (0, 1500, 100, 700), (1, 9000, 64, 300)])
+def test_captured_many_rows(dtype, rows, d_in, classes):
+    test_captured(dtype, rows, d_in, classes)
+
+
+def test_refused_overlaps():
+    import torch
+    from paper_2007_10412_amd import binding as B
+    room = torch.randn(4096, device="cuda")
+    kept = room.clone()
+    x, W = room[:32].view(4, 8), room[32:160].view(8, 16)
+    labels = torch.zeros(4, device="cuda", dtype=torch.int32)
+    index, logit = torch.zeros(4, 2, device="cuda", dtype=torch.int32), torch.zeros(4, 2, device="cuda")
+    z = room[1000:1064].view(4, 16)
+    layer = B.make_layer(4, 8, 16, relu=False)
+    teacher = B.make_teacher(index, logit)
+    row = torch.zeros(4, device="cuda")
+    with Ctx() as ctx:
+        for out in (dict(dX=x), dict(dW=W), dict(dX=room[8:40].view(4, 8)), dict(dW=room[150:278].view(8, 16)), dict(row_loss=room[30:34]),
+                    dict(loss=room[100:101]), dict(dbias=room[20:36]), dict(dX=room[200:232].view(4, 8), dW=room[231:359].view(8, 16)),
+                    dict(row_loss=row, row_weight=row)):
+            for call in (lambda: B.rad_linear_ce(ctx, layer, x, W, None, labels, **out),
+                         lambda: B.rad_linear_distill(ctx, layer, x, W, None, teacher, **out)):
+                with pytest.raises(B.RadError) as e:
+                    call()
+                assert e.value.status == B.RAD_ERR_PARAM, out.keys()
+        with pytest.raises(B.RadError) as e:
+            B.rad_linear_ce(ctx, layer, x, W, None, labels, loss=labels[2:3].view(torch.float32))
+        assert e.value.status == B.RAD_ERR_PARAM
+        for out in (dict(dlogits=room[1001:1065].view(4, 16)), dict(row_loss=room[1060:1064]), dict(dlogits=z, loss=room[1000:1001]),
+                    dict(loss=logit[1, :1]), dict(row_loss=row, row_weight=row)):
+            with pytest.raises(B.RadError) as e:
+                B.rad_distill_ce(ctx, z, teacher, B.RAD_F32, **out)
+            assert e.value.status == B.RAD_ERR_PARAM, out.keys()
+        B.rad_ctx_synchronize(ctx)
+    assert torch.equal(room, kept)

@@ -1,0 +1,70 @@
+"""What the Python calls of the losses over a vocabulary refuse before the library sees a pointer: tensors of another size, type or
+layout than the layer says."""
+import math
+
+import pytest
+import torch
+
+from paper_2007_10412_amd import binding as B
+
+F, H, I = torch.float32, torch.bfloat16, torch.int32
+
+
+def refused(call, status=None):
+    with pytest.raises(B.RadError) as e:
+        call()
+    assert e.value.status == (B.RAD_ERR_SHAPE if status is None else status), e.value
+
+
+@pytest.mark.parametrize("index,logit", [
+    (torch.zeros(4, 2, dtype=torch.int64), torch.zeros(4, 2)), (torch.zeros(4, 2, dtype=I), torch.zeros(4, 2, dtype=torch.float64)),
+    (torch.zeros(4, 2, dtype=I), torch.zeros(4, 3)), (torch.zeros(4, 2, dtype=I), torch.zeros(2, 4)), (torch.zeros(8, dtype=I), torch.zeros(8)),
+    (torch.zeros(2, 4, dtype=I).t(), torch.zeros(4, 2)), (torch.zeros(4, 2, dtype=I), torch.zeros(4, 4)[:, ::2])])
+def test_lists(index, logit):
+    refused(lambda: B.make_teacher(index, logit))
+
+
+def test_a_teacher_holds_its_lists():
+    t = B.make_teacher(torch.zeros(4, 2, dtype=I), torch.zeros(4, 2), 2.0)
+    assert t.k == 2 and t.temperature == 2.0 and t.index == t.lists[0].data_ptr() and t.logit == t.lists[1].data_ptr()
+
+
+def bad(shape, dtype):
+    """tensors that are not contiguous ones of `shape` and `dtype`"""
+    n = math.prod(shape)
+    other = H if dtype == F else F
+    some = [torch.zeros(n + 1, dtype=dtype), torch.zeros(n - 1, dtype=dtype), torch.zeros(shape, dtype=other)]
+    return some + ([torch.zeros(2 * n, dtype=dtype)[::2]] if n > 1 else [])
+
+
+@pytest.mark.parametrize("kind,td", [(B.RAD_F32, F), (B.RAD_BF16, H)])
+def test_linear(kind, td):
+    layer = B.make_layer(4, 8, 16, dtype=kind, relu=False, has_bias=True)
+    given = dict(x=((4, 8), td), W=((8, 16), td), bias=((16,), F), row_weight=((4,), F), row_loss=((4,), F), loss=((1,), F),
+                 dX=((4, 8), td), dW=((8, 16), F), dbias=((16,), F))
+    labels, teacher = torch.zeros(4, dtype=I), B.make_teacher(torch.zeros(4, 2, dtype=I), torch.zeros(4, 2))
+    good = {n: torch.zeros(s, dtype=t) for n, (s, t) in given.items()}
+    for name, (shape, dtype) in given.items():
+        for t in bad(shape, dtype):
+            if name == "dW" and t.shape == shape:       # fp32 or the layer's type
+                continue
+            refused(lambda: B.rad_linear_ce(None, layer, labels=labels, **{**good, name: t}))
+            refused(lambda: B.rad_linear_distill(None, layer, teacher=teacher, **{**good, name: t}))
+    refused(lambda: B.rad_linear_ce(None, layer, labels=labels, **{**good, "dW": torch.zeros(8, 16, dtype=torch.float16)}), B.RAD_ERR_PARAM)
+    for t in (torch.zeros(4, dtype=torch.int64), torch.zeros(5, dtype=I), torch.zeros(8, dtype=I)[::2]):
+        refused(lambda: B.rad_linear_ce(None, layer, labels=t, **good))
+    few = B.make_teacher(torch.zeros(3, 2, dtype=I), torch.zeros(3, 2))
+    refused(lambda: B.rad_linear_distill(None, layer, teacher=few, **good))
+
+
+@pytest.mark.parametrize("kind,td", [(B.RAD_F32, F), (B.RAD_BF16, H)])
+def test_distill(kind, td):
+    teacher = B.make_teacher(torch.zeros(4, 2, dtype=I), torch.zeros(4, 2))
+    given = dict(row_weight=((4,), F), row_loss=((4,), F), loss=((1,), F), dlogits=((4, 16), td))
+    good = {n: torch.zeros(s, dtype=t) for n, (s, t) in given.items()}
+    z = torch.zeros(4, 16, dtype=td)
+    for name, (shape, dtype) in given.items():
+        for t in bad(shape, dtype):
+            refused(lambda: B.rad_distill_ce(None, z, teacher, kind, **{**good, name: t}))
+    for t in (torch.zeros(4, 16, dtype=H if td == F else F), torch.zeros(16, 4, dtype=td).t(), torch.zeros(5, 16, dtype=td)):
+        refused(lambda: B.rad_distill_ce(None, t, teacher, kind, **good))
