@@ -1,5 +1,7 @@
 // A small layer under a loss over up to 16 classes, where launches are most of the time: two kernels instead of five
-// (150 x 300 x 10 fp32 with biases and all gradients: 43 -> 20 us).
+// (150 x 300 x 10 with all gradients, against the general route: fp32 with biases 43 -> 15 us, bf16 28 -> 16).  What bounds
+// them is latency: two launches, the loads' way from memory (labels, weights and biases are asked for before the products) and
+// the exchanges between lanes.
 //
 // The first has a workgroup for 4 rows: its threads share the d_in products of a logit, and a transposing reduction leaves lane
 // 16 r + v of every wave with z_v of row r, so the softmax is a few exchanges among the 16 lanes of a row.
@@ -44,18 +46,16 @@ __global__ __launch_bounds__(256) void few_classes_kernel(FewClasses a) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const VocabTargets& t = a.t;
   const int V = a.classes;
-  float inv_count = 0.f;
-  if (!t.weight) {
-    float n = 0.f;
-    for (int r = threadIdx.x; r < a.rows; r += 256) n += row_counts(t, r, V) ? 1.f : 0.f;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
-    if (lane == 0) s_w[w] = n;
-    __syncthreads();
-    n = (s_w[0] + s_w[1]) + (s_w[2] + s_w[3]);
-    inv_count = n > 0.f ? 1.f / n : 0.f;
-  }
   const int row0 = (int)blockIdx.x * R;
+  const int r = lane / VP, v = lane % VP, row = row0 + r;
+  // (what the softmax needs is asked for before the products, whose loads it then does not follow)
+  float n = 0.f;
+  if (!t.weight)
+    for (int q = threadIdx.x; q < a.rows; q += 256) n += row_counts(t, q, V) ? 1.f : 0.f;
+  const bool counts = row < a.rows && row_counts(t, row, V);
+  const int label = t.labels && row < a.rows ? t.labels[row] : -1;
+  const float weight = t.weight && row < a.rows ? t.weight[row] : 0.f;
+  const float bias = a.bias && v < V ? a.bias[v] : 0.f;
   const T* const W = static_cast<const T*>(a.W);
   float acc[64];
 #pragma unroll
@@ -72,16 +72,18 @@ __global__ __launch_bounds__(256) void few_classes_kernel(FewClasses a) {
     }
   }
   reduce_scatter<32>(acc, lane);
-  const int r = lane / VP, v = lane % VP, row = row0 + r;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
   s_z[w][lane] = acc[0];
+  if (lane == 0) s_w[w] = n;
   __syncthreads();
+  n = (s_w[0] + s_w[1]) + (s_w[2] + s_w[3]);
+  const float inv_count = n > 0.f ? 1.f / n : 0.f;
   float z = (s_z[0][lane] + s_z[1][lane]) + (s_z[2][lane] + s_z[3][lane]);     // (the same in all waves from here on)
-  if (a.bias && v < V) z += a.bias[v];
-  if (v >= V) z = -INFINITY;
-  const bool counts = row < a.rows && row_counts(t, row, V);
+  z = v < V ? z + bias : -INFINITY;
   float p = 0.f;
   if (counts) {
-    if (t.labels) p = t.labels[row] == v ? 1.f : 0.f;
+    if (t.labels) p = label == v ? 1.f : 0.f;
     else
       for (int j = 0; j < t.k; ++j) {                   // (sorted, joined: at most V of them)
         const int i = t.index[(int64_t)row * t.k + j];
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(256) void few_classes_kernel(FewClasses a) {
   const float T1 = t.temperature;
   if (w == 0 && v == 0 && row < a.rows)
     a.row_loss[row] = counts ? T1 * T1 * ((t.labels ? 0.f : t.entropy[row]) + (logf(s) - dot / T1)) : 0.f;
-  const float wt = counts ? (t.weight ? t.weight[row] : inv_count) * T1 : 0.f;
+  const float wt = counts ? (t.weight ? weight : inv_count) * T1 : 0.f;
   const float g = counts && v < V ? wt / s * e - wt * p : 0.f;
   if (a.dz && w == 0 && row < a.rows) a.dz[(int64_t)row * VP + v] = g;
   if (!a.dx) return;
@@ -128,7 +130,7 @@ __global__ __launch_bounds__(256) void few_classes_kernel(FewClasses a) {
 // workgroup, where a loss is asked for, adds the rows' losses.
 template <typename T, typename O>
 __global__ __launch_bounds__(1024) void few_classes_dw_kernel(FewClasses a, int blocks) {
-  __shared__ float s_sum[16][64];
+  __shared__ float s_sum[16][VP][64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const VocabTargets& t = a.t;
   const int V = a.classes;
@@ -138,40 +140,38 @@ __global__ __launch_bounds__(1024) void few_classes_dw_kernel(FewClasses a, int 
       if (row_counts(t, r, V)) { sum += (t.weight ? t.weight[r] : 1.f) * a.row_loss[r]; n += 1.f; }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) { sum += __shfl_xor(sum, o); n += __shfl_xor(n, o); }
-    if (lane == 0) { s_sum[0][w] = sum; s_sum[1][w] = n; }
+    if (lane == 0) { s_sum[0][0][w] = sum; s_sum[0][1][w] = n; }
     __syncthreads();
     if (threadIdx.x != 0) return;
-    for (int q = 1; q < 16; ++q) { sum += s_sum[0][q]; n += s_sum[1][q]; }
+    for (int q = 1; q < 16; ++q) { sum += s_sum[0][0][q]; n += s_sum[0][1][q]; }
     *a.loss = t.weight ? sum : n > 0.f ? sum / n : 0.f;
     return;
   }
+  static_assert(VP == 16, "a wave of the 16 for each class");
   const int d = (int)blockIdx.x * 64 + lane;
   float acc[VP];
 #pragma unroll
   for (int v = 0; v < VP; ++v) acc[v] = 0.f;
 #pragma unroll 4
   for (int r = w; r < a.rows; r += 16) {
-    const bool counts = row_counts(t, r, V);            // (the same for the wave)
-    const float* const g = a.dz + (int64_t)r * VP;
-    const float x = !counts ? 0.f : d < a.d_in ? ld_elem(static_cast<const T*>(a.x) + (int64_t)r * a.d_in + d) : 1.f;
+    const float* const g = a.dz + (int64_t)r * VP;      // (the same for the wave, as is whether the row counts)
+    float x = d < a.d_in ? ld_elem(static_cast<const T*>(a.x) + (int64_t)r * a.d_in + d) : 1.f;
+    if (!row_counts(t, r, V)) x = 0.f;
 #pragma unroll
     for (int v = 0; v < VP; ++v) acc[v] += x * g[v];
   }
 #pragma unroll
-  for (int v = 0; v < VP; ++v) {
-    __syncthreads();
-    s_sum[w][lane] = acc[v];
-    __syncthreads();
-    if (v < V && w == v % 16) {
-      float sum = 0.f;
-      for (int q = 0; q < 16; ++q) sum += s_sum[q][lane];
-      if (d < a.d_in && a.dw) {
-        O* const o = static_cast<O*>(a.dw) + (int64_t)d * V + v;
-        st_elem(o, a.beta ? ld_elem(o) + sum : sum);
-      } else if (d == a.d_in && a.dbias) {
-        a.dbias[v] = a.beta ? a.dbias[v] + sum : sum;
-      }
-    }
+  for (int v = 0; v < VP; ++v) s_sum[w][v][lane] = acc[v];
+  __syncthreads();
+  if (w >= V) return;                                   // a wave joins a class
+  float sum = 0.f;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) sum += s_sum[q][w][lane];
+  if (d < a.d_in && a.dw) {
+    O* const o = static_cast<O*>(a.dw) + (int64_t)d * V + w;
+    st_elem(o, a.beta ? ld_elem(o) + sum : sum);
+  } else if (d == a.d_in && a.dbias) {
+    a.dbias[w] = a.beta ? a.dbias[w] + sum : sum;
   }
 }
 
