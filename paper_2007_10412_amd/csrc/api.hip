@@ -1598,7 +1598,7 @@ static rad_status head_split_sum(rad_ctx* c, const SplitSum& sum) {
   return RAD_OK;
 }
 
-// Two kernels against the general route's five or more, us with all gradients, fp32 / bf16: 150 x 300 x 10 20 / 22 against
+// Two kernels against the general route's five or more, us with all gradients, fp32 / bf16: 150 x 300 x 10 15 / 16 against
 // 43 / 28; 1000 x 300 x 10 50 against 48, 150 x 4096 x 10 53 against 43, 1000 x 4096 x 10 88 / 97 against 62 / 38.
 static bool few_classes_pay(int64_t rows, int64_t d_in, int64_t d_out) {
   return d_out <= kFewClasses && rows <= 1024 && rows * d_in <= 100000;
@@ -1686,7 +1686,12 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     else { tp.index += r0 * t.k; tp.prob += r0 * t.k; tp.entropy += r0; tp.counts += r0; }
     if (tp.weight) tp.weight += r0;
     float* const inv_count = one && !row_weight ? const_cast<float*>(t.inv_count) : nullptr;
-    const bool own_list = n <= kOwnListRows && fwd.tile != 256;
+    const int64_t fwd_tiles = (int64_t)((n + fwd.tile - 1) / fwd.tile) * ((d_out + 127) / 128) * fwd.splits;
+    // A launch for the list costs 5 us; lists made in the tiles cost each of them 1 or 2, which two bf16 tiles on a CU hide where
+    // rows are few.  us with / without a launch: bf16 4096 x 4096 x 1000 (256 tiles) 151 / 148, 2000 x 512 x 5000 (640) 68 / 67,
+    // 3000 x 512 x 4000 (768) 94 / 95, 1999 x 1000 x 50257 655 / 685, but 1000 x 1000 x 50257 502 / 498; fp32 1500 x 512 x 2000
+    // (192) 135 / 134, 1000 x 256 x 20000 (1256) 337 / 350.
+    const bool own_list = n <= kOwnListRows && fwd.tile != 256 && (dtype == kBF16 ? n <= 1024 || fwd_tiles <= 640 : fwd_tiles <= 768);
     if (!own_list)
       HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(tp, n, d_out, list, live, inv_count, common, c->stream); }));
     GemmArgs g = gemm_zero();

@@ -371,7 +371,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
     }
   }
   if constexpr (EPI == kEpiVocab) {
-    epilogue_vocab<uint16_t, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, live, g.head.row_map);
+    epilogue_vocab<uint16_t, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, live, g.head.row_map + m0);
   } else if constexpr (EPI == kEpiHeadX || EPI == kEpiHeadW) {
     epilogue_head<EPI == kEpiHeadX, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, EPI == kEpiHeadX ? live : g.M);
   } else if constexpr (EPI == kEpiStore && AKIND == kOpMN) {      // dW from a dense store: fp32 out

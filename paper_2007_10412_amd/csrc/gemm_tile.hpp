@@ -27,7 +27,7 @@ template <typename T, int R, bool MN> struct TileOperand {
     const int r = u / CPR, c = u % CPR;
     return !MN ? c ^ ((r >> 1) & 7) : ES == 2 ? c ^ (4 * (r & 3)) : c;
   }
-  // rows past rmax (K contiguous; of the list map, where there is one) and chunks past it (M/N contiguous, rmax whole
+  // rows past rmax (K contiguous; row r0 + r is row map[r] of p, where there is a map) and chunks past it (M/N contiguous, rmax whole
   // chunks) read the last one instead
   __device__ __forceinline__ void init(const void* p, int64_t ld, int r0, int kbeg, int rmax, const int32_t* map) {
 #pragma unroll
@@ -35,7 +35,7 @@ template <typename T, int R, bool MN> struct TileOperand {
       const int u = unit(i), r = line(u);
       const uint32_t pitch = (uint32_t)ld * ES;
       if (MN) voff[i] = (uint32_t)r * pitch + (uint32_t)min(chunk(u), (rmax - r0) / EPC - 1) * 16u;
-      else if (map) voff[i] = (uint32_t)map[min(r0 + r, rmax - 1)] * pitch + (uint32_t)chunk(u) * 16u;
+      else if (map) voff[i] = (uint32_t)map[min(r, rmax - 1 - r0)] * pitch + (uint32_t)chunk(u) * 16u;
       else voff[i] = (uint32_t)min(r, rmax - 1 - r0) * pitch + (uint32_t)chunk(u) * 16u;
     }
     base = static_cast<const unsigned char*>(p) + (MN ? (int64_t)kbeg * ld + r0 : (map ? 0 : (int64_t)r0 * ld) + kbeg) * ES;
@@ -164,12 +164,15 @@ __device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* s
 
   // the workgroups of an XCD (ids equal mod 8) take neighbouring tiles, in columns of up to 8 tile rows; the grid is made for
   // all rows, the tiles dealt out are those of the rows that count
-  const int32_t* row_map = g.head.row_map;
   int live;
+  uint32_t mine = 0u;
+  int mine_at = 0;
   if (EPI == kEpiVocab && g.head.list_out) {
-    __shared__ int32_t s_list[kOwnListRows], s_n[kGemmThreads / 64];
-    live = own_row_list(g.head, g.N, s_list, s_n, block == 0 && split == 0);
-    row_map = s_list;
+    __shared__ int32_t s_n[kGemmThreads / 64];
+    __shared__ float s_max[kGemmThreads / 64];
+    const bool write = block == 0 && split == 0;
+    live = g.head.rows <= 4 * kGemmThreads ? own_rows<4>(g.head, g.N, s_n, s_max, write, &mine, &mine_at)
+                                           : own_rows<kOwnListRows / kGemmThreads>(g.head, g.N, s_n, s_max, write, &mine, &mine_at);
   } else {
     live = *g.head.live;
   }
@@ -181,6 +184,22 @@ __device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* s
   const int m0 = (grp * GM + within % gh) * BM, n0 = (within / gh) * BN;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int wm0 = (w >> 1) * (BM / 2), wn0 = (w & 1) * (BN / 2);
+  const int32_t* tile_rows = nullptr;                   // rows of the batch of the tile's rows
+  if (EPI == kEpiVocab && g.head.list_out) {
+    __shared__ int32_t s_list[BM];
+    const int per = g.head.rows <= 4 * kGemmThreads ? 4 : kOwnListRows / kGemmThreads;
+    for (int q0 = 0; q0 < per; q0 += 4) {
+#pragma unroll
+      for (int q = q0; q < q0 + 4; ++q) {
+        const int at = mine_at + __popc(mine & ((1u << q) - 1u)) - m0;
+        if (((mine >> q) & 1u) && (uint32_t)at < (uint32_t)BM) s_list[at] = (int)threadIdx.x * per + q;
+      }
+    }
+    __syncthreads();
+    tile_rows = s_list;
+  } else if (EPI == kEpiVocab) {
+    tile_rows = g.head.row_map + m0;
+  }
 
   floatx16 acc[TM][TN];
 #pragma unroll
@@ -195,7 +214,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* s
   const int kend = g.k_splits > 1 ? min(k_all, kbeg + g.k_split) : k_all;
   const int KT = max(0, (kend - kbeg + BK - 1) / BK);
   LoadA la; LoadB lb;
-  if (EPI == kEpiVocab) la.init(g.A, g.lda, m0, kbeg, live, row_map);
+  if (EPI == kEpiVocab) la.init(g.A, g.lda, m0, kbeg, live, tile_rows);
   else if (EPI == kEpiHeadW) la.init(live == g.head.rows ? g.head.whole : g.A, g.lda, m0, kbeg, g.m_load, nullptr);
   else la.init(g.A, g.lda, m0, kbeg, g.M, nullptr);
   lb.init(g.B, g.ldb, n0, kbeg, kBT ? g.head.n_load : g.N, nullptr);
@@ -223,7 +242,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* s
   T* const ct = reinterpret_cast<T*>(smem_raw);
   if constexpr (EPI == kEpiVocab) {
     if (g.k_splits > 1) { store_partial_rows<TM, TN>(g, acc, m0, n0, wm0, wn0, live, split); return; }
-    epilogue_vocab<T, BM, BN, TM, TN>(g, acc, ct, m0, n0, wm0, wn0, live, row_map);
+    epilogue_vocab<T, BM, BN, TM, TN>(g, acc, ct, m0, n0, wm0, wn0, live, tile_rows);
   } else {
     if (g.k_splits > 1) {                               // this split's partial sums, in fp32
       GemmArgs gs = g;

@@ -4,13 +4,15 @@
 
 namespace rad {
 
-// The rows that count, in order, into LDS (kOwnListRows entries, and 4 for the waves' counts); returns their number.  A thread
-// has four consecutive rows.
-__device__ __forceinline__ int own_row_list(const HeadArgs& h, int classes, int32_t* s_list, int32_t* s_n, bool write) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r0 = (int)threadIdx.x * 4;
+// The rows that count, made into a list by a workgroup for itself: a thread has PER consecutive rows, of which `mine` count, the
+// first of them at place `at`.  Returns their number; the workgroup that writes leaves the whole list in memory.
+// s_n: a word a wave.
+template <int PER>
+__device__ __forceinline__ int own_rows(const HeadArgs& h, int classes, int32_t* s_n, float* s_max, bool write, uint32_t* mine_out, int* at_out) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r0 = (int)threadIdx.x * PER;
   uint32_t mine = 0u;
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
+  for (int q = 0; q < PER; ++q)
     if (r0 + q < h.rows && (h.labels ? (uint32_t)h.labels[r0 + q] < (uint32_t)classes : h.counts[r0 + q] != 0)) mine |= 1u << q;
   const int n = __popc(mine);
   int up = n;
@@ -20,36 +22,34 @@ __device__ __forceinline__ int own_row_list(const HeadArgs& h, int classes, int3
   if (write && h.weight) {
     float m = 0.f;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) if ((mine >> q) & 1u) m = fmaxf(m, fabsf(h.weight[r0 + q]));
+    for (int q = 0; q < PER; ++q) if ((mine >> q) & 1u) m = fmaxf(m, fabsf(h.weight[r0 + q]));
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    if (lane == 0) s_list[w] = (int32_t)__float_as_uint(m);
+    if (lane == 0) s_max[w] = m;
   }
   __syncthreads();
   int at = up - n, all = 0;
 #pragma unroll
   for (int q = 0; q < kGemmThreads / 64; ++q) { if (q < w) at += s_n[q]; all += s_n[q]; }
+  *mine_out = mine; *at_out = at;
   if (write) {
     if (threadIdx.x == 0) {
       const float inv = h.inv_count_out ? (all > 0 ? 1.f / (float)all : 0.f) : h.weight ? 0.f : *h.inv_count;
       float m = 0.f;
-      if (h.weight) for (int q = 0; q < kGemmThreads / 64; ++q) m = fmaxf(m, __uint_as_float((uint32_t)s_list[q]));
+      if (h.weight) for (int q = 0; q < kGemmThreads / 64; ++q) m = fmaxf(m, s_max[q]);
       *h.live_out = all;
       if (h.inv_count_out) *h.inv_count_out = inv;
       *h.common_out = h.temperature * (h.weight ? m : inv);
     }
-    __syncthreads();
-  }
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int r = r0 + q;
-    if (r >= h.rows) break;
-    const bool c = (mine >> q) & 1u;
-    if (c) s_list[at] = r;
-    if (write) h.list_out[c ? at : all + (r - at)] = r;      // (r - at rows before this one do not count)
-    at += c ? 1 : 0;
+    for (int q = 0; q < PER; ++q) {
+      const int r = r0 + q;
+      if (r >= h.rows) break;
+      const bool c = (mine >> q) & 1u;
+      h.list_out[c ? at : all + (r - at)] = r;                 // (r - at rows before this one do not count)
+      at += c ? 1 : 0;
+    }
   }
-  __syncthreads();
   return all;
 }
 
@@ -103,7 +103,7 @@ __device__ __forceinline__ void store_tile(const T* ct, T* C, int64_t ldc, int r
 // between the two lanes that share the row.
 template <typename T, int BM, int BN, int TM, int TN>
 __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc)[TM][TN], T* ct, int m0, int n0, int wm0,
-                                               int wn0, int live, const int32_t* row_map) {
+                                               int wn0, int live, const int32_t* tile_rows) {
   constexpr bool kCodes = sizeof(T) == 2;
   constexpr int CP = BN + 16 / (int)sizeof(T), kPart = 32 * TN;            // a wave's columns are one part of a row
   const HeadArgs& h = g.head;
@@ -143,7 +143,7 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
     // targets among these columns
     int t0 = 0, t1 = 0, row = 0;
     if (there) {
-      row = row_map[place];
+      row = tile_rows[place - m0];
       if (h.labels) { t1 = (uint32_t)(h.labels[row] - nw) < (uint32_t)kPart ? 1 : 0; }
       else {
         const uint16_t* const f = h.first + (int64_t)row * h.first_ld + part;

@@ -56,10 +56,10 @@ enum EpiKind : int {
 
 // The rows of the batch that have a target come first in a list; the products run over that list, whose length only the
 // device knows.
-constexpr int kOwnListRows = 1024;
+constexpr int kOwnListRows = 4096;
 struct HeadArgs {
   const int32_t* live;          // length of the list
-  // kEpiVocab with few rows: the list is made here, by every workgroup for itself, and written by one (rows <= kOwnListRows)
+  // kEpiVocab with few rows: every workgroup makes its tile's part of the list, one writes the whole (rows <= kOwnListRows)
   const int32_t* counts;        // which rows count, where there are no labels
   int32_t* list_out; int32_t* live_out; float* inv_count_out;   // list_out null: the list is there; the others as in launch_row_list
   float* common_out; const float* weight; const float* inv_count; float temperature;
