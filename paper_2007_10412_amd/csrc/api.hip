@@ -1598,10 +1598,12 @@ static rad_status head_split_sum(rad_ctx* c, const SplitSum& sum) {
   return RAD_OK;
 }
 
-// Two kernels against the general route's five or more, us with all gradients, fp32 / bf16: 150 x 300 x 10 15 / 16 against
-// 43 / 28; 1000 x 300 x 10 50 against 48, 150 x 4096 x 10 53 against 43, 1000 x 4096 x 10 88 / 97 against 62 / 38.
-static bool few_classes_pay(int64_t rows, int64_t d_in, int64_t d_out) {
-  return d_out <= kFewClasses && rows <= 1024 && rows * d_in <= 100000;
+// Two kernels, about 9 + rows / 50 + d_in / 115 us with all gradients, against the general route's five or more, about 45 us in
+// fp32 and 30 in bf16 at such sizes.  fp32: 150 x 300 x 10 15.1 against 44.5, 1000 x 300 x 10 31.8 against 48, 600 x 1024 x 10
+// 29 against 44, but 2000 x 64 x 10 49 against 45, 150 x 4096 x 10 48 against 44; bf16: 500 x 300 x 10 23.6 against 31.8,
+// 300 x 1024 x 10 25.7 against 30, but 1000 x 300 x 10 35 against 32.5, 150 x 4096 x 10 56 against 31.
+static bool few_classes_pay(int dtype, int64_t rows, int64_t d_in, int64_t d_out) {
+  return d_out <= kFewClasses && 9 * rows + 4 * d_in <= (dtype == kF32 ? 16000 : 9000);
 }
 
 static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* labels, const rad_teacher* teacher,
@@ -1624,7 +1626,7 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
                        {row_weight, (size_t)L->batch * 4}}));
   DeviceGuard guard(c->device);
   const int rows = (int)L->batch, d_in = (int)L->d_in, d_out = (int)L->d_out, dtype = L->dtype;
-  if (few_classes_pay(rows, d_in, d_out)) {
+  if (few_classes_pay(dtype, rows, d_in, d_out)) {
     FewClasses f;
     std::memset(&f, 0, sizeof(f));
     f.dtype = dtype; f.rows = rows; f.d_in = d_in; f.classes = d_out;

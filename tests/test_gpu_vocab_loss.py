@@ -761,7 +761,8 @@ def test_rows_without_a_target_hold_anything(dtype, rows, d_in, classes, k):
 
 
 @pytest.mark.parametrize("dtype,dw_dtype", [(0, 0), (1, 0), (1, 1)])
-@pytest.mark.parametrize("rows,d_in,classes,k", [(1, 1, 16, 1), (37, 65, 16, 16), (1000, 99, 7, 3), (256, 390, 12, 0), (5, 3001, 2, 0), (33, 64, 1, 2)])
+@pytest.mark.parametrize("rows,d_in,classes,k", [(1, 1, 16, 1), (37, 65, 16, 16), (1000, 99, 7, 3), (256, 390, 12, 0), (5, 3001, 2, 0), (33, 64, 1, 2),
+                                               (1700, 64, 10, 4), (1800, 64, 10, 4), (2, 3990, 16, 0), (2, 4000, 16, 0)])
 def test_few_classes(dtype, dw_dtype, rows, d_in, classes, k):
     import torch
     gen = torch.Generator(device="cuda").manual_seed(rows)
