@@ -309,12 +309,20 @@ def make_teacher(index, logit, temperature=1.0):
     return teacher
 
 
-def _check_tensors(*tensors):
-    """(name, tensor or None, elements, dtype or None: any) of what a call reads and writes"""
-    for name, t, n, dtype in tensors:
-        if t is not None and (t.numel() != n or not t.is_contiguous() or (dtype is not None and t.dtype != dtype)):
-            raise RadError(RAD_ERR_SHAPE, "%s is not a contiguous tensor of %d elements%s" % (
-                name, n, "" if dtype is None else " of " + str(dtype)))
+def _arg(name, t, n, dtype):
+    """The address of a tensor (or None) that a call reads or writes as n elements of a type.  (An int, not a c_void_p: a call
+    on a small layer takes as long on the host as on the device.)"""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise RadError(RAD_ERR_SHAPE, "%s is not a contiguous tensor of %d elements of %s" % (name, n, dtype))
+    return t.data_ptr()
+
+
+def _kind(t, dtype):
+    """The torch type of RAD_F32 or RAD_BF16; the tensor's own for a type that the library is to refuse."""
+    import torch
+    return torch.float32 if dtype == RAD_F32 else torch.bfloat16 if dtype == RAD_BF16 else t.dtype
 
 
 def _check_lists(teacher, rows):
@@ -325,41 +333,41 @@ def _check_lists(teacher, rows):
 def rad_distill_ce(ctx, logits, teacher, dtype, dlogits=None, row_weight=None, row_loss=None, loss=None):
     import torch
     rows, classes = logits.shape
-    f32, kind = torch.float32, {RAD_F32: torch.float32, RAD_BF16: torch.bfloat16}.get(dtype)
+    n, f32, kind = rows * classes, torch.float32, _kind(logits, dtype)
     _check_lists(teacher, rows)
-    _check_tensors(("logits", logits, rows * classes, kind), ("dlogits", dlogits, rows * classes, kind),
-                   ("row_weight", row_weight, rows, f32), ("row_loss", row_loss, rows, f32), ("loss", loss, 1, f32))
-    _check(ctx, lib().rad_distill_ce(ctx, _ptr(logits), C.byref(teacher), _ptr(row_weight), rows, classes, dtype,
-                                     _ptr(dlogits), _ptr(row_loss), _ptr(loss)))
+    _check(ctx, lib().rad_distill_ce(
+        ctx, _arg("logits", logits, n, kind), teacher, _arg("row_weight", row_weight, rows, f32), rows, classes, dtype,
+        _arg("dlogits", dlogits, n, kind), _arg("row_loss", row_loss, rows, f32), _arg("loss", loss, 1, f32)))
 
 
-def _head_args(layer, x, W, bias, row_weight, row_loss, loss, dX, dW, dbias, beta):
+def _head_call(call, ctx, layer, x, W, bias, targets, row_weight, row_loss, loss, dX, dW, dbias, beta):
     import torch
     n, d, v = layer.batch, layer.d_in, layer.d_out
-    f32, td = torch.float32, {RAD_F32: torch.float32, RAD_BF16: torch.bfloat16}.get(layer.dtype)
-    _check_tensors(("x", x, n * d, td), ("W", W, d * v, td), ("bias", bias, v, f32), ("row_weight", row_weight, n, f32),
-                   ("row_loss", row_loss, n, f32), ("loss", loss, 1, f32), ("dX", dX, n * d, td), ("dW", dW, d * v, None),
-                   ("dbias", dbias, v, f32))
-    if dW is not None and dW.dtype not in (f32, torch.bfloat16):
-        raise RadError(RAD_ERR_PARAM, "dW is fp32 or of the layer's type")
-    kind = RAD_BF16 if dW is not None and dW.dtype == torch.bfloat16 else RAD_F32
-    return _ptr(row_weight), _ptr(row_loss), _ptr(loss), _ptr(dX), _ptr(dW), kind, _ptr(dbias), beta
+    f32 = torch.float32
+    td = f32 if x is None else _kind(x, layer.dtype)
+    dw_kind = RAD_F32
+    if dW is not None and dW.dtype is not f32:
+        dw_kind = RAD_BF16
+        if dW.dtype is not torch.bfloat16:
+            raise RadError(RAD_ERR_PARAM, "dW is fp32 or of the layer's type")
+    _check(ctx, call(
+        ctx, layer, _arg("x", x, n * d, td), _arg("W", W, d * v, td), _arg("bias", bias, v, f32), targets,
+        _arg("row_weight", row_weight, n, f32), _arg("row_loss", row_loss, n, f32), _arg("loss", loss, 1, f32),
+        _arg("dX", dX, n * d, td), None if dW is None else _arg("dW", dW, d * v, dW.dtype), dw_kind, _arg("dbias", dbias, v, f32), beta))
 
 
 def rad_linear_ce(ctx, layer, x, W, bias, labels, row_weight=None, row_loss=None, loss=None, dX=None, dW=None, dbias=None,
                   beta=0.0):
     """dW: an fp32 tensor, or one of the layer's type."""
     import torch
-    _check_tensors(("labels", labels, layer.batch, torch.int32))
-    _check(ctx, lib().rad_linear_ce(ctx, C.byref(layer), _ptr(x), _ptr(W), _ptr(bias), _ptr(labels),
-                                    *_head_args(layer, x, W, bias, row_weight, row_loss, loss, dX, dW, dbias, beta)))
+    _head_call(lib().rad_linear_ce, ctx, layer, x, W, bias, _arg("labels", labels, layer.batch, torch.int32), row_weight, row_loss,
+               loss, dX, dW, dbias, beta)
 
 
 def rad_linear_distill(ctx, layer, x, W, bias, teacher, row_weight=None, row_loss=None, loss=None, dX=None, dW=None,
                        dbias=None, beta=0.0):
     _check_lists(teacher, layer.batch)
-    _check(ctx, lib().rad_linear_distill(ctx, C.byref(layer), _ptr(x), _ptr(W), _ptr(bias), C.byref(teacher),
-                                         *_head_args(layer, x, W, bias, row_weight, row_loss, loss, dX, dW, dbias, beta)))
+    _head_call(lib().rad_linear_distill, ctx, layer, x, W, bias, teacher, row_weight, row_loss, loss, dX, dW, dbias, beta)
 
 
 def rad_model_create_mlp(ctx, dtype, batch, dims, has_bias, scheme, p):
