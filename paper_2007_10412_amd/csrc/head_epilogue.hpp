@@ -136,23 +136,43 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
         for (int i = 0; i < TM; ++i) acc[i][j][e] = out ? -INFINITY : acc[i][j][e];
       }
   }
+  // Targets t0 .. t1 - 1 of each row lie among these columns, the first of them in column next.  That takes three loads, each of
+  // which waits for the one before: in bf16 they are made for all rows at once, as a wave has nothing else to do meanwhile
+  // (4096 x 2048 x 32000 with lists of 32 1536 -> 1524 us); in fp32 the registers for it cost more (1024 x 512 x 8003 254 -> 266).
+  int row[TM], t0[TM], t1[TM], next[TM];
+  auto find = [&](int i0, int i1) {
+#pragma unroll
+    for (int i = i0; i < i1; ++i) {
+      const int r = wm0 + i * 32 + lr;
+      row[i] = m0 + r < live && nw < g.N ? tile_rows[r] : -1;   // (the last tile may reach a whole part past the classes)
+      t0[i] = 0; t1[i] = 0; next[i] = -1;
+    }
+    if (h.labels) {
+#pragma unroll
+      for (int i = i0; i < i1; ++i) {
+        if (row[i] >= 0) next[i] = h.labels[row[i]] - nw;
+        t1[i] = (uint32_t)next[i] < (uint32_t)kPart ? 1 : 0;
+      }
+      return;
+    }
+#pragma unroll
+    for (int i = i0; i < i1; ++i)
+      if (row[i] >= 0) {
+        const uint16_t* const f = h.first + (int64_t)row[i] * h.first_ld + part;
+        t0[i] = f[0]; t1[i] = f[1];
+      }
+#pragma unroll
+    for (int i = i0; i < i1; ++i)
+      if (t0[i] < t1[i]) next[i] = h.index[(int64_t)row[i] * h.k + t0[i]] - nw;
+  };
+  if constexpr (kCodes) find(0, TM);
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
+    if constexpr (!kCodes) find(i, i + 1);
     const int place = m0 + wm0 + i * 32 + lr;
-    const bool there = place < live && nw < g.N;         // (the last tile may reach a whole part past the classes)
-    // targets among these columns
-    int t0 = 0, t1 = 0, row = 0;
-    if (there) {
-      row = tile_rows[place - m0];
-      if (h.labels) { t1 = (uint32_t)(h.labels[row] - nw) < (uint32_t)kPart ? 1 : 0; }
-      else {
-        const uint16_t* const f = h.first + (int64_t)row * h.first_ld + part;
-        t0 = f[0]; t1 = f[1];
-      }
-    }
-    for (int t = t0; __any(t < t1); ++t) {
-      int col = -1;
-      if (t < t1) col = (h.labels ? h.labels[row] : h.index[(int64_t)row * h.k + t]) - nw;
+    for (int t = t0[i]; __any(t < t1[i]); ++t) {
+      const int col = t < t1[i] ? next[i] : -1;
+      if (t + 1 < t1[i]) next[i] = h.index[(int64_t)row[i] * h.k + t + 1] - nw;
       float z = 0.f;
 #pragma unroll
       for (int j = 0; j < TN; ++j)
@@ -176,7 +196,7 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
         if (kCodes) acc[i][j][e] = d * c_code;
       }
     s += __shfl_xor(s, 32);
-    if (there && hh == 0) *reinterpret_cast<float2*>(h.stats + ((int64_t)part * h.stats_ld + place) * 2) = make_float2(m, s);
+    if (row[i] >= 0 && hh == 0) *reinterpret_cast<float2*>(h.stats + ((int64_t)part * h.stats_ld + place) * 2) = make_float2(m, s);
     if (g.y) {
       T* const crow = ct + (wm0 + i * 32 + lr) * CP + wn0 + hh * 4;
 #pragma unroll
