@@ -218,7 +218,8 @@ def test_scoring(dtype, rows, d_in, classes):
 
 
 @pytest.mark.parametrize("dtype,dw_dtype", [(0, 0), (1, 0), (1, 1)])
-@pytest.mark.parametrize("rows,d_in,classes", [(70, 136, 264), (257, 129, 1003), (512, 512, 4096), (600, 200, 20005)])
+@pytest.mark.parametrize("rows,d_in,classes", [(70, 136, 264), (257, 129, 1003), (512, 512, 4096), (600, 200, 20005),
+                                               (700, 2048, 8003)])
 def test_weights_and_accumulation(dtype, dw_dtype, rows, d_in, classes):
     """Row weights of any sign, gradients added to what is there."""
     import torch
