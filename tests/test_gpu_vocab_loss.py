@@ -864,3 +864,114 @@ def test_refused_overlaps():
             assert e.value.status == B.RAD_ERR_PARAM, out.keys()
         B.rad_ctx_synchronize(ctx)
     assert torch.equal(room, kept)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,d_in,classes,ignored", [(4096, 1024, 8000, 0.97), (4096, 512, 1000, 0.995), (2048, 256, 300, 0.99)])
+def test_few_rows_of_many(dtype, rows, d_in, classes, ignored):
+    """Products that are laid out for all rows, where the last parts of a split K have none that count."""
+    with Ctx() as ctx:
+        check_linear(ctx, dtype, rows, d_in, classes, ignored=ignored)
+        check_linear(ctx, dtype, rows, d_in, classes, ignored=ignored, beta=1.0, dw_dtype=dtype)
+
+
+def test_two_graphs_of_one_context():
+    """They share its workspaces: replayed in turn, with eager calls of both sizes and other inputs in between."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    stream = torch.cuda.Stream()
+    jobs = [inputs(dtype, *shape, seed=n) for n, (dtype, *shape) in enumerate(((1, 600, 264, 20000), (0, 300, 200, 1003), (1, 40, 30, 10)))]
+    jobs = [(gen, x, W, layer, labels_for(len(x), W.shape[1], gen, 0.2), *teacher_for(len(x), W.shape[1], 6, gen, 0.1)) for gen, x, W, layer in jobs]
+
+    def outputs(j):
+        return [torch.empty(1, device="cuda"), torch.empty_like(j[1]), torch.empty_like(j[2]), torch.empty(1, device="cuda"),
+                torch.empty_like(j[1]), torch.empty_like(j[2])]
+
+    def calls(ctx, j, o):
+        B.rad_linear_ce(ctx, j[3], j[1], j[2], None, j[4], loss=o[0], dX=o[1], dW=o[2])
+        B.rad_linear_distill(ctx, j[3], j[1], j[2], None, B.make_teacher(j[5], j[6]), loss=o[3], dX=o[4], dW=o[5])
+    held, eager = [outputs(j) for j in jobs], [outputs(j) for j in jobs]
+    torch.cuda.synchronize()
+    with Ctx(stream) as ctx:
+        for j, o in zip(jobs, eager):                               # (the workspaces grow here)
+            calls(ctx, j, o)
+        torch.cuda.synchronize()
+        graphs = []
+        for j, o in zip(jobs, held):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=stream):
+                calls(ctx, j, o)
+        for n in range(3):
+            for j in jobs:
+                j[1].copy_(torch.randn(j[1].shape, device="cuda", generator=j[0]))
+                j[4].copy_(labels_for(len(j[1]), j[2].shape[1], j[0], 0.2))
+            for o in held:
+                for t in o:
+                    t.fill_(math.nan)
+            torch.cuda.synchronize()
+            for g in graphs if n % 2 else graphs[::-1]:
+                g.replay()
+            torch.cuda.synchronize()
+            for j, h, e in zip(jobs, held, eager):
+                calls(ctx, j, e)
+                torch.cuda.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(h, e)), n
+        graphs = None
+
+
+def test_logits_past_32_bits():
+    """Dense logits of over 2^32 elements, in place: the first, middle and last rows."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    rows, classes, k = 33000, 131071, 3
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    z = torch.empty(rows, classes, device="cuda", dtype=torch.bfloat16)
+    z.normal_(0, 2, generator=gen)
+    some = torch.tensor([0, 1, 16384, 16385, 32767, 32768, 32769, rows - 2, rows - 1], device="cuda")
+    kept = z[some].double()
+    index, logit = torch.randint(0, classes, (rows, k), device="cuda", generator=gen).to(torch.int32), torch.randn(rows, k, device="cuda", generator=gen)
+    row = torch.empty(rows, device="cuda")
+    with Ctx() as ctx:
+        B.rad_distill_ce(ctx, z, B.make_teacher(index, logit), B.RAD_BF16, z, row_loss=row)
+        B.rad_ctx_synchronize(ctx)
+    targets = lists(teacher=(index[some], logit[some]), classes=classes)
+    want_row, _, _, _, _ = definition(kept, targets, None, 1.0)
+    _, _, dz, soft, target = definition(kept, targets, torch.full((len(some),), 1 / rows, device="cuda"), 1.0)
+    rel = softmax_error(4 * U * float(kept.abs().max()), classes)
+    close(row[some], want_row, (rel + 8 * U * 50) * torch.ones_like(want_row), "row_loss")
+    close(z[some], dz, soft * rel + (6 * U + list_error((index[some], logit[some]), 1.0)) * target + HALF[1] * dz.abs() + 1e-37, "dlogits")
+
+
+def test_rows_past_32_bits():
+    """x of over 2^32 bytes: rows in pieces, dW and the loss over all of them."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    rows, d_in, classes = 1100001, 2048, 24
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.empty(rows, d_in, device="cuda", dtype=torch.bfloat16)
+    x.normal_(0, 1, generator=gen)
+    W = (torch.randn(d_in, classes, device="cuda", generator=gen) / math.sqrt(d_in)).to(torch.bfloat16)
+    labels = labels_for(rows, classes, gen, 0.2)
+    counts = (labels >= 0) & (labels < classes)
+    row, loss, dX, dW = torch.empty(rows, device="cuda"), torch.empty(1, device="cuda"), torch.full_like(x, math.nan), torch.empty(d_in, classes, device="cuda")
+    with Ctx() as ctx:
+        B.rad_linear_ce(ctx, B.make_layer(rows, d_in, classes, dtype=1, relu=False), x, W, None, labels, row_loss=row, loss=loss, dX=dX, dW=dW)
+        B.rad_ctx_synchronize(ctx)
+    n, Wd, total = int(counts.sum()), W.double(), 0.0
+    want_dW, bound, mass = (torch.zeros(d_in, classes, device="cuda", dtype=torch.float64) for _ in range(3))
+    for r in range(0, rows, 100000):
+        at = slice(r, min(rows, r + 100000))
+        xd = x[at].double()
+        weight = torch.full((len(xd),), 1 / n, device="cuda", dtype=torch.float64)
+        want, part, dz, soft, target = definition(xd @ Wd, lists(labels=labels[at], classes=classes), weight, 1.0)
+        rel = softmax_error(8 * U * math.sqrt(d_in) * float((xd.abs() @ Wd.abs()).max()), classes)
+        close(row[at], want, (rel + 8 * U * 50) * torch.ones_like(want), "row_loss %d" % r)
+        total += float(part)
+        e = soft * rel + 2.02 * HALF[1] * (soft + target) + 4 * U * target
+        want_dX = dz @ Wd.t().contiguous()
+        close(dX[at], want_dX, (e + 8 * U * math.sqrt(classes) * dz.abs()) @ Wd.abs().t().contiguous() + HALF[1] * want_dX.abs() + 1e-37, "dX %d" % r)
+        want_dW += xd.t().contiguous() @ dz
+        bound += xd.abs().t().contiguous() @ e
+        mass += xd.abs().t().contiguous() @ dz.abs()
+    close(dW, want_dW, bound + 8 * U * math.sqrt(rows) * mass, "dW")
+    assert abs(float(loss) - total) < (rel + 8 * U * 50 + 8 * U * math.sqrt(rows)) * max(1.0, total)
