@@ -975,3 +975,17 @@ def test_rows_past_32_bits():
         mass += xd.abs().t().contiguous() @ dz.abs()
     close(dW, want_dW, bound + 8 * U * math.sqrt(rows) * mass, "dW")
     assert abs(float(loss) - total) < (rel + 8 * U * 50 + 8 * U * math.sqrt(rows)) * max(1.0, total)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,classes,k", [(204, 3000, 20), (205, 3000, 20), (256, 500, 16), (257, 500, 2), (16, 50257, 256), (15, 50257, 257), (2, 300001, 129),
+                                            (255, 140003, 3), (1, 40, 200)])
+@pytest.mark.parametrize("how", ["", "missing", "doubles", "weight", "in_place", "loss", "gradient"])
+def test_short_lists(dtype, rows, classes, k, how):
+    """Few rows: whole ones of every size of part, and rows in parts, with lists of up to 257 entries."""
+    import torch
+    weight = torch.randn(rows, device="cuda", generator=torch.Generator(device="cuda").manual_seed(rows)) if how == "weight" else None
+    with Ctx() as ctx:
+        check_distill(ctx, dtype, rows, classes, k, T=1.3, missing=0.4 if how == "missing" else 0.0, weight=weight, in_place=how == "in_place",
+                      doubles=how == "doubles", outputs=("loss",) if how == "loss" else ("dlogits",) if how in ("gradient", "in_place") else
+                      ("dlogits", "row_loss", "loss"))
