@@ -173,6 +173,8 @@ def rad_ctx_create(stream=None):
     st = lib().rad_ctx_create(C.byref(ctx), handle)
     if st != RAD_OK:
         raise RadError(st, "rad_ctx_create failed (is a gfx950 device present?)")
+    import torch
+    ctx.device = torch.cuda.current_device()             # (the library takes the current device too)
     return ctx
 
 
@@ -325,6 +327,19 @@ def _kind(t, dtype):
     return torch.float32 if dtype == RAD_F32 else torch.bfloat16 if dtype == RAD_BF16 else t.dtype
 
 
+def _on_device(ctx, *tensors):
+    """Refuses tensors that lie elsewhere than on the context's GPU (on several, where the context's is not known): a kernel
+    that was given their addresses would fault."""
+    at = getattr(ctx, "device", None)
+    for t in tensors:
+        if t is None:
+            continue
+        where = t.get_device()                           # (-1: no GPU's)
+        if where < 0 or (at is not None and where != at):
+            raise RadError(RAD_ERR_PARAM, "a tensor on %s, not on the context's GPU" % t.device)
+        at = where
+
+
 def _check_lists(teacher, rows):
     if len(teacher.lists[0]) != rows:
         raise RadError(RAD_ERR_SHAPE, "the teacher has %d rows, not %d" % (len(teacher.lists[0]), rows))
@@ -335,12 +350,13 @@ def rad_distill_ce(ctx, logits, teacher, dtype, dlogits=None, row_weight=None, r
     rows, classes = logits.shape
     n, f32, kind = rows * classes, torch.float32, _kind(logits, dtype)
     _check_lists(teacher, rows)
-    _check(ctx, lib().rad_distill_ce(
-        ctx, _arg("logits", logits, n, kind), teacher, _arg("row_weight", row_weight, rows, f32), rows, classes, dtype,
-        _arg("dlogits", dlogits, n, kind), _arg("row_loss", row_loss, rows, f32), _arg("loss", loss, 1, f32)))
+    args = (_arg("logits", logits, n, kind), teacher, _arg("row_weight", row_weight, rows, f32), rows, classes, dtype,
+            _arg("dlogits", dlogits, n, kind), _arg("row_loss", row_loss, rows, f32), _arg("loss", loss, 1, f32))
+    _on_device(ctx, logits, *teacher.lists, row_weight, dlogits, row_loss, loss)
+    _check(ctx, lib().rad_distill_ce(ctx, *args))
 
 
-def _head_call(call, ctx, layer, x, W, bias, targets, row_weight, row_loss, loss, dX, dW, dbias, beta):
+def _head_call(call, ctx, layer, x, W, bias, targets, lists, row_weight, row_loss, loss, dX, dW, dbias, beta):
     import torch
     n, d, v = layer.batch, layer.d_in, layer.d_out
     f32 = torch.float32
@@ -350,24 +366,25 @@ def _head_call(call, ctx, layer, x, W, bias, targets, row_weight, row_loss, loss
         dw_kind = RAD_BF16
         if dW.dtype is not torch.bfloat16:
             raise RadError(RAD_ERR_PARAM, "dW is fp32 or of the layer's type")
-    _check(ctx, call(
-        ctx, layer, _arg("x", x, n * d, td), _arg("W", W, d * v, td), _arg("bias", bias, v, f32), targets,
-        _arg("row_weight", row_weight, n, f32), _arg("row_loss", row_loss, n, f32), _arg("loss", loss, 1, f32),
-        _arg("dX", dX, n * d, td), None if dW is None else _arg("dW", dW, d * v, dW.dtype), dw_kind, _arg("dbias", dbias, v, f32), beta))
+    args = (_arg("x", x, n * d, td), _arg("W", W, d * v, td), _arg("bias", bias, v, f32), targets,
+            _arg("row_weight", row_weight, n, f32), _arg("row_loss", row_loss, n, f32), _arg("loss", loss, 1, f32),
+            _arg("dX", dX, n * d, td), None if dW is None else _arg("dW", dW, d * v, dW.dtype), dw_kind, _arg("dbias", dbias, v, f32), beta)
+    _on_device(ctx, x, W, bias, *lists, row_weight, row_loss, loss, dX, dW, dbias)
+    _check(ctx, call(ctx, layer, *args))
 
 
 def rad_linear_ce(ctx, layer, x, W, bias, labels, row_weight=None, row_loss=None, loss=None, dX=None, dW=None, dbias=None,
                   beta=0.0):
     """dW: an fp32 tensor, or one of the layer's type."""
     import torch
-    _head_call(lib().rad_linear_ce, ctx, layer, x, W, bias, _arg("labels", labels, layer.batch, torch.int32), row_weight, row_loss,
-               loss, dX, dW, dbias, beta)
+    _head_call(lib().rad_linear_ce, ctx, layer, x, W, bias, _arg("labels", labels, layer.batch, torch.int32), (labels,), row_weight,
+               row_loss, loss, dX, dW, dbias, beta)
 
 
 def rad_linear_distill(ctx, layer, x, W, bias, teacher, row_weight=None, row_loss=None, loss=None, dX=None, dW=None,
                        dbias=None, beta=0.0):
     _check_lists(teacher, layer.batch)
-    _head_call(lib().rad_linear_distill, ctx, layer, x, W, bias, teacher, row_weight, row_loss, loss, dX, dW, dbias, beta)
+    _head_call(lib().rad_linear_distill, ctx, layer, x, W, bias, teacher, teacher.lists, row_weight, row_loss, loss, dX, dW, dbias, beta)
 
 
 def rad_model_create_mlp(ctx, dtype, batch, dims, has_bias, scheme, p):

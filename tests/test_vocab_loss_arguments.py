@@ -68,3 +68,73 @@ def test_distill(kind, td):
             refused(lambda: B.rad_distill_ce(None, z, teacher, kind, **{**good, name: t}))
     for t in (torch.zeros(4, 16, dtype=H if td == F else F), torch.zeros(16, 4, dtype=td).t(), torch.zeros(5, 16, dtype=td)):
         refused(lambda: B.rad_distill_ce(None, t, teacher, kind, **good))
+
+
+@pytest.mark.parametrize("kind,td", [(B.RAD_F32, F), (B.RAD_BF16, H)])
+def test_tensors_in_host_memory(kind, td):
+    """Labels and lists come from data loaders: a call on host tensors of the right sizes is refused, not handed to a kernel."""
+    layer = B.make_layer(4, 8, 16, dtype=kind, relu=False, has_bias=True)
+    x, W, bias, loss = torch.zeros(4, 8, dtype=td), torch.zeros(8, 16, dtype=td), torch.zeros(16), torch.zeros(1)
+    teacher = B.make_teacher(torch.zeros(4, 2, dtype=I), torch.zeros(4, 2))
+    for call in (lambda: B.rad_linear_ce(None, layer, x, W, bias, torch.zeros(4, dtype=I), loss=loss),
+                 lambda: B.rad_linear_distill(None, layer, x, W, bias, teacher, loss=loss),
+                 lambda: B.rad_distill_ce(None, torch.zeros(4, 16, dtype=td), teacher, kind, loss=loss)):
+        with pytest.raises(B.RadError, match="not on the context's GPU") as e:
+            call()
+        assert e.value.status == B.RAD_ERR_PARAM
+
+
+class Placed:
+    """What the checks read of a tensor that lies on GPU `at` (-1: in host memory)."""
+
+    def __init__(self, t, at):
+        self.t, self.at, self.device = t, at, "cuda:%d" % at if at >= 0 else "cpu"
+
+    def get_device(self):
+        return self.at
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def __len__(self):
+        return len(self.t)
+
+
+@pytest.mark.parametrize("known", [True, False])
+def test_every_tensor_is_on_the_context_s_gpu(known, monkeypatch):
+    """Each argument in turn in host memory or on a second GPU; the call itself is taken out, and seen only where all are right."""
+    given = dict(x=(4, 8), W=(8, 16), bias=(16,), row_weight=(4,), row_loss=(4,), loss=(1,), dX=(4, 8), dW=(8, 16), dbias=(16,))
+    layer, reached = B.make_layer(4, 8, 16, relu=False, has_bias=True), []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *_: reached.append(name) or B.RAD_OK
+    monkeypatch.setattr(B, "lib", Library)
+    ctx = B.P()
+    if known:
+        ctx.device = 1
+
+    def arguments(other=None, at=1):
+        place = lambda name, t: Placed(t, at if name == other else 1)  # noqa: E731
+        teacher = B.rad_teacher(2, 1.0, None, None)
+        teacher.lists = place("index", torch.zeros(4, 2, dtype=I)), place("logit", torch.zeros(4, 2))
+        tensors = {n: place(n, torch.zeros(s)) for n, s in given.items()}
+        return tensors, place("labels", torch.zeros(4, dtype=I)), teacher, place("logits", torch.zeros(4, 16)), place("dlogits", torch.zeros(4, 16))
+
+    def calls(other=None, at=1):
+        t, labels, teacher, z, dz = arguments(other, at)
+        dense = {n: t[n] for n in ("row_weight", "row_loss", "loss")}
+        return [("rad_linear_ce", set(given) | {"labels"}, lambda: B.rad_linear_ce(ctx, layer, labels=labels, **t)),
+                ("rad_linear_distill", set(given) | {"index", "logit"}, lambda: B.rad_linear_distill(ctx, layer, teacher=teacher, **t)),
+                ("rad_distill_ce", {"logits", "dlogits", "index", "logit", *dense}, lambda: B.rad_distill_ce(ctx, z, teacher, B.RAD_F32, dz, **dense))]
+    for name, _, call in calls():
+        call()
+    assert reached == ["rad_linear_ce", "rad_linear_distill", "rad_distill_ce"]
+    for other in list(given) + ["labels", "index", "logit", "logits", "dlogits"]:
+        for at in (-1, 0):
+            for name, takes, call in calls(other, at):
+                if other in takes:
+                    with pytest.raises(B.RadError) as e:
+                        call()
+                    assert e.value.status == B.RAD_ERR_PARAM, (name, other, at)
+    assert len(reached) == 3
