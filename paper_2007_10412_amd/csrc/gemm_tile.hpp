@@ -169,10 +169,10 @@ __device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* s
   int mine_at = 0;
   if (EPI == kEpiVocab && g.head.list_out) {
     __shared__ int32_t s_n[kGemmThreads / 64];
-    __shared__ float s_max[kGemmThreads / 64];
+    __shared__ float2 s_w[kGemmThreads / 64];
     const bool write = block == 0 && split == 0;
-    live = g.head.rows <= 4 * kGemmThreads ? own_rows<4>(g.head, g.N, s_n, s_max, write, &mine, &mine_at)
-                                           : own_rows<kOwnListRows / kGemmThreads>(g.head, g.N, s_n, s_max, write, &mine, &mine_at);
+    live = g.head.rows <= 4 * kGemmThreads ? own_rows<4>(g.head, g.N, s_n, s_w, write, &mine, &mine_at)
+                                           : own_rows<kOwnListRows / kGemmThreads>(g.head, g.N, s_n, s_w, write, &mine, &mine_at);
   } else {
     live = *g.head.live;
   }

@@ -4,11 +4,32 @@
 
 namespace rad {
 
+// What row gradients are divided by and the products multiplied by at their ends (row weights w of the rows that count): T x the
+// largest |w|.  Not where that is infinite or NaN, whose rows would take the others' gradients with them, nor where rows whose
+// weight is below 2^-60 of a factor above 1 would lose theirs to underflow; then 1, and each row has its own weight.
+struct WeightRange {
+  float most = 0.f, least = INFINITY;                      // of |w|; infinite or NaN: infinity; zeros are not among the least
+  __device__ __forceinline__ void add(float w) {
+    w = fabsf(w);
+    most = fmaxf(most, w < INFINITY ? w : INFINITY);
+    if (w > 0.f) least = fminf(least, w);
+  }
+  __device__ __forceinline__ void join(float m, float l) { most = fmaxf(most, m); least = fminf(least, l); }
+  __device__ __forceinline__ void join_wave() {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) join(__shfl_xor(most, o), __shfl_xor(least, o));
+  }
+  __device__ __forceinline__ float common(float T) const {
+    const float f = T * most;
+    return f > 0.f && f < INFINITY && (f <= 1.f || least >= most * 0x1p-60f) ? f : 1.f;
+  }
+};
+
 // The rows that count, made into a list by a workgroup for itself: a thread has PER consecutive rows, of which `mine` count, the
 // first of them at place `at`.  Returns their number; the workgroup that writes leaves the whole list in memory.
-// s_n: a word a wave.
+// s_n: a word a wave; s_w: a pair.
 template <int PER>
-__device__ __forceinline__ int own_rows(const HeadArgs& h, int classes, int32_t* s_n, float* s_max, bool write, uint32_t* mine_out, int* at_out) {
+__device__ __forceinline__ int own_rows(const HeadArgs& h, int classes, int32_t* s_n, float2* s_w, bool write, uint32_t* mine_out, int* at_out) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r0 = (int)threadIdx.x * PER;
   uint32_t mine = 0u;
 #pragma unroll
@@ -20,12 +41,11 @@ __device__ __forceinline__ int own_rows(const HeadArgs& h, int classes, int32_t*
   for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(up, o); if (lane >= o) up += v; }
   if (lane == 63) s_n[w] = up;
   if (write && h.weight) {
-    float m = 0.f;
+    WeightRange of;
 #pragma unroll
-    for (int q = 0; q < PER; ++q) if ((mine >> q) & 1u) m = fmaxf(m, fabsf(h.weight[r0 + q]));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    if (lane == 0) s_max[w] = m;
+    for (int q = 0; q < PER; ++q) if ((mine >> q) & 1u) of.add(h.weight[r0 + q]);
+    of.join_wave();
+    if (lane == 0) s_w[w] = make_float2(of.most, of.least);
   }
   __syncthreads();
   int at = up - n, all = 0;
@@ -35,11 +55,11 @@ __device__ __forceinline__ int own_rows(const HeadArgs& h, int classes, int32_t*
   if (write) {
     if (threadIdx.x == 0) {
       const float inv = h.inv_count_out ? (all > 0 ? 1.f / (float)all : 0.f) : h.weight ? 0.f : *h.inv_count;
-      float m = 0.f;
-      if (h.weight) for (int q = 0; q < kGemmThreads / 64; ++q) m = fmaxf(m, s_max[q]);
+      WeightRange of;
+      if (h.weight) for (int q = 0; q < kGemmThreads / 64; ++q) of.join(s_w[q].x, s_w[q].y);
       *h.live_out = all;
       if (h.inv_count_out) *h.inv_count_out = inv;
-      *h.common_out = h.temperature * (h.weight ? m : inv);
+      *h.common_out = h.weight ? of.common(h.temperature) : h.temperature * inv;
     }
 #pragma unroll
     for (int q = 0; q < PER; ++q) {

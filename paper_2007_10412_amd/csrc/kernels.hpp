@@ -319,8 +319,8 @@ hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, 
 
 // ---- the layer under such a loss, fp32 or bf16 (vocab_head.hip), around the products with HeadArgs
 // list [rows]: the rows that count, in order, then the others; *live: how many count; *inv_count: 1 / that (null: *t.inv_count
-// is there); *common = T x (the largest |weight| of these rows, or, without weights, the inverse count): what dX, dW and dbias
-// are multiplied by at their ends.  dz holds row gradients of weight 1 (or a share of 1): a factor that all rows have in common,
+// is there); *common = T x the largest |weight| of these rows (1 where that would lose some of them: WeightRange) or, without
+// weights, T x the inverse count: what dX, dW and dbias are multiplied by at their ends.  dz holds row gradients of weight 1 (or a share of 1): a factor that all rows have in common,
 // rounded into each of them, would put its one rounding error on the whole gradient (0.3 % of dW where 1 / n falls badly).
 hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, float* common,
                            hipStream_t st);

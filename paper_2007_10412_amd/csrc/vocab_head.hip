@@ -19,6 +19,7 @@ __global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows
                                                         int32_t* __restrict__ live, float* __restrict__ inv_count,
                                                         float* __restrict__ common) {
   __shared__ int s_n[16];
+  __shared__ float2 s_w[16];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   auto counts = [&](int r) { return t.labels ? (uint32_t)t.labels[r] < (uint32_t)classes : t.counts[r] != 0; };
   int total = 0;                                        // rows that count (of one block of rows: below)
@@ -57,21 +58,19 @@ __global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows
     }
     before += all;
   }
-  float m = 0.f;
+  WeightRange of;
   if (t.weight) {
-    for (int r = threadIdx.x; r < rows; r += 1024) if (counts(r)) m = fmaxf(m, fabsf(t.weight[r]));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    for (int r = threadIdx.x; r < rows; r += 1024) if (counts(r)) of.add(t.weight[r]);
+    of.join_wave();
+    if (lane == 0) s_w[w] = make_float2(of.most, of.least);
     __syncthreads();
-    if (lane == 0) s_n[w] = (int)__float_as_uint(m);
-    __syncthreads();
-    for (int q = 0; q < 16; ++q) m = fmaxf(m, __uint_as_float((uint32_t)s_n[q]));
+    for (int q = 0; q < 16; ++q) of.join(s_w[q].x, s_w[q].y);
   }
   if (threadIdx.x == 0) {
     const float inv = inv_count ? (total > 0 ? 1.f / (float)total : 0.f) : t.weight ? 0.f : *t.inv_count;
     *live = total;
     if (inv_count) *inv_count = inv;
-    *common = t.temperature * (t.weight ? m : inv);
+    *common = t.weight ? of.common(t.temperature) : t.temperature * inv;
   }
 }
 
@@ -127,9 +126,9 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(GemmArgs g) {
   }
 }
 
-// a row's share of *common
+// a row's share of *common (with weights never zero)
 __device__ __forceinline__ float row_share(const VocabTargets& t, int row, float common) {
-  return !t.weight ? 1.f : common > 0.f ? t.weight[row] * t.temperature / common : 0.f;
+  return !t.weight ? 1.f : t.weight[row] * t.temperature / common;
 }
 
 // (maximum, sum of exponentials from it) of two parts; one with nothing in it adds its 0, or its NaN

@@ -1,0 +1,64 @@
+"""Losses over a vocabulary at the ends of what their arguments may hold, against the definition in fp64 with the bounds of
+test_gpu_vocab_loss (whose helpers these tests use)."""
+import math
+
+import pytest
+
+from tests.test_gpu_vocab_loss import (HALF, ROUTES, U, Ctx, check_linear, close, definition, inputs, labels_for, lists, run_linear,
+                                       softmax_error, teacher_for, torch_dtype)
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ row weights
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,d_in,classes", ROUTES)
+@pytest.mark.parametrize("k", [0, 4])
+@pytest.mark.parametrize("how", ["nan", "inf", "all_nan"])
+def test_weights_that_are_not_finite(dtype, rows, d_in, classes, k, how):
+    """They reach their own rows of dX, and all of dW, dbias and the loss; rows of other weights keep their gradient."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen, x, W, layer = inputs(dtype, rows, d_in, classes)
+    labels = labels_for(rows, classes, gen, 0.3)
+    labels[1], labels[2] = 1, -1
+    counts = (labels >= 0) & (labels < classes)
+    index, logit = teacher_for(rows, classes, k or 1, gen)
+    index[~counts] = -1
+    asked = dict(labels=labels) if not k else dict(teacher=B.make_teacher(index, logit))
+    finite = torch.rand(rows, device="cuda", generator=gen) + 0.5
+    bad = torch.arange(rows, device="cuda") % 17 == 1
+    if how == "all_nan":
+        bad = counts.clone()
+    weight = torch.where(bad, torch.full_like(finite, math.inf if how == "inf" else math.nan), finite)
+    with Ctx() as ctx:
+        out = run_linear(ctx, layer, x, W, weight=weight, **asked)
+    xd, Wd = x.double(), W.double()
+    z = xd @ Wd
+    targets = lists(labels=labels, classes=classes) if not k else lists(teacher=(index, logit), classes=classes)
+    row, _, dz, soft, target = definition(z, targets, finite, 1.0)
+    rel = softmax_error(8 * U * math.sqrt(d_in + 2) * float((xd.abs() @ Wd.abs()).max()), classes)
+    ep = U * (6 * float(logit.abs().max()) + 6 + 8 * math.sqrt(logit.shape[1])) if k else 0.0
+    e = soft * rel + 2.02 * HALF[dtype] * (soft + target) + (4 * U + ep) * target
+    want = dz @ Wd.t().contiguous()
+    bound = (e + 8 * U * math.sqrt(classes) * dz.abs()) @ Wd.abs().t().contiguous() + HALF[dtype] * want.abs() + 1e-37
+    good = ~(bad & counts)
+    close(out["dX"][good], want[good], bound[good], "dX")
+    assert (out["dX"][~counts] == 0).all()
+    close(out["row_loss"], row, (rel + 8 * U * (targets[2].abs() + z.abs().max() + 30)) * torch.ones_like(row), "row_loss")
+    assert not torch.isfinite(out["dX"][bad & counts]).any()
+    for n in ("loss", "dW", "dbias"):
+        assert not torch.isfinite(out[n]).any(), n
+
+
+@pytest.mark.parametrize("dtype,dw_dtype", [(0, 0), (1, 0), (1, 1)])
+@pytest.mark.parametrize("rows,d_in,classes", ROUTES)
+@pytest.mark.parametrize("scale", [1e22, 1e-15, 1e-34])
+def test_weights_far_apart(dtype, dw_dtype, rows, d_in, classes, scale):
+    """Weights of 10^44 times each other (down to 10^-35 of 1): none of them is lost beside the others."""
+    import torch
+    weight = torch.tensor([scale, 1e-22, -1.0, 0.0] if scale > 1 else [scale, -scale, 0.1 * scale], device="cuda")
+    weight = weight[torch.arange(rows, device="cuda") % len(weight)].contiguous()
+    with Ctx() as ctx:
+        check_linear(ctx, dtype, rows, d_in, classes, bias=True, ignored=0.3, weight=weight, dw_dtype=dw_dtype)
+        check_linear(ctx, dtype, rows, d_in, classes, k=5, T=2.0, weight=weight, dw_dtype=dw_dtype)
