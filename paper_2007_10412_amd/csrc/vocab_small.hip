@@ -107,6 +107,7 @@ __global__ __launch_bounds__(256) void few_classes_kernel(FewClasses a) {
   const float g = counts && v < V ? wt / s * e - wt * p : 0.f;
   if (a.dz && w == 0 && row < a.rows) a.dz[(int64_t)row * VP + v] = g;
   if (!a.dx) return;
+  const uint64_t live = __ballot(counts);               // (a row that does not count: zeros, also where W holds what 0 times is NaN)
   for (int d0 = 0; d0 < a.d_in; d0 += 256) {
     const int d = d0 + (int)threadIdx.x;
     float sum[R];
@@ -121,7 +122,7 @@ __global__ __launch_bounds__(256) void few_classes_kernel(FewClasses a) {
     if (d < a.d_in) {
 #pragma unroll
       for (int rr = 0; rr < R; ++rr)
-        if (row0 + rr < a.rows) st_elem(static_cast<T*>(a.dx) + (int64_t)(row0 + rr) * a.d_in + d, sum[rr]);
+        if (row0 + rr < a.rows) st_elem(static_cast<T*>(a.dx) + (int64_t)(row0 + rr) * a.d_in + d, (live >> (rr * VP)) & 1u ? sum[rr] : 0.f);
     }
   }
 }

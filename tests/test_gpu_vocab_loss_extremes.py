@@ -62,3 +62,23 @@ def test_weights_far_apart(dtype, dw_dtype, rows, d_in, classes, scale):
     with Ctx() as ctx:
         check_linear(ctx, dtype, rows, d_in, classes, bias=True, ignored=0.3, weight=weight, dw_dtype=dw_dtype)
         check_linear(ctx, dtype, rows, d_in, classes, k=5, T=2.0, weight=weight, dw_dtype=dw_dtype)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,d_in,classes", ROUTES)
+@pytest.mark.parametrize("k", [0, 4])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_rows_without_a_target_have_no_gradient_whatever_w_holds(dtype, rows, d_in, classes, k, value):
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen, x, W, layer = inputs(dtype, rows, d_in, classes)
+    labels = labels_for(rows, classes, gen, 0.3)
+    labels[:2] = -1
+    gone = (labels < 0) | (labels >= classes)
+    index, logit = teacher_for(rows, classes, k or 1, gen)
+    index[gone] = -1
+    W[d_in // 2, classes // 2] = value
+    asked = dict(labels=labels) if not k else dict(teacher=B.make_teacher(index, logit))
+    with Ctx() as ctx:
+        out = run_linear(ctx, layer, x, W, **asked)
+    assert (out["dX"][gone] == 0).all() and (out["row_loss"][gone] == 0).all()
