@@ -25,6 +25,32 @@ struct WeightRange {
   }
 };
 
+// sum_j p_j (z_j - base) over a row's targets of p > 0, base the largest of their logits: with it a loss is (lse - base) minus this
+// sum, and nothing large cancels, whichever targets a mask of the type's lowest value has taken out (from the first target's
+// logit, masked so and of probability 0, the loss came out as -8e31).
+struct TargetSum {
+  float base = -INFINITY, mass = 0.f, dot = 0.f;
+  __device__ __forceinline__ void add(float p, float z) {
+    if (z == -INFINITY) { dot = -INFINITY; return; }       // (such a target costs infinity)
+    if (z > base) {
+      if (mass > 0.f) dot += mass * (base - z);
+      base = z;
+    }
+    mass += p;
+    dot += p * (z - base);
+  }
+  __device__ __forceinline__ void join(float b, float m, float d) {
+    const float most = fmaxf(base, b);
+    if (mass > 0.f) dot += mass * (base - most);
+    if (m > 0.f) d += m * (b - most);
+    base = most; mass += m; dot += d;
+  }
+  __device__ __forceinline__ void join_lane(int o) { join(__shfl_xor(base, o), __shfl_xor(mass, o), __shfl_xor(dot, o)); }
+  __device__ __forceinline__ void put(float3* to) const { *to = make_float3(base, mass, dot); }
+  __device__ __forceinline__ void join(const float3& o) { join(o.x, o.y, o.z); }
+  __device__ __forceinline__ float from() const { return base == -INFINITY ? 0.f : base; }
+};
+
 // The rows that count, made into a list by a workgroup for itself: a thread has PER consecutive rows, of which `mine` count, the
 // first of them at place `at`.  Returns their number; the workgroup that writes leaves the whole list in memory.
 // s_n: a word a wave; s_w: a pair.

@@ -146,7 +146,8 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2, flo
 constexpr int kFinishThreads = 1024, kFinishRows = 16, kFinishAhead = 4;
 template <typename T>
 __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinish a, int shift) {
-  __shared__ float s_m[16][kFinishRows], s_s[16][kFinishRows], s_d[16][kFinishRows];
+  __shared__ float s_m[16][kFinishRows], s_s[16][kFinishRows];
+  __shared__ float3 s_t[16][kFinishRows];
   __shared__ int s_row[kFinishRows];
   const int R = 1 << shift, r = (int)threadIdx.x & (R - 1), grp = (int)threadIdx.x >> shift, groups = kFinishThreads >> shift;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -157,7 +158,8 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinis
   const bool counts = place < live;
   const int row = place < a.rows ? a.list[place] : -1;
 
-  float m = -INFINITY, s = 0.f, dot = 0.f, z0 = 0.f;
+  float m = -INFINITY, s = 0.f;
+  TargetSum sum;
   if (counts) {
     for (int p = grp; p < a.parts; p += groups * kFinishAhead) {
       float2 v[kFinishAhead];
@@ -169,28 +171,25 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinis
 #pragma unroll
       for (int q = 0; q < kFinishAhead; ++q) join(m, s, v[q].x, v[q].y, c);
     }
-    // sum_j p_j (z_j - z_0), z_0 the first target's logit
-    z0 = a.target[(int64_t)place * t.k];
-    if (z0 == -INFINITY) z0 = 0.f;
     for (int j = grp; j < t.k; j += groups) {
       const float pj = t.labels ? 1.f : t.prob[(int64_t)row * t.k + j];
-      if (pj != 0.f) dot += pj * (a.target[(int64_t)place * t.k + j] - z0);
+      if (pj != 0.f) sum.add(pj, a.target[(int64_t)place * t.k + j]);
     }
   }
   for (int o = R; o < 64; o <<= 1) {
     join(m, s, __shfl_xor(m, o), __shfl_xor(s, o), c);
-    dot += __shfl_xor(dot, o);
+    sum.join_lane(o);
   }
-  if (lane < R) { s_m[wave][r] = m; s_s[wave][r] = s; s_d[wave][r] = dot; }
+  if (lane < R) { s_m[wave][r] = m; s_s[wave][r] = s; sum.put(&s_t[wave][r]); }
   __syncthreads();
   if ((int)threadIdx.x < R) {
-    for (int w = 1; w < 16; ++w) { join(m, s, s_m[w][r], s_s[w][r], c); dot += s_d[w][r]; }
+    for (int w = 1; w < 16; ++w) { join(m, s, s_m[w][r], s_s[w][r], c); sum.join(s_t[w][r]); }
     s_row[r] = row;
     float part = 0.f;                                   // of the batch's loss
     if (counts) {
       const float T1 = t.temperature, top = m == -INFINITY ? 0.f : m;
       const float weight = t.weight ? t.weight[row] : *t.inv_count;
-      const float loss = T1 * T1 * ((t.labels ? 0.f : t.entropy[row]) + (logf(s) + ((top - z0) - dot) / T1));
+      const float loss = T1 * T1 * ((t.labels ? 0.f : t.entropy[row]) + (logf(s) + ((top - sum.from()) - sum.dot) / T1));
       a.row_loss[row] = loss;
       a.top[place] = top;
       a.factor[place] = row_share(t, row, *a.common) / s;

@@ -267,7 +267,7 @@ __device__ __forceinline__ void store_part(T* out, const RowPart<T, NT, NV>& p, 
 }
 
 // SPLIT: the row's parts are dealt to gridDim.x workgroups.  PASS 0 leaves each part's maximum and sum in stats
-// [rows][parts][2] and, with part 0, the first target's logit z_0 and sum_j p_j (z_{i_j} - z_0) in dots [rows][2]; PASS 1 joins
+// [rows][parts][2] and, with part 0, the targets' largest logit z_0 and sum_j p_j (z_{i_j} - z_0) in dots [rows][2]; PASS 1 joins
 // them, part by part in order, and writes.  Without SPLIT one workgroup has the whole row in its registers, and memory bounds it:
 // 4096 x 32000 bf16 101 us (5.2 TB/s), 777 x 50257 40 (3.9; three rows a CU).  4 x 128000 fp32 takes 4 + 9 in parts.
 // count: the rows that count are counted here (by every workgroup for itself).
@@ -277,6 +277,7 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
   typedef RowPart<T, NT, NV> Part;
   constexpr int VPL = Part::VPL, NW = NT / 64;
   __shared__ float s_m[NW], s_s[NW], s_w[NW], s_tz[kTeacherMax];
+  __shared__ float3 s_t[NW];
   const int row = SPLIT ? blockIdx.y + blockIdx.z * 65535 : blockIdx.x + blockIdx.y * kRowsX;
   if (row >= a.rows) return;
   const int part = SPLIT ? blockIdx.x : 0, v0 = part * NT * NV;
@@ -307,16 +308,20 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
   }
   // The targets' logits: all of them for the loss (one part of a row), those of this part for the gradient.  They are read
   // here, ahead of any store: dz may be z.
-  float dot = 0.f, z0 = 0.f;
-  if (part == 0 && !(SPLIT && PASS == 1)) { z0 = ld_elem(z + index[0]); if (z0 == -INFINITY) z0 = 0.f; }
+  TargetSum sum;
   for (int j = threadIdx.x; j < t.k; j += NT) {
     const int i = index[j];
     const float pj = prob[j];
     const bool mine = i >= c_lo && i < c_hi;
     if (i < 0 || pj == 0.f || (!mine && (PASS == 1 && SPLIT ? true : part != 0))) continue;
     const float v = ld_elem(z + i);
-    dot += pj * (v - z0);
+    if (!(SPLIT && PASS == 1)) sum.add(pj, v);
     s_tz[j] = v;
+  }
+  if (!(SPLIT && PASS == 1) && part == 0) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum.join_lane(o);
+    if ((threadIdx.x & 63) == 0) sum.put(&s_t[threadIdx.x >> 6]);
   }
 
   float m = -INFINITY, s = 0.f, wm = -INFINITY;
@@ -330,7 +335,12 @@ __global__ __launch_bounds__(NT) void vocab_rows_kernel(VocabRows a, float* __re
     const float b = exp_base(m);
 #pragma unroll
     for (int w = 0; w < NW; ++w) s += rebased(s_s[w], s_m[w], b, c);
-    if (part == 0) dot = block_sum<NT>(dot, s_w);
+  }
+  float z0 = 0.f, dot = 0.f;
+  if (!(SPLIT && PASS == 1) && part == 0 && threadIdx.x == 0) {
+    TargetSum all;
+    for (int w = 0; w < NW; ++w) all.join(s_t[w]);
+    z0 = all.from(); dot = all.dot;
   }
   if (SPLIT && PASS == 0) {
     if (threadIdx.x == 0) {

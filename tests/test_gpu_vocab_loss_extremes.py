@@ -82,3 +82,60 @@ def test_rows_without_a_target_have_no_gradient_whatever_w_holds(dtype, rows, d_
     with Ctx() as ctx:
         out = run_linear(ctx, layer, x, W, **asked)
     assert (out["dX"][gone] == 0).all() and (out["row_loss"][gone] == 0).all()
+
+
+# ------------------------------------------------------------------ masks of the type's lowest value
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,classes", [(5, 40), (300, 1000), (40, 20000), (3, 140001)])
+@pytest.mark.parametrize("T", [1.0, 2.0, 0.7])
+def test_first_target_masked_in_both(dtype, rows, classes, T):
+    """The teacher's list begins with classes that both models mask with their type's lowest value: they have no share of the
+    loss, which is the others'."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    td = torch_dtype(dtype)
+    z = (3 * torch.randn(rows, classes, device="cuda", generator=gen)).to(td)
+    top = float(z.abs().max())
+    z[:, :3] = torch.finfo(td).min
+    index = torch.cat([torch.tensor([[1, 0, 2]], device="cuda").repeat(rows, 1),
+                       3 + torch.rand(rows, min(classes - 3, 4096), device="cuda", generator=gen).argsort(dim=1)[:, :6]], dim=1).to(torch.int32)
+    logit = 2 * torch.randn(rows, 9, device="cuda", generator=gen)
+    logit[:, :3] = torch.finfo(torch.float32).min
+    row, dz = torch.empty(rows, device="cuda"), torch.empty_like(z)
+    with Ctx() as ctx:
+        B.rad_distill_ce(ctx, z, B.make_teacher(index, logit, T), dtype, dz, row_loss=row)
+        B.rad_ctx_synchronize(ctx)
+    targets = lists(teacher=(index, logit), classes=classes, T=T)
+    want, _, g, soft, target = definition(z.double(), targets, None, T)
+    rel = softmax_error(4 * U * top / T, classes)
+    close(row, want, T * T * (rel + 8 * U * (targets[2].abs() + 30 + top / T)) * torch.ones_like(want), "row_loss")
+    ep = U * (6 * float(logit[:, 3:].abs().max()) / T + 6 + 8 * 3)
+    close(dz, g, soft * rel + (4 * U + ep) * target + HALF[dtype] * g.abs() + 1e-37, "dlogits")
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,d_in,classes", ROUTES)
+@pytest.mark.parametrize("T", [1.0, 0.7])
+def test_first_target_masked_by_a_bias(dtype, rows, d_in, classes, T):
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen, x, W, _ = inputs(dtype, rows, d_in, classes)
+    layer = B.make_layer(rows, d_in, classes, dtype=dtype, relu=False, has_bias=True)
+    bias = torch.zeros(classes, device="cuda")
+    bias[:2] = torch.finfo(torch.float32).min
+    index = torch.tensor([[0, 5, 1, 7]], device="cuda", dtype=torch.int32).repeat(rows, 1)
+    logit = torch.randn(rows, 4, device="cuda", generator=gen)
+    logit[:, 0] = logit[:, 2] = torch.finfo(torch.float32).min
+    row, loss = torch.empty(rows, device="cuda"), torch.empty(1, device="cuda")
+    with Ctx() as ctx:
+        B.rad_linear_distill(ctx, layer, x, W, bias, B.make_teacher(index, logit, T), row_loss=row, loss=loss)
+        B.rad_ctx_synchronize(ctx)
+    xd, Wd = x.double(), W.double()
+    z = xd @ Wd
+    size, top = float((xd.abs() @ Wd.abs()).max()), float(z.abs().max())
+    targets = lists(teacher=(index, logit), classes=classes, T=T)
+    want, total, _, _, _ = definition(z + bias.double(), targets, None, T)
+    bound = T * T * (softmax_error(8 * U * math.sqrt(d_in + 2) * size / T, classes) + 8 * U * (float(targets[2].abs().max()) + top / T + 30))
+    close(row, want, bound * torch.ones_like(want), "row_loss")
+    assert abs(float(loss) - float(total)) <= bound + 8 * U * math.sqrt(rows) * float(want.abs().max())
