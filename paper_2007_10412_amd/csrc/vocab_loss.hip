@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int32_t* __restrict_
     float t = -INFINITY;
     if (live && j < k) {
       const int32_t i = index[at + j];
-      const float l = logit[at + j] * inv_t;
+      const float l = logit[at + j];
       if ((uint32_t)i < (uint32_t)classes && l != -INFINITY) { kj = ((uint64_t)(uint32_t)i << 32) | (uint32_t)j; t = l; }
     }
     key[j] = kj;
@@ -99,13 +99,13 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int32_t* __restrict_
   if (__any(bad)) m = NAN;
   float s = 0.f, h = 0.f;
   for (int j = lane; j < P; j += 64)
-    if (key[j] != kNone) s += expf(p[j] - m);
+    if (key[j] != kNone) s += expf((p[j] - m) * inv_t);   // (divided by T after the maximum is off: the logits may be fp32's last)
   s = wave_sum(s);
   const float log_s = logf(s), inv_s = 1.f / s;
   for (int j = lane; j < P; j += 64) {
     float pj = 0.f;
     if (key[j] != kNone) {
-      const float d = p[j] - m;
+      const float d = (p[j] - m) * inv_t;
       pj = expf(d) * inv_s;
       if (pj != 0.f) h += pj * (d - log_s);             // p log p -> 0
     }

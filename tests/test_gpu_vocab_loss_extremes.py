@@ -139,3 +139,32 @@ def test_first_target_masked_by_a_bias(dtype, rows, d_in, classes, T):
     bound = T * T * (softmax_error(8 * U * math.sqrt(d_in + 2) * size / T, classes) + 8 * U * (float(targets[2].abs().max()) + top / T + 30))
     close(row, want, bound * torch.ones_like(want), "row_loss")
     assert abs(float(loss) - float(total)) <= bound + 8 * U * math.sqrt(rows) * float(want.abs().max())
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,classes", [(6, 40), (300, 1000), (3, 140001)])
+@pytest.mark.parametrize("T", [0.5, 1e-6, 3.0])
+def test_teacher_logits_at_the_ends_of_fp32(dtype, rows, classes, T):
+    """Logits that leave fp32 when they are divided by T count as what they are: a list of the lowest value is one of equal
+    entries, the highest value has all of its row."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    z = torch.randn(rows, classes, device="cuda", generator=gen).to(torch_dtype(dtype)) * min(T, 1.0)
+    f = torch.finfo(torch.float32)
+    index = torch.tensor([[3, 11, 7, 2]], device="cuda", dtype=torch.int32).repeat(rows, 1)
+    logit = torch.tensor([[f.min] * 4, [f.max, 0.0, 1.0, f.min], [f.min, -math.inf, f.min, 0.25 * f.min]], device="cuda")
+    logit = logit[torch.arange(rows, device="cuda") % 3].contiguous()
+    row, loss, dz = torch.empty(rows, device="cuda"), torch.empty(1, device="cuda"), torch.empty_like(z)
+    with Ctx() as ctx:
+        B.rad_distill_ce(ctx, z, B.make_teacher(index, logit, T), dtype, dz, row_loss=row, loss=loss)
+        B.rad_ctx_synchronize(ctx)
+    targets = lists(teacher=(index, logit), classes=classes, T=T)
+    assert targets[3].all()
+    want, total, g, soft, target = definition(z.double(), targets, None, T)
+    # (the lists' probabilities are 1, 0, 1/4: the exponentials of 0 and -infinity, and a division)
+    rel = softmax_error(4 * U * float(z.double().abs().max()) / T, classes)
+    bound = T * T * (rel + 8 * U * (targets[2].abs() + 30 + float(z.double().abs().max()) / T))
+    close(row, want, bound * torch.ones_like(want), "row_loss")
+    close(loss.double(), total.reshape(1), (bound + 8 * U * math.sqrt(rows) * want.abs()).mean().reshape(1), "loss")
+    close(dz, g, soft * rel + 8 * U * target + HALF[dtype] * g.abs() + 1e-37, "dlogits")
