@@ -326,12 +326,15 @@ rad_status rad_distill_ce(rad_ctx* ctx, const void* logits, const rad_teacher* t
  * are formed from, is rounded to that type; sums are fp32).  bias, dbias,
  * row_loss [batch] and loss [1] are fp32.  beta is 0 or 1.  Outputs may be null,
  * not all: without dX, dW and dbias the call scores, as for the
- * log-probabilities of tokens that a model has answered.  Logits (bf16 layers:
- * 16-bit codes of them, then dz) exist for a piece of the rows at a time, in a
- * context workspace of at most 2 GiB (or 256 rows, if they are more).  Further
- * workspaces: a copy of W or x where its rows are not whole 16-byte vectors (or
- * its address is no multiple of 16); for a bf16 dW of several pieces, or with
- * beta = 1, the fp32 sums [d_in, d_out]; partial sums where a product has few
+ * log-probabilities of tokens that a model has answered.  The rows go through in
+ * pieces whose logits (bf16 layers: 16-bit codes of them, then dz) and whose rows
+ * of x have at most 2 GiB each, or of 256 rows if those are more.  Context
+ * workspaces: the logits of a piece where there is a gradient; the rows of x of
+ * a piece where there is a dW; a copy of W, and of a piece of x, where rows are
+ * not whole 16-byte vectors (or the address is no multiple of 16); 8 bytes per
+ * row and 64 classes of a piece, 16 per row of it and 12 per row of the batch;
+ * for a bf16 dW of several pieces, or with beta = 1, the fp32 sums
+ * [d_in, d_out]; 128 bytes a class for dbias; partial sums where a product has few
  * tiles.  d_in * d_out < 2^32, both at most 2^22 - 64.  Outputs overlap neither
  * inputs nor each other.  Enqueued on the context's stream; results do not vary
  * from call to call. */
@@ -341,7 +344,7 @@ rad_status rad_linear_ce(rad_ctx* ctx, const rad_layer* layer, const void* x, co
 
 /* The same with a teacher's lists in the place of labels: the loss and dz of
  * rad_distill_ce on the logits of the layer.  Its workspaces hold 8 k + d_out / 32
- * bytes a row besides. */
+ * bytes per row of the batch and 4 k per row of a piece besides. */
 rad_status rad_linear_distill(rad_ctx* ctx, const rad_layer* layer, const void* x, const void* W, const float* bias,
                               const rad_teacher* teacher, const float* row_weight, float* row_loss, float* loss,
                               void* dX, void* dW, int32_t dw_dtype, float* dbias, float beta);

@@ -1517,9 +1517,9 @@ extern "C" rad_status rad_distill_ce(rad_ctx* c, const void* logits, const rad_t
   return vocab_loss_sum(c, a.t, losses, (int)rows, (int)classes, loss);
 }
 
-// Bytes of logits (bf16: their 16-bit codes) and then of their gradient that exist at a time: rows go through the layer in
-// pieces of this size.
-constexpr size_t kLogitPieceBytes = (size_t)2 << 30;
+// Rows go through the layer in pieces, of which the logits (bf16: their 16-bit codes, then their gradient) have at most this many
+// bytes, and so has x (whose rows are gathered for dW, or copied to whole vectors).
+constexpr size_t kPieceBytes = (size_t)2 << 30;
 
 struct HeadCall {
   const void* x; const void* W; const float* bias;
@@ -1643,17 +1643,16 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   const int64_t esz = dtype == kF32 ? 4 : 2, vec = 16 / esz;
   const int64_t dp = (d_in + vec - 1) / vec * vec, vp8 = (d_out + vec - 1) / vec * vec, vp = (d_out + 63) / 64 * 64;
   const bool train = h.dX || h.dW || h.dbias;
-  // a piece: logits of 2 GiB, rows of x that 32-bit byte offsets reach
-  int64_t piece = std::min<int64_t>((int64_t)(kLogitPieceBytes / ((size_t)vp * esz)), (((int64_t)1 << 32) - 1) / (dp * esz));
+  // (32-bit byte offsets reach the rows of x in a piece, also where it is the least of 256 rows)
+  int64_t piece = (int64_t)(kPieceBytes / ((size_t)std::max(vp, dp) * esz));
   piece = std::max<int64_t>(std::min<int64_t>(piece / 256 * 256, 1 << 19), 256);
   if (piece > rows) piece = rows;
   const bool one = piece >= rows;
 
-  const void *W = nullptr, *x = nullptr;
+  const void* W = nullptr;
   // (a copy's rows are whole cache lines: the tiles' 256-byte pieces of them then take two lines, not three)
   const int64_t w_ld = vp8 == d_out && (reinterpret_cast<uintptr_t>(h.W) & 15) == 0 ? d_out : vp;
   RAD_TRY(head_padded(c, WS_HEADW, dtype, h.W, d_in, d_out, w_ld, &W));
-  RAD_TRY(head_padded(c, WS_HEADX, dtype, h.x, rows, d_in, dp, &x));
 
   const HeadPlan fwd = head_plan(dtype, kEpiVocab, piece, d_out, d_in, true);
   const int part = fwd.splits > 1 ? 64 : head_part(fwd.tile), parts = (d_out + part - 1) / part;
@@ -1684,6 +1683,8 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
 
   for (int64_t r0 = 0; r0 < rows; r0 += piece) {
     const int n = (int)std::min<int64_t>(piece, rows - r0);
+    const void* x = nullptr;
+    RAD_TRY(head_padded(c, WS_HEADX, dtype, static_cast<const char*>(h.x) + r0 * d_in * esz, n, d_in, dp, &x));
     VocabTargets tp = t;
     if (tp.labels) tp.labels += r0;
     else { tp.index += r0 * t.k; tp.prob += r0 * t.k; tp.entropy += r0; tp.counts += r0; }
@@ -1699,7 +1700,7 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
       HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(tp, n, d_out, list, live, inv_count, common, c->stream); }));
     GemmArgs g = gemm_zero();
     g.M = n; g.N = d_out; g.K = d_in;
-    g.A = static_cast<const char*>(x) + r0 * dp * esz; g.lda = dp; g.B = W; g.ldb = w_ld;
+    g.A = x; g.lda = dp; g.B = W; g.ldb = w_ld;
     g.bias = h.bias; g.y = z; g.ldy = vp;
     HeadArgs& a = g.head;
     a.live = live; a.row_map = list; a.rows = n; a.n_load = (int)vp8;

@@ -168,3 +168,75 @@ def test_teacher_logits_at_the_ends_of_fp32(dtype, rows, classes, T):
     close(row, want, bound * torch.ones_like(want), "row_loss")
     close(loss.double(), total.reshape(1), (bound + 8 * U * math.sqrt(rows) * want.abs()).mean().reshape(1), "loss")
     close(dz, g, soft * rel + 8 * U * target + HALF[dtype] * g.abs() + 1e-37, "dlogits")
+
+
+# ------------------------------------------------------------------ rows in pieces
+def test_workspaces_of_wide_rows():
+    """x of 5 GB in rows of odd width: they are copied, and gathered for dW, a piece at a time, and the context holds no more than
+    its header says; the gradients are those of all rows."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    rows, d_in, classes = 600001, 4095, 24
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.empty(rows, d_in, device="cuda", dtype=torch.bfloat16)
+    x.normal_(0, 1, generator=gen)
+    W = (torch.randn(d_in, classes, device="cuda", generator=gen) / math.sqrt(d_in)).to(torch.bfloat16)
+    labels = labels_for(rows, classes, gen, 0.2)
+    counts = (labels >= 0) & (labels < classes)
+    row, dX, dW = torch.empty(rows, device="cuda"), torch.full_like(x, math.nan), torch.empty(d_in, classes, device="cuda")
+    with Ctx() as ctx:
+        torch.cuda.synchronize()
+        before = torch.cuda.mem_get_info()[0]
+        B.rad_linear_ce(ctx, B.make_layer(rows, d_in, classes, dtype=1, relu=False), x, W, None, labels, row_loss=row, dX=dX, dW=dW)
+        B.rad_ctx_synchronize(ctx)
+        held = before - torch.cuda.mem_get_info()[0]
+    piece = 2 ** 31 // (4096 * 2)
+    partial = 64 * d_in * 64 * 4                                    # K of dW in up to 64 splits
+    small = piece * (64 * 2 + 8 + 16) + rows * 12 + d_in * 64 * 2
+    assert held <= 2 * 2 ** 31 + small + partial + 2 ** 26, held    # (and what modules and allocation granules take)
+    n, Wd = int(counts.sum()), W.double()
+    want_dW, bound, mass = (torch.zeros(d_in, classes, device="cuda", dtype=torch.float64) for _ in range(3))
+    for r in range(0, rows, 60000):
+        at = slice(r, min(rows, r + 60000))
+        xd = x[at].double()
+        weight = torch.full((len(xd),), 1 / n, device="cuda", dtype=torch.float64)
+        want, _, dz, soft, target = definition(xd @ Wd, lists(labels=labels[at], classes=classes), weight, 1.0)
+        rel = softmax_error(8 * U * math.sqrt(d_in) * float((xd.abs() @ Wd.abs()).max()), classes)
+        close(row[at], want, (rel + 8 * U * 50) * torch.ones_like(want), "row_loss %d" % r)
+        e = soft * rel + 2.02 * HALF[1] * (soft + target) + 4 * U * target
+        want_dX = dz @ Wd.t().contiguous()
+        close(dX[at], want_dX, (e + 8 * U * math.sqrt(classes) * dz.abs()) @ Wd.abs().t().contiguous() + HALF[1] * want_dX.abs() + 1e-37, "dX %d" % r)
+        xt = xd.t().contiguous()
+        want_dW += xt @ dz
+        bound += xt.abs() @ e
+        mass += xt.abs() @ dz.abs()
+    close(dW, want_dW, bound + 8 * U * math.sqrt(rows) * mass, "dW")
+
+
+def test_most_rows_of_an_odd_width():
+    """2^24 rows of x, whose copy to whole vectors has 2^32 of them: more than one launch has threads."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    rows, d_in, classes = 1 << 24, 2041, 17
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 90 << 30:
+        pytest.skip("takes 76 GB of GPU memory")
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    some = (torch.randn(4093, d_in, device="cuda", generator=gen)).to(torch.bfloat16)
+    x = torch.empty(rows, d_in, device="cuda", dtype=torch.bfloat16)
+    for r in range(0, rows, len(some)):
+        x[r:r + len(some)] = some[:min(len(some), rows - r)]
+    W = (torch.randn(d_in, classes, device="cuda", generator=gen) / math.sqrt(d_in)).to(torch.bfloat16)
+    label = labels_for(len(some), classes, gen, 0.2)
+    labels = label.repeat(rows // len(some) + 1)[:rows].contiguous()
+    row = torch.full((rows,), math.nan, device="cuda")
+    with Ctx() as ctx:
+        B.rad_linear_ce(ctx, B.make_layer(rows, d_in, classes, dtype=1, relu=False), x, W, None, labels, row_loss=row)
+        B.rad_ctx_synchronize(ctx)
+    xd, Wd = some.double(), W.double()
+    want, _, _, _, _ = definition(xd @ Wd, lists(labels=label, classes=classes), None, 1.0)
+    rel = softmax_error(8 * U * math.sqrt(d_in) * float((xd.abs() @ Wd.abs()).max()), classes)
+    close(row[:len(some)], want, (rel + 8 * U * 50) * torch.ones_like(want), "row_loss")
+    for r in range(len(some), rows, 512 * len(some)):               # (the same rows, in other places of other pieces)
+        n = min(512 * len(some), rows - r)
+        assert torch.equal(row[r:r + n], row[:len(some)].repeat(512)[:n]), r
