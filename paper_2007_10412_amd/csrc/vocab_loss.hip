@@ -411,17 +411,29 @@ hipError_t rows_whole(const VocabRows& a, hipStream_t st) {
   hipLaunchKernelGGL((vocab_rows_kernel<T, NT, NV, false, 1>), dim3(std::min(a.rows, kRowsX), (a.rows + kRowsX - 1) / kRowsX), dim3(NT), 0, st, a, (float*)nullptr, vocab_rows_count(a) ? 1 : 0);
   return hipGetLastError();
 }
+// Long rows that are few go in parts too, which takes a launch and a second read but gives them more than a CU each.  us of a call
+// with lists of 16, whole / in parts.  bf16 with gradients: 1 x 128000 24.9 / 16.4, 64 x 128000 29.4 / 22.3, 128 x 66000 26.5 / 22.8,
+// 128 x 128000 33.2 / 32.5, but 200 x 128000 34.8 / 47.3; 1 x 33000 16.2 / 14.8, 64 x 33000 17.9 / 17.0, but 256 x 33000 20.4 / 22.0,
+// 1 x 20000 12.0 / 14.4.  The loss alone: 1 x 128000 17.9 / 14.9, 64 x 128000 19.4 / 17.7, but 128 x 128000 22.5 / 24.8, 64 x 33000
+// 15.0 / 15.1.  fp32 (half the exponentials in a vector) with gradients: 1 x 65000 16.4 / 15.4, 16 x 33000 16.1 / 16.0, but
+// 64 x 33000 17.2 / 17.8, 1 x 25000 12.6 / 14.0; the loss alone 1 x 65000 12.8 / 13.8.
+template <typename T> bool few_long_rows(int rows, int64_t vecs, bool gradient) {
+  const bool longest = vecs > 512 * 16;                               // (they take 1024 threads a row)
+  if (sizeof(T) == 4) return gradient && longest && rows <= 16;
+  return longest ? rows <= (gradient ? 128 : 64) : gradient && vecs > 512 * 8 && rows <= 64;
+}
 template <typename T>
 hipError_t rows_any(const VocabRows& a, hipStream_t st) {
   constexpr int VPL = 16 / (int)sizeof(T);
   const int64_t vecs = (int64_t)a.classes / VPL + 1;                  // (one for the single elements at the end)
+  const bool whole = !few_long_rows<T>(a.rows, vecs, a.dz != nullptr);
   if (vecs <= 64 * 4) return rows_whole<T, 64, 4>(a, st);
   if (vecs <= 128 * 4) return rows_whole<T, 128, 4>(a, st);
   if (vecs <= 256 * 4) return rows_whole<T, 256, 4>(a, st);
   if (vecs <= 256 * 8) return rows_whole<T, 256, 8>(a, st);
   if (vecs <= 512 * 8) return rows_whole<T, 512, 8>(a, st);
-  if (vecs <= 512 * 16) return rows_whole<T, 512, 16>(a, st);
-  if (vecs <= 1024 * 16) return rows_whole<T, 1024, 16>(a, st);
+  if (vecs <= 512 * 16 && whole) return rows_whole<T, 512, 16>(a, st);
+  if (vecs <= 1024 * 16 && whole) return rows_whole<T, 1024, 16>(a, st);
   const int64_t parts = (vecs + kPartThreads * kPartVecs - 1) / (kPartThreads * kPartVecs);
   float* const dots = a.stats + (int64_t)a.rows * parts * 2;
   const dim3 grid((unsigned)parts, (unsigned)(a.rows < 65535 ? a.rows : 65535), (unsigned)((a.rows + 65534) / 65535));

@@ -4,8 +4,8 @@ import math
 
 import pytest
 
-from tests.test_gpu_vocab_loss import (HALF, ROUTES, U, Ctx, check_linear, close, definition, inputs, labels_for, lists, run_linear,
-                                       softmax_error, teacher_for, torch_dtype)
+from tests.test_gpu_vocab_loss import (HALF, ROUTES, U, Ctx, check_distill, check_linear, close, definition, inputs, labels_for, lists,
+                                       run_linear, softmax_error, teacher_for, torch_dtype)
 
 pytestmark = pytest.mark.gpu
 
@@ -240,3 +240,13 @@ def test_most_rows_of_an_odd_width():
     for r in range(len(some), rows, 512 * len(some)):               # (the same rows, in other places of other pieces)
         n = min(512 * len(some), rows - r)
         assert torch.equal(row[r:r + n], row[:len(some)].repeat(512)[:n]), r
+
+
+@pytest.mark.parametrize("dtype,rows,classes", [(1, 1, 32760), (1, 64, 33000), (1, 65, 33000), (1, 1, 65537), (1, 128, 66001), (1, 129, 66001), (1, 3, 131064),
+                                                (0, 1, 32765), (0, 16, 33001), (0, 17, 33001), (0, 5, 65530)])
+@pytest.mark.parametrize("how", ["", "missing", "in_place", "shifted", "loss"])
+def test_few_long_rows(dtype, rows, classes, how):
+    """Rows of one workgroup or of several, on both sides of the borders between them."""
+    with Ctx() as ctx:
+        check_distill(ctx, dtype, rows, classes, 9, T=1.3, missing=0.4 if how == "missing" else 0.0, in_place=how == "in_place",
+                      shift=3 if how == "shifted" else 0, outputs=("row_loss", "loss") if how == "loss" else ("dlogits", "row_loss", "loss"))
