@@ -292,7 +292,8 @@ rad_status rad_softmax_ce(rad_ctx* ctx, const void* logits, const int32_t* label
  * logit[r][j] with index in [0, classes) and logit above -infinity; others are
  * left out, so a list may be shorter than k (fill with index -1) or empty.  The
  * target is the softmax of logit / temperature over the list; an index that
- * comes twice has the sum of its probabilities. */
+ * comes twice has the sum of its probabilities (the sums over j below are over
+ * the list's entries, each with the p of its own). */
 typedef struct {
   int32_t k;            /* entries per row, 1 to 1024 */
   double temperature;   /* T, 1e-6 to 1e6 */

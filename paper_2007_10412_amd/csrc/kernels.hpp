@@ -280,9 +280,8 @@ hipError_t launch_conv_dw_direct(const float* xt, const float* g, float* part, i
                                  int ks, hipStream_t st);
 
 // ---- losses over a vocabulary (vocab_loss.hip).  What the rows are to learn, cross entropy being the list of one entry
-// of probability 1: labels [rows], or prepared lists index [rows][k] (ascending; a row's missing entries, -1, at the end)
-// with probabilities prob [rows][k] (entries of one index joined in the first of them, 0 in the others), entropy [rows]
-// (sum p log p) and counts [rows] (1 where a row has an entry, else 0).
+// of probability 1: labels [rows], or prepared lists index [rows][k] (ascending, each class once; the rest of a row, -1,
+// at the end) with probabilities prob [rows][k], entropy [rows] (sum p log p of the entries as they were given) and counts [rows] (1 where a row has an entry, else 0).
 struct VocabTargets {
   const int32_t* labels;
   const int32_t* index; const float* prob; const float* entropy; const int32_t* counts;

@@ -64,7 +64,7 @@ __device__ __forceinline__ void wave_lds_fence() {
 
 // ------------------------------------------------------------------ targets
 // A wave per row.  Keys (index, place in the list) are sorted in LDS by a bitonic network over P >= k places, which puts
-// entries of one index side by side; the first of them takes their probabilities.  Missing entries sort to the end.  The chain of
+// entries of one index side by side; they become one of their probabilities' sum.  Missing entries sort to the end.  The chain of
 // exchanges bounds it (4 lists of 128 5.7 us) until its loads do (4096 of 64 8.3).
 template <int P>
 __global__ __launch_bounds__(256) void teacher_kernel(const int32_t* __restrict__ index, const float* __restrict__ logit, int rows,
@@ -125,19 +125,33 @@ __global__ __launch_bounds__(256) void teacher_kernel(const int32_t* __restrict_
     }
   if (!live) return;
   const bool some = key[0] != kNone;
-  for (int j = lane; j < k; j += 64) {
-    const uint64_t kj = key[j];
+  // Entries of one index become one, in the first places; the places behind the last one hold none.  (64 of them at a time: an
+  // entry moves to a place at or before its own, once all of the 64 are read.)
+  int kept = 0;
+  for (int j0 = 0; j0 < k; j0 += 64) {
+    const int j = j0 + lane;
+    const uint64_t kj = j < k ? key[j] : kNone;
+    const bool head = kj != kNone && (j == 0 || (key[j - 1] >> 32) != (kj >> 32));
     float sum = 0.f;
-    if (kj != kNone && (j == 0 || (key[j - 1] >> 32) != (kj >> 32)))
+    if (head)
       for (int q = j; q < k && (key[q] >> 32) == (kj >> 32) && key[q] != kNone; ++q) sum += p[(uint32_t)key[q]];
-    index_out[at + j] = kj == kNone ? -1 : (int32_t)(kj >> 32);
-    prob[at + j] = sum;
+    const uint64_t heads = __ballot(head);
+    const int to = kept + __popcll(heads & ((1ull << lane) - 1));
+    wave_lds_fence();
+    if (head) {
+      key[to] = kj;
+      index_out[at + to] = (int32_t)(kj >> 32);
+      prob[at + to] = sum;
+    }
+    wave_lds_fence();
+    kept += __popcll(heads);
   }
+  for (int j = kept + lane; j < k; j += 64) { index_out[at + j] = -1; prob[at + j] = 0.f; }
   if (lane == 0) { entropy[row] = some ? h : 0.f; counts[row] = some ? 1 : 0; }
   if (!first) return;
   // entries before class part t (missing ones lie after all); a kernel of its own for this: 200 x 768 x 10007, k = 16 174 us, not 170
   for (int t = lane; t <= parts; t += 64) {
-    int lo = 0, hi = k;
+    int lo = 0, hi = kept;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
       if ((uint32_t)(key[mid] >> 32) < (uint32_t)t * (uint32_t)part) lo = mid + 1; else hi = mid;

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void few_classes_kernel(FewClasses a) {
   if (counts) {
     if (t.labels) p = label == v ? 1.f : 0.f;
     else
-      for (int j = 0; j < t.k; ++j) {                   // (sorted, joined: at most V of them)
+      for (int j = 0; j < t.k; ++j) {                   // (sorted, each class once)
         const int i = t.index[(int64_t)row * t.k + j];
         if (i < 0) break;
         if (i == v) p += t.prob[(int64_t)row * t.k + j];

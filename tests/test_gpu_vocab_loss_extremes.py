@@ -250,3 +250,38 @@ def test_few_long_rows(dtype, rows, classes, how):
     with Ctx() as ctx:
         check_distill(ctx, dtype, rows, classes, 9, T=1.3, missing=0.4 if how == "missing" else 0.0, in_place=how == "in_place",
                       shift=3 if how == "shifted" else 0, outputs=("row_loss", "loss") if how == "loss" else ("dlogits", "row_loss", "loss"))
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,d_in,classes,k", [(150, 300, 10, 1024), (5, 64, 1, 130), (300, 512, 1000, 1024), (64, 128, 300, 129), (7, 64, 2100, 64)])
+def test_lists_that_repeat_themselves(dtype, rows, d_in, classes, k):
+    """Longer than there are classes, or from half of them: every class of a list comes several times."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen, x, W, layer = inputs(dtype, rows, d_in, classes)
+    index, logit = teacher_for(rows, classes, k, gen, missing=0.2, doubles=True)
+    row, dX, dW, dz = torch.empty(rows, device="cuda"), torch.empty_like(x), torch.empty_like(W), torch.empty(rows, classes, device="cuda")
+    z32 = (x.float() @ W.float()).contiguous()
+    dense = torch.empty(rows, device="cuda")
+    with Ctx() as ctx:
+        B.rad_linear_distill(ctx, layer, x, W, None, B.make_teacher(index, logit, 1.5), row_loss=row, dX=dX, dW=dW)
+        B.rad_distill_ce(ctx, z32, B.make_teacher(index, logit, 1.5), B.RAD_F32, dz, row_loss=dense)
+        B.rad_ctx_synchronize(ctx)
+    xd, Wd = x.double(), W.double()
+    z = xd @ Wd
+    targets = lists(teacher=(index, logit), classes=classes, T=1.5)
+    want, _, g, soft, target = definition(z, targets, None, 1.5)
+    rel = softmax_error(8 * U * math.sqrt(d_in + 2) * float((xd.abs() @ Wd.abs()).max()) / 1.5, classes)
+    ep = U * (6 * float(logit[torch.isfinite(logit)].abs().max()) / 1.5 + 6 + 8 * math.sqrt(k))
+    bound = 1.5 ** 2 * (rel + ep * (z.abs().max() + 30) + 8 * U * (targets[2].abs() + z.abs().max() / 1.5 + 30)) * torch.ones_like(want)
+    close(row, want, bound, "row_loss")
+    e = soft * rel + 2.02 * HALF[dtype] * (soft + target) + (4 * U + ep) * target
+    want_dX = g @ Wd.t().contiguous()
+    close(dX, want_dX, (e + 8 * U * math.sqrt(classes) * g.abs()) @ Wd.abs().t().contiguous() + HALF[dtype] * want_dX.abs() + 1e-37, "dX")
+    want_dW = xd.t().contiguous() @ g
+    close(dW, want_dW, xd.abs().t().contiguous() @ (e + 8 * U * math.sqrt(rows) * g.abs()) + HALF[dtype] * want_dW.abs() + 1e-37, "dW")
+    # (dense logits: as z32 has them)
+    want, _, g, soft, target = definition(z32.double(), targets, None, 1.5)
+    rel = softmax_error(4 * U * float(z32.abs().max()) / 1.5, classes)
+    close(dense, want, bound, "dense row_loss")
+    close(dz, g, soft * rel + (4 * U + ep) * target + U * g.abs() + 1e-37, "dlogits")
