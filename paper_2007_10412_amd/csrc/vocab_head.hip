@@ -197,10 +197,7 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinis
     } else if (place < a.rows) {
       a.row_loss[row] = 0.f;
     }
-    if (a.loss && gridDim.x == 1 && !a.z) {
-      for (int o = 1; o < R; o <<= 1) part += __shfl_xor(part, o);
-      if (r == 0) *a.loss = part;
-    }
+    if (a.loss && !a.z) *a.loss = part;                 // (of one row: vocab_loss_inside)
   }
   __syncthreads();
   if (a.xs && live < a.rows) {
@@ -432,7 +429,7 @@ template <typename T> static hipError_t gradient_of(const VocabFinish& a, hipStr
   else hipLaunchKernelGGL((vocab_gradient_kernel<T, 4>), grid, dim3(256), 0, st, a, sum_column);
   return hipGetLastError();
 }
-bool vocab_loss_inside(const VocabFinish& a) { return a.z || a.rows <= 1 << finish_shift(a.rows); }
+bool vocab_loss_inside(const VocabFinish& a) { return a.z || a.rows == 1; }
 hipError_t launch_vocab_finish(const VocabFinish& a, hipStream_t st) {
   const int shift = finish_shift(a.rows);
   const dim3 grid((a.rows + (1 << shift) - 1) >> shift);
