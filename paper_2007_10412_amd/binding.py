@@ -341,8 +341,9 @@ def _on_device(ctx, *tensors):
 
 
 def _check_lists(teacher, rows):
-    if len(teacher.lists[0]) != rows:
-        raise RadError(RAD_ERR_SHAPE, "the teacher has %d rows, not %d" % (len(teacher.lists[0]), rows))
+    have, k = teacher.lists[0].shape
+    if have != rows or k != teacher.k:
+        raise RadError(RAD_ERR_SHAPE, "the teacher has %d rows of %d entries, not %d of %d" % (have, k, rows, teacher.k))
 
 
 def rad_distill_ce(ctx, logits, teacher, dtype, dlogits=None, row_weight=None, row_loss=None, loss=None):

@@ -138,3 +138,13 @@ def test_every_tensor_is_on_the_context_s_gpu(known, monkeypatch):
                         call()
                     assert e.value.status == B.RAD_ERR_PARAM, (name, other, at)
     assert len(reached) == 3
+
+
+def test_lists_of_another_length_than_the_teacher_says():
+    """k is a field that a program can set: more than the tensors have would be read past their ends."""
+    layer = B.make_layer(4, 8, 16, relu=False)
+    for k in (1, 3, 1024):
+        teacher = B.make_teacher(torch.zeros(4, 2, dtype=I), torch.zeros(4, 2))
+        teacher.k = k
+        refused(lambda: B.rad_linear_distill(None, layer, torch.zeros(4, 8), torch.zeros(8, 16), None, teacher, loss=torch.zeros(1)))
+        refused(lambda: B.rad_distill_ce(None, torch.zeros(4, 16), teacher, B.RAD_F32, loss=torch.zeros(1)))
