@@ -308,9 +308,12 @@ typedef struct {
  * of rows whose list is not empty.  A row with an empty list has no loss and a
  * gradient of zeros, whatever its weight.  logits and dlogits [rows, classes]
  * in dtype; dlogits may be logits (outputs that overlap an input or each other in
- * any other way are refused).  row_loss [rows] and loss [1]: fp32 on the device.  Any of dlogits, row_loss, loss may be null, not all.  Statistics and
- * sums are fp32, in a fixed order.  A logit of -infinity has probability zero;
- * a row of nothing else gives NaN.  Enqueued on the context's stream. */
+ * any other way are refused).  row_loss [rows] and loss [1]: fp32 on the device.
+ * Any of dlogits, row_loss, loss may be null, not all.  Statistics and sums are
+ * fp32, in a fixed order; a row loss, T^2 times a difference of numbers of the
+ * order of log(classes) + |logits| / T, is off by some 10^-6 T^2.  A logit of
+ * -infinity has probability zero; a row of nothing else gives NaN.  Enqueued on
+ * the context's stream. */
 rad_status rad_distill_ce(rad_ctx* ctx, const void* logits, const rad_teacher* teacher, const float* row_weight,
                           int64_t rows, int64_t classes, int32_t dtype, void* dlogits, float* row_loss, float* loss);
 
@@ -323,8 +326,9 @@ rad_status rad_distill_ce(rad_ctx* ctx, const void* logits, const rad_teacher* t
  * labels: int32 DEVICE [batch]; a row whose label lies outside [0, d_out) has no
  * loss and adds to no gradient (its dX is zero).  w_r = row_weight[r] (DEVICE
  * [batch], may be null: 1 / the number of the other rows).  dX is in the
- * layer's dtype; dw_dtype is RAD_F32 or the layer's dtype (dz, which dW and dX
- * are formed from, is rounded to that type; sums are fp32).  bias, dbias,
+ * layer's dtype; dw_dtype is RAD_F32 or the layer's dtype.  dz, which dX, dW and
+ * dbias are formed from, is rounded to the layer's type (but for small layers of
+ * up to 16 classes, where it stays fp32); sums are fp32.  bias, dbias,
  * row_loss [batch] and loss [1] are fp32.  beta is 0 or 1.  Outputs may be null,
  * not all: without dX, dW and dbias the call scores, as for the
  * log-probabilities of tokens that a model has answered.  The rows go through in

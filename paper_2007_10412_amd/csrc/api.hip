@@ -1532,8 +1532,11 @@ struct HeadCall {
 //   and a launch)
 // with what these took for 16 to 4000 rows, 300 to 4096 columns of x and 1000 to 100000 classes, in us.  In bf16, 256-row
 // tiles are the cheapest per slice and the dearest to begin and end, and a CU alone runs them faster than all together:
-// x W of 4000 x 1000 x 20000 takes 236 us in 256-row tiles, 233 in 128, 277 in 64; 1500 x 4096 x 20000 244, 277, 367;
-// 300 x 1000 x 20000 43, 26, 30; 100 x 1000 x 5000 38, 18, 14.
+// x W of 4000 x 1000 x 20000 takes 180 us in 256-row tiles, 188 in 128, 241 in 64; 1500 x 4096 x 20000 194, 241, 317;
+// 300 x 1000 x 20000 32, 23, 29; 100 x 1000 x 5000 29, 16, 13 (called alone in a loop).  The prices order the tiles rather than
+// foretell a time: they are 0.97 to 1.45 of what these take, but 45 us for x W of 4096 x 4096 x 1000, which takes 46 alone and 55
+// among the kernels of its step.  The worst choice among 11 measured is 6 % from the best (fp32 1500 x 512 x 2000, 46.4 in 128-row tiles, 43.7 in 64).
+// All rows are planned for: how many of them have a target only the device knows.
 struct HeadPlan { int tile, k_split, splits; };
 static HeadPlan head_plan(int dtype, int epi, int64_t M, int64_t N, int64_t K, bool may_split) {
   struct Kind { int dtype, tile, cols; double fill_us, slice_us, alone_us, end_us; };
@@ -1598,10 +1601,11 @@ static rad_status head_split_sum(rad_ctx* c, const SplitSum& sum) {
   return RAD_OK;
 }
 
-// Two kernels, about 9 + rows / 50 + d_in / 115 us with all gradients, against the general route's five or more, about 45 us in
-// fp32 and 30 in bf16 at such sizes.  fp32: 150 x 300 x 10 15.1 against 44.5, 1000 x 300 x 10 31.8 against 48, 600 x 1024 x 10
-// 29 against 44, but 2000 x 64 x 10 49 against 45, 150 x 4096 x 10 48 against 44; bf16: 500 x 300 x 10 23.6 against 31.8,
-// 300 x 1024 x 10 25.7 against 30, but 1000 x 300 x 10 35 against 32.5, 150 x 4096 x 10 56 against 31.
+// Two kernels, about 9 + rows / 50 + d_in / 115 us with dX and dW, against the general route's five or more, about 45 us in
+// fp32 and 30 in bf16 at such sizes.  fp32: 150 x 300 x 10 14.4 against 43.7, 1000 x 300 x 10 31.2 against 47.4, 1500 x 300 x 10
+// 42.6 against 51.7, but 2000 x 64 x 10 47.6 against 44.1, 150 x 4096 x 10 48.7 against 41.9; bf16: 500 x 300 x 10 23.1 against 30.3,
+// 300 x 1024 x 10 25.2 against 27.0, but 1000 x 300 x 10 34.3 against 30.7, 150 x 4096 x 10 56.8 against 29.0.  (A bias gradient
+// costs the general route 5 to 8 more, here nothing: with one the borders would lie a fifth higher.)
 static bool few_classes_pay(int dtype, int64_t rows, int64_t d_in, int64_t d_out) {
   return d_out <= kFewClasses && 9 * rows + 4 * d_in <= (dtype == kF32 ? 16000 : 9000);
 }
@@ -1692,9 +1696,9 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     float* const inv_count = one && !row_weight ? const_cast<float*>(t.inv_count) : nullptr;
     const int64_t fwd_tiles = (int64_t)((n + fwd.tile - 1) / fwd.tile) * ((d_out + 127) / 128) * fwd.splits;
     // A launch for the list costs 5 us; lists made in the tiles cost each of them 1 or 2, which two bf16 tiles on a CU hide where
-    // rows are few.  us with / without a launch: bf16 4096 x 4096 x 1000 (256 tiles) 151 / 148, 2000 x 512 x 5000 (640) 68 / 67,
-    // 3000 x 512 x 4000 (768) 94 / 95, 1999 x 1000 x 50257 655 / 685, but 1000 x 1000 x 50257 502 / 498; fp32 1500 x 512 x 2000
-    // (192) 135 / 134, 1000 x 256 x 20000 (1256) 337 / 350.
+    // rows are few.  us with / without a launch: bf16 4096 x 4096 x 1000 (256 tiles) 152 / 151, 2000 x 512 x 5000 (640) 85 / 87,
+    // 3000 x 512 x 4000 (768) 94 / 95, 1000 x 1000 x 50257 493 / 495, but 1999 x 1000 x 50257 871 / 900; fp32 1500 x 512 x 2000
+    // (192) 135 / 134, 1000 x 256 x 20000 (1256) 339 / 337: 2 % either way but for many tiles.
     const bool own_list = n <= kOwnListRows && fwd.tile != 256 && (dtype == kBF16 ? n <= 1024 || fwd_tiles <= 640 : fwd_tiles <= 768);
     if (!own_list)
       HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(tp, n, d_out, list, live, inv_count, common, c->stream); }));
@@ -1753,8 +1757,9 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
       sw.scale = common;
       pw = head_plan(dtype, kEpiHeadW, d_in, d_out, n, d_in <= 65535);
     }
-    // One launch for both where both have small tiles: in bf16 (4096 x 1024 x 1000 84 -> 73 us, 500 x 1000 x 10000 90 -> 83), in
-    // fp32 where together they do not fill the chip (150 x 300 x 10 51 -> 45; 30 x 1000 x 20000 would go from 119 to 127).
+    // One launch for both where both have small tiles: in bf16 (4096 x 1024 x 1000 74 -> 67 us, 500 x 1000 x 10000 86 -> 83), in
+    // fp32 where together they do not fill the chip (a launch of the host's less: on the device 150 x 300 x 10 stays at 43;
+    // 30 x 1000 x 20000 would go from 130 to 132).
     const bool pair = h.dX && h.dW && px.tile != 256 && pw.tile == 128 &&
                       (dtype == kBF16 || head_workgroups(px, gx) + head_workgroups(pw, gw) <= 256);
     const size_t x_bytes = head_plan_bytes(px, gx), w_bytes = head_plan_bytes(pw, gw);

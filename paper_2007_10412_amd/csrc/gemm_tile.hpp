@@ -2,7 +2,7 @@
 // into LDS as in gemm_bf16_dma.hpp, slices of 128 bytes of K (64 bf16, 32 fp32) in a ring of S stages, S - 1 of them on their way.
 //
 // bf16: the 256 x 256 kernel needs 256 tiles to give every CU work.  100 rows x 1024 x 10000 are 40 of them, for whose 16
-// slices each CU waits alone (34 us, of which the weights' way from memory is 4); here they are 79 or 158, two to a CU, and a
+// slices each CU waits alone (28 us, of which the weights' way from memory is 4); here they are 79 or 158, two to a CU, and a
 // slice of the weights is asked for S - 1 slices ahead: 16 us in 128-row tiles, 13 in 64-row ones.
 // fp32: bound by the matrix cores (16 products of 32 x 32 x 2 per four 16-byte reads of LDS).
 #pragma once

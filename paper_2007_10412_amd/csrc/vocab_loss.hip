@@ -44,7 +44,8 @@ template <int NT> __device__ __forceinline__ float block_sum(float v, float* s_w
   return t;
 }
 
-// exp((v - m) / T) with c = log2(e) / T; m is finite
+// exp((v - m) / T) with c = log2(e) / T; m is finite.  (The product's rounding is an error of |v - m| c 2^-24 of the exponential, more than
+// expf's: gradients of 4 x 128000 fp32 logits are off by 1.3e-7 rms, where expf with a division gives 0.8e-7.)
 __device__ __forceinline__ float exp_from(float v, float m, float c) { return __builtin_amdgcn_exp2f((v - m) * c); }
 // what exponentials are taken from: the maximum, or 0 where nothing is left of a row (every exponential is 0 then)
 __device__ __forceinline__ float exp_base(float m) { return m == -INFINITY ? 0.f : m; }
