@@ -312,8 +312,9 @@ typedef struct {
  * Any of dlogits, row_loss, loss may be null, not all.  Statistics and sums are
  * fp32, in a fixed order; a row loss, T^2 times a difference of numbers of the
  * order of log(classes) + |logits| / T, is off by some 10^-6 T^2.  A logit of
- * -infinity has probability zero; a row of nothing else gives NaN.  Enqueued on
- * the context's stream. */
+ * -infinity has probability zero; a row of nothing else gives NaN.  Context
+ * workspaces: 44 + 8 k + classes / 512 bytes a row.  Enqueued on the context's
+ * stream. */
 rad_status rad_distill_ce(rad_ctx* ctx, const void* logits, const rad_teacher* teacher, const float* row_weight,
                           int64_t rows, int64_t classes, int32_t dtype, void* dlogits, float* row_loss, float* loss);
 
