@@ -447,14 +447,47 @@ typedef struct {
  * null for RAD_SGD).  dtype RAD_F32: params[i] fp32, updated in place, master
  * is ignored (may be null).  dtype RAD_BF16: master[i] holds the fp32 master
  * copy that is updated in place, and params[i] (bf16) receives its rounding
- * to nearest even.  Enqueued on the context's stream; does not wait.
+ * to nearest even.  Tensors that share memory are stepped in the order of the
+ * lists.  Enqueued on the context's stream; does not wait.
  * Errors (nothing is launched): RAD_ERR_NULL for a missing array or entry,
- * RAD_ERR_SHAPE for a negative count or n_tensors, RAD_ERR_PARAM for an
+ * RAD_ERR_SHAPE for a negative or too large (2^35) count or n_tensors, RAD_ERR_PARAM for an
  * unknown kind or dtype, t < 1, or coefficients outside the ranges above. */
 rad_status rad_optimizer_step(rad_ctx* ctx, const rad_optimizer* opt, int64_t t, int32_t dtype,
                               int32_t n_tensors, const int64_t* counts, void* const* params,
                               const void* const* grads, void* const* m, void* const* v,
                               void* const* master);
+
+/* The norm of n_tensors gradients together, as for clipping them:
+ *   *norm = sqrt(sum over tensors and elements of g^2),
+ *   *scale = min(1, max_norm / *norm), or 0 where the norm is not finite (a
+ *   gradient holds an infinity or a NaN, or the norm is beyond fp32's range).
+ * counts, grads and dtypes (rad_dtype each; null: all RAD_F32) are HOST arrays,
+ * grads' entries DEVICE tensors of counts[i] elements (16-byte aligned ones are
+ * read in vectors), which may come twice; norm and scale are DEVICE fp32, one of
+ * them may be null.  max_norm > 0, infinity for the norm alone.  At most 2^35
+ * elements in all.  Squares and sums are fp64, in a fixed order.  No tensors:
+ * a norm of 0.  Context workspace: 8 KiB per 128 tensors.  Enqueued on the
+ * context's stream. */
+rad_status rad_gradient_norm(rad_ctx* ctx, int32_t n_tensors, const int64_t* counts, const void* const* grads,
+                             const int32_t* dtypes, double max_norm, float* norm, float* scale);
+
+/* The gradients under that scale: clipped[i] = *scale * grads[i], rounded to the
+ * gradient's type; where the norm is not finite (*norm says so) the gradients as
+ * they are.  clipped: HOST array of DEVICE tensors; clipped[i] may be grads[i]
+ * (which then is neither read again nor written where nothing is to be clipped);
+ * outputs that overlap anything else are refused, and so is one tensor twice.
+ * norm (DEVICE) may be null. */
+rad_status rad_clip_gradients(rad_ctx* ctx, int32_t n_tensors, const int64_t* counts, const void* const* grads,
+                              const int32_t* dtypes, double max_norm, void* const* clipped, float* norm);
+
+/* rad_optimizer_step with *scale g in the place of g (*scale: DEVICE fp32, as
+ * rad_gradient_norm leaves it; g is not changed).  A scale of 0 leaves
+ * parameters, moments and master copies as they are: the step of a gradient
+ * whose norm is not finite is skipped, without the host knowing. */
+rad_status rad_optimizer_step_scaled(rad_ctx* ctx, const rad_optimizer* opt, int64_t t, int32_t dtype,
+                                     int32_t n_tensors, const int64_t* counts, void* const* params,
+                                     const void* const* grads, void* const* m, void* const* v,
+                                     void* const* master, const float* scale);
 
 /* ---- reaction-diffusion PDE-constrained optimisation -----------------------
  * Section 5 and Appendix B: phi on the nodes (i, j), 0 <= i, j <= n, of the

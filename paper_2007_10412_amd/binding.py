@@ -113,6 +113,9 @@ SIGNATURES = {
     "rad_optimizer_step": (C.c_int, [P, C.POINTER(rad_optimizer), C.c_int64, C.c_int32, C.c_int32,
                                      C.POINTER(C.c_int64), C.POINTER(P), C.POINTER(P), C.POINTER(P), C.POINTER(P),
                                      C.POINTER(P)]),
+    "rad_optimizer_step_scaled": (C.c_int, [P, C.POINTER(rad_optimizer), C.c_int64, C.c_int32, C.c_int32] + [P] * 7),
+    "rad_gradient_norm": (C.c_int, [P, C.c_int32, P, P, P, C.c_double, P, P]),
+    "rad_clip_gradients": (C.c_int, [P, C.c_int32, P, P, P, C.c_double, P, P]),
 }
 
 _lib = None
@@ -469,6 +472,64 @@ def rad_optimizer_step(ctx, opt, t, dtype, params, grads, m=None, v=None, master
     counts = (C.c_int64 * n)(*[int(x.numel()) for x in params])
     _check(ctx, lib().rad_optimizer_step(ctx, C.byref(opt), int(t), dtype, n, counts, arr(params), arr(grads), arr(m),
                                          arr(v), arr(master)))
+
+
+def _tensors(name, tensors, like, kinds):
+    """The HOST array of addresses of tensors (None: no array) that are to be contiguous, as large as those of `like`, and of the
+    given types."""
+    if tensors is None:
+        return None
+    if len(tensors) != len(like):
+        raise RadError(RAD_ERR_SHAPE, "%d tensors of %s, not %d" % (len(tensors), name, len(like)))
+    at = []
+    for t, other, kind in zip(tensors, like, kinds):
+        if t.dtype is not kind or t.numel() != other.numel() or not t.is_contiguous():
+            raise RadError(RAD_ERR_SHAPE, "%s holds a tensor that is not a contiguous one of %d elements of %s" % (name, other.numel(), kind))
+        at.append(t.data_ptr())
+    return (P * len(at))(*at)
+
+
+def _gradients(grads):
+    """(counts, addresses, types, rad_dtypes) of a list of gradients, fp32 and bf16"""
+    import torch
+    kinds = [t.dtype for t in grads]
+    for k in kinds:
+        if k is not torch.float32 and k is not torch.bfloat16:
+            raise RadError(RAD_ERR_PARAM, "gradients are fp32 or bf16")
+    n = len(grads)
+    return ((C.c_int64 * n)(*[t.numel() for t in grads]), _tensors("grads", grads, grads, kinds), kinds,
+            (C.c_int32 * n)(*[RAD_F32 if k is torch.float32 else RAD_BF16 for k in kinds]))
+
+
+def rad_gradient_norm(ctx, grads, max_norm=float("inf"), norm=None, scale=None):
+    """grads: a list of fp32 and bf16 tensors; norm and scale: fp32 tensors of one element, or None."""
+    import torch
+    counts, at, _, dtypes = _gradients(grads)
+    args = (_arg("norm", norm, 1, torch.float32), _arg("scale", scale, 1, torch.float32))
+    _on_device(ctx, *grads, norm, scale)
+    _check(ctx, lib().rad_gradient_norm(ctx, len(grads), counts, at, dtypes, max_norm, *args))
+
+
+def rad_clip_gradients(ctx, grads, max_norm, clipped=None, norm=None):
+    """clipped: a list of tensors of the gradients' sizes and types; None: the gradients themselves."""
+    import torch
+    counts, at, kinds, dtypes = _gradients(grads)
+    to = at if clipped is None else _tensors("clipped", clipped, grads, kinds)
+    arg = _arg("norm", norm, 1, torch.float32)
+    _on_device(ctx, *grads, *(clipped or ()), norm)
+    _check(ctx, lib().rad_clip_gradients(ctx, len(grads), counts, at, dtypes, max_norm, to, arg))
+
+
+def rad_optimizer_step_scaled(ctx, opt, t, dtype, params, grads, scale, m=None, v=None, master=None):
+    """As rad_optimizer_step; scale: an fp32 tensor of one element on the GPU."""
+    import torch
+    n, f32 = len(params), torch.float32
+    fp = [f32] * n
+    kinds = fp if dtype == RAD_F32 else [torch.bfloat16] * n if dtype == RAD_BF16 else [p.dtype for p in params]
+    args = ((C.c_int64 * n)(*[p.numel() for p in params]), _tensors("params", params, params, kinds), _tensors("grads", grads, params, fp),
+            _tensors("m", m, params, fp), _tensors("v", v, params, fp), _tensors("master", master, params, fp), _arg("scale", scale, 1, f32))
+    _on_device(ctx, *params, *grads, *(m or ()), *(v or ()), *(master or ()), scale)
+    _check(ctx, lib().rad_optimizer_step_scaled(ctx, C.byref(opt), int(t), dtype, n, *args))
 
 
 def make_pde_grid(n=32, steps=40960, D=0.25, dt=1.0 / 4096):

@@ -44,13 +44,14 @@ struct rad_ctx {
   std::vector<hipEvent_t> pool;
   // grow-only workspaces, a set for each of the two streams: what is enqueued on one never shares a buffer with what
   // runs beside it on the other
-  void* ws[2][18] = {};
-  size_t ws_bytes[2][18] = {};
+  void* ws[2][19] = {};
+  size_t ws_bytes[2][19] = {};
   float* loss_dev = nullptr;
 };
 
 enum { WS_BITMAP = 0, WS_DENSE = 1, WS_ROWLOSS = 2, WS_COLSUM = 3, WS_SPLITK = 4, WS_WT = 5, WS_PROJ_R = 6, WS_PROJ_T = 7,
-       WS_PROJ_TB = 8, WS_REINDEX = 9, WS_CONVG = 10, WS_RNNSYNC = 11, WS_TARGETS = 12, WS_LOGITS = 13, WS_LOGITGRAD = 14, WS_HEADDW = 15, WS_HEADW = 16, WS_HEADX = 17 };
+       WS_PROJ_TB = 8, WS_REINDEX = 9, WS_CONVG = 10, WS_RNNSYNC = 11, WS_TARGETS = 12, WS_LOGITS = 13, WS_LOGITGRAD = 14, WS_HEADDW = 15, WS_HEADW = 16, WS_HEADX = 17, WS_NORM = 18 };
+constexpr size_t kNormHead = 256;                        // WS_NORM: a scale, then the partial sums
 
 static const char* kNoCtx = "no context";
 
@@ -1806,11 +1807,28 @@ extern "C" rad_status rad_linear_distill(rad_ctx* c, const rad_layer* L, const v
 }
 
 // ------------------------------------------------------------------ parameter updates
-extern "C" rad_status rad_optimizer_step(rad_ctx* c, const rad_optimizer* opt, int64_t t, int32_t dtype,
-                                         int32_t n_tensors, const int64_t* counts, void* const* params,
-                                         const void* const* grads, void* const* m, void* const* v,
-                                         void* const* master) {
-  if (!c) return RAD_ERR_NULL;
+constexpr int64_t kMaxElements = (int64_t)1 << 35;       // of a call's gradients (a grid's chunks stay below 2^24)
+
+// Memory of many tensors, some of it written: whether nothing that is written meets anything else.
+struct TensorSpan { uintptr_t from, to; bool out; };
+static bool tensors_apart(std::vector<TensorSpan>* spans) {
+  std::sort(spans->begin(), spans->end(), [](const TensorSpan& a, const TensorSpan& b) { return a.from < b.from; });
+  uintptr_t end = 0, out_end = 0;                        // of the spans so far, and of what is written among them
+  for (const TensorSpan& s : *spans) {
+    if (s.from < (s.out ? end : out_end)) return false;
+    end = std::max(end, s.to);
+    if (s.out) out_end = std::max(out_end, s.to);
+  }
+  return true;
+}
+static void add_span(std::vector<TensorSpan>* spans, const void* p, int64_t n, int size, bool out) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  if (p && n > 0) spans->push_back({at, at + (uintptr_t)n * size, out});
+}
+
+static rad_status optimizer_step(rad_ctx* c, const rad_optimizer* opt, int64_t t, int32_t dtype, int32_t n_tensors,
+                                 const int64_t* counts, void* const* params, const void* const* grads, void* const* m,
+                                 void* const* v, void* const* master, const float* scale) {
   if (!opt || !counts || !params || !grads) return fail(c, RAD_ERR_NULL, "null argument");
   if (opt->kind != RAD_SGD && opt->kind != RAD_ADAM) return fail(c, RAD_ERR_PARAM, "unknown optimiser kind");
   if (dtype != RAD_F32 && dtype != RAD_BF16) return fail(c, RAD_ERR_PARAM, "unknown dtype");
@@ -1826,24 +1844,158 @@ extern "C" rad_status rad_optimizer_step(rad_ctx* c, const rad_optimizer* opt, i
   if (dtype == RAD_BF16 && !master) return fail(c, RAD_ERR_NULL, "bf16 parameters need fp32 master copies");
   for (int i = 0; i < n_tensors; ++i) {
     if (counts[i] < 0) return fail(c, RAD_ERR_SHAPE, "negative element count");
+    if (counts[i] > kMaxElements) return fail(c, RAD_ERR_SHAPE, "more than 2^35 elements");
     if (counts[i] == 0) continue;
     if (!params[i] || !grads[i] || (adam && (!m[i] || !v[i])) || (dtype == RAD_BF16 && !master[i]))
       return fail(c, RAD_ERR_NULL, "null tensor pointer");
   }
-  OptimArgs a;
+  DeviceGuard guard(c->device);
+  OptimList l;
+  OptimArgs& a = l.a;
   a.lr = (float)opt->lr; a.l2 = (float)opt->l2;
   a.beta1 = adam ? (float)opt->beta1 : 0.f; a.beta2 = adam ? (float)opt->beta2 : 0.f; a.eps = adam ? (float)opt->eps : 0.f;
   a.omb1 = adam ? (float)(1.0 - opt->beta1) : 0.f; a.omb2 = adam ? (float)(1.0 - opt->beta2) : 0.f;
   a.inv_bc1 = adam ? (float)(1.0 / (1.0 - std::pow(opt->beta1, (double)t))) : 1.f;
   a.inv_bc2 = adam ? (float)(1.0 / (1.0 - std::pow(opt->beta2, (double)t))) : 1.f;
+  l.scale = scale;
+  l.n = 0;
+  // Tensors that share memory are stepped one after the other, as they are listed; others side by side.
+  std::vector<TensorSpan> spans;
+  spans.reserve((size_t)n_tensors * 5);
+  for (int i = 0; i < n_tensors; ++i) {
+    add_span(&spans, grads[i], counts[i], 4, false);
+    add_span(&spans, dtype == RAD_BF16 ? master[i] : params[i], counts[i], 4, true);
+    if (dtype == RAD_BF16) add_span(&spans, params[i], counts[i], 2, true);
+    if (adam) { add_span(&spans, m[i], counts[i], 4, true); add_span(&spans, v[i], counts[i], 4, true); }
+  }
+  const int together = tensors_apart(&spans) ? kStepTensors : 1;
+  int64_t elements = 0;                                  // of the tensors that wait for their launch
+  auto launch = [&]() -> rad_status {
+    if (l.n == 0) return RAD_OK;
+    HIP_TRY(c, timed(c, adam ? "optim_adam" : "optim_sgd", [&](const char**) { return launch_optim(adam, &l, c->stream); }));
+    l.n = 0; elements = 0;
+    return RAD_OK;
+  };
   for (int i = 0; i < n_tensors; ++i) {
     if (counts[i] == 0) continue;
-    float* w = static_cast<float*>(dtype == RAD_BF16 ? master[i] : params[i]);
-    uint16_t* lo = dtype == RAD_BF16 ? static_cast<uint16_t*>(params[i]) : nullptr;
-    HIP_TRY(c, timed(c, adam ? "optim_adam" : "optim_sgd", [&](const char**) {
-      return launch_optim(adam, w, lo, static_cast<const float*>(grads[i]), adam ? static_cast<float*>(m[i]) : nullptr,
-                          adam ? static_cast<float*>(v[i]) : nullptr, counts[i], a, c->stream);
-    }));
+    if (l.n >= together || elements + counts[i] > kMaxElements) RAD_TRY(launch());
+    l.w[l.n] = static_cast<float*>(dtype == RAD_BF16 ? master[i] : params[i]);
+    l.lo[l.n] = dtype == RAD_BF16 ? static_cast<uint16_t*>(params[i]) : nullptr;
+    l.g[l.n] = static_cast<const float*>(grads[i]);
+    l.m[l.n] = adam ? static_cast<float*>(m[i]) : nullptr;
+    l.v[l.n] = adam ? static_cast<float*>(v[i]) : nullptr;
+    l.count[l.n++] = counts[i];
+    elements += counts[i];
+  }
+  return launch();
+}
+
+extern "C" rad_status rad_optimizer_step(rad_ctx* c, const rad_optimizer* opt, int64_t t, int32_t dtype,
+                                         int32_t n_tensors, const int64_t* counts, void* const* params,
+                                         const void* const* grads, void* const* m, void* const* v,
+                                         void* const* master) {
+  if (!c) return RAD_ERR_NULL;
+  return optimizer_step(c, opt, t, dtype, n_tensors, counts, params, grads, m, v, master, nullptr);
+}
+
+extern "C" rad_status rad_optimizer_step_scaled(rad_ctx* c, const rad_optimizer* opt, int64_t t, int32_t dtype,
+                                                int32_t n_tensors, const int64_t* counts, void* const* params,
+                                                const void* const* grads, void* const* m, void* const* v,
+                                                void* const* master, const float* scale) {
+  if (!c) return RAD_ERR_NULL;
+  if (!scale) return fail(c, RAD_ERR_NULL, "null argument");
+  return optimizer_step(c, opt, t, dtype, n_tensors, counts, params, grads, m, v, master, scale);
+}
+
+static rad_status check_gradients(rad_ctx* c, int32_t n_tensors, const int64_t* counts, const void* const* grads, const int32_t* dtypes,
+                                  double max_norm) {
+  if (n_tensors < 0) return fail(c, RAD_ERR_SHAPE, "negative tensor count");
+  if (n_tensors > 0 && (!counts || !grads)) return fail(c, RAD_ERR_NULL, "null argument");
+  if (!(max_norm > 0.0)) return fail(c, RAD_ERR_PARAM, "max_norm must be positive");
+  int64_t elements = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    if (counts[i] < 0) return fail(c, RAD_ERR_SHAPE, "negative element count");
+    if (counts[i] > kMaxElements - elements) return fail(c, RAD_ERR_SHAPE, "more than 2^35 elements");
+    elements += counts[i];
+    if (dtypes && dtypes[i] != RAD_F32 && dtypes[i] != RAD_BF16) return fail(c, RAD_ERR_PARAM, "unknown dtype");
+    if (counts[i] > 0 && !grads[i]) return fail(c, RAD_ERR_NULL, "null tensor pointer");
+  }
+  return RAD_OK;
+}
+static int gradient_size(const int32_t* dtypes, int i) { return dtypes && dtypes[i] == RAD_BF16 ? 2 : 4; }
+
+static rad_status gradient_norm(rad_ctx* c, int32_t n_tensors, const int64_t* counts, const void* const* grads, const int32_t* dtypes,
+                                double max_norm, float* norm, float* scale) {
+  double* partial = nullptr;
+  RAD_TRY(ws_get(c, WS_NORM, kNormHead + ((size_t)n_tensors / kNormTensors + 1) * kNormBlocks * 8, reinterpret_cast<void**>(&partial)));
+  partial += kNormHead / 8;
+  NormList l;
+  int sums = 0;
+  auto launch = [&]() -> rad_status {
+    int more = 0;
+    l.partial = partial + sums;
+    HIP_TRY(c, timed(c, "square_sums", [&](const char**) { return launch_square_sums(&l, &more, c->stream); }));
+    sums += more;
+    return RAD_OK;
+  };
+  for (int i = 0; i < n_tensors;) {
+    std::memset(l.bf16, 0, sizeof(l.bf16));
+    for (l.n = 0; i < n_tensors && l.n < kNormTensors; ++i) {
+      if (counts[i] == 0) continue;
+      if (gradient_size(dtypes, i) == 2) l.bf16[l.n >> 5] |= 1u << (l.n & 31);
+      l.g[l.n] = grads[i];
+      l.count[l.n++] = counts[i];
+    }
+    if (l.n > 0) RAD_TRY(launch());
+  }
+  HIP_TRY(c, timed(c, "gradient_norm", [&](const char**) { return launch_norm(partial, sums, max_norm, norm, scale, c->stream); }));
+  return RAD_OK;
+}
+
+extern "C" rad_status rad_gradient_norm(rad_ctx* c, int32_t n_tensors, const int64_t* counts, const void* const* grads,
+                                        const int32_t* dtypes, double max_norm, float* norm, float* scale) {
+  if (!c) return RAD_ERR_NULL;
+  RAD_TRY(check_gradients(c, n_tensors, counts, grads, dtypes, max_norm));
+  if (!norm && !scale) return fail(c, RAD_ERR_NULL, "no output asked for");
+  std::vector<TensorSpan> spans;
+  spans.reserve((size_t)n_tensors + 2);
+  for (int i = 0; i < n_tensors; ++i) add_span(&spans, grads[i], counts[i], gradient_size(dtypes, i), false);
+  add_span(&spans, norm, 1, 4, true);
+  add_span(&spans, scale, 1, 4, true);
+  if (!tensors_apart(&spans)) return fail(c, RAD_ERR_PARAM, "an output overlaps a gradient or the other output");
+  DeviceGuard guard(c->device);
+  return gradient_norm(c, n_tensors, counts, grads, dtypes, max_norm, norm, scale);
+}
+
+extern "C" rad_status rad_clip_gradients(rad_ctx* c, int32_t n_tensors, const int64_t* counts, const void* const* grads,
+                                         const int32_t* dtypes, double max_norm, void* const* clipped, float* norm) {
+  if (!c) return RAD_ERR_NULL;
+  RAD_TRY(check_gradients(c, n_tensors, counts, grads, dtypes, max_norm));
+  if (n_tensors > 0 && !clipped) return fail(c, RAD_ERR_NULL, "null argument");
+  std::vector<TensorSpan> spans;
+  spans.reserve((size_t)n_tensors * 2 + 1);
+  for (int i = 0; i < n_tensors; ++i) {
+    if (counts[i] > 0 && !clipped[i]) return fail(c, RAD_ERR_NULL, "null tensor pointer");
+    if (clipped[i] != grads[i]) add_span(&spans, grads[i], counts[i], gradient_size(dtypes, i), false);
+    add_span(&spans, clipped[i], counts[i], gradient_size(dtypes, i), true);
+  }
+  add_span(&spans, norm, 1, 4, true);
+  if (!tensors_apart(&spans)) return fail(c, RAD_ERR_PARAM, "an output overlaps another tensor");
+  DeviceGuard guard(c->device);
+  float* scale = nullptr;
+  RAD_TRY(ws_get(c, WS_NORM, kNormHead + ((size_t)n_tensors / kNormTensors + 1) * kNormBlocks * 8, reinterpret_cast<void**>(&scale)));
+  RAD_TRY(gradient_norm(c, n_tensors, counts, grads, dtypes, max_norm, norm, scale));
+  ClipList l;
+  l.scale = scale;
+  for (int i = 0; i < n_tensors;) {
+    std::memset(l.bf16, 0, sizeof(l.bf16));
+    for (l.n = 0; i < n_tensors && l.n < kClipTensors; ++i) {
+      if (counts[i] == 0) continue;
+      if (gradient_size(dtypes, i) == 2) l.bf16[l.n >> 5] |= 1u << (l.n & 31);
+      l.g[l.n] = grads[i]; l.out[l.n] = clipped[i];
+      l.count[l.n++] = counts[i];
+    }
+    if (l.n > 0) HIP_TRY(c, timed(c, "clip", [&](const char**) { return launch_clip(&l, c->stream); }));
   }
   return RAD_OK;
 }

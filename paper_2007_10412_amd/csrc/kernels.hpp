@@ -189,13 +189,43 @@ hipError_t launch_path_sampling(int n, int n_levels, const int32_t* level_ptr_ho
                                 const int32_t* succ_ptr, const int32_t* succ, const double* partial, int y,
                                 const int32_t* inputs, int n_inputs, int k, uint32_t seed_lo, uint32_t seed_hi,
                                 uint32_t stream_id, double* adj, uint32_t* reached, int* bad, hipStream_t st);
-// One optimiser step over n parameters: w (fp32, updated in place), g (fp32 gradient), Adam moments m, v (fp32,
-// updated in place; unused for SGD), lo: bf16 copy of w to refresh, or null.  inv_bc1 / inv_bc2 are
-// 1 / (1 - beta^t) of the step number and omb1 / omb2 are 1 - beta, all formed in double by the caller (in fp32
-// 1 - 0.9f is off by 2e-7 of its value).
+// One optimiser step over the parameters of up to kStepTensors tensors: w (fp32, updated in place), g (fp32 gradient, times
+// *scale where that is given; a scale of zero leaves everything as it is), Adam moments m, v (fp32, updated in place; unused for
+// SGD), lo: bf16 copy of w to refresh, or null.  inv_bc1 / inv_bc2 are 1 / (1 - beta^t) of the step number and omb1 / omb2 are
+// 1 - beta, all formed in double by the caller (in fp32 1 - 0.9f is off by 2e-7 of its value).
 struct OptimArgs { float lr, l2, beta1, beta2, omb1, omb2, eps, inv_bc1, inv_bc2; };
-hipError_t launch_optim(bool adam, float* w, uint16_t* lo, const float* g, float* m, float* v, int64_t n,
-                        const OptimArgs& a, hipStream_t st);
+// (Lists of tensors go in the kernels' arguments, which a recorded graph keeps: a list in memory would have to outlive it.)
+constexpr int kStepTensors = 64, kNormTensors = 128, kClipTensors = 96;
+struct OptimList {
+  OptimArgs a;
+  const float* scale;
+  int n;
+  float* w[kStepTensors]; const float* g[kStepTensors]; float* m[kStepTensors]; float* v[kStepTensors]; uint16_t* lo[kStepTensors];
+  int64_t count[kStepTensors];
+  int32_t chunk_end[kStepTensors];      // set by the launch
+};
+hipError_t launch_optim(bool adam, OptimList* l, hipStream_t st);
+// partial[first ..]: sums of squares, in fp64, of the elements that each workgroup takes; returns how many there are in *partials
+constexpr int kNormBlocks = 1024;       // of one launch, at most
+struct NormList {
+  double* partial;
+  int n;
+  const void* g[kNormTensors]; int64_t count[kNormTensors];
+  int32_t chunk_end[kNormTensors];      // set by the launch
+  uint32_t bf16[kNormTensors / 32];     // bit i: tensor i is bf16, else fp32
+};
+hipError_t launch_square_sums(NormList* l, int* partials, hipStream_t st);
+// *norm = sqrt(sum of partials), *scale = min(1, max_norm / norm), 0 where the norm is not finite; either may be null
+hipError_t launch_norm(const double* partial, int partials, double max_norm, float* norm, float* scale, hipStream_t st);
+// out[i] = *scale g[i] (a scale of 0: g[i]); out[i] may be g[i]
+struct ClipList {
+  const float* scale;
+  int n;
+  const void* g[kClipTensors]; void* out[kClipTensors]; int64_t count[kClipTensors];
+  int32_t chunk_end[kClipTensors];      // set by the launch
+  uint32_t bf16[kClipTensors / 32];
+};
+hipError_t launch_clip(ClipList* l, hipStream_t st);
 // db[c] = sum over b, y, x of g[b,c,y,x]; partial: [C][splits] scratch (workgroup (c, s) adds examples s, s + splits, ...)
 hipError_t launch_channel_sum(const float* g, int batch, int C, int HW, float* db, float* partial, int splits,
                               hipStream_t st);

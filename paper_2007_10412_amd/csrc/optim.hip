@@ -1,7 +1,9 @@
 // Parameter updates (Section 4.3 and Appendix A, training details): plain SGD for the recurrent model, Adam for the
-// feedforward ones, each with an l2 term added to the gradient as l2 * w.  One pass over a tensor: every operand
-// is read once and every result written once, so the kernels are HBM streams (SGD 8 bytes read + 4 written per
-// fp32 parameter; Adam 16 read + 12 written, 2 more written when a bf16 copy of the parameter is kept).
+// feedforward ones, each with an l2 term added to the gradient as l2 * w; and the norm of many gradients together, by which
+// they are clipped.  One pass over a tensor: every operand is read once and every result written once, so the kernels are HBM
+// streams (SGD 8 bytes read + 4 written per fp32 parameter; Adam 16 read + 12 written, 2 more written when a bf16 copy of the
+// parameter is kept; a norm reads its gradients, and the step that follows applies the clipping factor as it reads them again).
+// A launch takes many tensors: each is cut into chunks of kChunk elements, which the workgroups take in turn.
 #include "kernels.hpp"
 
 namespace rad {
@@ -28,68 +30,224 @@ __device__ __forceinline__ float update_one(float w, float g, float& m, float& v
   }
 }
 
-// w: the fp32 parameter (or the fp32 master copy); lo: bf16 copy to refresh, or null.  VEC = 4: whole 16-byte
-// vectors of every array; VEC = 1: any alignment, and the tail of the vector form.
-template <bool ADAM, int VEC>
-__global__ __launch_bounds__(256) void optim_kernel(float* __restrict__ w, uint16_t* __restrict__ lo,
-                                                    const float* __restrict__ g, float* __restrict__ m,
-                                                    float* __restrict__ v, int64_t first, int64_t n, OptimArgs a) {
-  const int64_t i = first + ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC;
-  if (i >= n) return;
-  if constexpr (VEC == 4) {
-    auto ld = [](const float* p) { return *reinterpret_cast<const float4*>(p); };
-    auto stv = [](float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; };
-    float4 wv = ld(w + i);
-    const float4 gv = ld(g + i);
-    float4 mv = make_float4(0.f, 0.f, 0.f, 0.f), vv = mv;
-    if constexpr (ADAM) { mv = ld(m + i); vv = ld(v + i); }
-    wv.x = update_one<ADAM>(wv.x, gv.x, mv.x, vv.x, a);
-    wv.y = update_one<ADAM>(wv.y, gv.y, mv.y, vv.y, a);
-    wv.z = update_one<ADAM>(wv.z, gv.z, mv.z, vv.z, a);
-    wv.w = update_one<ADAM>(wv.w, gv.w, mv.w, vv.w, a);
-    stv(w + i, wv);
-    if constexpr (ADAM) { stv(m + i, mv); stv(v + i, vv); }
-    if (lo) {
-      uint2 p;
-      p.x = (uint32_t)to_bf16(wv.x) | ((uint32_t)to_bf16(wv.y) << 16);
-      p.y = (uint32_t)to_bf16(wv.z) | ((uint32_t)to_bf16(wv.w) << 16);
-      *reinterpret_cast<uint2*>(lo + i) = p;
+constexpr int kChunk = 4096;                            // elements: 16 KB of fp32, four 16-byte vectors a lane
+
+// the tensor that chunk c lies in
+__device__ __forceinline__ int tensor_of(const int32_t* chunk_end, int n, int c) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (c < chunk_end[mid]) hi = mid; else lo = mid + 1;
+  }
+  return lo;
+}
+
+// Chunks of tensors in whole 16-byte vectors; what is left of a tensor, or a tensor at another address, element by element.
+template <bool ADAM, bool SCALED>
+__global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
+  float scale = 1.f;
+  if constexpr (SCALED) {
+    scale = *l.scale;
+    if (scale == 0.f) return;
+  }
+  const int t = tensor_of(l.chunk_end, l.n, blockIdx.x), c = (int)blockIdx.x - (t ? l.chunk_end[t - 1] : 0);
+  float* const w = l.w[t]; float* const m = l.m[t]; float* const v = l.v[t];
+  const float* const g = l.g[t];
+  uint16_t* const lo = l.lo[t];
+  const int64_t i0 = (int64_t)c * kChunk, n = l.count[t];
+  const uintptr_t align = reinterpret_cast<uintptr_t>(w) | reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(m) |
+                          reinterpret_cast<uintptr_t>(v) | (reinterpret_cast<uintptr_t>(lo) << 1);   // (8-byte vectors of the bf16 copy)
+  const OptimArgs& a = l.a;
+  auto grad = [&](float x) {                            // (rounded, as if the scaled gradient had been stored)
+#pragma clang fp contract(off)
+    if constexpr (SCALED) return x * scale; else return x;
+  };
+  auto ld = [](const float* p) { return *reinterpret_cast<const floatx4*>(p); };
+#pragma unroll
+  for (int q = 0; q < kChunk / 1024; ++q) {
+    const int64_t i = i0 + q * 1024 + (int)threadIdx.x * 4;
+    if (i >= n) return;
+    if (i + 4 <= n && (align & 15) == 0) {
+      floatx4 wv = ld(w + i), gv = ld(g + i), mv = {0.f, 0.f, 0.f, 0.f}, vv = mv;
+      if constexpr (ADAM) { mv = ld(m + i); vv = ld(v + i); }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float me = mv[e], ve = vv[e];
+        wv[e] = update_one<ADAM>(wv[e], grad(gv[e]), me, ve, a);
+        mv[e] = me; vv[e] = ve;
+      }
+      *reinterpret_cast<floatx4*>(w + i) = wv;
+      if constexpr (ADAM) { *reinterpret_cast<floatx4*>(m + i) = mv; *reinterpret_cast<floatx4*>(v + i) = vv; }
+      if (lo) {
+        const u32x2 p = {(uint32_t)to_bf16(wv[0]) | ((uint32_t)to_bf16(wv[1]) << 16), (uint32_t)to_bf16(wv[2]) | ((uint32_t)to_bf16(wv[3]) << 16)};
+        *reinterpret_cast<u32x2*>(lo + i) = p;
+      }
+      continue;
     }
-  } else {
-    float mm = 0.f, vv = 0.f;
-    if constexpr (ADAM) { mm = m[i]; vv = v[i]; }
-    const float wn = update_one<ADAM>(w[i], g[i], mm, vv, a);
-    w[i] = wn;
-    if constexpr (ADAM) { m[i] = mm; v[i] = vv; }
-    if (lo) lo[i] = to_bf16(wn);
+    for (int64_t j = i; j < n && j < i + 4; ++j) {
+      float mm = 0.f, vv = 0.f;
+      if constexpr (ADAM) { mm = m[j]; vv = v[j]; }
+      const float wn = update_one<ADAM>(w[j], grad(g[j]), mm, vv, a);
+      w[j] = wn;
+      if constexpr (ADAM) { m[j] = mm; v[j] = vv; }
+      if (lo) lo[j] = to_bf16(wn);
+    }
   }
 }
 
-template <bool ADAM>
-hipError_t run(float* w, uint16_t* lo, const float* g, float* m, float* v, int64_t n, const OptimArgs& a,
-               hipStream_t st) {
-  const uintptr_t align = reinterpret_cast<uintptr_t>(w) | reinterpret_cast<uintptr_t>(g) |
-                          reinterpret_cast<uintptr_t>(m) | reinterpret_cast<uintptr_t>(v) |
-                          (reinterpret_cast<uintptr_t>(lo) << 1);        // 8-byte vectors of the bf16 copy
-  const int64_t nv = (align & 15) ? 0 : n & ~int64_t(3);
-  if (nv) {
-    const int64_t threads = nv / 4;
-    hipLaunchKernelGGL((optim_kernel<ADAM, 4>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, w, lo, g, m,
-                       v, int64_t(0), nv, a);
+// a sum over 256 threads in a fixed order, for thread 0
+__device__ __forceinline__ double block_sum(double s, double* s_w) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = s;
+  __syncthreads();
+  double all = 0.0;
+  if (threadIdx.x == 0) for (int w = 0; w < (int)blockDim.x / 64; ++w) all += s_w[w];
+  return all;
+}
+
+// Squares and their sums are fp64: fp32's largest gradients do not overflow them, nor do its smallest vanish, and a sum of 10^9
+// squares is as good as one of ten.  Each workgroup takes chunks gridDim.x apart: the same ones in every call.
+__global__ __launch_bounds__(256) void square_sums_kernel(NormList l) {
+  __shared__ double s_w[4];
+  double sum = 0.0;
+  const int chunks = l.chunk_end[l.n - 1];
+  for (int b = blockIdx.x; b < chunks; b += gridDim.x) {
+    const int t = tensor_of(l.chunk_end, l.n, b), c = b - (t ? l.chunk_end[t - 1] : 0);
+    const int64_t i0 = (int64_t)c * kChunk, n = l.count[t];
+    const bool half = (l.bf16[t >> 5] >> (t & 31)) & 1u, aligned = (reinterpret_cast<uintptr_t>(l.g[t]) & 15) == 0;
+    if (half) {
+      const uint16_t* const g = static_cast<const uint16_t*>(l.g[t]);
+#pragma unroll
+      for (int q = 0; q < kChunk / 2048; ++q) {
+        const int64_t i = i0 + q * 2048 + (int)threadIdx.x * 8;
+        if (i + 8 <= n && aligned) {
+          const u32x4 v = *reinterpret_cast<const u32x4*>(g + i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const double x = __uint_as_float(v[e] << 16), y = __uint_as_float(v[e] & 0xFFFF0000u);
+            sum += x * x; sum += y * y;
+          }
+        } else {
+          for (int64_t j = i; j < n && j < i + 8; ++j) { const double x = bf16_bits_to_f32(g[j]); sum += x * x; }
+        }
+      }
+    } else {
+      const float* const g = static_cast<const float*>(l.g[t]);
+#pragma unroll
+      for (int q = 0; q < kChunk / 1024; ++q) {
+        const int64_t i = i0 + q * 1024 + (int)threadIdx.x * 4;
+        if (i + 4 <= n && aligned) {
+          const floatx4 v = *reinterpret_cast<const floatx4*>(g + i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { const double x = v[e]; sum += x * x; }
+        } else {
+          for (int64_t j = i; j < n && j < i + 4; ++j) { const double x = g[j]; sum += x * x; }
+        }
+      }
+    }
   }
-  if (n > nv) {
-    hipLaunchKernelGGL((optim_kernel<ADAM, 1>), dim3((unsigned)((n - nv + 255) / 256)), dim3(256), 0, st, w, lo, g, m,
-                       v, nv, n, a);
+  sum = block_sum(sum, s_w);
+  if (threadIdx.x == 0) l.partial[blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(256) void norm_kernel(const double* __restrict__ partial, int partials, double max_norm, float* norm, float* scale) {
+  __shared__ double s_w[4];
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < partials; i += 256) sum += partial[i];
+  sum = block_sum(sum, s_w);
+  if (threadIdx.x != 0) return;
+  const double r = sqrt(sum);
+  const float f = (float)r;
+  if (norm) *norm = f;
+  if (scale) *scale = !(f < INFINITY) ? 0.f : r > max_norm ? (float)(max_norm / r) : 1.f;
+}
+
+__global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
+  float f = *l.scale;
+  if (f == 0.f) f = 1.f;                                // (a norm that is not finite: the gradients as they are)
+  const int t = tensor_of(l.chunk_end, l.n, blockIdx.x), c = (int)blockIdx.x - (t ? l.chunk_end[t - 1] : 0);
+  if (f == 1.f && l.out[t] == l.g[t]) return;
+  const int64_t i0 = (int64_t)c * kChunk, n = l.count[t];
+  const bool half = (l.bf16[t >> 5] >> (t & 31)) & 1u;
+  const bool aligned = ((reinterpret_cast<uintptr_t>(l.g[t]) | reinterpret_cast<uintptr_t>(l.out[t])) & 15) == 0;
+  if (half) {
+    const uint16_t* const g = static_cast<const uint16_t*>(l.g[t]);
+    uint16_t* const o = static_cast<uint16_t*>(l.out[t]);
+#pragma unroll
+    for (int q = 0; q < kChunk / 2048; ++q) {
+      const int64_t i = i0 + q * 2048 + (int)threadIdx.x * 8;
+      if (i + 8 <= n && aligned) {
+        u32x4 v = *reinterpret_cast<const u32x4*>(g + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[e] = (uint32_t)to_bf16(__uint_as_float(v[e] << 16) * f) | ((uint32_t)to_bf16(__uint_as_float(v[e] & 0xFFFF0000u) * f) << 16);
+        *reinterpret_cast<u32x4*>(o + i) = v;
+      } else {
+        for (int64_t j = i; j < n && j < i + 8; ++j) o[j] = to_bf16(bf16_bits_to_f32(g[j]) * f);
+      }
+    }
+    return;
   }
-  return hipGetLastError();
+  const float* const g = static_cast<const float*>(l.g[t]);
+  float* const o = static_cast<float*>(l.out[t]);
+#pragma unroll
+  for (int q = 0; q < kChunk / 1024; ++q) {
+    const int64_t i = i0 + q * 1024 + (int)threadIdx.x * 4;
+    if (i + 4 <= n && aligned) {
+      floatx4 v = *reinterpret_cast<const floatx4*>(g + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] *= f;
+      *reinterpret_cast<floatx4*>(o + i) = v;
+    } else {
+      for (int64_t j = i; j < n && j < i + 4; ++j) o[j] = g[j] * f;
+    }
+  }
+}
+
+// fills chunk_end; their number, or -1 where a grid cannot have so many
+int64_t count_chunks(int n, const int64_t* count, int32_t* chunk_end) {
+  int64_t chunks = 0;
+  for (int i = 0; i < n; ++i) {
+    chunks += (count[i] + kChunk - 1) / kChunk;
+    if (chunks >= (int64_t(1) << 24)) return -1;        // (a grid of 256 threads a workgroup: 2^32 at most)
+    chunk_end[i] = (int32_t)chunks;
+  }
+  return chunks;
 }
 
 }  // namespace
 
-hipError_t launch_optim(bool adam, float* w, uint16_t* lo, const float* g, float* m, float* v, int64_t n,
-                        const OptimArgs& a, hipStream_t st) {
-  if (n <= 0) return hipSuccess;
-  return adam ? run<true>(w, lo, g, m, v, n, a, st) : run<false>(w, lo, g, m, v, n, a, st);
+hipError_t launch_optim(bool adam, OptimList* l, hipStream_t st) {
+  const int64_t chunks = count_chunks(l->n, l->count, l->chunk_end);
+  if (chunks < 0) return hipErrorInvalidValue;
+  if (chunks == 0) return hipSuccess;
+  auto kern = adam ? l->scale ? optim_kernel<true, true> : optim_kernel<true, false> : l->scale ? optim_kernel<false, true> : optim_kernel<false, false>;
+  hipLaunchKernelGGL(kern, dim3((unsigned)chunks), dim3(256), 0, st, *l);
+  return hipGetLastError();
+}
+
+hipError_t launch_square_sums(NormList* l, int* partials, hipStream_t st) {
+  const int64_t chunks = count_chunks(l->n, l->count, l->chunk_end);
+  *partials = 0;
+  if (chunks < 0) return hipErrorInvalidValue;
+  if (chunks == 0) return hipSuccess;
+  *partials = chunks < kNormBlocks ? (int)chunks : kNormBlocks;
+  hipLaunchKernelGGL(square_sums_kernel, dim3(*partials), dim3(256), 0, st, *l);
+  return hipGetLastError();
+}
+
+hipError_t launch_norm(const double* partial, int partials, double max_norm, float* norm, float* scale, hipStream_t st) {
+  hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(256), 0, st, partial, partials, max_norm, norm, scale);
+  return hipGetLastError();
+}
+
+hipError_t launch_clip(ClipList* l, hipStream_t st) {
+  const int64_t chunks = count_chunks(l->n, l->count, l->chunk_end);
+  if (chunks < 0) return hipErrorInvalidValue;
+  if (chunks == 0) return hipSuccess;
+  hipLaunchKernelGGL(clip_kernel, dim3((unsigned)chunks), dim3(256), 0, st, *l);
+  return hipGetLastError();
 }
 
 }  // namespace rad
