@@ -355,6 +355,69 @@ rad_status rad_linear_distill(rad_ctx* ctx, const rad_layer* layer, const void* 
                               const rad_teacher* teacher, const float* row_weight, float* row_loss, float* loss,
                               void* dX, void* dW, int32_t dw_dtype, float* dbias, float beta);
 
+/* ---- log probabilities of given classes, entropies, the likeliest classes ----
+ * For scoring a model's answers, for an objective that depends on their log
+ * probabilities, for the lists of a teacher.  With q = softmax(z / T) of a row's
+ * logits z:
+ *   logprob[r] = log q[token[r]],   entropy[r] = - sum_v q_v log q_v,
+ *   top_index[r], top_logprob[r]: the top_k classes of the largest logits, best
+ *   first (of equal logits the lowest class first), and their log q.
+ * Logits of -infinity and NaN are not listed; places that are left have index -1
+ * and log probability -infinity, which rad_teacher leaves out: with T = 1
+ * top_index and top_logprob are a teacher's lists.  A row whose token lies
+ * outside [0, classes) does not count: zeros, and an empty list.  token null:
+ * every row counts.  A row that holds a NaN or +infinity, or -infinity alone, has
+ * NaN for its log probabilities and entropy. */
+typedef struct {
+  double temperature;   /* T, 1e-6 to 1e6 */
+  const int32_t* token; /* DEVICE [rows], or null (then logprob is null too) */
+  float* logprob;       /* DEVICE [rows], or null */
+  float* entropy;       /* DEVICE [rows], or null */
+  int32_t top_k;        /* 0 to 256 */
+  int32_t* top_index;   /* DEVICE [rows, top_k] */
+  float* top_logprob;   /* DEVICE [rows, top_k] */
+} rad_logprobs;
+
+/* Of logits [rows, classes] in dtype that are there.  Statistics are fp32; a log
+ * probability is off by some 10^-7 (|z| / T + log(classes)).  Outputs overlap
+ * neither inputs nor each other; results do not vary from call to call.  Context
+ * workspace where rows are few or wider than a workgroup's registers (131072
+ * elements of bf16, 65536 of fp32): 12 + 8 top_k bytes per row and 8192 (4096)
+ * classes.  Enqueued on the context's stream. */
+rad_status rad_token_logprobs(rad_ctx* ctx, const void* logits, int64_t rows, int64_t classes, int32_t dtype,
+                              const rad_logprobs* out);
+
+/* The logits' gradient from those of log probabilities and entropies (DEVICE
+ * [rows], either may be null: zeros; d_logprob needs token):
+ *   dlogits[r][v] = (1/T) (a (1[v = token[r]] - q_v) - h q_v (log q_v + entropy[r])),
+ * a = d_logprob[r], h = d_entropy[r]; zeros in a row that does not count, whatever
+ * its a and h.  Everything is formed from the logits again; dlogits, in dtype, may
+ * be logits.  Context workspace as above, with top_k = 0. */
+rad_status rad_token_logprobs_grad(rad_ctx* ctx, const void* logits, int64_t rows, int64_t classes, int32_t dtype,
+                                   const int32_t* token, double temperature, const float* d_logprob,
+                                   const float* d_entropy, void* dlogits);
+
+/* rad_token_logprobs of the logits z = x W + bias of a linear layer (RAD_LINEAR,
+ * no ReLU), which are formed in fp32 and not kept.  Rows go through in pieces, of
+ * which the logits (fp32, where top_k > 0) and the rows of x have at most 2 GiB
+ * each, or of 256 rows if those are more.  Context workspaces: the logits of a
+ * piece where top_k > 0; copies of W and of a piece of x as for rad_linear_ce; 12
+ * bytes per row and 64 classes of a piece, 8 per row of it; partial sums where the
+ * product has few tiles.  Limits of the layer as for rad_linear_ce. */
+rad_status rad_linear_logprobs(rad_ctx* ctx, const rad_layer* layer, const void* x, const void* W, const float* bias,
+                               const rad_logprobs* out);
+
+/* The layer's gradients from those of log probabilities and entropies, with dz the
+ * dlogits of rad_token_logprobs_grad:
+ *   dX = dz W^T,  dW = beta dW + x^T dz,  dbias = beta dbias + sum_r dz[r].
+ * The logits are formed again; dz is rounded to the layer's type.  Types, beta,
+ * which outputs may be null, overlaps, limits, pieces and workspaces are as for
+ * rad_linear_ce with the gradients in the place of row weights, and 4 bytes per
+ * row and 64 classes of a piece and 4 per row of it besides. */
+rad_status rad_linear_logprobs_grad(rad_ctx* ctx, const rad_layer* layer, const void* x, const void* W, const float* bias,
+                                    const int32_t* token, double temperature, const float* d_logprob, const float* d_entropy,
+                                    void* dX, void* dW, int32_t dw_dtype, float* dbias, float beta);
+
 /* ---- whole training steps ------------------------------------------------
  * A model owns its stores and transient activation buffers; parameters and
  * gradients stay with the caller.  `params` / `grads` are HOST arrays of

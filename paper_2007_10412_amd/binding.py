@@ -58,6 +58,11 @@ class rad_teacher(C.Structure):
     _fields_ = [("k", C.c_int32), ("temperature", C.c_double), ("index", P), ("logit", P)]
 
 
+class rad_logprobs(C.Structure):
+    _fields_ = [("temperature", C.c_double), ("token", P), ("logprob", P), ("entropy", P), ("top_k", C.c_int32),
+                ("top_index", P), ("top_logprob", P)]
+
+
 _HEAD = [P, P, P, P, P, C.c_int32, P, C.c_float]     # row_weight, row_loss, loss, dX, dW, dw_dtype, dbias, beta
 SIGNATURES = {
     "rad_fixed_k": (C.c_int64, [C.c_double, C.c_int64]),
@@ -89,6 +94,10 @@ SIGNATURES = {
     "rad_distill_ce": (C.c_int, [P, P, C.POINTER(rad_teacher), P, C.c_int64, C.c_int64, C.c_int32, P, P, P]),
     "rad_linear_ce": (C.c_int, [P, C.POINTER(rad_layer), P, P, P, P] + _HEAD),
     "rad_linear_distill": (C.c_int, [P, C.POINTER(rad_layer), P, P, P, C.POINTER(rad_teacher)] + _HEAD),
+    "rad_token_logprobs": (C.c_int, [P, P, C.c_int64, C.c_int64, C.c_int32, C.POINTER(rad_logprobs)]),
+    "rad_token_logprobs_grad": (C.c_int, [P, P, C.c_int64, C.c_int64, C.c_int32, P, C.c_double, P, P, P]),
+    "rad_linear_logprobs": (C.c_int, [P, C.POINTER(rad_layer), P, P, P, C.POINTER(rad_logprobs)]),
+    "rad_linear_logprobs_grad": (C.c_int, [P, C.POINTER(rad_layer), P, P, P, P, C.c_double, P, P, P, P, C.c_int32, P, C.c_float]),
     "rad_model_create_mlp": (C.c_int, [P, C.c_int32, C.c_int64, C.c_int32, C.POINTER(C.c_int64), C.c_int32,
                                        C.c_int32, C.c_double, C.POINTER(P)]),
     "rad_model_create_rnn": (C.c_int, [P, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32,
@@ -358,6 +367,67 @@ def rad_distill_ce(ctx, logits, teacher, dtype, dlogits=None, row_weight=None, r
             _arg("dlogits", dlogits, n, kind), _arg("row_loss", row_loss, rows, f32), _arg("loss", loss, 1, f32))
     _on_device(ctx, logits, *teacher.lists, row_weight, dlogits, row_loss, loss)
     _check(ctx, lib().rad_distill_ce(ctx, *args))
+
+
+def _logprobs(rows, tokens, temperature, logprob, entropy, top_index, top_logprob):
+    import torch
+    f32, i32 = torch.float32, torch.int32
+    if (top_index is None) != (top_logprob is None):
+        raise RadError(RAD_ERR_NULL, "a list needs both of its arrays")
+    k = 0
+    if top_index is not None:
+        if top_index.dim() != 2 or top_index.shape[0] != rows or top_index.shape != top_logprob.shape:
+            raise RadError(RAD_ERR_SHAPE, "lists are tensors [rows, k] of one shape")
+        k = int(top_index.shape[1])
+    return rad_logprobs(temperature, _arg("tokens", tokens, rows, i32), _arg("logprob", logprob, rows, f32), _arg("entropy", entropy, rows, f32),
+                        k, _arg("top_index", top_index, rows * k, i32), _arg("top_logprob", top_logprob, rows * k, f32))
+
+
+def rad_token_logprobs(ctx, logits, dtype, tokens=None, temperature=1.0, logprob=None, entropy=None, top_index=None, top_logprob=None):
+    """tokens: int32 [rows]; top_index (int32) and top_logprob: [rows, k]."""
+    rows, classes = logits.shape
+    out = _logprobs(rows, tokens, temperature, logprob, entropy, top_index, top_logprob)
+    at = _arg("logits", logits, rows * classes, _kind(logits, dtype))
+    _on_device(ctx, logits, tokens, logprob, entropy, top_index, top_logprob)
+    _check(ctx, lib().rad_token_logprobs(ctx, at, rows, classes, dtype, out))
+
+
+def rad_token_logprobs_grad(ctx, logits, dtype, dlogits, tokens=None, temperature=1.0, d_logprob=None, d_entropy=None):
+    import torch
+    rows, classes = logits.shape
+    n, kind, f32 = rows * classes, _kind(logits, dtype), torch.float32
+    args = (_arg("logits", logits, n, kind), rows, classes, dtype, _arg("tokens", tokens, rows, torch.int32), temperature,
+            _arg("d_logprob", d_logprob, rows, f32), _arg("d_entropy", d_entropy, rows, f32), _arg("dlogits", dlogits, n, kind))
+    _on_device(ctx, logits, tokens, d_logprob, d_entropy, dlogits)
+    _check(ctx, lib().rad_token_logprobs_grad(ctx, *args))
+
+
+def rad_linear_logprobs(ctx, layer, x, W, bias, tokens=None, temperature=1.0, logprob=None, entropy=None, top_index=None, top_logprob=None):
+    import torch
+    n, d, v = layer.batch, layer.d_in, layer.d_out
+    out = _logprobs(n, tokens, temperature, logprob, entropy, top_index, top_logprob)
+    td = torch.float32 if x is None else _kind(x, layer.dtype)
+    args = (_arg("x", x, n * d, td), _arg("W", W, d * v, td), _arg("bias", bias, v, torch.float32))
+    _on_device(ctx, x, W, bias, tokens, logprob, entropy, top_index, top_logprob)
+    _check(ctx, lib().rad_linear_logprobs(ctx, layer, *args, out))
+
+
+def rad_linear_logprobs_grad(ctx, layer, x, W, bias, tokens=None, temperature=1.0, d_logprob=None, d_entropy=None, dX=None, dW=None,
+                             dbias=None, beta=0.0):
+    """dW: an fp32 tensor, or one of the layer's type."""
+    import torch
+    n, d, v, f32 = layer.batch, layer.d_in, layer.d_out, torch.float32
+    td = f32 if x is None else _kind(x, layer.dtype)
+    dw_kind = RAD_F32
+    if dW is not None and dW.dtype is not f32:
+        dw_kind = RAD_BF16
+        if dW.dtype is not torch.bfloat16:
+            raise RadError(RAD_ERR_PARAM, "dW is fp32 or of the layer's type")
+    args = (_arg("x", x, n * d, td), _arg("W", W, d * v, td), _arg("bias", bias, v, f32), _arg("tokens", tokens, n, torch.int32), temperature,
+            _arg("d_logprob", d_logprob, n, f32), _arg("d_entropy", d_entropy, n, f32), _arg("dX", dX, n * d, td),
+            None if dW is None else _arg("dW", dW, d * v, dW.dtype), dw_kind, _arg("dbias", dbias, v, f32), beta)
+    _on_device(ctx, x, W, bias, tokens, d_logprob, d_entropy, dX, dW, dbias)
+    _check(ctx, lib().rad_linear_logprobs_grad(ctx, layer, *args))
 
 
 def _head_call(call, ctx, layer, x, W, bias, targets, lists, row_weight, row_loss, loss, dX, dW, dbias, beta):

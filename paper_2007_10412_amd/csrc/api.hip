@@ -1464,11 +1464,11 @@ static rad_status vocab_targets(rad_ctx* c, const int32_t* labels, const rad_tea
   int32_t* const counts = reinterpret_cast<int32_t*>(entropy + rows);
   int32_t* const index = counts + rows;
   float* const prob = reinterpret_cast<float*>(index + lists);
-  *t = VocabTargets{labels, nullptr, nullptr, nullptr, nullptr, 1, 1.f, weight, inv_count};
+  *t = VocabTargets{labels, nullptr, nullptr, nullptr, nullptr, 1, 1.f, weight, inv_count, 1.f, nullptr};
   if (!*row_loss) *row_loss = losses;
   if (teacher) {
     t->index = index; t->prob = prob; t->entropy = entropy; t->counts = counts;
-    t->k = teacher->k; t->temperature = (float)teacher->temperature;
+    t->k = teacher->k; t->temperature = t->lead = (float)teacher->temperature;
     HIP_TRY(c, timed(c, "teacher", [&](const char**) {
       return launch_teacher(teacher->index, teacher->logit, rows, teacher->k, classes, t->temperature, index, prob, entropy, counts, first,
                             part, parts, c->stream);
@@ -1611,27 +1611,36 @@ static bool few_classes_pay(int dtype, int64_t rows, int64_t d_in, int64_t d_out
   return d_out <= kFewClasses && 9 * rows + 4 * d_in <= (dtype == kF32 ? 16000 : 9000);
 }
 
-static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* labels, const rad_teacher* teacher,
-                            const float* row_weight, const HeadCall& h) {
+// What a call that takes gradients of log probabilities and entropies has in the place of targets and weights.
+struct LogprobGrads { double temperature; const float* d_logprob; const float* d_entropy; };
+
+static rad_status check_head(rad_ctx* c, const rad_layer* L, const void* x, const void* W, const float* bias) {
   RAD_TRY(check_layer(c, L));
   if (L->kind != RAD_LINEAR || L->relu) return fail(c, RAD_ERR_PARAM, "the loss takes a linear layer without ReLU");
-  if (!h.x || !h.W) return fail(c, RAD_ERR_NULL, "null argument");
-  if (!L->has_bias != !h.bias) return fail(c, RAD_ERR_NULL, "bias must be given iff the layer has one");
+  if (!x || !W) return fail(c, RAD_ERR_NULL, "null argument");
+  if (!L->has_bias != !bias) return fail(c, RAD_ERR_NULL, "bias must be given iff the layer has one");
+  if (L->d_in * L->d_out >= ((int64_t)1 << 32)) return fail(c, RAD_ERR_SHAPE, "weights of 2^32 elements or more");
+  if (std::max(L->d_in, L->d_out) > ((int64_t)1 << 22) - 64) return fail(c, RAD_ERR_SHAPE, "d_in or d_out above 2^22 - 64");
+  return RAD_OK;
+}
+
+static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* labels, const rad_teacher* teacher,
+                            const float* row_weight, const HeadCall& h, const LogprobGrads* lp = nullptr) {
+  RAD_TRY(check_head(c, L, h.x, h.W, h.bias));
   if (!h.row_loss && !h.loss && !h.dX && !h.dW && !h.dbias) return fail(c, RAD_ERR_NULL, "no output asked for");
   if (h.beta != 0.f && h.beta != 1.f) return fail(c, RAD_ERR_PARAM, "beta must be 0 or 1");
   if (h.dW && h.dw_dtype != RAD_F32 && h.dw_dtype != L->dtype) return fail(c, RAD_ERR_PARAM, "dW is fp32 or of the layer's type");
-  if (L->d_in * L->d_out >= ((int64_t)1 << 32)) return fail(c, RAD_ERR_SHAPE, "weights of 2^32 elements or more");
-  if (std::max(L->d_in, L->d_out) > ((int64_t)1 << 22) - 64) return fail(c, RAD_ERR_SHAPE, "d_in or d_out above 2^22 - 64");
   const size_t esize = L->dtype == RAD_F32 ? 4 : 2, xs_n = (size_t)L->batch * L->d_in, ws_n = (size_t)L->d_in * L->d_out;
   const size_t lists = teacher ? (size_t)L->batch * teacher->k * 4 : 0;
   RAD_TRY(check_apart(c, {{h.dX, xs_n * esize}, {h.dW, ws_n * (h.dw_dtype == RAD_F32 ? 4 : 2)}, {h.dbias, (size_t)L->d_out * 4},
                           {h.row_loss, (size_t)L->batch * 4}, {h.loss, 4}},
                       {{h.x, xs_n * esize}, {h.W, ws_n * esize}, {h.bias, (size_t)L->d_out * 4}, {labels, (size_t)L->batch * 4},
                        {teacher ? teacher->index : nullptr, lists}, {teacher ? teacher->logit : nullptr, lists},
-                       {row_weight, (size_t)L->batch * 4}}));
+                       {row_weight, (size_t)L->batch * 4}, {lp ? lp->d_logprob : nullptr, (size_t)L->batch * 4},
+                       {lp ? lp->d_entropy : nullptr, (size_t)L->batch * 4}}));
   DeviceGuard guard(c->device);
   const int rows = (int)L->batch, d_in = (int)L->d_in, d_out = (int)L->d_out, dtype = L->dtype;
-  if (few_classes_pay(dtype, rows, d_in, d_out)) {
+  if (!lp && few_classes_pay(dtype, rows, d_in, d_out)) {
     FewClasses f;
     std::memset(&f, 0, sizeof(f));
     f.dtype = dtype; f.rows = rows; f.d_in = d_in; f.classes = d_out;
@@ -1664,7 +1673,8 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   const int first_ld = parts + 1, list_k = teacher ? teacher->k : 1;
   const size_t first_bytes = teacher ? ((size_t)rows * first_ld * 2 + 255) / 256 * 256 : 0;
   char* ws = nullptr;
-  RAD_TRY(ws_get(c, WS_ROWLOSS, 256 + first_bytes + (size_t)piece * (8 * (size_t)parts + 12 + 4 * (size_t)list_k), reinterpret_cast<void**>(&ws)));
+  RAD_TRY(ws_get(c, WS_ROWLOSS, 256 + first_bytes + (size_t)piece * ((lp ? 12 : 8) * (size_t)parts + (lp ? 16 : 12) + 4 * (size_t)list_k),
+                 reinterpret_cast<void**>(&ws)));
   int32_t* const live = reinterpret_cast<int32_t*>(ws);
   float* const common = reinterpret_cast<float*>(ws) + 1;
   uint16_t* const first = reinterpret_cast<uint16_t*>(ws + 256);
@@ -1673,9 +1683,16 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   float* const top = reinterpret_cast<float*>(list + piece);
   float* const factor = top + piece;
   float* const target = factor + piece;
+  float* const slope = lp ? target + piece : nullptr;
+  float* const spread = lp ? slope + piece : nullptr;
   VocabTargets t;
   float* losses = h.row_loss;
-  RAD_TRY(vocab_targets(c, labels, teacher, row_weight, rows, d_out, !one, &t, &losses, first, part, parts));
+  if (lp) {
+    const float T = (float)lp->temperature;
+    t = VocabTargets{labels, nullptr, nullptr, nullptr, nullptr, 1, T, lp->d_logprob, nullptr, 1.f / T, lp->d_entropy};
+  } else {
+    RAD_TRY(vocab_targets(c, labels, teacher, row_weight, rows, d_out, !one, &t, &losses, first, part, parts));
+  }
 
   const bool cast = h.dW && h.dw_dtype == kBF16 && (!one || h.beta != 0.f);     // sums of several pieces are kept in fp32
   // (so is one to be added to a bf16 dW: 512 x 4096 x 32000 887 us; 1084 with it added in the product's epilogue, two bytes a lane)
@@ -1692,9 +1709,10 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     RAD_TRY(head_padded(c, WS_HEADX, dtype, static_cast<const char*>(h.x) + r0 * d_in * esz, n, d_in, dp, &x));
     VocabTargets tp = t;
     if (tp.labels) tp.labels += r0;
-    else { tp.index += r0 * t.k; tp.prob += r0 * t.k; tp.entropy += r0; tp.counts += r0; }
+    else if (!lp) { tp.index += r0 * t.k; tp.prob += r0 * t.k; tp.entropy += r0; tp.counts += r0; }
     if (tp.weight) tp.weight += r0;
-    float* const inv_count = one && !row_weight ? const_cast<float*>(t.inv_count) : nullptr;
+    if (tp.weight2) tp.weight2 += r0;
+    float* const inv_count = one && !row_weight && !lp ? const_cast<float*>(t.inv_count) : nullptr;
     const int64_t fwd_tiles = (int64_t)((n + fwd.tile - 1) / fwd.tile) * ((d_out + 127) / 128) * fwd.splits;
     // A launch for the list costs 5 us; lists made in the tiles cost each of them 1 or 2, which two bf16 tiles on a CU hide where
     // rows are few.  us with / without a launch: bf16 4096 x 4096 x 1000 (256 tiles) 152 / 151, 2000 x 512 x 5000 (640) 85 / 87,
@@ -1710,10 +1728,11 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     HeadArgs& a = g.head;
     a.live = live; a.row_map = list; a.rows = n; a.n_load = (int)vp8;
     if (own_list) { a.counts = tp.counts; a.list_out = list; a.live_out = live; a.inv_count_out = inv_count; a.common_out = common; }
-    a.weight = tp.weight; a.inv_count = t.inv_count; a.temperature = t.temperature;
+    a.weight = tp.weight; a.weight2 = tp.weight2; a.inv_count = t.inv_count; a.lead = t.lead;
+    a.spread = spread;
     a.c = 1.44269504088896340736f / t.temperature;
     a.stats = stats; a.stats_ld = piece;
-    a.labels = tp.labels; a.index = tp.index; a.first = t.labels ? nullptr : first + r0 * first_ld; a.k = t.k; a.first_ld = first_ld;
+    a.labels = tp.labels; a.index = tp.index; a.first = teacher ? first + r0 * first_ld : nullptr; a.k = t.k; a.first_ld = first_ld;
     a.target = target;
     if (fwd.splits > 1) {
       g.k_split = fwd.k_split; g.k_splits = fwd.splits;
@@ -1722,14 +1741,15 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
       RAD_TRY(ws_get(c, WS_SPLITK, (size_t)fwd.splits * g.split_stride * 4, &g.C));
     }
     a.tile = fwd.tile;
-    RAD_TRY(run_gemm_call(c, dtype, kOpK, kOpMN, kEpiVocab, g));
-    if (fwd.splits > 1) HIP_TRY(c, timed(c, "vocab_join", [&](const char**) { return launch_vocab_join(dtype, g, c->stream); }));
+    RAD_TRY(run_gemm_call(c, dtype, kOpK, kOpMN, lp ? kEpiLogprob : kEpiVocab, g));
+    if (fwd.splits > 1) HIP_TRY(c, timed(c, "vocab_join", [&](const char**) { return launch_vocab_join(dtype, lp != nullptr, g, c->stream); }));
     VocabFinish f;
     std::memset(&f, 0, sizeof(f));
     f.dtype = dtype;
     f.list = list; f.live = live; f.rows = n; f.classes = d_out; f.parts = parts; f.part = part; f.t = tp;
     f.stats = stats; f.stats_ld = piece; f.target = target;
-    f.row_loss = losses + r0; f.top = top; f.factor = factor; f.common = common;
+    f.spread = spread; f.slope = slope;
+    f.row_loss = lp ? nullptr : losses + r0; f.top = top; f.factor = factor; f.common = common;
     f.z = z; f.z_ld = vp; f.first = a.first; f.first_ld = first_ld;
     f.x = g.A; f.x_ld = dp; f.d_in = d_in; f.xs = xs;
     f.dx = h.dX ? static_cast<char*>(h.dX) + r0 * d_in * esz : nullptr;
@@ -1804,6 +1824,160 @@ extern "C" rad_status rad_linear_distill(rad_ctx* c, const rad_layer* L, const v
   if (!c) return RAD_ERR_NULL;
   RAD_TRY(check_teacher(c, teacher));
   return head_loss(c, L, nullptr, teacher, row_weight, HeadCall{x, W, bias, row_loss, loss, dX, dW, dw_dtype, dbias, beta});
+}
+
+// ------------------------------------------------------------------ log probabilities, entropies, the likeliest classes
+static rad_status check_temperature(rad_ctx* c, double T) {
+  if (!(T >= 1e-6) || !(T <= 1e6)) return fail(c, RAD_ERR_PARAM, "temperature must be in [1e-6, 1e6]");
+  return RAD_OK;
+}
+
+static rad_status check_logprobs(rad_ctx* c, const rad_logprobs* o) {
+  if (!o) return fail(c, RAD_ERR_NULL, "null argument");
+  RAD_TRY(check_temperature(c, o->temperature));
+  if (o->top_k < 0 || o->top_k > kTopMax) return fail(c, RAD_ERR_SHAPE, "lists hold 0 to 256 classes");
+  if (o->top_k > 0 && (!o->top_index || !o->top_logprob)) return fail(c, RAD_ERR_NULL, "a list needs both of its arrays");
+  if (o->logprob && !o->token) return fail(c, RAD_ERR_NULL, "log probabilities need tokens");
+  if (!o->logprob && !o->entropy && o->top_k == 0) return fail(c, RAD_ERR_NULL, "no output asked for");
+  return RAD_OK;
+}
+
+static rad_status check_logprob_grads(rad_ctx* c, const int32_t* token, double T, const float* d_logprob, const float* d_entropy) {
+  RAD_TRY(check_temperature(c, T));
+  if (!d_logprob && !d_entropy) return fail(c, RAD_ERR_NULL, "no gradient given");
+  if (d_logprob && !token) return fail(c, RAD_ERR_NULL, "log probabilities need tokens");
+  return RAD_OK;
+}
+
+static rad_status logprob_rows(rad_ctx* c, LogprobRows a) {
+  RAD_TRY(ws_get(c, WS_ROWLOSS, logprob_rows_bytes(a), &a.ws));
+  HIP_TRY(c, timed(c, a.dz ? "logprob_grad" : "logprob_rows", [&](const char**) { return launch_logprob_rows(a, c->stream); }));
+  return RAD_OK;
+}
+
+extern "C" rad_status rad_token_logprobs(rad_ctx* c, const void* logits, int64_t rows, int64_t classes, int32_t dtype,
+                                         const rad_logprobs* out) {
+  if (!c) return RAD_ERR_NULL;
+  if (!logits) return fail(c, RAD_ERR_NULL, "null argument");
+  RAD_TRY(check_logprobs(c, out));
+  if (rows < 1 || classes < 1 || rows > (1 << 24) || classes > (1 << 24)) return fail(c, RAD_ERR_SHAPE, "bad shape");
+  if (dtype != RAD_F32 && dtype != RAD_BF16) return fail(c, RAD_ERR_PARAM, "unknown dtype");
+  const size_t n = (size_t)rows, list = n * out->top_k * 4;
+  RAD_TRY(check_apart(c, {{out->logprob, n * 4}, {out->entropy, n * 4}, {out->top_k ? out->top_index : nullptr, list},
+                          {out->top_k ? out->top_logprob : nullptr, list}},
+                      {{logits, n * (size_t)classes * (dtype == RAD_F32 ? 4 : 2)}, {out->token, n * 4}}));
+  DeviceGuard guard(c->device);
+  LogprobRows a;
+  std::memset(&a, 0, sizeof(a));
+  a.dtype = dtype; a.rows = (int)rows; a.classes = (int)classes;
+  a.z = logits; a.token = out->token; a.temperature = (float)out->temperature;
+  a.logprob = out->logprob; a.entropy = out->entropy;
+  a.k = out->top_k; a.top_index = out->top_index; a.top_logprob = out->top_logprob;
+  return logprob_rows(c, a);
+}
+
+extern "C" rad_status rad_token_logprobs_grad(rad_ctx* c, const void* logits, int64_t rows, int64_t classes, int32_t dtype,
+                                              const int32_t* token, double temperature, const float* d_logprob,
+                                              const float* d_entropy, void* dlogits) {
+  if (!c) return RAD_ERR_NULL;
+  if (!logits || !dlogits) return fail(c, RAD_ERR_NULL, "null argument");
+  RAD_TRY(check_logprob_grads(c, token, temperature, d_logprob, d_entropy));
+  if (rows < 1 || classes < 1 || rows > (1 << 24) || classes > (1 << 24)) return fail(c, RAD_ERR_SHAPE, "bad shape");
+  if (dtype != RAD_F32 && dtype != RAD_BF16) return fail(c, RAD_ERR_PARAM, "unknown dtype");
+  const size_t n = (size_t)rows, all = n * (size_t)classes * (dtype == RAD_F32 ? 4 : 2);
+  RAD_TRY(check_apart(c, {{dlogits, all}}, {{dlogits == logits ? nullptr : logits, all}, {token, n * 4}, {d_logprob, n * 4}, {d_entropy, n * 4}}));
+  DeviceGuard guard(c->device);
+  LogprobRows a;
+  std::memset(&a, 0, sizeof(a));
+  a.dtype = dtype; a.rows = (int)rows; a.classes = (int)classes;
+  a.z = logits; a.token = token; a.temperature = (float)temperature;
+  a.dz = dlogits; a.d_logprob = d_logprob; a.d_entropy = d_entropy;
+  return logprob_rows(c, a);
+}
+
+extern "C" rad_status rad_linear_logprobs(rad_ctx* c, const rad_layer* L, const void* x, const void* W, const float* bias,
+                                          const rad_logprobs* out) {
+  if (!c) return RAD_ERR_NULL;
+  RAD_TRY(check_logprobs(c, out));
+  RAD_TRY(check_head(c, L, x, W, bias));
+  const int rows = (int)L->batch, d_in = (int)L->d_in, d_out = (int)L->d_out, dtype = L->dtype, k = out->top_k;
+  const int64_t esz = dtype == kF32 ? 4 : 2, vec = 16 / esz;
+  const size_t n_all = (size_t)rows, lists = n_all * k * 4;
+  RAD_TRY(check_apart(c, {{out->logprob, n_all * 4}, {out->entropy, n_all * 4}, {k ? out->top_index : nullptr, lists}, {k ? out->top_logprob : nullptr, lists}},
+                      {{x, n_all * d_in * esz}, {W, (size_t)d_in * d_out * esz}, {bias, (size_t)d_out * 4}, {out->token, n_all * 4}}));
+  DeviceGuard guard(c->device);
+  const int64_t dp = (d_in + vec - 1) / vec * vec, vp8 = (d_out + vec - 1) / vec * vec, vp = (d_out + 63) / 64 * 64;
+  int64_t piece = (int64_t)(kPieceBytes / (size_t)std::max(k ? vp * 4 : vp * esz, dp * esz));
+  piece = std::max<int64_t>(std::min<int64_t>(piece / 256 * 256, 1 << 19), 256);
+  if (piece > rows) piece = rows;
+  const void* Wp = nullptr;
+  const int64_t w_ld = vp8 == d_out && (reinterpret_cast<uintptr_t>(W) & 15) == 0 ? d_out : vp;
+  RAD_TRY(head_padded(c, WS_HEADW, dtype, W, d_in, d_out, w_ld, &Wp));
+  const HeadPlan plan = head_plan(dtype, kEpiVocab, piece, d_out, d_in, true);
+  const int part = plan.splits > 1 ? 64 : head_part(plan.tile), parts = (d_out + part - 1) / part;
+  char* ws = nullptr;
+  RAD_TRY(ws_get(c, WS_ROWLOSS, 256 + (size_t)piece * (12 * (size_t)parts + 8), reinterpret_cast<void**>(&ws)));
+  int32_t* const live = reinterpret_cast<int32_t*>(ws);
+  float* const common = reinterpret_cast<float*>(ws) + 1;
+  float* const inv_count = common + 1;
+  float* const stats = reinterpret_cast<float*>(ws + 256);
+  float* const spread = stats + (size_t)piece * parts * 2;
+  int32_t* const list = reinterpret_cast<int32_t*>(spread + (size_t)piece * parts);
+  float* const target = reinterpret_cast<float*>(list + piece);
+  void* z = nullptr;
+  if (k) RAD_TRY(ws_get(c, WS_LOGITS, (size_t)(piece * vp * 4), &z));
+  const float T = (float)out->temperature;
+  for (int64_t r0 = 0; r0 < rows; r0 += piece) {
+    const int n = (int)std::min<int64_t>(piece, rows - r0);
+    const void* xp = nullptr;
+    RAD_TRY(head_padded(c, WS_HEADX, dtype, static_cast<const char*>(x) + r0 * d_in * esz, n, d_in, dp, &xp));
+    const VocabTargets t{out->token ? out->token + r0 : nullptr, nullptr, nullptr, nullptr, nullptr, 1, T, nullptr, inv_count, 1.f, nullptr};
+    const int64_t tiles = (int64_t)((n + plan.tile - 1) / plan.tile) * ((d_out + 127) / 128) * plan.splits;
+    const bool own_list = n <= kOwnListRows && plan.tile != 256 && (dtype == kBF16 ? n <= 1024 || tiles <= 640 : tiles <= 768);
+    if (!own_list)
+      HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(t, n, d_out, list, live, inv_count, common, c->stream); }));
+    GemmArgs g = gemm_zero();
+    g.M = n; g.N = d_out; g.K = d_in;
+    g.A = xp; g.lda = dp; g.B = Wp; g.ldb = w_ld;
+    g.bias = bias;
+    HeadArgs& a = g.head;
+    a.live = live; a.row_map = list; a.rows = n; a.n_load = (int)vp8;
+    if (own_list) { a.list_out = list; a.live_out = live; a.inv_count_out = inv_count; a.common_out = common; }
+    a.lead = 1.f;
+    a.c = 1.44269504088896340736f / T;
+    a.stats = stats; a.stats_ld = piece; a.spread = spread;
+    a.labels = t.labels; a.k = 1; a.target = target;
+    if (dtype == kF32 || plan.splits > 1) { g.y = z; g.ldy = vp; }
+    else { a.z32 = static_cast<float*>(z); a.z32_ld = vp; }
+    if (plan.splits > 1) {
+      g.k_split = plan.k_split; g.k_splits = plan.splits;
+      g.ldc = vp;
+      g.split_stride = (int64_t)n * vp;
+      RAD_TRY(ws_get(c, WS_SPLITK, (size_t)plan.splits * g.split_stride * 4, &g.C));
+    }
+    a.tile = plan.tile;
+    RAD_TRY(run_gemm_call(c, dtype, kOpK, kOpMN, kEpiLogprob, g));
+    if (plan.splits > 1) HIP_TRY(c, timed(c, "vocab_join", [&](const char**) { return launch_vocab_join(kF32, true, g, c->stream); }));
+    LogprobFinish f;
+    std::memset(&f, 0, sizeof(f));
+    f.list = list; f.live = live; f.rows = n; f.classes = d_out; f.parts = parts; f.part = part; f.temperature = T;
+    f.stats = stats; f.spread = spread; f.stats_ld = piece; f.target = target;
+    f.z = static_cast<const float*>(z); f.z_ld = vp;
+    f.logprob = out->logprob ? out->logprob + r0 : nullptr; f.entropy = out->entropy ? out->entropy + r0 : nullptr;
+    f.k = k;
+    if (k) { f.top_index = out->top_index + r0 * k; f.top_logprob = out->top_logprob + r0 * k; }
+    HIP_TRY(c, timed(c, "logprob_finish", [&](const char**) { return launch_logprob_finish(f, c->stream); }));
+  }
+  return RAD_OK;
+}
+
+extern "C" rad_status rad_linear_logprobs_grad(rad_ctx* c, const rad_layer* L, const void* x, const void* W, const float* bias,
+                                               const int32_t* token, double temperature, const float* d_logprob, const float* d_entropy,
+                                               void* dX, void* dW, int32_t dw_dtype, float* dbias, float beta) {
+  if (!c) return RAD_ERR_NULL;
+  RAD_TRY(check_logprob_grads(c, token, temperature, d_logprob, d_entropy));
+  const LogprobGrads lp{temperature, d_logprob, d_entropy};
+  return head_loss(c, L, token, nullptr, nullptr, HeadCall{x, W, bias, nullptr, nullptr, dX, dW, dw_dtype, dbias, beta}, &lp);
 }
 
 // ------------------------------------------------------------------ parameter updates

@@ -23,7 +23,7 @@ hipError_t launch_gemm_bf16(int a_kind, int b_kind, int epi, const GemmArgs& g, 
 
 hipError_t launch_gemm(int dtype, int a_kind, int b_kind, int epi, const GemmArgs& g, hipStream_t st,
                        const char** name) {
-  if (epi == kEpiVocab || epi == kEpiHeadX || epi == kEpiHeadW) return launch_gemm_head(dtype, epi, g, st, name);
+  if (epi == kEpiVocab || epi == kEpiLogprob || epi == kEpiHeadX || epi == kEpiHeadW) return launch_gemm_head(dtype, epi, g, st, name);
   if (dtype == kBF16) return launch_gemm_bf16(a_kind, b_kind, epi, g, st, name);
   if (dtype == kF32) return launch_gemm_f32(a_kind, b_kind, epi, g, st, name);
   return hipErrorInvalidValue;

@@ -155,8 +155,8 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
   const uint32_t smem_lds = (uint32_t)reinterpret_cast<uintptr_t>(smem_raw);
   constexpr int kStageElems = S::STAGE / 2, kAElems = BM * BK;
 
-  constexpr bool kHead = EPI == kEpiVocab || EPI == kEpiHeadX || EPI == kEpiHeadW;
-  constexpr bool kSwap = EPI == kEpiVocab;
+  constexpr bool kVocab = EPI == kEpiVocab || EPI == kEpiLogprob, kHead = kVocab || EPI == kEpiHeadX || EPI == kEpiHeadW;
+  constexpr bool kSwap = kVocab;
   // (N may be ragged for an M/N-contiguous B; under a loss M too, and N whatever B is, and only the tiles of the rows that
   // count are dealt out)
   int live = 0;
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
   const bool ragged = krem < BK;                       // its loads read zeros past K; the steady loop never issues it
   const int KTs = ragged ? KT - 1 : KT;
   LoadA la; LoadB lb;
-  if constexpr (EPI == kEpiVocab) la.init_mapped(g.A, g.lda, m0, kbeg, live, g.head.row_map);
+  if constexpr (kVocab) la.init_mapped(g.A, g.lda, m0, kbeg, live, g.head.row_map);
   else if constexpr (EPI == kEpiHeadW) la.init(live == g.head.rows ? g.head.whole : g.A, g.lda, m0, kbeg, g.m_load);
   else la.init(g.A, g.lda, m0, kbeg, g.M);
   lb.init(g.B, g.ldb, n0, kbeg, kHead && kBT ? g.head.n_load : g.N);
@@ -370,8 +370,8 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_dma64_bf16_kernel(GemmArgs 
       return;
     }
   }
-  if constexpr (EPI == kEpiVocab) {
-    epilogue_vocab<uint16_t, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, live, g.head.row_map + m0);
+  if constexpr (kVocab) {
+    epilogue_vocab<uint16_t, BM, BN, TM, TN, EPI == kEpiLogprob>(g, acc, smem, m0, n0, wm0, wn0, live, g.head.row_map + m0);
   } else if constexpr (EPI == kEpiHeadX || EPI == kEpiHeadW) {
     epilogue_head<EPI == kEpiHeadX, BM, BN, TM, TN>(g, acc, smem, m0, n0, wm0, wn0, EPI == kEpiHeadX ? live : g.M);
   } else if constexpr (EPI == kEpiStore && AKIND == kOpMN) {      // dW from a dense store: fp32 out

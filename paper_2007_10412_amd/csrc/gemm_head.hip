@@ -51,7 +51,7 @@ template <typename T, int AKIND, int BKIND, int EPI> hipError_t run_head(const G
   if (e != hipSuccess || g.dry_run) return e;
   if constexpr (sizeof(T) == 2) {
     if (g.head.tile == 256) {
-      if (EPI == kEpiVocab && (g.head.list_out || g.k_splits > 1)) return hipErrorInvalidValue;
+      if ((EPI == kEpiVocab || EPI == kEpiLogprob) && (g.head.list_out || g.k_splits > 1)) return hipErrorInvalidValue;
       static bool prepared = false;
       return launch_sized(gemm_dma64_bf16_kernel<AKIND, BKIND, EPI, 256, 256>, &prepared, GemmDma64Smem<EPI, 256, 256>::BYTES, 256, 256, g, st);
     }
@@ -68,6 +68,7 @@ template <typename T, int AKIND, int BKIND, int EPI> hipError_t run_head(const G
 }
 template <typename T> hipError_t run_any(int epi, const GemmArgs& g, hipStream_t st) {
   if (epi == kEpiVocab) return run_head<T, kOpK, kOpMN, kEpiVocab>(g, st);
+  if (epi == kEpiLogprob) return run_head<T, kOpK, kOpMN, kEpiLogprob>(g, st);
   if (epi == kEpiHeadX) return run_head<T, kOpK, kOpK, kEpiHeadX>(g, st);
   if (epi == kEpiHeadW) return run_head<T, kOpMN, kOpMN, kEpiHeadW>(g, st);
   return hipErrorInvalidValue;
@@ -90,7 +91,7 @@ hipError_t launch_gemm_head_pair(int dtype, const GemmArgs& x, const GemmArgs& w
 hipError_t launch_gemm_head(int dtype, int epi, const GemmArgs& g, hipStream_t st, const char** name) {
   static const char* const names[2][3] = {{"gemm_f32_head_fwd", "gemm_f32_head_dx", "gemm_f32_head_dw"},
                                           {"gemm_bf16_head_fwd", "gemm_bf16_head_dx", "gemm_bf16_head_dw"}};
-  if (name) *name = names[dtype == kBF16][epi == kEpiVocab ? 0 : epi == kEpiHeadX ? 1 : 2];
+  if (name) *name = names[dtype == kBF16][epi == kEpiHeadX ? 1 : epi == kEpiHeadW ? 2 : 0];
   return dtype == kBF16 ? run_any<uint16_t>(epi, g, st) : run_any<float>(epi, g, st);
 }
 

@@ -155,7 +155,7 @@ template <bool AT, bool BT, int BM, int BN, int TM, int TN, bool SWAP> struct Ti
 template <typename T, int AKIND, int BKIND, int EPI, int BM, int BN, int S>
 __device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* smem_raw, int block, int split) {
   constexpr int TM = BM / 64, TN = BN / 64;
-  constexpr bool kAT = AKIND == kOpMN, kBT = BKIND == kOpMN, kSwap = EPI == kEpiVocab;
+  constexpr bool kAT = AKIND == kOpMN, kBT = BKIND == kOpMN, kVocab = EPI == kEpiVocab || EPI == kEpiLogprob, kSwap = kVocab;
   typedef TileOperand<T, BM, kAT> LoadA;
   typedef TileOperand<T, BN, kBT> LoadB;
   typedef TileSmem<T, BM, BN, S> Smem;
@@ -167,7 +167,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* s
   int live;
   uint32_t mine = 0u;
   int mine_at = 0;
-  if (EPI == kEpiVocab && g.head.list_out) {
+  if (kVocab && g.head.list_out) {
     __shared__ int32_t s_n[kGemmThreads / 64];
     __shared__ float2 s_w[kGemmThreads / 64];
     const bool write = block == 0 && split == 0;
@@ -185,7 +185,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* s
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int wm0 = (w >> 1) * (BM / 2), wn0 = (w & 1) * (BN / 2);
   const int32_t* tile_rows = nullptr;                   // rows of the batch of the tile's rows
-  if (EPI == kEpiVocab && g.head.list_out) {
+  if (kVocab && g.head.list_out) {
     __shared__ int32_t s_list[BM];
     const int per = g.head.rows <= 4 * kGemmThreads ? 4 : kOwnListRows / kGemmThreads;
     for (int q0 = 0; q0 < per; q0 += 4) {
@@ -197,7 +197,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* s
     }
     __syncthreads();
     tile_rows = s_list;
-  } else if (EPI == kEpiVocab) {
+  } else if (kVocab) {
     tile_rows = g.head.row_map + m0;
   }
 
@@ -214,7 +214,7 @@ __device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* s
   const int kend = g.k_splits > 1 ? min(k_all, kbeg + g.k_split) : k_all;
   const int KT = max(0, (kend - kbeg + BK - 1) / BK);
   LoadA la; LoadB lb;
-  if (EPI == kEpiVocab) la.init(g.A, g.lda, m0, kbeg, live, tile_rows);
+  if (kVocab) la.init(g.A, g.lda, m0, kbeg, live, tile_rows);
   else if (EPI == kEpiHeadW) la.init(live == g.head.rows ? g.head.whole : g.A, g.lda, m0, kbeg, g.m_load, nullptr);
   else la.init(g.A, g.lda, m0, kbeg, g.M, nullptr);
   lb.init(g.B, g.ldb, n0, kbeg, kBT ? g.head.n_load : g.N, nullptr);
@@ -240,9 +240,9 @@ __device__ __forceinline__ void tile_product(const GemmArgs& g, unsigned char* s
   }
   __syncthreads();                                      // the stages become the output tile
   T* const ct = reinterpret_cast<T*>(smem_raw);
-  if constexpr (EPI == kEpiVocab) {
+  if constexpr (kVocab) {
     if (g.k_splits > 1) { store_partial_rows<TM, TN>(g, acc, m0, n0, wm0, wn0, live, split); return; }
-    epilogue_vocab<T, BM, BN, TM, TN>(g, acc, ct, m0, n0, wm0, wn0, live, tile_rows);
+    epilogue_vocab<T, BM, BN, TM, TN, EPI == kEpiLogprob>(g, acc, ct, m0, n0, wm0, wn0, live, tile_rows);
   } else {
     if (g.k_splits > 1) {                               // this split's partial sums, in fp32
       GemmArgs gs = g;

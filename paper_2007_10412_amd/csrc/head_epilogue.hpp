@@ -4,8 +4,8 @@
 
 namespace rad {
 
-// What row gradients are divided by and the products multiplied by at their ends (row weights w of the rows that count): T x the
-// largest |w|.  Not where that is infinite or NaN, whose rows would take the others' gradients with them, nor where rows whose
+// What row gradients are divided by and the products multiplied by at their ends (row weights w of the rows that count): the lead
+// (T, or 1 / T of log probabilities) x the largest |w|.  Not where that is infinite or NaN, whose rows would take the others' gradients with them, nor where rows whose
 // weight is below 2^-60 of a factor above 1 would lose theirs to underflow; then 1, and each row has its own weight.
 struct WeightRange {
   float most = 0.f, least = INFINITY;                      // of |w|; infinite or NaN: infinity; zeros are not among the least
@@ -14,13 +14,18 @@ struct WeightRange {
     most = fmaxf(most, w < INFINITY ? w : INFINITY);
     if (w > 0.f) least = fminf(least, w);
   }
+  // a row's, of one or two kinds
+  __device__ __forceinline__ void add(const float* weight, const float* weight2, int row) {
+    if (!weight2) add(weight[row]);
+    else add(fmaxf(weight ? fabsf(weight[row]) : 0.f, fabsf(weight2[row])));
+  }
   __device__ __forceinline__ void join(float m, float l) { most = fmaxf(most, m); least = fminf(least, l); }
   __device__ __forceinline__ void join_wave() {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) join(__shfl_xor(most, o), __shfl_xor(least, o));
   }
-  __device__ __forceinline__ float common(float T) const {
-    const float f = T * most;
+  __device__ __forceinline__ float common(float lead) const {
+    const float f = lead * most;
     return f > 0.f && f < INFINITY && (f <= 1.f || least >= most * 0x1p-60f) ? f : 1.f;
   }
 };
@@ -60,16 +65,17 @@ __device__ __forceinline__ int own_rows(const HeadArgs& h, int classes, int32_t*
   uint32_t mine = 0u;
 #pragma unroll
   for (int q = 0; q < PER; ++q)
-    if (r0 + q < h.rows && (h.labels ? (uint32_t)h.labels[r0 + q] < (uint32_t)classes : h.counts[r0 + q] != 0)) mine |= 1u << q;
+    if (r0 + q < h.rows && (h.labels ? (uint32_t)h.labels[r0 + q] < (uint32_t)classes : !h.counts || h.counts[r0 + q] != 0)) mine |= 1u << q;
   const int n = __popc(mine);
   int up = n;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(up, o); if (lane >= o) up += v; }
   if (lane == 63) s_n[w] = up;
-  if (write && h.weight) {
+  const bool weights = h.weight || h.weight2;
+  if (write && weights) {
     WeightRange of;
 #pragma unroll
-    for (int q = 0; q < PER; ++q) if ((mine >> q) & 1u) of.add(h.weight[r0 + q]);
+    for (int q = 0; q < PER; ++q) if ((mine >> q) & 1u) of.add(h.weight, h.weight2, r0 + q);
     of.join_wave();
     if (lane == 0) s_w[w] = make_float2(of.most, of.least);
   }
@@ -80,12 +86,12 @@ __device__ __forceinline__ int own_rows(const HeadArgs& h, int classes, int32_t*
   *mine_out = mine; *at_out = at;
   if (write) {
     if (threadIdx.x == 0) {
-      const float inv = h.inv_count_out ? (all > 0 ? 1.f / (float)all : 0.f) : h.weight ? 0.f : *h.inv_count;
+      const float inv = h.inv_count_out ? (all > 0 ? 1.f / (float)all : 0.f) : weights ? 0.f : *h.inv_count;
       WeightRange of;
-      if (h.weight) for (int q = 0; q < kGemmThreads / 64; ++q) of.join(s_w[q].x, s_w[q].y);
+      if (weights) for (int q = 0; q < kGemmThreads / 64; ++q) of.join(s_w[q].x, s_w[q].y);
       *h.live_out = all;
       if (h.inv_count_out) *h.inv_count_out = inv;
-      *h.common_out = h.weight ? of.common(h.temperature) : h.temperature * inv;
+      *h.common_out = weights ? of.common(h.lead) : h.lead * inv;
     }
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
@@ -105,6 +111,9 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   put_pair(p, a, b);
   return (uint32_t)p[0] | ((uint32_t)p[1] << 16);
 }
+
+// a power of two that is zero in fp32: what an exponent is clamped to where it is multiplied by its (vanished) exponential
+constexpr float kNoPower = -200.f;
 
 // two distances below a maximum, as shares of the range, to 16 bits each (round to nearest; clamped to [0, 1])
 constexpr float kCodeRange = 128.f;
@@ -147,7 +156,9 @@ __device__ __forceinline__ void store_tile(const T* ct, T* C, int64_t ldc, int r
 // fp32: the logits themselves take the place of the codes.
 // The product is transposed (lane = row of the tile): a row's 64 values are one lane's, so maximum and sum take one exchange
 // between the two lanes that share the row.
-template <typename T, int BM, int BN, int TM, int TN>
+// LOGPROB: the sum of 2^l l besides, l = (z - m) c, of which a row's entropy is made, and the bf16 layer's logits in fp32 where the
+// likeliest of them are to be found; its targets are labels or none.
+template <typename T, int BM, int BN, int TM, int TN, bool LOGPROB>
 __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc)[TM][TN], T* ct, int m0, int n0, int wm0,
                                                int wn0, int live, const int32_t* tile_rows) {
   constexpr bool kCodes = sizeof(T) == 2;
@@ -201,6 +212,7 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
       }
       return;
     }
+    if constexpr (LOGPROB) return;
 #pragma unroll
     for (int i = i0; i < i1; ++i)
       if (row[i] >= 0) {
@@ -232,16 +244,41 @@ __device__ __forceinline__ void epilogue_vocab(const GemmArgs& g, floatx16 (&acc
 #pragma unroll
       for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
     m = fmaxf(m, __shfl_xor(m, 32));
+    if constexpr (LOGPROB && kCodes) {
+      if (h.z32 && row[i] >= 0) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int col = nw + j * 32 + q * 8 + hh * 4;
+            if (col < h.z32_ld)
+              *reinterpret_cast<floatx4*>(h.z32 + (int64_t)place * h.z32_ld + col) =
+                  floatx4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+          }
+      }
+    }
     const float from = m == -INFINITY ? 0.f : m;
+    float spread = 0.f;
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float d = acc[i][j][e] - from;
-        s += __builtin_amdgcn_exp2f(d * c);
+        if constexpr (LOGPROB) {
+          const float x = __builtin_amdgcn_exp2f(d * c);
+          s += x;
+          spread += x * fmaxf(d * c, kNoPower);
+        } else {
+          s += __builtin_amdgcn_exp2f(d * c);
+        }
         if (kCodes) acc[i][j][e] = d * c_code;
+        if constexpr (LOGPROB) { if (e % 8 == 7) asm volatile("" : "+v"(s), "+v"(spread)); }   // (both sums move on together)
       }
     s += __shfl_xor(s, 32);
+    if constexpr (LOGPROB) {
+      spread += __shfl_xor(spread, 32);
+      if (row[i] >= 0 && hh == 0) h.spread[(int64_t)part * h.stats_ld + place] = spread;
+    }
     if (row[i] >= 0 && hh == 0) *reinterpret_cast<float2*>(h.stats + ((int64_t)part * h.stats_ld + place) * 2) = make_float2(m, s);
     if (g.y) {
       T* const crow = ct + (wm0 + i * 32 + lr) * CP + wn0 + hh * 4;

@@ -51,7 +51,8 @@ enum EpiKind : int {
   // a layer under a loss over its classes (direct-to-LDS kernels; HeadArgs):
   kEpiVocab = 4,  // what a softmax needs of the logits, per row and part of its columns, and the logits (bf16: in 16 bits)
   kEpiHeadX = 5,  // dX: rows put in their places; or fp32 partial sums
-  kEpiHeadW = 6   // dW, in fp32 (+= if beta) or bf16; or fp32 partial sums
+  kEpiHeadW = 6,  // dW, in fp32 (+= if beta) or bf16; or fp32 partial sums
+  kEpiLogprob = 7 // kEpiVocab with what an entropy needs besides (HeadArgs.spread), and fp32 logits where they are asked for
 };
 
 // The rows of the batch that have a target come first in a list; the products run over that list, whose length only the
@@ -62,7 +63,7 @@ struct HeadArgs {
   // kEpiVocab with few rows: every workgroup makes its tile's part of the list, one writes the whole (rows <= kOwnListRows)
   const int32_t* counts;        // which rows count, where there are no labels
   int32_t* list_out; int32_t* live_out; float* inv_count_out;   // list_out null: the list is there; the others as in launch_row_list
-  float* common_out; const float* weight; const float* inv_count; float temperature;
+  float* common_out; const float* weight; const float* weight2; const float* inv_count; float lead;
   const float* common;          // kEpiHeadX, kEpiHeadW: factor of the product
   const int32_t* row_map;       // row of x and dX of every place in the list (kEpiVocab: of A; kEpiHeadX: of C)
   const void* whole; int rows;  // rows of the batch; kEpiHeadW: what A is where the list has them all
@@ -74,6 +75,9 @@ struct HeadArgs {
   const int32_t* labels;        // [rows of the batch], or
   const int32_t* index; const uint16_t* first; int k, first_ld;   // lists [rows][k], and how many of a row's entries lie before part t
   float* target;                // [place][k]: the logits of the targets
+  // kEpiLogprob (labels may be null: no targets)
+  float* spread;                // [columns / part][stats_ld]: sums of 2^l l, l = (z - m) c
+  float* z32; int64_t z32_ld;   // bf16: the logits in fp32, or null
 };
 
 struct GemmArgs {
@@ -319,6 +323,10 @@ struct VocabTargets {
   float temperature;
   const float* weight;          // the caller's row weights, or null: every row that counts weighs *inv_count
   const float* inv_count;
+  float lead;                   // what a row's gradient has beside its weight: T for these losses, 1 / T for log probabilities
+  // log probabilities: labels null: every row counts; weight and weight2: the gradients of a row's log probability and entropy
+  // (null: zeros)
+  const float* weight2;
 };
 constexpr int kTeacherMax = 1024;                     // longest list
 // lists sorted, joined and turned into probabilities (softmax of logit / temperature over the entries in [0, classes) whose
@@ -343,20 +351,55 @@ int64_t vocab_rows_stats_floats(int rows, int classes);
 // whether the kernel counts the rows that count itself, and *t.inv_count is not read
 bool vocab_rows_count(const VocabRows& a);
 hipError_t launch_vocab_rows(const VocabRows& a, hipStream_t st);
+// ---- log probabilities, entropies and the likeliest classes (logprob.hip).  A row's q = softmax(z / T); token null: every row
+// counts, else those whose token is a class.
+constexpr int kTopMax = 256;                          // longest list of likeliest classes
+struct LogprobRows {
+  int dtype, rows, classes;
+  const void* z;
+  const int32_t* token;
+  float temperature;
+  // forward: log q[token], entropy (either may be null), and the k likeliest classes [rows][k] with their log q, ties to the
+  // lowest class; -1 and -infinity where there are fewer.  A row that does not count: zeros and no classes.
+  float* logprob; float* entropy;
+  int k; int32_t* top_index; float* top_logprob;
+  // backward (dz not null): dz (may be z) from the gradients of a row's log q[token] and entropy (null: zeros)
+  void* dz; const float* d_logprob; const float* d_entropy;
+  void* ws;                     // logprob_rows_bytes of scratch
+};
+size_t logprob_rows_bytes(const LogprobRows& a);
+// (three floats a part of a row, before the parts' lists)
+__host__ __device__ constexpr size_t logprob_stats_bytes(int rows, int parts) { return ((size_t)rows * parts * 12 + 255) / 256 * 256; }
+hipError_t launch_logprob_rows(const LogprobRows& a, hipStream_t st);
+// The same after a layer's product (kEpiLogprob), for the places of its list: from the parts' statistics, the tokens' logits
+// [place] and, where k > 0, the logits in fp32.
+struct LogprobFinish {
+  const int32_t* list; const int32_t* live;
+  int rows, classes, parts, part;
+  float temperature;
+  const float* stats; const float* spread; int64_t stats_ld;
+  const float* target;
+  const float* z; int64_t z_ld;
+  float* logprob; float* entropy;       // in the batch's order
+  int k; int32_t* top_index; float* top_logprob;
+};
+hipError_t launch_logprob_finish(const LogprobFinish& a, hipStream_t st);
+
 // out (bf16) = beta out + in (fp32), n elements
 hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, hipStream_t st);
 
 // ---- the layer under such a loss, fp32 or bf16 (vocab_head.hip), around the products with HeadArgs
 // list [rows]: the rows that count, in order, then the others; *live: how many count; *inv_count: 1 / that (null: *t.inv_count
-// is there); *common = T x the largest |weight| of these rows (1 where that would lose some of them: WeightRange) or, without
-// weights, T x the inverse count: what dX, dW and dbias are multiplied by at their ends.  dz holds row gradients of weight 1 (or a share of 1): a factor that all rows have in common,
+// is there); *common = t.lead x the largest |weight| of these rows (1 where that would lose some of them: WeightRange) or, without
+// weights, t.lead x the inverse count: what dX, dW and dbias are multiplied by at their ends.  dz holds row gradients of weight 1 (or a share of 1): a factor that all rows have in common,
 // rounded into each of them, would put its one rounding error on the whole gradient (0.3 % of dW where 1 / n falls badly).
 hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, float* common,
                            hipStream_t st);
-// kEpiVocab's work on the partial sums of a product with a split K, which that epilogue has left in C; parts are 64 wide
-hipError_t launch_vocab_join(int dtype, const GemmArgs& g, hipStream_t st);
+// kEpiVocab's work (logprob: kEpiLogprob's) on the partial sums of a product with a split K, which that epilogue has left in C;
+// parts are 64 wide; dtype: of the logits that y gets (kF32: fp32, kBF16: codes)
+hipError_t launch_vocab_join(int dtype, bool logprob, const GemmArgs& g, hipStream_t st);
 // After the logits' product, for every place of the list: the row's loss, its maximum top and what its exponentials
-// 2^((z - top) c) are multiplied by, factor = share / their sum, share = weight T / *common.  For dW the rows of x side by side (xs, rows x_ld apart),
+// 2^((z - top) c) are multiplied by, factor = share / their sum, share = weight t.lead / *common.  For dW the rows of x side by side (xs, rows x_ld apart),
 // unless the list has them all.  Rows that do not count: no loss, dX zero.
 struct VocabFinish {
   int dtype;
@@ -364,6 +407,9 @@ struct VocabFinish {
   int rows, classes, parts, part;   // `parts` parts of `part` (64 or 128) classes
   VocabTargets t;               // of the rows of x
   const float* stats; int64_t stats_ld;
+  // The gradient of log probabilities and entropies (null: of a loss): there are no losses, and exponentials 2^l, l = (z - top) c,
+  // are multiplied by factor + slope l.
+  const float* spread; float* slope;
   const float* target;          // [place][k]
   float* row_loss;              // [rows], in the batch's order
   float* loss;                  // the sum over these rows, or null: left to another call

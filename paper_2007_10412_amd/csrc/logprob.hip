@@ -1,0 +1,542 @@
+// Log probabilities of given classes, entropies and the likeliest classes of rows of logits, and the logits' gradient from those of
+// the first two.
+//
+// q = softmax(z / T).  With m a row's maximum, l_v = (z_v - m) log2(e) / T, s = sum_v 2^l_v and u = sum_v 2^l_v l_v:
+//   log q_v = (z_v - m) / T - ln s,   H = - sum_v q_v log q_v = ln s - ln 2 u / s,
+//   dz_v = (a (1[v = token] - q_v) - h q_v (log q_v + H)) / T = 2^l_v (A + B l_v) + (a / T) 1[v = token]
+// for the gradients a of log q[token] and h of H, A = (h ln 2 u / s - a) / (T s), B = - h ln 2 / (T s).  So a row is read once and
+// kept in registers between its statistics and whatever follows, 16 bytes a lane.
+//
+// The k likeliest classes.  Any class of the list is at least as large as the k-th largest of the maxima of disjoint groups of
+// the row (k groups then hold one such class each).  A thread's maxima are there already; one wave finds that bound of them bit by
+// bit, and the few classes that reach it (of n groups some -n ln(1 - k / n): 1.4 k where n = 2 k) are placed by counting those before them.  Rows of which too
+// many reach it (equal logits above all) are searched digit by digit, as often as it takes: the list is exact for every row.
+#include "vocab_row.hpp"
+
+namespace rad {
+namespace {
+
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// ------------------------------------------------------------------ selection
+// Logits as whole numbers in their order (-0 as 0); 0 for -infinity and NaN, which are not listed.
+__device__ __forceinline__ uint32_t order_key(float z) {
+  const uint32_t u = __float_as_uint(z + 0.f);
+  return z > -INFINITY ? u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u) : 0u;
+}
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+constexpr uint32_t kLowestKey = 0x00800000u;            // of -FLT_MAX
+// of two classes the one that comes first in a list has the larger entry; 0 is none
+__device__ __forceinline__ uint64_t make_entry(uint32_t key, int index) { return key ? ((uint64_t)key << 32) | (uint32_t)~index : 0ull; }
+__device__ __forceinline__ uint32_t entry_key(uint64_t e) { return (uint32_t)(e >> 32); }
+__device__ __forceinline__ int entry_index(uint64_t e) { return (int)~(uint32_t)e; }
+
+// entries that may wait for their places, at most kCand; counting takes their number squared over the threads
+template <int NT> constexpr int cand_max() { return NT <= 128 ? 384 : NT <= 256 ? 512 : 1024; }
+template <int NT, int GROUPS> struct TopLds {
+  uint64_t cand[cand_max<NT>()];
+  uint32_t group[GROUPS];
+  uint32_t hist[256];
+  int wave_n[NT / 64];
+  int n; uint32_t bound; int digit, need;
+};
+
+// wave 0: the 16 upper bits (0 below) of the k-th largest of 64 R maxima, each of `GROUPS` / (64 R) groups; at least kLowestKey
+template <int GROUPS, int R>
+__device__ __forceinline__ uint32_t group_bound(const uint32_t* group, int k) {
+  static_assert(GROUPS % (64 * R) == 0, "whole waves");
+  uint32_t m[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) m[r] = 0u;
+#pragma unroll
+  for (int j = 0; j < GROUPS / 64; ++j) m[j % R] = max(m[j % R], group[j * 64 + (int)threadIdx.x]);
+  uint32_t p = 0u;
+  for (int b = 31; b >= 16; --b) {
+    const uint32_t with = p | (1u << b);
+    int n = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) n += __popcll(__ballot(m[r] >= with));
+    if (n >= k) p = with;
+  }
+  return max(p, kLowestKey);
+}
+
+template <int NT, int GROUPS> __device__ __forceinline__ void append(TopLds<NT, GROUPS>& lds, uint32_t key, int index) {
+  const int at = atomicAdd(&lds.n, 1);
+  if (at < cand_max<NT>()) lds.cand[at] = make_entry(key, index);
+}
+
+// after the groups' maxima are in place (a barrier): the bound, the same for the workgroup, and room for entries
+template <int NT, int GROUPS> __device__ __forceinline__ uint32_t find_bound(TopLds<NT, GROUPS>& lds, int k) {
+  if (threadIdx.x < 64) {
+    constexpr int R = GROUPS >= 512 ? 8 : GROUPS / 64;
+    const uint32_t b = R > 4 && k <= 128 ? group_bound<GROUPS, 4>(lds.group, k) : group_bound<GROUPS, R>(lds.group, k);
+    if (threadIdx.x == 0) { lds.bound = b; lds.n = 0; }
+  }
+  __syncthreads();
+  return lds.bound;
+}
+
+// The k largest of n entries, more than k of which are there, wherever equal keys come with ascending indexes: the k-th key digit
+// by digit, then those above it and the first that equal it, in any order into cand.
+template <int NT, int GROUPS, class F> __device__ __forceinline__ void select_exact(TopLds<NT, GROUPS>& lds, F entry, int64_t n, int k) {
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  uint32_t kth = 0u;
+  int need = k;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int t = tid; t < 256; t += NT) lds.hist[t] = 0u;
+    __syncthreads();
+    for (int64_t i = tid; i < n; i += NT) {
+      const uint32_t key = entry_key(entry(i));
+      if (key && (shift == 24 || (key >> (shift + 8)) == (kth >> (shift + 8)))) atomicAdd(&lds.hist[(key >> shift) & 255u], 1u);
+    }
+    __syncthreads();
+    if (tid < 64) {                                     // lane l: digits 255 - 4 l and the three below
+      int c[4], sum = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) { c[q] = (int)lds.hist[255 - 4 * lane - q]; sum += c[q]; }
+      int up = sum;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(up, o); if (lane >= o) up += v; }
+      int before = up - sum;
+      if (before < need && need <= up) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (before < need && need <= before + c[q]) { lds.digit = 255 - 4 * lane - q; lds.need = need - before; }
+          before += c[q];
+        }
+      }
+    }
+    __syncthreads();
+    kth |= (uint32_t)lds.digit << shift;
+    need = lds.need;
+    __syncthreads();
+  }
+  if (tid == 0) lds.n = 0;
+  __syncthreads();
+  int taken = 0;                                        // entries of the k-th key: the first `need` belong to the list
+  for (int64_t i0 = 0; i0 < n; i0 += NT) {
+    const int64_t i = i0 + tid;
+    const uint64_t e = i < n ? entry(i) : 0ull;
+    const uint32_t key = entry_key(e);
+    if (key > kth) lds.cand[atomicAdd(&lds.n, 1)] = e;
+    if (taken >= need) continue;
+    const uint64_t ties = __ballot(e != 0ull && key == kth);
+    if (lane == 0) lds.wave_n[w] = __popcll(ties);
+    __syncthreads();
+    int before = taken + lanes_below(ties), all = taken;
+#pragma unroll
+    for (int q = 0; q < NT / 64; ++q) { if (q < w) before += lds.wave_n[q]; all += lds.wave_n[q]; }
+    if (e != 0ull && key == kth && before < need) lds.cand[k - need + before] = e;
+    taken = all;
+    __syncthreads();
+  }
+  __syncthreads();
+}
+
+// the first k of the n entries in cand (a barrier before): put(place, entry) for those that are there
+template <int NT, int GROUPS, class F> __device__ __forceinline__ void place_entries(const TopLds<NT, GROUPS>& lds, int n, int k, F put) {
+  for (int i = threadIdx.x; i < n; i += NT) {
+    const uint64_t e = lds.cand[i];
+    int before = 0;
+    for (int j = 0; j < n; ++j) before += lds.cand[j] > e ? 1 : 0;
+    if (before < k) put(before, e);
+  }
+  for (int i = n + (int)threadIdx.x; i < k; i += NT) put(i, 0ull);
+}
+
+// ------------------------------------------------------------------ statistics
+// (m, s, u) of parts of a row; one with nothing in it adds its 0, or its NaN
+struct RowStats {
+  float m = -INFINITY, s = 0.f, u = 0.f;
+  __device__ __forceinline__ void join(float m2, float s2, float u2, float c) {
+    if (m2 == -INFINITY) { s += s2; u += s2; return; }
+    if (m == -INFINITY) { m = m2; s += s2; u += u2; return; }
+    const float M = fmaxf(m, m2), l = (m - M) * c, l2 = (m2 - M) * c;
+    const float f = __builtin_amdgcn_exp2f(l), f2 = __builtin_amdgcn_exp2f(l2);
+    u = f * (u + s * fmaxf(l, kNoPower)) + f2 * (u2 + s2 * fmaxf(l2, kNoPower));
+    s = f * s + f2 * s2;
+    m = M;
+  }
+  __device__ __forceinline__ void join_wave(float c) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) join(__shfl_xor(m, o), __shfl_xor(s, o), __shfl_xor(u, o), c);
+  }
+};
+// a workgroup's, the same for all of its threads; s_w: a triple a wave
+template <int NT> __device__ __forceinline__ RowStats block_join(RowStats r, bool wave_joined, float c, float3* s_w) {
+  if (!wave_joined) r.join_wave(c);
+  if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = make_float3(r.m, r.s, r.u);
+  __syncthreads();
+  RowStats all;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) all.join(s_w[w].x, s_w[w].y, s_w[w].z, c);
+  return all;
+}
+
+// what a row's statistics say
+struct RowEnd {
+  float base, log_s, inv_t, entropy;
+  __device__ __forceinline__ RowEnd(const RowStats& r, float T) {
+    base = exp_base(r.m); log_s = logf(r.s); inv_t = 1.f / T;
+    entropy = log_s - kLn2 * (r.u / r.s);
+  }
+  __device__ __forceinline__ float log_q(float z) const { return (z - base) * inv_t - log_s; }
+};
+
+__device__ __forceinline__ bool token_counts(const int32_t* token, int row, int classes) {
+  return !token || (uint32_t)token[row] < (uint32_t)classes;
+}
+
+// a row that does not count
+template <int NT> __device__ __forceinline__ void leave_row(float* logprob, float* entropy, int k, int32_t* top_index, float* top_logprob, int row) {
+  if (threadIdx.x == 0) {
+    if (logprob) logprob[row] = 0.f;
+    if (entropy) entropy[row] = 0.f;
+  }
+  for (int i = threadIdx.x; i < k; i += NT) {
+    top_index[(int64_t)row * k + i] = -1;
+    top_logprob[(int64_t)row * k + i] = -INFINITY;
+  }
+}
+__device__ __forceinline__ void put_top(int32_t* top_index, float* top_logprob, int64_t at, uint64_t e, const RowEnd& end) {
+  top_index[at] = e ? entry_index(e) : -1;
+  top_logprob[at] = e ? end.log_q(key_value(entry_key(e))) : -INFINITY;
+}
+
+// ------------------------------------------------------------------ dense rows
+// statistics of a wave's vectors; e (kKeep): exponentials from the wave's maximum
+template <typename T, int NT, int NV> __device__ __forceinline__ RowStats part_stats(RowPart<T, NT, NV>& p, float c) {
+  typedef RowPart<T, NT, NV> Part;
+  RowStats r;
+  r.m = p.single;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+#pragma unroll
+    for (int q = 0; q < Part::VPL; ++q) r.m = fmaxf(r.m, p.at(i, q));
+    if (i % 2) __builtin_amdgcn_sched_barrier(0);
+  }
+  r.m = wave_max(r.m);
+  if (sizeof(T) == 2) p.forget();
+  const float b = exp_base(r.m), l0 = (p.single - b) * c, e0 = __builtin_amdgcn_exp2f(l0);
+  r.s = e0; r.u = e0 * fmaxf(l0, kNoPower);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+#pragma unroll
+    for (int q = 0; q < Part::VPL; ++q) {
+      const float l = (p.at(i, q) - b) * c, e = __builtin_amdgcn_exp2f(l);
+      r.s += e; r.u += e * fmaxf(l, kNoPower);
+    }
+    asm volatile("" : "+v"(r.s), "+v"(r.u));            // (both sums move on: the exponents of one are not kept for the other)
+  }
+  r.s = wave_sum(r.s); r.u = wave_sum(r.u);
+  if (sizeof(T) == 2) p.forget();
+  return r;
+}
+
+// a thread's groups for a list's bound: all its vectors, or a part of them where a workgroup has few threads
+template <int NT, int NV> constexpr int groups_of() { return NT >= 512 ? 1 : NT == 256 ? 2 : 4; }
+
+// forward; SPLIT: the row's parts are dealt to gridDim.x workgroups, which leave their statistics and lists
+template <typename T, int NT, int NV, bool SPLIT>
+__global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a) {
+  typedef RowPart<T, NT, NV> Part;
+  constexpr int VPL = Part::VPL, G = groups_of<NT, NV>();
+  static_assert(NV % G == 0, "whole vectors");
+  __shared__ float3 s_w[NT / 64];
+  __shared__ TopLds<NT, NT * G> top;
+  const int row = SPLIT ? blockIdx.y + blockIdx.z * 65535 : blockIdx.x + blockIdx.y * kRowsX;
+  if (row >= a.rows) return;
+  const int part = SPLIT ? blockIdx.x : 0, v0 = part * NT * NV, classes = a.classes, tid = threadIdx.x;
+  if (!token_counts(a.token, row, classes)) {
+    if (!SPLIT) leave_row<NT>(a.logprob, a.entropy, a.k, a.top_index, a.top_logprob, row);
+    return;
+  }
+  const T* const z = static_cast<const T*>(a.z) + (int64_t)row * classes;
+  const float c = kLog2e / a.temperature;
+  Part p;
+  const int head = Part::head(z);
+  p.load(z, v0, head, classes);
+  float z_token = 0.f;
+  if (!SPLIT && a.logprob && tid == 0) z_token = ld_elem(z + a.token[row]);
+  if (a.k > 0) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float m = g == 0 ? p.single : -INFINITY;
+#pragma unroll
+      for (int i = g * NV / G; i < (g + 1) * NV / G; ++i) {
+#pragma unroll
+        for (int q = 0; q < VPL; ++q) m = fmaxf(m, p.at(i, q));
+        if (i % 2) __builtin_amdgcn_sched_barrier(0);
+      }
+      top.group[g * NT + tid] = order_key(m);
+    }
+    if (sizeof(T) == 2) p.forget();
+  }
+  const RowStats r = block_join<NT>(part_stats(p, c), true, c, s_w);
+  const RowEnd end(r, a.temperature);
+  if (tid == 0) {
+    if (SPLIT) {
+      float* const st = static_cast<float*>(a.ws) + ((int64_t)row * gridDim.x + part) * 3;
+      st[0] = r.m; st[1] = r.s; st[2] = r.u;
+    } else {
+      if (a.logprob) a.logprob[row] = end.log_q(z_token);
+      if (a.entropy) a.entropy[row] = end.entropy;
+    }
+  }
+  if (a.k == 0) return;
+  const uint32_t bound = find_bound(top, a.k);
+  const float least = key_value(bound);
+  auto look = [&](float v, int col) { if (v >= least) append(top, order_key(v), col); };
+  if (p.single_col >= 0) look(p.single, p.single_col);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float m = p.at(i, 0);
+#pragma unroll
+    for (int q = 1; q < VPL; ++q) m = fmaxf(m, p.at(i, q));
+    if (m >= least) {
+      const int col = Part::col(v0, i, head);
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) look(p.at(i, q), col + q);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __syncthreads();
+  int n = top.n;
+  __syncthreads();
+  if (n > cand_max<NT>()) {
+    const int lo = v0 == 0 ? 0 : head + v0 * VPL, hi = min(classes, head + (v0 + NT * NV) * VPL);    // (with the single elements)
+    select_exact(top, [&](int64_t i) { return make_entry(order_key(ld_elem(z + lo + i)), lo + (int)i); }, hi - lo, a.k);
+    n = a.k;
+  }
+  if constexpr (SPLIT) {
+    uint64_t* const list = reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + logprob_stats_bytes(a.rows, (int)gridDim.x)) +
+                           ((int64_t)row * gridDim.x + part) * a.k;
+    place_entries(top, n, a.k, [&](int at, uint64_t e) { list[at] = e; });
+  } else {
+    place_entries(top, n, a.k, [&](int at, uint64_t e) { put_top(a.top_index, a.top_logprob, (int64_t)row * a.k + at, e, end); });
+  }
+}
+
+// a row's parts joined
+constexpr int kJoinThreads = 512;
+template <typename T>
+__global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobRows a, int parts) {
+  constexpr int NT = kJoinThreads;
+  __shared__ float3 s_w[NT / 64];
+  __shared__ TopLds<NT, NT> top;
+  const int row = blockIdx.x, tid = threadIdx.x;
+  if (!token_counts(a.token, row, a.classes)) {
+    leave_row<NT>(a.logprob, a.entropy, a.k, a.top_index, a.top_logprob, row);
+    return;
+  }
+  const float c = kLog2e / a.temperature;
+  const float* const st = static_cast<const float*>(a.ws) + (int64_t)row * parts * 3;
+  const uint64_t* const list = reinterpret_cast<const uint64_t*>(static_cast<const char*>(a.ws) + logprob_stats_bytes(a.rows, parts)) +
+                               (int64_t)row * parts * a.k;
+  const int64_t n_all = (int64_t)parts * a.k;
+  RowStats r;
+  for (int p = tid; p < parts; p += NT) r.join(st[3 * p], st[3 * p + 1], st[3 * p + 2], c);
+  if (a.k > 0) {
+    uint32_t m = 0u;
+    for (int64_t i = tid; i < n_all; i += NT) m = max(m, entry_key(list[i]));
+    top.group[tid] = m;
+  }
+  r = block_join<NT>(r, false, c, s_w);
+  const RowEnd end(r, a.temperature);
+  if (tid == 0) {
+    if (a.logprob) a.logprob[row] = end.log_q(ld_elem(static_cast<const T*>(a.z) + (int64_t)row * a.classes + a.token[row]));
+    if (a.entropy) a.entropy[row] = end.entropy;
+  }
+  if (a.k == 0) return;
+  const uint32_t bound = find_bound(top, a.k);
+  for (int64_t i = tid; i < n_all; i += NT) {
+    const uint64_t e = list[i];
+    if (entry_key(e) >= bound) append(top, entry_key(e), entry_index(e));
+  }
+  __syncthreads();
+  int n = top.n;
+  __syncthreads();
+  if (n > cand_max<NT>()) {
+    select_exact(top, [&](int64_t i) { return list[i]; }, n_all, a.k);       // (parts lie in the order of their classes)
+    n = a.k;
+  }
+  place_entries(top, n, a.k, [&](int at, uint64_t e) { put_top(a.top_index, a.top_logprob, (int64_t)row * a.k + at, e, end); });
+}
+
+// backward: SPLIT: PASS 0 leaves the parts' statistics, PASS 1 joins them (each workgroup for itself) and writes
+template <typename T, int NT, int NV, bool SPLIT, int PASS>
+__global__ __launch_bounds__(NT) void logprob_grad_kernel(LogprobRows a) {
+  typedef RowPart<T, NT, NV> Part;
+  constexpr int VPL = Part::VPL;
+  __shared__ float3 s_w[NT / 64];
+  __shared__ float s_token;
+  const int row = SPLIT ? blockIdx.y + blockIdx.z * 65535 : blockIdx.x + blockIdx.y * kRowsX;
+  if (row >= a.rows) return;
+  const int part = SPLIT ? blockIdx.x : 0, v0 = part * NT * NV, classes = a.classes, tid = threadIdx.x;
+  const T* const z = static_cast<const T*>(a.z) + (int64_t)row * classes;
+  T* const dz = static_cast<T*>(a.dz) + (int64_t)row * classes;
+  const int head = Part::head(z), c_lo = part == 0 ? 0 : head + v0 * VPL, c_hi = min(classes, head + (v0 + NT * NV) * VPL);
+  if (!token_counts(a.token, row, classes)) {
+    if (!(SPLIT && PASS == 0)) for (int q = c_lo + tid; q < c_hi; q += NT) st_elem(dz + q, 0.f);
+    return;
+  }
+  const float c = kLog2e / a.temperature;
+  Part p;
+  p.load(z, v0, head, classes);
+  const int token = a.d_logprob ? a.token[row] : -1;
+  const bool mine = token >= c_lo && token < c_hi;
+  if (mine && tid == 0) s_token = ld_elem(z + token);    // (a barrier ahead of any store: dz may be z)
+  RowStats r;
+  if constexpr (!SPLIT || PASS == 0) {
+    r = block_join<NT>(part_stats(p, c), true, c, s_w);
+    if constexpr (SPLIT) {
+      if (tid == 0) {
+        float* const st = static_cast<float*>(a.ws) + ((int64_t)row * gridDim.x + part) * 3;
+        st[0] = r.m; st[1] = r.s; st[2] = r.u;
+      }
+      return;
+    }
+  } else {
+    const float* const st = static_cast<const float*>(a.ws) + (int64_t)row * gridDim.x * 3;
+    for (int q = tid; q < (int)gridDim.x; q += NT) r.join(st[3 * q], st[3 * q + 1], st[3 * q + 2], c);
+    r = block_join<NT>(r, false, c, s_w);
+  }
+  const float b = exp_base(r.m), inv_t = 1.f / a.temperature;
+  const float ga = a.d_logprob ? a.d_logprob[row] * inv_t : 0.f, gh = a.d_entropy ? a.d_entropy[row] * inv_t : 0.f;
+  const float slope = -(gh * kLn2) / r.s, factor = (gh * kLn2 * (r.u / r.s) - ga) / r.s;
+  auto grad = [&](float v) {
+    const float l = (v - b) * c;
+    return __builtin_amdgcn_exp2f(l) * fmaf(fmaxf(l, kNoPower), slope, factor);
+  };
+  const float single = grad(p.single);
+  store_part<T, NT, NV>(dz, p, v0, head, classes, single, [&](int i, int q) { return grad(p.at(i, q)); });
+  __threadfence_block();
+  __syncthreads();                                      // the token's element is written again, after its vector
+  if (mine && tid == 0) st_elem(dz + token, grad(s_token) + ga);
+}
+
+// ------------------------------------------------------------------ after a layer's product
+// A workgroup a place: its parts' statistics joined, and of its logits (in fp32) those of the parts that may hold a listed one.
+__global__ __launch_bounds__(kJoinThreads) void logprob_finish_kernel(LogprobFinish a) {
+  constexpr int NT = kJoinThreads;
+  __shared__ float3 s_w[NT / 64];
+  __shared__ TopLds<NT, NT> top;
+  const int place = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int row = a.list[place];
+  if (place >= *a.live) {
+    leave_row<NT>(a.logprob, a.entropy, a.k, a.top_index, a.top_logprob, row);
+    return;
+  }
+  const float c = kLog2e / a.temperature;
+  const float* const z = a.z + (int64_t)place * a.z_ld;
+  // groups: parts, where there are enough of them for a tight bound, else classes
+  const bool by_part = a.parts >= 2 * a.k;
+  RowStats r;
+  float most = -INFINITY;
+  for (int p = tid; p < a.parts; p += NT) {
+    const float2 ms = *reinterpret_cast<const float2*>(a.stats + ((int64_t)p * a.stats_ld + place) * 2);
+    r.join(ms.x, ms.y, a.spread[(int64_t)p * a.stats_ld + place], c);
+    most = fmaxf(most, ms.x);
+  }
+  if (a.k > 0) {
+    if (!by_part) for (int v = tid; v < a.classes; v += NT) most = v == tid ? z[v] : fmaxf(most, z[v]);
+    if (!by_part && tid >= a.classes) most = -INFINITY;
+    top.group[tid] = order_key(most);
+  }
+  r = block_join<NT>(r, false, c, s_w);
+  const RowEnd end(r, a.temperature);
+  if (tid == 0) {
+    if (a.logprob) a.logprob[row] = end.log_q(a.target[place]);
+    if (a.entropy) a.entropy[row] = end.entropy;
+  }
+  if (a.k == 0) return;
+  const uint32_t bound = find_bound(top, a.k);
+  const float least = key_value(bound);
+  auto look = [&](int v) { if (v < a.classes && z[v] >= least) append(top, order_key(z[v]), v); };
+  if (by_part) {
+    for (int p0 = w * 64; p0 < a.parts; p0 += NT) {
+      const int p = p0 + lane;
+      uint64_t some = __ballot(p < a.parts && a.stats[((int64_t)p * a.stats_ld + place) * 2] >= least);
+      while (some) {
+        const int q = __ffsll((unsigned long long)some) - 1;
+        some &= some - 1;
+        for (int v = lane; v < a.part; v += 64) look((p0 + q) * a.part + v);
+      }
+    }
+  } else {
+    for (int v = tid; v < a.classes; v += NT) look(v);
+  }
+  __syncthreads();
+  int n = top.n;
+  __syncthreads();
+  if (n > cand_max<NT>()) {
+    select_exact(top, [&](int64_t i) { return make_entry(order_key(z[i]), (int)i); }, a.classes, a.k);
+    n = a.k;
+  }
+  place_entries(top, n, a.k, [&](int at, uint64_t e) { put_top(a.top_index, a.top_logprob, (int64_t)row * a.k + at, e, end); });
+}
+
+// ------------------------------------------------------------------ launches
+template <typename T, int NT, int NV> hipError_t rows_whole(const LogprobRows& a, hipStream_t st) {
+  const dim3 grid(a.rows < kRowsX ? a.rows : kRowsX, (a.rows + kRowsX - 1) / kRowsX);
+  if (a.dz) hipLaunchKernelGGL((logprob_grad_kernel<T, NT, NV, false, 1>), grid, dim3(NT), 0, st, a);
+  else hipLaunchKernelGGL((logprob_rows_kernel<T, NT, NV, false>), grid, dim3(NT), 0, st, a);
+  return hipGetLastError();
+}
+
+template <typename T> int64_t row_vectors(int classes) { return (int64_t)classes / (16 / (int)sizeof(T)) + 1; }   // (one for the single elements at the end)
+template <typename T> int row_parts(int classes) { return (int)((row_vectors<T>(classes) + kPartThreads * kPartVecs - 1) / (kPartThreads * kPartVecs)); }
+
+template <typename T> bool rows_in_parts(const LogprobRows& a) {
+  const int64_t vecs = row_vectors<T>(a.classes);
+  return vecs > 1024 * 16 || (vecs > 512 * 8 && a.rows <= 64);
+}
+
+template <typename T> hipError_t rows_any(const LogprobRows& a, hipStream_t st) {
+  const int64_t vecs = row_vectors<T>(a.classes);
+  if (rows_in_parts<T>(a)) {
+    const int parts = row_parts<T>(a.classes);
+    const dim3 grid((unsigned)parts, (unsigned)(a.rows < 65535 ? a.rows : 65535), (unsigned)((a.rows + 65534) / 65535));
+    if (a.dz) {
+      hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 0>), grid, dim3(kPartThreads), 0, st, a);
+      hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 1>), grid, dim3(kPartThreads), 0, st, a);
+    } else {
+      hipLaunchKernelGGL((logprob_rows_kernel<T, kPartThreads, kPartVecs, true>), grid, dim3(kPartThreads), 0, st, a);
+      hipLaunchKernelGGL(logprob_join_kernel<T>, dim3((unsigned)a.rows), dim3(kJoinThreads), 0, st, a, parts);
+    }
+    return hipGetLastError();
+  }
+  if (vecs <= 64 * 4) return rows_whole<T, 64, 4>(a, st);
+  if (vecs <= 128 * 4) return rows_whole<T, 128, 4>(a, st);
+  if (vecs <= 256 * 4) return rows_whole<T, 256, 4>(a, st);
+  if (vecs <= 256 * 8) return rows_whole<T, 256, 8>(a, st);
+  if (vecs <= 512 * 8) return rows_whole<T, 512, 8>(a, st);
+  if (vecs <= 512 * 16) return rows_whole<T, 512, 16>(a, st);
+  return rows_whole<T, 1024, 16>(a, st);
+}
+
+template <typename T> size_t rows_bytes(const LogprobRows& a) {
+  if (!rows_in_parts<T>(a)) return 0;
+  const int parts = row_parts<T>(a.classes);
+  return logprob_stats_bytes(a.rows, parts) + (a.dz ? 0 : (size_t)a.rows * parts * a.k * 8);
+}
+
+}  // namespace
+
+size_t logprob_rows_bytes(const LogprobRows& a) { return a.dtype == kBF16 ? rows_bytes<uint16_t>(a) : rows_bytes<float>(a); }
+
+hipError_t launch_logprob_rows(const LogprobRows& a, hipStream_t st) {
+  if (a.rows <= 0) return hipSuccess;
+  if (a.k < 0 || a.k > kTopMax) return hipErrorInvalidValue;
+  return a.dtype == kBF16 ? rows_any<uint16_t>(a, st) : rows_any<float>(a, st);
+}
+
+hipError_t launch_logprob_finish(const LogprobFinish& a, hipStream_t st) {
+  if (a.rows <= 0) return hipSuccess;
+  if (a.k < 0 || a.k > kTopMax || (a.k > 0 && !a.z)) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(logprob_finish_kernel, dim3((unsigned)a.rows), dim3(kJoinThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace rad

@@ -10,7 +10,7 @@
 namespace rad {
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // ------------------------------------------------------------------ the list of rows
 // One workgroup: a thread has 8 consecutive rows of 8192 at a time, and places them by a count over the threads before it.  A
@@ -21,7 +21,7 @@ __global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows
   __shared__ int s_n[16];
   __shared__ float2 s_w[16];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  auto counts = [&](int r) { return t.labels ? (uint32_t)t.labels[r] < (uint32_t)classes : t.counts[r] != 0; };
+  auto counts = [&](int r) { return t.labels ? (uint32_t)t.labels[r] < (uint32_t)classes : !t.counts || t.counts[r] != 0; };
   int total = 0;                                        // rows that count (of one block of rows: below)
   if (rows > 8192) {
     for (int r = threadIdx.x; r < rows; r += 1024) total += counts(r) ? 1 : 0;
@@ -59,25 +59,26 @@ __global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows
     before += all;
   }
   WeightRange of;
-  if (t.weight) {
-    for (int r = threadIdx.x; r < rows; r += 1024) if (counts(r)) of.add(t.weight[r]);
+  const bool weights = t.weight || t.weight2;
+  if (weights) {
+    for (int r = threadIdx.x; r < rows; r += 1024) if (counts(r)) of.add(t.weight, t.weight2, r);
     of.join_wave();
     if (lane == 0) s_w[w] = make_float2(of.most, of.least);
     __syncthreads();
     for (int q = 0; q < 16; ++q) of.join(s_w[q].x, s_w[q].y);
   }
   if (threadIdx.x == 0) {
-    const float inv = inv_count ? (total > 0 ? 1.f / (float)total : 0.f) : t.weight ? 0.f : *t.inv_count;
+    const float inv = inv_count ? (total > 0 ? 1.f / (float)total : 0.f) : weights ? 0.f : *t.inv_count;
     *live = total;
     if (inv_count) *inv_count = inv;
-    *common = t.weight ? of.common(t.temperature) : t.temperature * inv;
+    *common = weights ? of.common(t.lead) : t.lead * inv;
   }
 }
 
 // ------------------------------------------------------------------ between the products
 // What epilogue_vocab does, on partial sums: 16 lanes have 64 columns of a row, four each.  40 x 2000 of 13 splits 5.3 us,
 // the launch and two loads after one another.
-template <typename T>
+template <typename T, bool LOGPROB>
 __global__ __launch_bounds__(256) void vocab_join_kernel(GemmArgs g) {
   const HeadArgs& h = g.head;
   const int l = threadIdx.x & 15, place = (int)blockIdx.y * 16 + (threadIdx.x >> 4), live = *h.live;
@@ -104,11 +105,21 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(GemmArgs g) {
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
   const float from = m == -INFINITY ? 0.f : m;
-  float below[4];
+  float below[4], spread = 0.f;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) { below[e] = z[e] - from; s += __builtin_amdgcn_exp2f(below[e] * h.c); }
+  for (int e = 0; e < 4; ++e) {
+    below[e] = z[e] - from;
+    const float x = __builtin_amdgcn_exp2f(below[e] * h.c);
+    s += x;
+    if constexpr (LOGPROB) spread += x * fmaxf(below[e] * h.c, kNoPower);
+  }
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if constexpr (LOGPROB) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) spread += __shfl_xor(spread, o);
+    if (l == 0) h.spread[(int64_t)part * h.stats_ld + place] = spread;
+  }
   if (l == 0) *reinterpret_cast<float2*>(h.stats + ((int64_t)part * h.stats_ld + place) * 2) = make_float2(m, s);
   if (g.y) {
     T* const y = static_cast<T*>(g.y) + (int64_t)place * g.ldy + col;
@@ -119,7 +130,7 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(GemmArgs g) {
   const int row = h.row_map[place];
   int t0 = 0, t1 = 0;
   if (h.labels) t1 = 1;
-  else { t0 = h.first[(int64_t)row * h.first_ld + part]; t1 = h.first[(int64_t)row * h.first_ld + part + 1]; }
+  else if (!LOGPROB) { t0 = h.first[(int64_t)row * h.first_ld + part]; t1 = h.first[(int64_t)row * h.first_ld + part + 1]; }
   for (int t = t0; t < t1; ++t) {
     const int at = (h.labels ? h.labels[row] : h.index[(int64_t)row * h.k + t]) - col;
     if (at >= 0 && at < 4) h.target[(int64_t)place * h.k + t] = at == 0 ? z[0] : at == 1 ? z[1] : at == 2 ? z[2] : z[3];
@@ -127,8 +138,11 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(GemmArgs g) {
 }
 
 // a row's share of *common (with weights never zero)
+__device__ __forceinline__ float row_share(const float* weight, const VocabTargets& t, int row, float common) {
+  return weight[row] * t.lead / common;
+}
 __device__ __forceinline__ float row_share(const VocabTargets& t, int row, float common) {
-  return !t.weight ? 1.f : t.weight[row] * t.temperature / common;
+  return !t.weight ? 1.f : row_share(t.weight, t, row, common);
 }
 
 // (maximum, sum of exponentials from it) of two parts; one with nothing in it adds its 0, or its NaN
@@ -140,13 +154,27 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2, flo
   m = M;
 }
 
+// with the sum of 2^l l beside it (LOGPROB), whose exponents move with the maximum
+template <bool LOGPROB>
+__device__ __forceinline__ void join(float& m, float& s, float& u, float m2, float s2, float u2, float c) {
+  if constexpr (LOGPROB) {
+    if (m2 == -INFINITY) { u += s2; }                    // (0, or a NaN)
+    else if (m == -INFINITY) { u += u2; }
+    else {
+      const float M = fmaxf(m, m2), l = (m - M) * c, l2 = (m2 - M) * c;
+      u = __builtin_amdgcn_exp2f(l) * (u + s * fmaxf(l, kNoPower)) + __builtin_amdgcn_exp2f(l2) * (u2 + s2 * fmaxf(l2, kNoPower));
+    }
+  }
+  join(m, s, m2, s2, c);
+}
+
 // R = 2^shift places a workgroup, 1024 / R threads for the parts of each: the statistics of neighbouring places lie side by
 // side, so a load brings R rows' pairs of several parts.  4096 rows of 1000 parts 15 us (2.2 TB/s), of 8 parts 6, the launch and
 // its chain of loads (list, statistics, probabilities).
 constexpr int kFinishThreads = 1024, kFinishRows = 16, kFinishAhead = 4;
-template <typename T>
+template <typename T, bool LOGPROB>
 __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinish a, int shift) {
-  __shared__ float s_m[16][kFinishRows], s_s[16][kFinishRows];
+  __shared__ float s_m[16][kFinishRows], s_s[16][kFinishRows], s_u[LOGPROB ? 16 : 1][kFinishRows];
   __shared__ float3 s_t[16][kFinishRows];
   __shared__ int s_row[kFinishRows];
   const int R = 1 << shift, r = (int)threadIdx.x & (R - 1), grp = (int)threadIdx.x >> shift, groups = kFinishThreads >> shift;
@@ -158,35 +186,52 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinis
   const bool counts = place < live;
   const int row = place < a.rows ? a.list[place] : -1;
 
-  float m = -INFINITY, s = 0.f;
+  float m = -INFINITY, s = 0.f, u = 0.f;
   TargetSum sum;
   if (counts) {
     for (int p = grp; p < a.parts; p += groups * kFinishAhead) {
       float2 v[kFinishAhead];
+      float w[kFinishAhead];
 #pragma unroll
       for (int q = 0; q < kFinishAhead; ++q) {
         const int pq = p + q * groups;
         v[q] = pq < a.parts ? *reinterpret_cast<const float2*>(a.stats + ((int64_t)pq * a.stats_ld + place) * 2) : make_float2(-INFINITY, 0.f);
+        w[q] = LOGPROB && pq < a.parts ? a.spread[(int64_t)pq * a.stats_ld + place] : 0.f;
       }
 #pragma unroll
-      for (int q = 0; q < kFinishAhead; ++q) join(m, s, v[q].x, v[q].y, c);
+      for (int q = 0; q < kFinishAhead; ++q) join<LOGPROB>(m, s, u, v[q].x, v[q].y, w[q], c);
     }
-    for (int j = grp; j < t.k; j += groups) {
+    if constexpr (!LOGPROB) for (int j = grp; j < t.k; j += groups) {
       const float pj = t.labels ? 1.f : t.prob[(int64_t)row * t.k + j];
       if (pj != 0.f) sum.add(pj, a.target[(int64_t)place * t.k + j]);
     }
   }
   for (int o = R; o < 64; o <<= 1) {
-    join(m, s, __shfl_xor(m, o), __shfl_xor(s, o), c);
-    sum.join_lane(o);
+    join<LOGPROB>(m, s, u, __shfl_xor(m, o), __shfl_xor(s, o), LOGPROB ? __shfl_xor(u, o) : 0.f, c);
+    if constexpr (!LOGPROB) sum.join_lane(o);
   }
-  if (lane < R) { s_m[wave][r] = m; s_s[wave][r] = s; sum.put(&s_t[wave][r]); }
+  if (lane < R) {
+    s_m[wave][r] = m; s_s[wave][r] = s;
+    if constexpr (LOGPROB) s_u[wave][r] = u; else sum.put(&s_t[wave][r]);
+  }
   __syncthreads();
   if ((int)threadIdx.x < R) {
-    for (int w = 1; w < 16; ++w) { join(m, s, s_m[w][r], s_s[w][r], c); sum.join(s_t[w][r]); }
+    for (int w = 1; w < 16; ++w) {
+      join<LOGPROB>(m, s, u, s_m[w][r], s_s[w][r], LOGPROB ? s_u[w][r] : 0.f, c);
+      if constexpr (!LOGPROB) sum.join(s_t[w][r]);
+    }
     s_row[r] = row;
     float part = 0.f;                                   // of the batch's loss
-    if (counts) {
+    if (LOGPROB) {
+      // dz_v = (a (1[v = token] - q_v) - h q_v (log q_v + H)) / T with q_v = 2^l / s, log q_v = l ln 2 - ln s and
+      // H = ln s - ln 2 sum(2^l l) / s, so H - ln s is all that is left of both beside l
+      if (counts) {
+        const float ga = t.weight ? row_share(t.weight, t, row, *a.common) : 0.f, gh = t.weight2 ? row_share(t.weight2, t, row, *a.common) : 0.f;
+        a.top[place] = m == -INFINITY ? 0.f : m;
+        a.factor[place] = (gh * kLn2 * (u / s) - ga) / s;
+        a.slope[place] = -(gh * kLn2) / s;
+      }
+    } else if (counts) {
       const float T1 = t.temperature, top = m == -INFINITY ? 0.f : m;
       const float weight = t.weight ? t.weight[row] : *t.inv_count;
       const float loss = T1 * T1 * ((t.labels ? 0.f : t.entropy[row]) + (logf(s) + ((top - sum.from()) - sum.dot) / T1));
@@ -197,7 +242,7 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinis
     } else if (place < a.rows) {
       a.row_loss[row] = 0.f;
     }
-    if (a.loss && !a.z) *a.loss = part;                 // (of one row: vocab_loss_inside)
+    if (!LOGPROB && a.loss && !a.z) *a.loss = part;                 // (of one row: vocab_loss_inside)
   }
   __syncthreads();
   if (a.xs && live < a.rows) {
@@ -222,7 +267,7 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinis
 // 404 us (5.2 TB/s), 4096 x 32000 97, 1024 x 8003 fp32 12.  The last column of
 // workgroups (where there is a loss to sum) has no logits: its first one adds the rows' losses.
 constexpr int kGradRows = 16;
-template <typename T, int kGradSteps>
+template <typename T, int kGradSteps, bool LOGPROB>
 __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int sum_column) {
   constexpr int VPL = 16 / (int)sizeof(T), kCols = 16 * VPL * kGradSteps;
   __shared__ float s_w[4];
@@ -248,9 +293,11 @@ __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int 
   const int c0 = (int)blockIdx.x * kCols, shift = a.part == 64 ? 6 : 7;
   const bool counts = place < live;
   T* const zr = static_cast<T*>(a.z) + (int64_t)place * a.z_ld;
-  float top = 0.f, f = 0.f;
+  float top = 0.f, f = 0.f, slope = 0.f;
+  auto times = [&](float e, float l) { return LOGPROB ? e * fmaf(fmaxf(l, kNoPower), slope, f) : e * f; };
   if (counts) {
     top = a.top[place]; f = a.factor[place];
+    if constexpr (LOGPROB) slope = a.slope[place];
     u32x4 w[kGradSteps];
     float m[kGradSteps];
 #pragma unroll
@@ -271,13 +318,16 @@ __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int 
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t lo = w[q][e] & 0xFFFFu, hi = w[q][e] >> 16;
-          const float e0 = __builtin_amdgcn_exp2f(fmaf((float)lo, -kCodeRange / 65535.f, off));
-          const float e1 = __builtin_amdgcn_exp2f(fmaf((float)hi, -kCodeRange / 65535.f, off));
-          o[e] = bf16_pair((lo == kCodeLast ? 0.f : e0) * f, (hi == kCodeLast ? 0.f : e1) * f);
+          const float l0 = fmaf((float)lo, -kCodeRange / 65535.f, off), l1 = fmaf((float)hi, -kCodeRange / 65535.f, off);
+          const float e0 = __builtin_amdgcn_exp2f(l0), e1 = __builtin_amdgcn_exp2f(l1);
+          o[e] = bf16_pair(times(lo == kCodeLast ? 0.f : e0, l0), times(hi == kCodeLast ? 0.f : e1, l1));
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(__builtin_amdgcn_exp2f((__uint_as_float(w[q][e]) - top) * c) * f);
+        for (int e = 0; e < 4; ++e) {
+          const float l = (__uint_as_float(w[q][e]) - top) * c;
+          o[e] = __float_as_uint(times(__builtin_amdgcn_exp2f(l), l));
+        }
       }
       *reinterpret_cast<u32x4*>(zr + col) = o;
     }
@@ -288,16 +338,16 @@ __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int 
   const int row = a.list[place];
   int t0 = 0, t1 = 0;
   if (t.labels) t1 = (uint32_t)(t.labels[row] - c0) < (uint32_t)kCols ? 1 : 0;
-  else {
+  else if (!LOGPROB) {
     const uint16_t* const fr = a.first + (int64_t)row * a.first_ld;
     t0 = fr[c0 >> shift]; t1 = fr[min((c0 + kCols) >> shift, a.parts)];
   }
-  const float wt = row_share(t, row, *a.common);
+  const float wt = LOGPROB ? (t.weight ? -row_share(t.weight, t, row, *a.common) : 0.f) : row_share(t, row, *a.common);
   for (int j = t0 + l; j < t1; j += 16) {
     const float pj = t.labels ? 1.f : t.prob[(int64_t)row * t.k + j];
     if (pj == 0.f) continue;
     const int col = t.labels ? t.labels[row] : t.index[(int64_t)row * t.k + j];
-    const float g = __builtin_amdgcn_exp2f((a.target[(int64_t)place * t.k + j] - top) * c) * f - wt * pj;
+    const float l = (a.target[(int64_t)place * t.k + j] - top) * c, g = times(__builtin_amdgcn_exp2f(l), l) - wt * pj;
     if constexpr (sizeof(T) == 2) zr[col] = (uint16_t)bf16_pair(g, 0.f);
     else zr[col] = g;
   }
@@ -404,11 +454,12 @@ hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t
   hipLaunchKernelGGL(row_list_kernel, dim3(1), dim3(1024), 0, st, t, rows, classes, list, live, inv_count, common);
   return hipGetLastError();
 }
-hipError_t launch_vocab_join(int dtype, const GemmArgs& g, hipStream_t st) {
+hipError_t launch_vocab_join(int dtype, bool logprob, const GemmArgs& g, hipStream_t st) {
   const dim3 grid((g.N + 63) / 64, (g.M + 15) / 16);
   if (grid.y > 65535 || g.ldc % 64) return hipErrorInvalidValue;
-  if (dtype == kBF16) hipLaunchKernelGGL(vocab_join_kernel<uint16_t>, grid, dim3(256), 0, st, g);
-  else hipLaunchKernelGGL(vocab_join_kernel<float>, grid, dim3(256), 0, st, g);
+  auto kern = dtype == kBF16 ? logprob ? vocab_join_kernel<uint16_t, true> : vocab_join_kernel<uint16_t, false>
+                             : logprob ? vocab_join_kernel<float, true> : vocab_join_kernel<float, false>;
+  hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, g);
   return hipGetLastError();
 }
 // places of a finishing workgroup: up to 16, while there is a workgroup for every other CU
@@ -418,7 +469,7 @@ static int finish_shift(int rows) {
   return shift;
 }
 // 16 vectors a lane where that makes a workgroup for every other CU, 4 where it does not
-template <typename T> static hipError_t gradient_of(const VocabFinish& a, hipStream_t st) {
+template <typename T, bool LOGPROB> static hipError_t gradient_of(const VocabFinish& a, hipStream_t st) {
   const unsigned rows = (unsigned)((a.rows + kGradRows - 1) / kGradRows);
   if (rows > 65535) return hipErrorInvalidValue;
   const int64_t width = 16 * (16 / (int)sizeof(T));
@@ -426,20 +477,22 @@ template <typename T> static hipError_t gradient_of(const VocabFinish& a, hipStr
   const unsigned cols = (unsigned)((a.z_ld + (wide ? 16 : 4) * width - 1) / ((wide ? 16 : 4) * width));
   const dim3 grid(cols + (a.loss ? 1 : 0), rows);
   const int sum_column = a.loss ? (int)cols : -1;
-  if (wide) hipLaunchKernelGGL((vocab_gradient_kernel<T, 16>), grid, dim3(256), 0, st, a, sum_column);
-  else hipLaunchKernelGGL((vocab_gradient_kernel<T, 4>), grid, dim3(256), 0, st, a, sum_column);
+  if (wide) hipLaunchKernelGGL((vocab_gradient_kernel<T, 16, LOGPROB>), grid, dim3(256), 0, st, a, sum_column);
+  else hipLaunchKernelGGL((vocab_gradient_kernel<T, 4, LOGPROB>), grid, dim3(256), 0, st, a, sum_column);
   return hipGetLastError();
 }
 bool vocab_loss_inside(const VocabFinish& a) { return a.z || a.rows == 1; }
 hipError_t launch_vocab_finish(const VocabFinish& a, hipStream_t st) {
   const int shift = finish_shift(a.rows);
   const dim3 grid((a.rows + (1 << shift) - 1) >> shift);
-  if (a.dtype == kBF16) hipLaunchKernelGGL(vocab_finish_kernel<uint16_t>, grid, dim3(kFinishThreads), 0, st, a, shift);
-  else hipLaunchKernelGGL(vocab_finish_kernel<float>, grid, dim3(kFinishThreads), 0, st, a, shift);
+  auto kern = a.dtype == kBF16 ? a.spread ? vocab_finish_kernel<uint16_t, true> : vocab_finish_kernel<uint16_t, false>
+                               : a.spread ? vocab_finish_kernel<float, true> : vocab_finish_kernel<float, false>;
+  hipLaunchKernelGGL(kern, grid, dim3(kFinishThreads), 0, st, a, shift);
   return hipGetLastError();
 }
 hipError_t launch_vocab_gradient(const VocabFinish& a, hipStream_t st) {
-  return a.dtype == kBF16 ? gradient_of<uint16_t>(a, st) : gradient_of<float>(a, st);
+  if (a.spread) return a.dtype == kBF16 ? gradient_of<uint16_t, true>(a, st) : gradient_of<float, true>(a, st);
+  return a.dtype == kBF16 ? gradient_of<uint16_t, false>(a, st) : gradient_of<float, false>(a, st);
 }
 hipError_t launch_split_sum(const SplitSum& a, hipStream_t st) {
   if (a.rows > 65535 || a.in_ld % 4) return hipErrorInvalidValue;
