@@ -381,9 +381,8 @@ typedef struct {
 /* Of logits [rows, classes] in dtype that are there.  Statistics are fp32; a log
  * probability is off by some 10^-7 (|z| / T + log(classes)).  Outputs overlap
  * neither inputs nor each other; results do not vary from call to call.  Context
- * workspace where rows are few or wider than a workgroup's registers (131072
- * elements of bf16, 65536 of fp32): 12 + 8 top_k bytes per row and 8192 (4096)
- * classes.  Enqueued on the context's stream. */
+ * workspace for up to 256 long rows: 512 (12 + 8 top_k) bytes at most.  Enqueued on
+ * the context's stream. */
 rad_status rad_token_logprobs(rad_ctx* ctx, const void* logits, int64_t rows, int64_t classes, int32_t dtype,
                               const rad_logprobs* out);
 
@@ -392,7 +391,9 @@ rad_status rad_token_logprobs(rad_ctx* ctx, const void* logits, int64_t rows, in
  *   dlogits[r][v] = (1/T) (a (1[v = token[r]] - q_v) - h q_v (log q_v + entropy[r])),
  * a = d_logprob[r], h = d_entropy[r]; zeros in a row that does not count, whatever
  * its a and h.  Everything is formed from the logits again; dlogits, in dtype, may
- * be logits.  Context workspace as above, with top_k = 0. */
+ * be logits.  Context workspace where rows are few or wider than a workgroup's
+ * registers (131072 elements of bf16, 65536 of fp32): 12 bytes per row and 8192
+ * (4096) classes. */
 rad_status rad_token_logprobs_grad(rad_ctx* ctx, const void* logits, int64_t rows, int64_t classes, int32_t dtype,
                                    const int32_t* token, double temperature, const float* d_logprob,
                                    const float* d_entropy, void* dlogits);
@@ -529,7 +530,7 @@ rad_status rad_optimizer_step(rad_ctx* ctx, const rad_optimizer* opt, int64_t t,
  * read in vectors), which may come twice; norm and scale are DEVICE fp32, one of
  * them may be null.  max_norm > 0, infinity for the norm alone.  At most 2^35
  * elements in all.  Squares and sums are fp64, in a fixed order.  No tensors:
- * a norm of 0.  Context workspace: 8 KiB per 128 tensors.  Enqueued on the
+ * a norm of 0.  Context workspace: 4 KiB per 128 tensors.  Enqueued on the
  * context's stream. */
 rad_status rad_gradient_norm(rad_ctx* ctx, int32_t n_tensors, const int64_t* counts, const void* const* grads,
                              const int32_t* dtypes, double max_norm, float* norm, float* scale);

@@ -544,62 +544,75 @@ def rad_optimizer_step(ctx, opt, t, dtype, params, grads, m=None, v=None, master
                                          arr(v), arr(master)))
 
 
-def _tensors(name, tensors, like, kinds):
-    """The HOST array of addresses of tensors (None: no array) that are to be contiguous, as large as those of `like`, and of the
-    given types."""
+def _counts(tensors):
+    return [t.numel() for t in tensors]
+
+
+def _tensors(name, tensors, counts, kind):
+    """The HOST array of addresses of tensors (None: no array) that are to be contiguous, of so many elements each and of one
+    type."""
     if tensors is None:
         return None
-    if len(tensors) != len(like):
-        raise RadError(RAD_ERR_SHAPE, "%d tensors of %s, not %d" % (len(tensors), name, len(like)))
-    at = []
-    for t, other, kind in zip(tensors, like, kinds):
-        if t.dtype is not kind or t.numel() != other.numel() or not t.is_contiguous():
-            raise RadError(RAD_ERR_SHAPE, "%s holds a tensor that is not a contiguous one of %d elements of %s" % (name, other.numel(), kind))
-        at.append(t.data_ptr())
+    at = [t.data_ptr() for t, n in zip(tensors, counts) if t.dtype is kind and t.numel() == n and t.is_contiguous()]
+    if len(at) != len(counts) or len(tensors) != len(counts):
+        raise RadError(RAD_ERR_SHAPE, "%s are not %d contiguous tensors of %s elements of %s" % (name, len(counts), counts, kind))
     return (P * len(at))(*at)
 
 
+def _lists_on_device(ctx, *lists):
+    """_on_device for lists of tensors (None: none)"""
+    at = getattr(ctx, "device", None)
+    where = {t.get_device() for ts in lists if ts is not None for t in ts}
+    if where - {at} and (at is not None or len(where) > 1 or min(where) < 0):
+        _on_device(ctx, *[t for ts in lists if ts is not None for t in ts])
+
+
 def _gradients(grads):
-    """(counts, addresses, types, rad_dtypes) of a list of gradients, fp32 and bf16"""
+    """(counts, HOST arrays of counts, addresses and rad_dtypes) of a list of gradients, fp32 and bf16"""
     import torch
-    kinds = [t.dtype for t in grads]
-    for k in kinds:
-        if k is not torch.float32 and k is not torch.bfloat16:
+    counts, kinds, n = _counts(grads), {t.dtype for t in grads}, len(grads)
+    dtypes = None                                        # (all fp32)
+    if kinds - {torch.float32}:
+        if kinds - {torch.float32, torch.bfloat16}:
             raise RadError(RAD_ERR_PARAM, "gradients are fp32 or bf16")
-    n = len(grads)
-    return ((C.c_int64 * n)(*[t.numel() for t in grads]), _tensors("grads", grads, grads, kinds), kinds,
-            (C.c_int32 * n)(*[RAD_F32 if k is torch.float32 else RAD_BF16 for k in kinds]))
+        dtypes = (C.c_int32 * n)(*[RAD_F32 if t.dtype is torch.float32 else RAD_BF16 for t in grads])
+    if not all([t.is_contiguous() for t in grads]):
+        raise RadError(RAD_ERR_SHAPE, "a gradient is not contiguous")
+    return counts, (C.c_int64 * n)(*counts), (P * n)(*[t.data_ptr() for t in grads]), dtypes
 
 
 def rad_gradient_norm(ctx, grads, max_norm=float("inf"), norm=None, scale=None):
     """grads: a list of fp32 and bf16 tensors; norm and scale: fp32 tensors of one element, or None."""
     import torch
-    counts, at, _, dtypes = _gradients(grads)
+    _, counts, at, dtypes = _gradients(grads)
     args = (_arg("norm", norm, 1, torch.float32), _arg("scale", scale, 1, torch.float32))
-    _on_device(ctx, *grads, norm, scale)
+    _lists_on_device(ctx, grads, [t for t in (norm, scale) if t is not None])
     _check(ctx, lib().rad_gradient_norm(ctx, len(grads), counts, at, dtypes, max_norm, *args))
 
 
 def rad_clip_gradients(ctx, grads, max_norm, clipped=None, norm=None):
     """clipped: a list of tensors of the gradients' sizes and types; None: the gradients themselves."""
     import torch
-    counts, at, kinds, dtypes = _gradients(grads)
-    to = at if clipped is None else _tensors("clipped", clipped, grads, kinds)
+    sizes, counts, at, dtypes = _gradients(grads)
+    to = at
+    if clipped is not None:
+        if [(t.numel(), t.dtype, t.is_contiguous()) for t in clipped] != [(n, t.dtype, True) for n, t in zip(sizes, grads)]:
+            raise RadError(RAD_ERR_SHAPE, "clipped are not contiguous tensors of the gradients' sizes and types")
+        to = (P * len(grads))(*[t.data_ptr() for t in clipped])
     arg = _arg("norm", norm, 1, torch.float32)
-    _on_device(ctx, *grads, *(clipped or ()), norm)
+    _lists_on_device(ctx, grads, clipped, None if norm is None else [norm])
     _check(ctx, lib().rad_clip_gradients(ctx, len(grads), counts, at, dtypes, max_norm, to, arg))
 
 
 def rad_optimizer_step_scaled(ctx, opt, t, dtype, params, grads, scale, m=None, v=None, master=None):
     """As rad_optimizer_step; scale: an fp32 tensor of one element on the GPU."""
     import torch
-    n, f32 = len(params), torch.float32
-    fp = [f32] * n
-    kinds = fp if dtype == RAD_F32 else [torch.bfloat16] * n if dtype == RAD_BF16 else [p.dtype for p in params]
-    args = ((C.c_int64 * n)(*[p.numel() for p in params]), _tensors("params", params, params, kinds), _tensors("grads", grads, params, fp),
-            _tensors("m", m, params, fp), _tensors("v", v, params, fp), _tensors("master", master, params, fp), _arg("scale", scale, 1, f32))
-    _on_device(ctx, *params, *grads, *(m or ()), *(v or ()), *(master or ()), scale)
-    _check(ctx, lib().rad_optimizer_step_scaled(ctx, C.byref(opt), int(t), dtype, n, *args))
+    counts, f32 = _counts(params), torch.float32
+    kind = f32 if dtype == RAD_F32 else torch.bfloat16 if dtype == RAD_BF16 or not params else params[0].dtype
+    args = ((C.c_int64 * len(counts))(*counts), _tensors("params", params, counts, kind), _tensors("grads", grads, counts, f32),
+            _tensors("m", m, counts, f32), _tensors("v", v, counts, f32), _tensors("master", master, counts, f32), _arg("scale", scale, 1, f32))
+    _lists_on_device(ctx, params, grads, m, v, master, [scale])
+    _check(ctx, lib().rad_optimizer_step_scaled(ctx, opt, int(t), dtype, len(counts), *args))
 
 
 def make_pde_grid(n=32, steps=40960, D=0.25, dt=1.0 / 4096):

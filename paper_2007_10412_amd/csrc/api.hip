@@ -44,14 +44,13 @@ struct rad_ctx {
   std::vector<hipEvent_t> pool;
   // grow-only workspaces, a set for each of the two streams: what is enqueued on one never shares a buffer with what
   // runs beside it on the other
-  void* ws[2][19] = {};
-  size_t ws_bytes[2][19] = {};
+  void* ws[2][20] = {};
+  size_t ws_bytes[2][20] = {};
   float* loss_dev = nullptr;
 };
 
 enum { WS_BITMAP = 0, WS_DENSE = 1, WS_ROWLOSS = 2, WS_COLSUM = 3, WS_SPLITK = 4, WS_WT = 5, WS_PROJ_R = 6, WS_PROJ_T = 7,
-       WS_PROJ_TB = 8, WS_REINDEX = 9, WS_CONVG = 10, WS_RNNSYNC = 11, WS_TARGETS = 12, WS_LOGITS = 13, WS_LOGITGRAD = 14, WS_HEADDW = 15, WS_HEADW = 16, WS_HEADX = 17, WS_NORM = 18 };
-constexpr size_t kNormHead = 256;                        // WS_NORM: a scale, then the partial sums
+       WS_PROJ_TB = 8, WS_REINDEX = 9, WS_CONVG = 10, WS_RNNSYNC = 11, WS_TARGETS = 12, WS_LOGITS = 13, WS_LOGITGRAD = 14, WS_HEADDW = 15, WS_HEADW = 16, WS_HEADX = 17, WS_NORM = 18, WS_DONE = 19 };
 
 static const char* kNoCtx = "no context";
 
@@ -108,6 +107,15 @@ static rad_status ws_get(rad_ctx* c, int which, size_t bytes, void** out) {
     have = bytes;
   }
   *out = ws;
+  return RAD_OK;
+}
+
+// Counts of workgroups that are done, one for each thing that they share: zero before and after every call.
+enum { kDoneNorm = 256, kDoneWords = 512 };             // rows that are split, then others
+static rad_status ws_counters(rad_ctx* c, uint32_t** out) {
+  const bool fresh = !c->ws[c->on_side][WS_DONE];
+  RAD_TRY(ws_get(c, WS_DONE, kDoneWords * 4, reinterpret_cast<void**>(out)));
+  if (fresh) HIP_TRY(c, launch_fill_u32(*out, 0u, kDoneWords, c->stream));
   return RAD_OK;
 }
 
@@ -1851,6 +1859,7 @@ static rad_status check_logprob_grads(rad_ctx* c, const int32_t* token, double T
 
 static rad_status logprob_rows(rad_ctx* c, LogprobRows a) {
   RAD_TRY(ws_get(c, WS_ROWLOSS, logprob_rows_bytes(a), &a.ws));
+  if (logprob_rows_bytes(a)) RAD_TRY(ws_counters(c, &a.done));
   HIP_TRY(c, timed(c, a.dz ? "logprob_grad" : "logprob_rows", [&](const char**) { return launch_logprob_rows(a, c->stream); }));
   return RAD_OK;
 }
@@ -2098,31 +2107,33 @@ static rad_status check_gradients(rad_ctx* c, int32_t n_tensors, const int64_t* 
 }
 static int gradient_size(const int32_t* dtypes, int i) { return dtypes && dtypes[i] == RAD_BF16 ? 2 : 4; }
 
+constexpr size_t kNormHead = 256;                        // WS_NORM: a scale, then partial sums
+static rad_status norm_workspace(rad_ctx* c, int32_t n_tensors, char** ws) {
+  return ws_get(c, WS_NORM, kNormHead + ((size_t)n_tensors / kNormTensors + 1) * kNormBlocks * 8, reinterpret_cast<void**>(ws));
+}
+
 static rad_status gradient_norm(rad_ctx* c, int32_t n_tensors, const int64_t* counts, const void* const* grads, const int32_t* dtypes,
-                                double max_norm, float* norm, float* scale) {
-  double* partial = nullptr;
-  RAD_TRY(ws_get(c, WS_NORM, kNormHead + ((size_t)n_tensors / kNormTensors + 1) * kNormBlocks * 8, reinterpret_cast<void**>(&partial)));
-  partial += kNormHead / 8;
+                                double max_norm, char* ws, float* norm, float* scale) {
   NormList l;
-  int sums = 0;
-  auto launch = [&]() -> rad_status {
-    int more = 0;
-    l.partial = partial + sums;
-    HIP_TRY(c, timed(c, "square_sums", [&](const char**) { return launch_square_sums(&l, &more, c->stream); }));
-    sums += more;
-    return RAD_OK;
-  };
-  for (int i = 0; i < n_tensors;) {
+  l.partial = reinterpret_cast<double*>(ws + kNormHead);
+  l.first = 0;
+  l.max_norm = max_norm; l.norm = norm; l.scale = scale;
+  uint32_t* done = nullptr;
+  RAD_TRY(ws_counters(c, &done));
+  int i = 0;
+  do {
     std::memset(l.bf16, 0, sizeof(l.bf16));
-    for (l.n = 0; i < n_tensors && l.n < kNormTensors; ++i) {
+    for (l.n = 0; i < n_tensors && (l.n < kNormTensors || counts[i] == 0); ++i) {
       if (counts[i] == 0) continue;
       if (gradient_size(dtypes, i) == 2) l.bf16[l.n >> 5] |= 1u << (l.n & 31);
       l.g[l.n] = grads[i];
       l.count[l.n++] = counts[i];
     }
-    if (l.n > 0) RAD_TRY(launch());
-  }
-  HIP_TRY(c, timed(c, "gradient_norm", [&](const char**) { return launch_norm(partial, sums, max_norm, norm, scale, c->stream); }));
+    l.done = i == n_tensors ? done + kDoneNorm : nullptr;
+    int sums = 0;
+    HIP_TRY(c, timed(c, "square_sums", [&](const char**) { return launch_square_sums(&l, &sums, c->stream); }));
+    l.first += sums;
+  } while (i < n_tensors);
   return RAD_OK;
 }
 
@@ -2138,7 +2149,9 @@ extern "C" rad_status rad_gradient_norm(rad_ctx* c, int32_t n_tensors, const int
   add_span(&spans, scale, 1, 4, true);
   if (!tensors_apart(&spans)) return fail(c, RAD_ERR_PARAM, "an output overlaps a gradient or the other output");
   DeviceGuard guard(c->device);
-  return gradient_norm(c, n_tensors, counts, grads, dtypes, max_norm, norm, scale);
+  char* ws = nullptr;
+  RAD_TRY(norm_workspace(c, n_tensors, &ws));
+  return gradient_norm(c, n_tensors, counts, grads, dtypes, max_norm, ws, norm, scale);
 }
 
 extern "C" rad_status rad_clip_gradients(rad_ctx* c, int32_t n_tensors, const int64_t* counts, const void* const* grads,
@@ -2156,9 +2169,10 @@ extern "C" rad_status rad_clip_gradients(rad_ctx* c, int32_t n_tensors, const in
   add_span(&spans, norm, 1, 4, true);
   if (!tensors_apart(&spans)) return fail(c, RAD_ERR_PARAM, "an output overlaps another tensor");
   DeviceGuard guard(c->device);
-  float* scale = nullptr;
-  RAD_TRY(ws_get(c, WS_NORM, kNormHead + ((size_t)n_tensors / kNormTensors + 1) * kNormBlocks * 8, reinterpret_cast<void**>(&scale)));
-  RAD_TRY(gradient_norm(c, n_tensors, counts, grads, dtypes, max_norm, norm, scale));
+  char* ws = nullptr;
+  RAD_TRY(norm_workspace(c, n_tensors, &ws));
+  float* const scale = reinterpret_cast<float*>(ws);
+  RAD_TRY(gradient_norm(c, n_tensors, counts, grads, dtypes, max_norm, ws, norm, scale));
   ClipList l;
   l.scale = scale;
   for (int i = 0; i < n_tensors;) {

@@ -209,18 +209,19 @@ struct OptimList {
   int32_t chunk_end[kStepTensors];      // set by the launch
 };
 hipError_t launch_optim(bool adam, OptimList* l, hipStream_t st);
-// partial[first ..]: sums of squares, in fp64, of the elements that each workgroup takes; returns how many there are in *partials
-constexpr int kNormBlocks = 1024;       // of one launch, at most
+// partial[first ..]: sums of squares, in fp64, of the elements that each workgroup takes; square_sums_blocks of them.  The launch
+// that is given norm or scale ends with *norm = sqrt(sum of partial[0 .. first + its own)), *scale = min(1, max_norm / norm), 0 where the norm is not
+// finite; *done is zero before it and after it.
+constexpr int kNormBlocks = 512;        // of one launch, at most (each counts itself done at one address, 10 ns after the one before)
 struct NormList {
-  double* partial;
+  double* partial; int first;
+  uint32_t* done; double max_norm; float* norm; float* scale;
   int n;
   const void* g[kNormTensors]; int64_t count[kNormTensors];
   int32_t chunk_end[kNormTensors];      // set by the launch
   uint32_t bf16[kNormTensors / 32];     // bit i: tensor i is bf16, else fp32
 };
 hipError_t launch_square_sums(NormList* l, int* partials, hipStream_t st);
-// *norm = sqrt(sum of partials), *scale = min(1, max_norm / norm), 0 where the norm is not finite; either may be null
-hipError_t launch_norm(const double* partial, int partials, double max_norm, float* norm, float* scale, hipStream_t st);
 // out[i] = *scale g[i] (a scale of 0: g[i]); out[i] may be g[i]
 struct ClipList {
   const float* scale;
@@ -366,7 +367,9 @@ struct LogprobRows {
   // backward (dz not null): dz (may be z) from the gradients of a row's log q[token] and entropy (null: zeros)
   void* dz; const float* d_logprob; const float* d_entropy;
   void* ws;                     // logprob_rows_bytes of scratch
+  uint32_t* done;               // kLogprobSplitRows words, zero before and after a launch
 };
+constexpr int kLogprobSplitRows = 256;                // forward: more rows than these are not split
 size_t logprob_rows_bytes(const LogprobRows& a);
 // (three floats a part of a row, before the parts' lists)
 __host__ __device__ constexpr size_t logprob_stats_bytes(int rows, int parts) { return ((size_t)rows * parts * 12 + 255) / 256 * 256; }

@@ -11,6 +11,8 @@
 // the row (k groups then hold one such class each).  A thread's maxima are there already; one wave finds that bound of them bit by
 // bit, and the few classes that reach it (of n groups some -n ln(1 - k / n): 1.4 k where n = 2 k) are placed by counting those before them.  Rows of which too
 // many reach it (equal logits above all) are searched digit by digit, as often as it takes: the list is exact for every row.
+#include <algorithm>
+
 #include "vocab_row.hpp"
 
 namespace rad {
@@ -68,6 +70,7 @@ template <int NT, int GROUPS> __device__ __forceinline__ void append(TopLds<NT, 
 
 // after the groups' maxima are in place (a barrier): the bound, the same for the workgroup, and room for entries
 template <int NT, int GROUPS> __device__ __forceinline__ uint32_t find_bound(TopLds<NT, GROUPS>& lds, int k) {
+  if constexpr (NT == 64) __syncthreads();              // (a larger workgroup has had one)
   if (threadIdx.x < 64) {
     constexpr int R = GROUPS >= 512 ? 8 : GROUPS / 64;
     const uint32_t b = R > 4 && k <= 128 ? group_bound<GROUPS, 4>(lds.group, k) : group_bound<GROUPS, R>(lds.group, k);
@@ -134,43 +137,91 @@ template <int NT, int GROUPS, class F> __device__ __forceinline__ void select_ex
   __syncthreads();
 }
 
-// the first k of the n entries in cand (a barrier before): put(place, entry) for those that are there
+// the first k of the n entries in cand (a barrier before): put(place, entry) for those that are there.  Several neighbouring lanes
+// count for one entry, as many as the workgroup has for each.
 template <int NT, int GROUPS, class F> __device__ __forceinline__ void place_entries(const TopLds<NT, GROUPS>& lds, int n, int k, F put) {
-  for (int i = threadIdx.x; i < n; i += NT) {
-    const uint64_t e = lds.cand[i];
+  int lanes = 1;
+  while (lanes < 64 && 2 * lanes * n <= NT) lanes *= 2;
+  const int sub = (int)threadIdx.x & (lanes - 1);
+  for (int i0 = 0; i0 < n; i0 += NT / lanes) {           // (the same for all lanes: shuffles below)
+    const int i = i0 + (int)threadIdx.x / lanes;
+    const uint64_t e = i < n ? lds.cand[i] : ~0ull;
     int before = 0;
-    for (int j = 0; j < n; ++j) before += lds.cand[j] > e ? 1 : 0;
-    if (before < k) put(before, e);
+#pragma unroll 4
+    for (int j = sub; j < n; j += lanes) before += lds.cand[j] > e ? 1 : 0;
+    for (int o = 1; o < lanes; o <<= 1) before += __shfl_xor(before, o);
+    if (i < n && sub == 0 && before < k) put(before, e);
   }
   for (int i = n + (int)threadIdx.x; i < k; i += NT) put(i, 0ull);
 }
 
 // ------------------------------------------------------------------ statistics
+// Sums and maxima of a wave by moves between its lanes' rows: 6 operations of a few cycles each, where shuffles take a trip through LDS.
+template <int CTRL, int ROWS> __device__ __forceinline__ float moved(float none, float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float of_lane(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
+constexpr int kRowShr = 0x110, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
+__device__ __forceinline__ float lanes_max(float v) {
+  v = fmaxf(v, moved<kRowShr + 1, 0xf>(-INFINITY, v));
+  v = fmaxf(v, moved<kRowShr + 2, 0xf>(-INFINITY, v));
+  v = fmaxf(v, moved<kRowShr + 4, 0xf>(-INFINITY, v));
+  v = fmaxf(v, moved<kRowShr + 8, 0xf>(-INFINITY, v));
+  v = fmaxf(v, moved<kRowBcast15, 0xa>(-INFINITY, v));
+  v = fmaxf(v, moved<kRowBcast31, 0xc>(-INFINITY, v));
+  return of_lane(v, 63);
+}
+__device__ __forceinline__ float lanes_sum(float v) {
+  v += moved<kRowShr + 1, 0xf>(0.f, v);
+  v += moved<kRowShr + 2, 0xf>(0.f, v);
+  v += moved<kRowShr + 4, 0xf>(0.f, v);
+  v += moved<kRowShr + 8, 0xf>(0.f, v);
+  v += moved<kRowBcast15, 0xa>(0.f, v);
+  v += moved<kRowBcast31, 0xc>(0.f, v);
+  return of_lane(v, 63);
+}
+
 // (m, s, u) of parts of a row; one with nothing in it adds its 0, or its NaN
 struct RowStats {
   float m = -INFINITY, s = 0.f, u = 0.f;
-  __device__ __forceinline__ void join(float m2, float s2, float u2, float c) {
-    if (m2 == -INFINITY) { s += s2; u += s2; return; }
-    if (m == -INFINITY) { m = m2; s += s2; u += u2; return; }
-    const float M = fmaxf(m, m2), l = (m - M) * c, l2 = (m2 - M) * c;
-    const float f = __builtin_amdgcn_exp2f(l), f2 = __builtin_amdgcn_exp2f(l2);
-    u = f * (u + s * fmaxf(l, kNoPower)) + f2 * (u2 + s2 * fmaxf(l2, kNoPower));
-    s = f * s + f2 * s2;
+  // as they are from another maximum: M >= m, neither it nor c infinite
+  __device__ __forceinline__ void rebase(float M, float c) {
+    if (m == -INFINITY) { u += s; m = M; return; }
+    const float l = (m - M) * c, f = __builtin_amdgcn_exp2f(l);
+    u = f * (u + s * fmaxf(l, kNoPower));
+    s *= f;
     m = M;
   }
+  __device__ __forceinline__ void join(float m2, float s2, float u2, float c) {
+    RowStats o;
+    o.m = m2; o.s = s2; o.u = u2;
+    const float M = fmaxf(m, m2);
+    rebase(M, c); o.rebase(M, c);
+    s += o.s; u += o.u;
+  }
   __device__ __forceinline__ void join_wave(float c) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) join(__shfl_xor(m, o), __shfl_xor(s, o), __shfl_xor(u, o), c);
+    rebase(lanes_max(m), c);
+    s = lanes_sum(s); u = lanes_sum(u);
   }
 };
 // a workgroup's, the same for all of its threads; s_w: a triple a wave
 template <int NT> __device__ __forceinline__ RowStats block_join(RowStats r, bool wave_joined, float c, float3* s_w) {
+  constexpr int NW = NT / 64;
   if (!wave_joined) r.join_wave(c);
+  if constexpr (NW == 1) return r;
   if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = make_float3(r.m, r.s, r.u);
   __syncthreads();
-  RowStats all;
+  RowStats all, of[NW];
 #pragma unroll
-  for (int w = 0; w < NT / 64; ++w) all.join(s_w[w].x, s_w[w].y, s_w[w].z, c);
+  for (int w = 0; w < NW; ++w) {
+    of[w].m = s_w[w].x; of[w].s = s_w[w].y; of[w].u = s_w[w].z;
+    all.m = fmaxf(all.m, of[w].m);
+  }
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    of[w].rebase(all.m, c);
+    all.s += of[w].s; all.u += of[w].u;
+  }
   return all;
 }
 
@@ -216,7 +267,7 @@ template <typename T, int NT, int NV> __device__ __forceinline__ RowStats part_s
     for (int q = 0; q < Part::VPL; ++q) r.m = fmaxf(r.m, p.at(i, q));
     if (i % 2) __builtin_amdgcn_sched_barrier(0);
   }
-  r.m = wave_max(r.m);
+  r.m = lanes_max(r.m);
   if (sizeof(T) == 2) p.forget();
   const float b = exp_base(r.m), l0 = (p.single - b) * c, e0 = __builtin_amdgcn_exp2f(l0);
   r.s = e0; r.u = e0 * fmaxf(l0, kNoPower);
@@ -229,139 +280,237 @@ template <typename T, int NT, int NV> __device__ __forceinline__ RowStats part_s
     }
     asm volatile("" : "+v"(r.s), "+v"(r.u));            // (both sums move on: the exponents of one are not kept for the other)
   }
-  r.s = wave_sum(r.s); r.u = wave_sum(r.u);
+  r.s = lanes_sum(r.s); r.u = lanes_sum(r.u);
   if (sizeof(T) == 2) p.forget();
   return r;
 }
 
-// a thread's groups for a list's bound: all its vectors, or a part of them where a workgroup has few threads
-template <int NT, int NV> constexpr int groups_of() { return NT >= 512 ? 1 : NT == 256 ? 2 : 4; }
+// Forward.  A row is read once and not kept: each thread runs over its vectors with a maximum and sums of its own, whose base
+// moves up when a larger logit comes (l = z c - m c is one operation so, with m c rounded once for all and what that rounding
+// moved put right at the end), and reads those of its vectors again, from a cache, of which a logit may be on the list.
+// Bases lie within +-2^24 T ln 2, where m c is rounded by one power of two at most; rows whose largest logit does not, and such as hold
+// infinities or NaN, are done again, maximum first, by slow_stats.
+constexpr float kFar = 0x1p24f;
+constexpr int kAhead = 4;                               // vectors in flight
+template <int NT> constexpr int groups_of() { return NT >= 512 ? 1 : NT == 256 ? 2 : 4; }   // a thread's, for a list's bound
 
-// forward; SPLIT: the row's parts are dealt to gridDim.x workgroups, which leave their statistics and lists
-template <typename T, int NT, int NV, bool SPLIT>
-__global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a) {
-  typedef RowPart<T, NT, NV> Part;
-  constexpr int VPL = Part::VPL, G = groups_of<NT, NV>();
-  static_assert(NV % G == 0, "whole vectors");
+__device__ __forceinline__ bool plain_stats(const RowStats& r, float c) { return r.s > 0.5f && r.s < INFINITY && r.m * c <= kFar; }
+
+template <typename T, int NT> __device__ __noinline__ RowStats slow_stats(const T* z, int lo, int hi, float c, float3* s_w) {
+  RowStats r;
+  for (int v = lo + (int)threadIdx.x; v < hi; v += NT) r.m = fmaxf(r.m, ld_elem(z + v));
+  __syncthreads();
+  r = block_join<NT>(r, false, c, s_w);
+  const float b = exp_base(r.m);
+  r.s = r.u = 0.f;
+  for (int v = lo + (int)threadIdx.x; v < hi; v += NT) {
+    const float l = (ld_elem(z + v) - b) * c, e = __builtin_amdgcn_exp2f(l);
+    r.s += e; r.u += e * fmaxf(l, kNoPower);
+  }
+  __syncthreads();
+  return block_join<NT>(r, false, c, s_w);              // (all from one maximum)
+}
+
+template <typename T> struct Stream {
+  static constexpr int VPL = 16 / (int)sizeof(T);
+  static constexpr uint32_t kEmpty = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;     // -inf
+  static __device__ __forceinline__ float at(const u32x4& v, int q) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(v[q]);
+    else return __uint_as_float(q & 1 ? v[q >> 1] & 0xFFFF0000u : v[q >> 1] << 16);
+  }
+  static __device__ __forceinline__ float most(const u32x4& v) {
+    float m = at(v, 0);
+#pragma unroll
+    for (int q = 1; q < VPL; ++q) m = fmaxf(m, at(v, q));
+    return m;
+  }
+};
+__device__ __forceinline__ float rounded_product(float m, float c) {   // (the same everywhere: never part of a fused operation)
+#pragma clang fp contract(off)
+  return m * c;
+}
+
+// a row's parts joined, by the last of its workgroups to be done
+template <int NT, int GROUPS>
+__device__ __forceinline__ void join_parts(const LogprobRows& a, int row, int parts, float z_token, TopLds<NT, GROUPS>& top, float3* s_w) {
+  constexpr int kKept = 4;                               // entries of a thread that wait in registers
+  const float c = kLog2e / a.temperature;
+  const float* const st = static_cast<const float*>(a.ws) + (int64_t)row * parts * 3;
+  const uint64_t* const list = reinterpret_cast<const uint64_t*>(static_cast<const char*>(a.ws) + logprob_stats_bytes(a.rows, parts)) +
+                               (int64_t)row * parts * a.k;
+  const int n_all = parts * a.k, tid = threadIdx.x;
+  uint64_t kept[kKept];
+#pragma unroll
+  for (int q = 0; q < kKept; ++q) { const int i = tid + q * NT; kept[q] = i < n_all ? load_of_all(list + i) : 0ull; }
+  RowStats r;
+  for (int p = tid; p < parts; p += NT) r.join(load_of_all(st + 3 * p), load_of_all(st + 3 * p + 1), load_of_all(st + 3 * p + 2), c);
+  if (a.k > 0) {
+#pragma unroll
+    for (int g = 0; g < GROUPS / NT; ++g) {              // (entry i belongs to group i mod GROUPS)
+      uint32_t m = 0u;
+#pragma unroll
+      for (int q = g; q < kKept; q += GROUPS / NT) m = max(m, entry_key(kept[q]));
+      for (int i = tid + g * NT + (kKept + GROUPS / NT - 1) / (GROUPS / NT) * GROUPS; i < n_all; i += GROUPS) m = max(m, entry_key(load_of_all(list + i)));
+      top.group[g * NT + tid] = m;
+    }
+  }
+  r = block_join<NT>(r, false, c, s_w);
+  const RowEnd end(r, a.temperature);
+  if (tid == 0) {
+    if (a.logprob) a.logprob[row] = end.log_q(z_token);
+    if (a.entropy) a.entropy[row] = end.entropy;
+  }
+  if (a.k == 0) return;
+  const uint32_t bound = find_bound(top, a.k);
+  auto look = [&](uint64_t e) { if (entry_key(e) >= bound) append(top, entry_key(e), entry_index(e)); };
+#pragma unroll
+  for (int q = 0; q < kKept; ++q) look(kept[q]);
+  for (int i = tid + kKept * NT; i < n_all; i += NT) look(load_of_all(list + i));
+  __syncthreads();
+  int n = top.n;
+  __syncthreads();
+  if (n > cand_max<NT>()) {
+    select_exact(top, [&](int64_t i) { return load_of_all(list + i); }, n_all, a.k);       // (parts lie in the order of their classes)
+    n = a.k;
+  }
+  place_entries(top, n, a.k, [&](int at, uint64_t e) { put_top(a.top_index, a.top_logprob, (int64_t)row * a.k + at, e, end); });
+}
+
+// SPLIT: the row's vectors are dealt to gridDim.x workgroups, part_vecs each; the last one to be done joins what all have left
+// ONE: kAhead vectors a thread are all, and stay in registers
+template <typename T, int NT, bool SPLIT, bool ONE>
+__global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a, int part_vecs) {
+  typedef Stream<T> S;
+  constexpr int VPL = S::VPL, G = groups_of<NT>();
   __shared__ float3 s_w[NT / 64];
   __shared__ TopLds<NT, NT * G> top;
-  const int row = SPLIT ? blockIdx.y + blockIdx.z * 65535 : blockIdx.x + blockIdx.y * kRowsX;
+  __shared__ bool s_last;
+  const int row = SPLIT ? blockIdx.y : blockIdx.x + blockIdx.y * kRowsX;
   if (row >= a.rows) return;
-  const int part = SPLIT ? blockIdx.x : 0, v0 = part * NT * NV, classes = a.classes, tid = threadIdx.x;
+  const int part = SPLIT ? blockIdx.x : 0, classes = a.classes, tid = threadIdx.x;
   if (!token_counts(a.token, row, classes)) {
-    if (!SPLIT) leave_row<NT>(a.logprob, a.entropy, a.k, a.top_index, a.top_logprob, row);
+    if (part == 0) leave_row<NT>(a.logprob, a.entropy, a.k, a.top_index, a.top_logprob, row);
     return;
   }
   const T* const z = static_cast<const T*>(a.z) + (int64_t)row * classes;
   const float c = kLog2e / a.temperature;
-  Part p;
-  const int head = Part::head(z);
-  p.load(z, v0, head, classes);
+  const int head = min(classes, RowPart<T, 64, 1>::head(z)), whole = (classes - head) / VPL;      // whole vectors from `head` on
+  const int v_lo = SPLIT ? min(part * part_vecs, whole) : 0, v_hi = SPLIT ? min(v_lo + part_vecs, whole) : whole;
+  const bool first = part == 0, last = !SPLIT || part == (int)gridDim.x - 1;
+  const T* const zv = z + head;
+  // the elements before the first vector and behind the last one: one of each to a thread
+  int single_col = -1;
+  if (first && tid < head) single_col = tid;
+  else if (last && tid >= VPL && tid < 2 * VPL && head + whole * VPL + tid - VPL < classes) single_col = head + whole * VPL + tid - VPL;
   float z_token = 0.f;
-  if (!SPLIT && a.logprob && tid == 0) z_token = ld_elem(z + a.token[row]);
+  if (a.logprob && tid == 0) z_token = ld_elem(z + a.token[row]);
+  const float single = single_col >= 0 ? ld_elem(z + single_col) : -INFINITY;
+
+  float g[G];
+#pragma unroll
+  for (int q = 0; q < G; ++q) g[q] = -INFINITY;
+  g[0] = single;
+  const float lowest = -kFar / c;
+  float m = fmaxf(single, lowest), mc = rounded_product(m, c);
+  const float l0 = fmaf(single, c, -mc), e0 = __builtin_amdgcn_exp2f(l0);
+  float s = e0, u = e0 * fmaxf(l0, kNoPower);
+  u32x4 raw[kAhead];
+  auto load = [&](int v0) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      raw[i] = u32x4{S::kEmpty, S::kEmpty, S::kEmpty, S::kEmpty};
+      if (v0 + i * NT < v_hi) raw[i] = *reinterpret_cast<const u32x4*>(zv + (int64_t)(v0 + i * NT) * VPL);
+    }
+  };
+  for (int v0 = v_lo + tid; ONE ? v0 == v_lo + tid : v0 < v_hi; v0 += NT * kAhead) {
+    load(v0);
+    float most = m;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const float mi = S::most(raw[i]);
+      g[i % G] = fmaxf(g[i % G], mi);
+      most = fmaxf(most, mi);
+    }
+    if (most > m) {
+      const float mc2 = rounded_product(most, c), d = mc - mc2, f = __builtin_amdgcn_exp2f(d);
+      u = f * (u + s * fmaxf(d, kNoPower));
+      s *= f;
+      m = most; mc = mc2;
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) {
+        const float l = fmaf(S::at(raw[i], q), c, -mc), e = __builtin_amdgcn_exp2f(l);
+        s += e; u = fmaf(e, fmaxf(l, kNoPower), u);
+      }
+      asm volatile("" : "+v"(s), "+v"(u));              // (both sums move on: the exponents of one are not kept for the other)
+    }
+  }
+  RowStats r;
+  {
+    const float moved = fmaf(m, c, -mc), f = __builtin_amdgcn_exp2f(-moved);
+    r.m = m; r.s = f * s; r.u = f * (u - moved * s);
+  }
+  float most = g[0];
+#pragma unroll
+  for (int q = 1; q < G; ++q) most = fmaxf(most, g[q]);
   if (a.k > 0) {
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      float m = g == 0 ? p.single : -INFINITY;
-#pragma unroll
-      for (int i = g * NV / G; i < (g + 1) * NV / G; ++i) {
-#pragma unroll
-        for (int q = 0; q < VPL; ++q) m = fmaxf(m, p.at(i, q));
-        if (i % 2) __builtin_amdgcn_sched_barrier(0);
-      }
-      top.group[g * NT + tid] = order_key(m);
-    }
-    if (sizeof(T) == 2) p.forget();
+    for (int q = 0; q < G; ++q) top.group[q * NT + tid] = order_key(g[q]);
   }
-  const RowStats r = block_join<NT>(part_stats(p, c), true, c, s_w);
+  r = block_join<NT>(r, false, c, s_w);
+  const int c_lo = first ? 0 : head + v_lo * VPL, c_hi = last ? classes : head + v_hi * VPL;
+  if (!plain_stats(r, c)) r = slow_stats<T, NT>(z, c_lo, c_hi, c, s_w);
   const RowEnd end(r, a.temperature);
   if (tid == 0) {
     if (SPLIT) {
       float* const st = static_cast<float*>(a.ws) + ((int64_t)row * gridDim.x + part) * 3;
-      st[0] = r.m; st[1] = r.s; st[2] = r.u;
+      store_for_all(st, r.m); store_for_all(st + 1, r.s); store_for_all(st + 2, r.u);
     } else {
       if (a.logprob) a.logprob[row] = end.log_q(z_token);
       if (a.entropy) a.entropy[row] = end.entropy;
     }
   }
-  if (a.k == 0) return;
-  const uint32_t bound = find_bound(top, a.k);
-  const float least = key_value(bound);
-  auto look = [&](float v, int col) { if (v >= least) append(top, order_key(v), col); };
-  if (p.single_col >= 0) look(p.single, p.single_col);
+  if (a.k > 0) {
+    const float least = key_value(find_bound(top, a.k));
+    auto look = [&](float v, int col) { if (v >= least) append(top, order_key(v), col); };
+    if (most >= least) {
+      if (single_col >= 0) look(single, single_col);
+      for (int v0 = v_lo + tid; ONE ? v0 == v_lo + tid : v0 < v_hi; v0 += NT * kAhead) {
+        if (!ONE) load(v0);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    float m = p.at(i, 0);
+        for (int i = 0; i < kAhead; ++i)
+          if (S::most(raw[i]) >= least) {
 #pragma unroll
-    for (int q = 1; q < VPL; ++q) m = fmaxf(m, p.at(i, q));
-    if (m >= least) {
-      const int col = Part::col(v0, i, head);
-#pragma unroll
-      for (int q = 0; q < VPL; ++q) look(p.at(i, q), col + q);
+            for (int q = 0; q < VPL; ++q) look(S::at(raw[i], q), head + (v0 + i * NT) * VPL + q);
+          }
+      }
     }
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  __syncthreads();
-  int n = top.n;
-  __syncthreads();
-  if (n > cand_max<NT>()) {
-    const int lo = v0 == 0 ? 0 : head + v0 * VPL, hi = min(classes, head + (v0 + NT * NV) * VPL);    // (with the single elements)
-    select_exact(top, [&](int64_t i) { return make_entry(order_key(ld_elem(z + lo + i)), lo + (int)i); }, hi - lo, a.k);
-    n = a.k;
+    __syncthreads();
+    int n = top.n;
+    __syncthreads();
+    if (n > cand_max<NT>()) {
+      select_exact(top, [&](int64_t i) { return make_entry(order_key(ld_elem(z + c_lo + i)), c_lo + (int)i); }, c_hi - c_lo, a.k);
+      n = a.k;
+    }
+    if constexpr (SPLIT) {
+      uint64_t* const list = reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + logprob_stats_bytes(a.rows, (int)gridDim.x)) +
+                             ((int64_t)row * gridDim.x + part) * a.k;
+      place_entries(top, n, a.k, [&](int at, uint64_t e) { store_for_all(list + at, e); });
+    } else {
+      place_entries(top, n, a.k, [&](int at, uint64_t e) { put_top(a.top_index, a.top_logprob, (int64_t)row * a.k + at, e, end); });
+    }
   }
   if constexpr (SPLIT) {
-    uint64_t* const list = reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + logprob_stats_bytes(a.rows, (int)gridDim.x)) +
-                           ((int64_t)row * gridDim.x + part) * a.k;
-    place_entries(top, n, a.k, [&](int at, uint64_t e) { list[at] = e; });
-  } else {
-    place_entries(top, n, a.k, [&](int at, uint64_t e) { put_top(a.top_index, a.top_logprob, (int64_t)row * a.k + at, e, end); });
+    stores_done();
+    __syncthreads();
+    if (tid == 0) s_last = count_done(a.done + row) == gridDim.x - 1;
+    __syncthreads();
+    if (!s_last) return;
+    if (tid == 0) a.done[row] = 0u;
+    join_parts(a, row, (int)gridDim.x, z_token, top, s_w);
   }
-}
-
-// a row's parts joined
-constexpr int kJoinThreads = 512;
-template <typename T>
-__global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobRows a, int parts) {
-  constexpr int NT = kJoinThreads;
-  __shared__ float3 s_w[NT / 64];
-  __shared__ TopLds<NT, NT> top;
-  const int row = blockIdx.x, tid = threadIdx.x;
-  if (!token_counts(a.token, row, a.classes)) {
-    leave_row<NT>(a.logprob, a.entropy, a.k, a.top_index, a.top_logprob, row);
-    return;
-  }
-  const float c = kLog2e / a.temperature;
-  const float* const st = static_cast<const float*>(a.ws) + (int64_t)row * parts * 3;
-  const uint64_t* const list = reinterpret_cast<const uint64_t*>(static_cast<const char*>(a.ws) + logprob_stats_bytes(a.rows, parts)) +
-                               (int64_t)row * parts * a.k;
-  const int64_t n_all = (int64_t)parts * a.k;
-  RowStats r;
-  for (int p = tid; p < parts; p += NT) r.join(st[3 * p], st[3 * p + 1], st[3 * p + 2], c);
-  if (a.k > 0) {
-    uint32_t m = 0u;
-    for (int64_t i = tid; i < n_all; i += NT) m = max(m, entry_key(list[i]));
-    top.group[tid] = m;
-  }
-  r = block_join<NT>(r, false, c, s_w);
-  const RowEnd end(r, a.temperature);
-  if (tid == 0) {
-    if (a.logprob) a.logprob[row] = end.log_q(ld_elem(static_cast<const T*>(a.z) + (int64_t)row * a.classes + a.token[row]));
-    if (a.entropy) a.entropy[row] = end.entropy;
-  }
-  if (a.k == 0) return;
-  const uint32_t bound = find_bound(top, a.k);
-  for (int64_t i = tid; i < n_all; i += NT) {
-    const uint64_t e = list[i];
-    if (entry_key(e) >= bound) append(top, entry_key(e), entry_index(e));
-  }
-  __syncthreads();
-  int n = top.n;
-  __syncthreads();
-  if (n > cand_max<NT>()) {
-    select_exact(top, [&](int64_t i) { return list[i]; }, n_all, a.k);       // (parts lie in the order of their classes)
-    n = a.k;
-  }
-  place_entries(top, n, a.k, [&](int at, uint64_t e) { put_top(a.top_index, a.top_logprob, (int64_t)row * a.k + at, e, end); });
 }
 
 // backward: SPLIT: PASS 0 leaves the parts' statistics, PASS 1 joins them (each workgroup for itself) and writes
@@ -417,6 +566,7 @@ __global__ __launch_bounds__(NT) void logprob_grad_kernel(LogprobRows a) {
 }
 
 // ------------------------------------------------------------------ after a layer's product
+constexpr int kJoinThreads = 512;
 // A workgroup a place: its parts' statistics joined, and of its logits (in fp32) those of the parts that may hold a listed one.
 __global__ __launch_bounds__(kJoinThreads) void logprob_finish_kernel(LogprobFinish a) {
   constexpr int NT = kJoinThreads;
@@ -478,47 +628,67 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_finish_kernel(LogprobFin
 }
 
 // ------------------------------------------------------------------ launches
-template <typename T, int NT, int NV> hipError_t rows_whole(const LogprobRows& a, hipStream_t st) {
+template <typename T> int64_t row_vectors(int classes) { return (int64_t)classes / (16 / (int)sizeof(T)) + 1; }   // (one for the single elements at the end)
+
+// forward: workgroups that a row is dealt to
+template <typename T> int forward_parts(const LogprobRows& a) {
+  const int64_t vecs = row_vectors<T>(a.classes);
+  if (a.rows > kLogprobSplitRows || vecs < 2 * 256 * kAhead) return 1;
+  return (int)std::min<int64_t>(std::max<int64_t>(1, 512 / a.rows), (vecs + 256 * kAhead - 1) / (256 * kAhead));
+}
+template <typename T, int NT> hipError_t forward_whole(const LogprobRows& a, hipStream_t st) {
   const dim3 grid(a.rows < kRowsX ? a.rows : kRowsX, (a.rows + kRowsX - 1) / kRowsX);
-  if (a.dz) hipLaunchKernelGGL((logprob_grad_kernel<T, NT, NV, false, 1>), grid, dim3(NT), 0, st, a);
-  else hipLaunchKernelGGL((logprob_rows_kernel<T, NT, NV, false>), grid, dim3(NT), 0, st, a);
+  if (row_vectors<T>(a.classes) <= NT * kAhead) hipLaunchKernelGGL((logprob_rows_kernel<T, NT, false, true>), grid, dim3(NT), 0, st, a, 0);
+  else hipLaunchKernelGGL((logprob_rows_kernel<T, NT, false, false>), grid, dim3(NT), 0, st, a, 0);
   return hipGetLastError();
 }
-
-template <typename T> int64_t row_vectors(int classes) { return (int64_t)classes / (16 / (int)sizeof(T)) + 1; }   // (one for the single elements at the end)
-template <typename T> int row_parts(int classes) { return (int)((row_vectors<T>(classes) + kPartThreads * kPartVecs - 1) / (kPartThreads * kPartVecs)); }
-
-template <typename T> bool rows_in_parts(const LogprobRows& a) {
+template <typename T> hipError_t forward(const LogprobRows& a, hipStream_t st) {
   const int64_t vecs = row_vectors<T>(a.classes);
-  return vecs > 1024 * 16 || (vecs > 512 * 8 && a.rows <= 64);
-}
-
-template <typename T> hipError_t rows_any(const LogprobRows& a, hipStream_t st) {
-  const int64_t vecs = row_vectors<T>(a.classes);
-  if (rows_in_parts<T>(a)) {
-    const int parts = row_parts<T>(a.classes);
-    const dim3 grid((unsigned)parts, (unsigned)(a.rows < 65535 ? a.rows : 65535), (unsigned)((a.rows + 65534) / 65535));
-    if (a.dz) {
-      hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 0>), grid, dim3(kPartThreads), 0, st, a);
-      hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 1>), grid, dim3(kPartThreads), 0, st, a);
-    } else {
-      hipLaunchKernelGGL((logprob_rows_kernel<T, kPartThreads, kPartVecs, true>), grid, dim3(kPartThreads), 0, st, a);
-      hipLaunchKernelGGL(logprob_join_kernel<T>, dim3((unsigned)a.rows), dim3(kJoinThreads), 0, st, a, parts);
-    }
+  const int parts = forward_parts<T>(a);
+  if (parts > 1) {
+    const int part_vecs = (int)((vecs + parts - 1) / parts);
+    auto kern = part_vecs <= 256 * kAhead ? logprob_rows_kernel<T, 256, true, true> : logprob_rows_kernel<T, 256, true, false>;
+    hipLaunchKernelGGL(kern, dim3(parts, a.rows), dim3(256), 0, st, a, part_vecs);
     return hipGetLastError();
   }
-  if (vecs <= 64 * 4) return rows_whole<T, 64, 4>(a, st);
-  if (vecs <= 128 * 4) return rows_whole<T, 128, 4>(a, st);
-  if (vecs <= 256 * 4) return rows_whole<T, 256, 4>(a, st);
-  if (vecs <= 256 * 8) return rows_whole<T, 256, 8>(a, st);
-  if (vecs <= 512 * 8) return rows_whole<T, 512, 8>(a, st);
-  if (vecs <= 512 * 16) return rows_whole<T, 512, 16>(a, st);
-  return rows_whole<T, 1024, 16>(a, st);
+  if (vecs <= 64 * kAhead && a.k <= 128) return forward_whole<T, 64>(a, st);
+  if (vecs <= 2 * 128 * kAhead) return forward_whole<T, 128>(a, st);
+  if (vecs <= 32 * 256) return forward_whole<T, 256>(a, st);
+  return forward_whole<T, 512>(a, st);
+}
+
+// backward
+template <typename T, int NT, int NV> hipError_t backward_whole(const LogprobRows& a, hipStream_t st) {
+  const dim3 grid(a.rows < kRowsX ? a.rows : kRowsX, (a.rows + kRowsX - 1) / kRowsX);
+  hipLaunchKernelGGL((logprob_grad_kernel<T, NT, NV, false, 1>), grid, dim3(NT), 0, st, a);
+  return hipGetLastError();
+}
+template <typename T> int backward_parts(const LogprobRows& a) {
+  const int64_t vecs = row_vectors<T>(a.classes);
+  if (!(vecs > 1024 * 16 || (vecs > 512 * 8 && a.rows <= 64))) return 1;
+  return (int)((vecs + kPartThreads * kPartVecs - 1) / (kPartThreads * kPartVecs));
+}
+template <typename T> hipError_t backward(const LogprobRows& a, hipStream_t st) {
+  const int64_t vecs = row_vectors<T>(a.classes);
+  const int parts = backward_parts<T>(a);
+  if (parts > 1) {
+    const dim3 grid((unsigned)parts, (unsigned)(a.rows < 65535 ? a.rows : 65535), (unsigned)((a.rows + 65534) / 65535));
+    hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 0>), grid, dim3(kPartThreads), 0, st, a);
+    hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 1>), grid, dim3(kPartThreads), 0, st, a);
+    return hipGetLastError();
+  }
+  if (vecs <= 64 * 4) return backward_whole<T, 64, 4>(a, st);
+  if (vecs <= 128 * 4) return backward_whole<T, 128, 4>(a, st);
+  if (vecs <= 256 * 4) return backward_whole<T, 256, 4>(a, st);
+  if (vecs <= 256 * 8) return backward_whole<T, 256, 8>(a, st);
+  if (vecs <= 512 * 8) return backward_whole<T, 512, 8>(a, st);
+  if (vecs <= 512 * 16) return backward_whole<T, 512, 16>(a, st);
+  return backward_whole<T, 1024, 16>(a, st);
 }
 
 template <typename T> size_t rows_bytes(const LogprobRows& a) {
-  if (!rows_in_parts<T>(a)) return 0;
-  const int parts = row_parts<T>(a.classes);
+  const int parts = a.dz ? backward_parts<T>(a) : forward_parts<T>(a);
+  if (parts <= 1) return 0;
   return logprob_stats_bytes(a.rows, parts) + (a.dz ? 0 : (size_t)a.rows * parts * a.k * 8);
 }
 
@@ -529,7 +699,8 @@ size_t logprob_rows_bytes(const LogprobRows& a) { return a.dtype == kBF16 ? rows
 hipError_t launch_logprob_rows(const LogprobRows& a, hipStream_t st) {
   if (a.rows <= 0) return hipSuccess;
   if (a.k < 0 || a.k > kTopMax) return hipErrorInvalidValue;
-  return a.dtype == kBF16 ? rows_any<uint16_t>(a, st) : rows_any<float>(a, st);
+  if (a.dz) return a.dtype == kBF16 ? backward<uint16_t>(a, st) : backward<float>(a, st);
+  return a.dtype == kBF16 ? forward<uint16_t>(a, st) : forward<float>(a, st);
 }
 
 hipError_t launch_logprob_finish(const LogprobFinish& a, hipStream_t st) {

@@ -17,20 +17,24 @@ __device__ __forceinline__ uint16_t to_bf16(float f) {      // round to nearest 
   return (uint16_t)(u >> 16);
 }
 
-template <bool ADAM>
+// (Which product of a moment's sum is rounded ahead of it differs between whole vectors and single elements, and is spelled out: a
+// parameter gets the same bits in every build.)
+template <bool ADAM, bool VECTOR>
 __device__ __forceinline__ float update_one(float w, float g, float& m, float& v, const OptimArgs& a) {
-  g += a.l2 * w;
+#pragma clang fp contract(off)
+  g = fmaf(a.l2, w, g);
   if constexpr (ADAM) {
-    m = a.beta1 * m + a.omb1 * g;
-    v = a.beta2 * v + a.omb2 * g * g;
+    m = VECTOR ? fmaf(a.omb1, g, a.beta1 * m) : fmaf(a.beta1, m, a.omb1 * g);
+    v = VECTOR ? fmaf(g, a.omb2 * g, a.beta2 * v) : fmaf(a.beta2, v, g * (a.omb2 * g));
     const float m_hat = m * a.inv_bc1, v_hat = v * a.inv_bc2;
     return w - a.lr * m_hat / (sqrtf(v_hat) + a.eps);
   } else {
-    return w - a.lr * g;
+    return fmaf(-a.lr, g, w);
   }
 }
 
-constexpr int kChunk = 4096;                            // elements: 16 KB of fp32, four 16-byte vectors a lane
+constexpr int kChunk = 4096;                            // elements: 16 KB of fp32, four 16-byte vectors a lane of 256
+constexpr int kNormThreads = 1024, kNormChunk = 16384;
 
 // the tensor that chunk c lies in
 __device__ __forceinline__ int tensor_of(const int32_t* chunk_end, int n, int c) {
@@ -73,7 +77,7 @@ __global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float me = mv[e], ve = vv[e];
-        wv[e] = update_one<ADAM>(wv[e], grad(gv[e]), me, ve, a);
+        wv[e] = update_one<ADAM, true>(wv[e], grad(gv[e]), me, ve, a);
         mv[e] = me; vv[e] = ve;
       }
       *reinterpret_cast<floatx4*>(w + i) = wv;
@@ -87,7 +91,7 @@ __global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
     for (int64_t j = i; j < n && j < i + 4; ++j) {
       float mm = 0.f, vv = 0.f;
       if constexpr (ADAM) { mm = m[j]; vv = v[j]; }
-      const float wn = update_one<ADAM>(w[j], grad(g[j]), mm, vv, a);
+      const float wn = update_one<ADAM, false>(w[j], grad(g[j]), mm, vv, a);
       w[j] = wn;
       if constexpr (ADAM) { m[j] = mm; v[j] = vv; }
       if (lo) lo[j] = to_bf16(wn);
@@ -95,72 +99,84 @@ __global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
   }
 }
 
-// a sum over 256 threads in a fixed order, for thread 0
+// a sum over the workgroup in a fixed order
 __device__ __forceinline__ double block_sum(double s, double* s_w) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
   if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = s;
   __syncthreads();
   double all = 0.0;
-  if (threadIdx.x == 0) for (int w = 0; w < (int)blockDim.x / 64; ++w) all += s_w[w];
+#pragma unroll
+  for (int w = 0; w < kNormThreads / 64; ++w) all += s_w[w];
   return all;
 }
 
 // Squares and their sums are fp64: fp32's largest gradients do not overflow them, nor do its smallest vanish, and a sum of 10^9
-// squares is as good as one of ten.  Each workgroup takes chunks gridDim.x apart: the same ones in every call.
-__global__ __launch_bounds__(256) void square_sums_kernel(NormList l) {
-  __shared__ double s_w[4];
+// squares is as good as one of ten.  Each workgroup takes chunks gridDim.x apart, the same ones in every call, and the last one to
+// be done adds what all have left, in their order, so that the norm takes no launch of its own.
+__global__ __launch_bounds__(kNormThreads) void square_sums_kernel(NormList l) {
+  __shared__ double s_w[kNormThreads / 64];
+  __shared__ bool s_last;
   double sum = 0.0;
-  const int chunks = l.chunk_end[l.n - 1];
+  const int chunks = l.n > 0 ? l.chunk_end[l.n - 1] : 0;
   for (int b = blockIdx.x; b < chunks; b += gridDim.x) {
     const int t = tensor_of(l.chunk_end, l.n, b), c = b - (t ? l.chunk_end[t - 1] : 0);
-    const int64_t i0 = (int64_t)c * kChunk, n = l.count[t];
+    const int64_t i0 = (int64_t)c * kNormChunk, n = l.count[t];
     const bool half = (l.bf16[t >> 5] >> (t & 31)) & 1u, aligned = (reinterpret_cast<uintptr_t>(l.g[t]) & 15) == 0;
     if (half) {
       const uint16_t* const g = static_cast<const uint16_t*>(l.g[t]);
+      auto add = [&](u32x4 v) {
 #pragma unroll
-      for (int q = 0; q < kChunk / 2048; ++q) {
-        const int64_t i = i0 + q * 2048 + (int)threadIdx.x * 8;
-        if (i + 8 <= n && aligned) {
-          const u32x4 v = *reinterpret_cast<const u32x4*>(g + i);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const double x = __uint_as_float(v[e] << 16), y = __uint_as_float(v[e] & 0xFFFF0000u);
-            sum += x * x; sum += y * y;
-          }
-        } else {
-          for (int64_t j = i; j < n && j < i + 8; ++j) { const double x = bf16_bits_to_f32(g[j]); sum += x * x; }
+        for (int e = 0; e < 4; ++e) {
+          const double x = __uint_as_float(v[e] << 16), y = __uint_as_float(v[e] & 0xFFFF0000u);
+          sum += x * x; sum += y * y;
         }
+      };
+      if (i0 + kNormChunk <= n && aligned) {                 // (all loads of a chunk in flight at once)
+        u32x4 v[kNormChunk / (8 * kNormThreads)];
+#pragma unroll
+        for (int q = 0; q < kNormChunk / (8 * kNormThreads); ++q) v[q] = *reinterpret_cast<const u32x4*>(g + i0 + q * 8 * kNormThreads + (int)threadIdx.x * 8);
+#pragma unroll
+        for (int q = 0; q < kNormChunk / (8 * kNormThreads); ++q) add(v[q]);
+      } else {
+        for (int64_t i = i0 + (int)threadIdx.x; i < n && i < i0 + kNormChunk; i += kNormThreads) { const double x = bf16_bits_to_f32(g[i]); sum += x * x; }
       }
     } else {
       const float* const g = static_cast<const float*>(l.g[t]);
+      if (i0 + kNormChunk <= n && aligned) {
+        floatx4 v[kNormChunk / (4 * kNormThreads)];
 #pragma unroll
-      for (int q = 0; q < kChunk / 1024; ++q) {
-        const int64_t i = i0 + q * 1024 + (int)threadIdx.x * 4;
-        if (i + 4 <= n && aligned) {
-          const floatx4 v = *reinterpret_cast<const floatx4*>(g + i);
+        for (int q = 0; q < kNormChunk / (4 * kNormThreads); ++q) v[q] = *reinterpret_cast<const floatx4*>(g + i0 + q * 4 * kNormThreads + (int)threadIdx.x * 4);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) { const double x = v[e]; sum += x * x; }
-        } else {
-          for (int64_t j = i; j < n && j < i + 4; ++j) { const double x = g[j]; sum += x * x; }
-        }
+        for (int q = 0; q < kNormChunk / (4 * kNormThreads); ++q)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { const double x = v[q][e]; sum += x * x; }
+      } else {
+        for (int64_t i = i0 + (int)threadIdx.x; i < n && i < i0 + kNormChunk; i += kNormThreads) { const double x = g[i]; sum += x * x; }
       }
     }
   }
   sum = block_sum(sum, s_w);
-  if (threadIdx.x == 0) l.partial[blockIdx.x] = sum;
-}
-
-__global__ __launch_bounds__(256) void norm_kernel(const double* __restrict__ partial, int partials, double max_norm, float* norm, float* scale) {
-  __shared__ double s_w[4];
-  double sum = 0.0;
-  for (int i = threadIdx.x; i < partials; i += 256) sum += partial[i];
-  sum = block_sum(sum, s_w);
+  double* const mine = l.partial + l.first + blockIdx.x;
+  if (!l.done) { if (threadIdx.x == 0) *mine = sum; return; }
+  if (threadIdx.x == 0) {
+    store_for_all(mine, sum);
+    stores_done();
+    s_last = count_done(l.done) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  const int all = l.first + (int)gridDim.x;
+  double total = 0.0;
+  for (int i = threadIdx.x; i < all; i += kNormThreads) total += load_of_all(l.partial + i);
+  __syncthreads();
+  total = block_sum(total, s_w);
   if (threadIdx.x != 0) return;
-  const double r = sqrt(sum);
+  *l.done = 0u;
+  const double r = sqrt(total);
   const float f = (float)r;
-  if (norm) *norm = f;
-  if (scale) *scale = !(f < INFINITY) ? 0.f : r > max_norm ? (float)(max_norm / r) : 1.f;
+  if (l.norm) *l.norm = f;
+  if (l.scale) *l.scale = !(f < INFINITY) ? 0.f : r > l.max_norm ? (float)(l.max_norm / r) : 1.f;
 }
 
 __global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
@@ -206,10 +222,10 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
 }
 
 // fills chunk_end; their number, or -1 where a grid cannot have so many
-int64_t count_chunks(int n, const int64_t* count, int32_t* chunk_end) {
+int64_t count_chunks(int n, const int64_t* count, int32_t* chunk_end, int chunk = kChunk) {
   int64_t chunks = 0;
   for (int i = 0; i < n; ++i) {
-    chunks += (count[i] + kChunk - 1) / kChunk;
+    chunks += (count[i] + chunk - 1) / chunk;
     if (chunks >= (int64_t(1) << 24)) return -1;        // (a grid of 256 threads a workgroup: 2^32 at most)
     chunk_end[i] = (int32_t)chunks;
   }
@@ -228,17 +244,12 @@ hipError_t launch_optim(bool adam, OptimList* l, hipStream_t st) {
 }
 
 hipError_t launch_square_sums(NormList* l, int* partials, hipStream_t st) {
-  const int64_t chunks = count_chunks(l->n, l->count, l->chunk_end);
+  const int64_t chunks = count_chunks(l->n, l->count, l->chunk_end, kNormChunk);
   *partials = 0;
   if (chunks < 0) return hipErrorInvalidValue;
-  if (chunks == 0) return hipSuccess;
-  *partials = chunks < kNormBlocks ? (int)chunks : kNormBlocks;
-  hipLaunchKernelGGL(square_sums_kernel, dim3(*partials), dim3(256), 0, st, *l);
-  return hipGetLastError();
-}
-
-hipError_t launch_norm(const double* partial, int partials, double max_norm, float* norm, float* scale, hipStream_t st) {
-  hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(256), 0, st, partial, partials, max_norm, norm, scale);
+  if (chunks == 0 && !l->done) return hipSuccess;
+  *partials = chunks < 1 ? 1 : chunks < kNormBlocks ? (int)chunks : kNormBlocks;
+  hipLaunchKernelGGL(square_sums_kernel, dim3(*partials), dim3(kNormThreads), 0, st, *l);
   return hipGetLastError();
 }
 

@@ -88,6 +88,7 @@ def close(got, want, bound, tag):
     import torch
     got = got.double()
     assert got.shape == want.shape, tag
+    want = torch.where(want.float().isinf(), want.float().double(), want)           # (what fp32 cannot hold is an infinity)
     same = (got == want) | (torch.isnan(got) & torch.isnan(want))
     assert (torch.isfinite(got) | same).all(), tag + ": not finite"
     over = torch.where(same, torch.zeros_like(want), (got - want).abs() - bound)
@@ -238,6 +239,25 @@ def test_odd_rows(dtype, classes):
                     assert torch.isnan(one["top_logprob"][want >= 0]).all() and (one["top_logprob"][want < 0] == -math.inf).all(), tag
                     continue
                 check_answer(one, Row(zi, 1.0), tokens[i:i + 1], k, tag)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("T", [1.0, 0.01])
+@pytest.mark.parametrize("rows,classes", [(9, 700), (4, 5001), (90, 50257), (2, 140000)])
+def test_rows_far_from_zero(dtype, T, rows, classes):
+    """Offsets that an exponential's argument cannot carry along, up to the type's last values; and rows in which they meet."""
+    import torch
+    gen = gen_for(rows, classes, 9)
+    r = 3 * torch.randn(rows, classes, device="cuda", generator=gen)
+    tokens = tokens_for(rows, classes, gen)
+    with Ctx() as ctx:
+        for offset in (1e3, -1e3, 3e5, -3e5, 2e7, -2e7, 1e9, -1e9, 1e20, -1e20, 3e38, -3e38):
+            # (a few multiples of the offset's last place apart: distinct values, a type's resolution there being what it is)
+            step = abs(offset) * 2.0 ** (-7 if dtype else -22)
+            z = (offset + torch.round(r) * (step if abs(offset) > 1e6 else 1.0)).clamp(-3.38e38, 3.38e38).to(torch_dtype(dtype))
+            check_answer(call_dense(ctx, dtype, z, 12, T, tokens), Row(z.double(), float(torch.tensor(T, dtype=torch.float32))), tokens, 12, "offset %g T %g %d x %d" % (offset, T, rows, classes))
+        z = torch.where(torch.arange(classes, device="cuda") % 11 == 3, r, -1e9 * r.abs()).to(torch_dtype(dtype))
+        check_answer(call_dense(ctx, dtype, z, 12, T, tokens), Row(z.double(), float(torch.tensor(T, dtype=torch.float32))), tokens, 12, "mixed")
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
