@@ -35,12 +35,15 @@ __device__ __forceinline__ int entry_index(uint64_t e) { return (int)~(uint32_t)
 
 // entries that may wait for their places, at most kCand; counting takes their number squared over the threads
 template <int NT> constexpr int cand_max() { return NT <= 128 ? 384 : NT <= 256 ? 512 : 1024; }
+constexpr int kStrips = 512;
 template <int NT, int GROUPS> struct TopLds {
   uint64_t cand[cand_max<NT>()];
   uint32_t group[GROUPS];
   uint32_t hist[256];
   int wave_n[NT / 64];
-  int n; uint32_t bound; int digit, need;
+  uint16_t strip[kStrips];      // parts of a row that are to be looked at again
+  int n, strips; uint32_t bound; int digit, need;
+  __device__ __forceinline__ void begin() { if (threadIdx.x == 0) n = strips = 0; }     // (a barrier ahead of the first entry)
 };
 
 // wave 0: the 16 upper bits (0 below) of the k-th largest of 64 R maxima, each of `GROUPS` / (64 R) groups; at least kLowestKey
@@ -68,13 +71,12 @@ template <int NT, int GROUPS> __device__ __forceinline__ void append(TopLds<NT, 
   if (at < cand_max<NT>()) lds.cand[at] = make_entry(key, index);
 }
 
-// after the groups' maxima are in place (a barrier): the bound, the same for the workgroup, and room for entries
+// after the groups' maxima are in place (a barrier): the bound, the same for the workgroup
 template <int NT, int GROUPS> __device__ __forceinline__ uint32_t find_bound(TopLds<NT, GROUPS>& lds, int k) {
-  if constexpr (NT == 64) __syncthreads();              // (a larger workgroup has had one)
   if (threadIdx.x < 64) {
     constexpr int R = GROUPS >= 512 ? 8 : GROUPS / 64;
     const uint32_t b = R > 4 && k <= 128 ? group_bound<GROUPS, 4>(lds.group, k) : group_bound<GROUPS, R>(lds.group, k);
-    if (threadIdx.x == 0) { lds.bound = b; lds.n = 0; }
+    if (threadIdx.x == 0) lds.bound = b;
   }
   __syncthreads();
   return lds.bound;
@@ -291,7 +293,7 @@ template <typename T, int NT, int NV> __device__ __forceinline__ RowStats part_s
 // Bases lie within +-2^24 T ln 2, where m c is rounded by one power of two at most; rows whose largest logit does not, and such as hold
 // infinities or NaN, are done again, maximum first, by slow_stats.
 constexpr float kFar = 0x1p24f;
-constexpr int kAhead = 4;                               // vectors in flight
+constexpr int kAhead = 4, kSlots = 8;                   // vectors in flight
 template <int NT> constexpr int groups_of() { return NT >= 512 ? 1 : NT == 256 ? 2 : 4; }   // a thread's, for a list's bound
 
 __device__ __forceinline__ bool plain_stats(const RowStats& r, float c) { return r.s > 0.5f && r.s < INFINITY && r.m * c <= kFar; }
@@ -339,6 +341,7 @@ __device__ __forceinline__ void join_parts(const LogprobRows& a, int row, int pa
   const uint64_t* const list = reinterpret_cast<const uint64_t*>(static_cast<const char*>(a.ws) + logprob_stats_bytes(a.rows, parts)) +
                                (int64_t)row * parts * a.k;
   const int n_all = parts * a.k, tid = threadIdx.x;
+  top.begin();
   uint64_t kept[kKept];
 #pragma unroll
   for (int q = 0; q < kKept; ++q) { const int i = tid + q * NT; kept[q] = i < n_all ? load_of_all(list + i) : 0ull; }
@@ -384,6 +387,7 @@ __global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a, int par
   constexpr int VPL = S::VPL, G = groups_of<NT>();
   __shared__ float3 s_w[NT / 64];
   __shared__ TopLds<NT, NT * G> top;
+  __shared__ float s_most[ONE ? 1 : kSlots][ONE ? 1 : NT];         // of a thread's kAhead vectors at a time, in turn
   __shared__ bool s_last;
   const int row = SPLIT ? blockIdx.y : blockIdx.x + blockIdx.y * kRowsX;
   if (row >= a.rows) return;
@@ -422,14 +426,22 @@ __global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a, int par
       if (v0 + i * NT < v_hi) raw[i] = *reinterpret_cast<const u32x4*>(zv + (int64_t)(v0 + i * NT) * VPL);
     }
   };
+  const bool list = a.k > 1;                             // (the first place alone takes no search)
+  top.begin();
+  int turn = 0;
   for (int v0 = v_lo + tid; ONE ? v0 == v_lo + tid : v0 < v_hi; v0 += NT * kAhead) {
     load(v0);
-    float most = m;
+    float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const float mi = S::most(raw[i]);
       g[i % G] = fmaxf(g[i % G], mi);
       most = fmaxf(most, mi);
+    }
+    if (!ONE && a.k > 0) {
+      float* const slot = &s_most[turn % kSlots][tid];
+      *slot = turn < kSlots ? most : fmaxf(*slot, most);
+      ++turn;
     }
     if (most > m) {
       const float mc2 = rounded_product(most, c), d = mc - mc2, f = __builtin_amdgcn_exp2f(d);
@@ -455,11 +467,12 @@ __global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a, int par
   float most = g[0];
 #pragma unroll
   for (int q = 1; q < G; ++q) most = fmaxf(most, g[q]);
-  if (a.k > 0) {
+  if (list) {
 #pragma unroll
     for (int q = 0; q < G; ++q) top.group[q * NT + tid] = order_key(g[q]);
   }
   r = block_join<NT>(r, false, c, s_w);
+  if (NT == 64) __syncthreads();                        // (a larger workgroup has had one)
   const int c_lo = first ? 0 : head + v_lo * VPL, c_hi = last ? classes : head + v_hi * VPL;
   if (!plain_stats(r, c)) r = slow_stats<T, NT>(z, c_lo, c_hi, c, s_w);
   const RowEnd end(r, a.temperature);
@@ -473,19 +486,41 @@ __global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a, int par
     }
   }
   if (a.k > 0) {
-    const float least = key_value(find_bound(top, a.k));
-    auto look = [&](float v, int col) { if (v >= least) append(top, order_key(v), col); };
-    if (most >= least) {
-      if (single_col >= 0) look(single, single_col);
-      for (int v0 = v_lo + tid; ONE ? v0 == v_lo + tid : v0 < v_hi; v0 += NT * kAhead) {
-        if (!ONE) load(v0);
+    const float least = list ? key_value(find_bound(top, a.k)) : fmaxf(r.m, key_value(kLowestKey));
+    auto look = [&](const u32x4& v, int col) {
+      if (S::most(v) < least) return;
+      uint32_t hits = 0u;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-          if (S::most(raw[i]) >= least) {
-#pragma unroll
-            for (int q = 0; q < VPL; ++q) look(S::at(raw[i], q), head + (v0 + i * NT) * VPL + q);
-          }
+      for (int q = 0; q < VPL; ++q) hits |= S::at(v, q) >= least ? 1u << q : 0u;
+      while (hits) {                                     // (nearly always one)
+        const int q = __ffs(hits) - 1, w = sizeof(T) == 2 ? q >> 1 : q;
+        const uint32_t word = w == 0 ? v[0] : w == 1 ? v[1] : w == 2 ? v[2] : v[3];
+        append(top, order_key(__uint_as_float(sizeof(T) == 4 ? word : q & 1 ? word & 0xFFFF0000u : word << 16)), col + q);
+        hits &= hits - 1u;
       }
+    };
+    if (single >= least) append(top, order_key(single), single_col);
+    if constexpr (ONE) {
+      if (most >= least) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) look(raw[i], head + (v_lo + tid + i * NT) * VPL);
+      }
+    } else {
+      // Slots that hold such an element, by four lanes each: a lane has a vector.
+      if (most >= least)
+        for (int q = 0; q < min(turn, kSlots); ++q)
+          if (s_most[q][tid] >= least) {
+            const int at = atomicAdd(&top.strips, 1);
+            if (at < kStrips) top.strip[at] = (uint16_t)(q * NT + tid);
+          }
+      __syncthreads();
+      const int strips = min(top.strips, kStrips);
+      for (int t = tid / kAhead; t < strips; t += NT / kAhead) {
+        const int q = top.strip[t];
+        for (int v = v_lo + q % NT + (q / NT * kAhead + tid % kAhead) * NT; v < v_hi; v += kSlots * kAhead * NT)
+          look(*reinterpret_cast<const u32x4*>(zv + (int64_t)v * VPL), head + v * VPL);
+      }
+      if (tid == 0 && top.strips > kStrips) atomicAdd(&top.n, cand_max<NT>() + 1);    // (too many: as if all were there)
     }
     __syncthreads();
     int n = top.n;
@@ -574,6 +609,7 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_finish_kernel(LogprobFin
   __shared__ TopLds<NT, NT> top;
   const int place = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int row = a.list[place];
+  top.begin();
   if (place >= *a.live) {
     leave_row<NT>(a.logprob, a.entropy, a.k, a.top_index, a.top_logprob, row);
     return;

@@ -179,6 +179,7 @@ __global__ __launch_bounds__(kNormThreads) void square_sums_kernel(NormList l) {
   if (l.scale) *l.scale = !(f < INFINITY) ? 0.f : r > l.max_norm ? (float)(l.max_norm / r) : 1.f;
 }
 
+// (Stored past the caches: 1023-4097-1000-50257 in bf16 61 us with the norm, 71 where the end of the kernel waits for them.)
 __global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
   float f = *l.scale;
   if (f == 0.f) f = 1.f;                                // (a norm that is not finite: the gradients as they are)
@@ -198,7 +199,7 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           v[e] = (uint32_t)to_bf16(__uint_as_float(v[e] << 16) * f) | ((uint32_t)to_bf16(__uint_as_float(v[e] & 0xFFFF0000u) * f) << 16);
-        *reinterpret_cast<u32x4*>(o + i) = v;
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(o + i));
       } else {
         for (int64_t j = i; j < n && j < i + 8; ++j) o[j] = to_bf16(bf16_bits_to_f32(g[j]) * f);
       }
@@ -214,7 +215,7 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
       floatx4 v = *reinterpret_cast<const floatx4*>(g + i);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] *= f;
-      *reinterpret_cast<floatx4*>(o + i) = v;
+      __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(o + i));
     } else {
       for (int64_t j = i; j < n && j < i + 4; ++j) o[j] = g[j] * f;
     }
