@@ -258,35 +258,6 @@ __device__ __forceinline__ void put_top(int32_t* top_index, float* top_logprob, 
 }
 
 // ------------------------------------------------------------------ dense rows
-// statistics of a wave's vectors; e (kKeep): exponentials from the wave's maximum
-template <typename T, int NT, int NV> __device__ __forceinline__ RowStats part_stats(RowPart<T, NT, NV>& p, float c) {
-  typedef RowPart<T, NT, NV> Part;
-  RowStats r;
-  r.m = p.single;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-#pragma unroll
-    for (int q = 0; q < Part::VPL; ++q) r.m = fmaxf(r.m, p.at(i, q));
-    if (i % 2) __builtin_amdgcn_sched_barrier(0);
-  }
-  r.m = lanes_max(r.m);
-  if (sizeof(T) == 2) p.forget();
-  const float b = exp_base(r.m), l0 = (p.single - b) * c, e0 = __builtin_amdgcn_exp2f(l0);
-  r.s = e0; r.u = e0 * fmaxf(l0, kNoPower);
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-#pragma unroll
-    for (int q = 0; q < Part::VPL; ++q) {
-      const float l = (p.at(i, q) - b) * c, e = __builtin_amdgcn_exp2f(l);
-      r.s += e; r.u += e * fmaxf(l, kNoPower);
-    }
-    asm volatile("" : "+v"(r.s), "+v"(r.u));            // (both sums move on: the exponents of one are not kept for the other)
-  }
-  r.s = lanes_sum(r.s); r.u = lanes_sum(r.u);
-  if (sizeof(T) == 2) p.forget();
-  return r;
-}
-
 // Forward.  A row is read once and not kept: each thread runs over its vectors with a maximum and sums of its own, whose base
 // moves up when a larger logit comes (l = z c - m c is one operation so, with m c rounded once for all and what that rounding
 // moved put right at the end), and reads those of its vectors again, from a cache, of which a logit may be on the list.
@@ -548,8 +519,76 @@ __global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a, int par
   }
 }
 
-// backward: SPLIT: PASS 0 leaves the parts' statistics, PASS 1 joins them (each workgroup for itself) and writes
-template <typename T, int NT, int NV, bool SPLIT, int PASS>
+// Backward: a row stays in registers between its sums and its gradient, from one maximum m, with l = z c - m c in one operation as
+// above; where m lies too far from zero for that, from memory element by element.  SPLIT: PASS 0 leaves the parts' statistics, PASS 1
+// joins them (each workgroup for itself) and writes.
+template <int NT> __device__ __forceinline__ float block_max(float m, float3* s_w) {
+  m = lanes_max(m);
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6].x = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) m = fmaxf(m, s_w[w].x);
+  }
+  __syncthreads();
+  return m;
+}
+// sums of what threads have from one maximum
+template <int NT> __device__ __forceinline__ RowStats block_sums(float m, float s, float u, float3* s_w) {
+  RowStats r;
+  r.m = m; r.s = lanes_sum(s); r.u = lanes_sum(u);
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = make_float3(0.f, r.s, r.u);
+    __syncthreads();
+    r.s = r.u = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) { r.s += s_w[w].y; r.u += s_w[w].z; }
+  }
+  return r;
+}
+template <int NT> __device__ __forceinline__ RowStats joined_parts(const float* st, float c, float3* s_w) {
+  RowStats r;
+  for (int q = threadIdx.x; q < (int)gridDim.x; q += NT) r.join(st[3 * q], st[3 * q + 1], st[3 * q + 2], c);
+  return block_join<NT>(r, false, c, s_w);
+}
+__device__ __forceinline__ void put_part(float* st, const RowStats& r) {
+  float* const mine = st + blockIdx.x * 3;
+  mine[0] = r.m; mine[1] = r.s; mine[2] = r.u;
+}
+// what multiplies a row's exponentials (factor + slope l), and what its token's element has besides
+struct RowGrad {
+  float slope, factor, token;
+  __device__ __forceinline__ RowGrad(float ga, float gh, const RowStats& r) {
+    token = ga;
+    slope = -(gh * kLn2) / r.s;
+    factor = (gh * kLn2 * (r.u / r.s) - token) / r.s;
+  }
+  __device__ __forceinline__ float operator()(float l) const { return __builtin_amdgcn_exp2f(l) * fmaf(fmaxf(l, kNoPower), slope, factor); }
+};
+
+template <typename T, int NT, bool SPLIT, int PASS>
+__device__ __noinline__ void slow_gradient(const T* z, T* dz, float* st, int lo, int hi, float c, float ga, float gh, float m, int token,
+                                           float token_logit, float3* s_w) {
+  const float b = exp_base(m);
+  RowStats r;
+  if constexpr (SPLIT && PASS == 1) r = joined_parts<NT>(st, c, s_w);
+  else {
+    float s = 0.f, u = 0.f;
+    for (int v = lo + (int)threadIdx.x; v < hi; v += NT) {
+      const float l = (ld_elem(z + v) - b) * c, e = __builtin_amdgcn_exp2f(l);
+      s += e; u += e * fmaxf(l, kNoPower);
+    }
+    r = block_sums<NT>(m, s, u, s_w);
+  }
+  if constexpr (SPLIT && PASS == 0) { if (threadIdx.x == 0) put_part(st, r); return; }
+  const RowGrad grad(ga, gh, r);
+  for (int v = lo + (int)threadIdx.x; v < hi; v += NT)
+    if (v != token) st_elem(dz + v, grad((ld_elem(z + v) - b) * c));
+  if (token >= 0 && threadIdx.x == 0) st_elem(dz + token, grad((token_logit - b) * c) + grad.token);
+}
+
+// PAST: stored past the caches
+template <typename T, int NT, int NV, bool SPLIT, int PASS, bool PAST>
 __global__ __launch_bounds__(NT) void logprob_grad_kernel(LogprobRows a) {
   typedef RowPart<T, NT, NV> Part;
   constexpr int VPL = Part::VPL;
@@ -565,93 +604,155 @@ __global__ __launch_bounds__(NT) void logprob_grad_kernel(LogprobRows a) {
     if (!(SPLIT && PASS == 0)) for (int q = c_lo + tid; q < c_hi; q += NT) st_elem(dz + q, 0.f);
     return;
   }
-  const float c = kLog2e / a.temperature;
+  const float c = kLog2e / a.temperature, inv_t = 1.f / a.temperature;
+  float* const st = SPLIT ? static_cast<float*>(a.ws) + (int64_t)row * gridDim.x * 3 : nullptr;
   Part p;
   p.load(z, v0, head, classes);
-  const int token = a.d_logprob ? a.token[row] : -1;
-  const bool mine = token >= c_lo && token < c_hi;
-  if (mine && tid == 0) s_token = ld_elem(z + token);    // (a barrier ahead of any store: dz may be z)
+  const float ga = a.d_logprob ? a.d_logprob[row] * inv_t : 0.f, gh = a.d_entropy ? a.d_entropy[row] * inv_t : 0.f;
+  int token = a.d_logprob ? a.token[row] : -1;
+  if (token < c_lo || token >= c_hi) token = -1;
+  if (token >= 0 && tid == 0) s_token = ld_elem(z + token);    // (a barrier ahead of any store: dz may be z)
+  float m = p.single;
+  if constexpr (SPLIT && PASS == 1) {
+    for (int q = tid; q < (int)gridDim.x; q += NT) m = fmaxf(m, st[3 * q]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) m = fmaxf(m, p.at(i, q));
+      if (i % 2) __builtin_amdgcn_sched_barrier(0);
+    }
+    p.forget();
+  }
+  m = block_max<NT>(m, s_w);
+  const float mc = rounded_product(m, c), moved = fmaf(m, c, -mc);
+  if (!(fabsf(mc) <= kFar)) {
+    slow_gradient<T, NT, SPLIT, PASS>(z, dz, st, c_lo, c_hi, c, ga, gh, m, token, s_token, s_w);
+    return;
+  }
   RowStats r;
-  if constexpr (!SPLIT || PASS == 0) {
-    r = block_join<NT>(part_stats(p, c), true, c, s_w);
-    if constexpr (SPLIT) {
-      if (tid == 0) {
-        float* const st = static_cast<float*>(a.ws) + ((int64_t)row * gridDim.x + part) * 3;
-        st[0] = r.m; st[1] = r.s; st[2] = r.u;
+  if constexpr (SPLIT && PASS == 1) {
+    r = joined_parts<NT>(st, c, s_w);
+    const float f = __builtin_amdgcn_exp2f(moved);       // (from m to the base)
+    r.u = f * (r.u + moved * r.s); r.s *= f;
+  } else {
+    const float l0 = fmaf(p.single, c, -mc), e0 = __builtin_amdgcn_exp2f(l0);
+    float s = e0, u = e0 * fmaxf(l0, kNoPower);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) {
+        const float l = fmaf(p.at(i, q), c, -mc), e = __builtin_amdgcn_exp2f(l);
+        s += e; u = fmaf(e, fmaxf(l, kNoPower), u);
       }
+      asm volatile("" : "+v"(s), "+v"(u));              // (both sums move on: the exponents of one are not kept for the other)
+    }
+    p.forget();
+    r = block_sums<NT>(m, s, u, s_w);
+    if constexpr (SPLIT) {
+      const float f = __builtin_amdgcn_exp2f(-moved);
+      r.u = f * (r.u - moved * r.s); r.s *= f;
+      if (tid == 0) put_part(st, r);
       return;
     }
-  } else {
-    const float* const st = static_cast<const float*>(a.ws) + (int64_t)row * gridDim.x * 3;
-    for (int q = tid; q < (int)gridDim.x; q += NT) r.join(st[3 * q], st[3 * q + 1], st[3 * q + 2], c);
-    r = block_join<NT>(r, false, c, s_w);
   }
-  const float b = exp_base(r.m), inv_t = 1.f / a.temperature;
-  const float ga = a.d_logprob ? a.d_logprob[row] * inv_t : 0.f, gh = a.d_entropy ? a.d_entropy[row] * inv_t : 0.f;
-  const float slope = -(gh * kLn2) / r.s, factor = (gh * kLn2 * (r.u / r.s) - ga) / r.s;
-  auto grad = [&](float v) {
-    const float l = (v - b) * c;
-    return __builtin_amdgcn_exp2f(l) * fmaf(fmaxf(l, kNoPower), slope, factor);
-  };
-  const float single = grad(p.single);
-  store_part<T, NT, NV>(dz, p, v0, head, classes, single, [&](int i, int q) { return grad(p.at(i, q)); });
+  const RowGrad grad(ga, gh, r);
+  const float single = grad(fmaf(p.single, c, -mc));
+  store_part<T, NT, NV, PAST>(dz, p, v0, head, classes, single, [&](int i, int q) { return grad(fmaf(p.at(i, q), c, -mc)); });
   __threadfence_block();
   __syncthreads();                                      // the token's element is written again, after its vector
-  if (mine && tid == 0) st_elem(dz + token, grad(s_token) + ga);
+  if (token >= 0 && tid == 0) st_elem(dz + token, grad(fmaf(s_token, c, -mc)) + grad.token);
 }
 
 // ------------------------------------------------------------------ after a layer's product
 constexpr int kJoinThreads = 512;
-// A workgroup a place: its parts' statistics joined, and of its logits (in fp32) those of the parts that may hold a listed one.
+// A workgroup a place: its parts' statistics joined, and of its logits (in fp32) those of the parts that may hold a listed one; where the
+// parts are too few for a tight bound, all of them twice.
 __global__ __launch_bounds__(kJoinThreads) void logprob_finish_kernel(LogprobFinish a) {
-  constexpr int NT = kJoinThreads;
+  constexpr int NT = kJoinThreads, kKept = 4;            // parts of a thread that wait in registers
   __shared__ float3 s_w[NT / 64];
   __shared__ TopLds<NT, NT> top;
-  const int place = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int row = a.list[place];
-  top.begin();
-  if (place >= *a.live) {
+  const int place = blockIdx.x, tid = threadIdx.x;
+  const int row = a.list[place], live = *a.live;
+  auto stats_of = [&](int p) { return *reinterpret_cast<const float2*>(a.stats + ((int64_t)p * a.stats_ld + place) * 2); };
+  auto spread_of = [&](int p) { return a.spread[(int64_t)p * a.stats_ld + place]; };
+  float2 ms[kKept];
+  float u[kKept];
+#pragma unroll
+  for (int q = 0; q < kKept; ++q) {                      // (all on their way at once, whether the place counts or not)
+    const int p = tid + q * NT;
+    ms[q] = p < a.parts ? stats_of(p) : make_float2(-INFINITY, 0.f);
+    u[q] = p < a.parts ? spread_of(p) : 0.f;
+  }
+  const float target = a.logprob && tid == 0 ? a.target[place] : 0.f;
+  if (place >= live) {
     leave_row<NT>(a.logprob, a.entropy, a.k, a.top_index, a.top_logprob, row);
     return;
   }
+  top.begin();
   const float c = kLog2e / a.temperature;
   const float* const z = a.z + (int64_t)place * a.z_ld;
-  // groups: parts, where there are enough of them for a tight bound, else classes
-  const bool by_part = a.parts >= 2 * a.k;
+  const bool list = a.k > 1, by_part = a.parts >= 2 * a.k;
+  const int vecs = (a.classes + 3) / 4;                  // (rows are whole 256-byte pieces, -infinity behind the classes)
+  auto vec = [&](int v) { return *reinterpret_cast<const u32x4*>(z + 4 * (int64_t)v); };
   RowStats r;
-  float most = -INFINITY;
-  for (int p = tid; p < a.parts; p += NT) {
-    const float2 ms = *reinterpret_cast<const float2*>(a.stats + ((int64_t)p * a.stats_ld + place) * 2);
-    r.join(ms.x, ms.y, a.spread[(int64_t)p * a.stats_ld + place], c);
-    most = fmaxf(most, ms.x);
+#pragma unroll
+  for (int q = 0; q < kKept; ++q) r.m = fmaxf(r.m, ms[q].x);
+  for (int p = tid + kKept * NT; p < a.parts; p += NT) r.m = fmaxf(r.m, stats_of(p).x);
+  const float mine = r.m;
+#pragma unroll
+  for (int q = 0; q < kKept; ++q) {
+    RowStats o;
+    o.m = ms[q].x; o.s = ms[q].y; o.u = u[q];
+    o.rebase(mine, c);
+    r.s += o.s; r.u += o.u;
   }
+  for (int p = tid + kKept * NT; p < a.parts; p += NT) r.join(stats_of(p).x, stats_of(p).y, spread_of(p), c);
+  float most = mine;
   if (a.k > 0) {
-    if (!by_part) for (int v = tid; v < a.classes; v += NT) most = v == tid ? z[v] : fmaxf(most, z[v]);
-    if (!by_part && tid >= a.classes) most = -INFINITY;
-    top.group[tid] = order_key(most);
+    if (!by_part) {
+      most = -INFINITY;
+#pragma unroll 4
+      for (int v = tid; v < vecs; v += NT) most = fmaxf(most, Stream<float>::most(vec(v)));
+    }
+    if (list) top.group[tid] = order_key(most);
   }
   r = block_join<NT>(r, false, c, s_w);
   const RowEnd end(r, a.temperature);
   if (tid == 0) {
-    if (a.logprob) a.logprob[row] = end.log_q(a.target[place]);
+    if (a.logprob) a.logprob[row] = end.log_q(target);
     if (a.entropy) a.entropy[row] = end.entropy;
   }
   if (a.k == 0) return;
-  const uint32_t bound = find_bound(top, a.k);
-  const float least = key_value(bound);
-  auto look = [&](int v) { if (v < a.classes && z[v] >= least) append(top, order_key(z[v]), v); };
+  const float least = list ? key_value(find_bound(top, a.k)) : fmaxf(r.m, key_value(kLowestKey));
+  auto look = [&](int v) {
+    const u32x4 w = vec(v);
+    if (Stream<float>::most(w) < least) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (__uint_as_float(w[q]) >= least && 4 * v + q < a.classes) append(top, order_key(__uint_as_float(w[q])), 4 * v + q);
+  };
   if (by_part) {
-    for (int p0 = w * 64; p0 < a.parts; p0 += NT) {
-      const int p = p0 + lane;
-      uint64_t some = __ballot(p < a.parts && a.stats[((int64_t)p * a.stats_ld + place) * 2] >= least);
-      while (some) {
-        const int q = __ffsll((unsigned long long)some) - 1;
-        some &= some - 1;
-        for (int v = lane; v < a.part; v += 64) look((p0 + q) * a.part + v);
-      }
+    auto note = [&](float m, int p) {
+      if (!(m >= least)) return;
+      const int at = atomicAdd(&top.strips, 1);
+      if (at < kStrips) top.strip[at] = (uint16_t)p;
+    };
+    if (most >= least) {
+#pragma unroll
+      for (int q = 0; q < kKept; ++q) note(ms[q].x, tid + q * NT);
+      for (int p = tid + kKept * NT; p < a.parts; p += NT) note(stats_of(p).x, p);
     }
-  } else {
-    for (int v = tid; v < a.classes; v += NT) look(v);
+    __syncthreads();
+    const int strips = min(top.strips, kStrips), lanes = a.part / 4;      // 16 or 32 for a part
+    for (int t = tid / lanes; t < strips; t += NT / lanes) {
+      const int v = (int)top.strip[t] * lanes + tid % lanes;
+      if (v < vecs) look(v);
+    }
+    if (tid == 0 && top.strips > kStrips) atomicAdd(&top.n, cand_max<NT>() + 1);        // (too many: as if all were there)
+  } else if (most >= least) {
+#pragma unroll 4
+    for (int v = tid; v < vecs; v += NT) look(v);
   }
   __syncthreads();
   int n = top.n;
@@ -693,15 +794,23 @@ template <typename T> hipError_t forward(const LogprobRows& a, hipStream_t st) {
   return forward_whole<T, 512>(a, st);
 }
 
-// backward
+// A gradient that the last-level cache (256 MB) cannot hold is stored past the caches, others stay there for whoever reads them next.  us
+// through / past: bf16 4096 x 32000 (262 MB) 109 / 101, 2000 x 50257 (201) 100 / 92, but 8192 x 8000 (131) 47 / 49, fp32 600 x 50257 (121)
+// 61 / 64.
+constexpr int64_t kPastBytes = 160 << 20;
 template <typename T, int NT, int NV> hipError_t backward_whole(const LogprobRows& a, hipStream_t st) {
   const dim3 grid(a.rows < kRowsX ? a.rows : kRowsX, (a.rows + kRowsX - 1) / kRowsX);
-  hipLaunchKernelGGL((logprob_grad_kernel<T, NT, NV, false, 1>), grid, dim3(NT), 0, st, a);
+  const bool past = (int64_t)a.rows * a.classes * (int)sizeof(T) >= kPastBytes;
+  auto kern = past ? logprob_grad_kernel<T, NT, NV, false, 1, true> : logprob_grad_kernel<T, NT, NV, false, 1, false>;
+  hipLaunchKernelGGL(kern, grid, dim3(NT), 0, st, a);
   return hipGetLastError();
 }
+// Few of the longest rows go in parts too, which takes a launch and a second read but gives each row more than a CU.  us whole / in parts:
+// bf16 1 x 128000 19.6 / 11.0, 64 x 128000 24.9 / 14.8, 128 x 128000 26.0 / 22.9, 256 x 128000 29.4 / 38.9; fp32 64 x 50257 14.9 / 12.0, 128 x 50257
+// 15.9 / 16.3; shorter ones bf16 64 x 50257 12.1 / 11.1, but fp32 64 x 20000 8.1 / 10.9.
 template <typename T> int backward_parts(const LogprobRows& a) {
   const int64_t vecs = row_vectors<T>(a.classes);
-  if (!(vecs > 1024 * 16 || (vecs > 512 * 8 && a.rows <= 64))) return 1;
+  if (!(vecs > 1024 * 16 || (vecs > 512 * 16 && a.rows <= 128))) return 1;
   return (int)((vecs + kPartThreads * kPartVecs - 1) / (kPartThreads * kPartVecs));
 }
 template <typename T> hipError_t backward(const LogprobRows& a, hipStream_t st) {
@@ -709,8 +818,8 @@ template <typename T> hipError_t backward(const LogprobRows& a, hipStream_t st) 
   const int parts = backward_parts<T>(a);
   if (parts > 1) {
     const dim3 grid((unsigned)parts, (unsigned)(a.rows < 65535 ? a.rows : 65535), (unsigned)((a.rows + 65534) / 65535));
-    hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 0>), grid, dim3(kPartThreads), 0, st, a);
-    hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 1>), grid, dim3(kPartThreads), 0, st, a);
+    hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 0, false>), grid, dim3(kPartThreads), 0, st, a);
+    hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 1, false>), grid, dim3(kPartThreads), 0, st, a);
     return hipGetLastError();
   }
   if (vecs <= 64 * 4) return backward_whole<T, 64, 4>(a, st);

@@ -116,9 +116,10 @@ template <typename T, int NT, int NV> struct RowPart {
   }
 };
 
-// stores a part of a row: f(i, q) is element q of vector i, single what the single element becomes
-template <typename T, int NT, int NV, class F>
+// stores a part of a row: f(i, q) is element q of vector i, single what the single element becomes; PAST: past the caches
+template <typename T, int NT, int NV, bool PAST = false, class F>
 __device__ __forceinline__ void store_part(T* out, const RowPart<T, NT, NV>& p, int v0, int head, int classes, float single, F f) {
+  typedef u32x4 u32x4_any __attribute__((aligned(2)));
   constexpr int VPL = 16 / (int)sizeof(T);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -130,7 +131,8 @@ __device__ __forceinline__ void store_part(T* out, const RowPart<T, NT, NV>& p, 
         if constexpr (sizeof(T) == 4) w[q] = __float_as_uint(f(i, q));
         else w[q] = bf16_pair(f(i, 2 * q), f(i, 2 * q + 1));
       }
-      __builtin_memcpy(out + c, &w, 16);                // (dz may be aligned otherwise)
+      u32x4_any* const to = reinterpret_cast<u32x4_any*>(out + c);      // (dz may be aligned otherwise)
+      if constexpr (PAST) __builtin_nontemporal_store(w, to); else *to = w;
     }
     if (i % 2) __builtin_amdgcn_sched_barrier(0);
   }

@@ -8,7 +8,8 @@ and S = sum q d:
   log q = -d - ln s: R + 4 u (d + ln n + S + 1);
   H = ln s - ln 2 u' / s, u' = sum e l: R (1 + S + ln n) + 4 u sum q d^2 + 4 u (S + ln n + 1);
   dz = q (-a - h (log q + H)) / T: with M = q (|a| + |h| (d + S + 1)) / T the size of its parts, M (2 R + 8 u (d + S)) + q |h| / T times
-  H's bound, 8 u |a| / T at the token, and the rounding to the type.
+  H's bound, 8 u |a| / T at the token, and the rounding to the type.  The hardware's exponential is 0 below 2^-126, and s is at least 1, so q may
+  be off by 2^-126 besides, and dz by as much of (|a| + |h| (d + S + 1)) / T.
 Logits of a layer are off by E = 8 u sqrt(d_in + 2) max sum |x| |W| each before T: 2 E / T in log q, 2 E / T (1 + S + ln n) in H (its derivative
 is q (log q + H)); in bf16 training a logit is a code, off by half a step of 2^-9 of a power of two (0.18 h), and dz is rounded to the
 type: 2.02 h M."""
@@ -79,8 +80,9 @@ class Row:
         at = torch.zeros_like(dz)
         if token is not None:
             at.scatter_(1, token.long().clamp(0, dz.shape[1] - 1)[:, None], a.expand(-1, 1))
-        parts = self.q * (a.abs() + h.abs() * (self.d + self.S[:, None] + 1))
-        e = parts * (2 * self.R + 2 * self.e + 8 * U * (self.d + self.S[:, None])) + self.q * h.abs() * (self.bound_H[:, None] + self.e) + 8 * U * at.abs()
+        size = a.abs() + h.abs() * (self.d + self.S[:, None] + 1)
+        parts = self.q * size
+        e = 2.0 ** -126 * size + parts * (2 * self.R + 2 * self.e + 8 * U * (self.d + self.S[:, None])) + self.q * h.abs() * (self.bound_H[:, None] + self.e) + 8 * U * at.abs()
         return dz + at, e, parts + at.abs()
 
 
@@ -366,6 +368,23 @@ def test_masked_grad(dtype, classes):
         assert (out[0, 5:] == 0).all() and (out[1, 5::2] == 0).all() and (out[2, classes // 2:] == 0).all()
         rest = torch.tensor([0, 1, 2, 6, 7], device="cuda")
         assert torch.isfinite(out[rest]).all()
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("T", [1.0, 0.01])
+@pytest.mark.parametrize("rows,classes", [(9, 700), (4, 5001), (90, 50257), (2, 140000)])
+def test_grad_of_rows_far_from_zero(dtype, T, rows, classes):
+    import torch
+    gen = gen_for(rows, classes, 10)
+    r = 3 * torch.randn(rows, classes, device="cuda", generator=gen)
+    tokens = tokens_for(rows, classes, gen, 0.2)
+    a, h = torch.randn(rows, device="cuda", generator=gen), torch.randn(rows, device="cuda", generator=gen)
+    T32 = float(torch.tensor(T, dtype=torch.float32))
+    with Ctx() as ctx:
+        for offset in (1e3, -3e5, 2e7, -2e7, 1e9, -1e20, 3e38, -3e38):
+            step = abs(offset) * 2.0 ** (-7 if dtype else -22)
+            z = (offset + torch.round(r) * (step if abs(offset) > 1e6 else 1.0)).clamp(-3.38e38, 3.38e38).to(torch_dtype(dtype))
+            check_dense_grad(ctx, dtype, z, tokens, a, h, T=T32, in_place=offset < 0, tag="offset %g T %g" % (offset, T))
 
 
 @pytest.mark.parametrize("dtype", [0])
