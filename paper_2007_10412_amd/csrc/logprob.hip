@@ -567,7 +567,7 @@ struct RowGrad {
 };
 
 template <typename T, int NT, bool SPLIT, int PASS>
-__device__ __noinline__ void slow_gradient(const T* z, T* dz, float* st, int lo, int hi, float c, float ga, float gh, float m, int token,
+__device__ __forceinline__ void slow_gradient(const T* z, T* dz, float* st, int lo, int hi, float c, float ga, float gh, float m, int token,
                                            float token_logit, float3* s_w) {
   const float b = exp_base(m);
   RowStats r;
@@ -587,19 +587,29 @@ __device__ __noinline__ void slow_gradient(const T* z, T* dz, float* st, int lo,
   if (token >= 0 && threadIdx.x == 0) st_elem(dz + token, grad((token_logit - b) * c) + grad.token);
 }
 
-// PAST: stored past the caches
-template <typename T, int NT, int NV, bool SPLIT, int PASS, bool PAST>
-__global__ __launch_bounds__(NT) void logprob_grad_kernel(LogprobRows a) {
+// PAST: stored past the caches.  NL: vectors of a thread that wait in LDS beside the NV in its registers, so that two rows of up to 13248
+// vectors share a CU and one row's loads pass while the other is summed (kLdsLess fewer than there is room for leave its LDS a little for
+// the rest).  us with 16 vectors in registers, one row a CU / with 8 and 5: fp32 333 x 50257 30.5 / 24.5, 1300 x 50257 132 / 115, bf16
+// 1300 x 100000 154 / 117, 150 x 50257 fp32 16.1 / 15.6.
+constexpr int kLdsLess = 64;
+static __device__ __align__(16) const uint32_t kEmpty16[4] = {0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u};     // -infinity
+static __device__ __align__(16) const uint32_t kEmpty32[4] = {0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u};
+template <typename T, int NT, int NV, int NL, bool SPLIT, int PASS, bool PAST>
+__global__ __launch_bounds__(NT, NL > 0 ? 8 : 1) void logprob_grad_kernel(LogprobRows a) {
   typedef RowPart<T, NT, NV> Part;
-  constexpr int VPL = Part::VPL;
+  typedef Stream<T> S;
+  static_assert(NL == 0 || !SPLIT, "whole rows");
+  constexpr int VPL = Part::VPL, kVecs = NT * (NV + NL);
+  constexpr int kLds = NL > 0 ? NL * NT - kLdsLess : 1;
+  __shared__ u32x4 s_row[kLds];
   __shared__ float3 s_w[NT / 64];
   __shared__ float s_token;
   const int row = SPLIT ? blockIdx.y + blockIdx.z * 65535 : blockIdx.x + blockIdx.y * kRowsX;
   if (row >= a.rows) return;
-  const int part = SPLIT ? blockIdx.x : 0, v0 = part * NT * NV, classes = a.classes, tid = threadIdx.x;
+  const int part = SPLIT ? blockIdx.x : 0, v0 = part * kVecs, classes = a.classes, tid = threadIdx.x;
   const T* const z = static_cast<const T*>(a.z) + (int64_t)row * classes;
   T* const dz = static_cast<T*>(a.dz) + (int64_t)row * classes;
-  const int head = Part::head(z), c_lo = part == 0 ? 0 : head + v0 * VPL, c_hi = min(classes, head + (v0 + NT * NV) * VPL);
+  const int head = Part::head(z), c_lo = part == 0 ? 0 : head + v0 * VPL, c_hi = min(classes, head + (v0 + kVecs) * VPL);
   if (!token_counts(a.token, row, classes)) {
     if (!(SPLIT && PASS == 0)) for (int q = c_lo + tid; q < c_hi; q += NT) st_elem(dz + q, 0.f);
     return;
@@ -608,6 +618,27 @@ __global__ __launch_bounds__(NT) void logprob_grad_kernel(LogprobRows a) {
   float* const st = SPLIT ? static_cast<float*>(a.ws) + (int64_t)row * gridDim.x * 3 : nullptr;
   Part p;
   p.load(z, v0, head, classes);
+  auto lds_col = [&](int i) { return Part::col(NV * NT, i, head); };
+  auto lds_vec = [&](int i) {                            // (each thread's own: no barriers)
+    const u32x4 none = {S::kEmpty, S::kEmpty, S::kEmpty, S::kEmpty};
+    return (i + 1) * NT <= kLds || i * NT + tid < kLds ? s_row[i * NT + tid] : none;
+  };
+  if constexpr (NL > 0) {
+    // (from memory into LDS, past the registers: lane l's 16 bytes go to a wave's 1 KB at 16 l)
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) * 64;
+#pragma unroll
+    for (int i = 0; i < NL; ++i)
+      if ((i + 1) * NT <= kLds || i * NT + wave + 64 <= kLds) {
+        const T* const from = lds_col(i) + VPL <= classes ? z + lds_col(i) : reinterpret_cast<const T*>(sizeof(T) == 2 ? kEmpty16 : kEmpty32);
+        __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) const uint32_t*)from,
+                                         (__attribute__((address_space(3))) uint32_t*)&s_row[i * NT + wave], 16, 0, 0);
+      }
+    const int tail = head + max(0, classes - head) / VPL * VPL + tid - VPL;    // (the elements behind the last vector, if Part has left them)
+    if (tid >= VPL && tid < 2 * VPL && p.single_col < 0 && tail < classes && tail >= head + NT * NV * VPL) {
+      p.single_col = tail;
+      p.single = ld_elem(z + tail);
+    }
+  }
   const float ga = a.d_logprob ? a.d_logprob[row] * inv_t : 0.f, gh = a.d_entropy ? a.d_entropy[row] * inv_t : 0.f;
   int token = a.d_logprob ? a.token[row] : -1;
   if (token < c_lo || token >= c_hi) token = -1;
@@ -623,6 +654,12 @@ __global__ __launch_bounds__(NT) void logprob_grad_kernel(LogprobRows a) {
       if (i % 2) __builtin_amdgcn_sched_barrier(0);
     }
     p.forget();
+    if constexpr (NL > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // (what went into LDS has arrived)
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      m = fmaxf(m, S::most(lds_vec(i)));
+      asm volatile("" : "+v"(m) :: "memory");            // (a vector of them in registers at a time)
+    }
   }
   m = block_max<NT>(m, s_w);
   const float mc = rounded_product(m, c), moved = fmaf(m, c, -mc);
@@ -638,16 +675,24 @@ __global__ __launch_bounds__(NT) void logprob_grad_kernel(LogprobRows a) {
   } else {
     const float l0 = fmaf(p.single, c, -mc), e0 = __builtin_amdgcn_exp2f(l0);
     float s = e0, u = e0 * fmaxf(l0, kNoPower);
+    auto add = [&](float v) {
+      const float l = fmaf(v, c, -mc), e = __builtin_amdgcn_exp2f(l);
+      s += e; u = fmaf(e, fmaxf(l, kNoPower), u);
+    };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
 #pragma unroll
-      for (int q = 0; q < VPL; ++q) {
-        const float l = fmaf(p.at(i, q), c, -mc), e = __builtin_amdgcn_exp2f(l);
-        s += e; u = fmaf(e, fmaxf(l, kNoPower), u);
-      }
+      for (int q = 0; q < VPL; ++q) add(p.at(i, q));
       asm volatile("" : "+v"(s), "+v"(u));              // (both sums move on: the exponents of one are not kept for the other)
     }
     p.forget();
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const u32x4 v = lds_vec(i);
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) add(S::at(v, q));
+      asm volatile("" : "+v"(s), "+v"(u));
+    }
     r = block_sums<NT>(m, s, u, s_w);
     if constexpr (SPLIT) {
       const float f = __builtin_amdgcn_exp2f(-moved);
@@ -659,6 +704,12 @@ __global__ __launch_bounds__(NT) void logprob_grad_kernel(LogprobRows a) {
   const RowGrad grad(ga, gh, r);
   const float single = grad(fmaf(p.single, c, -mc));
   store_part<T, NT, NV, PAST>(dz, p, v0, head, classes, single, [&](int i, int q) { return grad(fmaf(p.at(i, q), c, -mc)); });
+#pragma unroll
+  for (int i = 0; i < NL; ++i)
+    if (lds_col(i) + VPL <= classes) {
+      const u32x4 v = lds_vec(i);
+      store_vector<T, PAST>(dz + lds_col(i), [&](int q) { return grad(fmaf(S::at(v, q), c, -mc)); });
+    }
   __threadfence_block();
   __syncthreads();                                      // the token's element is written again, after its vector
   if (token >= 0 && tid == 0) st_elem(dz + token, grad(fmaf(s_token, c, -mc)) + grad.token);
@@ -798,10 +849,10 @@ template <typename T> hipError_t forward(const LogprobRows& a, hipStream_t st) {
 // through / past: bf16 4096 x 32000 (262 MB) 109 / 101, 2000 x 50257 (201) 100 / 92, but 8192 x 8000 (131) 47 / 49, fp32 600 x 50257 (121)
 // 61 / 64.
 constexpr int64_t kPastBytes = 160 << 20;
-template <typename T, int NT, int NV> hipError_t backward_whole(const LogprobRows& a, hipStream_t st) {
+template <typename T, int NT, int NV, int NL = 0> hipError_t backward_whole(const LogprobRows& a, hipStream_t st) {
   const dim3 grid(a.rows < kRowsX ? a.rows : kRowsX, (a.rows + kRowsX - 1) / kRowsX);
   const bool past = (int64_t)a.rows * a.classes * (int)sizeof(T) >= kPastBytes;
-  auto kern = past ? logprob_grad_kernel<T, NT, NV, false, 1, true> : logprob_grad_kernel<T, NT, NV, false, 1, false>;
+  auto kern = past ? logprob_grad_kernel<T, NT, NV, NL, false, 1, true> : logprob_grad_kernel<T, NT, NV, NL, false, 1, false>;
   hipLaunchKernelGGL(kern, grid, dim3(NT), 0, st, a);
   return hipGetLastError();
 }
@@ -818,8 +869,8 @@ template <typename T> hipError_t backward(const LogprobRows& a, hipStream_t st) 
   const int parts = backward_parts<T>(a);
   if (parts > 1) {
     const dim3 grid((unsigned)parts, (unsigned)(a.rows < 65535 ? a.rows : 65535), (unsigned)((a.rows + 65534) / 65535));
-    hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 0, false>), grid, dim3(kPartThreads), 0, st, a);
-    hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, true, 1, false>), grid, dim3(kPartThreads), 0, st, a);
+    hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, 0, true, 0, false>), grid, dim3(kPartThreads), 0, st, a);
+    hipLaunchKernelGGL((logprob_grad_kernel<T, kPartThreads, kPartVecs, 0, true, 1, false>), grid, dim3(kPartThreads), 0, st, a);
     return hipGetLastError();
   }
   if (vecs <= 64 * 4) return backward_whole<T, 64, 4>(a, st);
@@ -827,7 +878,9 @@ template <typename T> hipError_t backward(const LogprobRows& a, hipStream_t st) 
   if (vecs <= 256 * 4) return backward_whole<T, 256, 4>(a, st);
   if (vecs <= 256 * 8) return backward_whole<T, 256, 8>(a, st);
   if (vecs <= 512 * 8) return backward_whole<T, 512, 8>(a, st);
-  if (vecs <= 512 * 16) return backward_whole<T, 512, 16>(a, st);
+  // (us with 512 x 16 / 1024 x 8: bf16 1300 x 50257 67 / 62, 333 x 50257 22.8 / 23.5; fp32 150 x 32000 13.2 / 11.6, 333 x 32000 17.8 / 18.3)
+  if (vecs <= 1024 * 8) return backward_whole<T, 1024, 8>(a, st);
+  if (vecs <= 1024 * 13 - kLdsLess) return backward_whole<T, 1024, 8, 5>(a, st);
   return backward_whole<T, 1024, 16>(a, st);
 }
 

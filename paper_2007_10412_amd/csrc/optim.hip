@@ -54,7 +54,10 @@ __global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
     scale = *l.scale;
     if (scale == 0.f) return;
   }
-  const int t = tensor_of(l.chunk_end, l.n, blockIdx.x), c = (int)blockIdx.x - (t ? l.chunk_end[t - 1] : 0);
+  // (Adam after a norm begins with the gradients that the norm read last, of which the last-level cache still holds the most:
+  // 4096-4096-4096-1000 bf16 with its norm 248 us from the first, 244 from the last; SGD, which needs less of it besides, 109 and 110.)
+  const int b = ADAM && SCALED ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x;
+  const int t = tensor_of(l.chunk_end, l.n, b), c = b - (t ? l.chunk_end[t - 1] : 0);
   float* const w = l.w[t]; float* const m = l.m[t]; float* const v = l.v[t];
   const float* const g = l.g[t];
   uint16_t* const lo = l.lo[t];

@@ -116,24 +116,26 @@ template <typename T, int NT, int NV> struct RowPart {
   }
 };
 
-// stores a part of a row: f(i, q) is element q of vector i, single what the single element becomes; PAST: past the caches
+// stores a vector of a row: f(q) is its element q; PAST: past the caches
+template <typename T, bool PAST, class F> __device__ __forceinline__ void store_vector(T* out, F f) {
+  typedef u32x4 u32x4_any __attribute__((aligned(2)));
+  u32x4 w;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if constexpr (sizeof(T) == 4) w[q] = __float_as_uint(f(q));
+    else w[q] = bf16_pair(f(2 * q), f(2 * q + 1));
+  }
+  u32x4_any* const to = reinterpret_cast<u32x4_any*>(out);              // (dz may be aligned otherwise)
+  if constexpr (PAST) __builtin_nontemporal_store(w, to); else *to = w;
+}
+
+// stores a part of a row: f(i, q) is element q of vector i, single what the single element becomes
 template <typename T, int NT, int NV, bool PAST = false, class F>
 __device__ __forceinline__ void store_part(T* out, const RowPart<T, NT, NV>& p, int v0, int head, int classes, float single, F f) {
-  typedef u32x4 u32x4_any __attribute__((aligned(2)));
-  constexpr int VPL = 16 / (int)sizeof(T);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = RowPart<T, NT, NV>::col(v0, i, head);
-    if (c + VPL <= classes) {
-      u32x4 w;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if constexpr (sizeof(T) == 4) w[q] = __float_as_uint(f(i, q));
-        else w[q] = bf16_pair(f(i, 2 * q), f(i, 2 * q + 1));
-      }
-      u32x4_any* const to = reinterpret_cast<u32x4_any*>(out + c);      // (dz may be aligned otherwise)
-      if constexpr (PAST) __builtin_nontemporal_store(w, to); else *to = w;
-    }
+    if (c + RowPart<T, NT, NV>::VPL <= classes) store_vector<T, PAST>(out + c, [&](int q) { return f(i, q); });
     if (i % 2) __builtin_amdgcn_sched_barrier(0);
   }
   if (p.single_col >= 0) st_elem(out + p.single_col, single);

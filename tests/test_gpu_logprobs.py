@@ -166,7 +166,7 @@ def call_dense(ctx, dtype, z, k, T=1.0, tokens=None, names=("logprob", "entropy"
 
 
 # (every size of row that a workgroup keeps, and rows in parts; widths that are no whole vectors)
-WIDTHS = [1, 2, 7, 9, 64, 255, 1000, 2047, 2048, 2049, 4100, 8191, 8200, 16390, 33001, 65536, 65600, 131071, 131080, 150001]
+WIDTHS = [1, 2, 7, 9, 64, 255, 1000, 2047, 2048, 2049, 4100, 8191, 8200, 16390, 33001, 52900, 53100, 65536, 65600, 105900, 131071, 131080, 150001]
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
