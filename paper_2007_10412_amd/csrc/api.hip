@@ -1545,20 +1545,25 @@ struct HeadCall {
 // 300 x 1000 x 20000 32, 23, 29; 100 x 1000 x 5000 29, 16, 13 (called alone in a loop).  The prices order the tiles rather than
 // foretell a time: they are 0.97 to 1.45 of what these take, but 45 us for x W of 4096 x 4096 x 1000, which takes 46 alone and 55
 // among the kernels of its step.  The worst choice among 11 measured is 6 % from the best (fp32 1500 x 512 x 2000, 46.4 in 128-row tiles, 43.7 in 64).
+// 192-row tiles are for products that leave what an entropy needs, up to two rounds of them: with the other tiles / with them x W of
+// 192 x 4096 x 32000 with lists of 20 88 / 75, 384 x 4096 x 32000 147 / 131, 180 x 1024 x 50257 84 / 79, 300 x 2048 x 16000 41 / 43.
 // All rows are planned for: how many of them have a target only the device knows.
 struct HeadPlan { int tile, k_split, splits; };
 static HeadPlan head_plan(int dtype, int epi, int64_t M, int64_t N, int64_t K, bool may_split) {
   struct Kind { int dtype, tile, cols; double fill_us, slice_us, alone_us, end_us; };
   static const Kind kinds[] = {{kBF16, 256, 256, 3.0, 1.60, 1.00, 13.0}, {kBF16, 128, 128, 4.5, 0.58, 0.55, 2.5}, {kBF16, 64, 128, 4.5, 0.41, 0.40, 2.0},
+                               {kBF16, 192, 128, 4.5, 0.78, 0.78, 5.0},
                                {kF32, 128, 128, 6.0, 1.98, 2.00, 2.5}, {kF32, 64, 128, 6.0, 1.04, 1.15, 2.0}};
   const int bk = dtype == kBF16 ? 64 : 32;
+  const bool vocab = epi == kEpiVocab || epi == kEpiLogprob;
   HeadPlan best{128, 0, 1};
   double best_us = 1e30;
   for (const Kind& k : kinds) {
     if (k.dtype != dtype || (k.tile == 64 && epi == kEpiHeadW && dtype == kBF16)) continue;
-    const double end_us = k.end_us + (k.tile == 256 && epi == kEpiVocab ? 7.0 : 0.0);
+    const double end_us = k.end_us + (k.tile == 256 && vocab ? 7.0 : 0.0);
     const int64_t tiles = ((M + k.tile - 1) / k.tile) * ((N + k.cols - 1) / k.cols);
-    for (int s = 1; s <= 64 && (s == 1 || (may_split && K / s >= 128 && !(k.tile == 256 && epi == kEpiVocab))); ++s) {
+    if (k.tile == 192 && (epi != kEpiLogprob || tiles > 512)) continue;
+    for (int s = 1; s <= 64 && (s == 1 || (may_split && K / s >= 128 && !(k.tile >= 192 && vocab))); ++s) {
       const int64_t k_split = ((K + s - 1) / s + 63) / 64 * 64;
       const int splits = (int)((K + k_split - 1) / k_split);
       const double each = (double)((tiles * splits + 255) / 256), full = std::min(1.0, (double)(tiles * splits) / 256.0);
@@ -1676,7 +1681,7 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   const int64_t w_ld = vp8 == d_out && (reinterpret_cast<uintptr_t>(h.W) & 15) == 0 ? d_out : vp;
   RAD_TRY(head_padded(c, WS_HEADW, dtype, h.W, d_in, d_out, w_ld, &W));
 
-  const HeadPlan fwd = head_plan(dtype, kEpiVocab, piece, d_out, d_in, true);
+  const HeadPlan fwd = head_plan(dtype, lp ? kEpiLogprob : kEpiVocab, piece, d_out, d_in, true);
   const int part = fwd.splits > 1 ? 64 : head_part(fwd.tile), parts = (d_out + part - 1) / part;
   const int first_ld = parts + 1, list_k = teacher ? teacher->k : 1;
   const size_t first_bytes = teacher ? ((size_t)rows * first_ld * 2 + 255) / 256 * 256 : 0;
@@ -1922,7 +1927,7 @@ extern "C" rad_status rad_linear_logprobs(rad_ctx* c, const rad_layer* L, const 
   const void* Wp = nullptr;
   const int64_t w_ld = vp8 == d_out && (reinterpret_cast<uintptr_t>(W) & 15) == 0 ? d_out : vp;
   RAD_TRY(head_padded(c, WS_HEADW, dtype, W, d_in, d_out, w_ld, &Wp));
-  const HeadPlan plan = head_plan(dtype, kEpiVocab, piece, d_out, d_in, true);
+  const HeadPlan plan = head_plan(dtype, kEpiLogprob, piece, d_out, d_in, true);
   const int part = plan.splits > 1 ? 64 : head_part(plan.tile), parts = (d_out + part - 1) / part;
   char* ws = nullptr;
   RAD_TRY(ws_get(c, WS_ROWLOSS, 256 + (size_t)piece * (12 * (size_t)parts + 8), reinterpret_cast<void**>(&ws)));

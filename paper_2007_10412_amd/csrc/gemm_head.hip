@@ -63,6 +63,9 @@ template <typename T, int AKIND, int BKIND, int EPI> hipError_t run_head(const G
       return run_tile<T, AKIND, BKIND, EPI, 128, 4>(g, st);
   }
   if (g.head.tile == 128) return run_tile<T, AKIND, BKIND, EPI, 128, 2>(g, st);
+  // Alone on its CU, for up to two rounds of tiles: us with 128 / 192 rows a tile, 2048 x 32000 with lists of 5, 130 rows 48.9 / 44.4, 190
+  // 51.9 / 47.1, 300 84.8 / 78.6, but 250 58.3 / 78 (as many tiles of either), and 300 x 2048 x 128000, eight rounds, 238 / 271.
+  if constexpr (EPI == kEpiLogprob && sizeof(T) == 2) { if (g.head.tile == 192) return run_tile<T, AKIND, BKIND, EPI, 192, 3>(g, st); }
   if constexpr (AKIND == kOpK || sizeof(T) == 4) { if (g.head.tile == 64) return run_tile<T, AKIND, BKIND, EPI, 64, 3>(g, st); }
   return hipErrorInvalidValue;
 }

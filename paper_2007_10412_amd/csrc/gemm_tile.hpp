@@ -1,4 +1,4 @@
-// Products of a layer under a loss over its classes (HeadArgs), bf16 and fp32: 128 x 128 or 64 x 128 tiles, operands straight
+// Products of a layer under a loss over its classes (HeadArgs), bf16 and fp32: tiles of 64, 128 or 192 rows x 128, operands straight
 // into LDS as in gemm_bf16_dma.hpp, slices of 128 bytes of K (64 bf16, 32 fp32) in a ring of S stages, S - 1 of them on their way.
 //
 // bf16: the 256 x 256 kernel needs 256 tiles to give every CU work.  100 rows x 1024 x 10000 are 40 of them, for whose 16

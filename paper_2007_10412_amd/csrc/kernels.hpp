@@ -116,7 +116,7 @@ struct GemmArgs {
 
 // dtype: operand element type; returns hipErrorInvalidValue for combinations
 // without a kernel.  `name` (out, may be null) receives the kernel's label.
-// (head products: tile is the height of the tiles, 64, 128 or 256; the part of a row that kEpiVocab's statistics are for is
+// (head products: tile is the height of the tiles, 64, 128, 256 or, for bf16's kEpiLogprob, 192; the part of a row that kEpiVocab's statistics are for is
 // head_part(tile) columns wide)
 inline int head_part(int tile) { return tile == 256 ? 128 : 64; }
 // dX and dW of such a layer in one launch: tiles of 64 or 128 rows, and of 128

@@ -470,7 +470,7 @@ def check_linear(ctx, dtype, rows, d_in, classes, k, bias=False, ignored=0.0, T=
 
 SHAPES = [(1, 1, 1), (1, 5, 3), (3, 7, 1), (5, 64, 33), (150, 300, 10), (64, 256, 1000), (130, 129, 131), (257, 520, 1003),
           (300, 512, 4096), (1000, 72, 2500), (512, 1024, 8192), (17, 1030, 20011), (513, 260, 25601), (700, 512, 32000),
-          (20, 129, 30000), (1025, 1000, 8200), (1, 2048, 50257), (2, 300, 128000)]
+          (20, 129, 30000), (1025, 1000, 8200), (1, 2048, 50257), (2, 300, 128000), (190, 1000, 28003), (381, 1000, 25009)]
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
