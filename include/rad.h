@@ -402,7 +402,8 @@ rad_status rad_token_logprobs_grad(rad_ctx* ctx, const void* logits, int64_t row
  * no ReLU), which are formed in fp32 and not kept.  Rows go through in pieces, of
  * which the logits (fp32, where top_k > 0) and the rows of x have at most 2 GiB
  * each, or of 256 rows if those are more.  Context workspaces: the logits of a
- * piece where top_k > 0; copies of W and of a piece of x as for rad_linear_ce; 12
+ * piece where top_k > 0; copies of W and of a piece of x as for rad_linear_ce (none
+ * for 1 to 4 rows, in fp32 8, of 4096 classes or more, which read W as it lies); 12
  * bytes per row and 64 classes of a piece, 8 per row of it; partial sums where the
  * product has few tiles.  Limits of the layer as for rad_linear_ce. */
 rad_status rad_linear_logprobs(rad_ctx* ctx, const rad_layer* layer, const void* x, const void* W, const float* bias,

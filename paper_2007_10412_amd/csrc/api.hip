@@ -1909,6 +1909,20 @@ extern "C" rad_status rad_token_logprobs_grad(rad_ctx* c, const void* logits, in
   return logprob_rows(c, a);
 }
 
+// Few rows without matrix instructions (launch_few_rows) or with; copied: the latter would need a copy of W, whose rows are not whole 16-byte
+// vectors.  us with matrix instructions / without: bf16 1 x 4096 x 128000 193 / 171, 4 x 4096 x 128000 195 / 182, 1 x 2048 x 8192 17.2 / 13.3, 4 x
+// 2048 x 16384 20.6 / 18.9, but 4 x 4096 x 16384 36.1 / 39.8, 4 x 512 x 50000 15.6 / 19.8, 8 x 4096 x 128000 205 / 404 (unpacking and adding
+// then take longer than W's way from memory); fp32 1 x 4096 x 128000 503 / 341, 8 x 4096 x 128000 507 / 405, but 8 x 2048 x 4096 21.4 / 22.1.
+// Where a workgroup has far more than half a megabyte of W and most CUs have nothing, K is better split: bf16 1 x 4096 x 1000 20.8 / 23.5, 1 x 8192 x
+// 4096 25.3 / 34.4.  With a copy: bf16 1 x 1024 x 50257 55.5 / 28.0, 4 x 4096 x 30001 138 / 63, 1 x 8192 x 10007 91 / 74, fp32 1 x 4096 x 8191 94 / 40.
+static bool few_rows_pay(int dtype, int64_t rows, int64_t d_in, int64_t d_out, bool copied) {
+  if (rows > (dtype == kBF16 ? 4 : kFewRows) || d_out < 64) return false;
+  if (copied && d_out >= 4096) return true;
+  if (rows > 4 && d_out < 8192) return d_in <= 1024;
+  if (rows > 2 && dtype == kBF16) return d_in <= 2048 ? d_out <= 32768 : d_out >= 65536;
+  return d_in <= 2048 || d_out >= (dtype == kBF16 ? 16384 : 8192);
+}
+
 extern "C" rad_status rad_linear_logprobs(rad_ctx* c, const rad_layer* L, const void* x, const void* W, const float* bias,
                                           const rad_logprobs* out) {
   if (!c) return RAD_ERR_NULL;
@@ -1924,10 +1938,11 @@ extern "C" rad_status rad_linear_logprobs(rad_ctx* c, const rad_layer* L, const 
   int64_t piece = (int64_t)(kPieceBytes / (size_t)std::max(k ? vp * 4 : vp * esz, dp * esz));
   piece = std::max<int64_t>(std::min<int64_t>(piece / 256 * 256, 1 << 19), 256);
   if (piece > rows) piece = rows;
-  const void* Wp = nullptr;
+  const void* Wp = W;
   const int64_t w_ld = vp8 == d_out && (reinterpret_cast<uintptr_t>(W) & 15) == 0 ? d_out : vp;
-  RAD_TRY(head_padded(c, WS_HEADW, dtype, W, d_in, d_out, w_ld, &Wp));
-  const HeadPlan plan = head_plan(dtype, kEpiLogprob, piece, d_out, d_in, true);
+  const bool few = few_rows_pay(dtype, rows, d_in, d_out, w_ld != d_out);
+  if (!few) RAD_TRY(head_padded(c, WS_HEADW, dtype, W, d_in, d_out, w_ld, &Wp));
+  const HeadPlan plan = few ? HeadPlan{64, 0, 1} : head_plan(dtype, kEpiLogprob, piece, d_out, d_in, true);
   const int part = plan.splits > 1 ? 64 : head_part(plan.tile), parts = (d_out + part - 1) / part;
   char* ws = nullptr;
   RAD_TRY(ws_get(c, WS_ROWLOSS, 256 + (size_t)piece * (12 * (size_t)parts + 8), reinterpret_cast<void**>(&ws)));
@@ -1944,34 +1959,40 @@ extern "C" rad_status rad_linear_logprobs(rad_ctx* c, const rad_layer* L, const 
   for (int64_t r0 = 0; r0 < rows; r0 += piece) {
     const int n = (int)std::min<int64_t>(piece, rows - r0);
     const void* xp = nullptr;
-    RAD_TRY(head_padded(c, WS_HEADX, dtype, static_cast<const char*>(x) + r0 * d_in * esz, n, d_in, dp, &xp));
+    if (!few) RAD_TRY(head_padded(c, WS_HEADX, dtype, static_cast<const char*>(x) + r0 * d_in * esz, n, d_in, dp, &xp));
     const VocabTargets t{out->token ? out->token + r0 : nullptr, nullptr, nullptr, nullptr, nullptr, 1, T, nullptr, inv_count, 1.f, nullptr};
     const int64_t tiles = (int64_t)((n + plan.tile - 1) / plan.tile) * ((d_out + 127) / 128) * plan.splits;
     const bool own_list = n <= kOwnListRows && plan.tile != 256 && (dtype == kBF16 ? n <= 1024 || tiles <= 640 : tiles <= 768);
-    if (!own_list)
+    if (!few && !own_list)
       HIP_TRY(c, timed(c, "row_list", [&](const char**) { return launch_row_list(t, n, d_out, list, live, inv_count, common, c->stream); }));
-    GemmArgs g = gemm_zero();
-    g.M = n; g.N = d_out; g.K = d_in;
-    g.A = xp; g.lda = dp; g.B = Wp; g.ldb = w_ld;
-    g.bias = bias;
-    HeadArgs& a = g.head;
-    a.live = live; a.row_map = list; a.rows = n; a.n_load = (int)vp8;
-    if (own_list) { a.list_out = list; a.live_out = live; a.inv_count_out = inv_count; a.common_out = common; }
-    a.lead = 1.f;
-    a.c = 1.44269504088896340736f / T;
-    a.stats = stats; a.stats_ld = piece; a.spread = spread;
-    a.labels = t.labels; a.k = 1; a.target = target;
-    if (dtype == kF32 || plan.splits > 1) { g.y = z; g.ldy = vp; }
-    else { a.z32 = static_cast<float*>(z); a.z32_ld = vp; }
-    if (plan.splits > 1) {
-      g.k_split = plan.k_split; g.k_splits = plan.splits;
-      g.ldc = vp;
-      g.split_stride = (int64_t)n * vp;
-      RAD_TRY(ws_get(c, WS_SPLITK, (size_t)plan.splits * g.split_stride * 4, &g.C));
+    if (few) {
+      const FewRows f{dtype, n, d_in, d_out, x, d_in, W, d_out, bias, t.labels, 1.44269504088896340736f / T, list, live, stats, spread, piece, target,
+                      static_cast<float*>(z), vp};
+      HIP_TRY(c, timed(c, "few_rows", [&](const char**) { return launch_few_rows(f, c->stream); }));
+    } else {
+      GemmArgs g = gemm_zero();
+      g.M = n; g.N = d_out; g.K = d_in;
+      g.A = xp; g.lda = dp; g.B = Wp; g.ldb = w_ld;
+      g.bias = bias;
+      HeadArgs& a = g.head;
+      a.live = live; a.row_map = list; a.rows = n; a.n_load = (int)vp8;
+      if (own_list) { a.list_out = list; a.live_out = live; a.inv_count_out = inv_count; a.common_out = common; }
+      a.lead = 1.f;
+      a.c = 1.44269504088896340736f / T;
+      a.stats = stats; a.stats_ld = piece; a.spread = spread;
+      a.labels = t.labels; a.k = 1; a.target = target;
+      if (dtype == kF32 || plan.splits > 1) { g.y = z; g.ldy = vp; }
+      else { a.z32 = static_cast<float*>(z); a.z32_ld = vp; }
+      if (plan.splits > 1) {
+        g.k_split = plan.k_split; g.k_splits = plan.splits;
+        g.ldc = vp;
+        g.split_stride = (int64_t)n * vp;
+        RAD_TRY(ws_get(c, WS_SPLITK, (size_t)plan.splits * g.split_stride * 4, &g.C));
+      }
+      a.tile = plan.tile;
+      RAD_TRY(run_gemm_call(c, dtype, kOpK, kOpMN, kEpiLogprob, g));
+      if (plan.splits > 1) HIP_TRY(c, timed(c, "vocab_join", [&](const char**) { return launch_vocab_join(kF32, true, g, c->stream); }));
     }
-    a.tile = plan.tile;
-    RAD_TRY(run_gemm_call(c, dtype, kOpK, kOpMN, kEpiLogprob, g));
-    if (plan.splits > 1) HIP_TRY(c, timed(c, "vocab_join", [&](const char**) { return launch_vocab_join(kF32, true, g, c->stream); }));
     LogprobFinish f;
     std::memset(&f, 0, sizeof(f));
     f.list = list; f.live = live; f.rows = n; f.classes = d_out; f.parts = parts; f.part = part; f.temperature = T;

@@ -387,6 +387,21 @@ struct LogprobFinish {
   int k; int32_t* top_index; float* top_logprob;
 };
 hipError_t launch_logprob_finish(const LogprobFinish& a, hipStream_t st);
+// The product before it for up to kFewRows rows, W [K][w_ld] and x [rows][x_ld] of any alignment, 16 classes or more: the places' list, what
+// kEpiLogprob leaves in parts of 64 classes and, where z is not null, the logits in fp32 (rows z_ld apart, -infinity from N to z_ld, at most the
+// next multiple of 64).
+constexpr int kFewRows = 8;
+struct FewRows {
+  int dtype, rows, K, N;
+  const void* x; int64_t x_ld; const void* W; int64_t w_ld; const float* bias;
+  const int32_t* token;
+  float c;
+  int32_t* list; int32_t* live;
+  float* stats; float* spread; int64_t stats_ld;
+  float* target;
+  float* z; int64_t z_ld;
+};
+hipError_t launch_few_rows(const FewRows& a, hipStream_t st);
 
 // out (bf16) = beta out + in (fp32), n elements
 hipError_t launch_cast_add(const float* in, uint16_t* out, int64_t n, int beta, hipStream_t st);

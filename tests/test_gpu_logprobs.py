@@ -485,6 +485,23 @@ def test_linear(dtype, rows, d_in, classes):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 8])
+@pytest.mark.parametrize("d_in,classes", [(1, 64), (31, 65), (32, 127), (33, 128), (100, 129), (512, 1000), (700, 4099), (2049, 20011), (1030, 16384),
+                                          (5000, 4097), (2048, 33000)])
+def test_linear_few_rows(dtype, rows, d_in, classes):
+    with Ctx() as ctx:
+        check_linear(ctx, dtype, rows, d_in, classes, 5, bias=rows % 2 == 0, ignored=0.4 if rows > 1 else 0.0)
+        check_linear(ctx, dtype, rows, d_in, classes, min(64, classes), bias=True, T=0.7, no_tokens=True)
+        check_linear(ctx, dtype, rows, d_in, classes, 0, grid=False, T=1.5)
+
+
+@pytest.mark.parametrize("dtype,rows,d_in,classes", [(0, 8, 4096, 8192), (1, 4, 4096, 65536), (1, 1, 4096, 16384), (0, 3, 2048, 16000)])
+def test_linear_few_rows_of_large_layers(dtype, rows, d_in, classes):
+    with Ctx() as ctx:
+        check_linear(ctx, dtype, rows, d_in, classes, 20, bias=True, ignored=0.3 if rows > 1 else 0.0)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("masked", [-math.inf, -3.0e38])
 @pytest.mark.parametrize("rows,d_in,classes", [(3, 64, 1000), (300, 256, 4096), (600, 256, 20000)])
 def test_linear_masked_classes(dtype, masked, rows, d_in, classes):
