@@ -135,7 +135,11 @@ int64_t rad_fixed_k(double p, int64_t d);
  * default stream) on the current device.  Allocates workspaces lazily.  A
  * workspace grows when a call needs a larger one, which frees the old one: a
  * HIP graph recorded from calls of a context refers to the workspaces of that
- * time, so make the context's largest calls before recording.  Calls that only
+ * time, so make the context's largest calls before recording, and run such
+ * graphs and the context's calls one after the other: they share them.  Calls
+ * that count their workgroups (rad_gradient_norm, rad_clip_gradients, rows of
+ * rad_token_logprobs in parts) refuse to be recorded before one of them has been
+ * made.  Calls that only
  * gain by a workspace (the masked gradient of bf16 layers with ReLU, the split
  * rows of dW from the store) do without one that cannot be had: while the
  * stream is being captured, or where the device's memory is used up. */
@@ -402,7 +406,7 @@ rad_status rad_token_logprobs_grad(rad_ctx* ctx, const void* logits, int64_t row
  * no ReLU), which are formed in fp32 and not kept.  Rows go through in pieces, of
  * which the logits (fp32, where top_k > 0) and the rows of x have at most 2 GiB
  * each, or of 256 rows if those are more.  Context workspaces: the logits of a
- * piece where top_k > 0; copies of W and of a piece of x as for rad_linear_ce (none
+ * piece where top_k > 0; copies of W and of a piece of x as for rad_linear_ce (of W none
  * for 1 to 4 rows, in fp32 8, of 4096 classes or more, which read W as it lies); 12
  * bytes per row and 64 classes of a piece, 8 per row of it; partial sums where the
  * product has few tiles.  Limits of the layer as for rad_linear_ce. */
@@ -548,7 +552,8 @@ rad_status rad_clip_gradients(rad_ctx* ctx, int32_t n_tensors, const int64_t* co
 /* rad_optimizer_step with *scale g in the place of g (*scale: DEVICE fp32, as
  * rad_gradient_norm leaves it; g is not changed).  A scale of 0 leaves
  * parameters, moments and master copies as they are: the step of a gradient
- * whose norm is not finite is skipped, without the host knowing. */
+ * whose norm is not finite is skipped, without the host knowing.  A scale that
+ * lies in a tensor that is stepped is refused (RAD_ERR_PARAM). */
 rad_status rad_optimizer_step_scaled(rad_ctx* ctx, const rad_optimizer* opt, int64_t t, int32_t dtype,
                                      int32_t n_tensors, const int64_t* counts, void* const* params,
                                      const void* const* grads, void* const* m, void* const* v,

@@ -113,10 +113,20 @@ static rad_status ws_get(rad_ctx* c, int which, size_t bytes, void** out) {
 // Counts of workgroups that are done, one for each thing that they share: zero before and after every call.
 enum { kDoneNorm = 256, kDoneWords = 512 };             // rows that are split, then others
 static rad_status ws_counters(rad_ctx* c, uint32_t** out) {
-  const bool fresh = !c->ws[c->on_side][WS_DONE];
+  void*& ws = c->ws[c->on_side][WS_DONE];
+  *out = static_cast<uint32_t*>(ws);
+  if (ws) return RAD_OK;
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(c->stream, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone) {
+    (void)hipGetLastError();                             // (a recorded fill would not have run yet when a call outside the graph counts)
+    return fail(c, RAD_ERR_DEVICE, "a context's first such call cannot be recorded into a graph");
+  }
   RAD_TRY(ws_get(c, WS_DONE, kDoneWords * 4, reinterpret_cast<void**>(out)));
-  if (fresh) HIP_TRY(c, launch_fill_u32(*out, 0u, kDoneWords, c->stream));
-  return RAD_OK;
+  const hipError_t e = launch_fill_u32(*out, 0u, kDoneWords, c->stream);
+  if (e == hipSuccess) return RAD_OK;
+  (void)hipFree(ws);
+  ws = nullptr; c->ws_bytes[c->on_side][WS_DONE] = 0;
+  return hip_fail(c, e, "launch_fill_u32");
 }
 
 // Whether a workspace holds `bytes`, grown where that is possible: not while the stream is being captured, not beyond the
@@ -1863,8 +1873,9 @@ static rad_status check_logprob_grads(rad_ctx* c, const int32_t* token, double T
 }
 
 static rad_status logprob_rows(rad_ctx* c, LogprobRows a) {
-  RAD_TRY(ws_get(c, WS_ROWLOSS, logprob_rows_bytes(a), &a.ws));
-  if (logprob_rows_bytes(a)) RAD_TRY(ws_counters(c, &a.done));
+  const size_t bytes = logprob_rows_bytes(a);
+  if (bytes && !a.dz) RAD_TRY(ws_counters(c, &a.done));  // (a row's parts; a gradient's are ordered by their launches)
+  RAD_TRY(ws_get(c, WS_ROWLOSS, bytes, &a.ws));
   HIP_TRY(c, timed(c, a.dz ? "logprob_grad" : "logprob_rows", [&](const char**) { return launch_logprob_rows(a, c->stream); }));
   return RAD_OK;
 }
@@ -2030,6 +2041,14 @@ static bool tensors_apart(std::vector<TensorSpan>* spans) {
   }
   return true;
 }
+static rad_status make_spans(rad_ctx* c, size_t n, std::vector<TensorSpan>* spans) {
+  try {
+    spans->reserve(n);
+  } catch (const std::exception&) {
+    return fail(c, RAD_ERR_SHAPE, "too many tensors");
+  }
+  return RAD_OK;
+}
 static void add_span(std::vector<TensorSpan>* spans, const void* p, int64_t n, int size, bool out) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(p);
   if (p && n > 0) spans->push_back({at, at + (uintptr_t)n * size, out});
@@ -2070,12 +2089,17 @@ static rad_status optimizer_step(rad_ctx* c, const rad_optimizer* opt, int64_t t
   l.n = 0;
   // Tensors that share memory are stepped one after the other, as they are listed; others side by side.
   std::vector<TensorSpan> spans;
-  spans.reserve((size_t)n_tensors * 5);
+  RAD_TRY(make_spans(c, (size_t)n_tensors * 5 + 1, &spans));
   for (int i = 0; i < n_tensors; ++i) {
     add_span(&spans, grads[i], counts[i], 4, false);
     add_span(&spans, dtype == RAD_BF16 ? master[i] : params[i], counts[i], 4, true);
     if (dtype == RAD_BF16) add_span(&spans, params[i], counts[i], 2, true);
     if (adam) { add_span(&spans, m[i], counts[i], 4, true); add_span(&spans, v[i], counts[i], 4, true); }
+  }
+  if (scale) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(scale);
+    for (const TensorSpan& s : spans)
+      if (s.out && s.from < at + 4 && at < s.to) return fail(c, RAD_ERR_PARAM, "the scale lies in a tensor that is stepped");
   }
   const int together = tensors_apart(&spans) ? kStepTensors : 1;
   int64_t elements = 0;                                  // of the tensors that wait for their launch
@@ -2135,6 +2159,8 @@ static int gradient_size(const int32_t* dtypes, int i) { return dtypes && dtypes
 
 constexpr size_t kNormHead = 256;                        // WS_NORM: a scale, then partial sums
 static rad_status norm_workspace(rad_ctx* c, int32_t n_tensors, char** ws) {
+  uint32_t* done = nullptr;
+  RAD_TRY(ws_counters(c, &done));                        // (first, as it may refuse)
   return ws_get(c, WS_NORM, kNormHead + ((size_t)n_tensors / kNormTensors + 1) * kNormBlocks * 8, reinterpret_cast<void**>(ws));
 }
 
@@ -2169,7 +2195,7 @@ extern "C" rad_status rad_gradient_norm(rad_ctx* c, int32_t n_tensors, const int
   RAD_TRY(check_gradients(c, n_tensors, counts, grads, dtypes, max_norm));
   if (!norm && !scale) return fail(c, RAD_ERR_NULL, "no output asked for");
   std::vector<TensorSpan> spans;
-  spans.reserve((size_t)n_tensors + 2);
+  RAD_TRY(make_spans(c, (size_t)n_tensors + 2, &spans));
   for (int i = 0; i < n_tensors; ++i) add_span(&spans, grads[i], counts[i], gradient_size(dtypes, i), false);
   add_span(&spans, norm, 1, 4, true);
   add_span(&spans, scale, 1, 4, true);
@@ -2186,7 +2212,7 @@ extern "C" rad_status rad_clip_gradients(rad_ctx* c, int32_t n_tensors, const in
   RAD_TRY(check_gradients(c, n_tensors, counts, grads, dtypes, max_norm));
   if (n_tensors > 0 && !clipped) return fail(c, RAD_ERR_NULL, "null argument");
   std::vector<TensorSpan> spans;
-  spans.reserve((size_t)n_tensors * 2 + 1);
+  RAD_TRY(make_spans(c, (size_t)n_tensors * 2 + 1, &spans));
   for (int i = 0; i < n_tensors; ++i) {
     if (counts[i] > 0 && !clipped[i]) return fail(c, RAD_ERR_NULL, "null tensor pointer");
     if (clipped[i] != grads[i]) add_span(&spans, grads[i], counts[i], gradient_size(dtypes, i), false);

@@ -263,6 +263,24 @@ def test_captured_and_other_stream():
         del graph
 
 
+def test_first_norm_is_not_recorded():
+    import torch
+    from paper_2007_10412_amd import binding as B
+    stream = torch.cuda.Stream()
+    g, n = torch.full((1000,), 2.0, device="cuda"), torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    with Ctx(stream) as ctx:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            torch.zeros(1, device="cuda").add_(1)
+            for call in (lambda: B.rad_gradient_norm(ctx, [g], 1.0, norm=n), lambda: B.rad_clip_gradients(ctx, [g], 1.0)):
+                with pytest.raises(B.RadError, match="recorded"):
+                    call()
+        B.rad_gradient_norm(ctx, [g], 1.0, norm=n)
+        B.rad_ctx_synchronize(ctx)
+        assert abs(float(n) - math.sqrt(4000.0)) <= 2 * U * math.sqrt(4000.0)
+
+
 def test_refusals():
     import torch
     from paper_2007_10412_amd import binding as B
@@ -280,6 +298,7 @@ def test_refusals():
                 (lambda: B.rad_clip_gradients(ctx, [g], 1.0, norm=g[:1]), B.RAD_ERR_PARAM),
                 (lambda: B.rad_clip_gradients(ctx, [g, h], 1.0, clipped=[h, g]), B.RAD_ERR_PARAM),
                 (lambda: B.rad_clip_gradients(ctx, [g[:60]], 1.0, clipped=[g[4:]]), B.RAD_ERR_PARAM),
+                (lambda: B.rad_optimizer_step_scaled(ctx, B.make_optimizer(B.RAD_SGD, 1e-2), 1, 0, [g], [h], g[63:]), B.RAD_ERR_PARAM),
                 (lambda: B.rad_optimizer_step_scaled(ctx, B.make_optimizer(B.RAD_SGD, 1e-2), 1, 7, [g], [h], n), B.RAD_ERR_PARAM)):
             with pytest.raises(B.RadError) as e:
                 call()

@@ -299,6 +299,39 @@ def test_many_short_rows(dtype):
         check_answer(call_dense(ctx, dtype, z, 3, 1.0, tokens), Row(z.double(), 1.0), tokens, 3, "short rows")
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_widest_rows(dtype):
+    """As many classes as a call may have, forward and backward."""
+    import torch
+    gen = gen_for(10, dtype)
+    z = (3 * torch.randn(1, 2 ** 24, device="cuda", generator=gen)).to(torch_dtype(dtype))
+    tokens, a, h = tokens_for(1, 2 ** 24, gen), torch.randn(1, device="cuda", generator=gen), torch.randn(1, device="cuda", generator=gen)
+    with Ctx() as ctx:
+        check_answer(call_dense(ctx, dtype, z, 256, 1.0, tokens), Row(z.double(), 1.0), tokens, 256, "2^24 classes")
+        check_dense_grad(ctx, dtype, z, tokens, a, h, tag="2^24 classes")
+
+
+def test_offsets_beyond_32_bits():
+    """1030 rows of 2^21 + 8 classes, 4.3 GB of bf16: the first rows and the last."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen = gen_for(12)
+    rows, classes = 1030, 2 ** 21 + 8
+    z = torch.randn(rows, classes, device="cuda", generator=gen, dtype=torch.bfloat16)
+    tokens = tokens_for(rows, classes, gen)
+    a, h = torch.randn(rows, device="cuda", generator=gen), torch.randn(rows, device="cuda", generator=gen)
+    at = torch.tensor([0, 1, 1027, 1028, 1029], device="cuda")
+    row = Row(z[at].double(), 1.0)
+    with Ctx() as ctx:
+        out = call_dense(ctx, 1, z, 5, 1.0, tokens)
+        check_answer({n: t[at] for n, t in out.items()}, row, tokens[at], 5, "far rows")
+        dz = torch.full_like(z, 77.0)
+        B.rad_token_logprobs_grad(ctx, z, 1, dz, tokens=tokens, d_logprob=a, d_entropy=h)
+        B.rad_ctx_synchronize(ctx)
+        want, e, _ = row.grad(tokens[at], torch.ones(5, dtype=torch.bool, device="cuda"), a[at], h[at])
+        close(dz[at], want, e + HALF[1] * want.abs() * 1.01 + 1e-38 * 2 ** 8, "far rows' gradients")
+
+
 # ------------------------------------------------------------------ gradients of dense logits
 def check_dense_grad(ctx, dtype, z, tokens, a, h, T=1.0, in_place=False, tag=""):
     import torch
@@ -334,6 +367,17 @@ def test_dense_grad(dtype, rows, classes):
         check_dense_grad(ctx, dtype, z, tokens, a, None, T=0.7, in_place=True, tag="in place")
         check_dense_grad(ctx, dtype, z, None, None, h, T=2.0, tag="entropy")
         check_dense_grad(ctx, dtype, z, tokens, None, h, T=2.0, tag="entropy of some rows")
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_grad_of_many_short_rows(dtype):
+    import torch
+    gen = gen_for(11, dtype)
+    z = torch.randn(70001 * 5 + 1, device="cuda", generator=gen).to(torch_dtype(dtype))[1:].view(70001, 5)
+    tokens = tokens_for(70001, 5, gen, 0.2)
+    a, h = torch.randn(70001, device="cuda", generator=gen), torch.randn(70001, device="cuda", generator=gen)
+    with Ctx() as ctx:
+        check_dense_grad(ctx, dtype, z, tokens, a, h, tag="short rows")
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
@@ -495,7 +539,7 @@ def test_linear_few_rows(dtype, rows, d_in, classes):
         check_linear(ctx, dtype, rows, d_in, classes, 0, grid=False, T=1.5)
 
 
-@pytest.mark.parametrize("dtype,rows,d_in,classes", [(0, 8, 4096, 8192), (1, 4, 4096, 65536), (1, 1, 4096, 16384), (0, 3, 2048, 16000)])
+@pytest.mark.parametrize("dtype,rows,d_in,classes", [(1, 4, 4096, 1000), (0, 8, 8192, 2048), (1, 3, 8192, 4096), (0, 8, 4096, 8192), (1, 4, 4096, 65536), (1, 1, 4096, 16384), (0, 3, 2048, 16000)])
 def test_linear_few_rows_of_large_layers(dtype, rows, d_in, classes):
     with Ctx() as ctx:
         check_linear(ctx, dtype, rows, d_in, classes, 20, bias=True, ignored=0.3 if rows > 1 else 0.0)
@@ -587,6 +631,38 @@ def test_linear_grad(dtype, rows, d_in, classes):
     with Ctx() as ctx:
         check_linear_grad(ctx, dtype, rows, d_in, classes, bias=rows % 2 == 0, ignored=0.3 if rows > 4 else 0.0)
         check_linear_grad(ctx, dtype, rows, d_in, classes, kinds="h", no_tokens=True, T=1.5)
+
+
+def test_linear_gradients_against_differences():
+    """As for dense logits, in directions of x, W and the bias of +-1 in a fifth of their elements: logits move by |dz| <= 3 times the step of 2^-6
+    (8 inputs of size 1/2, weights of size 1/2), so 4 rows of third derivatives of the order of 2 leave 4 x 2 x 27 x 2^-12 / 6 = 0.009 at most beside
+    rounding's 2^-19 / 2^-6; a bound of 0.03 covers both."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen = gen_for(78)
+    rows, d_in, classes = 4, 8, 11
+    x, W = torch.randn(rows, d_in, device="cuda", generator=gen) / 2, torch.randn(d_in, classes, device="cuda", generator=gen) / 2
+    b = torch.randn(classes, device="cuda", generator=gen) / 2
+    tokens = tokens_for(rows, classes, gen)
+    a, h = torch.randn(rows, device="cuda", generator=gen), torch.randn(rows, device="cuda", generator=gen)
+    layer = B.make_layer(rows, d_in, classes, dtype=0, relu=False, has_bias=True)
+    with Ctx() as ctx:
+        def f(*at):
+            out = outputs(rows, 0)
+            B.rad_linear_logprobs(ctx, layer, *at, tokens=tokens, temperature=1.3, **out)
+            B.rad_ctx_synchronize(ctx)
+            return float((a.double() * out["logprob"].double() + h.double() * out["entropy"].double()).sum())
+        dX, dW, db = torch.empty_like(x), torch.empty_like(W), torch.empty_like(b)
+        B.rad_linear_logprobs_grad(ctx, layer, x, W, b, tokens=tokens, temperature=1.3, d_logprob=a, d_entropy=h, dX=dX, dW=dW, dbias=db)
+        B.rad_ctx_synchronize(ctx)
+        for i in range(30):
+            which = i % 3
+            t, g = ((x, dX), (W, dW), (b, db))[which]
+            v = torch.randint(0, 2, t.shape, device="cuda", generator=gen).float() * 2 - 1
+            v *= (torch.rand(t.shape, device="cuda", generator=gen) < 0.2)
+            s = 2.0 ** -6
+            up, down = ([u + e * s * v if j == which else u for j, u in enumerate((x, W, b))] for e in (1.0, -1.0))
+            assert abs((f(*up) - f(*down)) / (2 * s) - float((g.double() * v.double()).sum())) < 0.03, (i, which)
 
 
 @pytest.mark.parametrize("dtype,dw_dtype", [(0, 0), (1, 0), (1, 1)])
@@ -853,6 +929,28 @@ def test_captured(dtype):
                 for n in want[name]:
                     assert torch.equal(got[name][n], want[name][n]) and torch.equal(second[name][n], want[name][n]), (r, name, n)
         del graph, other
+
+
+def test_first_call_is_not_recorded():
+    """Rows in parts count their workgroups in memory that a context clears once: not within a graph."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    gen = gen_for(22)
+    stream = torch.cuda.Stream()
+    z = torch.randn(2, 140000, device="cuda", generator=gen)
+    out, want = outputs(2, 5, ("entropy", "top")), None
+    torch.cuda.synchronize()
+    with Ctx(stream) as ctx:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            torch.zeros(1, device="cuda").add_(1)
+            with pytest.raises(B.RadError, match="recorded"):
+                B.rad_token_logprobs(ctx, z, 0, **out)
+        B.rad_token_logprobs(ctx, z, 0, **out)
+        B.rad_ctx_synchronize(ctx)
+        check_answer(out, Row(z.double(), 1.0), None, 5, "after a refusal")
+        with torch.cuda.graph(graph.__class__(), stream=stream):
+            B.rad_token_logprobs(ctx, z, 0, **out)
 
 
 def test_two_contexts_at_once():
