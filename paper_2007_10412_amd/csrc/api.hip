@@ -2028,6 +2028,7 @@ extern "C" rad_status rad_linear_logprobs_grad(rad_ctx* c, const rad_layer* L, c
 
 // ------------------------------------------------------------------ parameter updates
 constexpr int64_t kMaxElements = (int64_t)1 << 35;       // of a call's gradients (a grid's chunks stay below 2^24)
+constexpr int64_t kPastBytes = (int64_t)512 << 20;       // read and written by a call: twice what the last-level cache holds
 
 // Memory of many tensors, some of it written: whether nothing that is written meets anything else.
 struct TensorSpan { uintptr_t from, to; bool out; };
@@ -2102,10 +2103,12 @@ static rad_status optimizer_step(rad_ctx* c, const rad_optimizer* opt, int64_t t
       if (s.out && s.from < at + 4 && at < s.to) return fail(c, RAD_ERR_PARAM, "the scale lies in a tensor that is stepped");
   }
   const int together = tensors_apart(&spans) ? kStepTensors : 1;
-  int64_t elements = 0;                                  // of the tensors that wait for their launch
+  int64_t elements = 0, all = 0;                         // of the tensors that wait for their launch, of all
+  for (int i = 0; i < n_tensors; ++i) all = std::min(all + counts[i], kMaxElements);
+  const bool past = all * (adam ? 28 : 12) >= kPastBytes;
   auto launch = [&]() -> rad_status {
     if (l.n == 0) return RAD_OK;
-    HIP_TRY(c, timed(c, adam ? "optim_adam" : "optim_sgd", [&](const char**) { return launch_optim(adam, &l, c->stream); }));
+    HIP_TRY(c, timed(c, adam ? "optim_adam" : "optim_sgd", [&](const char**) { return launch_optim(adam, past, &l, c->stream); }));
     l.n = 0; elements = 0;
     return RAD_OK;
   };
@@ -2227,6 +2230,8 @@ extern "C" rad_status rad_clip_gradients(rad_ctx* c, int32_t n_tensors, const in
   RAD_TRY(gradient_norm(c, n_tensors, counts, grads, dtypes, max_norm, ws, norm, scale));
   ClipList l;
   l.scale = scale;
+  int64_t bytes = 0;
+  for (int i = 0; i < n_tensors; ++i) bytes += counts[i] * 2 * gradient_size(dtypes, i);
   for (int i = 0; i < n_tensors;) {
     std::memset(l.bf16, 0, sizeof(l.bf16));
     for (l.n = 0; i < n_tensors && l.n < kClipTensors; ++i) {
@@ -2235,7 +2240,7 @@ extern "C" rad_status rad_clip_gradients(rad_ctx* c, int32_t n_tensors, const in
       l.g[l.n] = grads[i]; l.out[l.n] = clipped[i];
       l.count[l.n++] = counts[i];
     }
-    if (l.n > 0) HIP_TRY(c, timed(c, "clip", [&](const char**) { return launch_clip(&l, c->stream); }));
+    if (l.n > 0) HIP_TRY(c, timed(c, "clip", [&](const char**) { return launch_clip(bytes >= kPastBytes, &l, c->stream); }));
   }
   return RAD_OK;
 }

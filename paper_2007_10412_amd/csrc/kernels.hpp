@@ -208,8 +208,8 @@ struct OptimList {
   int64_t count[kStepTensors];
   int32_t chunk_end[kStepTensors];      // set by the launch
 };
-hipError_t launch_optim(bool adam, OptimList* l, hipStream_t st);
-// partial[first ..]: sums of squares, in fp64, of the elements that each workgroup takes; square_sums_blocks of them.  The launch
+hipError_t launch_optim(bool adam, bool past, OptimList* l, hipStream_t st);       // past the caches
+// partial[first ..]: sums of squares, in fp64, of the elements that each workgroup takes; *partials of them.  The launch
 // that is given norm or scale ends with *norm = sqrt(sum of partial[0 .. first + its own)), *scale = min(1, max_norm / norm), 0 where the norm is not
 // finite; *done is zero before it and after it.
 constexpr int kNormBlocks = 512;        // of one launch, at most (each counts itself done at one address, 10 ns after the one before)
@@ -230,7 +230,7 @@ struct ClipList {
   int32_t chunk_end[kClipTensors];      // set by the launch
   uint32_t bf16[kClipTensors / 32];
 };
-hipError_t launch_clip(ClipList* l, hipStream_t st);
+hipError_t launch_clip(bool past, ClipList* l, hipStream_t st);
 // db[c] = sum over b, y, x of g[b,c,y,x]; partial: [C][splits] scratch (workgroup (c, s) adds examples s, s + splits, ...)
 hipError_t launch_channel_sum(const float* g, int batch, int C, int HW, float* db, float* partial, int splits,
                               hipStream_t st);

@@ -351,8 +351,8 @@ __device__ __forceinline__ void join_parts(const LogprobRows& a, int row, int pa
 }
 
 // SPLIT: the row's vectors are dealt to gridDim.x workgroups, part_vecs each; the last one to be done joins what all have left
-// ONE: kAhead vectors a thread are all, and stay in registers
-template <typename T, int NT, bool SPLIT, bool ONE>
+// ONE: kAhead vectors a thread are all, and stay in registers; PAST: rows are read past the caches
+template <typename T, int NT, bool SPLIT, bool ONE, bool PAST>
 __global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a, int part_vecs) {
   typedef Stream<T> S;
   constexpr int VPL = S::VPL, G = groups_of<NT>();
@@ -394,7 +394,10 @@ __global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a, int par
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       raw[i] = u32x4{S::kEmpty, S::kEmpty, S::kEmpty, S::kEmpty};
-      if (v0 + i * NT < v_hi) raw[i] = *reinterpret_cast<const u32x4*>(zv + (int64_t)(v0 + i * NT) * VPL);
+      if (v0 + i * NT < v_hi) {
+        const u32x4* const from = reinterpret_cast<const u32x4*>(zv + (int64_t)(v0 + i * NT) * VPL);
+        if constexpr (PAST) raw[i] = __builtin_nontemporal_load(from); else raw[i] = *from;
+      }
     }
   };
   const bool list = a.k > 1;                             // (the first place alone takes no search)
@@ -617,7 +620,7 @@ __global__ __launch_bounds__(NT, NL > 0 ? 8 : 1) void logprob_grad_kernel(Logpro
   const float c = kLog2e / a.temperature, inv_t = 1.f / a.temperature;
   float* const st = SPLIT ? static_cast<float*>(a.ws) + (int64_t)row * gridDim.x * 3 : nullptr;
   Part p;
-  p.load(z, v0, head, classes);
+  p.template load<PAST>(z, v0, head, classes);
   auto lds_col = [&](int i) { return Part::col(NV * NT, i, head); };
   auto lds_vec = [&](int i) {                            // (each thread's own: no barriers)
     const u32x4 none = {S::kEmpty, S::kEmpty, S::kEmpty, S::kEmpty};
@@ -818,6 +821,13 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_finish_kernel(LogprobFin
 // ------------------------------------------------------------------ launches
 template <typename T> int64_t row_vectors(int classes) { return (int64_t)classes / (16 / (int)sizeof(T)) + 1; }   // (one for the single elements at the end)
 
+// Logits and gradients that the last-level cache (256 MB) cannot hold beside anything else go past the caches, others stay there for whoever
+// reads them next.  us through / past: forward bf16 4096 x 32000 (262 MB) with lists of 5 55.0 / 51.1, 2000 x 50257 (201) 46 / 43, fp32 3000 x
+// 50257 108 / 100, but 777 x 50257 (156, a third of the rows left out) 28.3 / 29.4; backward, stores alone, bf16 4096 x 32000 109 / 101, 2000 x
+// 50257 100 / 92, but 8192 x 8000 (131) 47 / 49, fp32 600 x 50257 (121) 61 / 64, and loads too 101 / 97, fp32 2000 x 32000 98.7 / 94.4.
+constexpr int64_t kPastBytes = 160 << 20;
+template <typename T> bool past_caches(const LogprobRows& a) { return (int64_t)a.rows * a.classes * (int)sizeof(T) >= kPastBytes; }
+
 // forward: workgroups that a row is dealt to
 template <typename T> int forward_parts(const LogprobRows& a) {
   const int64_t vecs = row_vectors<T>(a.classes);
@@ -826,8 +836,10 @@ template <typename T> int forward_parts(const LogprobRows& a) {
 }
 template <typename T, int NT> hipError_t forward_whole(const LogprobRows& a, hipStream_t st) {
   const dim3 grid(a.rows < kRowsX ? a.rows : kRowsX, (a.rows + kRowsX - 1) / kRowsX);
-  if (row_vectors<T>(a.classes) <= NT * kAhead) hipLaunchKernelGGL((logprob_rows_kernel<T, NT, false, true>), grid, dim3(NT), 0, st, a, 0);
-  else hipLaunchKernelGGL((logprob_rows_kernel<T, NT, false, false>), grid, dim3(NT), 0, st, a, 0);
+  auto kern = row_vectors<T>(a.classes) <= NT * kAhead
+                  ? past_caches<T>(a) ? logprob_rows_kernel<T, NT, false, true, true> : logprob_rows_kernel<T, NT, false, true, false>
+                  : past_caches<T>(a) ? logprob_rows_kernel<T, NT, false, false, true> : logprob_rows_kernel<T, NT, false, false, false>;
+  hipLaunchKernelGGL(kern, grid, dim3(NT), 0, st, a, 0);
   return hipGetLastError();
 }
 template <typename T> hipError_t forward(const LogprobRows& a, hipStream_t st) {
@@ -835,7 +847,7 @@ template <typename T> hipError_t forward(const LogprobRows& a, hipStream_t st) {
   const int parts = forward_parts<T>(a);
   if (parts > 1) {
     const int part_vecs = (int)((vecs + parts - 1) / parts);
-    auto kern = part_vecs <= 256 * kAhead ? logprob_rows_kernel<T, 256, true, true> : logprob_rows_kernel<T, 256, true, false>;
+    auto kern = part_vecs <= 256 * kAhead ? logprob_rows_kernel<T, 256, true, true, false> : logprob_rows_kernel<T, 256, true, false, false>;
     hipLaunchKernelGGL(kern, dim3(parts, a.rows), dim3(256), 0, st, a, part_vecs);
     return hipGetLastError();
   }
@@ -845,14 +857,9 @@ template <typename T> hipError_t forward(const LogprobRows& a, hipStream_t st) {
   return forward_whole<T, 512>(a, st);
 }
 
-// A gradient that the last-level cache (256 MB) cannot hold is stored past the caches, others stay there for whoever reads them next.  us
-// through / past: bf16 4096 x 32000 (262 MB) 109 / 101, 2000 x 50257 (201) 100 / 92, but 8192 x 8000 (131) 47 / 49, fp32 600 x 50257 (121)
-// 61 / 64.
-constexpr int64_t kPastBytes = 160 << 20;
 template <typename T, int NT, int NV, int NL = 0> hipError_t backward_whole(const LogprobRows& a, hipStream_t st) {
   const dim3 grid(a.rows < kRowsX ? a.rows : kRowsX, (a.rows + kRowsX - 1) / kRowsX);
-  const bool past = (int64_t)a.rows * a.classes * (int)sizeof(T) >= kPastBytes;
-  auto kern = past ? logprob_grad_kernel<T, NT, NV, NL, false, 1, true> : logprob_grad_kernel<T, NT, NV, NL, false, 1, false>;
+  auto kern = past_caches<T>(a) ? logprob_grad_kernel<T, NT, NV, NL, false, 1, true> : logprob_grad_kernel<T, NT, NV, NL, false, 1, false>;
   hipLaunchKernelGGL(kern, grid, dim3(NT), 0, st, a);
   return hipGetLastError();
 }

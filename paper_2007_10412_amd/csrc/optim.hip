@@ -47,7 +47,10 @@ __device__ __forceinline__ int tensor_of(const int32_t* chunk_end, int n, int c)
 }
 
 // Chunks of tensors in whole 16-byte vectors; what is left of a tensor, or a tensor at another address, element by element.
-template <bool ADAM, bool SCALED>
+// PAST: past the caches, for steps that these cannot hold.  us through / past, with the norm: Adam 4096-4096-4096-1000 (1.1 GB) 243 / 210,
+// bf16 8192-8192-4096 651 / 565, SGD 8192-8192-8192 (1.6 GB) 409 / 340; but SGD 4096-4096-4096-1000 in fp32 (0.45 GB), step after step without the
+// norm, 68 / 77.  (The loads alone or the stores alone gain nothing, the gradients through the caches 212 for the first.)
+template <bool ADAM, bool SCALED, bool PAST>
 __global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
   float scale = 1.f;
   if constexpr (SCALED) {
@@ -55,7 +58,7 @@ __global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
     if (scale == 0.f) return;
   }
   // (Adam after a norm begins with the gradients that the norm read last, of which the last-level cache still holds the most:
-  // 4096-4096-4096-1000 bf16 with its norm 248 us from the first, 244 from the last; SGD, which needs less of it besides, 109 and 110.)
+  // bf16 8192-8192-4096 with its norm 582 us from the first, 565 from the last; SGD, which needs less of it besides, 109 and 110.)
   const int b = ADAM && SCALED ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x;
   const int t = tensor_of(l.chunk_end, l.n, b), c = b - (t ? l.chunk_end[t - 1] : 0);
   float* const w = l.w[t]; float* const m = l.m[t]; float* const v = l.v[t];
@@ -69,7 +72,14 @@ __global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
 #pragma clang fp contract(off)
     if constexpr (SCALED) return x * scale; else return x;
   };
-  auto ld = [](const float* p) { return *reinterpret_cast<const floatx4*>(p); };
+  auto ld = [](const float* p) {
+    if constexpr (PAST) return __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(p));
+    else return *reinterpret_cast<const floatx4*>(p);
+  };
+  auto st = [](float* p, floatx4 x) {
+    if constexpr (PAST) __builtin_nontemporal_store(x, reinterpret_cast<floatx4*>(p));
+    else *reinterpret_cast<floatx4*>(p) = x;
+  };
 #pragma unroll
   for (int q = 0; q < kChunk / 1024; ++q) {
     const int64_t i = i0 + q * 1024 + (int)threadIdx.x * 4;
@@ -83,8 +93,8 @@ __global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
         wv[e] = update_one<ADAM, true>(wv[e], grad(gv[e]), me, ve, a);
         mv[e] = me; vv[e] = ve;
       }
-      *reinterpret_cast<floatx4*>(w + i) = wv;
-      if constexpr (ADAM) { *reinterpret_cast<floatx4*>(m + i) = mv; *reinterpret_cast<floatx4*>(v + i) = vv; }
+      st(w + i, wv);
+      if constexpr (ADAM) { st(m + i, mv); st(v + i, vv); }
       if (lo) {
         const u32x2 p = {(uint32_t)to_bf16(wv[0]) | ((uint32_t)to_bf16(wv[1]) << 16), (uint32_t)to_bf16(wv[2]) | ((uint32_t)to_bf16(wv[3]) << 16)};
         *reinterpret_cast<u32x2*>(lo + i) = p;
@@ -182,8 +192,9 @@ __global__ __launch_bounds__(kNormThreads) void square_sums_kernel(NormList l) {
   if (l.scale) *l.scale = !(f < INFINITY) ? 0.f : r > l.max_norm ? (float)(l.max_norm / r) : 1.f;
 }
 
-// (Stored past the caches: 1023-4097-1000-50257 in bf16 61 us with the norm, 71 where the end of the kernel waits for them.)
-__global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
+// (Stored past the caches: 1023-4097-1000-50257 in bf16 61 us with the norm, 71 where the end of the kernel waits for them.)  PAST: read past
+// them too, where they cannot hold them: bf16 2048-4096-50000 (0.8 GB read and written) 219 us through them, 197 past, but the first 61 and 62.
+template <bool PAST> __global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
   float f = *l.scale;
   if (f == 0.f) f = 1.f;                                // (a norm that is not finite: the gradients as they are)
   const int t = tensor_of(l.chunk_end, l.n, blockIdx.x), c = (int)blockIdx.x - (t ? l.chunk_end[t - 1] : 0);
@@ -198,7 +209,8 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
     for (int q = 0; q < kChunk / 2048; ++q) {
       const int64_t i = i0 + q * 2048 + (int)threadIdx.x * 8;
       if (i + 8 <= n && aligned) {
-        u32x4 v = *reinterpret_cast<const u32x4*>(g + i);
+        u32x4 v;
+        if constexpr (PAST) v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(g + i)); else v = *reinterpret_cast<const u32x4*>(g + i);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           v[e] = (uint32_t)to_bf16(__uint_as_float(v[e] << 16) * f) | ((uint32_t)to_bf16(__uint_as_float(v[e] & 0xFFFF0000u) * f) << 16);
@@ -215,7 +227,8 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
   for (int q = 0; q < kChunk / 1024; ++q) {
     const int64_t i = i0 + q * 1024 + (int)threadIdx.x * 4;
     if (i + 4 <= n && aligned) {
-      floatx4 v = *reinterpret_cast<const floatx4*>(g + i);
+      floatx4 v;
+      if constexpr (PAST) v = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(g + i)); else v = *reinterpret_cast<const floatx4*>(g + i);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] *= f;
       __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(o + i));
@@ -223,6 +236,12 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
       for (int64_t j = i; j < n && j < i + 4; ++j) o[j] = g[j] * f;
     }
   }
+}
+
+template <bool PAST> void optim_run(bool adam, const OptimList& l, unsigned chunks, hipStream_t st) {
+  auto kern = adam ? l.scale ? optim_kernel<true, true, PAST> : optim_kernel<true, false, PAST>
+                   : l.scale ? optim_kernel<false, true, PAST> : optim_kernel<false, false, PAST>;
+  hipLaunchKernelGGL(kern, dim3(chunks), dim3(256), 0, st, l);
 }
 
 // fills chunk_end; their number, or -1 where a grid cannot have so many
@@ -238,12 +257,11 @@ int64_t count_chunks(int n, const int64_t* count, int32_t* chunk_end, int chunk 
 
 }  // namespace
 
-hipError_t launch_optim(bool adam, OptimList* l, hipStream_t st) {
+hipError_t launch_optim(bool adam, bool past, OptimList* l, hipStream_t st) {
   const int64_t chunks = count_chunks(l->n, l->count, l->chunk_end);
   if (chunks < 0) return hipErrorInvalidValue;
   if (chunks == 0) return hipSuccess;
-  auto kern = adam ? l->scale ? optim_kernel<true, true> : optim_kernel<true, false> : l->scale ? optim_kernel<false, true> : optim_kernel<false, false>;
-  hipLaunchKernelGGL(kern, dim3((unsigned)chunks), dim3(256), 0, st, *l);
+  if (past) optim_run<true>(adam, *l, (unsigned)chunks, st); else optim_run<false>(adam, *l, (unsigned)chunks, st);
   return hipGetLastError();
 }
 
@@ -257,11 +275,12 @@ hipError_t launch_square_sums(NormList* l, int* partials, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_clip(ClipList* l, hipStream_t st) {
+hipError_t launch_clip(bool past, ClipList* l, hipStream_t st) {
   const int64_t chunks = count_chunks(l->n, l->count, l->chunk_end);
   if (chunks < 0) return hipErrorInvalidValue;
   if (chunks == 0) return hipSuccess;
-  hipLaunchKernelGGL(clip_kernel, dim3((unsigned)chunks), dim3(256), 0, st, *l);
+  if (past) hipLaunchKernelGGL(clip_kernel<true>, dim3((unsigned)chunks), dim3(256), 0, st, *l);
+  else hipLaunchKernelGGL(clip_kernel<false>, dim3((unsigned)chunks), dim3(256), 0, st, *l);
   return hipGetLastError();
 }
 

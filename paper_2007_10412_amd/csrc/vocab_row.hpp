@@ -62,12 +62,16 @@ template <typename T, int NT, int NV> struct RowPart {
   }
   static __device__ __forceinline__ int col(int v0, int i, int head) { return head + (v0 + i * NT + (int)threadIdx.x) * VPL; }
   static constexpr uint32_t kEmpty = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;     // -inf
-  __device__ __forceinline__ void load(const T* row, int v0, int head, int classes) {
+  // PAST: past the caches
+  template <bool PAST = false> __device__ __forceinline__ void load(const T* row, int v0, int head, int classes) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = col(v0, i, head);
       raw[i] = u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
-      if (c + VPL <= classes) raw[i] = *reinterpret_cast<const u32x4*>(row + c);
+      if (c + VPL <= classes) {
+        if constexpr (PAST) raw[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + c));
+        else raw[i] = *reinterpret_cast<const u32x4*>(row + c);
+      }
     }
     const int whole = max(0, classes - head) / VPL, t = (int)threadIdx.x;
     single_col = -1;

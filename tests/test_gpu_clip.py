@@ -171,6 +171,59 @@ def test_scaled_step_is_the_step_of_scaled_gradients(dtype, kind, offset):
             assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("kind", [0, 1])
+@pytest.mark.parametrize("scaled", [False, True])
+def test_steps_that_the_caches_cannot_hold(dtype, kind, scaled):
+    """One step of 46 million elements (552 MB of SGD, 1288 of Adam) has the bits of steps of its pieces."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    n, piece = 46_000_003, 4096 * 700
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    g, w, m = (torch.randn(n, device="cuda", generator=gen) for _ in range(3))
+    v, scale = torch.rand(n, device="cuda", generator=gen), torch.full((1,), 0.3, device="cuda")
+    opt = B.make_optimizer(B.RAD_ADAM if kind else B.RAD_SGD, 1e-2, 1e-4)
+    with Ctx() as ctx:
+        def state():
+            return {"master": w.clone(), "m": m.clone(), "v": v.clone(), "params": w.to(torch.bfloat16) if dtype else None}
+
+        def step(s, lo, hi):
+            part = {k: None if t is None else [t[lo:hi]] for k, t in s.items()}
+            master = part.pop("master")
+            params = part.pop("params") if dtype else master
+            args = (ctx, opt, 3, dtype, params, [g[lo:hi]]) + ((scale,) if scaled else ())
+            part.pop("params", None)
+            if not kind:
+                part = {"m": None, "v": None}
+            (B.rad_optimizer_step_scaled if scaled else B.rad_optimizer_step)(*args, **part, master=master if dtype else None)
+        whole, pieces = state(), state()
+        step(whole, 0, n)
+        for lo in range(0, n, piece):
+            step(pieces, lo, min(n, lo + piece))
+        B.rad_ctx_synchronize(ctx)
+        for k in whole:
+            assert whole[k] is None or torch.equal(whole[k], pieces[k]), k
+        assert not torch.equal(whole["master"], w)
+
+
+@pytest.mark.parametrize("how,n", [("f32", 68_000_001), ("bf16", 136_000_001)])
+@pytest.mark.parametrize("place", ["in place", "apart"])
+def test_clipping_what_the_caches_cannot_hold(how, n, place):
+    """Bits: a product rounded to fp32 and that to the type."""
+    import torch
+    from paper_2007_10412_amd import binding as B
+    grads = tensors([n], mixed(1, how), 6)
+    norm, scale = torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    with Ctx() as ctx:
+        B.rad_gradient_norm(ctx, grads, 100.0, norm=norm, scale=scale)
+        B.rad_ctx_synchronize(ctx)
+        want = (grads[0].float() * scale).to(grads[0].dtype)
+        out = None if place == "in place" else [torch.zeros_like(grads[0])]
+        B.rad_clip_gradients(ctx, grads, 100.0, clipped=out)
+        B.rad_ctx_synchronize(ctx)
+        assert 0 < float(scale) < 1 and torch.equal((out or grads)[0], want)
+
+
 def test_tensors_that_share_memory_are_stepped_in_order():
     """A tensor that comes twice gets two steps, also when it is the second half of another."""
     import torch

@@ -311,25 +311,26 @@ def test_widest_rows(dtype):
         check_dense_grad(ctx, dtype, z, tokens, a, h, tag="2^24 classes")
 
 
-def test_offsets_beyond_32_bits():
-    """1030 rows of 2^21 + 8 classes, 4.3 GB of bf16: the first rows and the last."""
+@pytest.mark.parametrize("dtype,rows,classes", [(1, 1030, 2 ** 21 + 8), (1, 90000, 1001), (0, 45000, 1000), (1, 22000, 4100), (1, 6000, 16001),
+                                                (0, 1400, 32000), (0, 1300, 50257), (1, 1300, 100000)])
+def test_large_logits(dtype, rows, classes):
+    """More than the caches hold (180 MB to 4.3 GB, the first beyond offsets of 32 bits): the first rows, some between and the last."""
     import torch
     from paper_2007_10412_amd import binding as B
-    gen = gen_for(12)
-    rows, classes = 1030, 2 ** 21 + 8
-    z = torch.randn(rows, classes, device="cuda", generator=gen, dtype=torch.bfloat16)
+    gen = gen_for(12, rows)
+    z = torch.randn(rows, classes, device="cuda", generator=gen, dtype=torch_dtype(dtype))
     tokens = tokens_for(rows, classes, gen)
     a, h = torch.randn(rows, device="cuda", generator=gen), torch.randn(rows, device="cuda", generator=gen)
-    at = torch.tensor([0, 1, 1027, 1028, 1029], device="cuda")
+    at = torch.tensor([0, 1, rows // 3, rows - 2, rows - 1], device="cuda")
     row = Row(z[at].double(), 1.0)
     with Ctx() as ctx:
-        out = call_dense(ctx, 1, z, 5, 1.0, tokens)
+        out = call_dense(ctx, dtype, z, 5, 1.0, tokens)
         check_answer({n: t[at] for n, t in out.items()}, row, tokens[at], 5, "far rows")
         dz = torch.full_like(z, 77.0)
-        B.rad_token_logprobs_grad(ctx, z, 1, dz, tokens=tokens, d_logprob=a, d_entropy=h)
+        B.rad_token_logprobs_grad(ctx, z, dtype, dz, tokens=tokens, d_logprob=a, d_entropy=h)
         B.rad_ctx_synchronize(ctx)
         want, e, _ = row.grad(tokens[at], torch.ones(5, dtype=torch.bool, device="cuda"), a[at], h[at])
-        close(dz[at], want, e + HALF[1] * want.abs() * 1.01 + 1e-38 * 2 ** 8, "far rows' gradients")
+        close(dz[at], want, e + HALF[dtype] * want.abs() * 1.01 + 1e-38 * 2 ** (8 if dtype else 0), "far rows' gradients")
 
 
 # ------------------------------------------------------------------ gradients of dense logits
