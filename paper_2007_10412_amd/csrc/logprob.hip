@@ -851,6 +851,14 @@ template <typename T> hipError_t forward(const LogprobRows& a, hipStream_t st) {
     hipLaunchKernelGGL(kern, dim3(parts, a.rows), dim3(256), 0, st, a, part_vecs);
     return hipGetLastError();
   }
+  // Many rows of middling width: what a row takes besides its logits is least in one wave, or two.  us with 256 threads (128 up to 1024 vectors) /
+  // by this rule: bf16, lists of 5, 4096 x 6000 19.5 / 15.5, 4096 x 10000 28.0 / 20.4, 16384 x 10000 94 / 68, 1200 x 10000 13.6 / 12.7, 16384 x 16000
+  // 104 / 99, 2048 x 16000 18.7 / 17.5, fp32 4096 x 5000 23.3 / 19.0; but in one wave 1200 x 20000 17.4 / 20.7, 600 x 16000 12.8 / 13.5, and lists of
+  // 64 of 1200 x 10000 16.0 / 20.1.
+  if (a.k <= 32 && a.rows >= 1024) {
+    if (vecs <= 64 * 20 || (a.rows >= 4096 && vecs <= 64 * 40)) return forward_whole<T, 64>(a, st);
+    if (vecs <= 128 * 20) return forward_whole<T, 128>(a, st);
+  }
   if (vecs <= 64 * kAhead && a.k <= 128) return forward_whole<T, 64>(a, st);
   if (vecs <= 2 * 128 * kAhead) return forward_whole<T, 128>(a, st);
   if (vecs <= 32 * 256) return forward_whole<T, 256>(a, st);

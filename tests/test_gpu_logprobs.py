@@ -333,6 +333,24 @@ def test_large_logits(dtype, rows, classes):
         close(dz[at], want, e + HALF[dtype] * want.abs() * 1.01 + 1e-38 * 2 ** (8 if dtype else 0), "far rows' gradients")
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,classes", [(1100, 2050), (1100, 4999), (1100, 9001), (1100, 19001), (4100, 9003), (4100, 17001)])
+def test_many_rows(dtype, rows, classes):
+    """Rows that a wave or two have to themselves: as they come, with masks, and with so few values that lists end within ties."""
+    import torch
+    gen = gen_for(14, dtype, rows, classes)
+    z = (3 * torch.randn(rows, classes, device="cuda", generator=gen)).to(torch_dtype(dtype))
+    z[::5] = z[::5].round()
+    z[1::7, 3:] = -math.inf
+    z[2::7] = 0.5
+    z[3::7] = torch.where(torch.rand(z[3::7].shape, device="cuda", generator=gen) < 0.5, -math.inf, z[3::7].float()).to(z.dtype)
+    tokens = tokens_for(rows, classes, gen, 0.2)
+    row = Row(z.double(), 1.3)
+    with Ctx() as ctx:
+        for k in (32, 5, 1, 0):
+            check_answer(call_dense(ctx, dtype, z, k, 1.3, tokens), row, tokens, k, "k %d" % k)
+
+
 # ------------------------------------------------------------------ gradients of dense logits
 def check_dense_grad(ctx, dtype, z, tokens, a, h, T=1.0, in_place=False, tag=""):
     import torch
