@@ -385,7 +385,7 @@ typedef struct {
 /* Of logits [rows, classes] in dtype that are there.  Statistics are fp32; a log
  * probability is off by some 10^-7 (|z| / T + log(classes)).  Outputs overlap
  * neither inputs nor each other; results do not vary from call to call.  Context
- * workspace for up to 256 long rows: 512 (12 + 8 top_k) bytes at most.  Enqueued on
+ * workspace for up to 128 long rows: 512 (12 + 8 top_k) bytes at most.  Enqueued on
  * the context's stream. */
 rad_status rad_token_logprobs(rad_ctx* ctx, const void* logits, int64_t rows, int64_t classes, int32_t dtype,
                               const rad_logprobs* out);

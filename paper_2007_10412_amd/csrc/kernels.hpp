@@ -369,7 +369,7 @@ struct LogprobRows {
   void* ws;                     // logprob_rows_bytes of scratch
   uint32_t* done;               // kLogprobSplitRows words, zero before and after a launch
 };
-constexpr int kLogprobSplitRows = 256;                // forward: more rows than these are not split
+constexpr int kLogprobSplitRows = 128;                // forward: more rows than these are not split
 size_t logprob_rows_bytes(const LogprobRows& a);
 // (three floats a part of a row, before the parts' lists)
 __host__ __device__ constexpr size_t logprob_stats_bytes(int rows, int parts) { return ((size_t)rows * parts * 12 + 255) / 256 * 256; }

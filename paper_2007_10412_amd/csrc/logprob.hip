@@ -262,7 +262,9 @@ __device__ __forceinline__ void put_top(int32_t* top_index, float* top_logprob, 
 // moves up when a larger logit comes (l = z c - m c is one operation so, with m c rounded once for all and what that rounding
 // moved put right at the end), and reads those of its vectors again, from a cache, of which a logit may be on the list.
 // Bases lie within +-2^24 T ln 2, where m c is rounded by one power of two at most; rows whose largest logit does not, and such as hold
-// infinities or NaN, are done again, maximum first, by slow_stats.
+// infinities or NaN, are done again, maximum first, by slow_stats.  Bound by memory without lists, by the vector units with them (11 operations a
+// logit at 32000 classes, 4 of them a row's share of bound and list): bf16 4096 x 32000 44 us (5.9 TB/s), with lists of 5 50; fp32 777 x 50257 with
+// lists of 64 37 (4.3 TB/s).
 constexpr float kFar = 0x1p24f;
 constexpr int kAhead = 4, kSlots = 8;                   // vectors in flight
 template <int NT> constexpr int groups_of() { return NT >= 512 ? 1 : NT == 256 ? 2 : 4; }   // a thread's, for a list's bound
@@ -523,7 +525,8 @@ __global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a, int par
 }
 
 // Backward: a row stays in registers between its sums and its gradient, from one maximum m, with l = z c - m c in one operation as
-// above; where m lies too far from zero for that, from memory element by element.  SPLIT: PASS 0 leaves the parts' statistics, PASS 1
+// above; where m lies too far from zero for that, from memory element by element.  Bound by memory, with the vector units at work for most of that time
+// (exponentials are taken twice): bf16 4096 x 32000 95 us (5.5 TB/s read and written), fp32 333 x 50257 24.5 (5.5).  SPLIT: PASS 0 leaves the parts' statistics, PASS 1
 // joins them (each workgroup for itself) and writes.
 template <int NT> __device__ __forceinline__ float block_max(float m, float3* s_w) {
   m = lanes_max(m);
@@ -720,6 +723,7 @@ __global__ __launch_bounds__(NT, NL > 0 ? 8 : 1) void logprob_grad_kernel(Logpro
 
 // ------------------------------------------------------------------ after a layer's product
 constexpr int kJoinThreads = 512;
+// A chain of loads, a bound and a list: bf16 1 x 128000 (2000 parts) with lists of 20 6.2 us, 300 x 32000 with lists of 5 9.2.
 // A workgroup a place: its parts' statistics joined, and of its logits (in fp32) those of the parts that may hold a listed one; where the
 // parts are too few for a tight bound, all of them twice.
 __global__ __launch_bounds__(kJoinThreads) void logprob_finish_kernel(LogprobFinish a) {
@@ -828,10 +832,13 @@ template <typename T> int64_t row_vectors(int classes) { return (int64_t)classes
 constexpr int64_t kPastBytes = 160 << 20;
 template <typename T> bool past_caches(const LogprobRows& a) { return (int64_t)a.rows * a.classes * (int)sizeof(T) >= kPastBytes; }
 
-// forward: workgroups that a row is dealt to
+// forward: workgroups that a row is dealt to.  A few of the longest rows, longer ones where lists are long (every part makes one).  us of the kernel in
+// one / in parts: bf16 without lists 1 x 50257 7.4 / 6.2, 128 x 128000 13.5 / 11.4, but 64 x 20000 5.6 / 6.5, 256 x 128000 15.0 / 17.0; lists of 20 1 x
+// 100000 13.0 / 11.7, 128 x 200000 24.7 / 21.4, but 64 x 20000 8.9 / 11.6, 1 x 50257 11.0 / 11.8, 256 x 200000 26.0 / 30.4; lists of 200 64 x 128000
+// 24.4 / 35.6; fp32, of whose vectors each holds half as many, lists of 20 64 x 50257 11.6 / 13.6.
 template <typename T> int forward_parts(const LogprobRows& a) {
   const int64_t vecs = row_vectors<T>(a.classes);
-  if (a.rows > kLogprobSplitRows || vecs < 2 * 256 * kAhead) return 1;
+  if (a.rows > kLogprobSplitRows || vecs <= (a.k == 0 ? 4096 : a.k > 32 ? 65536 : sizeof(T) == 2 ? 12000 : 14000)) return 1;
   return (int)std::min<int64_t>(std::max<int64_t>(1, 512 / a.rows), (vecs + 256 * kAhead - 1) / (256 * kAhead));
 }
 template <typename T, int NT> hipError_t forward_whole(const LogprobRows& a, hipStream_t st) {
