@@ -2,6 +2,7 @@
 marshalling only.  Tensors are torch CUDA(HIP) tensors; every computation runs
 in the library's kernels.  There is no fallback: a missing library raises."""
 import ctypes as C
+import operator
 import os
 
 import numpy as np
@@ -544,25 +545,31 @@ def rad_optimizer_step(ctx, opt, t, dtype, params, grads, m=None, v=None, master
                                          arr(v), arr(master)))
 
 
-def _counts(tensors):
-    return [t.numel() for t in tensors]
+_DTYPE = operator.attrgetter("dtype")
 
 
-def _tensors(name, tensors, counts, kind):
+# (T: torch.Tensor, whose methods go over a list faster than the list's tensors are asked one by one.)
+def _addresses(T, tensors):
+    return (P * len(tensors))(*map(T.data_ptr, tensors))
+
+
+def _tensors(T, name, tensors, counts, kind):
     """The HOST array of addresses of tensors (None: no array) that are to be contiguous, of so many elements each and of one
     type."""
     if tensors is None:
         return None
-    at = [t.data_ptr() for t, n in zip(tensors, counts) if t.dtype is kind and t.numel() == n and t.is_contiguous()]
-    if len(at) != len(counts) or len(tensors) != len(counts):
+    if list(map(T.numel, tensors)) != counts or set(map(_DTYPE, tensors)) - {kind} or not all(map(T.is_contiguous, tensors)):
         raise RadError(RAD_ERR_SHAPE, "%s are not %d contiguous tensors of %s elements of %s" % (name, len(counts), counts, kind))
-    return (P * len(at))(*at)
+    return _addresses(T, tensors)
 
 
-def _lists_on_device(ctx, *lists):
+def _lists_on_device(T, ctx, *lists):
     """_on_device for lists of tensors (None: none)"""
     at = getattr(ctx, "device", None)
-    where = {t.get_device() for ts in lists if ts is not None for t in ts}
+    where = set()
+    for ts in lists:
+        if ts is not None:
+            where.update(map(T.get_device, ts))
     if where - {at} and (at is not None or len(where) > 1 or min(where) < 0):
         _on_device(ctx, *[t for ts in lists if ts is not None for t in ts])
 
@@ -570,15 +577,16 @@ def _lists_on_device(ctx, *lists):
 def _gradients(grads):
     """(counts, HOST arrays of counts, addresses and rad_dtypes) of a list of gradients, fp32 and bf16"""
     import torch
-    counts, kinds, n = _counts(grads), {t.dtype for t in grads}, len(grads)
+    T = torch.Tensor
+    counts, kinds, n = list(map(T.numel, grads)), set(map(_DTYPE, grads)), len(grads)
     dtypes = None                                        # (all fp32)
     if kinds - {torch.float32}:
         if kinds - {torch.float32, torch.bfloat16}:
             raise RadError(RAD_ERR_PARAM, "gradients are fp32 or bf16")
-        dtypes = (C.c_int32 * n)(*[RAD_F32 if t.dtype is torch.float32 else RAD_BF16 for t in grads])
-    if not all([t.is_contiguous() for t in grads]):
+        dtypes = (C.c_int32 * n)(*([RAD_BF16] * n if len(kinds) == 1 else [RAD_F32 if t.dtype is torch.float32 else RAD_BF16 for t in grads]))
+    if not all(map(T.is_contiguous, grads)):
         raise RadError(RAD_ERR_SHAPE, "a gradient is not contiguous")
-    return counts, (C.c_int64 * n)(*counts), (P * n)(*[t.data_ptr() for t in grads]), dtypes
+    return counts, (C.c_int64 * n)(*counts), _addresses(T, grads), dtypes
 
 
 def rad_gradient_norm(ctx, grads, max_norm=float("inf"), norm=None, scale=None):
@@ -586,7 +594,7 @@ def rad_gradient_norm(ctx, grads, max_norm=float("inf"), norm=None, scale=None):
     import torch
     _, counts, at, dtypes = _gradients(grads)
     args = (_arg("norm", norm, 1, torch.float32), _arg("scale", scale, 1, torch.float32))
-    _lists_on_device(ctx, grads, [t for t in (norm, scale) if t is not None])
+    _lists_on_device(torch.Tensor, ctx, grads, [t for t in (norm, scale) if t is not None])
     _check(ctx, lib().rad_gradient_norm(ctx, len(grads), counts, at, dtypes, max_norm, *args))
 
 
@@ -596,22 +604,24 @@ def rad_clip_gradients(ctx, grads, max_norm, clipped=None, norm=None):
     sizes, counts, at, dtypes = _gradients(grads)
     to = at
     if clipped is not None:
-        if [(t.numel(), t.dtype, t.is_contiguous()) for t in clipped] != [(n, t.dtype, True) for n, t in zip(sizes, grads)]:
+        T = torch.Tensor
+        if list(map(T.numel, clipped)) != sizes or list(map(_DTYPE, clipped)) != list(map(_DTYPE, grads)) or not all(map(T.is_contiguous, clipped)):
             raise RadError(RAD_ERR_SHAPE, "clipped are not contiguous tensors of the gradients' sizes and types")
-        to = (P * len(grads))(*[t.data_ptr() for t in clipped])
+        to = _addresses(T, clipped)
     arg = _arg("norm", norm, 1, torch.float32)
-    _lists_on_device(ctx, grads, clipped, None if norm is None else [norm])
+    _lists_on_device(torch.Tensor, ctx, grads, clipped, None if norm is None else [norm])
     _check(ctx, lib().rad_clip_gradients(ctx, len(grads), counts, at, dtypes, max_norm, to, arg))
 
 
 def rad_optimizer_step_scaled(ctx, opt, t, dtype, params, grads, scale, m=None, v=None, master=None):
     """As rad_optimizer_step; scale: an fp32 tensor of one element on the GPU."""
     import torch
-    counts, f32 = _counts(params), torch.float32
+    T, f32 = torch.Tensor, torch.float32
+    counts = list(map(T.numel, params))
     kind = f32 if dtype == RAD_F32 else torch.bfloat16 if dtype == RAD_BF16 or not params else params[0].dtype
-    args = ((C.c_int64 * len(counts))(*counts), _tensors("params", params, counts, kind), _tensors("grads", grads, counts, f32),
-            _tensors("m", m, counts, f32), _tensors("v", v, counts, f32), _tensors("master", master, counts, f32), _arg("scale", scale, 1, f32))
-    _lists_on_device(ctx, params, grads, m, v, master, [scale])
+    args = ((C.c_int64 * len(counts))(*counts), _tensors(T, "params", params, counts, kind), _tensors(T, "grads", grads, counts, f32),
+            _tensors(T, "m", m, counts, f32), _tensors(T, "v", v, counts, f32), _tensors(T, "master", master, counts, f32), _arg("scale", scale, 1, f32))
+    _lists_on_device(T, ctx, params, grads, m, v, master, [scale])
     _check(ctx, lib().rad_optimizer_step_scaled(ctx, opt, int(t), dtype, len(counts), *args))
 
 

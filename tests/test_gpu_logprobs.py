@@ -889,7 +889,7 @@ def test_two_calls_agree_bit_by_bit():
             a, h = torch.randn(200, device="cuda", generator=gen), torch.randn(200, device="cuda", generator=gen)
             first = None
             for _ in range(3):
-                one, two = call_dense(ctx, dtype, z, 99, 1.0, t1), outputs(200, 31)
+                one, two = call_dense(ctx, dtype, z, 29, 1.0, t1), outputs(200, 31)
                 B.rad_linear_logprobs(ctx, layer, x, W, b, tokens=t2, **two)
                 g = {"dX": torch.empty_like(x), "dW": torch.empty_like(W), "dbias": torch.empty_like(b)}
                 B.rad_linear_logprobs_grad(ctx, layer, x, W, b, tokens=t2, d_logprob=a, d_entropy=h, **g)
@@ -915,7 +915,7 @@ def test_captured(dtype):
     layer = B.make_layer(rows, d_in, classes, dtype=dtype, relu=False, has_bias=True)
 
     def fresh():
-        return {"dense": outputs(3, 33), "linear": outputs(rows, 12), "dz": {"dlogits": torch.zeros_like(z)},
+        return {"dense": outputs(3, 30), "linear": outputs(rows, 12), "dz": {"dlogits": torch.zeros_like(z)},
                 "grads": {"dX": torch.zeros_like(x), "dW": torch.zeros_like(W), "dbias": torch.zeros_like(b)}}
 
     def calls(c, o):
@@ -983,7 +983,7 @@ def test_two_contexts_at_once():
             gen = gen_for(31 + i)
             x, W, _ = layer_inputs(1, 300, 256, 8000, False, gen, grid=True)
             z = (3 * torch.randn(2, 140000, device="cuda", generator=gen)).to(torch.bfloat16)
-            work.append((c, x, W, z, outputs(300, 9, ("entropy", "top")), outputs(2, 50, ("entropy", "top"))))
+            work.append((c, x, W, z, outputs(300, 9, ("entropy", "top")), outputs(2, 30, ("entropy", "top"))))
         layer = B.make_layer(300, 256, 8000, dtype=1, relu=False)
         torch.cuda.synchronize()
         for _ in range(20):
@@ -992,7 +992,7 @@ def test_two_contexts_at_once():
                 B.rad_token_logprobs(c, z, 1, **two)
         torch.cuda.synchronize()
         for _, x, W, z, one, two in work:
-            w1, w2 = outputs(300, 9, ("entropy", "top")), outputs(2, 50, ("entropy", "top"))
+            w1, w2 = outputs(300, 9, ("entropy", "top")), outputs(2, 30, ("entropy", "top"))
             B.rad_linear_logprobs(plain, layer, x, W, None, **w1)
             B.rad_token_logprobs(plain, z, 1, **w2)
             torch.cuda.synchronize()
