@@ -262,14 +262,17 @@ __device__ __forceinline__ void put_top(int32_t* top_index, float* top_logprob, 
 // moves up when a larger logit comes (l = z c - m c is one operation so, with m c rounded once for all and what that rounding
 // moved put right at the end), and reads those of its vectors again, from a cache, of which a logit may be on the list.
 // Bases lie within +-2^24 T ln 2, where m c is rounded by one power of two at most; rows whose largest logit does not, and such as hold
-// infinities or NaN, are done again, maximum first, by slow_stats.  Bound by memory without lists, by the vector units with them (11 operations a
+// infinities or NaN, are done again, maximum first, by slow_stats.  (A row whose largest logit is just below the lowest base has a good sum
+// from there, but that base would pass for its maximum, which a list of one class begins from: it is done again too.)  Bound by memory without lists, by the vector units with them (11 operations a
 // logit at 32000 classes, 4 of them a row's share of bound and list): bf16 4096 x 32000 44 us (5.9 TB/s), with lists of 5 50; fp32 777 x 50257 with
 // lists of 64 37 (4.3 TB/s).
 constexpr float kFar = 0x1p24f;
 constexpr int kAhead = 4, kSlots = 8;                   // vectors in flight
 template <int NT> constexpr int groups_of() { return NT >= 512 ? 1 : NT == 256 ? 2 : 4; }   // a thread's, for a list's bound
 
-__device__ __forceinline__ bool plain_stats(const RowStats& r, float c) { return r.s > 0.5f && r.s < INFINITY && r.m * c <= kFar; }
+__device__ __forceinline__ bool plain_stats(const RowStats& r, float lowest, float c) {
+  return r.s > 0.5f && r.s < INFINITY && r.m > lowest && r.m * c <= kFar;
+}
 
 template <typename T, int NT> __device__ __noinline__ RowStats slow_stats(const T* z, int lo, int hi, float c, float3* s_w) {
   RowStats r;
@@ -450,7 +453,7 @@ __global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a, int par
   r = block_join<NT>(r, false, c, s_w);
   if (NT == 64) __syncthreads();                        // (a larger workgroup has had one)
   const int c_lo = first ? 0 : head + v_lo * VPL, c_hi = last ? classes : head + v_hi * VPL;
-  if (!plain_stats(r, c)) r = slow_stats<T, NT>(z, c_lo, c_hi, c, s_w);
+  if (!plain_stats(r, lowest, c)) r = slow_stats<T, NT>(z, c_lo, c_hi, c, s_w);
   const RowEnd end(r, a.temperature);
   if (tid == 0) {
     if (SPLIT) {
