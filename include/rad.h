@@ -530,6 +530,8 @@ rad_status rad_optimizer_step(rad_ctx* ctx, const rad_optimizer* opt, int64_t t,
  *   *norm = sqrt(sum over tensors and elements of g^2),
  *   *scale = min(1, max_norm / *norm), or 0 where the norm is not finite (a
  *   gradient holds an infinity or a NaN, or the norm is beyond fp32's range).
+ * The scale of a finite norm is never 0: where the quotient is below 2^-126 it is
+ * a subnormal number of fewer bits, 2^-149 at least.
  * counts, grads and dtypes (rad_dtype each; null: all RAD_F32) are HOST arrays,
  * grads' entries DEVICE tensors of counts[i] elements (16-byte aligned ones are
  * read in vectors), which may come twice; norm and scale are DEVICE fp32, one of
@@ -540,8 +542,9 @@ rad_status rad_optimizer_step(rad_ctx* ctx, const rad_optimizer* opt, int64_t t,
 rad_status rad_gradient_norm(rad_ctx* ctx, int32_t n_tensors, const int64_t* counts, const void* const* grads,
                              const int32_t* dtypes, double max_norm, float* norm, float* scale);
 
-/* The gradients under that scale: clipped[i] = *scale * grads[i], rounded to the
- * gradient's type; where the norm is not finite (*norm says so) the gradients as
+/* The gradients under that scale: clipped[i] = min(1, max_norm / *norm) grads[i],
+ * rounded to the gradient's type (by factors that keep their bits where the scale
+ * is subnormal); where the norm is not finite (*norm says so) the gradients as
  * they are.  clipped: HOST array of DEVICE tensors; clipped[i] may be grads[i]
  * (which then is neither read again nor written where nothing is to be clipped);
  * outputs that overlap anything else are refused, and so is one tensor twice.

@@ -2160,7 +2160,7 @@ static rad_status check_gradients(rad_ctx* c, int32_t n_tensors, const int64_t* 
 }
 static int gradient_size(const int32_t* dtypes, int i) { return dtypes && dtypes[i] == RAD_BF16 ? 2 : 4; }
 
-constexpr size_t kNormHead = 256;                        // WS_NORM: a scale, then partial sums
+constexpr size_t kNormHead = 256;                        // WS_NORM: clipping's factors, then partial sums
 static rad_status norm_workspace(rad_ctx* c, int32_t n_tensors, char** ws) {
   uint32_t* done = nullptr;
   RAD_TRY(ws_counters(c, &done));                        // (first, as it may refuse)
@@ -2168,11 +2168,11 @@ static rad_status norm_workspace(rad_ctx* c, int32_t n_tensors, char** ws) {
 }
 
 static rad_status gradient_norm(rad_ctx* c, int32_t n_tensors, const int64_t* counts, const void* const* grads, const int32_t* dtypes,
-                                double max_norm, char* ws, float* norm, float* scale) {
+                                double max_norm, char* ws, float* norm, float* scale, float* factors) {
   NormList l;
   l.partial = reinterpret_cast<double*>(ws + kNormHead);
   l.first = 0;
-  l.max_norm = max_norm; l.norm = norm; l.scale = scale;
+  l.max_norm = max_norm; l.norm = norm; l.scale = scale; l.factors = factors;
   uint32_t* done = nullptr;
   RAD_TRY(ws_counters(c, &done));
   int i = 0;
@@ -2206,7 +2206,7 @@ extern "C" rad_status rad_gradient_norm(rad_ctx* c, int32_t n_tensors, const int
   DeviceGuard guard(c->device);
   char* ws = nullptr;
   RAD_TRY(norm_workspace(c, n_tensors, &ws));
-  return gradient_norm(c, n_tensors, counts, grads, dtypes, max_norm, ws, norm, scale);
+  return gradient_norm(c, n_tensors, counts, grads, dtypes, max_norm, ws, norm, scale, nullptr);
 }
 
 extern "C" rad_status rad_clip_gradients(rad_ctx* c, int32_t n_tensors, const int64_t* counts, const void* const* grads,
@@ -2226,10 +2226,10 @@ extern "C" rad_status rad_clip_gradients(rad_ctx* c, int32_t n_tensors, const in
   DeviceGuard guard(c->device);
   char* ws = nullptr;
   RAD_TRY(norm_workspace(c, n_tensors, &ws));
-  float* const scale = reinterpret_cast<float*>(ws);
-  RAD_TRY(gradient_norm(c, n_tensors, counts, grads, dtypes, max_norm, ws, norm, scale));
+  float* const factors = reinterpret_cast<float*>(ws);
+  RAD_TRY(gradient_norm(c, n_tensors, counts, grads, dtypes, max_norm, ws, norm, nullptr, factors));
   ClipList l;
-  l.scale = scale;
+  l.factors = factors;
   int64_t bytes = 0;
   for (int i = 0; i < n_tensors; ++i) bytes += counts[i] * 2 * gradient_size(dtypes, i);
   for (int i = 0; i < n_tensors;) {

@@ -210,21 +210,22 @@ struct OptimList {
 };
 hipError_t launch_optim(bool adam, bool past, OptimList* l, hipStream_t st);       // past the caches
 // partial[first ..]: sums of squares, in fp64, of the elements that each workgroup takes; *partials of them.  The launch
-// that is given norm or scale ends with *norm = sqrt(sum of partial[0 .. first + its own)), *scale = min(1, max_norm / norm), 0 where the norm is not
-// finite; *done is zero before it and after it.
+// that is given done ends with *norm = sqrt(sum of partial[0 .. first + its own)), *scale = min(1, max_norm / norm) (at least 2^-149), 0 where the norm
+// is not finite, and two factors whose product is that quotient however small it is, both 1 where the norm is not finite; each may be null;
+// *done is zero before it and after it.
 constexpr int kNormBlocks = 512;        // of one launch, at most (each counts itself done at one address, 10 ns after the one before)
 struct NormList {
   double* partial; int first;
-  uint32_t* done; double max_norm; float* norm; float* scale;
+  uint32_t* done; double max_norm; float* norm; float* scale; float* factors;
   int n;
   const void* g[kNormTensors]; int64_t count[kNormTensors];
   int32_t chunk_end[kNormTensors];      // set by the launch
   uint32_t bf16[kNormTensors / 32];     // bit i: tensor i is bf16, else fp32
 };
 hipError_t launch_square_sums(NormList* l, int* partials, hipStream_t st);
-// out[i] = *scale g[i] (a scale of 0: g[i]); out[i] may be g[i]
+// out[i] = factors[0] g[i] factors[1], rounded in that order; out[i] may be g[i]
 struct ClipList {
-  const float* scale;
+  const float* factors;
   int n;
   const void* g[kClipTensors]; void* out[kClipTensors]; int64_t count[kClipTensors];
   int32_t chunk_end[kClipTensors];      // set by the launch

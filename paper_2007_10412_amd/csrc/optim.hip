@@ -190,16 +190,25 @@ __global__ __launch_bounds__(kNormThreads) void square_sums_kernel(NormList l) {
   const double r = sqrt(total);
   const float f = (float)r;
   if (l.norm) *l.norm = f;
-  if (l.scale) *l.scale = !(f < INFINITY) ? 0.f : r > l.max_norm ? (float)(l.max_norm / r) : 1.f;
+  const bool finite = f < INFINITY, over = finite && r > l.max_norm;
+  // (0 says that the norm is not finite, so the least scale of one that is, is the smallest subnormal number)
+  if (l.scale) *l.scale = !finite ? 0.f : over ? fmaxf((float)(l.max_norm / r), 0x1p-149f) : 1.f;
+  if (l.factors) {
+    const int e = over && l.max_norm / r < 0x1p-126 ? max(-126, min(126, ilogb(r))) : 0;
+    l.factors[0] = (float)ldexp(1.0, -e);
+    l.factors[1] = over ? (float)(l.max_norm / ldexp(r, -e)) : 1.f;
+  }
 }
 
+// Elements times two factors whose product is the scale: the first is 1, or, where the scale would be a subnormal number of few bits (or none:
+// max_norm is less than 2^-126 of the norm), a power of two that brings them to the norm's size.  It is exact but for elements below 2^-126 of
+// that, and the second, at most twice max_norm, has all its bits but where max_norm is subnormal itself.
 // (Stored past the caches: 1023-4097-1000-50257 in bf16 61 us with the norm, 71 where the end of the kernel waits for them.)  PAST: read past
 // them too, where they cannot hold them: bf16 2048-4096-50000 (0.8 GB read and written) 219 us through them, 197 past, but the first 61 and 62.
 template <bool PAST> __global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
-  float f = *l.scale;
-  if (f == 0.f) f = 1.f;                                // (a norm that is not finite: the gradients as they are)
+  const float lift = l.factors[0], f = l.factors[1];    // (1 and 1 for a norm that is not finite: the gradients as they are)
   const int t = tensor_of(l.chunk_end, l.n, blockIdx.x), c = (int)blockIdx.x - (t ? l.chunk_end[t - 1] : 0);
-  if (f == 1.f && l.out[t] == l.g[t]) return;
+  if (lift == 1.f && f == 1.f && l.out[t] == l.g[t]) return;
   const int64_t i0 = (int64_t)c * kChunk, n = l.count[t];
   const bool half = (l.bf16[t >> 5] >> (t & 31)) & 1u;
   const bool aligned = ((reinterpret_cast<uintptr_t>(l.g[t]) | reinterpret_cast<uintptr_t>(l.out[t])) & 15) == 0;
@@ -214,10 +223,10 @@ template <bool PAST> __global__ __launch_bounds__(256) void clip_kernel(ClipList
         if constexpr (PAST) v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(g + i)); else v = *reinterpret_cast<const u32x4*>(g + i);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          v[e] = (uint32_t)to_bf16(__uint_as_float(v[e] << 16) * f) | ((uint32_t)to_bf16(__uint_as_float(v[e] & 0xFFFF0000u) * f) << 16);
+          v[e] = (uint32_t)to_bf16(__uint_as_float(v[e] << 16) * lift * f) | ((uint32_t)to_bf16(__uint_as_float(v[e] & 0xFFFF0000u) * lift * f) << 16);
         __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(o + i));
       } else {
-        for (int64_t j = i; j < n && j < i + 8; ++j) o[j] = to_bf16(bf16_bits_to_f32(g[j]) * f);
+        for (int64_t j = i; j < n && j < i + 8; ++j) o[j] = to_bf16(bf16_bits_to_f32(g[j]) * lift * f);
       }
     }
     return;
@@ -231,10 +240,10 @@ template <bool PAST> __global__ __launch_bounds__(256) void clip_kernel(ClipList
       floatx4 v;
       if constexpr (PAST) v = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(g + i)); else v = *reinterpret_cast<const floatx4*>(g + i);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] *= f;
+      for (int e = 0; e < 4; ++e) v[e] = v[e] * lift * f;
       __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(o + i));
     } else {
-      for (int64_t j = i; j < n && j < i + 4; ++j) o[j] = g[j] * f;
+      for (int64_t j = i; j < n && j < i + 4; ++j) o[j] = g[j] * lift * f;
     }
   }
 }
