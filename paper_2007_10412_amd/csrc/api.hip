@@ -2027,7 +2027,8 @@ extern "C" rad_status rad_linear_logprobs_grad(rad_ctx* c, const rad_layer* L, c
 }
 
 // ------------------------------------------------------------------ parameter updates
-constexpr int64_t kMaxElements = (int64_t)1 << 35;       // of a call's gradients (a grid's chunks stay below 2^24)
+constexpr int64_t kMaxElements = (int64_t)1 << 35;       // of a call's gradients, of a stepped tensor
+constexpr int64_t kStepElements = (int64_t)1 << 33;      // of a launch that steps (its grid stays below 2^24 workgroups)
 constexpr int64_t kPastBytes = (int64_t)512 << 20;       // read and written by a call: twice what the last-level cache holds
 
 // Memory of many tensors, some of it written: whether nothing that is written meets anything else.
@@ -2114,14 +2115,17 @@ static rad_status optimizer_step(rad_ctx* c, const rad_optimizer* opt, int64_t t
   };
   for (int i = 0; i < n_tensors; ++i) {
     if (counts[i] == 0) continue;
-    if (l.n >= together || elements + counts[i] > kMaxElements) RAD_TRY(launch());
-    l.w[l.n] = static_cast<float*>(dtype == RAD_BF16 ? master[i] : params[i]);
-    l.lo[l.n] = dtype == RAD_BF16 ? static_cast<uint16_t*>(params[i]) : nullptr;
-    l.g[l.n] = static_cast<const float*>(grads[i]);
-    l.m[l.n] = adam ? static_cast<float*>(m[i]) : nullptr;
-    l.v[l.n] = adam ? static_cast<float*>(v[i]) : nullptr;
-    l.count[l.n++] = counts[i];
-    elements += counts[i];
+    for (int64_t at = 0; at < counts[i]; at += kStepElements) {      // (one piece, of nearly every tensor)
+      const int64_t n = std::min(counts[i] - at, kStepElements);
+      if (l.n >= together || elements + n > kStepElements) RAD_TRY(launch());
+      l.w[l.n] = static_cast<float*>(dtype == RAD_BF16 ? master[i] : params[i]) + at;
+      l.lo[l.n] = dtype == RAD_BF16 ? static_cast<uint16_t*>(params[i]) + at : nullptr;
+      l.g[l.n] = static_cast<const float*>(grads[i]) + at;
+      l.m[l.n] = adam ? static_cast<float*>(m[i]) + at : nullptr;
+      l.v[l.n] = adam ? static_cast<float*>(v[i]) + at : nullptr;
+      l.count[l.n++] = n;
+      elements += n;
+    }
   }
   return launch();
 }

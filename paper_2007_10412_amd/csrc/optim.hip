@@ -3,7 +3,7 @@
 // they are clipped.  One pass over a tensor: every operand is read once and every result written once, so the kernels are HBM
 // streams (SGD 8 bytes read + 4 written per fp32 parameter; Adam 16 read + 12 written, 2 more written when a bf16 copy of the
 // parameter is kept; a norm reads its gradients, and the step that follows applies the clipping factor as it reads them again).
-// A launch takes many tensors: each is cut into chunks of kChunk elements, which the workgroups take in turn.
+// A launch takes many tensors: each is cut into chunks, which the workgroups take in turn.
 #include "kernels.hpp"
 
 namespace rad {
@@ -33,7 +33,11 @@ __device__ __forceinline__ float update_one(float w, float g, float& m, float& v
   }
 }
 
-constexpr int kChunk = 4096;                            // elements: 16 KB of fp32, four 16-byte vectors a lane of 256
+// Elements of a chunk.  A step takes one vector a lane: with four, the loads of each wait behind the stores of the one before, which
+// steps past the caches do not hide (us with four / one, steps after their gradients were written: SGD bf16 2400 MB 830 / 778, 6400 MB 2225 /
+// 2080, fp32 545 MB 160 / 152, 6400 MB 1914 / 1790, Adam bf16 545 MB 123 / 114, 2400 MB 583 / 558).
+constexpr int kStepChunk = 1024;
+constexpr int kClipChunk = 4096;
 constexpr int kNormThreads = 1024, kNormChunk = 16384;
 
 // the tensor that chunk c lies in
@@ -47,9 +51,13 @@ __device__ __forceinline__ int tensor_of(const int32_t* chunk_end, int n, int c)
 }
 
 // Chunks of tensors in whole 16-byte vectors; what is left of a tensor, or a tensor at another address, element by element.
-// PAST: past the caches, for steps that these cannot hold.  us through / past, with the norm: Adam 4096-4096-4096-1000 (1.1 GB) 243 / 210,
-// bf16 8192-8192-4096 651 / 565, SGD 8192-8192-8192 (1.6 GB) 409 / 340; but SGD 4096-4096-4096-1000 in fp32 (0.45 GB), step after step without the
-// norm, 68 / 77.  Bound by memory: of the first the step takes 166 us (6.8 TB/s, part of the gradients from the cache).  (The loads alone or the stores alone gain nothing, the gradients through the caches 212 for the first.)
+// PAST: past the caches, for steps that these cannot hold, whatever came before them.  us through / past:
+//   with the norm ahead: Adam bf16 4096-4096-4096-1000 (1.1 GB) 248 / 197, 8192-8192-4096 628 / 543, SGD fp32 8192-8192-8192 387 / 334, 8192-8192-4096 295 / 246;
+//   alone, after their gradients were written (the writing included): SGD fp32 of 545 MB 168 / 152, 1600 MB 483 / 444, bf16 545 MB 187 / 165, Adam bf16
+//   545 MB 133 / 113, 2400 MB 604 / 552; the same step again and again: 85 / 83, 283 / 252, 113 / 95, 93 / 93, 475 / 402;
+//   but SGD 4096-4096-4096-1000 in fp32 (0.45 GB), again and again, 68 / 77 (with four vectors a lane).
+// Bound by memory.  (The loads alone or the stores alone gain nothing; the gradients through the caches and the rest past them: the first of these
+// 191, but 8192-8192-4096 553, SGD fp32 8192-8192-8192 348.)
 template <bool ADAM, bool SCALED, bool PAST>
 __global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
   float scale = 1.f;
@@ -58,13 +66,14 @@ __global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
     if (scale == 0.f) return;
   }
   // (Adam after a norm begins with the gradients that the norm read last, of which the last-level cache still holds the most:
-  // bf16 8192-8192-4096 with its norm 582 us from the first, 565 from the last; SGD, which needs less of it besides, 109 and 110.)
+  // bf16 8192-8192-4096 with its norm 552 us from the first, 543 from the last, 4096-4096-4096-1000 200 and 197; SGD, which needs less of it
+  // besides, fp32 8192-8192-4096 245 and 246.)
   const int b = ADAM && SCALED ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x;
   const int t = tensor_of(l.chunk_end, l.n, b), c = b - (t ? l.chunk_end[t - 1] : 0);
   float* const w = l.w[t]; float* const m = l.m[t]; float* const v = l.v[t];
   const float* const g = l.g[t];
   uint16_t* const lo = l.lo[t];
-  const int64_t i0 = (int64_t)c * kChunk, n = l.count[t];
+  const int64_t i0 = (int64_t)c * kStepChunk, n = l.count[t];
   const uintptr_t align = reinterpret_cast<uintptr_t>(w) | reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(m) |
                           reinterpret_cast<uintptr_t>(v) | (reinterpret_cast<uintptr_t>(lo) << 1);   // (8-byte vectors of the bf16 copy)
   const OptimArgs& a = l.a;
@@ -80,35 +89,32 @@ __global__ __launch_bounds__(256) void optim_kernel(OptimList l) {
     if constexpr (PAST) __builtin_nontemporal_store(x, reinterpret_cast<floatx4*>(p));
     else *reinterpret_cast<floatx4*>(p) = x;
   };
+  const int64_t i = i0 + (int)threadIdx.x * 4;
+  if (i >= n) return;
+  if (i + 4 <= n && (align & 15) == 0) {
+    floatx4 wv = ld(w + i), gv = ld(g + i), mv = {0.f, 0.f, 0.f, 0.f}, vv = mv;
+    if constexpr (ADAM) { mv = ld(m + i); vv = ld(v + i); }
 #pragma unroll
-  for (int q = 0; q < kChunk / 1024; ++q) {
-    const int64_t i = i0 + q * 1024 + (int)threadIdx.x * 4;
-    if (i >= n) return;
-    if (i + 4 <= n && (align & 15) == 0) {
-      floatx4 wv = ld(w + i), gv = ld(g + i), mv = {0.f, 0.f, 0.f, 0.f}, vv = mv;
-      if constexpr (ADAM) { mv = ld(m + i); vv = ld(v + i); }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float me = mv[e], ve = vv[e];
-        wv[e] = update_one<ADAM, true>(wv[e], grad(gv[e]), me, ve, a);
-        mv[e] = me; vv[e] = ve;
-      }
-      st(w + i, wv);
-      if constexpr (ADAM) { st(m + i, mv); st(v + i, vv); }
-      if (lo) {
-        const u32x2 p = {(uint32_t)to_bf16(wv[0]) | ((uint32_t)to_bf16(wv[1]) << 16), (uint32_t)to_bf16(wv[2]) | ((uint32_t)to_bf16(wv[3]) << 16)};
-        *reinterpret_cast<u32x2*>(lo + i) = p;
-      }
-      continue;
+    for (int e = 0; e < 4; ++e) {
+      float me = mv[e], ve = vv[e];
+      wv[e] = update_one<ADAM, true>(wv[e], grad(gv[e]), me, ve, a);
+      mv[e] = me; vv[e] = ve;
     }
-    for (int64_t j = i; j < n && j < i + 4; ++j) {
-      float mm = 0.f, vv = 0.f;
-      if constexpr (ADAM) { mm = m[j]; vv = v[j]; }
-      const float wn = update_one<ADAM, false>(w[j], grad(g[j]), mm, vv, a);
-      w[j] = wn;
-      if constexpr (ADAM) { m[j] = mm; v[j] = vv; }
-      if (lo) lo[j] = to_bf16(wn);
+    st(w + i, wv);
+    if constexpr (ADAM) { st(m + i, mv); st(v + i, vv); }
+    if (lo) {
+      const u32x2 p = {(uint32_t)to_bf16(wv[0]) | ((uint32_t)to_bf16(wv[1]) << 16), (uint32_t)to_bf16(wv[2]) | ((uint32_t)to_bf16(wv[3]) << 16)};
+      *reinterpret_cast<u32x2*>(lo + i) = p;
     }
+    return;
+  }
+  for (int64_t j = i; j < n && j < i + 4; ++j) {
+    float mm = 0.f, vv = 0.f;
+    if constexpr (ADAM) { mm = m[j]; vv = v[j]; }
+    const float wn = update_one<ADAM, false>(w[j], grad(g[j]), mm, vv, a);
+    w[j] = wn;
+    if constexpr (ADAM) { m[j] = mm; v[j] = vv; }
+    if (lo) lo[j] = to_bf16(wn);
   }
 }
 
@@ -209,14 +215,14 @@ template <bool PAST> __global__ __launch_bounds__(256) void clip_kernel(ClipList
   const float lift = l.factors[0], f = l.factors[1];    // (1 and 1 for a norm that is not finite: the gradients as they are)
   const int t = tensor_of(l.chunk_end, l.n, blockIdx.x), c = (int)blockIdx.x - (t ? l.chunk_end[t - 1] : 0);
   if (lift == 1.f && f == 1.f && l.out[t] == l.g[t]) return;
-  const int64_t i0 = (int64_t)c * kChunk, n = l.count[t];
+  const int64_t i0 = (int64_t)c * kClipChunk, n = l.count[t];
   const bool half = (l.bf16[t >> 5] >> (t & 31)) & 1u;
   const bool aligned = ((reinterpret_cast<uintptr_t>(l.g[t]) | reinterpret_cast<uintptr_t>(l.out[t])) & 15) == 0;
   if (half) {
     const uint16_t* const g = static_cast<const uint16_t*>(l.g[t]);
     uint16_t* const o = static_cast<uint16_t*>(l.out[t]);
 #pragma unroll
-    for (int q = 0; q < kChunk / 2048; ++q) {
+    for (int q = 0; q < kClipChunk / 2048; ++q) {
       const int64_t i = i0 + q * 2048 + (int)threadIdx.x * 8;
       if (i + 8 <= n && aligned) {
         u32x4 v;
@@ -234,7 +240,7 @@ template <bool PAST> __global__ __launch_bounds__(256) void clip_kernel(ClipList
   const float* const g = static_cast<const float*>(l.g[t]);
   float* const o = static_cast<float*>(l.out[t]);
 #pragma unroll
-  for (int q = 0; q < kChunk / 1024; ++q) {
+  for (int q = 0; q < kClipChunk / 1024; ++q) {
     const int64_t i = i0 + q * 1024 + (int)threadIdx.x * 4;
     if (i + 4 <= n && aligned) {
       floatx4 v;
@@ -255,7 +261,7 @@ template <bool PAST> void optim_run(bool adam, const OptimList& l, unsigned chun
 }
 
 // fills chunk_end; their number, or -1 where a grid cannot have so many
-int64_t count_chunks(int n, const int64_t* count, int32_t* chunk_end, int chunk = kChunk) {
+int64_t count_chunks(int n, const int64_t* count, int32_t* chunk_end, int chunk) {
   int64_t chunks = 0;
   for (int i = 0; i < n; ++i) {
     chunks += (count[i] + chunk - 1) / chunk;
@@ -268,7 +274,7 @@ int64_t count_chunks(int n, const int64_t* count, int32_t* chunk_end, int chunk 
 }  // namespace
 
 hipError_t launch_optim(bool adam, bool past, OptimList* l, hipStream_t st) {
-  const int64_t chunks = count_chunks(l->n, l->count, l->chunk_end);
+  const int64_t chunks = count_chunks(l->n, l->count, l->chunk_end, kStepChunk);
   if (chunks < 0) return hipErrorInvalidValue;
   if (chunks == 0) return hipSuccess;
   if (past) optim_run<true>(adam, *l, (unsigned)chunks, st); else optim_run<false>(adam, *l, (unsigned)chunks, st);
@@ -286,7 +292,7 @@ hipError_t launch_square_sums(NormList* l, int* partials, hipStream_t st) {
 }
 
 hipError_t launch_clip(bool past, ClipList* l, hipStream_t st) {
-  const int64_t chunks = count_chunks(l->n, l->count, l->chunk_end);
+  const int64_t chunks = count_chunks(l->n, l->count, l->chunk_end, kClipChunk);
   if (chunks < 0) return hipErrorInvalidValue;
   if (chunks == 0) return hipSuccess;
   if (past) hipLaunchKernelGGL(clip_kernel<true>, dim3((unsigned)chunks), dim3(256), 0, st, *l);
