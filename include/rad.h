@@ -416,10 +416,14 @@ rad_status rad_linear_logprobs(rad_ctx* ctx, const rad_layer* layer, const void*
 /* The layer's gradients from those of log probabilities and entropies, with dz the
  * dlogits of rad_token_logprobs_grad:
  *   dX = dz W^T,  dW = beta dW + x^T dz,  dbias = beta dbias + sum_r dz[r].
- * The logits are formed again; dz is rounded to the layer's type.  Types, beta,
- * which outputs may be null, overlaps, limits, pieces and workspaces are as for
- * rad_linear_ce with the gradients in the place of row weights, and 4 bytes per
- * row and 64 classes of a piece and 4 per row of it besides. */
+ * The logits are formed again; for dX and dW, dz is rounded to the layer's type
+ * (what a bf16 layer's dX and dW are off by beside their own rounding), for dbias
+ * it is not.  Between the products a bf16 layer's logits are kept as 16-bit codes,
+ * to 2^-10 of a power of two each (0.0007 of their probability; the tokens' own
+ * and all statistics are fp32).  Types, beta, which outputs may be null, overlaps,
+ * limits, pieces and workspaces are as for rad_linear_ce with the gradients in the
+ * place of row weights, and 4 bytes per row and 64 classes of a piece, 4 per row
+ * of it and, for a bf16 layer's dbias, 4 per 16 rows of it and class besides. */
 rad_status rad_linear_logprobs_grad(rad_ctx* ctx, const rad_layer* layer, const void* x, const void* W, const float* bias,
                                     const int32_t* token, double temperature, const float* d_logprob, const float* d_entropy,
                                     void* dX, void* dW, int32_t dw_dtype, float* dbias, float beta);

@@ -1724,6 +1724,11 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   void *z = nullptr, *xs = nullptr;
   if (train) RAD_TRY(ws_get(c, WS_LOGITS, (size_t)(piece * vp * esz), &z));
   if (h.dW) RAD_TRY(ws_get(c, WS_LOGITGRAD, (size_t)(piece * dp * esz), &xs));
+  // The bias gradient's parts; of bf16 log probabilities it sums what dz was ahead of its rounding, formed with it.
+  float* bias_part = nullptr;
+  const bool sums = lp && dtype == kBF16 && h.dbias;
+  const size_t part_floats = ((size_t)kHeadColsumSplits * d_out + 63) / 64 * 64;
+  if (h.dbias) RAD_TRY(ws_get(c, WS_COLSUM, (part_floats + (sums ? (size_t)((piece + kGradRows - 1) / kGradRows * vp) : 0)) * 4, reinterpret_cast<void**>(&bias_part)));
   bool summed = false;
 
   for (int64_t r0 = 0; r0 < rows; r0 += piece) {
@@ -1771,7 +1776,7 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     f.dtype = dtype;
     f.list = list; f.live = live; f.rows = n; f.classes = d_out; f.parts = parts; f.part = part; f.t = tp;
     f.stats = stats; f.stats_ld = piece; f.target = target;
-    f.spread = spread; f.slope = slope;
+    f.spread = spread; f.slope = slope; f.sums = sums ? bias_part + part_floats : nullptr;
     f.row_loss = lp ? nullptr : losses + r0; f.top = top; f.factor = factor; f.common = common;
     f.z = z; f.z_ld = vp; f.first = a.first; f.first_ld = first_ld;
     f.x = g.A; f.x_ld = dp; f.d_in = d_in; f.xs = xs;
@@ -1818,13 +1823,11 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
       if (h.dX) { RAD_TRY(run_gemm_call(c, dtype, kOpK, kOpK, kEpiHeadX, gx)); RAD_TRY(head_split_sum(c, sx)); }
       if (h.dW) { RAD_TRY(run_gemm_call(c, dtype, kOpMN, kOpMN, kEpiHeadW, gw)); RAD_TRY(head_split_sum(c, sw)); }
     }
-    if (h.dbias) {
-      void* partial = nullptr;
-      RAD_TRY(ws_get(c, WS_COLSUM, (size_t)kHeadColsumSplits * d_out * 4, &partial));
+    if (h.dbias)
       HIP_TRY(c, timed(c, "head_colsum", [&](const char**) {
-        return launch_head_colsum(dtype, z, vp, live, common, d_out, static_cast<float*>(partial), h.dbias, r0 > 0 || h.beta != 0.f, c->stream);
+        return launch_head_colsum(sums ? kF32 : dtype, sums ? f.sums : z, vp, n, live, sums ? kGradRowsShift : 0, common, d_out, bias_part,
+                                  h.dbias, r0 > 0 || h.beta != 0.f, c->stream);
       }));
-    }
   }
   if (cast)
     HIP_TRY(c, timed(c, "cast_add", [&](const char**) {

@@ -420,6 +420,7 @@ hipError_t launch_vocab_join(int dtype, bool logprob, const GemmArgs& g, hipStre
 // After the logits' product, for every place of the list: the row's loss, its maximum top and what its exponentials
 // 2^((z - top) c) are multiplied by, factor = share / their sum, share = weight t.lead / *common.  For dW the rows of x side by side (xs, rows x_ld apart),
 // unless the list has them all.  Rows that do not count: no loss, dX zero.
+constexpr int kGradRowsShift = 4, kGradRows = 1 << kGradRowsShift;      // places of a workgroup that makes dz
 struct VocabFinish {
   int dtype;
   const int32_t* list; const int32_t* live;
@@ -429,6 +430,7 @@ struct VocabFinish {
   // The gradient of log probabilities and entropies (null: of a loss): there are no losses, and exponentials 2^l, l = (z - top) c,
   // are multiplied by factor + slope l.
   const float* spread; float* slope;
+  float* sums;                  // bf16: for dbias, sums over kGradRows places of dz ahead of its rounding [(rows + kGradRows - 1) / kGradRows][z_ld]; or null
   const float* target;          // [place][k]
   float* row_loss;              // [rows], in the batch's order
   float* loss;                  // the sum over these rows, or null: left to another call
@@ -452,10 +454,11 @@ struct SplitSum {
   void* out; int out_dtype; int64_t out_ld; int beta;
 };
 hipError_t launch_split_sum(const SplitSum& a, hipStream_t st);
-// out [cols] (+)= *scale x sum over the first *live rows of g[i][c]; part: [kHeadColsumSplits][cols]
+// out [cols] (+)= *scale x sum of g[i][c] over the first *live of `rows` rows, or, shift > 0, over g's rows that each are a sum of 2^shift of
+// those (fp32); part: [kHeadColsumSplits][cols]
 constexpr int kHeadColsumSplits = 32;
-hipError_t launch_head_colsum(int dtype, const void* g, int64_t g_ld, const int32_t* live, const float* scale, int cols, float* part,
-                              float* out, int beta, hipStream_t st);
+hipError_t launch_head_colsum(int dtype, const void* g, int64_t g_ld, int rows, const int32_t* live, int shift, const float* scale, int cols,
+                              float* part, float* out, int beta, hipStream_t st);
 // rows of any width and alignment to rows out_ld apart (whole 16-byte vectors), zeros past cols
 hipError_t launch_pad_rows(int dtype, const void* in, int64_t rows, int cols, void* out, int64_t out_ld, hipStream_t st);
 

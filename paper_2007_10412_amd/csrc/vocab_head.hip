@@ -266,11 +266,15 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinis
 // 16 rows x kSteps 16-byte vectors of 16 lanes a workgroup.  Reads and writes a logit, and is bound by that: 4096 x 128000 bf16
 // 404 us (5.2 TB/s), 4096 x 32000 97, 1024 x 8003 fp32 12.  The last column of
 // workgroups (where there is a loss to sum) has no logits: its first one adds the rows' losses.
-constexpr int kGradRows = 16;
-template <typename T, int kGradSteps, bool LOGPROB>
+// SUMS (log probabilities in bf16 with a bias): the sum of the workgroup's rows goes to a.sums besides, of dz as it is ahead of its rounding: an eighth
+// of the logits' bytes to write, where a sum of the rounded values reads all of them again.  Gradients of 8192 x 256 x 2000 130 -> 110 us, 4096 x 2048 x
+// 32000 1641 -> 1631; off by 7e-6 of the column sums (rms; the codes'), where the sum of rounded values was 0.0016 off.
+template <typename T, int kGradSteps, bool LOGPROB, bool SUMS>
 __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int sum_column) {
   constexpr int VPL = 16 / (int)sizeof(T), kCols = 16 * VPL * kGradSteps;
+  static_assert(!SUMS || (LOGPROB && sizeof(T) == 2), "log probabilities in bf16");
   __shared__ float s_w[4];
+  __shared__ float s_sum[SUMS ? 4 : 1][SUMS ? kCols : 1];
   const int live = *a.live;
   const VocabTargets& t = a.t;
   if ((int)blockIdx.x == sum_column) {
@@ -295,9 +299,19 @@ __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int 
   T* const zr = static_cast<T*>(a.z) + (int64_t)place * a.z_ld;
   float top = 0.f, f = 0.f, slope = 0.f;
   auto times = [&](float e, float l) { return LOGPROB ? e * fmaf(fmaxf(l, kNoPower), slope, f) : e * f; };
-  if (counts) {
-    top = a.top[place]; f = a.factor[place];
-    if constexpr (LOGPROB) slope = a.slope[place];
+  if (SUMS || counts) {                                 // (SUMS: a wave's lanes stay together)
+    int token = -1;
+    float token_grad = 0.f;
+    if (counts) {
+      top = a.top[place]; f = a.factor[place];
+      if constexpr (LOGPROB) slope = a.slope[place];
+      if (SUMS && t.labels) {
+        const int row = a.list[place];
+        const float l = (a.target[place] - top) * c;
+        token = t.labels[row];
+        token_grad = times(__builtin_amdgcn_exp2f(l), l) + (t.weight ? row_share(t.weight, t, row, *a.common) : 0.f);
+      }
+    }
     u32x4 w[kGradSteps];
     float m[kGradSteps];
 #pragma unroll
@@ -305,14 +319,15 @@ __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int 
       const int64_t col = (int64_t)c0 + (q * 16 + l) * VPL;
       w[q] = u32x4{0u, 0u, 0u, 0u};
       m[q] = -INFINITY;
-      if (col < a.z_ld) w[q] = *reinterpret_cast<const u32x4*>(zr + col);
-      if (sizeof(T) == 2 && col < a.classes) m[q] = a.stats[((col >> shift) * a.stats_ld + place) * 2];
+      if ((!SUMS || counts) && col < a.z_ld) w[q] = *reinterpret_cast<const u32x4*>(zr + col);
+      if ((!SUMS || counts) && sizeof(T) == 2 && col < a.classes) m[q] = a.stats[((col >> shift) * a.stats_ld + place) * 2];
     }
 #pragma unroll
     for (int q = 0; q < kGradSteps; ++q) {
       const int64_t col = (int64_t)c0 + (q * 16 + l) * VPL;
       if (col >= a.z_ld) continue;
       u32x4 o;
+      float v[SUMS ? 8 : 1];
       if constexpr (sizeof(T) == 2) {
         const float off = m[q] == -INFINITY ? 0.f : (m[q] - top) * c;
 #pragma unroll
@@ -320,7 +335,12 @@ __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int 
           const uint32_t lo = w[q][e] & 0xFFFFu, hi = w[q][e] >> 16;
           const float l0 = fmaf((float)lo, -kCodeRange / 65535.f, off), l1 = fmaf((float)hi, -kCodeRange / 65535.f, off);
           const float e0 = __builtin_amdgcn_exp2f(l0), e1 = __builtin_amdgcn_exp2f(l1);
-          o[e] = bf16_pair(times(lo == kCodeLast ? 0.f : e0, l0), times(hi == kCodeLast ? 0.f : e1, l1));
+          const float g0 = times(lo == kCodeLast ? 0.f : e0, l0), g1 = times(hi == kCodeLast ? 0.f : e1, l1);
+          o[e] = bf16_pair(g0, g1);
+          if constexpr (SUMS) {
+            v[2 * e] = !counts ? 0.f : col + 2 * e == token ? token_grad : g0;
+            v[2 * e + 1] = !counts ? 0.f : col + 2 * e + 1 == token ? token_grad : g1;
+          }
         }
       } else {
 #pragma unroll
@@ -329,11 +349,26 @@ __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int 
           o[e] = __float_as_uint(times(__builtin_amdgcn_exp2f(l), l));
         }
       }
-      *reinterpret_cast<u32x4*>(zr + col) = o;
+      if (!SUMS || counts) *reinterpret_cast<u32x4*>(zr + col) = o;
+      if constexpr (SUMS) {
+        // a wave's four rows: a lane gives half of its columns away and then half of what is left, and has two of them in the end
+        const bool upper = threadIdx.x & 32, odd = threadIdx.x & 16;
+        float half[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) half[e] = (upper ? v[e + 4] : v[e]) + __shfl_xor(upper ? v[e] : v[e + 4], 32);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          s_sum[threadIdx.x >> 6][(q * 16 + l) * 8 + (upper ? 4 : 0) + (odd ? 2 : 0) + e] =
+              (odd ? half[e + 2] : half[e]) + __shfl_xor(odd ? half[e] : half[e + 2], 16);
+      }
     }
   }
   __threadfence_block();
   __syncthreads();                                      // the targets' elements are written again, after their vectors
+  if constexpr (SUMS) {
+    for (int q = threadIdx.x; q < kCols && c0 + q < a.classes; q += 256)
+      a.sums[(int64_t)blockIdx.y * a.z_ld + c0 + q] = (s_sum[0][q] + s_sum[1][q]) + (s_sum[2][q] + s_sum[3][q]);
+  }
   if (!counts) return;
   const int row = a.list[place];
   int t0 = 0, t1 = 0;
@@ -389,16 +424,17 @@ __global__ __launch_bounds__(256) void split_sum_kernel(SplitSum a) {
   for (int e = 0; e < 4; ++e) if (c + e < a.cols) o[e] = (uint16_t)bf16_pair(a.beta ? bf16_bits_to_f32(o[e]) + v[e] : v[e], 0.f);
 }
 
-// (the sum is of dz as the products take it, in the layer's type, as rad_backward_dW's is of the dy that it is given)
+// (the sum is of dz as the products take it, in the layer's type, as rad_backward_dW's is of the dy that it is given; of log probabilities'
+// in bf16, of the sums over groups of 2^shift rows that vocab_gradient_kernel has left)
 // 64 lanes' vectors of columns and one range of rows a workgroup, its four waves every fourth row: 1024 x 8003 fp32 6 us (5.4
 // TB/s) and 4.6 for the ranges' sum; in one range 512 x 1024 x 8192 took 110 us instead of 80
 template <typename T>
-__global__ __launch_bounds__(256) void head_colsum_kernel(const T* __restrict__ g, int64_t g_ld, const int32_t* __restrict__ live,
+__global__ __launch_bounds__(256) void head_colsum_kernel(const T* __restrict__ g, int64_t g_ld, const int32_t* __restrict__ live, int shift,
                                                           int cols, float* __restrict__ part) {
   constexpr int VPL = 16 / (int)sizeof(T), W = 64 * VPL;
   __shared__ float s_sum[4][W];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int n = *live, per = (n + kHeadColsumSplits - 1) / kHeadColsumSplits;
+  const int n = (*live + (1 << shift) - 1) >> shift, per = (n + kHeadColsumSplits - 1) / kHeadColsumSplits;
   const int r0 = (int)blockIdx.y * per, r1 = min(n, r0 + per);
   const int c = (int)blockIdx.x * W + lane * VPL;
   float sum[VPL] = {};
@@ -419,12 +455,16 @@ __global__ __launch_bounds__(256) void head_colsum_kernel(const T* __restrict__ 
     if (col < cols) part[(int64_t)blockIdx.y * cols + col] = (s_sum[0][q] + s_sum[1][q]) + (s_sum[2][q] + s_sum[3][q]);
   }
 }
-__global__ __launch_bounds__(256) void head_colsum_final_kernel(const float* __restrict__ part, int cols, const float* __restrict__ scale,
-                                                                float* __restrict__ out, int beta) {
+// GROUPS: part has the sums over groups of 2^shift of the *live rows (few of them)
+template <bool GROUPS>
+__global__ __launch_bounds__(256) void head_colsum_final_kernel(const float* __restrict__ part, int64_t part_ld, const int32_t* __restrict__ live,
+                                                                int shift, int cols, const float* __restrict__ scale, float* __restrict__ out, int beta) {
   const int c = blockIdx.x * 256 + threadIdx.x;
   if (c >= cols) return;
+  const int n = GROUPS ? (*live + (1 << shift) - 1) >> shift : kHeadColsumSplits;
   float s = 0.f;
-  for (int q = 0; q < kHeadColsumSplits; ++q) s += part[(int64_t)q * cols + c];
+#pragma unroll 8
+  for (int q = 0; q < n; ++q) s += part[(int64_t)q * part_ld + c];
   out[c] = (beta ? out[c] : 0.f) + *scale * s;
 }
 
@@ -477,8 +517,11 @@ template <typename T, bool LOGPROB> static hipError_t gradient_of(const VocabFin
   const unsigned cols = (unsigned)((a.z_ld + (wide ? 16 : 4) * width - 1) / ((wide ? 16 : 4) * width));
   const dim3 grid(cols + (a.loss ? 1 : 0), rows);
   const int sum_column = a.loss ? (int)cols : -1;
-  if (wide) hipLaunchKernelGGL((vocab_gradient_kernel<T, 16, LOGPROB>), grid, dim3(256), 0, st, a, sum_column);
-  else hipLaunchKernelGGL((vocab_gradient_kernel<T, 4, LOGPROB>), grid, dim3(256), 0, st, a, sum_column);
+  auto kern = wide ? vocab_gradient_kernel<T, 16, LOGPROB, false> : vocab_gradient_kernel<T, 4, LOGPROB, false>;
+  if constexpr (LOGPROB && sizeof(T) == 2) {
+    if (a.sums) kern = wide ? vocab_gradient_kernel<T, 16, true, true> : vocab_gradient_kernel<T, 4, true, true>;
+  }
+  hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a, sum_column);
   return hipGetLastError();
 }
 bool vocab_loss_inside(const VocabFinish& a) { return a.z || a.rows == 1; }
@@ -499,13 +542,20 @@ hipError_t launch_split_sum(const SplitSum& a, hipStream_t st) {
   hipLaunchKernelGGL(split_sum_kernel, dim3((a.cols + 1023) / 1024, a.rows), dim3(256), 0, st, a);
   return hipGetLastError();
 }
-hipError_t launch_head_colsum(int dtype, const void* g, int64_t g_ld, const int32_t* live, const float* scale, int cols, float* part,
-                              float* out, int beta, hipStream_t st) {
+hipError_t launch_head_colsum(int dtype, const void* g, int64_t g_ld, int rows, const int32_t* live, int shift, const float* scale, int cols,
+                              float* part, float* out, int beta, hipStream_t st) {
+  const dim3 last((cols + 255) / 256);
+  // (a gradient call with few groups of rows in two launches / in one: 16 x 1024 x 50257 bf16 141.8 / 136.0 us, 200 x 768 x 10007 70.5 / 69.4, but 512 x
+  // 1024 x 8192 81 / 82, 600 x 512 x 20000 121 / 122)
+  if (shift > 0 && rows <= 16 << shift) {
+    hipLaunchKernelGGL(head_colsum_final_kernel<true>, last, dim3(256), 0, st, (const float*)g, g_ld, live, shift, cols, scale, out, beta);
+    return hipGetLastError();
+  }
   const int W = dtype == kBF16 ? 512 : 256;
   const dim3 grid((cols + W - 1) / W, kHeadColsumSplits);
-  if (dtype == kBF16) hipLaunchKernelGGL(head_colsum_kernel<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)g, g_ld, live, cols, part);
-  else hipLaunchKernelGGL(head_colsum_kernel<float>, grid, dim3(256), 0, st, (const float*)g, g_ld, live, cols, part);
-  hipLaunchKernelGGL(head_colsum_final_kernel, dim3((cols + 255) / 256), dim3(256), 0, st, part, cols, scale, out, beta);
+  if (dtype == kBF16) hipLaunchKernelGGL(head_colsum_kernel<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)g, g_ld, live, shift, cols, part);
+  else hipLaunchKernelGGL(head_colsum_kernel<float>, grid, dim3(256), 0, st, (const float*)g, g_ld, live, shift, cols, part);
+  hipLaunchKernelGGL(head_colsum_final_kernel<false>, last, dim3(256), 0, st, part, (int64_t)cols, live, shift, cols, scale, out, beta);
   return hipGetLastError();
 }
 hipError_t launch_pad_rows(int dtype, const void* in, int64_t rows, int cols, void* out, int64_t out_ld, hipStream_t st) {
