@@ -48,6 +48,9 @@ __device__ __forceinline__ void mask_bf16x8(u32x4& t, uint32_t mb) {
 // device's scope, so that it passes the XCDs' caches by itself, and a workgroup counts itself done when its stores have arrived.  (With the
 // fences that plain stores need, 2048 workgroups that leave a sum each took 125 us for what takes 45: each writes back and empties its
 // XCD's cache.)
+// This leans on how gfx950 works rather than on an order that the memory model promises: a relaxed store of the device's scope is written through
+// to memory that all XCDs share, s_waitcnt vmcnt(0) ends no sooner than such stores have arrived there, and a relaxed load of that scope does not
+// take a line that its XCD's cache kept from before.  Another target takes a release ahead of the count and an acquire behind it.
 template <typename T> __device__ __forceinline__ void store_for_all(T* p, T v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }

@@ -14,7 +14,8 @@ struct WeightRange {
     most = fmaxf(most, w < INFINITY ? w : INFINITY);
     if (w > 0.f) least = fminf(least, w);
   }
-  // a row's, of one or two kinds
+  // A row's, of one or two kinds: the larger one.  (Of a NaN beside a number that is the number, of two NaN a NaN: such a row's gradient is NaN by
+  // itself under any finite factor, so it need not make the others' 1.)
   __device__ __forceinline__ void add(const float* weight, const float* weight2, int row) {
     if (!weight2) add(weight[row]);
     else add(fmaxf(weight ? fabsf(weight[row]) : 0.f, fabsf(weight2[row])));

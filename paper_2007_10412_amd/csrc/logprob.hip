@@ -4,8 +4,9 @@
 // q = softmax(z / T).  With m a row's maximum, l_v = (z_v - m) log2(e) / T, s = sum_v 2^l_v and u = sum_v 2^l_v l_v:
 //   log q_v = (z_v - m) / T - ln s,   H = - sum_v q_v log q_v = ln s - ln 2 u / s,
 //   dz_v = (a (1[v = token] - q_v) - h q_v (log q_v + H)) / T = 2^l_v (A + B l_v) + (a / T) 1[v = token]
-// for the gradients a of log q[token] and h of H, A = (h ln 2 u / s - a) / (T s), B = - h ln 2 / (T s).  So a row is read once and
-// kept in registers between its statistics and whatever follows, 16 bytes a lane.
+// for the gradients a of log q[token] and h of H, A = (h ln 2 u / s - a) / (T s), B = - h ln 2 / (T s).  Forward a row is streamed once, 16 bytes a
+// lane, and not kept (rows of up to four vectors a thread are); vectors that may hold a listed class are read again, from a cache.  Backward it is kept
+// between its statistics and its gradient, in registers and, of the longer rows, in LDS; rows in parts are read twice, once in each of two launches.
 //
 // The k likeliest classes.  Any class of the list is at least as large as the k-th largest of the maxima of disjoint groups of
 // the row (k groups then hold one such class each).  A thread's maxima are there already; one wave finds that bound of them bit by
@@ -529,7 +530,7 @@ __global__ __launch_bounds__(NT) void logprob_rows_kernel(LogprobRows a, int par
 
 // Backward: a row stays in registers between its sums and its gradient, from one maximum m, with l = z c - m c in one operation as
 // above; where m lies too far from zero for that, from memory element by element.  Bound by memory, with the vector units at work for most of that time
-// (exponentials are taken twice): bf16 4096 x 32000 95 us (5.5 TB/s read and written), fp32 333 x 50257 24.5 (5.5).  SPLIT: PASS 0 leaves the parts' statistics, PASS 1
+// (exponentials are taken twice): bf16 4096 x 32000 95 us (5.5 TB/s read and written), fp32 333 x 50257 24.5-26.7 (5.1-5.5).  SPLIT: PASS 0 leaves the parts' statistics, PASS 1
 // joins them (each workgroup for itself) and writes.
 template <int NT> __device__ __forceinline__ float block_max(float m, float3* s_w) {
   m = lanes_max(m);
