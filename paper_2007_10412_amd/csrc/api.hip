@@ -1482,11 +1482,11 @@ static rad_status vocab_targets(rad_ctx* c, const int32_t* labels, const rad_tea
   int32_t* const counts = reinterpret_cast<int32_t*>(entropy + rows);
   int32_t* const index = counts + rows;
   float* const prob = reinterpret_cast<float*>(index + lists);
-  *t = VocabTargets{labels, nullptr, nullptr, nullptr, nullptr, 1, 1.f, weight, inv_count, 1.f, nullptr};
+  *t = VocabTargets{labels, nullptr, nullptr, nullptr, nullptr, 1, 1.f, weight, inv_count};
   if (!*row_loss) *row_loss = losses;
   if (teacher) {
     t->index = index; t->prob = prob; t->entropy = entropy; t->counts = counts;
-    t->k = teacher->k; t->temperature = t->lead = (float)teacher->temperature;
+    t->k = teacher->k; t->temperature = (float)teacher->temperature;
     HIP_TRY(c, timed(c, "teacher", [&](const char**) {
       return launch_teacher(teacher->index, teacher->logit, rows, teacher->k, classes, t->temperature, index, prob, entropy, counts, first,
                             part, parts, c->stream);
@@ -1708,13 +1708,14 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
   float* const target = factor + piece;
   float* const slope = lp ? target + piece : nullptr;
   float* const spread = lp ? slope + piece : nullptr;
-  VocabTargets t;
+  HeadTargets t;
   float* losses = h.row_loss;
   if (lp) {
     const float T = (float)lp->temperature;
-    t = VocabTargets{labels, nullptr, nullptr, nullptr, nullptr, 1, T, lp->d_logprob, nullptr, 1.f / T, lp->d_entropy};
+    t = HeadTargets{{labels, nullptr, nullptr, nullptr, nullptr, 1, T, lp->d_logprob, nullptr}, 1.f / T, lp->d_entropy};
   } else {
     RAD_TRY(vocab_targets(c, labels, teacher, row_weight, rows, d_out, !one, &t, &losses, first, part, parts));
+    t.lead = t.temperature; t.weight2 = nullptr;
   }
 
   const bool cast = h.dW && h.dw_dtype == kBF16 && (!one || h.beta != 0.f);     // sums of several pieces are kept in fp32
@@ -1735,7 +1736,7 @@ static rad_status head_loss(rad_ctx* c, const rad_layer* L, const int32_t* label
     const int n = (int)std::min<int64_t>(piece, rows - r0);
     const void* x = nullptr;
     RAD_TRY(head_padded(c, WS_HEADX, dtype, static_cast<const char*>(h.x) + r0 * d_in * esz, n, d_in, dp, &x));
-    VocabTargets tp = t;
+    HeadTargets tp = t;
     if (tp.labels) tp.labels += r0;
     else if (!lp) { tp.index += r0 * t.k; tp.prob += r0 * t.k; tp.entropy += r0; tp.counts += r0; }
     if (tp.weight) tp.weight += r0;
@@ -1974,7 +1975,7 @@ extern "C" rad_status rad_linear_logprobs(rad_ctx* c, const rad_layer* L, const 
     const int n = (int)std::min<int64_t>(piece, rows - r0);
     const void* xp = nullptr;
     if (!few) RAD_TRY(head_padded(c, WS_HEADX, dtype, static_cast<const char*>(x) + r0 * d_in * esz, n, d_in, dp, &xp));
-    const VocabTargets t{out->token ? out->token + r0 : nullptr, nullptr, nullptr, nullptr, nullptr, 1, T, nullptr, inv_count, 1.f, nullptr};
+    const HeadTargets t{{out->token ? out->token + r0 : nullptr, nullptr, nullptr, nullptr, nullptr, 1, T, nullptr, inv_count}, 1.f, nullptr};
     const int64_t tiles = (int64_t)((n + plan.tile - 1) / plan.tile) * ((d_out + 127) / 128) * plan.splits;
     const bool own_list = n <= kOwnListRows && plan.tile != 256 && (dtype == kBF16 ? n <= 1024 || tiles <= 640 : tiles <= 768);
     if (!few && !own_list)

@@ -59,24 +59,24 @@ struct TargetSum {
 
 // The rows that count, made into a list by a workgroup for itself: a thread has PER consecutive rows, of which `mine` count, the
 // first of them at place `at`.  Returns their number; the workgroup that writes leaves the whole list in memory.
-// s_n: a word a wave; s_w: a pair.
-template <int PER>
+// s_n: a word a wave; s_w: a pair.  LOGPROB: rows may count without labels or counts, and have weights of two kinds.
+template <int PER, bool LOGPROB>
 __device__ __forceinline__ int own_rows(const HeadArgs& h, int classes, int32_t* s_n, float2* s_w, bool write, uint32_t* mine_out, int* at_out) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r0 = (int)threadIdx.x * PER;
   uint32_t mine = 0u;
 #pragma unroll
   for (int q = 0; q < PER; ++q)
-    if (r0 + q < h.rows && (h.labels ? (uint32_t)h.labels[r0 + q] < (uint32_t)classes : !h.counts || h.counts[r0 + q] != 0)) mine |= 1u << q;
+    if (r0 + q < h.rows && (h.labels ? (uint32_t)h.labels[r0 + q] < (uint32_t)classes : (LOGPROB && !h.counts) || h.counts[r0 + q] != 0)) mine |= 1u << q;
   const int n = __popc(mine);
   int up = n;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(up, o); if (lane >= o) up += v; }
   if (lane == 63) s_n[w] = up;
-  const bool weights = h.weight || h.weight2;
+  const bool weights = h.weight || (LOGPROB && h.weight2);
   if (write && weights) {
     WeightRange of;
 #pragma unroll
-    for (int q = 0; q < PER; ++q) if ((mine >> q) & 1u) of.add(h.weight, h.weight2, r0 + q);
+    for (int q = 0; q < PER; ++q) if ((mine >> q) & 1u) of.add(h.weight, LOGPROB ? h.weight2 : nullptr, r0 + q);
     of.join_wave();
     if (lane == 0) s_w[w] = make_float2(of.most, of.least);
   }

@@ -15,7 +15,7 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 // ------------------------------------------------------------------ the list of rows
 // One workgroup: a thread has 8 consecutive rows of 8192 at a time, and places them by a count over the threads before it.  A
 // launch and the latency of a few dependent steps: 2000 rows 5 us, 4096 7.
-__global__ __launch_bounds__(1024) void row_list_kernel(VocabTargets t, int rows, int classes, int32_t* __restrict__ list,
+__global__ __launch_bounds__(1024) void row_list_kernel(HeadTargets t, int rows, int classes, int32_t* __restrict__ list,
                                                         int32_t* __restrict__ live, float* __restrict__ inv_count,
                                                         float* __restrict__ common) {
   __shared__ int s_n[16];
@@ -138,10 +138,10 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(GemmArgs g) {
 }
 
 // a row's share of *common (with weights never zero)
-__device__ __forceinline__ float row_share(const float* weight, const VocabTargets& t, int row, float common) {
+__device__ __forceinline__ float row_share(const float* weight, const HeadTargets& t, int row, float common) {
   return weight[row] * t.lead / common;
 }
-__device__ __forceinline__ float row_share(const VocabTargets& t, int row, float common) {
+__device__ __forceinline__ float row_share(const HeadTargets& t, int row, float common) {
   return !t.weight ? 1.f : row_share(t.weight, t, row, common);
 }
 
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kFinishThreads) void vocab_finish_kernel(VocabFinis
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int place0 = (int)blockIdx.x << shift, place = place0 + r;
   const int live = *a.live;
-  const VocabTargets& t = a.t;
+  const HeadTargets& t = a.t;
   const float c = kLog2e / t.temperature;
   const bool counts = place < live;
   const int row = place < a.rows ? a.list[place] : -1;
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(256) void vocab_gradient_kernel(VocabFinish a, int 
   __shared__ float s_w[4];
   __shared__ float s_sum[SUMS ? 4 : 1][SUMS ? kCols : 1];
   const int live = *a.live;
-  const VocabTargets& t = a.t;
+  const HeadTargets& t = a.t;
   if ((int)blockIdx.x == sum_column) {
     if (blockIdx.y != 0) return;
     float sum = 0.f;
@@ -489,7 +489,7 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const T* __restrict__ in,
 
 }  // namespace
 
-hipError_t launch_row_list(const VocabTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, float* common,
+hipError_t launch_row_list(const HeadTargets& t, int rows, int classes, int32_t* list, int32_t* live, float* inv_count, float* common,
                            hipStream_t st) {
   hipLaunchKernelGGL(row_list_kernel, dim3(1), dim3(1024), 0, st, t, rows, classes, list, live, inv_count, common);
   return hipGetLastError();
