@@ -209,7 +209,9 @@ __global__ __launch_bounds__(kNormThreads) void square_sums_kernel(NormList l) {
 // Elements times two factors whose product is the scale: the first is 1, or, where the scale would be a subnormal number of few bits (or none:
 // max_norm is less than 2^-126 of the norm), a power of two that brings them to the norm's size.  It is exact but for elements below 2^-126 of
 // that, and the second, at most twice max_norm, has all its bits but where max_norm is subnormal itself.
-// (Stored past the caches: 1023-4097-1000-50257 in bf16 61 us with the norm, 71 where the end of the kernel waits for them.)  PAST: read past
+// (Stored past the caches: 1023-4097-1000-50257 in bf16 61 us with the norm, 71 where the end of the kernel waits for them; with a kernel that reads
+// the clipped gradients next, us through / past: fp32 60 MB 61 / 62, 117 MB 121 / 115, 200 MB 225 / 211, 600 MB 614 / 613, bf16 60 MB 104 / 82,
+// 200 MB 296 / 287, in place the same.)  PAST: read past
 // them too, where they cannot hold them: bf16 2048-4096-50000 (0.8 GB read and written) 219 us through them, 197 past, but the first 61 and 62.
 template <bool PAST> __global__ __launch_bounds__(256) void clip_kernel(ClipList l) {
   const float lift = l.factors[0], f = l.factors[1];    // (1 and 1 for a norm that is not finite: the gradients as they are)
