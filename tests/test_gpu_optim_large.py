@@ -19,3 +19,5 @@ def test_a_tensor_of_more_than_a_launch():
     w[2 ** 33 - 2:2 ** 33 + 2] = 0.5
     assert float(w.min()) == 0.5 and float(w.max()) == 0.5 and (w2 == 2.0).all()
     B.rad_ctx_destroy(ctx)
+    del w, g
+    torch.cuda.empty_cache()                             # (64 GiB)
